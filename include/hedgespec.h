@@ -55,6 +55,9 @@ extern "C" {
 #define HS_MAX_QUERIES 65535
 #define HS_MAX_TOPL 32      /* L: children per draft-tree node in hs_eval_topl           */
 #define HS_MAX_CANDIDATES 1024 /* C: candidate slots per node in hs_candidate_mass       */
+#define HS_MAX_BEAMS 64     /* W, K: beams of a query in hs_beam_step and hs_draft_tree  */
+#define HS_MAX_DEPTH 32     /* D: grown steps of a draft tree in hs_draft_tree           */
+#define HS_MAX_STATES 1024  /* n: tensors of one hs_beam_reorder call                    */
 /* V: at most 512 * 256 16-byte vectors per row (1048576 bf16 or fp16, or 524288 fp32
    logits), and for alpha the device must hold ceil(V / 2048) (bf16, fp16) or ceil(V / 1024)
    (fp32) evaluation workgroups at once: hs_eval_alpha returns HS_ERR_LIMIT otherwise. Agreement
@@ -400,6 +403,132 @@ typedef struct hs_round_args {
 } hs_round_args;
 
 int hs_round(const hs_round_args* args, void* stream);
+
+/*
+ * hs_beam_step - one step of a draft tree's growth or of a beam search: of the W beams of each
+ * query and the V tokens that may follow each, the K continuations of largest score
+ *   s(w, v) = score[b][w] + log softmax(logits[b][w] / T)_v,
+ * best first (EAGLE's dynamic draft tree grows by the cumulative log-probability of its nodes; with
+ * K = W it is beam search). Scores are formed and compared in fp64 and are good to about
+ * 1e-7; equal ones rank lower beam first, then lower token. Equal logits of a beam have equal
+ * scores, larger ones larger.
+ *   logits      : one view [B][W][V] (stride_k from beam to beam), dtype as in hs_eval_alpha. A
+ *                 logit of -inf is no continuation; one of the type's lowest finite value is.
+ *   score       : [B] rows of W fp32, score_stride elements apart (>= W). A beam whose score is not
+ *                 finite (an empty slot, -inf) holds nothing: it has no continuation, and its logits
+ *                 are not read. Nor has a row that defines no distribution (all -inf, or a NaN or
+ *                 +inf logit). Finite logits may have any size.
+ *   done        : NULL, or [B] rows of W uint8, score_stride apart: a beam marked nonzero has
+ *                 ended. It continues as itself, once, with its score, as token `eos`; its logits
+ *                 are not read.
+ *   eos         : the token that ends a beam, or negative: none does.
+ *   temperature : T, 1e-30 <= T <= 1e30. A double, as the scores are.
+ *   out_score   : [B][K] fp32: s rounded once; -inf for a slot without a continuation.
+ *   out_parent  : [B][K] int32: the beam w that the slot continues; -1 for none.
+ *   out_token   : [B][K] int32: its token; -1 for none.
+ *   out_done    : NULL, or [B][K] uint8: the slot continues an ended beam, or its token is eos.
+ *   out_score may be score itself, and out_done done, where K = W = score_stride; otherwise no
+ *   output may overlap an input.
+ * W, K          : 1 .. HS_MAX_BEAMS each; K may be larger or smaller than W, and than V.
+ * workspace     : at least hs_beam_step_workspace_size() bytes of device memory, 256-byte aligned;
+ *                 scratch only.
+ * Every logit of a live beam is read once. Deterministic, and the same for a row wherever it stands in
+ * a call of the same shape.
+ */
+typedef struct hs_beam_args {
+  hs_view logits;
+  int B, W, K;
+  int64_t V;
+  int dtype;
+  double temperature;
+  const float* score;
+  const uint8_t* done;
+  int64_t score_stride;
+  int32_t eos;
+  float* out_score;
+  int32_t* out_parent;
+  int32_t* out_token;
+  uint8_t* out_done;
+  void* workspace;
+  size_t workspace_bytes;
+} hs_beam_args;
+
+/* Bytes of device workspace hs_beam_step needs for this shape (0 on invalid shapes). */
+size_t hs_beam_step_workspace_size(int B, int W, int K, int64_t V, int dtype);
+int hs_beam_step(const hs_beam_args* args, void* stream);
+
+/*
+ * hs_beam_reorder - the beams' states follow their new parents: for every tensor of the call, query
+ * b and slot j < K, the state of slot j becomes that of beam parent[b][j] as it was before the call.
+ * Caches, hidden states, token histories: bytes of any type are copied.
+ * One tensor is described by an hs_state: the state of (b, w) is `rows` rows of `units` units of
+ * `unit` bytes each, row r starting at src + b src_stride_b + w src_stride_w + r src_stride_row (bytes),
+ * and likewise in dst. Rows are contiguous; a [B][W][heads][tokens][dim] cache has rows = heads,
+ * units = tokens, unit = dim * element size.
+ *   dst = src (with equal strides): in place; slots that are their own parent then move nothing.
+ *         Otherwise dst must not overlap any src of the call.
+ *   parent : [B] rows of K int32, parent_stride elements apart (>= K), device: hs_beam_step's out_parent,
+ *            or its first K of more slots. An entry outside [0, W) (an empty slot) leaves the slot's
+ *            state as it was.
+ *   count  : NULL, or [B] int32 device: only the first count[b] units of each row are copied (clamped to
+ *            [0, units]); what lies behind them is left as it was.
+ * W         : beams in src; K: slots in dst, 1 .. HS_MAX_BEAMS each (in place the buffer holds
+ *             max(W, K)). Any alignment; rows, pointers and strides that are multiples of 16 bytes
+ *             move fastest.
+ * n         : tensors, 1 .. HS_MAX_STATES. One launch for every 32 of them.
+ */
+typedef struct hs_state {
+  const void* src;
+  void* dst;
+  int64_t src_stride_b, src_stride_w, src_stride_row;
+  int64_t dst_stride_b, dst_stride_w, dst_stride_row;
+  int64_t rows, units, unit;
+} hs_state;
+
+int hs_beam_reorder(const hs_state* states_host, int n, int B, int W, int K, const int32_t* parent,
+                    int64_t parent_stride, const int32_t* count, void* stream);
+
+/*
+ * hs_draft_tree - EAGLE-2's dynamic pruning of a grown tree: of the nodes that D steps of
+ * hs_beam_step have left, the M - 1 of largest score, with the root, as the tree that is verified.
+ * A node ranks by the smaller of its score and its parent's rank, so that a kept node's parent is kept
+ * (a log-probability is never positive, so this is its score); equal ones rank lower step first, then
+ * lower slot.
+ *   score, parent, token : [D][B][K] fp32, int32, int32 device: the K slots of every step as
+ *       hs_beam_step writes them. A slot of step d continues slot `parent` of step d - 1 (of the first
+ *       step: the root). A slot with a negative parent or a score that is not finite is empty, and so
+ *       is one whose parent is empty or not in [0, K).
+ *   Nodes are numbered breadth first: 0 the root, then by step, then by slot, so a parent comes before
+ *   its children. Outputs, each [B][M], a node past count[b] as given last:
+ *   node_token  int32: the token (the root: -1); -1
+ *   node_parent int32: the parent's number (the root: -1); -1
+ *   node_depth  int32: steps from the root (0); -1
+ *   node_slot   int32: the slot that grew it (the root: -1), which its states are kept under; -1
+ *   node_score  fp32:  its score (the root: 0); -inf
+ *   node_mask   uint64: bit i set where node i is on its path, itself and the root included; 0
+ *   cand        [B][M][K] int32: the tokens of its kept children in slot order, which is rank order,
+ *       then -1: the kept children that hs_candidate_mass takes, with K = M positions and C = K.
+ *   count       [B] int32: nodes kept, the root included.
+ *   Any output may be NULL.
+ * 1 <= D <= HS_MAX_DEPTH, K <= HS_MAX_BEAMS, 2 <= M <= HS_MAX_POSITIONS. One launch, one wave a
+ * query.
+ */
+typedef struct hs_tree_args {
+  const float* score;
+  const int32_t* parent;
+  const int32_t* token;
+  int D, B, K, M;
+  int32_t* node_token;
+  int32_t* node_parent;
+  int32_t* node_depth;
+  int32_t* node_slot;
+  float* node_score;
+  uint64_t* node_mask;
+  int32_t* cand;
+  int32_t* count;
+} hs_tree_args;
+
+int hs_draft_tree(const hs_tree_args* args, void* stream);
 
 /* Name of a status code; the thread's last error message; library version (major*10000+minor*100+patch). */
 const char* hs_status_string(int status);

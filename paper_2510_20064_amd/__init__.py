@@ -4,7 +4,7 @@ Argument marshalling only: every step runs in the library's HIP kernels. PyTorch
 device memory and the current HIP stream. The function names match the C ABI declared in
 include/hedgespec.h (hs_softmax_stats, hs_eval_alpha, hs_eval_topl, hs_accept_len,
 hs_hedge_update, hs_normalhedge_update, hs_delayed_update, hs_play, hs_regret_update,
-hs_round). There is no CPU fallback: if the library is not built,
+hs_round, hs_beam_step, hs_beam_reorder, hs_draft_tree). There is no CPU fallback: if the library is not built,
 loading raises.
 """
 from __future__ import annotations
@@ -26,6 +26,9 @@ LOSS_LENGTH, LOSS_ACCEPT_TOKEN, LOSS_ACCEPT_CHUNK = 0, 1, 2
 MAX_DRAFTERS = 64
 MAX_POSITIONS = 64
 MAX_TOPL = 32  # HS_MAX_TOPL
+MAX_BEAMS = 64
+MAX_DEPTH = 32
+MAX_STATES = 1024
 
 
 class HsError(RuntimeError):
@@ -52,6 +55,32 @@ class hs_round_args(ctypes.Structure):
         ("p", ctypes.c_void_p), ("c", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
         ("workspace_bytes", ctypes.c_size_t),
     ]
+
+
+class hs_beam_args(ctypes.Structure):
+    _fields_ = [
+        ("logits", hs_view), ("B", ctypes.c_int), ("W", ctypes.c_int), ("K", ctypes.c_int),
+        ("V", ctypes.c_int64), ("dtype", ctypes.c_int), ("temperature", ctypes.c_double),
+        ("score", ctypes.c_void_p), ("done", ctypes.c_void_p), ("score_stride", ctypes.c_int64),
+        ("eos", ctypes.c_int32), ("out_score", ctypes.c_void_p), ("out_parent", ctypes.c_void_p),
+        ("out_token", ctypes.c_void_p), ("out_done", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
+class hs_state(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p)] + [
+        (n, ctypes.c_int64) for n in ("src_stride_b", "src_stride_w", "src_stride_row",
+                                      "dst_stride_b", "dst_stride_w", "dst_stride_row",
+                                      "rows", "units", "unit")]
+
+
+class hs_tree_args(ctypes.Structure):
+    _fields_ = [("score", ctypes.c_void_p), ("parent", ctypes.c_void_p),
+                ("token", ctypes.c_void_p), ("D", ctypes.c_int), ("B", ctypes.c_int),
+                ("K", ctypes.c_int), ("M", ctypes.c_int)] + [
+        (n, ctypes.c_void_p) for n in ("node_token", "node_parent", "node_depth", "node_slot",
+                                       "node_score", "node_mask", "cand", "count")]
 
 
 _lib = None
@@ -87,6 +116,11 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.hs_normalhedge_update.argtypes = [P, P, P, P, I, I, I, P]
     lib.hs_round.argtypes = [ctypes.POINTER(hs_round_args), P]
     lib.hs_delayed_update.argtypes = [P, P, I, I, I, I, P, I64, P, P, P, P, D, P, P, P, P, P, P]
+    lib.hs_beam_step_workspace_size.argtypes = [I, I, I, I64, I]
+    lib.hs_beam_step_workspace_size.restype = SZ
+    lib.hs_beam_step.argtypes = [ctypes.POINTER(hs_beam_args), P]
+    lib.hs_beam_reorder.argtypes = [ctypes.POINTER(hs_state), I, I, I, I, P, I64, P, P]
+    lib.hs_draft_tree.argtypes = [ctypes.POINTER(hs_tree_args), P]
     lib.hs_set_wait_limit.argtypes = [I]
     lib.hs_set_wait_limit.restype = None
     lib.hs_stream_read.argtypes = [P, SZ, I, I, I, P, P]
@@ -95,7 +129,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.hs_last_error.restype = ctypes.c_char_p
     for name in ["hs_softmax_stats", "hs_eval_alpha", "hs_eval_alpha_noalloc", "hs_eval_topl", "hs_play", "hs_regret_update",
                  "hs_accept_len", "hs_hedge_update",
-                 "hs_normalhedge_update", "hs_round", "hs_delayed_update", "hs_version"]:
+                 "hs_normalhedge_update", "hs_round", "hs_delayed_update", "hs_beam_step",
+                 "hs_beam_reorder", "hs_draft_tree", "hs_version"]:
         getattr(lib, name).restype = I
     _lib = lib
     return lib
@@ -571,3 +606,317 @@ class Round:
 
     def run(self, stream=None) -> None:
         _check(self.lib.hs_round(ctypes.byref(self.args), _stream(stream)))
+
+
+# ---- growing a draft tree, or a beam search -----------------------------------------------------
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _one_device(*tensors) -> torch.device:
+    """The GPU that every tensor (None: absent) is on."""
+    have = [t for t in tensors if t is not None]
+    dev = have[0].device
+    _need(dev.type == "cuda", "the tensors must be on a GPU, got %s" % dev)
+    _need(all(t.device == dev for t in have), "the tensors must be on one device")
+    return dev
+
+
+def _launch(fn, dev: torch.device, stream, *args) -> None:
+    """fn(*args, stream) on `stream`, or on dev's current stream, with dev current."""
+    if stream is None:
+        stream = torch.cuda.current_stream(dev)
+    _need(stream.device == dev, "the stream is on another device than the tensors")
+    if torch.cuda.current_device() == dev.index:
+        _check(fn(*args, stream.cuda_stream))
+    else:
+        with torch.cuda.device(dev):
+            _check(fn(*args, stream.cuda_stream))
+
+
+def _full(t: torch.Tensor, shape, dtype, what: str) -> None:
+    _need(tuple(t.shape) == tuple(shape) and t.dtype == dtype and t.is_contiguous(),
+          "%s must be a contiguous %s tensor of shape %s" % (what, dtype, list(shape)))
+
+
+def beam_step_workspace_size(B: int, W: int, K: int, V: int, dtype: int) -> int:
+    return int(load_library().hs_beam_step_workspace_size(B, W, K, V, dtype))
+
+
+class BeamStep:
+    """Pre-marshalled hs_beam_step call for fixed buffers: the K best continuations of each query's
+    W beams by score + log softmax(logits / temperature).
+
+    logits [B][W][>= V] (V contiguous, rows 16-byte aligned), score [B][W] f32 (rows may be further
+    apart), done [B][W] uint8 or bool with score's strides, or None. run() fills and returns `out`:
+    score [B][K] f32, parent and token [B][K] i32 (-1: empty slot) and, where `out` has it, or done
+    or an eos is given, done [B][K] uint8. `workspace` may be shared by calls that do not overlap."""
+
+    def __init__(self, logits: torch.Tensor, score: torch.Tensor, K: int, V: Optional[int] = None,
+                 temperature: float = 1.0, done: Optional[torch.Tensor] = None, eos: int = -1,
+                 out: Optional[dict] = None, workspace: Optional[torch.Tensor] = None):
+        _need(logits.dim() == 3, "logits must be [B][W][V]")
+        B, W, ld = logits.shape
+        V = ld if V is None else V
+        self.B, self.W, self.K, self.V, self.dtype = B, W, K, V, _dtype_code(logits)
+        a = hs_beam_args()
+        a.B, a.W, a.K, a.V, a.dtype = B, W, K, V, self.dtype
+        a.temperature, a.eos = temperature, eos
+        _need(tuple(score.shape) == (B, W) and score.dtype == torch.float32 and
+              (W == 1 or score.stride(1) == 1), "score must be a float32 [B][W] tensor")
+        a.score_stride = W if B == 1 else score.stride(0)
+        if done is not None:
+            _need(tuple(done.shape) == (B, W) and done.dtype in (torch.uint8, torch.bool) and
+                  (W == 1 or done.stride(1) == 1) and (B == 1 or done.stride(0) == score.stride(0)),
+                  "done must be a uint8 or bool [B][W] tensor with score's strides")
+        o = {} if out is None else out
+        dev = logits.device
+        for name, dt in (("score", torch.float32), ("parent", torch.int32), ("token", torch.int32)):
+            if name not in o:
+                o[name] = torch.empty((B, K), dtype=dt, device=dev)
+            _full(o[name], (B, K), dt, "out[%r]" % name)
+        if "done" not in o and (done is not None or eos >= 0):
+            o["done"] = torch.empty((B, K), dtype=torch.uint8, device=dev)
+        if "done" in o:
+            _full(o["done"], (B, K), torch.bool if o["done"].dtype == torch.bool else torch.uint8,
+                  "out['done']")
+        if workspace is None:
+            n = beam_step_workspace_size(B, W, K, V, self.dtype)
+            workspace = torch.empty(max(n, 1), dtype=torch.uint8, device=dev)
+        _need(workspace.is_contiguous(), "workspace must be contiguous")
+        self.score, self.done, self.out, self.workspace = score, done, o, workspace
+        a.score, a.done = score.data_ptr(), None if done is None else done.data_ptr()
+        a.out_score, a.out_parent = o["score"].data_ptr(), o["parent"].data_ptr()
+        a.out_token = o["token"].data_ptr()
+        a.out_done = o["done"].data_ptr() if "done" in o else None
+        a.workspace = workspace.data_ptr()
+        a.workspace_bytes = workspace.numel() * workspace.element_size()
+        self.args, self._ref = a, ctypes.byref(a)
+        self.set_logits(logits)
+        self.device = _one_device(logits, score, done, workspace, *o.values())
+        self._fn = load_library().hs_beam_step
+
+    def set_logits(self, logits: torch.Tensor) -> None:
+        """Another logits tensor of the same shape and type."""
+        _need(logits.dim() == 3 and logits.shape[0] == self.B and logits.shape[1] == self.W and
+              logits.shape[2] >= self.V and _dtype_code(logits) == self.dtype,
+              "logits shape or type changed")
+        _need(logits.stride(2) == 1, "logits rows must be contiguous")
+        _need(not hasattr(self, "device") or logits.device == self.device, "logits device changed")
+        self.logits = logits
+        self.args.logits = hs_view(logits.data_ptr(), logits.stride(0) if self.B > 1 else 0,
+                                   logits.stride(1) if self.W > 1 else 0)
+
+    def run(self, stream=None) -> dict:
+        _launch(self._fn, self.device, stream, self._ref)
+        return self.out
+
+
+def _lend(stream, *tensors) -> None:
+    """Tensors made on the current stream and dropped after a call on another one."""
+    if stream is not None:
+        for t in tensors:
+            t.record_stream(stream)
+
+
+def beam_step(logits: torch.Tensor, score: torch.Tensor, K: int, V: Optional[int] = None,
+              temperature: float = 1.0, done: Optional[torch.Tensor] = None, eos: int = -1,
+              out: Optional[dict] = None, workspace: Optional[torch.Tensor] = None,
+              stream=None) -> dict:
+    """hs_beam_step, once (see BeamStep, which a loop keeps)."""
+    plan = BeamStep(logits, score, K, V=V, temperature=temperature, done=done, eos=eos, out=out,
+                    workspace=workspace)
+    if workspace is None:
+        _lend(stream, plan.workspace)
+    return plan.run(stream)
+
+
+def _state_rows(t: torch.Tensor, axis: Optional[int], what: str):
+    """(row stride in bytes, rows, units, bytes of a unit) of one [B][W]... state."""
+    es = t.element_size()
+    shape, stride = list(t.shape), list(t.stride())
+    first = 2 if axis is None else axis
+    unit = 1
+    for d in range(t.dim() - 1, first - 1, -1):  # units, contiguous
+        _need(shape[d] == 1 or stride[d] == unit, "%s: the dims %s must be contiguous" %
+              (what, "after the beams" if axis is None else "from `axis` on"))
+        unit *= shape[d]
+    units = 1 if axis is None else shape[axis]
+    rows, step = 1, 0
+    for d in range(first - 1, 1, -1):  # rows, one stride
+        if shape[d] == 1:
+            continue
+        _need(rows == 1 or stride[d] == rows * step,
+              "%s: the dims before `axis` must collapse to one stride" % what)
+        step = step if rows > 1 else stride[d]
+        rows *= shape[d]
+    return step * es, rows, units, unit // max(units, 1) * es
+
+
+class BeamReorder:
+    """Pre-marshalled hs_beam_reorder call: the states of every beam follow parent.
+
+    states: tensors [B][W]..., in place, or `out`: as many tensors [B][K]... of the same types.
+    parent [B][K] i32 (rows may be further apart; outside [0, W): the slot keeps its state), K <= W in
+    place. axis: the dim (>= 2) along which count [B] i32 bounds what is moved; the dims from it on are
+    contiguous, those between the beams and it collapse to one stride (axis=3 for
+    [B][W][heads][tokens][dim]). Without an axis all dims after the beams are contiguous.
+    run() returns the tensors that hold the result."""
+
+    def __init__(self, states, parent: torch.Tensor, count: Optional[torch.Tensor] = None,
+                 axis: Optional[int] = None, out=None):
+        src = [states] if isinstance(states, torch.Tensor) else list(states)
+        dst = src if out is None else [out] if isinstance(out, torch.Tensor) else list(out)
+        _need(len(src) >= 1 and len(src) == len(dst), "as many out tensors as states, one at least")
+        _need(parent.dim() == 2 and parent.dtype == torch.int32 and
+              (parent.shape[1] == 1 or parent.stride(1) == 1), "parent must be an int32 [B][K] tensor")
+        B, K = parent.shape
+        _need(all(t.dim() >= 2 for t in src + dst), "a state is [B][W]...")
+        W = src[0].shape[1]
+        if count is not None:
+            _full(count, (B,), torch.int32, "count")
+            _need(axis is not None, "count needs the axis it bounds")
+        descs = []
+        for i, (x, y) in enumerate(zip(src, dst)):
+            what = "state %d" % i
+            _need(x.dtype == y.dtype and x.shape[2:] == y.shape[2:], "%s: out differs in type or dims" % what)
+            _need(tuple(x.shape[:2]) == (B, W), "%s: must be [B][W]... like the others" % what)
+            _need(y.shape[0] == B and (y.shape[1] >= K if y is x else y.shape[1] == K),
+                  "%s: out must be [B][K]... (in place K <= W)" % what)
+            _need(axis is None or 2 <= axis < x.dim(), "%s: axis must be one of the dims after the beams" % what)
+            if x.numel() == 0 or y.numel() == 0:
+                continue
+            es = x.element_size()
+            xr, rows, units, unit = _state_rows(x, axis, what)
+            yr = _state_rows(y, axis, what)[0]
+            descs.append(hs_state(
+                x.data_ptr(), y.data_ptr(), x.stride(0) * es if B > 1 else 0,
+                x.stride(1) * es if W > 1 else 0, xr, y.stride(0) * es if B > 1 else 0,
+                y.stride(1) * es if y.shape[1] > 1 else 0, yr, rows, units, unit))
+        self.src, self.dst, self.parent, self.count = src, dst, parent, count
+        self.n, self.B, self.W, self.K = len(descs), B, W, K
+        self.states = (hs_state * max(1, len(descs)))(*descs)
+        self.device = _one_device(parent, count, *src, *dst)
+        self._args = (self.states, self.n, B, W, K, parent.data_ptr(),
+                      parent.stride(0) if B > 1 else K, None if count is None else count.data_ptr())
+        self._fn = load_library().hs_beam_reorder
+
+    def run(self, stream=None) -> list:
+        if self.n:
+            _launch(self._fn, self.device, stream, *self._args)
+        return self.dst
+
+
+def beam_reorder(states, parent: torch.Tensor, count: Optional[torch.Tensor] = None,
+                 axis: Optional[int] = None, out=None, stream=None) -> list:
+    """hs_beam_reorder, once (see BeamReorder, which a loop keeps)."""
+    return BeamReorder(states, parent, count=count, axis=axis, out=out).run(stream)
+
+
+class DraftTree:
+    """Pre-marshalled hs_draft_tree call: the M - 1 best nodes of D grown steps and the root as a
+    breadth-first tree.
+
+    score f32, parent and token i32: [D][B][K], as D calls of BeamStep leave them. run() fills and
+    returns `out`: token, parent, depth, slot [B][M] i32, score [B][M] f32, mask [B][M] i64 (ancestor
+    bits), cand [B][M][K] i32 (candidate_mass takes it as cand[:, None]) and count [B] i32."""
+
+    def __init__(self, score: torch.Tensor, parent: torch.Tensor, token: torch.Tensor, M: int,
+                 out: Optional[dict] = None):
+        _need(score.dim() == 3, "score must be [D][B][K]")
+        D, B, K = score.shape
+        _full(score, (D, B, K), torch.float32, "score")
+        _full(parent, (D, B, K), torch.int32, "parent")
+        _full(token, (D, B, K), torch.int32, "token")
+        o = {} if out is None else out
+        i32 = torch.int32
+        for name, shape, dt in (("token", (B, M), i32), ("parent", (B, M), i32),
+                                ("depth", (B, M), i32), ("slot", (B, M), i32),
+                                ("score", (B, M), torch.float32), ("mask", (B, M), torch.int64),
+                                ("cand", (B, M, K), i32), ("count", (B,), i32)):
+            if name not in o:
+                o[name] = torch.empty(shape, dtype=dt, device=score.device)
+            _full(o[name], shape, dt, "out[%r]" % name)
+        a = hs_tree_args(score.data_ptr(), parent.data_ptr(), token.data_ptr(), D, B, K, M,
+                         *[o[n].data_ptr() for n in ("token", "parent", "depth", "slot", "score",
+                                                     "mask", "cand", "count")])
+        self.score, self.parent, self.token, self.out = score, parent, token, o
+        self.args, self._ref = a, ctypes.byref(a)
+        self.device = _one_device(score, parent, token, *o.values())
+        self._fn = load_library().hs_draft_tree
+
+    def run(self, stream=None) -> dict:
+        _launch(self._fn, self.device, stream, self._ref)
+        return self.out
+
+
+def draft_tree(score: torch.Tensor, parent: torch.Tensor, token: torch.Tensor, M: int,
+               out: Optional[dict] = None, stream=None) -> dict:
+    """hs_draft_tree, once (see DraftTree, which a loop keeps)."""
+    return DraftTree(score, parent, token, M, out=out).run(stream)
+
+
+class TreeGrowth:
+    """EAGLE-2's dynamic draft tree, level by level, for B queries: from the root each of depth levels
+    keeps the K best continuations, the W best of which are drafted further, and M - 1 nodes of all
+    levels are verified with the root. Scheduling only: the steps run in the library's kernels.
+
+    states: the drafter's per-beam tensors [B][W]... (caches, hidden states; the root's in beam 0),
+    which follow the W beams in place after every level but the last.
+
+        growth = TreeGrowth(B, depth, W, K, M, states=[hidden], device=dev)
+        token = growth.level(draft(root))        # logits [B][1][V]; token [B][W] to draft from
+        for _ in range(depth - 1):
+            token = growth.level(draft(token))   # logits [B][W][V]
+        tree = growth.tree()                     # DraftTree's outputs
+        gamma = candidate_mass(target, lse, tree["cand"][:, None])
+    """
+
+    def __init__(self, B: int, depth: int, W: int, K: int, M: int, states=(), temperature: float = 1.0,
+                 count: Optional[torch.Tensor] = None, axis: Optional[int] = None, device="cuda"):
+        _need(1 <= depth <= MAX_DEPTH and 1 <= W <= K <= MAX_BEAMS and 2 <= M <= MAX_POSITIONS,
+              "need 1 <= depth <= %d, 1 <= W <= K <= %d and 2 <= M <= %d" %
+              (MAX_DEPTH, MAX_BEAMS, MAX_POSITIONS))
+        self.B, self.depth, self.W, self.K, self.temperature = B, depth, W, K, temperature
+        dev = torch.device(device)
+        shape = (depth, B, K)
+        self.score = torch.empty(shape, dtype=torch.float32, device=dev)
+        self.parent = torch.empty(shape, dtype=torch.int32, device=dev)
+        self.token = torch.empty(shape, dtype=torch.int32, device=dev)
+        self.root = torch.zeros((B, 1), dtype=torch.float32, device=dev)
+        states = [states] if isinstance(states, torch.Tensor) else list(states)
+        _need(all(t.dim() >= 2 and t.shape[1] == W for t in states), "a state is [B][W]...")
+        self._moves = [BeamReorder(states, self.parent[d][:, :W], count=count, axis=axis)
+                       for d in range(depth - 1)] if states else []
+        self._plans = [None] * depth
+        self._tree = DraftTree(self.score, self.parent, self.token, M)
+        self.d = 0
+
+    def level(self, logits: torch.Tensor, V: Optional[int] = None, stream=None) -> torch.Tensor:
+        """One level from logits [B][n][V], n = 1 for the first and W after it. Returns the tokens
+        [B][W] of the beams to draft from next (-1: an empty slot)."""
+        d = self.d
+        _need(d < self.depth, "the tree has all its levels: tree() ends it")
+        plan = self._plans[d]
+        if plan is None or plan.V != (logits.shape[2] if V is None else V) or \
+                plan.dtype != _dtype_code(logits):
+            up = self.root if d == 0 else self.score[d - 1][:, :self.W]
+            plan = BeamStep(logits, up, self.K, V=V, temperature=self.temperature,
+                            out={"score": self.score[d], "parent": self.parent[d],
+                                 "token": self.token[d]})
+            _lend(stream, plan.workspace)
+            self._plans[d] = plan
+        plan.set_logits(logits)
+        plan.run(stream)
+        if d < len(self._moves):
+            self._moves[d].run(stream)
+        self.d += 1
+        return self.token[d][:, :self.W]
+
+    def tree(self, stream=None) -> dict:
+        """The kept nodes of the levels grown; the next level() starts a new tree."""
+        _need(self.d == self.depth, "%d of %d levels are grown" % (self.d, self.depth))
+        self.d = 0
+        return self._tree.run(stream)

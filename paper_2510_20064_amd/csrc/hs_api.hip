@@ -7,7 +7,7 @@
 
 #include <mutex>
 
-#include "hs_internal.h"
+#include "hs_beam.h"
 
 #define HS_API extern "C" __attribute__((visibility("default")))
 
@@ -611,5 +611,146 @@ HS_API int hs_round(const hs_round_args* r, void* stream) {
   a.c = r->c;
   if ((rc = check_capacity(q, g))) return rc;
   if ((rc = run_eval(q, g, rows, &a, (hipStream_t)stream))) return rc;
+  return ok();
+}
+
+HS_API size_t hs_beam_step_workspace_size(int B, int W, int K, int64_t V, int dtype) {
+  hs::BeamGeom g;
+  if (!hs::beam_geom(B, W, K, V, dtype, &g)) return 0;
+  return hs::beam_ws_bytes(g);
+}
+
+namespace {
+
+// Whether [a, a + na) and [b, b + nb) share a byte (an absent buffer shares none).
+bool overlap(const void* a, uint64_t na, const void* b, uint64_t nb) {
+  const uint64_t x = (uint64_t)(uintptr_t)a, y = (uint64_t)(uintptr_t)b;
+  return a && b && x < y + nb && y < x + na;
+}
+
+}  // namespace
+
+HS_API int hs_beam_step(const hs_beam_args* a, void* stream) {
+  if (!a) return fail(HS_ERR_NULL, "args is NULL");
+  if (a->B < 1 || a->W < 1 || a->K < 1 || a->V < 1)
+    return fail(HS_ERR_SHAPE, "B, W, K and V must be >= 1 (got B=%d W=%d K=%d V=%lld)", a->B, a->W,
+                a->K, (long long)a->V);
+  if (a->B > HS_MAX_QUERIES || a->W > HS_MAX_BEAMS || a->K > HS_MAX_BEAMS)
+    return fail(HS_ERR_LIMIT, "limits: B <= %d, W <= %d, K <= %d (got B=%d W=%d K=%d)",
+                HS_MAX_QUERIES, HS_MAX_BEAMS, HS_MAX_BEAMS, a->B, a->W, a->K);
+  if (a->dtype != HS_F32 && a->dtype != HS_BF16 && a->dtype != HS_F16)
+    return fail(HS_ERR_DTYPE, "unknown dtype %d", a->dtype);
+  int rc = check_view(&a->logits, a->dtype, "logits");
+  if (rc) return rc;
+  if (!a->score || !a->out_score || !a->out_parent || !a->out_token)
+    return fail(HS_ERR_NULL, "score, out_score, out_parent and out_token are required");
+  if (a->score_stride < a->W) return fail(HS_ERR_SHAPE, "score_stride must be >= W");
+  if (!(a->temperature >= 1e-30 && a->temperature <= 1e30))
+    return fail(HS_ERR_TEMPERATURE, "temperature must be in [1e-30, 1e30] (got %g)", a->temperature);
+  const bool own = a->K == a->W && a->score_stride == a->W;  // an output may be its input
+  const uint64_t in = (uint64_t)(a->B - 1) * (uint64_t)a->score_stride + (uint64_t)a->W;
+  const uint64_t out = (uint64_t)a->B * (uint64_t)a->K;
+  struct {
+    const void* p;
+    uint64_t bytes;
+  } ins[] = {{a->score, 4 * in}, {a->done, in}},
+    outs[] = {{a->out_score, 4 * out}, {a->out_done, out}, {a->out_parent, 4 * out},
+              {a->out_token, 4 * out}};
+  for (int i = 0; i < 2; ++i)
+    for (int o = 0; o < 4; ++o)
+      if (overlap(ins[i].p, ins[i].bytes, outs[o].p, outs[o].bytes) &&
+          !(own && i == o && ins[i].p == outs[o].p))
+        return fail(HS_ERR_ARG, "an output overlaps score or done");
+  hs::BeamGeom g;
+  if (!hs::beam_geom(a->B, a->W, a->K, a->V, a->dtype, &g))
+    return fail(HS_ERR_LIMIT, "V = %lld is beyond the limit of %lld logits per row", (long long)a->V,
+                (long long)hs::kMaxTeamSlices * hs::kThreads * (16 / elem_bytes(a->dtype)));
+  const size_t need = hs::beam_ws_bytes(g);
+  if (!a->workspace) return fail(HS_ERR_WORKSPACE, "workspace is NULL (need %zu bytes)", need);
+  if (a->workspace_bytes < need)
+    return fail(HS_ERR_WORKSPACE, "workspace too small: %zu < %zu bytes", a->workspace_bytes, need);
+  if (((uintptr_t)a->workspace & 255) != 0)
+    return fail(HS_ERR_ALIGN, "workspace must be 256-byte aligned");
+  rc = hs::launch_beam_step(g, *a, (hipStream_t)stream);
+  if (rc) return fail(rc, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+  return ok();
+}
+
+namespace {
+
+// The bytes that `beams` beams of every query span in a state's buffer, from its pointer; false where
+// they do not fit 62 bits.
+bool state_span(const hs_state& s, int B, int beams, int64_t sb, int64_t sw, int64_t sr, uint64_t* n) {
+  const __int128 row = (__int128)s.units * s.unit;
+  const __int128 all = row + (__int128)(B - 1) * sb + (__int128)(beams - 1) * sw +
+                       (__int128)(s.rows - 1) * sr;
+  if (all >= ((__int128)1 << 62)) return false;
+  *n = (uint64_t)all;
+  return true;
+}
+
+}  // namespace
+
+HS_API int hs_beam_reorder(const hs_state* states, int n, int B, int W, int K,
+                           const int32_t* parent, int64_t parent_stride, const int32_t* count,
+                           void* stream) {
+  if (!states || !parent) return fail(HS_ERR_NULL, "states_host and parent are required");
+  if (n < 1 || B < 1 || W < 1 || K < 1)
+    return fail(HS_ERR_SHAPE, "n, B, W and K must be >= 1 (got n=%d B=%d W=%d K=%d)", n, B, W, K);
+  if (n > HS_MAX_STATES || B > HS_MAX_QUERIES || W > HS_MAX_BEAMS || K > HS_MAX_BEAMS)
+    return fail(HS_ERR_LIMIT, "limits: n <= %d, B <= %d, W <= %d, K <= %d (got n=%d B=%d W=%d K=%d)",
+                HS_MAX_STATES, HS_MAX_QUERIES, HS_MAX_BEAMS, HS_MAX_BEAMS, n, B, W, K);
+  if (parent_stride < K) return fail(HS_ERR_SHAPE, "parent_stride must be >= K");
+  for (int i = 0; i < n; ++i) {
+    const hs_state& s = states[i];
+    if (!s.src || !s.dst) return fail(HS_ERR_NULL, "state %d: NULL pointer", i);
+    if (s.rows < 1 || s.units < 1 || s.unit < 1)
+      return fail(HS_ERR_SHAPE, "state %d: rows, units and unit must be >= 1", i);
+    if (s.src_stride_b < 0 || s.src_stride_w < 0 || s.src_stride_row < 0 || s.dst_stride_b < 0 ||
+        s.dst_stride_w < 0 || s.dst_stride_row < 0)
+      return fail(HS_ERR_SHAPE, "state %d: negative stride", i);
+    uint64_t from = 0, to = 0;
+    if (s.rows > INT32_MAX || s.units > ((int64_t)1 << 62) / s.unit ||
+        !state_span(s, B, W, s.src_stride_b, s.src_stride_w, s.src_stride_row, &from) ||
+        !state_span(s, B, K, s.dst_stride_b, s.dst_stride_w, s.dst_stride_row, &to))
+      return fail(HS_ERR_LIMIT, "state %d: too large", i);
+    if (!hs::reorder_fits(s, B)) return fail(HS_ERR_LIMIT, "state %d: too many rows or bytes", i);
+    // two slots' bytes must be apart where both are written
+    const int64_t row = s.units * s.unit;
+    if (!hs::state_apart(s, B, K, row))
+      return fail(HS_ERR_SHAPE, "state %d: rows, slots or queries of dst share bytes", i);
+    if (s.src == s.dst) {
+      if (s.src_stride_b != s.dst_stride_b || s.src_stride_w != s.dst_stride_w ||
+          s.src_stride_row != s.dst_stride_row)
+        return fail(HS_ERR_ARG, "state %d: in place with other strides", i);
+      if (from > to) to = from;
+    }
+    for (int j = 0; j < n; ++j) {
+      const hs_state& o = states[j];
+      if (j == i && s.src == s.dst) continue;
+      uint64_t bytes = 0;
+      if (!state_span(o, B, W, o.src_stride_b, o.src_stride_w, o.src_stride_row, &bytes) ||
+          overlap(o.src, bytes, s.dst, to))
+        return fail(HS_ERR_ARG, "state %d: dst overlaps the src of state %d", i, j);
+    }
+  }
+  const int rc = hs::launch_reorder(states, n, B, W, K, parent, parent_stride, count, (hipStream_t)stream);
+  if (rc) return fail(rc, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+  return ok();
+}
+
+HS_API int hs_draft_tree(const hs_tree_args* a, void* stream) {
+  if (!a) return fail(HS_ERR_NULL, "args is NULL");
+  if (a->D < 1 || a->B < 1 || a->K < 1 || a->M < 2)
+    return fail(HS_ERR_SHAPE, "need D, B, K >= 1 and M >= 2 (got D=%d B=%d K=%d M=%d)", a->D, a->B,
+                a->K, a->M);
+  if (a->D > HS_MAX_DEPTH || a->B > HS_MAX_QUERIES || a->K > HS_MAX_BEAMS || a->M > HS_MAX_POSITIONS)
+    return fail(HS_ERR_LIMIT, "limits: D <= %d, B <= %d, K <= %d, M <= %d (got D=%d B=%d K=%d M=%d)",
+                HS_MAX_DEPTH, HS_MAX_QUERIES, HS_MAX_BEAMS, HS_MAX_POSITIONS, a->D, a->B, a->K,
+                a->M);
+  if (!a->score || !a->parent || !a->token)
+    return fail(HS_ERR_NULL, "score, parent and token are required");
+  const int rc = hs::launch_draft_tree(*a, (hipStream_t)stream);
+  if (rc) return fail(rc, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
   return ok();
 }

@@ -1,0 +1,121 @@
+// Declarations shared by the kernels that grow a draft tree or run a beam search (hs_beam.hip,
+// hs_reorder.hip, hs_tree.hip) and their host entries, with the wave-wide selection they use.
+#pragma once
+
+#include "hs_wave.h"
+
+namespace hs {
+
+// ---- launches (host side, defined next to their kernels) ----------------------------------------
+
+// How a step's rows are cut: slices of `chunks` chunks of kBeamChunk vectors, one wave each.
+constexpr int kBeamChunk = 256;       // 16-byte vectors of a chunk, four per lane
+constexpr int kBeamMaxSlices = 128;   // slices of a row
+struct BeamGeom {
+  int B, W, K, S, chunks;
+  int64_t V, nvec;
+  int dtype;
+};
+bool beam_geom(int B, int W, int K, int64_t V, int dtype, BeamGeom* g);
+size_t beam_ws_bytes(const BeamGeom& g);
+int launch_beam_step(const BeamGeom& g, const hs_beam_args& a, hipStream_t stream);
+bool reorder_fits(const hs_state& s, int B);  // its workgroups are numbered with 31 bits
+// Whether the rows of a state's dst (B queries, K slots, `row` bytes a row) are apart from each other.
+bool state_apart(const hs_state& s, int B, int K, int64_t row);
+int launch_reorder(const hs_state* states, int n, int B, int W, int K, const int32_t* parent,
+                   int64_t parent_stride, const int32_t* count, hipStream_t stream);
+int launch_draft_tree(const hs_tree_args& a, hipStream_t stream);
+
+// ---- wave-wide selection -------------------------------------------------------------------------
+
+// Lanes below this one whose bit is set in m.
+__device__ inline int lanes_below(uint64_t m) {
+  return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32),
+                                        __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u));
+}
+// LDS written by some lanes of a wave, then read by others of the same wave.
+__device__ inline void lds_wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+__device__ inline uint32_t uniform(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
+}
+__device__ inline uint64_t uniform(uint64_t x) {
+  return ((uint64_t)uniform((uint32_t)(x >> 32)) << 32) | uniform((uint32_t)x);
+}
+__device__ inline uint32_t wave_or_bits(uint32_t x) {
+  x |= (uint32_t)dpp_i<0xB1>((int)x);
+  x |= (uint32_t)dpp_i<0x4E>((int)x);
+  x |= (uint32_t)dpp_i<0x141>((int)x);
+  x |= (uint32_t)dpp_i<0x140>((int)x);
+  return (uint32_t)(__builtin_amdgcn_readlane((int)x, 0) | __builtin_amdgcn_readlane((int)x, 16) |
+                    __builtin_amdgcn_readlane((int)x, 32) | __builtin_amdgcn_readlane((int)x, 48));
+}
+
+// The largest x with at least n of the wave's keys >= x, bit by bit from the highest one on which
+// two keys differ: the n-th largest key, or, with fewer than n keys, at most the smallest (0 with
+// none). u[j] of every lane, j < nu (the same in every lane), 0 = no key. All lanes are active.
+template <int NU>
+__device__ inline uint64_t nth_largest(const uint64_t (&u)[NU], int nu, int n) {
+  uint32_t or_lo = 0, or_hi = 0, nand_lo = 0, nand_hi = 0;  // bits some key has, and some lacks
+#pragma unroll
+  for (int j = 0; j < NU; ++j)
+    if (j < nu && u[j] != 0) {
+      or_lo |= (uint32_t)u[j];
+      or_hi |= (uint32_t)(u[j] >> 32);
+      nand_lo |= ~(uint32_t)u[j];
+      nand_hi |= ~(uint32_t)(u[j] >> 32);
+    }
+  const uint64_t some = ((uint64_t)wave_or_bits(or_hi) << 32) | wave_or_bits(or_lo);
+  uint64_t open = some & (((uint64_t)wave_or_bits(nand_hi) << 32) | wave_or_bits(nand_lo));
+  uint64_t x = some & ~open;  // the bits that every key has
+  while (open) {
+    const uint64_t bit = 1ull << (63 - __builtin_clzll(open));
+    open &= ~bit;
+    int c = 0;
+#pragma unroll
+    for (int j = 0; j < NU; ++j)
+      if (j < nu) c += __builtin_popcountll(__ballot(u[j] >= (x | bit)));
+    if (c >= n) x |= bit;
+  }
+  return x;
+}
+
+// How many of list[0 .. n) exceed `mine`, n <= 64 the same in every lane; list is 16-byte aligned in
+// LDS and holds zeros from n up to the next multiple of 16.
+__device__ inline int count_above(const uint64_t* list, int n, uint64_t mine) {
+  typedef unsigned long long u2 __attribute__((ext_vector_type(2)));
+  int r = 0;
+  for (int c = 0; c < n; c += 16) {
+    u2 v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const u2*>(list + c + 2 * i);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r += (v[i][0] > mine ? 1 : 0) + (v[i][1] > mine ? 1 : 0);
+  }
+  return r;
+}
+
+// An fp32 value (no NaN) as an unsigned integer that orders like it, -0 as +0, and back (0 as +0).
+__device__ inline uint32_t ordered_of(float f) {
+  const int32_t x = __float_as_int(f), m = x >> 31;
+  return (uint32_t)((x ^ (m & 0x7FFFFFFF)) - m) ^ 0x80000000u;
+}
+__device__ inline float value_of(uint32_t u) {
+  const int32_t k = (int32_t)(u ^ 0x80000000u);
+  return __int_as_float(k >= 0 ? k : (int32_t)(0x80000000u | (uint32_t)(-k)));
+}
+// The same for fp64 (0 is below every value's image).
+__device__ inline uint64_t ordered_of(double d) {
+  const int64_t x = __double_as_longlong(d), m = x >> 63;
+  return (uint64_t)((x ^ (m & 0x7FFFFFFFFFFFFFFFll)) - m) ^ 0x8000000000000000ull;
+}
+__device__ inline double value_of(uint64_t u) {
+  const int64_t k = (int64_t)(u ^ 0x8000000000000000ull);
+  return __longlong_as_double(k >= 0 ? k
+                                     : (int64_t)(0x8000000000000000ull | (uint64_t)(-k)));
+}
+
+}  // namespace hs

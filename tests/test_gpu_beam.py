@@ -1,0 +1,626 @@
+"""GPU parity of hs_beam_step, hs_beam_reorder, hs_draft_tree and the growth of a tree by them, against
+oracle/beam.py in fp64.
+
+Tolerances. Parents, tokens and ended marks are exact: the order is that of fp64 scores. A score is
+rounded once to fp32 (2^-24 of its size) after a normaliser whose fp32 exponentials are off by at most
+  2^-23 (the exponential) + 17 * 2 * 2^-24 * ln 2 (the exponent: two roundings of at most 17 bits,
+  where e^-|x| |x| has its weight in a row of 2^17 logits) + 10 * 2^-24 (sums of 32)
+of themselves: 2.2e-6 together if every one were off the same way.
+Moved bytes and trees are exact.
+"""
+import numpy as np
+import pytest
+import torch
+
+import paper_2510_20064_amd as hs
+from oracle import beam
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+NORM_TOL = 2.2e-6
+
+
+def note(msg):
+    print("\n[case] " + msg, flush=True)
+
+
+def rows(g, B, W, V, dt, pad=8, scale=3.0):
+    """[B][W][ld] logits on the GPU, ld a multiple of 8, NaN behind V."""
+    ld = (V + pad - 1) // pad * pad
+    x = torch.full((B, W, ld), float("nan"), dtype=dt)
+    x[:, :, :V] = (torch.randn((B, W, V), generator=g) * scale).to(dt)
+    return x
+
+
+def scores(g, B, W):
+    return -torch.rand((B, W), generator=g).cumsum(1) - 1.0
+
+
+def check_step(x, score, K, V, T=1.0, done=None, eos=-1, **kw):
+    out = hs.beam_step(x.cuda() if not x.is_cuda else x, score.cuda(), K, V=V, temperature=T,
+                       done=None if done is None else done.cuda(), eos=eos, **kw)
+    torch.cuda.synchronize()
+    got = {k: v.cpu().numpy() for k, v in out.items()}
+    ref = beam.beam_step(x.cpu()[:, :, :V].double().numpy(), score.numpy(), K, T=T,
+                         done=None if done is None else done.numpy(), eos=eos)
+    same_step(got, ref)
+    return got
+
+
+def same_step(got, ref):
+    assert np.array_equal(got["parent"], ref["parent"])
+    assert np.array_equal(got["token"], ref["token"])
+    if "done" in got:
+        assert np.array_equal(got["done"].astype(np.uint8), ref["done"])
+    some = ref["parent"] >= 0
+    assert np.all(got["score"][~some] == -np.inf)
+    with np.errstate(over="ignore"):
+        near = np.abs(ref["score"][some]) < 1e38
+    r, s = ref["score"][some][near], got["score"][some][near].astype(np.float64)
+    assert np.all(np.abs(s - r) <= np.abs(r) * 2.0 ** -24 + NORM_TOL), np.abs(s - r).max()
+
+
+# ---- hs_beam_step ----------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("B,W,K,V", [(1, 1, 1, 1), (1, 1, 5, 3), (2, 3, 4, 7), (1, 64, 64, 9),
+                                     (3, 1, 64, 64), (2, 4, 10, 2048), (2, 4, 10, 2049),
+                                     (1, 7, 33, 4095), (3, 5, 11, 50257), (1, 2, 64, 70001)])
+def test_step_sizes(dtype, B, W, K, V):
+    note("step %s B=%d W=%d K=%d V=%d" % (dtype, B, W, K, V))
+    g = torch.Generator().manual_seed(B * 1000 + W * 100 + K + V)
+    x = rows(g, B, W, V, DTYPES[dtype])
+    check_step(x, scores(g, B, W), K, V, T=0.7)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("K", [1, 10, 64])
+def test_step_longest_rows(dtype, K):
+    V = (1 << 19) if dtype == "f32" else (1 << 20)
+    note("longest rows %s K=%d" % (dtype, K))
+    g = torch.Generator().manual_seed(K)
+    x = rows(g, 1, 2, V, DTYPES[dtype])
+    check_step(x, scores(g, 1, 2), K, V)
+
+
+@pytest.mark.parametrize("T", [1e-3, 0.25, 1.0, 1.4426950408889634, 30.0])
+def test_step_temperatures(T):
+    note("temperature %g" % T)
+    g = torch.Generator().manual_seed(7)
+    x = rows(g, 2, 3, 5000, torch.float32)
+    x[:, :, 17] = float("-inf")
+    check_step(x, scores(g, 2, 3), 12, 5000, T=T)
+
+
+def test_step_peaked_rows_like_a_model():
+    # 20 boosted tokens a row hold most of the mass; 32 beams, 64 kept
+    note("peaked rows")
+    g = torch.Generator().manual_seed(11)
+    V = 32000
+    z = torch.randn((2, 32, V), generator=g) * 3.0
+    z.scatter_add_(2, torch.randint(0, V, (2, 32, 20), generator=g), torch.full((2, 32, 20), 8.0))
+    check_step(z.to(torch.bfloat16), scores(g, 2, 32), 64, V)
+
+
+def test_step_ties():
+    # few levels of logits: ties within rows, across slices, and across identical beams
+    note("ties")
+    g = torch.Generator().manual_seed(13)
+    V = 9000
+    for dt in DTYPES.values():
+        x = torch.randint(-3, 3, (2, 4, V), generator=g).to(dt)
+        x[0, 1] = x[0, 0]          # identical beams of equal score: the lower beam first
+        x[1, 2] = x[1, 1]
+        x[1, 0, ::2] = -0.0        # signed zeros are equal
+        x[1, 0, 1::2] = 0.0
+        s = torch.tensor([[-1.0, -1.0, -3.0, -4.0], [-5.0, -2.0, -2.0, -9.0]])
+        for K in (1, 7, 64):
+            check_step(x, s, K, V)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_step_orders_that_fill_the_lists(dtype):
+    # rising, falling and constant rows: many chunks bring more candidates than a list holds
+    note("orders %s" % dtype)
+    V = 30000
+    dt = DTYPES[dtype]
+    up = torch.linspace(-20, 20, V)
+    x = torch.stack([up, up.flip(0), torch.full((V,), 3.0), up.abs(), -up.abs()])[None].to(dt)
+    s = torch.tensor([[-1.0, -1.25, -1.5, -1.75, -2.0]])
+    for K in (1, 10, 64):
+        check_step(x, s, K, V)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_step_masks_and_empty_rows(dtype):
+    note("masks %s" % dtype)
+    dt = DTYPES[dtype]
+    g = torch.Generator().manual_seed(17)
+    V = 5003
+    x = rows(g, 3, 8, V, dt)
+    low = torch.finfo(dt).min
+    x[0, 0, :V] = float("-inf")                    # nothing left
+    x[0, 1, :V] = float("-inf")
+    x[0, 1, 4321] = 1.0                            # one token left
+    x[0, 2, 100:] = float("-inf")                  # the tail masked
+    x[0, 3, :4990] = float("-inf")                 # all but the tail
+    x[0, 4, :V] = low                              # every logit at the lowest value
+    x[0, 5, 5:V] = low
+    x[0, 6, 77] = float("nan")                     # no distribution
+    x[0, 7, 78] = float("inf")
+    x[1, :, :V] = float("-inf")                    # a query with nothing at all
+    x[2, :, :V] = low
+    x[2, :, 9] = 0.0
+    for K in (4, 64):
+        check_step(x, scores(g, 3, 8), K, V, T=1.0)
+
+
+def test_step_large_logits():
+    note("large logits")
+    g = torch.Generator().manual_seed(19)
+    x = rows(g, 1, 4, 3000, torch.float32)
+    x[0, 1, :3000] += 1e6
+    x[0, 2, :3000] *= 1e5
+    x[0, 3, :3000] -= 1e7
+    check_step(x, scores(g, 1, 4), 16, 3000)
+    x[0, 3, 5] = 3e38                              # one token has it all
+    x[0, 2, :3000] = 3e38                          # and these share it
+    x[0, 1, :3000] = -3e38
+    for K in (8, 64):
+        check_step(x, scores(g, 1, 4), K, 3000)
+    check_step(x, scores(g, 1, 4), 64, 3000, T=0.1)
+
+
+def test_step_dead_and_finished_beams():
+    note("dead and finished beams")
+    g = torch.Generator().manual_seed(23)
+    B, W, V = 4, 6, 1000
+    x = rows(g, B, W, V, torch.bfloat16)
+    s = scores(g, B, W)
+    s[0, 2], s[0, 4] = float("-inf"), float("nan")
+    x[0, 2, :V] = float("nan")
+    s[1] = float("-inf")
+    s[2, 1] = float("inf")
+    done = torch.zeros((B, W), dtype=torch.uint8)
+    done[0, 0] = done[0, 4] = 1                    # finished; finished and holding nothing
+    done[2] = 1                                    # every beam has ended
+    done[3, 5] = 1
+    x[0, 0, :V] = float("nan")                     # not read
+    for K in (3, 6, 20):
+        check_step(x, s, K, V, done=done, eos=2)
+        check_step(x, s, K, V, eos=int(x[3, 0, :V].float().argmax()))
+        check_step(x, s, K, V, done=done, eos=V + 5)   # an end token that is no column
+    check_step(x, s, 6, V, done=done.bool(), eos=2)
+
+
+def test_step_strides_and_views():
+    note("strides")
+    g = torch.Generator().manual_seed(29)
+    V = 3001
+    big = torch.full((3, 5, 4, 3008), float("nan"), dtype=torch.float16, device="cuda")
+    big[:, :, 1, :V] = (torch.randn((3, 5, V), generator=g) * 3).half().cuda()
+    x = big[:, :, 1]                               # rows apart by four, queries by twenty
+    s = scores(g, 3, 9)
+    check_step(x, s[:, :5], 7, V)                  # a slice of wider rows of scores
+    shared = big[:, :1, 1].expand(3, 5, 3008)      # one row for every beam (the root's children)
+    check_step(shared, s[:, :5].contiguous(), 7, V)
+    check_step(big[:1, :1, 1], s[:1, :1], 7, V)
+    odd = torch.randn((1, 1, V), generator=g).cuda()  # one row needs no padding
+    check_step(odd, s[:1, :1], 7, V)
+
+
+def test_step_in_place_and_reused_workspace():
+    note("in place")
+    g = torch.Generator().manual_seed(31)
+    B, W, V = 5, 6, 4000
+    x = rows(g, B, W, V, torch.bfloat16)
+    s, done = scores(g, B, W), torch.zeros((B, W), dtype=torch.uint8)
+    done[:, 1] = 1
+    sd, dd = s.cuda(), done.cuda()
+    plan = hs.BeamStep(x.cuda(), sd, W, V=V, done=dd, eos=3, out={"score": sd, "done": dd})
+    ws = plan.workspace
+    for _ in range(3):                             # each step continues the last one's scores
+        ref = beam.beam_step(x[:, :, :V].double().numpy(), sd.cpu().numpy(), W,
+                             done=dd.cpu().numpy(), eos=3)
+        out = plan.run()
+        same_step({k: v.cpu().numpy() for k, v in out.items()}, ref)
+    ws.fill_(255)                                  # scratch: whatever it holds
+    a = {k: v.clone() for k, v in hs.beam_step(x.cuda(), s.cuda(), W, V=V, workspace=ws).items()}
+    b = hs.beam_step(x.cuda(), s.cuda(), W, V=V, workspace=ws)
+    assert all(torch.equal(a[k], b[k]) for k in a)
+
+
+def test_step_leaves_what_is_not_its_own():
+    note("guards")
+    g = torch.Generator().manual_seed(37)
+    x = rows(g, 3, 4, 2500, torch.float32).cuda()
+    K = 5
+    n = hs.beam_step_workspace_size(3, 4, K, 2500, hs.HS_F32)
+    ws = torch.full((n + 512,), 0xA5, dtype=torch.uint8, device="cuda")
+    bufs = {k: torch.full((5, K), -77, dtype=dt, device="cuda") for k, dt in
+            (("score", torch.float32), ("parent", torch.int32), ("token", torch.int32))}
+    hs.beam_step(x, scores(g, 3, 4).cuda(), K, V=2500, workspace=ws[:n],
+                 out={k: v[1:4] for k, v in bufs.items()})
+    torch.cuda.synchronize()
+    assert torch.all(ws[n:] == 0xA5)
+    for v in bufs.values():
+        assert torch.all(v[0] == -77) and torch.all(v[4] == -77) and not torch.any(v[1:4] == -77)
+
+
+def test_step_on_another_stream_and_in_a_graph():
+    note("stream and graph")
+    g = torch.Generator().manual_seed(41)
+    V = 20000
+    x = rows(g, 2, 5, V, torch.bfloat16)
+    other = rows(g, 2, 5, V, torch.bfloat16)
+    s = scores(g, 2, 5)
+    xd = x.cuda()
+    plan = hs.BeamStep(xd, s.cuda(), 9, V=V)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    plan.run(stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    ref = beam.beam_step(x[:, :, :V].double().numpy(), s.numpy(), 9)
+    same_step({k: v.cpu().numpy() for k, v in plan.out.items()}, ref)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        plan.run()
+    for y in (other, x, other):
+        xd.copy_(y)
+        graph.replay()
+        torch.cuda.synchronize()
+        ref = beam.beam_step(y[:, :, :V].double().numpy(), s.numpy(), 9)
+        same_step({k: v.cpu().numpy() for k, v in plan.out.items()}, ref)
+        eager = hs.beam_step(xd, s.cuda(), 9, V=V)
+        assert all(torch.equal(eager[k], plan.out[k]) for k in eager)
+
+
+def test_step_same_row_same_result_wherever_it_stands():
+    note("row independence")
+    g = torch.Generator().manual_seed(43)
+    x = rows(g, 1, 1, 40000, torch.bfloat16).expand(8, 4, -1).contiguous()
+    s = torch.full((8, 4), -1.5)
+    out = hs.beam_step(x.cuda(), s.cuda(), 16, V=40000)
+    assert all(torch.equal(v, v[:1].expand_as(v)) for v in out.values())
+    assert out["parent"][0].tolist() == [0, 1, 2, 3] * 4
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_step_random_shapes(seed):
+    rng = np.random.default_rng(seed)
+    B, W, K = int(rng.integers(1, 9)), int(rng.integers(1, 65)), int(rng.integers(1, 65))
+    V = int(np.exp(rng.uniform(0, np.log(60000))))
+    V = max(1, min(V, 2_000_000 // (B * W)))
+    dtype = list(DTYPES)[int(rng.integers(3))]
+    T = float(rng.choice([0.5, 0.7, 1.0, 1.3]))
+    note("random step seed=%d B=%d W=%d K=%d V=%d %s T=%g" % (seed, B, W, K, V, dtype, T))
+    g = torch.Generator().manual_seed(100 + seed)
+    x = rows(g, B, W, V, DTYPES[dtype])
+    ban = torch.rand((B, W, V), generator=g) < 0.3
+    x[:, :, :V][ban] = float("-inf")
+    done = (torch.rand((B, W), generator=g) < 0.2).to(torch.uint8)
+    s = scores(g, B, W)
+    s[torch.rand((B, W), generator=g) < 0.1] = float("-inf")
+    check_step(x, s, K, V, T=T, done=done, eos=min(2, V - 1))
+
+
+# ---- hs_beam_reorder -------------------------------------------------------------------------------
+
+def check_reorder(states, parent, count=None, axis=None, out=None):
+    """In place (out None) or into `out`; every byte of the buffers against the oracle."""
+    src = [s.clone() for s in states]
+    dst = src if out is None else [o.clone() for o in out]
+    got = hs.beam_reorder(src, parent.cuda(), count=None if count is None else count.cuda(),
+                          axis=axis, out=None if out is None else dst)
+    torch.cuda.synchronize()
+    for s0, d0, d, s in zip(states, states if out is None else out, got, src):
+        want = beam.beam_reorder(s0.cpu().numpy(), d0.cpu().numpy(), parent.numpy(),
+                                 None if count is None else count.numpy(), axis)
+        assert np.array_equal(d.cpu().numpy(), want)
+        if out is not None:
+            assert torch.equal(s, s0)
+
+
+def ints(g, shape, dtype=torch.int32):
+    hi = 250 if dtype == torch.uint8 else 30000
+    return torch.randint(0, hi, shape, generator=g).to(dtype).cuda()
+
+
+@pytest.mark.parametrize("W,K", [(1, 1), (4, 4), (5, 9), (9, 5), (17, 17), (32, 20), (64, 64)])
+@pytest.mark.parametrize("shape", [(), (1,), (33,), (4096,), (3, 7, 5)])
+def test_reorder_shapes(W, K, shape):
+    note("reorder W=%d K=%d %s" % (W, K, shape))
+    g = torch.Generator().manual_seed(W * 100 + K + len(shape))
+    B = 3
+    p = torch.randint(-1, W + 1, (B, K), generator=g, dtype=torch.int32)  # some of them no beam
+    for dt in (torch.uint8, torch.int16, torch.int32, torch.float64):
+        x = ints(g, (B, W) + shape, dt)
+        check_reorder([x], p, out=[ints(g, (B, K) + shape, dt)])
+        if K <= W:
+            check_reorder([x], p)
+
+
+def test_reorder_permutations_cycles_and_copies_in_place():
+    note("permutations")
+    g = torch.Generator().manual_seed(3)
+    W = 11
+    x = ints(g, (6, W, 500))
+    p = torch.stack([torch.arange(W), torch.arange(W).flip(0), torch.arange(W).roll(1),
+                     torch.zeros(W, dtype=torch.long), torch.full((W,), W - 1),
+                     torch.randperm(W, generator=g)]).to(torch.int32)
+    check_reorder([x], p)
+
+
+@pytest.mark.parametrize("dtype,D", [(torch.float16, 128), (torch.int32, 33), (torch.uint8, 7)])
+@pytest.mark.parametrize("inplace", [True, False])
+def test_reorder_counted_caches(dtype, D, inplace):
+    note("caches %s D=%d in place %s" % (dtype, D, inplace))
+    g = torch.Generator().manual_seed(D)
+    B, W, H, cap = 7, 5, 3, 77
+    x = [ints(g, (B, W, H, cap, D), dtype) for _ in range(3)]
+    p = torch.randint(0, W, (B, W), generator=g, dtype=torch.int32)
+    n = torch.tensor([0, 1, 5, 76, 77, 78, -3], dtype=torch.int32)  # clamped to [0, cap]
+    o = None if inplace else [ints(g, (B, W, H, cap, D), dtype) for _ in range(3)]
+    check_reorder(x, p, count=n, axis=3, out=o)
+    y = [t.reshape(B, W, H, cap * D) for t in x]
+    check_reorder(y, p, count=n, axis=2, out=None if o is None else [t.reshape(B, W, H, cap * D) for t in o])
+
+
+def test_reorder_views_and_offsets():
+    # strided queries, beams and rows; a row start at every byte; the rest of the buffers untouched
+    note("views")
+    g = torch.Generator().manual_seed(5)
+    big = ints(g, (4, 6, 3, 5, 40), torch.uint8)
+    p = torch.tensor([[2, 0, 0, 1], [3, 2, 1, 0]], dtype=torch.int32)
+    for off in (0, 1, 2, 4, 8, 16):
+        ref = big.clone()
+        x = ref[::2, 1:5, :, :3, off:off + 24]     # dims after the beams: rows of 24 bytes, 40 apart
+        x = x[:, :, :, 1]                          # [2][4][3][24], one row stride
+        want = big.cpu().clone()
+        v = want[::2, 1:5, :, :3, off:off + 24][:, :, :, 1]
+        v.copy_(torch.from_numpy(beam.beam_reorder(v.clone().numpy(), v.clone().numpy(), p.numpy(),
+                                                   [20, 24], 3)))
+        hs.beam_reorder(x, p.cuda(), count=torch.tensor([20, 24], dtype=torch.int32).cuda(), axis=3)
+        assert torch.equal(ref.cpu(), want), off
+    wide = torch.zeros((2, 10), dtype=torch.int32)  # the first beams of more slots
+    wide[:, :4] = p
+    y = ints(g, (2, 4, 9))
+    got = hs.beam_reorder(y.clone(), wide.cuda()[:, :4])[0]
+    assert np.array_equal(got.cpu().numpy(), beam.beam_reorder(y.cpu().numpy(), y.cpu().numpy(), p.numpy()))
+
+
+def test_reorder_many_tensors_of_mixed_widths():
+    note("many tensors")
+    g = torch.Generator().manual_seed(7)
+    B, W = 2, 6
+    kinds = [((64,), torch.float32), ((3,), torch.float32), ((5,), torch.uint8), ((16, 8), torch.int16)]
+    x = []
+    for i in range(75):
+        shape, dt = kinds[i % 4]
+        x.append(ints(g, (B, W) + shape, dt if dt != torch.float32 else torch.int32))
+    x.append(torch.zeros((B, W, 0), device="cuda"))  # nothing to move
+    p = torch.randint(0, W, (B, W), generator=g, dtype=torch.int32)
+    check_reorder(x, p)
+
+
+def test_reorder_offsets_past_32_bits():
+    note("long caches")
+    gib = 1 << 30
+    x = torch.zeros((1, 3, 3 * gib + 64), dtype=torch.uint8, device="cuda")
+    x[0, 0, -64:], x[0, 1, -64:], x[0, 2, -64:] = 1, 2, 3
+    hs.beam_reorder(x, torch.tensor([[2, 0, 1]], dtype=torch.int32).cuda())
+    assert x[0, :, -1].tolist() == [3, 1, 2] and x[0, :, -65].tolist() == [0, 0, 0]
+    n = torch.tensor([3 * gib], dtype=torch.int32).cuda() if 3 * gib < 2 ** 31 else None
+    assert n is None  # a count is 32 bits: units of two bytes below
+    y = x.view(torch.int16)
+    c = torch.tensor([y.shape[2] - 1], dtype=torch.int32).cuda()
+    hs.beam_reorder(y, torch.tensor([[1, 1, 1]], dtype=torch.int32).cuda(), count=c, axis=2)
+    assert x[0, :, -3].tolist() == [1, 1, 1] and x[0, :, -1].tolist() == [3, 1, 2]
+
+
+def test_reorder_on_another_stream_and_in_a_graph():
+    note("reorder stream and graph")
+    g = torch.Generator().manual_seed(9)
+    x = ints(g, (2, 5, 700))
+    p = torch.randint(0, 5, (2, 5), generator=g, dtype=torch.int32)
+    buf, pd = x.clone(), p.cuda()
+    plan = hs.BeamReorder(buf, pd)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    plan.run(stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    want = beam.beam_reorder(x.cpu().numpy(), x.cpu().numpy(), p.numpy())
+    assert np.array_equal(buf.cpu().numpy(), want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        plan.run()
+    for _ in range(3):
+        q = torch.randint(0, 5, (2, 5), generator=g, dtype=torch.int32)
+        pd.copy_(q)
+        want = beam.beam_reorder(buf.cpu().numpy(), buf.cpu().numpy(), q.numpy())
+        graph.replay()
+        torch.cuda.synchronize()
+        assert np.array_equal(buf.cpu().numpy(), want)
+
+
+# ---- hs_draft_tree -----------------------------------------------------------------------------------
+
+def grown(rng, D, B, K, W, ties=False, empty=0.1):
+    score = np.full((D, B, K), -np.inf, np.float32)
+    parent = np.full((D, B, K), -1, np.int32)
+    token = rng.integers(0, 151936, (D, B, K)).astype(np.int32)
+    for d in range(D):
+        for b in range(B):
+            p = rng.integers(0, 1 if d == 0 else W, K)
+            up = np.zeros(K, np.float32) if d == 0 else score[d - 1, b, p]
+            step = rng.integers(0, 3, K) if ties else rng.exponential(0.7, K)
+            s = (up - step).astype(np.float32)
+            order = np.argsort(-np.where(np.isnan(s), -np.inf, s), kind="stable")
+            score[d, b], parent[d, b] = s[order], p[order]
+    hole = rng.random((D, B, K)) < empty
+    score[hole] = -np.inf
+    parent[hole] = -1
+    token[hole] = -1
+    return score, parent, token
+
+
+def check_tree(score, parent, token, M):
+    out = hs.draft_tree(torch.from_numpy(score).cuda(), torch.from_numpy(parent).cuda(),
+                        torch.from_numpy(token).cuda(), M)
+    torch.cuda.synchronize()
+    ref = beam.draft_tree(score, parent, token, M)
+    for k, v in out.items():
+        got = v.cpu().numpy()
+        assert np.array_equal(got.view(np.uint64) if k == "mask" else got, ref[k]), k
+
+
+@pytest.mark.parametrize("D,K,M", [(1, 1, 2), (1, 64, 64), (7, 10, 61), (32, 64, 64), (32, 1, 64),
+                                   (5, 3, 64), (6, 13, 2), (9, 40, 33)])
+@pytest.mark.parametrize("ties", [False, True])
+def test_tree_matches_oracle(D, K, M, ties):
+    note("tree D=%d K=%d M=%d ties=%s" % (D, K, M, ties))
+    rng = np.random.default_rng(D * 100 + K + M)
+    check_tree(*grown(rng, D, 5, K, max(1, K // 2), ties=ties), M)
+
+
+def test_tree_of_odd_scores_and_parents():
+    # scores that rise along a path, NaN and infinities, parents that are empty or no slot
+    note("odd trees")
+    rng = np.random.default_rng(3)
+    D, B, K = 6, 8, 12
+    score = rng.normal(size=(D, B, K)).astype(np.float32)
+    score[rng.random((D, B, K)) < 0.1] = np.nan
+    score[rng.random((D, B, K)) < 0.1] = np.inf
+    score[rng.random((D, B, K)) < 0.1] = -np.inf
+    score[rng.random((D, B, K)) < 0.1] = -0.0
+    parent = rng.integers(-2, K + 3, (D, B, K)).astype(np.int32)
+    parent[:, 3] = -1                              # a query that grew nothing
+    parent[0, 5] = 7                               # of the first step every parent is the root
+    token = rng.integers(0, 1000, (D, B, K)).astype(np.int32)
+    for M in (2, 20, 64):
+        check_tree(score, parent, token, M)
+
+
+def test_tree_outputs_are_optional_and_guarded():
+    note("tree guards")
+    rng = np.random.default_rng(4)
+    s, p, t = (torch.from_numpy(v).cuda() for v in grown(rng, 4, 3, 9, 5))
+    full = hs.draft_tree(s, p, t, 17)
+    a = hs.hs_tree_args(s.data_ptr(), p.data_ptr(), t.data_ptr(), 4, 3, 9, 17)
+    bits = torch.full((5, 17), -7, dtype=torch.int64, device="cuda")
+    a.node_mask = bits[1:4].data_ptr()
+    hs._launch(hs.load_library().hs_draft_tree, s.device, None, hs.ctypes.byref(a))
+    torch.cuda.synchronize()
+    assert torch.equal(bits[1:4], full["mask"]) and torch.all(bits[0] == -7) and torch.all(bits[4] == -7)
+
+
+def test_tree_in_a_graph():
+    note("tree graph")
+    rng = np.random.default_rng(6)
+    s, p, t = (torch.from_numpy(v).cuda() for v in grown(rng, 5, 4, 8, 4))
+    plan = hs.DraftTree(s, p, t, 20)
+    graph = torch.cuda.CUDAGraph()
+    plan.run()
+    with torch.cuda.graph(graph):
+        plan.run()
+    for seed in range(3):
+        new = grown(np.random.default_rng(seed), 5, 4, 8, 4)
+        for d, v in zip((s, p, t), new):
+            d.copy_(torch.from_numpy(v))
+        graph.replay()
+        torch.cuda.synchronize()
+        ref = beam.draft_tree(*new, 20)
+        for k, v in plan.out.items():
+            got = v.cpu().numpy()
+            assert np.array_equal(got.view(np.uint64) if k == "mask" else got, ref[k]), k
+
+
+# ---- together ----------------------------------------------------------------------------------------
+
+def test_growing_a_draft_tree_and_its_mass():
+    """A drafter whose next logits depend on its hidden state grows a tree; the states follow the
+    beams, the kept nodes become candidate sets, and the target's mass on them is Theorem 2's."""
+    note("growth")
+    g = torch.Generator().manual_seed(47)
+    B, depth, W, K, M, V, C = 3, 5, 4, 12, 20, 2000, 16
+    head = (torch.randn((C, V), generator=g) * 1.5).cuda()
+    emb = torch.randn((V, C), generator=g).cuda()
+    h0 = torch.randn((B, C), generator=g).cuda()
+
+    def logits(hidden):
+        return (hidden @ head).to(torch.bfloat16)
+
+    def after(hidden, token):
+        return torch.tanh(0.5 * hidden + emb[token.long().clamp(min=0)])
+
+    hidden = torch.zeros((B, W, C), device="cuda")
+    growth = hs.TreeGrowth(B, depth, W, K, M, states=[hidden], temperature=0.8, device="cuda")
+    for _ in range(2):  # the second tree reuses every plan
+        hidden[:, 0] = h0
+        ref_h, ref_score, steps = h0[:, None].clone(), torch.zeros((B, 1)), []
+        for d in range(depth):
+            x = logits(hidden[:, :1] if d == 0 else hidden)
+            assert torch.equal(x, logits(ref_h))   # the states followed their beams
+            token = growth.level(x)
+            ref = beam.beam_step(x.cpu().double().numpy(), ref_score.numpy(), K, T=0.8)
+            same_step({"score": growth.score[d].cpu().numpy(), "parent": growth.parent[d].cpu().numpy(),
+                       "token": growth.token[d].cpu().numpy()}, ref)
+            steps.append(ref)
+            ref_score = growth.score[d][:, :W].cpu()
+            up = torch.from_numpy(ref["parent"][:, :W]).long().cuda()
+            ref_h = after(ref_h[torch.arange(B, device="cuda")[:, None], up],
+                          torch.from_numpy(ref["token"][:, :W]).cuda())
+            if d < depth - 1:
+                hidden.copy_(after(hidden, token))
+        tree = growth.tree()
+        want = beam.draft_tree(growth.score.cpu().numpy(), np.stack([s["parent"] for s in steps]),
+                               np.stack([s["token"] for s in steps]), M)
+        for k, v in tree.items():
+            got = v.cpu().numpy()
+            assert np.array_equal(got.view(np.uint64) if k == "mask" else got, want[k]), k
+    target = (torch.randn((B, M, V), generator=g) * 3).to(torch.bfloat16).cuda()
+    _, lse, _ = hs.softmax_stats(target.view(B * M, V), temperature=0.8)
+    gamma = hs.candidate_mass(target, lse.view(B, M), tree["cand"][:, None], temperature=0.8)
+    p = torch.softmax(target.double() / 0.8, 2).cpu().numpy()
+    for b in range(B):
+        for n in range(M):
+            kids = want["cand"][b, n]
+            mass = p[b, n, kids[kids >= 0]].sum()
+            assert abs(gamma[b, 0, n].item() - mass) <= 2e-5
+
+
+def test_beam_search_with_ends_and_histories():
+    """A whole beam search: step, token histories and caches moved in place, ends carried, against the
+    same search in fp64."""
+    note("beam search")
+    g = torch.Generator().manual_seed(53)
+    B, W, V, steps, eos = 2, 5, 600, 12, 0
+    table = torch.randn((V, V), generator=g) * 2.0
+    table[:, eos] += 3.0                            # ends come often
+    td = table.cuda()
+    first = torch.randint(0, V, (B,), generator=g)
+    hist = torch.full((B, W, steps), -1, dtype=torch.int32, device="cuda")
+    score = torch.full((B, W), float("-inf"))
+    score[:, 0] = 0.0                               # one live beam
+    done = torch.zeros((B, W), dtype=torch.uint8)
+    sd, dd = score.cuda(), done.cuda()
+    last = first[:, None].expand(B, W).cuda()
+    ref_hist = [[[] for _ in range(W)] for _ in range(B)]
+    ref_last = first[:, None].expand(B, W).numpy()
+    ref_done = done.numpy()
+    for t in range(steps):
+        x = td[last]
+        plan = hs.BeamStep(x, sd, W, done=dd, eos=eos, out={"score": sd, "done": dd})
+        ref = beam.beam_step(table.double().numpy()[ref_last], sd.cpu().numpy(), W, done=ref_done, eos=eos)
+        out = plan.run()
+        same_step({k: v.cpu().numpy() for k, v in out.items()}, ref)
+        hs.beam_reorder(hist, out["parent"], count=torch.full((B,), t, dtype=torch.int32, device="cuda"),
+                        axis=2)
+        hist[:, :, t] = out["token"]
+        last = out["token"].long()
+        ref_hist = [[ref_hist[b][ref["parent"][b, j]] + [int(ref["token"][b, j])] for j in range(W)]
+                    for b in range(B)]
+        ref_last, ref_done = ref["token"], ref["done"]
+    assert hist.cpu().tolist() == ref_hist
+    assert ref_done.any()
