@@ -8,11 +8,10 @@ namespace hs {
 
 // ---- launches (host side, defined next to their kernels) ----------------------------------------
 
-// How a step's rows are cut: slices of `chunks` chunks of kBeamChunk vectors, one wave each.
-constexpr int kBeamChunk = 256;       // 16-byte vectors of a chunk, four per lane
-constexpr int kBeamMaxSlices = 128;   // slices of a row
+// How a step's rows are cut: nc chunks of kBeamChunk vectors, in S slices of `chunks`, one wave each.
+constexpr int kBeamChunk = 256;  // 16-byte vectors of a chunk, four per lane
 struct BeamGeom {
-  int B, W, K, S, chunks;
+  int B, W, K, S, chunks, nc;
   int64_t V, nvec;
   int dtype;
 };
@@ -83,19 +82,63 @@ __device__ inline uint64_t nth_largest(const uint64_t (&u)[NU], int nu, int n) {
   return x;
 }
 
-// How many of list[0 .. n) exceed `mine`, n <= 64 the same in every lane; list is 16-byte aligned in
-// LDS and holds zeros from n up to the next multiple of 16.
-__device__ inline int count_above(const uint64_t* list, int n, uint64_t mine) {
-  typedef unsigned long long u2 __attribute__((ext_vector_type(2)));
-  int r = 0;
-  for (int c = 0; c < n; c += 16) {
-    u2 v[8];
+// The same of 32-bit keys.
+template <int NU>
+__device__ inline uint32_t nth_largest32(const uint32_t (&u)[NU], int nu, int n) {
+  uint32_t some = 0, lack = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const u2*>(list + c + 2 * i);
+  for (int j = 0; j < NU; ++j)
+    if (j < nu && u[j] != 0) {
+      some |= u[j];
+      lack |= ~u[j];
+    }
+  some = wave_or_bits(some);
+  uint32_t open = some & wave_or_bits(lack);
+  uint32_t x = some & ~open;
+  while (open) {
+    const uint32_t bit = 1u << (31 - __builtin_clz(open));
+    open &= ~bit;
+    int c = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r += (v[i][0] > mine ? 1 : 0) + (v[i][1] > mine ? 1 : 0);
+    for (int j = 0; j < NU; ++j)
+      if (j < nu) c += __builtin_popcountll(__ballot(u[j] >= (x | bit)));
+    if (c >= n) x |= bit;
   }
-  return r;
+  // fewer than n keys: no bound
+  int c = 0;
+#pragma unroll
+  for (int j = 0; j < NU; ++j)
+    if (j < nu) c += __builtin_popcountll(__ballot(u[j] != 0));
+  return c >= n ? x : 0;
+}
+
+// Sum and maximum of one fp64 value per lane, the same in every lane.
+template <int CTRL>
+__device__ inline double dpp_d(double v) {
+  const uint64_t x = (uint64_t)__double_as_longlong(v);
+  const uint32_t lo = (uint32_t)dpp_i<CTRL>((int)(uint32_t)x);
+  const uint32_t hi = (uint32_t)dpp_i<CTRL>((int)(uint32_t)(x >> 32));
+  return __longlong_as_double((long long)(((uint64_t)hi << 32) | lo));
+}
+__device__ inline double lane_d(double v, int l) {
+  const uint64_t x = (uint64_t)__double_as_longlong(v);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, l);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(x >> 32), l);
+  return __longlong_as_double((long long)(((uint64_t)hi << 32) | lo));
+}
+__device__ inline double wave_sum_d(double v) {
+  v += dpp_d<0xB1>(v);
+  v += dpp_d<0x4E>(v);
+  v += dpp_d<0x141>(v);
+  v += dpp_d<0x140>(v);
+  return (lane_d(v, 0) + lane_d(v, 16)) + (lane_d(v, 32) + lane_d(v, 48));
+}
+__device__ inline double wave_max_d(double v) {
+  v = fmax(v, dpp_d<0xB1>(v));
+  v = fmax(v, dpp_d<0x4E>(v));
+  v = fmax(v, dpp_d<0x141>(v));
+  v = fmax(v, dpp_d<0x140>(v));
+  return fmax(fmax(lane_d(v, 0), lane_d(v, 16)), fmax(lane_d(v, 32), lane_d(v, 48)));
 }
 
 // An fp32 value (no NaN) as an unsigned integer that orders like it, -0 as +0, and back (0 as +0).
