@@ -112,6 +112,25 @@ __device__ inline uint32_t nth_largest32(const uint32_t (&u)[NU], int nu, int n)
   return c >= n ? x : 0;
 }
 
+__device__ inline uint32_t wave_max_u(uint32_t x) {
+  x = max(x, (uint32_t)dpp_i<0xB1>((int)x));
+  x = max(x, (uint32_t)dpp_i<0x4E>((int)x));
+  x = max(x, (uint32_t)dpp_i<0x141>((int)x));
+  x = max(x, (uint32_t)dpp_i<0x140>((int)x));
+  return max(max((uint32_t)__builtin_amdgcn_readlane((int)x, 0),
+                 (uint32_t)__builtin_amdgcn_readlane((int)x, 16)),
+             max((uint32_t)__builtin_amdgcn_readlane((int)x, 32),
+                 (uint32_t)__builtin_amdgcn_readlane((int)x, 48)));
+}
+__device__ inline int wave_sum_i(int x) {
+  x += dpp_i<0xB1>(x);
+  x += dpp_i<0x4E>(x);
+  x += dpp_i<0x141>(x);
+  x += dpp_i<0x140>(x);
+  return __builtin_amdgcn_readlane(x, 0) + __builtin_amdgcn_readlane(x, 16) +
+         __builtin_amdgcn_readlane(x, 32) + __builtin_amdgcn_readlane(x, 48);
+}
+
 // Sum and maximum of one fp64 value per lane, the same in every lane.
 template <int CTRL>
 __device__ inline double dpp_d(double v) {

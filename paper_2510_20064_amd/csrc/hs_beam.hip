@@ -19,15 +19,17 @@
 // Sums are relative to an offset near the slice's maximum, and a slice whose maximum is large
 // (|z c| > 4096) takes z - maximum first, so that logits of any size do, the lowest finite value
 // in every place included.
+#include <cfloat>
+
 #include "hs_beam.h"
 
 namespace hs {
 
 namespace {
 
-constexpr int kMergeThreads = 512;
+constexpr int kMergeThreads = 1024;
 constexpr int kMergeWaves = kMergeThreads / 64;
-constexpr int kPairs = 1024;     // entries of one query held in LDS
+constexpr int kPairs = 2048;     // entries of one query held in LDS, twice what a round can add
 constexpr int kTokenBits = 26;
 constexpr uint32_t kTokenMask = (1u << kTokenBits) - 1;
 
@@ -35,11 +37,6 @@ struct SliceRec {
   double sum;  // of 2^(z c - off) over the slice (not finite: a NaN or +inf logit)
   double off;  // -inf: no logit above -inf
 };
-struct ChunkRec {
-  float max;  // the chunk's largest logit
-  float ref;  // the logit that its exponents' offset came from
-};
-
 struct StepArgs {
   const char* x;
   int64_t sb, sw;  // bytes between queries and between beams
@@ -57,7 +54,7 @@ struct StepArgs {
   int32_t* out_token;
   uint8_t* out_done;
   SliceRec* rec;   // [B * W][S]
-  ChunkRec* top;   // [B * W][nc]
+  float* top;      // [B * W][nc]: the chunks' largest logits
 };
 
 // The offset of exponents z c - off, from a logit at or near the largest.
@@ -79,6 +76,11 @@ struct Offset {
     return fmaf(z, cb, fmaf(z, ca, -o));
   }
 };
+
+// 2^d; d is a whole number between small offsets.
+__device__ inline double pow2(double d) {
+  return d == rint(d) ? ldexp(1.0, (int)fmax(d, -2000.0)) : exp2(d);
+}
 
 // A beam that continues by its logits: a finite score, and not finished.
 __device__ inline bool beam_grows(const StepArgs& A, int b, int w) {
@@ -123,12 +125,12 @@ __global__ __launch_bounds__(kThreads) void hs_beam_rows_kernel(StepArgs A) {
   if (!beam_grows(A, b, w)) return;
   const char* rowp = A.x + (int64_t)b * A.sb + (int64_t)w * A.sw;
   const int c0 = s * A.chunks, c1 = min(A.nc, c0 + A.chunks);
-  ChunkRec* top = A.top + (int64_t)row * A.nc;
   const float c = (float)A.c;
 
   Offset off(-INFINITY, c);
   bool any = false;   // an offset is set
   double sum = 0.0;   // the lane's
+  float mine = -INFINITY, mine_ref = -INFINITY;  // lane i: the slice's chunk i
   Raw cur[4], nxt[4];
   load_chunk<DT>(rowp, (int64_t)c0 * kBeamChunk, A.nvec, A.V, lane, cur);
   for (int k = c0; k < c1; ++k) {
@@ -175,105 +177,97 @@ __global__ __launch_bounds__(kThreads) void hs_beam_rows_kernel(StepArgs A) {
           acc[e & 3] += __builtin_amdgcn_exp2f(fmaf(z[i][e], A.cb, fmaf(z[i][e], A.ca, -off.o)));
     }
     sum += (double)((acc[0] + acc[1]) + (acc[2] + acc[3]));
-    if (lane == 0) top[k] = ChunkRec{m, off.ref};
+    if (lane == k - c0) {
+      mine = m;
+      mine_ref = off.ref;
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) cur[i] = nxt[i];
   }
+  if (any && mine > -INFINITY) {  // the chunks' largest terms, from fp32 to fp64
+    const Offset at(mine_ref, c);
+    sum += (exp2((double)mine * A.c - at.value(A.c)) -
+            (double)__builtin_amdgcn_exp2f(at.exponent(mine, A.ca, A.cb))) *
+           pow2(at.value(A.c) - off.value(A.c));
+  }
   sum = wave_sum_d(sum);
+  if (lane < c1 - c0) A.top[(int64_t)row * A.nc + c0 + lane] = mine;
   if (lane == 0) A.rec[u] = SliceRec{sum, any ? off.value(A.c) : -(double)INFINITY};
 }
 
 // ---- launch 2: the rows' normalisers and the K best ------------------------------------------------------
 
-// The K best of C <= kPairs pairs to the front of (hi, lo), best first; how many there are. One wave.
-__device__ __noinline__ int keep_best_pairs(uint64_t* hi, uint64_t* lo, int C, int K, int lane) {
-  constexpr int NU = kPairs / 64;
-  lds_wave_fence();
-  if (C > 64) {
-    uint64_t h[NU], l[NU];
-    const int nu = (C + 63) / 64;
-#pragma unroll
-    for (int j = 0; j < NU; ++j) {
-      const int i = j * 64 + lane;
-      h[j] = i < C ? hi[i] : 0;
-      l[j] = i < C ? lo[i] : 0;
-    }
-    const uint64_t x = nth_largest(h, nu, K);
-    int above = 0, equal = 0;
-#pragma unroll
-    for (int j = 0; j < NU; ++j) {
-      above += __builtin_popcountll(__ballot(h[j] > x));
-      equal += __builtin_popcountll(__ballot(h[j] != 0 && h[j] == x));
-    }
-    uint64_t y = 0;
-    if (above + equal > K) {  // ties at the K-th: the second words decide
-      uint64_t t[NU];
-#pragma unroll
-      for (int j = 0; j < NU; ++j) t[j] = h[j] != 0 && h[j] == x ? l[j] : 0;
-      y = nth_largest(t, nu, K - above);
-    }
-    lds_wave_fence();
-    C = 0;
-#pragma unroll
-    for (int j = 0; j < NU; ++j) {
-      const bool win = h[j] > x || (h[j] != 0 && h[j] == x && l[j] >= y);
-      const uint64_t m = __ballot(win);
-      const int at = C + lanes_below(m);
-      if (win) {
-        hi[at] = h[j];
-        lo[at] = l[j];
-      }
-      C += __builtin_popcountll(m);
-    }
-    lds_wave_fence();
+// The n-th largest x >= 1 of C words in LDS, as nth_largest; `of` maps a place to its key (0: none).
+template <typename F>
+__device__ inline uint64_t nth_of(F of, int C, int n, int lane) {
+  uint64_t x = 0;
+  for (int bit = 63; bit >= 0; --bit) {
+    const uint64_t y = x | (1ull << bit);
+    int c = 0;
+    for (int i = 0; i < C; i += 64) c += __builtin_popcountll(__ballot(i + lane < C && of(i + lane) >= y));
+    if (c >= n) x = y;
   }
-  const uint64_t mh = lane < C ? hi[lane] : 0, ml = lane < C ? lo[lane] : 0;
-  int rank = 0;
-  for (int i = 0; i < C; ++i) {
-    const uint64_t oh = hi[i], ol = lo[i];
-    rank += oh > mh || (oh == mh && ol > ml) ? 1 : 0;
-  }
-  lds_wave_fence();
-  if (lane < C && rank < K) {
-    hi[rank] = mh;
-    lo[rank] = ml;
-  }
-  lds_wave_fence();
-  return min(C, K);
+  return x;
 }
 
-// Pairs of one workgroup in LDS. Calls of room() and settle() are made by all of its threads together.
+// The K best of C pairs, ordered by h, then l, to the front in no order; *kth: the least h among them,
+// where there are K. One wave; rare (many equal scores).
+__device__ __noinline__ int keep_best(uint64_t* h, uint64_t* l, int C, int K, int lane, uint64_t* kth) {
+  lds_wave_fence();
+  if (C < K) return C;
+  const uint64_t x = nth_of([=](int i) { return h[i]; }, C, K, lane);
+  if (lane == 0) *kth = x;
+  int above = 0;
+  for (int i = 0; i < C; i += 64) above += __builtin_popcountll(__ballot(i + lane < C && h[i + lane] > x));
+  // ties at the K-th: the second words decide
+  const uint64_t y = nth_of([=](int i) { return h[i] == x ? l[i] : 0; }, C, K - above, lane);
+  int kept = 0;
+  for (int i = 0; i < C; i += 64) {
+    const uint64_t a = i + lane < C ? h[i + lane] : 0, c = i + lane < C ? l[i + lane] : 0;
+    const bool win = a > x || (a != 0 && a == x && c >= y);
+    const uint64_t m = __ballot(win);
+    lds_wave_fence();
+    if (win) {  // never past what has been read
+      h[kept + lanes_below(m)] = a;
+      l[kept + lanes_below(m)] = c;
+    }
+    lds_wave_fence();
+    kept += __builtin_popcountll(m);
+  }
+  return kept;
+}
+
+// Pairs of one workgroup in LDS, ordered by hi, then lo.
 struct PairList {
   uint64_t* hi;
   uint64_t* lo;
-  int* n;
-  // Space for `more` further pairs: where there may be none, only the K best are kept and *bound, if
-  // given, becomes the K-th.
-  __device__ void room(int more, int K, int wv, int lane, uint64_t* bound) {
-    __syncthreads();
-    const int have = *n;
-    __syncthreads();  // every wave has read it: the branch is the same for all
-    if (have + more > kPairs) {
-      if (wv == 0) {
-        const int C = keep_best_pairs(hi, lo, have, K, lane);
-        if (lane == 0) {
-          *n = C;
-          if (C == K) *bound = max(*bound, hi[K - 1]);
-        }
-      }
-      __syncthreads();
-    }
-  }
+  int* n;  // above kPairs: some found no room
+
   // A wave's lanes with `pass` add their pairs.
   __device__ void add(bool pass, uint64_t h, uint64_t l, int lane) {
     const uint64_t m = __ballot(pass);
     if (m == 0) return;
+    const int first = __builtin_ctzll(m);
     int at = 0;
-    if (lane == __builtin_ctzll(m)) at = atomicAdd(n, __builtin_popcountll(m));
-    at = __builtin_amdgcn_readlane(at, __builtin_ctzll(m)) + lanes_below(m);
-    if (pass) {
+    if (lane == first) at = atomicAdd(n, __builtin_popcountll(m));
+    at = __builtin_amdgcn_readlane(at, first) + lanes_below(m);
+    if (pass && at < kPairs) {
       hi[at] = h;
       lo[at] = l;
+    }
+  }
+  // Keeps the K best if there are more than `most`, and raises *bound to the K-th's hi. All threads of
+  // the workgroup together.
+  __device__ void shrink(int most, int K, int wv, int lane, uint64_t* bound) {
+    __syncthreads();
+    const int have = *n;
+    __syncthreads();  // every wave has read it: the branch is the same for all
+    if (have > most) {
+      if (wv == 0) {
+        const int C = keep_best(hi, lo, have, K, lane, bound);
+        if (lane == 0) *n = C;
+      }
+      __syncthreads();
     }
   }
 };
@@ -285,7 +279,7 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
   __shared__ double s_off[HS_MAX_BEAMS], s_lse[HS_MAX_BEAMS];  // a row's log2 normaliser: their sum
   __shared__ float s_score[HS_MAX_BEAMS];
   __shared__ uint8_t s_kind[HS_MAX_BEAMS];   // 0: gives nothing, 1: by its logits, 2: finished
-  __shared__ uint32_t s_group[256];
+  __shared__ __attribute__((aligned(16))) uint32_t s_group[128];
   __shared__ uint64_t s_chi[kPairs], s_clo[kPairs], s_hi[kPairs], s_lo[kPairs];
   __shared__ int s_rank[kPairs];
   __shared__ int s_chunks, s_count;
@@ -293,9 +287,8 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
   const int t = threadIdx.x, lane = t & 63;
   const int wv = __builtin_amdgcn_readfirstlane(t >> 6);
   const int b = blockIdx.x, W = A.W, S = A.S, K = A.K, nc = A.nc;
-  const ChunkRec* top = A.top + (int64_t)b * W * nc;
-  const float c32 = (float)A.c;
-  if (t < 256) s_group[t] = 0;
+  const float* top = A.top + (int64_t)b * W * nc;
+  if (t < 128) s_group[t] = 0;
   if (t == 0) s_chunks = s_count = 0;
   __syncthreads();
 
@@ -303,15 +296,20 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
     return ordered_of((double)s_score[w] +
                       (((double)z * A.c - s_off[w]) - s_lse[w]) * 0.69314718055994530942);
   };
-  // Groups of entries, each with its largest score's upper half: the K-th largest of them is a bound
-  // that K entries reach. 64 groups do while K is small against them.
-  const int groups = K <= 16 ? 64 : 256;
+  // Entries fall into groups, each with its largest score's upper half: the K-th largest of them is a
+  // bound that K entries reach. Of random scores 18 reach the 16th of 64 groups, and 89 the 64th of 128.
+  const int groups = K <= 16 ? 64 : 128;
 
   // the rows' normalisers, a wave a row, and the groups' largest chunks
   for (int w = wv; w < W; w += kMergeWaves) {
     const int64_t i = (int64_t)b * A.score_stride + w;
+    // every load first: a row that gives nothing has records of another call, which are not used
+    const SliceRec* rec = A.rec + ((int64_t)b * W + w) * S;
+    const SliceRec r0 = rec[min(lane, S - 1)], r1 = rec[min(lane + 64, S - 1)];
+    const float m0 = top[w * nc + min(lane, nc - 1)], m1 = top[w * nc + min(lane + 64, nc - 1)];
     const float sc = A.score[i];
-    const int kind = !isfinite(sc) ? 0 : A.done && A.done[i] ? 2 : 1;
+    const bool over = A.done && A.done[i];
+    const int kind = !isfinite(sc) ? 0 : over ? 2 : 1;
     if (kind != 1) {
       if (lane == 0) {
         s_score[w] = sc;
@@ -321,24 +319,14 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
       }
       continue;
     }
-    const SliceRec* rec = A.rec + ((int64_t)b * W + w) * S;
-    double o = -INFINITY;
-    for (int s = lane; s < S; s += 64) o = fmax(o, rec[s].off);
+    double o = fmax(r0.off, r1.off);
+    for (int s = lane + 128; s < S; s += 64) o = fmax(o, rec[s].off);
     o = wave_max_d(o);
+    auto part = [&](const SliceRec& r) { return r.off == -INFINITY ? r.sum : r.sum * pow2(r.off - o); };
     double sum = 0.0;
-    for (int s = lane; s < S; s += 64) {
-      const SliceRec r = rec[s];
-      sum += r.off == -INFINITY ? r.sum : r.sum * exp2(r.off - o);
-    }
-    for (int k = lane; k < nc; k += 64) {  // the chunks' largest terms, from fp32 to fp64
-      const ChunkRec r = top[w * nc + k];
-      const Offset off(r.ref, c32);
-      const double by = off.value(A.c) - o;
-      const float e = off.exponent(r.max, A.ca, A.cb);
-      if (by + e > -20.0)  // below, what this corrects is under 1e-13 of the sum
-        sum += (exp2((double)r.max * A.c - off.value(A.c)) - (double)__builtin_amdgcn_exp2f(e)) *
-               exp2(by);
-    }
+    if (lane < S) sum += part(r0);
+    if (lane + 64 < S) sum += part(r1);
+    for (int s = lane + 128; s < S; s += 64) sum += part(rec[s]);
     sum = wave_sum_d(sum);
     const bool live = isfinite(sum) && sum > 0.0;
     const double lg = log2(sum);
@@ -351,125 +339,142 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
     lds_wave_fence();
     if (live)
       for (int k = lane; k < nc; k += 64) {
-        const float m = top[w * nc + k].max;
+        const float m = k < 64 ? m0 : k < 128 ? m1 : top[w * nc + k];
         if (m > -INFINITY)
           atomicMax(&s_group[(w * nc + k) & (groups - 1)], (uint32_t)(score_of(w, m) >> 32));
       }
   }
   __syncthreads();
-  uint64_t bound;
+  uint64_t bound;  // the smallest group that fewer than K exceed; 0 (none) with fewer than K groups
   {
-    uint32_t u[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) u[j] = j * 64 < groups ? s_group[j * 64 + lane] : 0;
-    bound = (uint64_t)nth_largest32(u, groups / 64, K) << 32;
+    uint32_t least = 0xFFFFFFFFu;
+    for (int j = 0; j < groups; j += 64) {
+      const uint32_t mine = s_group[j + lane];
+      typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+      int above = 0;
+#pragma unroll 8
+      for (int i = 0; i < groups; i += 4) {
+        const u4 v = *reinterpret_cast<const u4*>(s_group + i);
+        above += (v[0] > mine ? 1 : 0) + (v[1] > mine ? 1 : 0) + (v[2] > mine ? 1 : 0) +
+                 (v[3] > mine ? 1 : 0);
+      }
+      if (above < K) least = min(least, mine);
+    }
+    bound = (uint64_t)~wave_max_u(~least) << 32;
   }
   if (t == 0) s_bound = bound;
 
-  // the chunks that reach it
+  // the chunks that reach it; a second time, keeping only the K first by (s, lower beam, lower chunk)
+  // on the way, if they are too many (equal maxima): their maxima all come before any other chunk's
   PairList chunks{s_chi, s_clo, &s_chunks};
-  for (int i0 = 0; i0 < W * nc; i0 += kMergeThreads) {
-    if (W * nc > kPairs) {
-      chunks.room(kMergeThreads, K, wv, lane, &s_bound);
-      bound = s_bound;
-    }
-    const int i = i0 + t;
-    bool pass = false;
-    uint64_t h = 0, l = 0;
-    if (i < W * nc) {
-      const int w = (int)fdiv((uint32_t)i, A.divC), k = i - w * nc;
-      if (s_kind[w] == 1) {
-        const float m = top[i].max;
-        if (m > -INFINITY) {
-          h = score_of(w, m);
-          l = ((uint64_t)(63 - w) << 32) | (uint64_t)(0xFFFFFFFFu - (uint32_t)k);
-          pass = h >= bound;
+  for (int slow = 0; slow < 2; ++slow) {
+    for (int i0 = 0; i0 < W * nc; i0 += kMergeThreads) {
+      if (slow) {
+        chunks.shrink(kPairs - kMergeThreads, K, wv, lane, &s_bound);
+        bound = s_bound;
+      }
+      const int i = i0 + t;
+      bool pass = false;
+      uint64_t h = 0, l = 0;
+      if (i < W * nc) {
+        const int w = (int)fdiv((uint32_t)i, A.divC), k = i - w * nc;
+        if (s_kind[w] == 1) {
+          const float m = top[i];
+          if (m > -INFINITY) {
+            h = score_of(w, m);
+            l = ((uint64_t)(63 - w) << 32) | (uint64_t)(0xFFFFFFFFu - (uint32_t)k);
+            pass = h >= bound;
+          }
         }
       }
-    }
-    chunks.add(pass, h, l, lane);
-  }
-  // more than K of them (equal maxima): the K first by (s, lower beam, lower chunk) are enough, since
-  // their maxima all come before any other chunk's
-  __syncthreads();
-  const int found = s_chunks;
-  __syncthreads();
-  int n = found;
-  if (found > 2 * K + 64) {
-    if (wv == 0) {
-      n = keep_best_pairs(s_chi, s_clo, found, K, lane);
-      if (lane == 0) {
-        s_chunks = n;
-        if (n == K) s_bound = max(s_bound, s_chi[K - 1]);
-      }
+      chunks.add(pass, h, l, lane);
     }
     __syncthreads();
-    n = s_chunks;
+    const bool room = s_chunks <= kPairs;
+    __syncthreads();
+    if (room) break;
+    if (t == 0) s_chunks = 0;
+    __syncthreads();
   }
+  chunks.shrink(2 * K + 64, K, wv, lane, &s_bound);
+  const int n = s_chunks;
   bound = s_bound;
 
-  // their entries, and the finished beams
+  // their entries, and the finished beams; again in two ways
   PairList best{s_hi, s_lo, &s_count};
-  if (wv == 0) {
-    const bool over = lane < W && s_kind[lane] == 2;
-    const uint64_t h = over ? ordered_of((double)s_score[lane]) : 0;
-    best.add(over && h >= bound, h, ((uint64_t)(63 - lane) << 58) | kTokenMask, lane);
-  }
-  for (int i0 = 0; i0 < n; i0 += kMergeWaves) {
-    if ((n + kMergeWaves) * 64 > kPairs) {
-      best.room(kMergeWaves * 64, K, wv, lane, &s_bound);
-      bound = s_bound;
-    }
-    const int i = i0 + wv;
-    if (i >= n) continue;
-    const int w = 63 - (int)(s_clo[i] >> 32);
-    const int k = (int)(0xFFFFFFFFu - (uint32_t)s_clo[i]);
-    typename Vt::Raw x[4];
-    load_chunk<DT>(A.x + (int64_t)b * A.sb + (int64_t)w * A.sw, (int64_t)k * kBeamChunk, A.nvec, A.V,
-                   lane, x);
-    // a logit that every entry reaching the bound exceeds; the chunk's largest does in any case
-    const double at = ((value_of(bound) - (double)s_score[w]) * 1.4426950408889634074 + s_lse[w] +
-                       s_off[w]) / A.c;
-    const double slack = 1e-6 * (fabs(at) + fabs((double)s_score[w] / A.c) + fabs(s_off[w] / A.c));
-    const float zmax = top[w * nc + k].max;
-    const float least = bound == 0 ? -INFINITY : fminf((float)(at - slack), zmax);
-    float z[4][E];
-    uint64_t key[4 * E];  // (s needs only the logit: keys order a chunk's entries)
-    int many = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      Vt::unpack(x[j], z[j]);
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const bool p = z[j][e] >= least && z[j][e] > -INFINITY;
-        many += __builtin_popcountll(__ballot(p));
-        key[j * E + e] = p ? ((uint64_t)ordered_of(z[j][e]) << kTokenBits) |
-                                 (kTokenMask - (uint32_t)((k * kBeamChunk + j * 64 + lane) * E + e))
-                           : 0;
-      }
-    }
-    const uint64_t cut = many > 64 ? nth_largest(key, 4 * E, min(K, 64)) : 1;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const uint64_t q = key[j * E + e];
-        if (__ballot(q >= cut) == 0) continue;
-        const uint64_t h = q >= cut ? score_of(w, z[j][e]) : 0;
-        best.add(h != 0 && h >= bound, h, ((uint64_t)(63 - w) << 58) | q, lane);
-      }
-  }
-  __syncthreads();
-  int C = s_count;
-  __syncthreads();
-  if (C > 256) {
+  for (int slow = 0; slow < 2; ++slow) {
     if (wv == 0) {
-      const int kept = keep_best_pairs(s_hi, s_lo, C, K, lane);
-      if (lane == 0) s_count = kept;
+      const bool over = lane < W && s_kind[lane] == 2;
+      const uint64_t h = over ? ordered_of((double)s_score[lane]) : 0;
+      best.add(over && h >= bound, h, ((uint64_t)(63 - lane) << 58) | kTokenMask, lane);
+    }
+    for (int i0 = 0; i0 < n; i0 += kMergeWaves) {
+      if (slow) {
+        best.shrink(kPairs - kMergeWaves * 64, K, wv, lane, &s_bound);
+        bound = s_bound;
+      }
+      const int i = i0 + wv;
+      if (i >= n) continue;
+      const int w = 63 - (int)uniform((uint32_t)(s_clo[i] >> 32));
+      const int k = (int)(0xFFFFFFFFu - uniform((uint32_t)s_clo[i]));
+      typename Vt::Raw x[4];
+      load_chunk<DT>(A.x + (int64_t)b * A.sb + (int64_t)w * A.sw, (int64_t)k * kBeamChunk, A.nvec, A.V,
+                     lane, x);
+      // a logit that every entry reaching the bound exceeds; the chunk's largest does in any case
+      const double at = ((value_of(bound) - (double)s_score[w]) * 1.4426950408889634074 + s_lse[w] +
+                         s_off[w]) / A.c;
+      const double slack = 1e-6 * (fabs(at) + fabs((double)s_score[w] / A.c) + fabs(s_off[w] / A.c));
+      const float least =
+          fmaxf(bound == 0 ? -FLT_MAX : fminf((float)(at - slack), top[w * nc + k]), -FLT_MAX);
+      float z[4 * E];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) Vt::unpack(x[j], z + j * E);
+      uint32_t pass = 0;  // of the lane's logits
+#pragma unroll
+      for (int j = 0; j < 4 * E; ++j) pass |= z[j] >= least ? 1u << j : 0u;
+      auto token_of = [&](int j) {
+        return (uint32_t)((k * kBeamChunk + (j / E) * 64 + lane) * E + j % E);
+      };
+      if (wave_sum_i(__builtin_popcount(pass)) > 64) {  // the chunk's K best: by logit, then by token
+        uint32_t u[4 * E];
+#pragma unroll
+        for (int j = 0; j < 4 * E; ++j) u[j] = (pass >> j) & 1 ? ordered_of(z[j]) : 0;
+        const uint32_t cut = nth_largest32(u, 4 * E, K);
+        int above = 0;
+#pragma unroll
+        for (int j = 0; j < 4 * E; ++j) above += __builtin_popcountll(__ballot(u[j] > cut));
+        uint32_t v[4 * E];
+#pragma unroll
+        for (int j = 0; j < 4 * E; ++j)
+          v[j] = u[j] != 0 && u[j] == cut ? kTokenMask - token_of(j) : 0;
+        const uint32_t last = nth_largest32(v, 4 * E, K - above);
+        pass = 0;
+#pragma unroll
+        for (int j = 0; j < 4 * E; ++j)
+          pass |= u[j] > cut || (v[j] != 0 && v[j] >= last) ? 1u << j : 0u;
+      }
+      while (__ballot(pass != 0)) {  // a lane's next entry; mostly there are one or two in a chunk
+        const bool has = pass != 0;
+        const int j = has ? __builtin_ctz(pass) : 0;
+        float y = z[0];
+#pragma unroll
+        for (int e = 1; e < 4 * E; ++e) y = j == e ? z[e] : y;
+        const uint64_t h = has ? score_of(w, y) : 0;
+        best.add(has && h >= bound, h,
+                 ((uint64_t)(63 - w) << 58) | ((uint64_t)ordered_of(y) << kTokenBits) |
+                     (uint64_t)(kTokenMask - token_of(j)), lane);
+        pass &= pass - 1;
+      }
     }
     __syncthreads();
-    C = s_count;
+    const bool room = s_count <= kPairs;
+    __syncthreads();
+    if (room) break;
+    if (t == 0) s_count = 0;
+    __syncthreads();
   }
+  best.shrink(256, K, wv, lane, &s_bound);
+  const int C = s_count;
   // every entry's rank: the waves compare it with a share of the others each
   for (int i = t; i < C; i += kMergeThreads) s_rank[i] = 0;
   __syncthreads();
@@ -531,14 +536,15 @@ bool beam_geom(int B, int W, int K, int64_t V, int dtype, BeamGeom* g) {
   if (g->nvec > (int64_t)kMaxTeamSlices * kThreads) return false;
   g->nc = (int)((g->nvec + kBeamChunk - 1) / kBeamChunk);
   const int64_t n = (int64_t)g->nc * B * W / 8192;
-  g->chunks = (int)(n < 1 ? 1 : n > g->nc ? g->nc : n);
+  const int most = g->nc < 64 ? g->nc : 64;  // a lane keeps each chunk's maximum
+  g->chunks = (int)(n < 1 ? 1 : n > most ? most : n);
   g->S = (g->nc + g->chunks - 1) / g->chunks;
   return true;
 }
 
 size_t beam_ws_bytes(const BeamGeom& g) {
   const size_t rows = (size_t)g.B * g.W;
-  return align256(rows * g.S * sizeof(SliceRec)) + align256(rows * g.nc * sizeof(ChunkRec));
+  return align256(rows * g.S * sizeof(SliceRec)) + align256(rows * g.nc * sizeof(float));
 }
 
 int launch_beam_step(const BeamGeom& g, const hs_beam_args& a, hipStream_t stream) {
@@ -577,7 +583,7 @@ int launch_beam_step(const BeamGeom& g, const hs_beam_args& a, hipStream_t strea
   A.out_done = a.out_done;
   char* ws = reinterpret_cast<char*>(a.workspace);
   A.rec = reinterpret_cast<SliceRec*>(ws);
-  A.top = reinterpret_cast<ChunkRec*>(ws + align256((size_t)A.units * sizeof(SliceRec)));
+  A.top = reinterpret_cast<float*>(ws + align256((size_t)A.units * sizeof(SliceRec)));
   if (g.dtype == HS_F32) launch_step<HS_F32>(A, g.B, stream);
   else if (g.dtype == HS_F16) launch_step<HS_F16>(A, g.B, stream);
   else launch_step<HS_BF16>(A, g.B, stream);
