@@ -82,46 +82,6 @@ __device__ inline uint64_t nth_largest(const uint64_t (&u)[NU], int nu, int n) {
   return x;
 }
 
-// The same of 32-bit keys.
-template <int NU>
-__device__ inline uint32_t nth_largest32(const uint32_t (&u)[NU], int nu, int n) {
-  uint32_t some = 0, lack = 0;
-#pragma unroll
-  for (int j = 0; j < NU; ++j)
-    if (j < nu && u[j] != 0) {
-      some |= u[j];
-      lack |= ~u[j];
-    }
-  some = wave_or_bits(some);
-  uint32_t open = some & wave_or_bits(lack);
-  uint32_t x = some & ~open;
-  while (open) {
-    const uint32_t bit = 1u << (31 - __builtin_clz(open));
-    open &= ~bit;
-    int c = 0;
-#pragma unroll
-    for (int j = 0; j < NU; ++j)
-      if (j < nu) c += __builtin_popcountll(__ballot(u[j] >= (x | bit)));
-    if (c >= n) x |= bit;
-  }
-  // fewer than n keys: no bound
-  int c = 0;
-#pragma unroll
-  for (int j = 0; j < NU; ++j)
-    if (j < nu) c += __builtin_popcountll(__ballot(u[j] != 0));
-  return c >= n ? x : 0;
-}
-
-__device__ inline uint32_t wave_max_u(uint32_t x) {
-  x = max(x, (uint32_t)dpp_i<0xB1>((int)x));
-  x = max(x, (uint32_t)dpp_i<0x4E>((int)x));
-  x = max(x, (uint32_t)dpp_i<0x141>((int)x));
-  x = max(x, (uint32_t)dpp_i<0x140>((int)x));
-  return max(max((uint32_t)__builtin_amdgcn_readlane((int)x, 0),
-                 (uint32_t)__builtin_amdgcn_readlane((int)x, 16)),
-             max((uint32_t)__builtin_amdgcn_readlane((int)x, 32),
-                 (uint32_t)__builtin_amdgcn_readlane((int)x, 48)));
-}
 __device__ inline int wave_sum_i(int x) {
   x += dpp_i<0xB1>(x);
   x += dpp_i<0x4E>(x);

@@ -29,6 +29,7 @@ namespace {
 
 constexpr int kMergeThreads = 1024;
 constexpr int kMergeWaves = kMergeThreads / 64;
+constexpr int kRows = HS_MAX_BEAMS / kMergeWaves;  // rows of a wave in the merge
 constexpr int kPairs = 2048;     // entries of one query held in LDS, twice what a round can add
 constexpr int kTokenBits = 26;
 constexpr uint32_t kTokenMask = (1u << kTokenBits) - 1;
@@ -45,7 +46,7 @@ struct StepArgs {
   uint32_t units;  // B * W * S
   FastDiv divS, divW, divC;  // by S, W and nc
   float ca, cb;
-  double c;
+  double c, inv_c;  // c and 1 / c
   const float* score;
   const uint8_t* done;
   int eos;
@@ -77,9 +78,30 @@ struct Offset {
   }
 };
 
-// 2^d; d is a whole number between small offsets.
-__device__ inline double pow2(double d) {
-  return d == rint(d) ? ldexp(1.0, (int)fmax(d, -2000.0)) : exp2(d);
+// x 2^d, d <= 0; a whole number between small offsets.
+__device__ inline double scaled(double x, double d) {
+  if (d == rint(d)) return ldexp(x, (int)fmax(d, -2000.0));
+  return x * exp2(d);
+}
+
+// log2 of a positive finite x to 1e-11: x = m 2^e with m near 1, log m = 2 artanh t, t = (m - 1) / (m + 1)
+// and |t| < 0.172. (A whole wave computes it for its row: a third of the instructions of log2().)
+__device__ inline double log2_of(double x) {
+  double m = __builtin_amdgcn_frexp_mant(x);
+  int e = __builtin_amdgcn_frexp_exp(x);
+  if (m < 0.70710678118654752440) {
+    m += m;
+    --e;
+  }
+  const double t = (m - 1.0) / (m + 1.0), q = t * t;
+  double p = 1.0 / 13.0;
+  p = fma(p, q, 1.0 / 11.0);
+  p = fma(p, q, 1.0 / 9.0);
+  p = fma(p, q, 1.0 / 7.0);
+  p = fma(p, q, 1.0 / 5.0);
+  p = fma(p, q, 1.0 / 3.0);
+  p = fma(p, q, 1.0);
+  return fma(2.0 * 1.4426950408889634074 * t, p, (double)e);
 }
 
 // A beam that continues by its logits: a finite score, and not finished.
@@ -186,9 +208,9 @@ __global__ __launch_bounds__(kThreads) void hs_beam_rows_kernel(StepArgs A) {
   }
   if (any && mine > -INFINITY) {  // the chunks' largest terms, from fp32 to fp64
     const Offset at(mine_ref, c);
-    sum += (exp2((double)mine * A.c - at.value(A.c)) -
-            (double)__builtin_amdgcn_exp2f(at.exponent(mine, A.ca, A.cb))) *
-           pow2(at.value(A.c) - off.value(A.c));
+    sum += scaled(exp2((double)mine * A.c - at.value(A.c)) -
+                      (double)__builtin_amdgcn_exp2f(at.exponent(mine, A.ca, A.cb)),
+                  at.value(A.c) - off.value(A.c));
   }
   sum = wave_sum_d(sum);
   if (lane < c1 - c0) A.top[(int64_t)row * A.nc + c0 + lane] = mine;
@@ -272,24 +294,77 @@ struct PairList {
   }
 };
 
+// The lanes with a logit >= least among their four vectors (for 16-bit logits: >= least cut to 16 bits,
+// for which positive values compare as integers); false where least is negative.
+template <int DT>
+__device__ inline bool lanes_with(const typename Vec<DT>::Raw (&x)[4], float least, uint64_t& hits) {
+  if (!(least > 0.0f)) return false;
+  if constexpr (DT == HS_F32) {
+    float m = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) m = fmaxf(fmaxf(m, fmaxf(x[j].x, x[j].y)), fmaxf(x[j].z, x[j].w));
+    hits = __ballot(m >= least);
+  } else {
+    typedef short s2 __attribute__((ext_vector_type(2)));
+    auto word = [](uint32_t u) { return __builtin_bit_cast(s2, u); };
+    s2 m = word(x[0].x);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      m = __builtin_elementwise_max(m, word(x[j].x));
+      m = __builtin_elementwise_max(m, word(x[j].y));
+      m = __builtin_elementwise_max(m, word(x[j].z));
+      m = __builtin_elementwise_max(m, word(x[j].w));
+    }
+    int16_t cut;
+    if constexpr (DT == HS_F16)
+      cut = (int16_t)(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(least, 0.0f)) & 0x7FFFu);
+    else
+      cut = (int16_t)(__float_as_uint(least) >> 16);
+    hits = __ballot(max(m[0], m[1]) >= cut);
+  }
+  return true;
+}
+
 template <int DT>
 __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A) {
   using Vt = Vec<DT>;
   constexpr int E = Vt::kElems;
+  constexpr int kHits = 64 / (4 * E);  // lanes whose logits a wave looks at together
   __shared__ double s_off[HS_MAX_BEAMS], s_lse[HS_MAX_BEAMS];  // a row's log2 normaliser: their sum
   __shared__ float s_score[HS_MAX_BEAMS];
   __shared__ uint8_t s_kind[HS_MAX_BEAMS];   // 0: gives nothing, 1: by its logits, 2: finished
   __shared__ __attribute__((aligned(16))) uint32_t s_group[128];
   __shared__ uint64_t s_chi[kPairs], s_clo[kPairs], s_hi[kPairs], s_lo[kPairs];
-  __shared__ int s_rank[kPairs];
+  __shared__ __attribute__((aligned(16))) char s_hit[kMergeWaves][kHits * 64];
   __shared__ int s_chunks, s_count;
   __shared__ uint64_t s_bound;
   const int t = threadIdx.x, lane = t & 63;
   const int wv = __builtin_amdgcn_readfirstlane(t >> 6);
   const int b = blockIdx.x, W = A.W, S = A.S, K = A.K, nc = A.nc;
   const float* top = A.top + (int64_t)b * W * nc;
+
+  // a wave's rows are w = wv + 16 r; every load first (a row that gives nothing has records of
+  // another call, which are not used)
+  SliceRec r0[kRows], r1[kRows];
+  float m0[kRows], m1[kRows], sc[kRows];
+  bool over[kRows];
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) {
+    const int w = wv + kMergeWaves * r;
+    if (w >= W) break;
+    const SliceRec* rec = A.rec + ((int64_t)b * W + w) * S;
+    r0[r] = rec[min(lane, S - 1)];
+    r1[r] = rec[min(lane + 64, S - 1)];
+    m0[r] = top[w * nc + min(lane, nc - 1)];
+    m1[r] = top[w * nc + min(lane + 64, nc - 1)];
+    sc[r] = A.score[(int64_t)b * A.score_stride + w];
+    over[r] = A.done && A.done[(int64_t)b * A.score_stride + w];
+  }
   if (t < 128) s_group[t] = 0;
-  if (t == 0) s_chunks = s_count = 0;
+  if (t == 0) {
+    s_chunks = s_count = 0;
+    s_bound = ~0ull;
+  }
   __syncthreads();
 
   auto score_of = [&](int w, float z) -> uint64_t {
@@ -300,38 +375,37 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
   // bound that K entries reach. Of random scores 18 reach the 16th of 64 groups, and 89 the 64th of 128.
   const int groups = K <= 16 ? 64 : 128;
 
-  // the rows' normalisers, a wave a row, and the groups' largest chunks
-  for (int w = wv; w < W; w += kMergeWaves) {
-    const int64_t i = (int64_t)b * A.score_stride + w;
-    // every load first: a row that gives nothing has records of another call, which are not used
-    const SliceRec* rec = A.rec + ((int64_t)b * W + w) * S;
-    const SliceRec r0 = rec[min(lane, S - 1)], r1 = rec[min(lane + 64, S - 1)];
-    const float m0 = top[w * nc + min(lane, nc - 1)], m1 = top[w * nc + min(lane + 64, nc - 1)];
-    const float sc = A.score[i];
-    const bool over = A.done && A.done[i];
-    const int kind = !isfinite(sc) ? 0 : over ? 2 : 1;
+  // the rows' normalisers, and the groups' largest chunks
+  uint64_t h0[kRows], h1[kRows];  // scores of the lane's first two chunks
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) {
+    h0[r] = h1[r] = 0;
+    const int w = wv + kMergeWaves * r;
+    if (w >= W) break;
+    const int kind = !isfinite(sc[r]) ? 0 : over[r] ? 2 : 1;
     if (kind != 1) {
       if (lane == 0) {
-        s_score[w] = sc;
+        s_score[w] = sc[r];
         s_kind[w] = (uint8_t)kind;
         if (kind == 2)
-          atomicMax(&s_group[w & (groups - 1)], (uint32_t)(ordered_of((double)sc) >> 32));
+          atomicMax(&s_group[w & (groups - 1)], (uint32_t)(ordered_of((double)sc[r]) >> 32));
       }
       continue;
     }
-    double o = fmax(r0.off, r1.off);
+    const SliceRec* rec = A.rec + ((int64_t)b * W + w) * S;
+    double o = fmax(r0[r].off, r1[r].off);
     for (int s = lane + 128; s < S; s += 64) o = fmax(o, rec[s].off);
     o = wave_max_d(o);
-    auto part = [&](const SliceRec& r) { return r.off == -INFINITY ? r.sum : r.sum * pow2(r.off - o); };
+    auto part = [&](const SliceRec& q) { return q.off == -INFINITY ? q.sum : scaled(q.sum, q.off - o); };
     double sum = 0.0;
-    if (lane < S) sum += part(r0);
-    if (lane + 64 < S) sum += part(r1);
+    if (lane < S) sum += part(r0[r]);
+    if (lane + 64 < S) sum += part(r1[r]);
     for (int s = lane + 128; s < S; s += 64) sum += part(rec[s]);
     sum = wave_sum_d(sum);
     const bool live = isfinite(sum) && sum > 0.0;
-    const double lg = log2(sum);
+    const double lg = log2_of(sum);
     if (lane == 0) {
-      s_score[w] = sc;
+      s_score[w] = sc[r];
       s_off[w] = o;
       s_lse[w] = lg;
       s_kind[w] = live ? 1 : 0;
@@ -339,62 +413,64 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
     lds_wave_fence();
     if (live)
       for (int k = lane; k < nc; k += 64) {
-        const float m = k < 64 ? m0 : k < 128 ? m1 : top[w * nc + k];
-        if (m > -INFINITY)
-          atomicMax(&s_group[(w * nc + k) & (groups - 1)], (uint32_t)(score_of(w, m) >> 32));
+        const float m = k < 64 ? m0[r] : k < 128 ? m1[r] : top[w * nc + k];
+        if (m > -INFINITY) {
+          const uint64_t h = score_of(w, m);
+          if (k < 64) h0[r] = h;
+          else if (k < 128) h1[r] = h;
+          atomicMax(&s_group[(w * nc + k) & (groups - 1)], (uint32_t)(h >> 32));
+        }
       }
   }
   __syncthreads();
-  uint64_t bound;  // the smallest group that fewer than K exceed; 0 (none) with fewer than K groups
+  // the smallest group that fewer than K exceed; 0 (no bound) with fewer than K groups. Each wave
+  // looks at its share of them
   {
+    const uint32_t g0 = s_group[lane], g1 = groups > 64 ? s_group[64 + lane] : 0;
     uint32_t least = 0xFFFFFFFFu;
-    for (int j = 0; j < groups; j += 64) {
-      const uint32_t mine = s_group[j + lane];
-      typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-      int above = 0;
-#pragma unroll 8
-      for (int i = 0; i < groups; i += 4) {
-        const u4 v = *reinterpret_cast<const u4*>(s_group + i);
-        above += (v[0] > mine ? 1 : 0) + (v[1] > mine ? 1 : 0) + (v[2] > mine ? 1 : 0) +
-                 (v[3] > mine ? 1 : 0);
-      }
-      if (above < K) least = min(least, mine);
+    for (int j = wv; j < groups; j += kMergeWaves) {
+      const uint32_t g = (uint32_t)__builtin_amdgcn_readlane((int)(j < 64 ? g0 : g1), j & 63);
+      const int above = __builtin_popcountll(__ballot(g0 > g)) + __builtin_popcountll(__ballot(g1 > g));
+      if (above < K) least = min(least, g);
     }
-    bound = (uint64_t)~wave_max_u(~least) << 32;
+    if (lane == 0) atomicMin((unsigned long long*)&s_bound, (unsigned long long)least << 32);
   }
-  if (t == 0) s_bound = bound;
+  __syncthreads();
+  uint64_t bound = s_bound;
 
   // the chunks that reach it; a second time, keeping only the K first by (s, lower beam, lower chunk)
   // on the way, if they are too many (equal maxima): their maxima all come before any other chunk's
   PairList chunks{s_chi, s_clo, &s_chunks};
-  for (int slow = 0; slow < 2; ++slow) {
-    for (int i0 = 0; i0 < W * nc; i0 += kMergeThreads) {
-      if (slow) {
-        chunks.shrink(kPairs - kMergeThreads, K, wv, lane, &s_bound);
-        bound = s_bound;
+  auto place = [](int w, int k) {
+    return ((uint64_t)(63 - w) << 32) | (uint64_t)(0xFFFFFFFFu - (uint32_t)k);
+  };
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) {
+    const int w = wv + kMergeWaves * r;
+    if (w >= W) break;
+    chunks.add(h0[r] != 0 && h0[r] >= bound, h0[r], place(w, lane), lane);
+    if (nc > 64) chunks.add(h1[r] != 0 && h1[r] >= bound, h1[r], place(w, lane + 64), lane);
+    if (nc > 128 && s_kind[w] == 1)
+      for (int k0 = 128; k0 < nc; k0 += 64) {
+        const float m = k0 + lane < nc ? top[w * nc + k0 + lane] : -INFINITY;
+        const uint64_t h = m > -INFINITY ? score_of(w, m) : 0;
+        chunks.add(h != 0 && h >= bound, h, place(w, k0 + lane), lane);
       }
-      const int i = i0 + t;
-      bool pass = false;
-      uint64_t h = 0, l = 0;
-      if (i < W * nc) {
-        const int w = (int)fdiv((uint32_t)i, A.divC), k = i - w * nc;
-        if (s_kind[w] == 1) {
-          const float m = top[i];
-          if (m > -INFINITY) {
-            h = score_of(w, m);
-            l = ((uint64_t)(63 - w) << 32) | (uint64_t)(0xFFFFFFFFu - (uint32_t)k);
-            pass = h >= bound;
-          }
-        }
-      }
-      chunks.add(pass, h, l, lane);
-    }
+  }
+  __syncthreads();
+  if (s_chunks > kPairs) {  // the same for all: nobody adds any more
     __syncthreads();
-    const bool room = s_chunks <= kPairs;
-    __syncthreads();
-    if (room) break;
     if (t == 0) s_chunks = 0;
     __syncthreads();
+    for (int i0 = 0; i0 < W * nc; i0 += kMergeThreads) {
+      chunks.shrink(kPairs - kMergeThreads, K, wv, lane, &s_bound);
+      bound = s_bound;
+      const int i = i0 + t;
+      uint64_t h = 0;
+      const int w = i < W * nc ? (int)fdiv((uint32_t)i, A.divC) : 0;
+      if (i < W * nc && s_kind[w] == 1 && top[i] > -INFINITY) h = score_of(w, top[i]);
+      chunks.add(h != 0 && h >= bound, h, place(w, i - w * nc), lane);
+    }
   }
   chunks.shrink(2 * K + 64, K, wv, lane, &s_bound);
   const int n = s_chunks;
@@ -408,6 +484,14 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
       const uint64_t h = over ? ordered_of((double)s_score[lane]) : 0;
       best.add(over && h >= bound, h, ((uint64_t)(63 - lane) << 58) | kTokenMask, lane);
     }
+    typename Vt::Raw x[4], nxt[4];
+    auto fetch = [&](int i, typename Vt::Raw (&y)[4]) {
+      const int w = 63 - (int)uniform((uint32_t)(s_clo[i] >> 32));
+      const int k = (int)(0xFFFFFFFFu - uniform((uint32_t)s_clo[i]));
+      load_chunk<DT>(A.x + (int64_t)b * A.sb + (int64_t)w * A.sw, (int64_t)k * kBeamChunk, A.nvec, A.V,
+                     lane, y);
+    };
+    if (wv < n) fetch(wv, nxt);
     for (int i0 = 0; i0 < n; i0 += kMergeWaves) {
       if (slow) {
         best.shrink(kPairs - kMergeWaves * 64, K, wv, lane, &s_bound);
@@ -415,17 +499,59 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
       }
       const int i = i0 + wv;
       if (i >= n) continue;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = nxt[j];
+      if (i + kMergeWaves < n) fetch(i + kMergeWaves, nxt);
       const int w = 63 - (int)uniform((uint32_t)(s_clo[i] >> 32));
       const int k = (int)(0xFFFFFFFFu - uniform((uint32_t)s_clo[i]));
-      typename Vt::Raw x[4];
-      load_chunk<DT>(A.x + (int64_t)b * A.sb + (int64_t)w * A.sw, (int64_t)k * kBeamChunk, A.nvec, A.V,
-                     lane, x);
-      // a logit that every entry reaching the bound exceeds; the chunk's largest does in any case
-      const double at = ((value_of(bound) - (double)s_score[w]) * 1.4426950408889634074 + s_lse[w] +
-                         s_off[w]) / A.c;
-      const double slack = 1e-6 * (fabs(at) + fabs((double)s_score[w] / A.c) + fabs(s_off[w] / A.c));
+      // a logit that every entry reaching the bound exceeds; the chunk's largest, if that is less,
+      // does in any case (its score here may be the bound itself)
+      const double base = (double)s_score[w] * 1.4426950408889634074;
+      const double at = (value_of(bound) * 1.4426950408889634074 - base + s_lse[w] + s_off[w]) * A.inv_c;
+      const double slack = 1e-6 * (fabs(at) + (fabs(base) + fabs(s_off[w])) * A.inv_c);
+      const double most = ((value_of(s_chi[i]) * 1.4426950408889634074 - base) + s_lse[w] + s_off[w]) *
+                          A.inv_c;  // of the chunk's largest
       const float least =
-          fmaxf(bound == 0 ? -FLT_MAX : fminf((float)(at - slack), top[w * nc + k]), -FLT_MAX);
+          fmaxf(bound == 0 ? -FLT_MAX : (float)(fmin(at, most) - slack), -FLT_MAX);
+      auto add_entry = [&](bool has, float y, uint32_t token) {
+        const uint64_t h = has && y > -INFINITY ? score_of(w, y) : 0;
+        best.add(h != 0 && h >= bound, h,
+                 ((uint64_t)(63 - w) << 58) | ((uint64_t)ordered_of(y) << kTokenBits) |
+                     (uint64_t)(kTokenMask - token), lane);
+      };
+      // mostly one or two lanes hold such a logit: their vectors go through LDS, a logit a lane
+      uint64_t hits = 0;
+      const bool quick = lanes_with<DT>(x, least, hits) && __builtin_popcountll(hits) <= 16 && !slow;
+      if (quick) {
+        while (hits) {
+          uint64_t rest = hits;
+          int turn = -1;  // of this lane among the next kHits
+#pragma unroll
+          for (int j = 0; j < kHits; ++j)
+            if (rest) {
+              if (lane == __builtin_ctzll(rest)) turn = j;
+              rest &= rest - 1;
+            }
+          if (turn >= 0)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              *reinterpret_cast<typename Vt::Raw*>(s_hit[wv] + turn * 64 + j * 16) = x[j];
+          lds_wave_fence();
+          const int which = lane / (4 * E), j = lane % (4 * E);  // a logit of the which-th lane
+          uint64_t m = hits;
+#pragma unroll
+          for (int i = 1; i < kHits; ++i) m = i <= which ? m & (m - 1) : m;
+          const int from = m ? __builtin_ctzll(m) : 0;
+          float y;
+          if constexpr (DT == HS_F32) y = reinterpret_cast<const float*>(s_hit[wv])[lane];
+          else y = Vt::lo(reinterpret_cast<const uint16_t*>(s_hit[wv])[lane]);
+          add_entry(m != 0 && y >= least, y,
+                    (uint32_t)((k * kBeamChunk + (j / E) * 64 + from) * E + j % E));
+          lds_wave_fence();
+          hits = rest;
+        }
+        continue;
+      }
       float z[4 * E];
 #pragma unroll
       for (int j = 0; j < 4; ++j) Vt::unpack(x[j], z + j * E);
@@ -436,22 +562,29 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
         return (uint32_t)((k * kBeamChunk + (j / E) * 64 + lane) * E + j % E);
       };
       if (wave_sum_i(__builtin_popcount(pass)) > 64) {  // the chunk's K best: by logit, then by token
-        uint32_t u[4 * E];
+        auto count = [&](auto reaches) {
+          int c = 0;
 #pragma unroll
-        for (int j = 0; j < 4 * E; ++j) u[j] = (pass >> j) & 1 ? ordered_of(z[j]) : 0;
-        const uint32_t cut = nth_largest32(u, 4 * E, K);
-        int above = 0;
+          for (int j = 0; j < 4 * E; ++j)
+            c += __builtin_popcountll(__ballot(((pass >> j) & 1) != 0 && reaches(j)));
+          return c;
+        };
+        uint32_t cut = 0, last = 0;
+        for (int bit = 31; bit >= 0; --bit) {
+          const uint32_t y = cut | (1u << bit);
+          if (count([&](int j) { return ordered_of(z[j]) >= y; }) >= K) cut = y;
+        }
+        const int left = K - count([&](int j) { return ordered_of(z[j]) > cut; });
+        for (int bit = kTokenBits - 1; bit >= 0; --bit) {
+          const uint32_t y = last | (1u << bit);
+          if (count([&](int j) { return ordered_of(z[j]) == cut && kTokenMask - token_of(j) >= y; }) >= left)
+            last = y;
+        }
 #pragma unroll
-        for (int j = 0; j < 4 * E; ++j) above += __builtin_popcountll(__ballot(u[j] > cut));
-        uint32_t v[4 * E];
-#pragma unroll
-        for (int j = 0; j < 4 * E; ++j)
-          v[j] = u[j] != 0 && u[j] == cut ? kTokenMask - token_of(j) : 0;
-        const uint32_t last = nth_largest32(v, 4 * E, K - above);
-        pass = 0;
-#pragma unroll
-        for (int j = 0; j < 4 * E; ++j)
-          pass |= u[j] > cut || (v[j] != 0 && v[j] >= last) ? 1u << j : 0u;
+        for (int j = 0; j < 4 * E; ++j) {
+          const uint32_t u = ordered_of(z[j]);
+          if (u < cut || (u == cut && kTokenMask - token_of(j) < last)) pass &= ~(1u << j);
+        }
       }
       while (__ballot(pass != 0)) {  // a lane's next entry; mostly there are one or two in a chunk
         const bool has = pass != 0;
@@ -459,10 +592,7 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
         float y = z[0];
 #pragma unroll
         for (int e = 1; e < 4 * E; ++e) y = j == e ? z[e] : y;
-        const uint64_t h = has ? score_of(w, y) : 0;
-        best.add(has && h >= bound, h,
-                 ((uint64_t)(63 - w) << 58) | ((uint64_t)ordered_of(y) << kTokenBits) |
-                     (uint64_t)(kTokenMask - token_of(j)), lane);
+        add_entry(has, y, token_of(j));
         pass &= pass - 1;
       }
     }
@@ -475,34 +605,32 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
   }
   best.shrink(256, K, wv, lane, &s_bound);
   const int C = s_count;
-  // every entry's rank: the waves compare it with a share of the others each
-  for (int i = t; i < C; i += kMergeThreads) s_rank[i] = 0;
-  __syncthreads();
-  for (int i0 = 0; i0 < C; i0 += 64) {
-    const int i = i0 + lane;
-    const uint64_t h = i < C ? s_hi[i] : 0, l = i < C ? s_lo[i] : 0;
-    int r = 0;
-    for (int j = wv; j < C; j += kMergeWaves) {
-      const uint64_t oh = s_hi[j], ol = s_lo[j];
-      r += oh > h || (oh == h && ol > l) ? 1 : 0;
-    }
-    if (i < C && r) atomicAdd(&s_rank[i], r);
+  // every entry's rank: a wave takes every 16th and compares it with all, four in each lane
+  uint64_t h[4], l[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    h[j] = j * 64 + lane < C ? s_hi[j * 64 + lane] : 0;
+    l[j] = j * 64 + lane < C ? s_lo[j * 64 + lane] : 0;
   }
-  __syncthreads();
-  for (int i = t; i < max(C, K); i += kMergeThreads) {
-    int at = i;  // a slot without an entry
+  for (int i = wv; i < max(C, K); i += kMergeWaves) {
+    int at = i;  // past the last entry: an empty slot
     float sc = -INFINITY;
     int parent = -1, token = -1;
     uint8_t over = 0;
     if (i < C) {
-      at = s_rank[i];
-      sc = (float)value_of(s_hi[i]);
-      parent = 63 - (int)(s_lo[i] >> 58);
+      const uint64_t hi = uniform(s_hi[i]), lo = uniform(s_lo[i]);
+      at = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j * 64 < C)
+          at += __builtin_popcountll(__ballot(h[j] > hi || (h[j] == hi && l[j] > lo)));
+      sc = (float)value_of(hi);
+      parent = 63 - (int)(lo >> 58);
       const bool was = s_kind[parent] == 2;
-      token = was ? A.eos : (int)(kTokenMask - ((uint32_t)s_lo[i] & kTokenMask));
+      token = was ? A.eos : (int)(kTokenMask - ((uint32_t)lo & kTokenMask));
       over = was || (A.eos >= 0 && token == A.eos) ? 1 : 0;
     }
-    if (at < K) {
+    if (at < K && lane == 0) {
       const int64_t o = (int64_t)b * K + at;
       A.out_score[o] = sc;
       A.out_parent[o] = parent;
@@ -566,6 +694,7 @@ int launch_beam_step(const BeamGeom& g, const hs_beam_args& a, hipStream_t strea
   A.divW = make_fastdiv((uint32_t)g.W);
   A.divC = make_fastdiv((uint32_t)g.nc);
   A.c = 1.4426950408889634074 / a.temperature;
+  A.inv_c = 1.0 / A.c;
   // ca: the top 12 bits of c; cb: the rest, above 0 so that -inf stays -inf in z cb + (z ca - offset)
   uint64_t bits;
   __builtin_memcpy(&bits, &A.c, 8);
