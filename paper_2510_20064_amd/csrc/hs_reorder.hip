@@ -18,7 +18,6 @@ struct MoveState {
   char* dst;
   int64_t ssb, ssw, ssr, dsb, dsw, dsr;
   int64_t units, unit;
-  uint32_t first;   // first workgroup of this tensor
   FastDiv div_chunks, div_rows;
   int chunks, rows;  // workgroups per row, rows per query
 };
@@ -27,32 +26,56 @@ struct MoveArgs {
   int64_t parent_stride;
   const int32_t* parent;
   const int32_t* count;
+  uint32_t first[kStates];  // first workgroup of each tensor (past the last one: none)
   MoveState st[kStates];
 };
 
+// A thread's word of up to BYTES bytes at `at` of a buffer of `bytes` bytes: what lies outside is not
+// read (0) and not written, by the bounds of the buffer's descriptor.
 template <int BYTES>
 struct Word;
 template <>
 struct Word<16> {
   typedef unsigned int T __attribute__((ext_vector_type(4)));
+  static __device__ T load(__amdgpu_buffer_rsrc_t r, int at) {
+    return __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0);
+  }
+  static __device__ void store(T x, __amdgpu_buffer_rsrc_t r, int at) {
+    __builtin_amdgcn_raw_buffer_store_b128(x, r, at, 0, 0);
+  }
 };
 template <>
 struct Word<4> {
   typedef uint32_t T;
+  static __device__ T load(__amdgpu_buffer_rsrc_t r, int at) {
+    return __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0);
+  }
+  static __device__ void store(T x, __amdgpu_buffer_rsrc_t r, int at) {
+    __builtin_amdgcn_raw_buffer_store_b32(x, r, at, 0, 0);
+  }
 };
 template <>
 struct Word<1> {
   typedef uint8_t T;
+  static __device__ T load(__amdgpu_buffer_rsrc_t r, int at) {
+    return __builtin_amdgcn_raw_buffer_load_b8(r, at, 0, 0);
+  }
+  static __device__ void store(T x, __amdgpu_buffer_rsrc_t r, int at) {
+    __builtin_amdgcn_raw_buffer_store_b8(x, r, at, 0, 0);
+  }
 };
+constexpr int kRawBuffer = 0x00020000;  // a descriptor's last word: plain 32-bit data
 
-// KMAX: slots handled at once, at least K in place (all loads come before the stores).
+// KMAX: at least K; every slot's word is in a register between the loads and the stores. A slot that
+// moves nothing has a descriptor of no bytes instead of a branch, so all loads go out together.
 template <int BYTES, int KMAX>
 __global__ __launch_bounds__(kThreads) void hs_reorder_kernel(MoveArgs A) {
-  typedef typename Word<BYTES>::T T;
+  using Wd = Word<BYTES>;
   int i = 0;
-  while (i + 1 < A.n && blockIdx.x >= A.st[i + 1].first) ++i;
-  const MoveState& S = A.st[i];
-  const uint32_t u = blockIdx.x - S.first;
+#pragma unroll
+  for (int j = 1; j < kStates; ++j) i += blockIdx.x >= A.first[j] ? 1 : 0;
+  const MoveState S = A.st[i];
+  const uint32_t u = blockIdx.x - A.first[i];
   const uint32_t br = fdiv(u, S.div_chunks);
   const int64_t chunk = u - br * (uint32_t)S.chunks;
   const int b = (int)fdiv(br, S.div_rows);
@@ -62,25 +85,33 @@ __global__ __launch_bounds__(kThreads) void hs_reorder_kernel(MoveArgs A) {
     const int64_t c = A.count[b];
     units = c < 0 ? 0 : c < units ? c : units;
   }
-  const int64_t at = (chunk * kThreads + threadIdx.x) * BYTES;
-  if (at >= units * S.unit) return;
-  const char* src = S.src + b * S.ssb + r * S.ssr + at;
-  char* dst = S.dst + b * S.dsb + r * S.dsr + at;
+  const int64_t begin = chunk * kThreads * BYTES, left = units * S.unit - begin;
+  if (left <= 0) return;  // the whole workgroup
+  const int bytes = (int)(left < kThreads * BYTES ? left : kThreads * BYTES);
   const bool inplace = S.src == S.dst;
-  const int32_t* parent = A.parent + b * A.parent_stride;
-  for (int j0 = 0; j0 < A.K; j0 += KMAX) {
-    T x[KMAX];
-    bool moves[KMAX];
+  // lane j: slot j's parent, -1 where nothing moves
+  const int lane = threadIdx.x & 63;
+  int mine = lane < A.K ? A.parent[b * A.parent_stride + lane] : -1;
+  if (mine >= A.W || (inplace && mine == lane)) mine = -1;
+  // (the same in every lane, told to the compiler: descriptors live in scalar registers)
+  const uint64_t src = uniform((uint64_t)(S.src + b * S.ssb + r * S.ssr + begin));
+  const uint64_t dst = uniform((uint64_t)(S.dst + b * S.dsb + r * S.dsr + begin));
+  const uint64_t ssw = uniform((uint64_t)S.ssw), dsw = uniform((uint64_t)S.dsw);
+  auto buffer = [&](uint64_t base, uint64_t stride, int w, bool some) {
+    return __builtin_amdgcn_make_buffer_rsrc(
+        reinterpret_cast<void*>(uniform(base + (uint64_t)(uint32_t)w * stride)), 0,
+        (int)uniform(some ? (uint32_t)bytes : 0u), kRawBuffer);
+  };
+  const int at = (int)threadIdx.x * BYTES;
+  typename Wd::T x[KMAX];
 #pragma unroll
-    for (int j = 0; j < KMAX; ++j) {
-      const int p = j0 + j < A.K ? parent[j0 + j] : -1;
-      moves[j] = p >= 0 && p < A.W && !(inplace && p == j0 + j);
-      if (moves[j]) x[j] = *reinterpret_cast<const T*>(src + p * S.ssw);
-    }
-#pragma unroll
-    for (int j = 0; j < KMAX; ++j)
-      if (moves[j]) *reinterpret_cast<T*>(dst + (j0 + j) * S.dsw) = x[j];
+  for (int j = 0; j < KMAX; ++j) {
+    const int p = __builtin_amdgcn_readlane(mine, j);
+    x[j] = Wd::load(buffer(src, ssw, max(p, 0), p >= 0), at);
   }
+#pragma unroll
+  for (int j = 0; j < KMAX; ++j)
+    Wd::store(x[j], buffer(dst, dsw, j, __builtin_amdgcn_readlane(mine, j) >= 0), at);
 }
 
 template <int BYTES>
@@ -150,6 +181,7 @@ int launch_reorder(const hs_state* states, int n, int B, int W, int K, const int
         const uint64_t chunks = chunks_of(s, word);
         const uint64_t wgs = chunks * (uint64_t)s.rows * (uint64_t)B;
         if (grid + wgs >= (1ull << 31)) break;
+        A.first[A.n] = (uint32_t)grid;
         MoveState& m = A.st[A.n++];
         m.src = reinterpret_cast<const char*>(s.src);
         m.dst = reinterpret_cast<char*>(s.dst);
@@ -161,7 +193,6 @@ int launch_reorder(const hs_state* states, int n, int B, int W, int K, const int
         m.dsr = s.dst_stride_row;
         m.units = s.units;
         m.unit = s.unit;
-        m.first = (uint32_t)grid;
         m.chunks = (int)chunks;
         m.rows = (int)s.rows;
         m.div_chunks = make_fastdiv((uint32_t)chunks);
@@ -169,6 +200,7 @@ int launch_reorder(const hs_state* states, int n, int B, int W, int K, const int
         grid += wgs;
       }
       if (A.n == 0) break;
+      for (int j = A.n; j < kStates; ++j) A.first[j] = 0xFFFFFFFFu;
       if (word == 16) launch_words<16>(A, (uint32_t)grid, stream);
       else if (word == 4) launch_words<4>(A, (uint32_t)grid, stream);
       else launch_words<1>(A, (uint32_t)grid, stream);
