@@ -1,5 +1,5 @@
 // hs_beam_reorder: dst[b][j] = src[b][parent[b][j]] for many tensors in one launch. A thread owns one
-// vector (16, 4 or 1 bytes) of a row position and moves it for every slot of the query: all of its
+// word (16 bytes, or 1) of a row position and moves it for every slot of the query: all of its
 // loads come before its first store and no other thread touches those bytes, so a tensor can be
 // reordered in place whatever the parents are (cycles, one beam continued by many), with no second
 // buffer. Bound by HBM: every byte that changes hands is read once and written once.
@@ -32,20 +32,22 @@ struct MoveArgs {
 
 // A thread's word of up to BYTES bytes at `at` of a buffer of `bytes` bytes: what lies outside is not
 // read (0) and not written, by the bounds of the buffer's descriptor.
-template <int BYTES>
+// STREAM: nontemporal.
+template <int BYTES, bool STREAM>
 struct Word;
-template <>
-struct Word<16> {
+template <bool STREAM>
+struct Word<16, STREAM> {
   typedef unsigned int T __attribute__((ext_vector_type(4)));
+  static constexpr int kHow = STREAM ? 2 : 0;  // the instructions' nt bit
   static __device__ T load(__amdgpu_buffer_rsrc_t r, int at) {
-    return __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0);
+    return __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, kHow);
   }
   static __device__ void store(T x, __amdgpu_buffer_rsrc_t r, int at) {
-    __builtin_amdgcn_raw_buffer_store_b128(x, r, at, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(x, r, at, 0, kHow);
   }
 };
 template <>
-struct Word<4> {
+struct Word<4, false> {
   typedef uint32_t T;
   static __device__ T load(__amdgpu_buffer_rsrc_t r, int at) {
     return __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0);
@@ -55,7 +57,7 @@ struct Word<4> {
   }
 };
 template <>
-struct Word<1> {
+struct Word<1, false> {
   typedef uint8_t T;
   static __device__ T load(__amdgpu_buffer_rsrc_t r, int at) {
     return __builtin_amdgcn_raw_buffer_load_b8(r, at, 0, 0);
@@ -66,11 +68,32 @@ struct Word<1> {
 };
 constexpr int kRawBuffer = 0x00020000;  // a descriptor's last word: plain 32-bit data
 
-// KMAX: at least K; every slot's word is in a register between the loads and the stores. A slot that
-// moves nothing has a descriptor of no bytes instead of a branch, so all loads go out together.
-template <int BYTES, int KMAX>
+// Moves the word at byte `at` < bytes of every slot, KMAX of them at most: every slot's word is in a
+// register between the loads and the stores. A slot that moves nothing (mine of its lane < 0) has a
+// descriptor of no bytes instead of a branch, so all loads go out together.
+template <typename Wd, int KMAX>
+__device__ __forceinline__ void move_words(int mine, uint64_t src, uint64_t ssw, uint64_t dst,
+                                           uint64_t dsw, int bytes, int at) {
+  auto buffer = [&](uint64_t base, uint64_t stride, int w, bool some) {
+    return __builtin_amdgcn_make_buffer_rsrc(
+        reinterpret_cast<void*>(uniform(base + (uint64_t)(uint32_t)w * stride)), 0,
+        (int)uniform(some ? (uint32_t)bytes : 0u), kRawBuffer);
+  };
+  typename Wd::T x[KMAX];
+#pragma unroll
+  for (int j = 0; j < KMAX; ++j) {
+    const int p = __builtin_amdgcn_readlane(mine, j);
+    x[j] = Wd::load(buffer(src, ssw, max(p, 0), p >= 0), at);
+  }
+#pragma unroll
+  for (int j = 0; j < KMAX; ++j)
+    Wd::store(x[j], buffer(dst, dsw, j, __builtin_amdgcn_readlane(mine, j) >= 0), at);
+}
+
+// KMAX: at least K.
+template <int BYTES, int KMAX, bool STREAM>
 __global__ __launch_bounds__(kThreads) void hs_reorder_kernel(MoveArgs A) {
-  using Wd = Word<BYTES>;
+  using Wd = Word<BYTES, STREAM>;
   int i = 0;
 #pragma unroll
   for (int j = 1; j < kStates; ++j) i += blockIdx.x >= A.first[j] ? 1 : 0;
@@ -97,38 +120,34 @@ __global__ __launch_bounds__(kThreads) void hs_reorder_kernel(MoveArgs A) {
   const uint64_t src = uniform((uint64_t)(S.src + b * S.ssb + r * S.ssr + begin));
   const uint64_t dst = uniform((uint64_t)(S.dst + b * S.dsb + r * S.dsr + begin));
   const uint64_t ssw = uniform((uint64_t)S.ssw), dsw = uniform((uint64_t)S.dsw);
-  auto buffer = [&](uint64_t base, uint64_t stride, int w, bool some) {
-    return __builtin_amdgcn_make_buffer_rsrc(
-        reinterpret_cast<void*>(uniform(base + (uint64_t)(uint32_t)w * stride)), 0,
-        (int)uniform(some ? (uint32_t)bytes : 0u), kRawBuffer);
-  };
-  const int at = (int)threadIdx.x * BYTES;
-  typename Wd::T x[KMAX];
-#pragma unroll
-  for (int j = 0; j < KMAX; ++j) {
-    const int p = __builtin_amdgcn_readlane(mine, j);
-    x[j] = Wd::load(buffer(src, ssw, max(p, 0), p >= 0), at);
-  }
-#pragma unroll
-  for (int j = 0; j < KMAX; ++j)
-    Wd::store(x[j], buffer(dst, dsw, j, __builtin_amdgcn_readlane(mine, j) >= 0), at);
+  move_words<Wd, KMAX>(mine, src, ssw, dst, dsw, bytes / BYTES * BYTES,
+                       (int)threadIdx.x * BYTES);
+  if (BYTES == 16 && (bytes & 15) != 0)  // a row's last one to three dwords
+    move_words<Word<4, false>, KMAX>(mine, src, ssw, dst, dsw, bytes,
+                                     bytes / 16 * 16 + (int)threadIdx.x * 4);
 }
 
-template <int BYTES>
+template <int BYTES, bool STREAM>
 void launch_words(const MoveArgs& A, uint32_t grid, hipStream_t st) {
-  if (A.K <= 8) hs_reorder_kernel<BYTES, 8><<<grid, kThreads, 0, st>>>(A);
-  else if (A.K <= 16) hs_reorder_kernel<BYTES, 16><<<grid, kThreads, 0, st>>>(A);
-  else if (A.K <= 32) hs_reorder_kernel<BYTES, 32><<<grid, kThreads, 0, st>>>(A);
-  else hs_reorder_kernel<BYTES, 64><<<grid, kThreads, 0, st>>>(A);
+  if (A.K <= 8) hs_reorder_kernel<BYTES, 8, STREAM><<<grid, kThreads, 0, st>>>(A);
+  else if (A.K <= 16) hs_reorder_kernel<BYTES, 16, STREAM><<<grid, kThreads, 0, st>>>(A);
+  else if (A.K <= 32) hs_reorder_kernel<BYTES, 32, STREAM><<<grid, kThreads, 0, st>>>(A);
+  else hs_reorder_kernel<BYTES, 64, STREAM><<<grid, kThreads, 0, st>>>(A);
 }
 
-// The widest word that every pointer, stride and unit of a tensor is a multiple of.
+// Slots' bytes of a call from which on its words are nontemporal. Four caches of 8 slots x 8 heads x 1024
+// tokens x 256 bytes a query, half of them moved, in us without and with: 67 MB 12.8 and 13.2, 134 MB
+// 23.3 and 23.0, 268 MB 51 and 46, 1.07 GB 183 and 166; 2.1 GB of 64 slots 404 and 379.
+constexpr __int128 kStreamBytes = (__int128)100 << 20;
+
+// The word a tensor moves by: 16 bytes where every pointer, stride and unit is a multiple of 4 (what the
+// loads and stores need), else 1.
 int word_of(const hs_state& s) {
   const uint64_t all = (uint64_t)(uintptr_t)s.src | (uint64_t)(uintptr_t)s.dst |
                        (uint64_t)s.src_stride_b | (uint64_t)s.src_stride_w |
                        (uint64_t)s.src_stride_row | (uint64_t)s.dst_stride_b |
                        (uint64_t)s.dst_stride_w | (uint64_t)s.dst_stride_row | (uint64_t)s.unit;
-  return (all & 15) == 0 ? 16 : (all & 3) == 0 ? 4 : 1;
+  return (all & 3) == 0 ? 16 : 1;
 }
 
 uint64_t chunks_of(const hs_state& s, int word) {
@@ -163,7 +182,10 @@ bool state_apart(const hs_state& s, int B, int K, int64_t row) {
 
 int launch_reorder(const hs_state* states, int n, int B, int W, int K, const int32_t* parent,
                    int64_t parent_stride, const int32_t* count, hipStream_t stream) {
-  for (int word = 16; word >= 1; word /= 4) {  // the tensors of one word width together
+  __int128 all = 0;
+  for (int i = 0; i < n; ++i) all += (__int128)B * K * states[i].rows * states[i].units * states[i].unit;
+  const bool stream_past = all >= kStreamBytes;
+  for (int word = 16; word >= 1; word /= 16) {  // the tensors of one word width together
     int i = 0;
     while (i < n) {
       MoveArgs A;
@@ -201,9 +223,9 @@ int launch_reorder(const hs_state* states, int n, int B, int W, int K, const int
       }
       if (A.n == 0) break;
       for (int j = A.n; j < kStates; ++j) A.first[j] = 0xFFFFFFFFu;
-      if (word == 16) launch_words<16>(A, (uint32_t)grid, stream);
-      else if (word == 4) launch_words<4>(A, (uint32_t)grid, stream);
-      else launch_words<1>(A, (uint32_t)grid, stream);
+      if (word == 16 && stream_past) launch_words<16, true>(A, (uint32_t)grid, stream);
+      else if (word == 16) launch_words<16, false>(A, (uint32_t)grid, stream);
+      else launch_words<1, false>(A, (uint32_t)grid, stream);
       if (hipGetLastError() != hipSuccess) return HS_ERR_HIP;
     }
   }
