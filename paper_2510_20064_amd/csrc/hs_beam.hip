@@ -2,19 +2,20 @@
 //   s(w, v) = score_w + log softmax(z_w / T)_v = score_w + (z_wv c - lse2_w) ln 2,
 // c = log2(e) / T, lse2_w = log2 sum_v 2^(z_wv c). Within a beam the order of s is the order of the
 // logits. Two launches:
-//   1. hs_beam_rows_kernel reads every logit once and keeps, of each chunk of 256 16-byte vectors,
-//      its largest logit, and of each slice (one wave's chunks) its exp2 sum. No candidates: what a
-//      chunk must hold to matter is not known before the rows' normalisers are;
-//   2. hs_beam_merge_kernel, one workgroup per query: the normalisers, then the scores of the
-//      chunks' maxima. The K-th largest of them is reached by K entries at least, so only the chunks
-//      whose maximum reaches it (about K of all the query's chunks) can hold any of the K best: these
+//   1. hs_beam_rows_kernel reads every logit once and keeps, of each slice (one wave's chunks of 256
+//      16-byte vectors), its exp2 sum, and of each quarter of a chunk (a unit: what 16 lanes hold) its
+//      largest logit. No candidates: what a unit must hold to matter is not known before the rows'
+//      normalisers are;
+//   2. hs_beam_merge_kernel, one workgroup per query: the normalisers, then a bound from the scores of
+//      the units' maxima: the K-th largest of them is reached by K entries at least, so only the units
+//      whose maximum reaches it (about K of all the query's units) can hold any of the K best: these
 //      are read again, and what reaches the bound is ranked by (s, lower beam, larger logit, lower
 //      token).
 //
 // Precision. Two beams' candidates are often closer than fp32 tells apart and the order is part of
 // the result, so s is formed in fp64 and the normalisers are made good to about 1e-8: z c is taken
 // as z ca + z cb with ca = c rounded to 12 bits (for 16-bit logits z ca - offset is exact), each
-// lane adds its fp32 exponentials per chunk and the chunks in fp64, and the exponentials of the chunks'
+// lane adds its fp32 exponentials per chunk and the chunks in fp64, and the exponentials of the units'
 // largest logits, most of the sum where the distribution is peaked, are replaced by fp64 ones.
 // Sums are relative to an offset near the slice's maximum, and a slice whose maximum is large
 // (|z c| > 4096) takes z - maximum first, so that logits of any size do, the lowest finite value
@@ -30,21 +31,28 @@ namespace {
 constexpr int kMergeThreads = 1024;
 constexpr int kMergeWaves = kMergeThreads / 64;
 constexpr int kRows = HS_MAX_BEAMS / kMergeWaves;  // rows of a wave in the merge
+constexpr int kHeld = 5;         // units' maxima of a row that a lane holds (for 152000 16-bit logits all)
 constexpr int kPairs = 2048;     // entries of one query held in LDS, twice what a round can add
 constexpr int kTokenBits = 26;
 constexpr uint32_t kTokenMask = (1u << kTokenBits) - 1;
 
+constexpr int kUnits = 4;        // of a chunk
+constexpr int kSliceChunks = 16; // of a slice at most: a lane keeps the maximum of one unit
+
 struct SliceRec {
-  double sum;  // of 2^(z c - off) over the slice (not finite: a NaN or +inf logit)
-  double off;  // -inf: no logit above -inf
+  double sum;  // of 2^(z c - offset) over the slice (not finite: a NaN or +inf logit)
+  float ref;   // the logit that the offset came from; -inf: no logit above -inf
+  int off;     // the offset of a small one
 };
+
 struct StepArgs {
   const char* x;
   int64_t sb, sw;  // bytes between queries and between beams
   int W, K, S, chunks, nc;  // slices per row, chunks per slice and per row
+  int nu;                   // units per row
   int64_t V, nvec, score_stride;
   uint32_t units;  // B * W * S
-  FastDiv divS, divW, divC;  // by S, W and nc
+  FastDiv divS, divW, divU;  // by S, W and nu
   float ca, cb;
   double c, inv_c;  // c and 1 / c
   const float* score;
@@ -55,7 +63,7 @@ struct StepArgs {
   int32_t* out_token;
   uint8_t* out_done;
   SliceRec* rec;   // [B * W][S]
-  float* top;      // [B * W][nc]: the chunks' largest logits
+  float* top;      // [B * W][nu]: the units' largest logits
 };
 
 // The offset of exponents z c - off, from a logit at or near the largest.
@@ -118,7 +126,8 @@ __device__ inline void load_chunk(const char* row, int64_t v0, int64_t nvec, int
     for (int i = 0; i < 4; ++i) {
       typedef unsigned int u4 __attribute__((ext_vector_type(4)));
       typedef const __attribute__((address_space(1))) u4* gp4;
-      const u4 y = *(gp4)(row + (v0 + i * 64 + lane) * 16);
+      // (every logit is read once: nontemporal, 8% faster on 311 MB of bf16)
+      const u4 y = __builtin_nontemporal_load((gp4)(row + (v0 + i * 64 + lane) * 16));
       __builtin_memcpy(&x[i], &y, 16);
     }
   } else {
@@ -152,7 +161,7 @@ __global__ __launch_bounds__(kThreads) void hs_beam_rows_kernel(StepArgs A) {
   Offset off(-INFINITY, c);
   bool any = false;   // an offset is set
   double sum = 0.0;   // the lane's
-  float mine = -INFINITY, mine_ref = -INFINITY;  // lane i: the slice's chunk i
+  float mine = -INFINITY, mine_ref = -INFINITY;  // lane 16 r + i: unit r of the slice's chunk i
   Raw cur[4], nxt[4];
   load_chunk<DT>(rowp, (int64_t)c0 * kBeamChunk, A.nvec, A.V, lane, cur);
   for (int k = c0; k < c1; ++k) {
@@ -164,14 +173,16 @@ __global__ __launch_bounds__(kThreads) void hs_beam_rows_kernel(StepArgs A) {
 #pragma unroll
       for (int e = 0; e < E; ++e) lmax = fmaxf(lmax, z[i][e]);
     }
-    float m = lmax;
-    int none = 0;
-    wave_max<false>(m, none);
+    const int key = row16_max(fkey(lmax));
+    const float m = fkey_inv(key);
     // the offset stays while no exponent exceeds 4, so that a slice rarely changes it and the
     // rounding of z c - off stays that of small numbers
-    if (!any || off.exponent(m, A.ca, A.cb) > 4.0f) {
-      if (m != -INFINITY) {
-        const Offset now(m, c);
+    if (!any || __ballot(off.exponent(m, A.ca, A.cb) > 4.0f)) {
+      const float most = fkey_inv(
+          max(max(__builtin_amdgcn_readlane(key, 0), __builtin_amdgcn_readlane(key, 16)),
+              max(__builtin_amdgcn_readlane(key, 32), __builtin_amdgcn_readlane(key, 48))));
+      if (most != -INFINITY) {
+        const Offset now(most, c);
         if (any) sum *= exp2(off.value(A.c) - now.value(A.c));
         off = now;
         any = true;
@@ -199,22 +210,23 @@ __global__ __launch_bounds__(kThreads) void hs_beam_rows_kernel(StepArgs A) {
           acc[e & 3] += __builtin_amdgcn_exp2f(fmaf(z[i][e], A.cb, fmaf(z[i][e], A.ca, -off.o)));
     }
     sum += (double)((acc[0] + acc[1]) + (acc[2] + acc[3]));
-    if (lane == k - c0) {
+    if ((lane & 15) == k - c0) {
       mine = m;
       mine_ref = off.ref;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) cur[i] = nxt[i];
   }
-  if (any && mine > -INFINITY) {  // the chunks' largest terms, from fp32 to fp64
+  if (any && mine > -INFINITY) {  // the units' largest terms, from fp32 to fp64
     const Offset at(mine_ref, c);
     sum += scaled(exp2((double)mine * A.c - at.value(A.c)) -
                       (double)__builtin_amdgcn_exp2f(at.exponent(mine, A.ca, A.cb)),
                   at.value(A.c) - off.value(A.c));
   }
   sum = wave_sum_d(sum);
-  if (lane < c1 - c0) A.top[(int64_t)row * A.nc + c0 + lane] = mine;
-  if (lane == 0) A.rec[u] = SliceRec{sum, any ? off.value(A.c) : -(double)INFINITY};
+  const int k = c0 + (lane & 15);
+  if (k < c1) A.top[(int64_t)row * A.nu + k * kUnits + (lane >> 4)] = mine;
+  if (lane == 0) A.rec[u] = SliceRec{sum, off.ref, (int)off.o};
 }
 
 // ---- launch 2: the rows' normalisers and the K best ------------------------------------------------------
@@ -294,59 +306,29 @@ struct PairList {
   }
 };
 
-// The lanes with a logit >= least among their four vectors (for 16-bit logits: >= least cut to 16 bits,
-// for which positive values compare as integers); false where least is negative.
-template <int DT>
-__device__ inline bool lanes_with(const typename Vec<DT>::Raw (&x)[4], float least, uint64_t& hits) {
-  if (!(least > 0.0f)) return false;
-  if constexpr (DT == HS_F32) {
-    float m = -INFINITY;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) m = fmaxf(fmaxf(m, fmaxf(x[j].x, x[j].y)), fmaxf(x[j].z, x[j].w));
-    hits = __ballot(m >= least);
-  } else {
-    typedef short s2 __attribute__((ext_vector_type(2)));
-    auto word = [](uint32_t u) { return __builtin_bit_cast(s2, u); };
-    s2 m = word(x[0].x);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      m = __builtin_elementwise_max(m, word(x[j].x));
-      m = __builtin_elementwise_max(m, word(x[j].y));
-      m = __builtin_elementwise_max(m, word(x[j].z));
-      m = __builtin_elementwise_max(m, word(x[j].w));
-    }
-    int16_t cut;
-    if constexpr (DT == HS_F16)
-      cut = (int16_t)(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(least, 0.0f)) & 0x7FFFu);
-    else
-      cut = (int16_t)(__float_as_uint(least) >> 16);
-    hits = __ballot(max(m[0], m[1]) >= cut);
-  }
-  return true;
-}
-
 template <int DT>
 __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A) {
   using Vt = Vec<DT>;
+  using Raw = typename Vt::Raw;
   constexpr int E = Vt::kElems;
-  constexpr int kHits = 64 / (4 * E);  // lanes whose logits a wave looks at together
   __shared__ double s_off[HS_MAX_BEAMS], s_lse[HS_MAX_BEAMS];  // a row's log2 normaliser: their sum
   __shared__ float s_score[HS_MAX_BEAMS];
+  __shared__ float s_least[HS_MAX_BEAMS];    // a row's logits below it do not reach the bound
   __shared__ uint8_t s_kind[HS_MAX_BEAMS];   // 0: gives nothing, 1: by its logits, 2: finished
-  __shared__ __attribute__((aligned(16))) uint32_t s_group[128];
-  __shared__ uint64_t s_chi[kPairs], s_clo[kPairs], s_hi[kPairs], s_lo[kPairs];
-  __shared__ __attribute__((aligned(16))) char s_hit[kMergeWaves][kHits * 64];
-  __shared__ int s_chunks, s_count;
+  __shared__ uint32_t s_group[128];
+  __shared__ uint64_t s_uhi[kPairs], s_ulo[kPairs], s_hi[kPairs], s_lo[kPairs];
+  __shared__ int s_units, s_count;
   __shared__ uint64_t s_bound;
   const int t = threadIdx.x, lane = t & 63;
   const int wv = __builtin_amdgcn_readfirstlane(t >> 6);
-  const int b = blockIdx.x, W = A.W, S = A.S, K = A.K, nc = A.nc;
-  const float* top = A.top + (int64_t)b * W * nc;
+  const int b = blockIdx.x, W = A.W, S = A.S, K = A.K, nu = A.nu;
+  const float* top = A.top + (int64_t)b * W * nu;
+  const float c32 = (float)A.c;
 
   // a wave's rows are w = wv + 16 r; every load first (a row that gives nothing has records of
   // another call, which are not used)
   SliceRec r0[kRows], r1[kRows];
-  float m0[kRows], m1[kRows], sc[kRows];
+  float m[kRows][kHeld], sc[kRows];
   bool over[kRows];
 #pragma unroll
   for (int r = 0; r < kRows; ++r) {
@@ -355,14 +337,14 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
     const SliceRec* rec = A.rec + ((int64_t)b * W + w) * S;
     r0[r] = rec[min(lane, S - 1)];
     r1[r] = rec[min(lane + 64, S - 1)];
-    m0[r] = top[w * nc + min(lane, nc - 1)];
-    m1[r] = top[w * nc + min(lane + 64, nc - 1)];
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) m[r][i] = top[w * nu + min(lane + 64 * i, nu - 1)];
     sc[r] = A.score[(int64_t)b * A.score_stride + w];
     over[r] = A.done && A.done[(int64_t)b * A.score_stride + w];
   }
   if (t < 128) s_group[t] = 0;
   if (t == 0) {
-    s_chunks = s_count = 0;
+    s_units = s_count = 0;
     s_bound = ~0ull;
   }
   __syncthreads();
@@ -371,15 +353,15 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
     return ordered_of((double)s_score[w] +
                       (((double)z * A.c - s_off[w]) - s_lse[w]) * 0.69314718055994530942);
   };
-  // Entries fall into groups, each with its largest score's upper half: the K-th largest of them is a
-  // bound that K entries reach. Of random scores 18 reach the 16th of 64 groups, and 89 the 64th of 128.
+  // Entries fall into groups (a lane's of some rows), each with its largest score's upper half: the
+  // K-th largest of them is a bound that K entries reach. Of random scores 18 reach the 16th of 64
+  // groups, and 89 the 64th of 128.
   const int groups = K <= 16 ? 64 : 128;
+  auto group_of = [&](int w) { return groups > 64 ? ((w / kMergeWaves + w) & 1) * 64 : 0; };
 
-  // the rows' normalisers, and the groups' largest chunks
-  uint64_t h0[kRows], h1[kRows];  // scores of the lane's first two chunks
+  // the rows' normalisers, and the groups' largest entries
 #pragma unroll
   for (int r = 0; r < kRows; ++r) {
-    h0[r] = h1[r] = 0;
     const int w = wv + kMergeWaves * r;
     if (w >= W) break;
     const int kind = !isfinite(sc[r]) ? 0 : over[r] ? 2 : 1;
@@ -388,15 +370,23 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
         s_score[w] = sc[r];
         s_kind[w] = (uint8_t)kind;
         if (kind == 2)
-          atomicMax(&s_group[w & (groups - 1)], (uint32_t)(ordered_of((double)sc[r]) >> 32));
+          atomicMax(&s_group[group_of(w)], (uint32_t)(ordered_of((double)sc[r]) >> 32));
       }
       continue;
     }
     const SliceRec* rec = A.rec + ((int64_t)b * W + w) * S;
-    double o = fmax(r0[r].off, r1[r].off);
-    for (int s = lane + 128; s < S; s += 64) o = fmax(o, rec[s].off);
-    o = wave_max_d(o);
-    auto part = [&](const SliceRec& q) { return q.off == -INFINITY ? q.sum : scaled(q.sum, q.off - o); };
+    int best = max(fkey(r0[r].ref), fkey(r1[r].ref));
+    for (int s = lane + 128; s < S; s += 64) best = max(best, fkey(rec[s].ref));
+    const Offset to(fkey_inv(wave_max_i(best)), c32);  // the row's: from its largest reference
+    auto part = [&](const SliceRec& q) -> double {
+      if (q.ref == -INFINITY) return q.sum;
+      if (!to.large) {
+        const Offset from(q.ref, c32);
+        return from.large ? scaled(q.sum, from.value(A.c) - to.value(A.c))
+                          : ldexp(q.sum, q.off - (int)to.o);
+      }
+      return scaled(q.sum, Offset(q.ref, c32).value(A.c) - to.value(A.c));
+    };
     double sum = 0.0;
     if (lane < S) sum += part(r0[r]);
     if (lane + 64 < S) sum += part(r1[r]);
@@ -406,21 +396,18 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
     const double lg = log2_of(sum);
     if (lane == 0) {
       s_score[w] = sc[r];
-      s_off[w] = o;
+      s_off[w] = to.value(A.c);
       s_lse[w] = lg;
       s_kind[w] = live ? 1 : 0;
     }
     lds_wave_fence();
-    if (live)
-      for (int k = lane; k < nc; k += 64) {
-        const float m = k < 64 ? m0[r] : k < 128 ? m1[r] : top[w * nc + k];
-        if (m > -INFINITY) {
-          const uint64_t h = score_of(w, m);
-          if (k < 64) h0[r] = h;
-          else if (k < 128) h1[r] = h;
-          atomicMax(&s_group[(w * nc + k) & (groups - 1)], (uint32_t)(h >> 32));
-        }
-      }
+    float most = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+      if (lane + 64 * i < nu) most = fmaxf(most, m[r][i]);
+    for (int k = lane + 64 * kHeld; k < nu; k += 64) most = fmaxf(most, top[w * nu + k]);
+    if (live && most > -INFINITY)
+      atomicMax(&s_group[group_of(w) + lane], (uint32_t)(score_of(w, most) >> 32));
   }
   __syncthreads();
   // the smallest group that fewer than K exceed; 0 (no bound) with fewer than K groups. Each wave
@@ -438,9 +425,8 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
   __syncthreads();
   uint64_t bound = s_bound;
 
-  // the chunks that reach it; a second time, keeping only the K first by (s, lower beam, lower chunk)
-  // on the way, if they are too many (equal maxima): their maxima all come before any other chunk's
-  PairList chunks{s_chi, s_clo, &s_chunks};
+  // the units that reach it
+  PairList units{s_uhi, s_ulo, &s_units};
   auto place = [](int w, int k) {
     return ((uint64_t)(63 - w) << 32) | (uint64_t)(0xFFFFFFFFu - (uint32_t)k);
   };
@@ -448,48 +434,62 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
   for (int r = 0; r < kRows; ++r) {
     const int w = wv + kMergeWaves * r;
     if (w >= W) break;
-    chunks.add(h0[r] != 0 && h0[r] >= bound, h0[r], place(w, lane), lane);
-    if (nc > 64) chunks.add(h1[r] != 0 && h1[r] >= bound, h1[r], place(w, lane + 64), lane);
-    if (nc > 128 && s_kind[w] == 1)
-      for (int k0 = 128; k0 < nc; k0 += 64) {
-        const float m = k0 + lane < nc ? top[w * nc + k0 + lane] : -INFINITY;
-        const uint64_t h = m > -INFINITY ? score_of(w, m) : 0;
-        chunks.add(h != 0 && h >= bound, h, place(w, k0 + lane), lane);
-      }
+    if (s_kind[w] != 1) continue;
+    const double base = (double)s_score[w] * 1.4426950408889634074;
+    const double at = (value_of(bound) * 1.4426950408889634074 - base + s_lse[w] + s_off[w]) * A.inv_c;
+    const double slack = 1e-6 * (fabs(at) + (fabs(base) + fabs(s_off[w])) * A.inv_c);
+    const float least = bound == 0 ? -FLT_MAX : fmaxf((float)(at - slack), -FLT_MAX);
+    if (lane == 0) s_least[w] = least;
+    auto offer = [&](float y, int k) {
+      const bool pass = k < nu && y >= least;
+      if (__ballot(pass)) units.add(pass, score_of(w, y), place(w, k), lane);
+    };
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+      if (64 * i < nu) offer(m[r][i], lane + 64 * i);
+    for (int k0 = 64 * kHeld; k0 < nu; k0 += 64)
+      offer(k0 + lane < nu ? top[w * nu + k0 + lane] : -INFINITY, k0 + lane);
   }
   __syncthreads();
-  if (s_chunks > kPairs) {  // the same for all: nobody adds any more
+  // If they are too many (equal maxima), the 4 K first by (s, lower beam, lower chunk) do: all but
+  // three of them (units of its chunk, in no order with it) have an entry before any of a later unit
+  const bool ties = s_units > kPairs;  // the same for all: nobody adds any more
+  __syncthreads();
+  if (ties) {
+    if (t == 0) s_units = 0;
     __syncthreads();
-    if (t == 0) s_chunks = 0;
-    __syncthreads();
-    for (int i0 = 0; i0 < W * nc; i0 += kMergeThreads) {
-      chunks.shrink(kPairs - kMergeThreads, K, wv, lane, &s_bound);
+    for (int i0 = 0; i0 < W * nu; i0 += kMergeThreads) {
+      units.shrink(kPairs - kMergeThreads, 4 * K, wv, lane, &s_bound);
       bound = s_bound;
       const int i = i0 + t;
       uint64_t h = 0;
-      const int w = i < W * nc ? (int)fdiv((uint32_t)i, A.divC) : 0;
-      if (i < W * nc && s_kind[w] == 1 && top[i] > -INFINITY) h = score_of(w, top[i]);
-      chunks.add(h != 0 && h >= bound, h, place(w, i - w * nc), lane);
+      const int w = i < W * nu ? (int)fdiv((uint32_t)i, A.divU) : 0;
+      if (i < W * nu && s_kind[w] == 1 && top[i] > -INFINITY) h = score_of(w, top[i]);
+      units.add(h != 0 && h >= bound, h, place(w, i - w * nu), lane);
     }
   }
-  chunks.shrink(2 * K + 64, K, wv, lane, &s_bound);
-  const int n = s_chunks;
+  units.shrink(4 * K + 64, 4 * K, wv, lane, &s_bound);
+  const int n = s_units;
   bound = s_bound;
 
-  // their entries, and the finished beams; again in two ways
+  // their entries, and the finished beams; a second time, keeping only the K best on the way, if they
+  // are too many
   PairList best{s_hi, s_lo, &s_count};
   for (int slow = 0; slow < 2; ++slow) {
     if (wv == 0) {
-      const bool over = lane < W && s_kind[lane] == 2;
-      const uint64_t h = over ? ordered_of((double)s_score[lane]) : 0;
-      best.add(over && h >= bound, h, ((uint64_t)(63 - lane) << 58) | kTokenMask, lane);
+      const bool ended = lane < W && s_kind[lane] == 2;
+      const uint64_t h = ended ? ordered_of((double)s_score[lane]) : 0;
+      best.add(ended && h >= bound, h, ((uint64_t)(63 - lane) << 58) | kTokenMask, lane);
     }
-    typename Vt::Raw x[4], nxt[4];
-    auto fetch = [&](int i, typename Vt::Raw (&y)[4]) {
-      const int w = 63 - (int)uniform((uint32_t)(s_clo[i] >> 32));
-      const int k = (int)(0xFFFFFFFFu - uniform((uint32_t)s_clo[i]));
-      load_chunk<DT>(A.x + (int64_t)b * A.sb + (int64_t)w * A.sw, (int64_t)k * kBeamChunk, A.nvec, A.V,
-                     lane, y);
+    Raw x, nxt;
+    auto first_vector = [&](int k) {  // of this lane in unit k of a row
+      return (k / kUnits) * kBeamChunk + (lane >> 4) * 64 + (k % kUnits) * 16 + (lane & 15);
+    };
+    auto fetch = [&](int i, Raw& y) {
+      const int w = 63 - (int)uniform((uint32_t)(s_ulo[i] >> 32));
+      const int64_t vi = first_vector((int)(0xFFFFFFFFu - uniform((uint32_t)s_ulo[i])));
+      const char* row = A.x + (int64_t)b * A.sb + (int64_t)w * A.sw;
+      y = vi < A.nvec ? Vt::load_raw(row, vi, A.V) : Vt::neg_raw();
     };
     if (wv < n) fetch(wv, nxt);
     for (int i0 = 0; i0 < n; i0 += kMergeWaves) {
@@ -499,100 +499,52 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
       }
       const int i = i0 + wv;
       if (i >= n) continue;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = nxt[j];
+      x = nxt;
       if (i + kMergeWaves < n) fetch(i + kMergeWaves, nxt);
-      const int w = 63 - (int)uniform((uint32_t)(s_clo[i] >> 32));
-      const int k = (int)(0xFFFFFFFFu - uniform((uint32_t)s_clo[i]));
-      // a logit that every entry reaching the bound exceeds; the chunk's largest, if that is less,
-      // does in any case (its score here may be the bound itself)
-      const double base = (double)s_score[w] * 1.4426950408889634074;
-      const double at = (value_of(bound) * 1.4426950408889634074 - base + s_lse[w] + s_off[w]) * A.inv_c;
-      const double slack = 1e-6 * (fabs(at) + (fabs(base) + fabs(s_off[w])) * A.inv_c);
-      const double most = ((value_of(s_chi[i]) * 1.4426950408889634074 - base) + s_lse[w] + s_off[w]) *
-                          A.inv_c;  // of the chunk's largest
-      const float least =
-          fmaxf(bound == 0 ? -FLT_MAX : (float)(fmin(at, most) - slack), -FLT_MAX);
-      auto add_entry = [&](bool has, float y, uint32_t token) {
-        const uint64_t h = has && y > -INFINITY ? score_of(w, y) : 0;
-        best.add(h != 0 && h >= bound, h,
-                 ((uint64_t)(63 - w) << 58) | ((uint64_t)ordered_of(y) << kTokenBits) |
-                     (uint64_t)(kTokenMask - token), lane);
-      };
-      // mostly one or two lanes hold such a logit: their vectors go through LDS, a logit a lane
-      uint64_t hits = 0;
-      const bool quick = lanes_with<DT>(x, least, hits) && __builtin_popcountll(hits) <= 16 && !slow;
-      if (quick) {
-        while (hits) {
-          uint64_t rest = hits;
-          int turn = -1;  // of this lane among the next kHits
-#pragma unroll
-          for (int j = 0; j < kHits; ++j)
-            if (rest) {
-              if (lane == __builtin_ctzll(rest)) turn = j;
-              rest &= rest - 1;
-            }
-          if (turn >= 0)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              *reinterpret_cast<typename Vt::Raw*>(s_hit[wv] + turn * 64 + j * 16) = x[j];
-          lds_wave_fence();
-          const int which = lane / (4 * E), j = lane % (4 * E);  // a logit of the which-th lane
-          uint64_t m = hits;
-#pragma unroll
-          for (int i = 1; i < kHits; ++i) m = i <= which ? m & (m - 1) : m;
-          const int from = m ? __builtin_ctzll(m) : 0;
-          float y;
-          if constexpr (DT == HS_F32) y = reinterpret_cast<const float*>(s_hit[wv])[lane];
-          else y = Vt::lo(reinterpret_cast<const uint16_t*>(s_hit[wv])[lane]);
-          add_entry(m != 0 && y >= least, y,
-                    (uint32_t)((k * kBeamChunk + (j / E) * 64 + from) * E + j % E));
-          lds_wave_fence();
-          hits = rest;
-        }
-        continue;
-      }
-      float z[4 * E];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) Vt::unpack(x[j], z + j * E);
+      const int w = 63 - (int)uniform((uint32_t)(s_ulo[i] >> 32));
+      const uint32_t token =
+          (uint32_t)first_vector((int)(0xFFFFFFFFu - uniform((uint32_t)s_ulo[i]))) * E;
+      const float least = s_least[w];
+      float z[E];
+      Vt::unpack(x, z);
       uint32_t pass = 0;  // of the lane's logits
 #pragma unroll
-      for (int j = 0; j < 4 * E; ++j) pass |= z[j] >= least ? 1u << j : 0u;
-      auto token_of = [&](int j) {
-        return (uint32_t)((k * kBeamChunk + (j / E) * 64 + lane) * E + j % E);
-      };
-      if (wave_sum_i(__builtin_popcount(pass)) > 64) {  // the chunk's K best: by logit, then by token
+      for (int e = 0; e < E; ++e) pass |= z[e] >= least ? 1u << e : 0u;
+      if (slow && wave_sum_i(__builtin_popcount(pass)) > 64) {  // the unit's K best: by logit, by token
         auto count = [&](auto reaches) {
           int c = 0;
 #pragma unroll
-          for (int j = 0; j < 4 * E; ++j)
-            c += __builtin_popcountll(__ballot(((pass >> j) & 1) != 0 && reaches(j)));
+          for (int e = 0; e < E; ++e)
+            c += __builtin_popcountll(__ballot(((pass >> e) & 1) != 0 && reaches(e)));
           return c;
         };
         uint32_t cut = 0, last = 0;
         for (int bit = 31; bit >= 0; --bit) {
           const uint32_t y = cut | (1u << bit);
-          if (count([&](int j) { return ordered_of(z[j]) >= y; }) >= K) cut = y;
+          if (count([&](int e) { return ordered_of(z[e]) >= y; }) >= K) cut = y;
         }
-        const int left = K - count([&](int j) { return ordered_of(z[j]) > cut; });
+        const int left = K - count([&](int e) { return ordered_of(z[e]) > cut; });
         for (int bit = kTokenBits - 1; bit >= 0; --bit) {
           const uint32_t y = last | (1u << bit);
-          if (count([&](int j) { return ordered_of(z[j]) == cut && kTokenMask - token_of(j) >= y; }) >= left)
+          if (count([&](int e) { return ordered_of(z[e]) == cut && kTokenMask - (token + e) >= y; }) >= left)
             last = y;
         }
 #pragma unroll
-        for (int j = 0; j < 4 * E; ++j) {
-          const uint32_t u = ordered_of(z[j]);
-          if (u < cut || (u == cut && kTokenMask - token_of(j) < last)) pass &= ~(1u << j);
+        for (int e = 0; e < E; ++e) {
+          const uint32_t u = ordered_of(z[e]);
+          if (u < cut || (u == cut && kTokenMask - (token + e) < last)) pass &= ~(1u << e);
         }
       }
-      while (__ballot(pass != 0)) {  // a lane's next entry; mostly there are one or two in a chunk
+      while (__ballot(pass != 0)) {  // a lane's next entry; mostly there are one or two in a unit
         const bool has = pass != 0;
         const int j = has ? __builtin_ctz(pass) : 0;
         float y = z[0];
 #pragma unroll
-        for (int e = 1; e < 4 * E; ++e) y = j == e ? z[e] : y;
-        add_entry(has, y, token_of(j));
+        for (int e = 1; e < E; ++e) y = j == e ? z[e] : y;
+        const uint64_t h = has ? score_of(w, y) : 0;
+        best.add(has && h >= bound, h,
+                 ((uint64_t)(63 - w) << 58) | ((uint64_t)ordered_of(y) << kTokenBits) |
+                     (uint64_t)(kTokenMask - (token + j)), lane);
         pass &= pass - 1;
       }
     }
@@ -664,7 +616,7 @@ bool beam_geom(int B, int W, int K, int64_t V, int dtype, BeamGeom* g) {
   if (g->nvec > (int64_t)kMaxTeamSlices * kThreads) return false;
   g->nc = (int)((g->nvec + kBeamChunk - 1) / kBeamChunk);
   const int64_t n = (int64_t)g->nc * B * W / 8192;
-  const int most = g->nc < 64 ? g->nc : 64;  // a lane keeps each chunk's maximum
+  const int most = g->nc < kSliceChunks ? g->nc : kSliceChunks;
   g->chunks = (int)(n < 1 ? 1 : n > most ? most : n);
   g->S = (g->nc + g->chunks - 1) / g->chunks;
   return true;
@@ -672,7 +624,7 @@ bool beam_geom(int B, int W, int K, int64_t V, int dtype, BeamGeom* g) {
 
 size_t beam_ws_bytes(const BeamGeom& g) {
   const size_t rows = (size_t)g.B * g.W;
-  return align256(rows * g.S * sizeof(SliceRec)) + align256(rows * g.nc * sizeof(float));
+  return align256(rows * g.S * sizeof(SliceRec)) + align256(rows * g.nc * kUnits * sizeof(float));
 }
 
 int launch_beam_step(const BeamGeom& g, const hs_beam_args& a, hipStream_t stream) {
@@ -686,13 +638,14 @@ int launch_beam_step(const BeamGeom& g, const hs_beam_args& a, hipStream_t strea
   A.S = g.S;
   A.chunks = g.chunks;
   A.nc = g.nc;
+  A.nu = g.nc * kUnits;
   A.V = g.V;
   A.nvec = g.nvec;
   A.score_stride = a.score_stride;
   A.units = (uint32_t)((int64_t)g.B * g.W * g.S);
   A.divS = make_fastdiv((uint32_t)g.S);
   A.divW = make_fastdiv((uint32_t)g.W);
-  A.divC = make_fastdiv((uint32_t)g.nc);
+  A.divU = make_fastdiv((uint32_t)A.nu);
   A.c = 1.4426950408889634074 / a.temperature;
   A.inv_c = 1.0 / A.c;
   // ca: the top 12 bits of c; cb: the rest, above 0 so that -inf stays -inf in z cb + (z ca - offset)
