@@ -32,6 +32,7 @@ constexpr int kMergeThreads = 1024;
 constexpr int kMergeWaves = kMergeThreads / 64;
 constexpr int kRows = HS_MAX_BEAMS / kMergeWaves;  // rows of a wave in the merge
 constexpr int kHeld = 5;         // units' maxima of a row that a lane holds (for 152000 16-bit logits all)
+constexpr int kAtOnce = 4;       // units that a wave reads at once
 constexpr int kPairs = 2048;     // entries of one query held in LDS, twice what a round can add
 constexpr int kTokenBits = 26;
 constexpr uint32_t kTokenMask = (1u << kTokenBits) - 1;
@@ -317,6 +318,8 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
   __shared__ uint8_t s_kind[HS_MAX_BEAMS];   // 0: gives nothing, 1: by its logits, 2: finished
   __shared__ uint32_t s_group[128];
   __shared__ uint64_t s_uhi[kPairs], s_ulo[kPairs], s_hi[kPairs], s_lo[kPairs];
+  __shared__ Raw s_vec[kMergeWaves][64];
+  __shared__ uint8_t s_from[kMergeWaves][64], s_unit[kMergeWaves][64];
   __shared__ int s_units, s_count;
   __shared__ uint64_t s_bound;
   const int t = threadIdx.x, lane = t & 63;
@@ -378,19 +381,18 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
     int best = max(fkey(r0[r].ref), fkey(r1[r].ref));
     for (int s = lane + 128; s < S; s += 64) best = max(best, fkey(rec[s].ref));
     const Offset to(fkey_inv(wave_max_i(best)), c32);  // the row's: from its largest reference
-    auto part = [&](const SliceRec& q) -> double {
-      if (q.ref == -INFINITY) return q.sum;
-      if (!to.large) {
-        const Offset from(q.ref, c32);
-        return from.large ? scaled(q.sum, from.value(A.c) - to.value(A.c))
-                          : ldexp(q.sum, q.off - (int)to.o);
-      }
-      return scaled(q.sum, Offset(q.ref, c32).value(A.c) - to.value(A.c));
-    };
     double sum = 0.0;
-    if (lane < S) sum += part(r0[r]);
-    if (lane + 64 < S) sum += part(r1[r]);
-    for (int s = lane + 128; s < S; s += 64) sum += part(rec[s]);
+    auto part = [&](const SliceRec& q, bool mine) {
+      const Offset from(q.ref, c32);
+      if (!__ballot(mine && (to.large || (from.large && q.ref != -INFINITY)))) {  // small offsets
+        if (mine) sum += ldexp(q.sum, q.off - (int)to.o);
+      } else if (mine) {
+        sum += q.ref == -INFINITY ? q.sum : scaled(q.sum, from.value(A.c) - to.value(A.c));
+      }
+    };
+    part(r0[r], lane < S);
+    if (S > 64) part(r1[r], lane + 64 < S);
+    for (int s0 = 128; s0 < S; s0 += 64) part(rec[min(s0 + lane, S - 1)], s0 + lane < S);
     sum = wave_sum_d(sum);
     const bool live = isfinite(sum) && sum > 0.0;
     const double lg = log2_of(sum);
@@ -440,22 +442,36 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
     const double slack = 1e-6 * (fabs(at) + (fabs(base) + fabs(s_off[w])) * A.inv_c);
     const float least = bound == 0 ? -FLT_MAX : fmaxf((float)(at - slack), -FLT_MAX);
     if (lane == 0) s_least[w] = least;
-    auto offer = [&](float y, int k) {
-      const bool pass = k < nu && y >= least;
-      if (__ballot(pass)) units.add(pass, score_of(w, y), place(w, k), lane);
-    };
+    uint64_t who[kHeld];  // lanes whose unit reaches it; one count for all of them
+    int found = 0;
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i)
-      if (64 * i < nu) offer(m[r][i], lane + 64 * i);
-    for (int k0 = 64 * kHeld; k0 < nu; k0 += 64)
-      offer(k0 + lane < nu ? top[w * nu + k0 + lane] : -INFINITY, k0 + lane);
+    for (int i = 0; i < kHeld; ++i) {
+      who[i] = __ballot(lane + 64 * i < nu && m[r][i] >= least);
+      found += __builtin_popcountll(who[i]);
+    }
+    if (found) {
+      int at = 0;
+      if (lane == 0) at = atomicAdd(&s_units, found);
+      at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) {
+        const int to = at + lanes_below(who[i]);
+        if (((who[i] >> lane) & 1) && to < kPairs) s_ulo[to] = place(w, lane + 64 * i);
+        at += __builtin_popcountll(who[i]);
+      }
+    }
+    for (int k0 = 64 * kHeld; k0 < nu; k0 += 64) {
+      const int k = k0 + lane;
+      const bool pass = k < nu && top[w * nu + min(k, nu - 1)] >= least;
+      units.add(pass, 0, place(w, k), lane);
+    }
   }
   __syncthreads();
+  int n = s_units;
   // If they are too many (equal maxima), the 4 K first by (s, lower beam, lower chunk) do: all but
   // three of them (units of its chunk, in no order with it) have an entry before any of a later unit
-  const bool ties = s_units > kPairs;  // the same for all: nobody adds any more
-  __syncthreads();
-  if (ties) {
+  if (n > 4 * K + 64) {  // the same for all: nobody adds any more
+    __syncthreads();
     if (t == 0) s_units = 0;
     __syncthreads();
     for (int i0 = 0; i0 < W * nu; i0 += kMergeThreads) {
@@ -467,50 +483,104 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
       if (i < W * nu && s_kind[w] == 1 && top[i] > -INFINITY) h = score_of(w, top[i]);
       units.add(h != 0 && h >= bound, h, place(w, i - w * nu), lane);
     }
+    units.shrink(4 * K, 4 * K, wv, lane, &s_bound);
+    n = s_units;
+    bound = s_bound;
   }
-  units.shrink(4 * K + 64, 4 * K, wv, lane, &s_bound);
-  const int n = s_units;
-  bound = s_bound;
 
   // their entries, and the finished beams; a second time, keeping only the K best on the way, if they
   // are too many
   PairList best{s_hi, s_lo, &s_count};
-  for (int slow = 0; slow < 2; ++slow) {
-    if (wv == 0) {
-      const bool ended = lane < W && s_kind[lane] == 2;
-      const uint64_t h = ended ? ordered_of((double)s_score[lane]) : 0;
-      best.add(ended && h >= bound, h, ((uint64_t)(63 - lane) << 58) | kTokenMask, lane);
+  auto add_finished = [&]() {
+    if (wv != 0) return;
+    const bool ended = lane < W && s_kind[lane] == 2;
+    const uint64_t h = ended ? ordered_of((double)s_score[lane]) : 0;
+    best.add(ended && h >= bound, h, ((uint64_t)(63 - lane) << 58) | kTokenMask, lane);
+  };
+  auto row_of = [](uint64_t lo) { return 63 - (int)(lo >> 32); };
+  auto first_vector = [](uint64_t lo, int l) {  // of lane l in a unit
+    const int k = (int)(0xFFFFFFFFu - (uint32_t)lo);
+    return (k / kUnits) * kBeamChunk + (l >> 4) * 64 + (k % kUnits) * 16 + (l & 15);
+  };
+  auto fetch = [&](uint64_t lo) {
+    const char* row = A.x + (int64_t)b * A.sb + (int64_t)row_of(lo) * A.sw;
+    const int64_t vi = first_vector(lo, lane);
+    return vi < A.nvec ? Vt::load_raw(row, vi, A.V) : Vt::neg_raw();
+  };
+  auto add_logit = [&](bool has, float y, uint64_t lo, int l, int e) {
+    const int w = has ? row_of(lo) : 0;
+    const uint64_t h = has ? score_of(w, y) : 0;
+    best.add(has && h >= bound, h,
+             ((uint64_t)(63 - w) << 58) | ((uint64_t)ordered_of(y) << kTokenBits) |
+                 (uint64_t)(kTokenMask - ((uint32_t)first_vector(lo, l) * E + e)), lane);
+  };
+  add_finished();
+  // four units of a wave at once, so that their loads are in flight together. The few lanes with a logit
+  // that reaches the bound leave their vectors in LDS, and then every lane looks at one logit
+  for (int i0 = wv; i0 < n; i0 += kMergeWaves * kAtOnce) {
+    Raw x[kAtOnce];
+    uint64_t of[kAtOnce];
+#pragma unroll
+    for (int q = 0; q < kAtOnce; ++q) {
+      if (i0 + q * kMergeWaves >= n) break;
+      of[q] = uniform(s_ulo[i0 + q * kMergeWaves]);
+      x[q] = fetch(of[q]);
     }
-    Raw x, nxt;
-    auto first_vector = [&](int k) {  // of this lane in unit k of a row
-      return (k / kUnits) * kBeamChunk + (lane >> 4) * 64 + (k % kUnits) * 16 + (lane & 15);
-    };
-    auto fetch = [&](int i, Raw& y) {
-      const int w = 63 - (int)uniform((uint32_t)(s_ulo[i] >> 32));
-      const int64_t vi = first_vector((int)(0xFFFFFFFFu - uniform((uint32_t)s_ulo[i])));
-      const char* row = A.x + (int64_t)b * A.sb + (int64_t)w * A.sw;
-      y = vi < A.nvec ? Vt::load_raw(row, vi, A.V) : Vt::neg_raw();
-    };
-    if (wv < n) fetch(wv, nxt);
-    for (int i0 = 0; i0 < n; i0 += kMergeWaves) {
-      if (slow) {
-        best.shrink(kPairs - kMergeWaves * 64, K, wv, lane, &s_bound);
-        bound = s_bound;
+    int hits = 0;
+#pragma unroll
+    for (int q = 0; q < kAtOnce; ++q) {
+      if (i0 + q * kMergeWaves >= n) break;
+      float z[E], most = -INFINITY;
+      Vt::unpack(x[q], z);
+#pragma unroll
+      for (int e = 0; e < E; ++e) most = fmaxf(most, z[e]);
+      const uint64_t who = __ballot(most >= s_least[row_of(of[q])]);
+      const int at = hits + lanes_below(who);
+      if (((who >> lane) & 1) && at < 64) {
+        s_vec[wv][at] = x[q];
+        s_from[wv][at] = (uint8_t)lane;
+        s_unit[wv][at] = (uint8_t)q;
       }
+      hits += __builtin_popcountll(who);
+    }
+    lds_wave_fence();
+    if (hits > 64) {
+      if (lane == 0) atomicAdd(&s_count, kPairs);  // no room: the second way
+      break;
+    }
+    for (int p = 0; p < hits; p += 64 / E) {
+      const int at = p + lane / E, e = lane % E;
+      const bool in = at < hits;
+      uint64_t lo = of[0];
+#pragma unroll
+      for (int q = 1; q < kAtOnce; ++q) lo = in && s_unit[wv][at & 63] == q ? of[q] : lo;
+      float y;
+      if constexpr (DT == HS_F32) y = reinterpret_cast<const float*>(&s_vec[wv][at & 63])[e];
+      else y = Vt::lo(reinterpret_cast<const uint16_t*>(&s_vec[wv][at & 63])[e]);
+      add_logit(in && y >= s_least[row_of(lo)], y, lo, s_from[wv][at & 63], e);
+    }
+    lds_wave_fence();
+  }
+  __syncthreads();
+  if (s_count > kPairs) {  // the same for all: nobody adds any more
+    __syncthreads();
+    if (t == 0) s_count = 0;
+    __syncthreads();
+    add_finished();
+    for (int i0 = 0; i0 < n; i0 += kMergeWaves) {
+      best.shrink(kPairs - kMergeWaves * 64, K, wv, lane, &s_bound);
+      bound = s_bound;
       const int i = i0 + wv;
       if (i >= n) continue;
-      x = nxt;
-      if (i + kMergeWaves < n) fetch(i + kMergeWaves, nxt);
-      const int w = 63 - (int)uniform((uint32_t)(s_ulo[i] >> 32));
-      const uint32_t token =
-          (uint32_t)first_vector((int)(0xFFFFFFFFu - uniform((uint32_t)s_ulo[i]))) * E;
-      const float least = s_least[w];
+      const uint64_t lo = uniform(s_ulo[i]);
+      const float least = s_least[row_of(lo)];
+      const uint32_t token = (uint32_t)first_vector(lo, lane) * E;
       float z[E];
-      Vt::unpack(x, z);
+      Vt::unpack(fetch(lo), z);
       uint32_t pass = 0;  // of the lane's logits
 #pragma unroll
       for (int e = 0; e < E; ++e) pass |= z[e] >= least ? 1u << e : 0u;
-      if (slow && wave_sum_i(__builtin_popcount(pass)) > 64) {  // the unit's K best: by logit, by token
+      if (wave_sum_i(__builtin_popcount(pass)) > 64) {  // the unit's K best: by logit, by token
         auto count = [&](auto reaches) {
           int c = 0;
 #pragma unroll
@@ -535,28 +605,17 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
           if (u < cut || (u == cut && kTokenMask - (token + e) < last)) pass &= ~(1u << e);
         }
       }
-      while (__ballot(pass != 0)) {  // a lane's next entry; mostly there are one or two in a unit
-        const bool has = pass != 0;
-        const int j = has ? __builtin_ctz(pass) : 0;
-        float y = z[0];
 #pragma unroll
-        for (int e = 1; e < E; ++e) y = j == e ? z[e] : y;
-        const uint64_t h = has ? score_of(w, y) : 0;
-        best.add(has && h >= bound, h,
-                 ((uint64_t)(63 - w) << 58) | ((uint64_t)ordered_of(y) << kTokenBits) |
-                     (uint64_t)(kTokenMask - (token + j)), lane);
-        pass &= pass - 1;
-      }
+      for (int e = 0; e < E; ++e)
+        if (__ballot((pass >> e) & 1)) add_logit((pass >> e) & 1, z[e], lo, lane, e);
     }
     __syncthreads();
-    const bool room = s_count <= kPairs;
-    __syncthreads();
-    if (room) break;
-    if (t == 0) s_count = 0;
-    __syncthreads();
   }
-  best.shrink(256, K, wv, lane, &s_bound);
-  const int C = s_count;
+  int C = s_count;
+  if (C > 256) {  // what a wave can rank
+    best.shrink(256, K, wv, lane, &s_bound);
+    C = s_count;
+  }
   // every entry's rank: a wave takes every 16th and compares it with all, four in each lane
   uint64_t h[4], l[4];
 #pragma unroll
