@@ -38,7 +38,6 @@ constexpr int kTokenBits = 26;
 constexpr uint32_t kTokenMask = (1u << kTokenBits) - 1;
 
 constexpr int kUnits = 4;        // of a chunk
-constexpr int kSliceChunks = 16; // of a slice at most: a lane keeps the maximum of one unit
 
 struct SliceRec {
   double sum;  // of 2^(z c - offset) over the slice (not finite: a NaN or +inf logit)
@@ -162,7 +161,7 @@ __global__ __launch_bounds__(kThreads) void hs_beam_rows_kernel(StepArgs A) {
   Offset off(-INFINITY, c);
   bool any = false;   // an offset is set
   double sum = 0.0;   // the lane's
-  float mine = -INFINITY, mine_ref = -INFINITY;  // lane 16 r + i: unit r of the slice's chunk i
+  float mine = -INFINITY, mine_ref = -INFINITY;  // lane 16 r + i: unit r of the slice's i-th chunk
   Raw cur[4], nxt[4];
   load_chunk<DT>(rowp, (int64_t)c0 * kBeamChunk, A.nvec, A.V, lane, cur);
   for (int k = c0; k < c1; ++k) {
@@ -660,7 +659,10 @@ void launch_step(const StepArgs& A, int B, hipStream_t st) {
 
 }  // namespace
 
-// One wave per slice: as many slices as give the device its 8192 resident waves, of one chunk at least.
+// One wave per slice, of two chunks (the second one's loads fly while the first is summed), or of one where
+// that leaves the device's 8192 waves unfilled. us with one, two, three and four chunks: 10 x 75 chunks 11.0,
+// 11.6, 12.0, 12.8; 8064 of 128 rows 16.1, 15.8, 16.1, 15.8; 16128 22.5, 21.3, 22.5, 22.3; 32256 32.7, 30.8,
+// 30.4, 31.6; 76800 78.8, 67.4, 66.9, 69.3; 64 x 8 fp32 rows of 126 53.1, 49.0, 50.1, 52.1.
 bool beam_geom(int B, int W, int K, int64_t V, int dtype, BeamGeom* g) {
   if (B < 1 || W < 1 || K < 1 || V < 1) return false;
   if (B > HS_MAX_QUERIES || W > HS_MAX_BEAMS || K > HS_MAX_BEAMS || V > INT32_MAX) return false;
@@ -674,9 +676,7 @@ bool beam_geom(int B, int W, int K, int64_t V, int dtype, BeamGeom* g) {
   g->dtype = dtype;
   if (g->nvec > (int64_t)kMaxTeamSlices * kThreads) return false;
   g->nc = (int)((g->nvec + kBeamChunk - 1) / kBeamChunk);
-  const int64_t n = (int64_t)g->nc * B * W / 8192;
-  const int most = g->nc < kSliceChunks ? g->nc : kSliceChunks;
-  g->chunks = (int)(n < 1 ? 1 : n > most ? most : n);
+  g->chunks = g->nc > 1 && (int64_t)g->nc * B * W >= 8000 ? 2 : 1;
   g->S = (g->nc + g->chunks - 1) / g->chunks;
   return true;
 }
