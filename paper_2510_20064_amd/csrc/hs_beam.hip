@@ -188,28 +188,27 @@ __global__ __launch_bounds__(kThreads) void hs_beam_rows_kernel(StepArgs A) {
         any = true;
       }
     }
-    float acc[4] = {0.f, 0.f, 0.f, 0.f};
-    if (!any) {
+    // a vector's exponentials are added in pairs and then in fp64: a term that is most of the row's sum
+    // is rounded three times at most
+    auto add_terms = [&](auto exponent) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 4; ++i) {
+        float e[E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e & 3] += __builtin_amdgcn_exp2f(z[i][e]);  // 0, or NaN
-    } else if (off.large) {
+        for (int j = 0; j < E; ++j) e[j] = __builtin_amdgcn_exp2f(exponent(z[i][j]));
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+        for (int n = E / 2; n > 0; n /= 2)
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float d = z[i][e] - off.ref;
-          acc[e & 3] += __builtin_amdgcn_exp2f(fmaf(d, A.cb, d * A.ca));
-        }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          acc[e & 3] += __builtin_amdgcn_exp2f(fmaf(z[i][e], A.cb, fmaf(z[i][e], A.ca, -off.o)));
-    }
-    sum += (double)((acc[0] + acc[1]) + (acc[2] + acc[3]));
+          for (int j = 0; j < n; ++j) e[j] += e[j + n];
+        sum += (double)e[0];
+      }
+    };
+    if (!any)
+      add_terms([](float y) { return y; });  // 0, or NaN
+    else if (off.large)
+      add_terms([&](float y) { return fmaf(y - off.ref, A.cb, (y - off.ref) * A.ca); });
+    else
+      add_terms([&](float y) { return fmaf(y, A.cb, fmaf(y, A.ca, -off.o)); });
     if ((lane & 15) == k - c0) {
       mine = m;
       mine_ref = off.ref;
