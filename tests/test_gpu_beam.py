@@ -156,6 +156,87 @@ def test_step_masks_and_empty_rows(dtype):
         check_step(x, scores(g, 3, 8), K, V, T=1.0)
 
 
+@pytest.mark.parametrize("K", [1, 10, 64])
+def test_step_every_unit_ties(K):
+    # identical constant rows: every entry of every unit of every beam has the same score, so each list
+    # overflows; then one score a beam, and one different token a beam
+    note("every unit ties K=%d" % K)
+    W, V = 64, 70000
+    x = torch.full((2, W, V), 1.5, dtype=torch.bfloat16)
+    s = torch.full((2, W), -2.0)
+    s[1] = -torch.arange(W) * 1e-3
+    got = check_step(x, s, K, V)
+    assert got["parent"][0].tolist() == [0] * K and got["token"][0].tolist() == list(range(K))
+    x[:, torch.arange(W), torch.arange(W) * 1000 + 77] = 2.5
+    check_step(x, s, K, V)
+
+
+def test_step_crowded_units():
+    # a few units hold most of the best entries: more lanes of a unit than the quick way takes
+    note("crowded units")
+    g = torch.Generator().manual_seed(71)
+    V = 40000
+    for dt in DTYPES.values():
+        z = torch.randn((2, 3, V), generator=g)
+        z[:, :, 5000:7000] += 30.0
+        z[1, :, 20000:20400] += 60.0
+        for K in (1, 16, 64):
+            check_step(z.to(dt), scores(g, 2, 3), K, V)
+    # negative logits throughout (log-probabilities)
+    z = torch.log_softmax(torch.randn((2, 3, V), generator=g) * 3, 2)
+    for dt in DTYPES.values():
+        check_step(z.to(dt), scores(g, 2, 3), 16, V)
+
+
+def test_step_many_queries():
+    note("65535 queries")
+    g = torch.Generator().manual_seed(73)
+    B, W, V, K = 65535, 2, 64, 3
+    x = torch.randn((B, W, V), generator=g).cuda()
+    s = scores(g, B, W).cuda()
+    out = hs.beam_step(x, s, K)
+    total = (torch.log_softmax(x.double(), 2) + s.double()[:, :, None]).view(B, -1)
+    top, at = total.topk(K + 1, 1)
+    clear = (top[:, :-1] - top[:, 1:]).amin(1) > 1e-6      # no near-ties
+    assert clear.float().mean() > 0.99
+    assert torch.equal((at[:, :K] // V).int()[clear], out["parent"][clear])
+    assert torch.equal((at[:, :K] % V).int()[clear], out["token"][clear])
+    assert (out["score"].double() - top[:, :K]).abs().max() <= NORM_TOL + 20 * 2.0 ** -24
+
+
+def test_step_offsets_past_32_bits():
+    note("logits far apart")
+    V, far = 3000, (1 << 32) + 4096
+    g = torch.Generator().manual_seed(79)
+    buf = torch.zeros((2 * far + V,), dtype=torch.bfloat16, device="cuda")
+    x = buf.as_strided((2, 2, V), (far, far, 1))   # the second query's first beam is the first's second
+    z = (torch.randn((3, V), generator=g) * 3).to(torch.bfloat16)
+    for i in range(3):
+        buf[i * far:i * far + V] = z[i].cuda()
+    s = scores(g, 2, 2)
+    out = hs.beam_step(x, s.cuda(), 9)
+    ref = beam.beam_step(torch.stack([z[:2], z[1:]]).double().numpy(), s.numpy(), 9)
+    same_step({k: v.cpu().numpy() for k, v in out.items()}, ref)
+
+
+def test_step_two_calls_at_once():
+    note("two streams")
+    g = torch.Generator().manual_seed(83)
+    V = 60000
+    x = [rows(g, 8, 8, V, torch.bfloat16) for _ in range(2)]
+    s = scores(g, 8, 8)
+    ref = [hs.beam_step(y.cuda(), s.cuda(), 12, V=V) for y in x]
+    plans = [hs.BeamStep(y.cuda(), s.cuda(), 12, V=V) for y in x]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for p, st in zip(plans, streams):
+            p.run(stream=st)
+    torch.cuda.synchronize()
+    for p, r in zip(plans, ref):
+        assert all(torch.equal(p.out[k], r[k]) for k in r)
+
+
 def test_step_large_logits():
     note("large logits")
     g = torch.Generator().manual_seed(19)
@@ -513,6 +594,22 @@ def test_tree_outputs_are_optional_and_guarded():
     hs._launch(hs.load_library().hs_draft_tree, s.device, None, hs.ctypes.byref(a))
     torch.cuda.synchronize()
     assert torch.equal(bits[1:4], full["mask"]) and torch.all(bits[0] == -7) and torch.all(bits[4] == -7)
+
+
+def test_tree_many_queries():
+    note("65535 trees")
+    rng = np.random.default_rng(8)
+    B, D, K, M = 65535, 2, 3, 5
+    score = -rng.random((D, B, K)).astype(np.float32)
+    score[1] -= 1.0
+    parent = rng.integers(0, K, (D, B, K)).astype(np.int32)
+    token = rng.integers(0, 100, (D, B, K)).astype(np.int32)
+    out = hs.draft_tree(*(torch.from_numpy(v).cuda() for v in (score, parent, token)), M)
+    pick = np.concatenate([np.arange(50), rng.integers(0, B, 100), np.arange(B - 50, B)])
+    ref = beam.draft_tree(score[:, pick], parent[:, pick], token[:, pick], M)
+    for k, v in out.items():
+        got = v.cpu().numpy()[pick]
+        assert np.array_equal(got.view(np.uint64) if k == "mask" else got, ref[k]), k
 
 
 def test_tree_in_a_graph():
