@@ -12,6 +12,7 @@ namespace hs {
 namespace {
 
 constexpr int kStates = 32;  // tensors of one launch (its arguments stay below 4 KB)
+constexpr int kFew = 4;      // ... where they are few: 3 KB less of arguments, 1 us of the host's time
 
 struct MoveState {
   const char* src;
@@ -21,13 +22,14 @@ struct MoveState {
   FastDiv div_chunks, div_rows;
   int chunks, rows;  // workgroups per row, rows per query
 };
+template <int STATES>
 struct MoveArgs {
-  int n, B, W, K;
+  int n, W, K;
   int64_t parent_stride;
   const int32_t* parent;
   const int32_t* count;
-  uint32_t first[kStates];  // first workgroup of each tensor (past the last one: none)
-  MoveState st[kStates];
+  uint32_t first[STATES];  // first workgroup of each tensor (past the last one: none)
+  MoveState st[STATES];
 };
 
 // A thread's word of up to BYTES bytes at `at` of a buffer of `bytes` bytes: what lies outside is not
@@ -91,14 +93,23 @@ __device__ __forceinline__ void move_words(int mine, uint64_t src, uint64_t ssw,
 }
 
 // KMAX: at least K.
-template <int BYTES, int KMAX, bool STREAM>
-__global__ __launch_bounds__(kThreads) void hs_reorder_kernel(MoveArgs A) {
+template <int BYTES, int KMAX, bool STREAM, int STATES>
+__global__ __launch_bounds__(kThreads) void hs_reorder_kernel(MoveArgs<STATES> A) {
   using Wd = Word<BYTES, STREAM>;
   int i = 0;
 #pragma unroll
-  for (int j = 1; j < kStates; ++j) i += blockIdx.x >= A.first[j] ? 1 : 0;
-  const MoveState S = A.st[i];
-  const uint32_t u = blockIdx.x - A.first[i];
+  for (int j = 1; j < STATES; ++j) i += blockIdx.x >= A.first[j] ? 1 : 0;
+  MoveState S = A.st[STATES > kFew ? i : 0];
+  uint32_t first = A.first[STATES > kFew ? i : 0];
+  if (STATES <= kFew) {  // loads that wait for none: the arguments are far away (host memory)
+#pragma unroll
+    for (int j = 1; j < STATES; ++j)
+      if (i == j) {
+        S = A.st[j];
+        first = A.first[j];
+      }
+  }
+  const uint32_t u = blockIdx.x - first;
   const uint32_t br = fdiv(u, S.div_chunks);
   const int64_t chunk = u - br * (uint32_t)S.chunks;
   const int b = (int)fdiv(br, S.div_rows);
@@ -127,12 +138,24 @@ __global__ __launch_bounds__(kThreads) void hs_reorder_kernel(MoveArgs A) {
                                      bytes / 16 * 16 + (int)threadIdx.x * 4);
 }
 
+template <int BYTES, bool STREAM, int STATES>
+void launch_slots(const MoveArgs<STATES>& A, uint32_t grid, hipStream_t st) {
+  if (A.K <= 8) hs_reorder_kernel<BYTES, 8, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
+  else if (A.K <= 16) hs_reorder_kernel<BYTES, 16, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
+  else if (A.K <= 32) hs_reorder_kernel<BYTES, 32, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
+  else hs_reorder_kernel<BYTES, 64, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
+}
+
 template <int BYTES, bool STREAM>
-void launch_words(const MoveArgs& A, uint32_t grid, hipStream_t st) {
-  if (A.K <= 8) hs_reorder_kernel<BYTES, 8, STREAM><<<grid, kThreads, 0, st>>>(A);
-  else if (A.K <= 16) hs_reorder_kernel<BYTES, 16, STREAM><<<grid, kThreads, 0, st>>>(A);
-  else if (A.K <= 32) hs_reorder_kernel<BYTES, 32, STREAM><<<grid, kThreads, 0, st>>>(A);
-  else hs_reorder_kernel<BYTES, 64, STREAM><<<grid, kThreads, 0, st>>>(A);
+void launch_words(const MoveArgs<kStates>& A, uint32_t grid, hipStream_t st) {
+  if (A.n > kFew) {
+    launch_slots<BYTES, STREAM, kStates>(A, grid, st);
+    return;
+  }
+  MoveArgs<kFew> few{A.n, A.W, A.K, A.parent_stride, A.parent, A.count, {}, {}};
+  for (int j = 0; j < kFew; ++j) few.first[j] = A.first[j];
+  for (int j = 0; j < A.n; ++j) few.st[j] = A.st[j];
+  launch_slots<BYTES, STREAM, kFew>(few, grid, st);
 }
 
 // Slots' bytes of a call from which on its words are nontemporal. Four caches of 8 slots x 8 heads x 1024
@@ -188,9 +211,8 @@ int launch_reorder(const hs_state* states, int n, int B, int W, int K, const int
   for (int word = 16; word >= 1; word /= 16) {  // the tensors of one word width together
     int i = 0;
     while (i < n) {
-      MoveArgs A;
+      MoveArgs<kStates> A;
       A.n = 0;
-      A.B = B;
       A.W = W;
       A.K = K;
       A.parent = parent;
