@@ -8,10 +8,11 @@
 //   4. lane n of it is node n: its parent's number from LDS, its path's bits by doubling (after r
 //      rounds a lane holds 2^r nodes of its path), its place among its siblings from the lanes with
 //      the same parent, six ballots;
-//   5. all waves write the children.
+//      The children's slots are filled with -1 while the loads of 1. fly, and the kept children then
+//      written over them.
 // Bound by latency: a few KB per query, and five short steps that depend on each other.
 // One query of 7 steps x 10 slots: kernel 3.6 us (one wave, its loads step by step, 19.5); 256 queries
-// of 8 x 64: 9.3 us (27).
+// of 8 x 64: 8.3 us (27).
 #include "hs_beam.h"
 
 namespace hs {
@@ -30,7 +31,6 @@ __global__ __launch_bounds__(kThreads) void hs_tree_kernel(hs_tree_args A) {
   __shared__ int32_t s_token[NU * 64];
   __shared__ uint8_t s_num[NU * 64];     // a kept node's number
   __shared__ int16_t s_grown[HS_MAX_POSITIONS];  // step * K + slot of every kept node
-  __shared__ int32_t s_cand[HS_MAX_POSITIONS * HS_MAX_BEAMS];
   const int t = threadIdx.x, lane = t & 63, b = blockIdx.x;
   const int D = A.D, K = A.K, M = A.M, N = D * K;
 
@@ -44,8 +44,15 @@ __global__ __launch_bounds__(kThreads) void hs_tree_kernel(hs_tree_args A) {
     p[j] = A.parent[at];
     token[j] = A.token[at];
   }
-  if (A.cand)
-    for (int i = t; i < M * K; i += kThreads) s_cand[i] = -1;
+  int32_t* cand = A.cand ? A.cand + (int64_t)b * M * K : nullptr;
+  if (cand) {
+    int i = t;
+    if ((M * K & 3) == 0 && ((uintptr_t)cand & 15) == 0) {
+      for (; i < M * K / 4; i += kThreads) reinterpret_cast<int4*>(cand)[i] = make_int4(-1, -1, -1, -1);
+    } else {
+      for (; i < M * K; i += kThreads) cand[i] = -1;
+    }
+  }
 #pragma unroll
   for (int j = 0; j < kMine; ++j) {
     const int i = j * kThreads + t;
@@ -80,10 +87,19 @@ __global__ __launch_bounds__(kThreads) void hs_tree_kernel(hs_tree_args A) {
     uint32_t least = 1;  // kept: ranks >= least, and the first `ties` of rank least - 1
     int ties = 0;
     if (have > M - 1) {
-      uint32_t x = 0;
+      // the bits that all ranks share first
+      uint32_t some = 0, lack = 0;
+#pragma unroll
+      for (int j = 0; j < NU; ++j) {
+        some |= u[j];
+        lack |= u[j] != 0 ? ~u[j] : 0;
+      }
+      const uint32_t vary = wave_or_bits(some) & wave_or_bits(lack);
+      const int top = vary ? 31 - __builtin_clz(vary) : -1;
+      uint32_t x = top < 31 ? wave_or_bits(some) >> (top + 1) << (top + 1) : 0;
       int above = 0;  // ranks > the largest value that starts with x's bits
       bool exact = false;
-      for (int bit = 31; bit >= 0 && !exact; --bit) {
+      for (int bit = top; bit >= 0 && !exact; --bit) {
         const uint32_t y = x | (1u << bit);
         int c = 0;
 #pragma unroll
@@ -141,8 +157,9 @@ __global__ __launch_bounds__(kThreads) void hs_tree_kernel(hs_tree_args A) {
       same &= (parent >> bit) & 1 ? m : ~m;
     }
     same &= n < 64 ? (1ull << n) - 1 : ~0ull;
-    if (A.cand && lane > 0 && lane < n)  // (the root has its own like, lane 0)
-      s_cand[parent * K + lanes_below(same & ~1ull)] = tok;
+    // (the two barriers order these stores after the -1 of every wave)
+    if (cand && lane > 0 && lane < n)  // (the root has its own like, lane 0)
+      cand[parent * K + lanes_below(same & ~1ull)] = tok;
 
     const int64_t o = (int64_t)b * M;
     if (lane < M) {
@@ -155,9 +172,6 @@ __global__ __launch_bounds__(kThreads) void hs_tree_kernel(hs_tree_args A) {
     }
     if (A.count && lane == 0) A.count[b] = n;
   }
-  if (!A.cand) return;
-  __syncthreads();
-  for (int i = t; i < M * K; i += kThreads) A.cand[(int64_t)b * M * K + i] = s_cand[i];
 }
 
 }  // namespace

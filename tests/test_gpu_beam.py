@@ -583,6 +583,20 @@ def test_tree_of_odd_scores_and_parents():
         check_tree(score, parent, token, M)
 
 
+@pytest.mark.parametrize("D,K", [(1, 64), (5, 20), (32, 64)])
+def test_tree_of_equal_scores(D, K):
+    note("equal scores D=%d K=%d" % (D, K))
+    rng = np.random.default_rng(9)
+    parent = rng.integers(0, K, (D, 2, K)).astype(np.int32)
+    token = rng.integers(0, 1000, (D, 2, K)).astype(np.int32)
+    for v in (-1.0, 0.0, -3e38):
+        score = np.full((D, 2, K), v, np.float32)
+        for M in (2, 30, 64):
+            check_tree(score, parent, token, M)
+        score[-1, :, K // 2] = np.nextafter(np.float32(v), np.float32(-np.inf))  # one below the rest
+        check_tree(score, parent, token, 64)
+
+
 def test_tree_outputs_are_optional_and_guarded():
     note("tree guards")
     rng = np.random.default_rng(4)
