@@ -25,9 +25,8 @@ constexpr int kNodes = HS_MAX_DEPTH * HS_MAX_BEAMS;
 template <int NU>
 __global__ __launch_bounds__(kThreads) void hs_tree_kernel(hs_tree_args A) {
   constexpr int kMine = (NU * 64 + kThreads - 1) / kThreads;  // nodes of a thread
-  __shared__ uint32_t s_score[NU * 64];  // a node's score as an ordered integer; 0: none
+  __shared__ uint2 s_node[NU * 64];      // a node's score as an ordered integer (0: none), its parent's slot
   __shared__ uint32_t s_rank[NU * 64];   // its rank
-  __shared__ int16_t s_up[NU * 64];      // its parent's slot
   __shared__ int32_t s_token[NU * 64];
   __shared__ uint8_t s_num[NU * 64];     // a kept node's number
   __shared__ int16_t s_grown[HS_MAX_POSITIONS];  // step * K + slot of every kept node
@@ -53,27 +52,34 @@ __global__ __launch_bounds__(kThreads) void hs_tree_kernel(hs_tree_args A) {
       for (; i < M * K; i += kThreads) cand[i] = -1;
     }
   }
+  uint32_t e[kMine], up[kMine];
+  int step_at[kMine];  // the first node of the step that the path has come to
 #pragma unroll
   for (int j = 0; j < kMine; ++j) {
     const int i = j * kThreads + t;
+    const bool node = i < N && isfinite(v[j]) && p[j] >= 0 && (i < K || p[j] < K);
+    e[j] = node ? ordered_of(v[j]) : 0;
+    up[j] = node ? (uint32_t)p[j] : 0;  // (of the first step: not used)
+    step_at[j] = i / K * K;
     if (i < N) {
-      const bool node = isfinite(v[j]) && p[j] >= 0 && (i < K || p[j] < K);
-      s_score[i] = node ? ordered_of(v[j]) : 0;
-      s_up[i] = (int16_t)(node ? min(p[j], K) : 0);  // (of the first step: not used)
+      s_node[i] = make_uint2(e[j], up[j]);
       s_token[i] = token[j];
     }
   }
   __syncthreads();
-  for (int i = t; i < N; i += kThreads) {
-    uint32_t e = s_score[i];
-    int step = i / K * K, up = s_up[i];  // the step's first node, the slot of the parent
-    while (step > 0 && e != 0) {
-      step -= K;
-      e = min(e, s_score[step + up]);  // 0 where the parent is none
-      up = s_up[step + up];
-    }
-    s_rank[i] = e;
+  for (int d = 1; d < D; ++d) {  // a thread's nodes side by side: their reads do not wait for each other
+#pragma unroll
+    for (int j = 0; j < kMine; ++j)
+      if (step_at[j] > 0 && e[j] != 0) {
+        step_at[j] -= K;
+        const uint2 above = s_node[step_at[j] + (int)up[j]];
+        e[j] = min(e[j], above.x);  // 0 where the parent is none
+        up[j] = above.y;
+      }
   }
+#pragma unroll
+  for (int j = 0; j < kMine; ++j)
+    if (j * kThreads + t < N) s_rank[j * kThreads + t] = e[j];
   __syncthreads();
 
   if (t < 64) {
@@ -139,16 +145,17 @@ __global__ __launch_bounds__(kThreads) void hs_tree_kernel(hs_tree_args A) {
       slot = g - d * K;
       depth = d + 1;
       tok = s_token[g];
-      score = value_of(s_score[g]);
-      parent = d == 0 ? 0 : s_num[(d - 1) * K + s_up[g]];
+      const uint2 node = s_node[g];
+      score = value_of(node.x);
+      parent = d == 0 ? 0 : s_num[(d - 1) * K + (int)node.y];
     }
     uint64_t mask = lane < n ? 1ull << lane : 0;
-    int up = parent < 0 ? 0 : parent;  // 2^r steps above; the root is its own parent
+    int far = parent < 0 ? 0 : parent;  // r steps above; the root is its own parent
     for (int r = 1; r <= D; r *= 2) {
-      const uint64_t above = __shfl(mask, up, 64);
-      const int further = __shfl(up, up, 64);
+      const uint64_t above = __shfl(mask, far, 64);
+      const int further = __shfl(far, far, 64);
       if (lane < n) mask |= above;
-      up = further;
+      far = further;
     }
     uint64_t same = ~0ull;
 #pragma unroll
