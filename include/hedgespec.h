@@ -428,11 +428,12 @@ int hs_round(const hs_round_args* args, void* stream);
  *   out_token   : [B][K] int32: its token; -1 for none.
  *   out_done    : NULL, or [B][K] uint8: the slot continues an ended beam, or its token is eos.
  *   out_score may be score itself, and out_done done, where K = W = score_stride; otherwise no
- *   output may overlap an input.
+ *   output may overlap an input, another output or the workspace.
  * W, K          : 1 .. HS_MAX_BEAMS each; K may be larger or smaller than W, and than V.
  * workspace     : at least hs_beam_step_workspace_size() bytes of device memory, 256-byte aligned;
  *                 scratch only.
- * Every logit of a live beam is read once. Deterministic, and the same for a row wherever it stands in
+ * Every logit of a live beam is read once, and of each query about K times 512 of them (K x 256 of fp32)
+ * again. Deterministic, and the same for a row wherever it stands in
  * a call of the same shape.
  */
 typedef struct hs_beam_args {
@@ -466,7 +467,9 @@ int hs_beam_step(const hs_beam_args* args, void* stream);
  * and likewise in dst. Rows are contiguous; a [B][W][heads][tokens][dim] cache has rows = heads,
  * units = tokens, unit = dim * element size.
  *   dst = src (with equal strides): in place; slots that are their own parent then move nothing.
- *         Otherwise dst must not overlap any src of the call.
+ *         No dst may share a byte with another tensor of the call, parent and count included.
+ *         Tensors that lie between each other's rows (slices of one buffer) share none, where their
+ *         strides are the same and each steps over all that the smaller ones span.
  *   parent : [B] rows of K int32, parent_stride elements apart (>= K), device: hs_beam_step's out_parent,
  *            or its first K of more slots. An entry outside [0, W) (an empty slot) leaves the slot's
  *            state as it was.
@@ -508,9 +511,9 @@ int hs_beam_reorder(const hs_state* states_host, int n, int B, int W, int K, con
  *   cand        [B][M][K] int32: the tokens of its kept children in slot order, which is rank order,
  *       then -1: the kept children that hs_candidate_mass takes, with K = M positions and C = K.
  *   count       [B] int32: nodes kept, the root included.
- *   Any output may be NULL.
- * 1 <= D <= HS_MAX_DEPTH, K <= HS_MAX_BEAMS, 2 <= M <= HS_MAX_POSITIONS. One launch, one wave a
- * query.
+ *   Any output may be NULL. None may overlap an input or another output.
+ * 1 <= D <= HS_MAX_DEPTH, K <= HS_MAX_BEAMS, 2 <= M <= HS_MAX_POSITIONS. One launch, one
+ * workgroup a query.
  */
 typedef struct hs_tree_args {
   const float* score;

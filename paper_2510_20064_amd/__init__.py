@@ -9,6 +9,7 @@ loading raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional, Sequence
@@ -718,22 +719,20 @@ class BeamStep:
         return self.out
 
 
-def _lend(stream, *tensors) -> None:
-    """Tensors made on the current stream and dropped after a call on another one."""
-    if stream is not None:
-        for t in tensors:
-            t.record_stream(stream)
+def _on(stream):
+    """Tensors made inside belong to `stream`: their memory is neither still used by the current stream's
+    work nor given to it while `stream` uses it."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
 def beam_step(logits: torch.Tensor, score: torch.Tensor, K: int, V: Optional[int] = None,
               temperature: float = 1.0, done: Optional[torch.Tensor] = None, eos: int = -1,
               out: Optional[dict] = None, workspace: Optional[torch.Tensor] = None,
               stream=None) -> dict:
-    """hs_beam_step, once (see BeamStep, which a loop keeps)."""
-    plan = BeamStep(logits, score, K, V=V, temperature=temperature, done=done, eos=eos, out=out,
-                    workspace=workspace)
-    if workspace is None:
-        _lend(stream, plan.workspace)
+    """hs_beam_step, once (see BeamStep, which a loop keeps). What it makes belongs to `stream`."""
+    with _on(stream):
+        plan = BeamStep(logits, score, K, V=V, temperature=temperature, done=done, eos=eos, out=out,
+                        workspace=workspace)
     return plan.run(stream)
 
 
@@ -858,8 +857,10 @@ class DraftTree:
 
 def draft_tree(score: torch.Tensor, parent: torch.Tensor, token: torch.Tensor, M: int,
                out: Optional[dict] = None, stream=None) -> dict:
-    """hs_draft_tree, once (see DraftTree, which a loop keeps)."""
-    return DraftTree(score, parent, token, M, out=out).run(stream)
+    """hs_draft_tree, once (see DraftTree, which a loop keeps). What it makes belongs to `stream`."""
+    with _on(stream):
+        plan = DraftTree(score, parent, token, M, out=out)
+    return plan.run(stream)
 
 
 class TreeGrowth:
@@ -900,17 +901,17 @@ class TreeGrowth:
 
     def level(self, logits: torch.Tensor, V: Optional[int] = None, stream=None) -> torch.Tensor:
         """One level from logits [B][n][V], n = 1 for the first and W after it. Returns the tokens
-        [B][W] of the beams to draft from next (-1: an empty slot)."""
+        [B][W] of the beams to draft from next (-1: an empty slot), until the next tree's same level."""
         d = self.d
         _need(d < self.depth, "the tree has all its levels: tree() ends it")
         plan = self._plans[d]
         if plan is None or plan.V != (logits.shape[2] if V is None else V) or \
                 plan.dtype != _dtype_code(logits):
             up = self.root if d == 0 else self.score[d - 1][:, :self.W]
-            plan = BeamStep(logits, up, self.K, V=V, temperature=self.temperature,
-                            out={"score": self.score[d], "parent": self.parent[d],
-                                 "token": self.token[d]})
-            _lend(stream, plan.workspace)
+            with _on(stream):
+                plan = BeamStep(logits, up, self.K, V=V, temperature=self.temperature,
+                                out={"score": self.score[d], "parent": self.parent[d],
+                                     "token": self.token[d]})
             self._plans[d] = plan
         plan.set_logits(logits)
         plan.run(stream)
@@ -920,7 +921,13 @@ class TreeGrowth:
         return self.token[d][:, :self.W]
 
     def tree(self, stream=None) -> dict:
-        """The kept nodes of the levels grown; the next level() starts a new tree."""
+        """The kept nodes of the levels grown, until the next tree(); the next level() starts a new
+        tree."""
         _need(self.d == self.depth, "%d of %d levels are grown" % (self.d, self.depth))
+        out = self._tree.run(stream)
+        self.restart()
+        return out
+
+    def restart(self) -> None:
+        """Drops the levels grown: the next level() is the first of a new tree."""
         self.d = 0
-        return self._tree.run(stream)

@@ -5,6 +5,7 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <algorithm>
 #include <mutex>
 
 #include "hs_beam.h"
@@ -622,10 +623,14 @@ HS_API size_t hs_beam_step_workspace_size(int B, int W, int K, int64_t V, int dt
 
 namespace {
 
-// Whether [a, a + na) and [b, b + nb) share a byte (an absent buffer shares none).
-bool overlap(const void* a, uint64_t na, const void* b, uint64_t nb) {
-  const uint64_t x = (uint64_t)(uintptr_t)a, y = (uint64_t)(uintptr_t)b;
-  return a && b && x < y + nb && y < x + na;
+struct Bytes {
+  const void* p;  // NULL: an absent buffer, which shares none
+  uint64_t n;
+};
+
+bool overlap(const Bytes& a, const Bytes& b) {
+  const uint64_t x = (uint64_t)(uintptr_t)a.p, y = (uint64_t)(uintptr_t)b.p;
+  return a.p && b.p && x < y + b.n && y < x + a.n;
 }
 
 }  // namespace
@@ -647,20 +652,6 @@ HS_API int hs_beam_step(const hs_beam_args* a, void* stream) {
   if (a->score_stride < a->W) return fail(HS_ERR_SHAPE, "score_stride must be >= W");
   if (!(a->temperature >= 1e-30 && a->temperature <= 1e30))
     return fail(HS_ERR_TEMPERATURE, "temperature must be in [1e-30, 1e30] (got %g)", a->temperature);
-  const bool own = a->K == a->W && a->score_stride == a->W;  // an output may be its input
-  const uint64_t in = (uint64_t)(a->B - 1) * (uint64_t)a->score_stride + (uint64_t)a->W;
-  const uint64_t out = (uint64_t)a->B * (uint64_t)a->K;
-  struct {
-    const void* p;
-    uint64_t bytes;
-  } ins[] = {{a->score, 4 * in}, {a->done, in}},
-    outs[] = {{a->out_score, 4 * out}, {a->out_done, out}, {a->out_parent, 4 * out},
-              {a->out_token, 4 * out}};
-  for (int i = 0; i < 2; ++i)
-    for (int o = 0; o < 4; ++o)
-      if (overlap(ins[i].p, ins[i].bytes, outs[o].p, outs[o].bytes) &&
-          !(own && i == o && ins[i].p == outs[o].p))
-        return fail(HS_ERR_ARG, "an output overlaps score or done");
   hs::BeamGeom g;
   if (!hs::beam_geom(a->B, a->W, a->K, a->V, a->dtype, &g))
     return fail(HS_ERR_LIMIT, "V = %lld is beyond the limit of %lld logits per row", (long long)a->V,
@@ -671,25 +662,27 @@ HS_API int hs_beam_step(const hs_beam_args* a, void* stream) {
     return fail(HS_ERR_WORKSPACE, "workspace too small: %zu < %zu bytes", a->workspace_bytes, need);
   if (((uintptr_t)a->workspace & 255) != 0)
     return fail(HS_ERR_ALIGN, "workspace must be 256-byte aligned");
+  const bool own = a->K == a->W && a->score_stride == a->W;  // an output may be its input
+  const uint64_t in = (uint64_t)(a->B - 1) * (uint64_t)a->score_stride + (uint64_t)a->W;
+  const uint64_t out = (uint64_t)a->B * (uint64_t)a->K;
+  const __int128 es = elem_bytes(a->dtype);
+  const __int128 read = es * ((__int128)(a->B - 1) * a->logits.stride_b +
+                              (__int128)(a->W - 1) * a->logits.stride_k + a->V);
+  const Bytes ins[] = {{a->score, 4 * in}, {a->done, in},
+                       {a->logits.ptr, (uint64_t)std::min(read, (__int128)1 << 62)}};
+  const Bytes outs[] = {{a->out_score, 4 * out}, {a->out_done, out}, {a->out_parent, 4 * out},
+                        {a->out_token, 4 * out}, {a->workspace, need}};
+  for (int o = 0; o < 5; ++o) {
+    for (int i = 0; i < 3; ++i)
+      if (overlap(ins[i], outs[o]) && !(own && i < 2 && i == o && ins[i].p == outs[o].p))
+        return fail(HS_ERR_ARG, "an output or the workspace overlaps an input");
+    for (int i = 0; i < o; ++i)
+      if (overlap(outs[i], outs[o])) return fail(HS_ERR_ARG, "two outputs, or one and the workspace, overlap");
+  }
   rc = hs::launch_beam_step(g, *a, (hipStream_t)stream);
   if (rc) return fail(rc, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
   return ok();
 }
-
-namespace {
-
-// The bytes that `beams` beams of every query span in a state's buffer, from its pointer; false where
-// they do not fit 62 bits.
-bool state_span(const hs_state& s, int B, int beams, int64_t sb, int64_t sw, int64_t sr, uint64_t* n) {
-  const __int128 row = (__int128)s.units * s.unit;
-  const __int128 all = row + (__int128)(B - 1) * sb + (__int128)(beams - 1) * sw +
-                       (__int128)(s.rows - 1) * sr;
-  if (all >= ((__int128)1 << 62)) return false;
-  *n = (uint64_t)all;
-  return true;
-}
-
-}  // namespace
 
 HS_API int hs_beam_reorder(const hs_state* states, int n, int B, int W, int K,
                            const int32_t* parent, int64_t parent_stride, const int32_t* count,
@@ -711,29 +704,21 @@ HS_API int hs_beam_reorder(const hs_state* states, int n, int B, int W, int K,
       return fail(HS_ERR_SHAPE, "state %d: negative stride", i);
     uint64_t from = 0, to = 0;
     if (s.rows > INT32_MAX || s.units > ((int64_t)1 << 62) / s.unit ||
-        !state_span(s, B, W, s.src_stride_b, s.src_stride_w, s.src_stride_row, &from) ||
-        !state_span(s, B, K, s.dst_stride_b, s.dst_stride_w, s.dst_stride_row, &to))
+        !hs::state_span(s, B, W, s.src_stride_b, s.src_stride_w, s.src_stride_row, &from) ||
+        !hs::state_span(s, B, K, s.dst_stride_b, s.dst_stride_w, s.dst_stride_row, &to))
       return fail(HS_ERR_LIMIT, "state %d: too large", i);
     if (!hs::reorder_fits(s, B)) return fail(HS_ERR_LIMIT, "state %d: too many rows or bytes", i);
     // two slots' bytes must be apart where both are written
     const int64_t row = s.units * s.unit;
-    if (!hs::state_apart(s, B, K, row))
+    if (!hs::state_apart(s, B, s.src == s.dst ? std::max(W, K) : K, row))
       return fail(HS_ERR_SHAPE, "state %d: rows, slots or queries of dst share bytes", i);
-    if (s.src == s.dst) {
-      if (s.src_stride_b != s.dst_stride_b || s.src_stride_w != s.dst_stride_w ||
-          s.src_stride_row != s.dst_stride_row)
-        return fail(HS_ERR_ARG, "state %d: in place with other strides", i);
-      if (from > to) to = from;
-    }
-    for (int j = 0; j < n; ++j) {
-      const hs_state& o = states[j];
-      if (j == i && s.src == s.dst) continue;
-      uint64_t bytes = 0;
-      if (!state_span(o, B, W, o.src_stride_b, o.src_stride_w, o.src_stride_row, &bytes) ||
-          overlap(o.src, bytes, s.dst, to))
-        return fail(HS_ERR_ARG, "state %d: dst overlaps the src of state %d", i, j);
-    }
+    if (s.src == s.dst && (s.src_stride_b != s.dst_stride_b || s.src_stride_w != s.dst_stride_w ||
+                           s.src_stride_row != s.dst_stride_row))
+      return fail(HS_ERR_ARG, "state %d: in place with other strides", i);
   }
+  int bad = 0;
+  if (!hs::states_apart(states, n, B, W, K, parent, parent_stride, count, &bad))
+    return fail(HS_ERR_ARG, "state %d: dst overlaps another tensor of the call", bad);
   const int rc = hs::launch_reorder(states, n, B, W, K, parent, parent_stride, count, (hipStream_t)stream);
   if (rc) return fail(rc, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
   return ok();
@@ -750,6 +735,18 @@ HS_API int hs_draft_tree(const hs_tree_args* a, void* stream) {
                 a->M);
   if (!a->score || !a->parent || !a->token)
     return fail(HS_ERR_NULL, "score, parent and token are required");
+  const uint64_t in = 4ull * a->D * a->B * a->K, nodes = (uint64_t)a->B * a->M;
+  const Bytes ins[] = {{a->score, in}, {a->parent, in}, {a->token, in}};
+  const Bytes outs[] = {{a->node_token, 4 * nodes}, {a->node_parent, 4 * nodes},
+                        {a->node_depth, 4 * nodes}, {a->node_slot, 4 * nodes},
+                        {a->node_score, 4 * nodes}, {a->node_mask, 8 * nodes},
+                        {a->cand, 4 * nodes * a->K}, {a->count, 4ull * a->B}};
+  for (int o = 0; o < 8; ++o) {
+    for (const Bytes& i : ins)
+      if (overlap(i, outs[o])) return fail(HS_ERR_ARG, "an output overlaps an input");
+    for (int i = 0; i < o; ++i)
+      if (overlap(outs[i], outs[o])) return fail(HS_ERR_ARG, "two outputs overlap");
+  }
   const int rc = hs::launch_draft_tree(*a, (hipStream_t)stream);
   if (rc) return fail(rc, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
   return ok();

@@ -21,6 +21,13 @@ int launch_beam_step(const BeamGeom& g, const hs_beam_args& a, hipStream_t strea
 bool reorder_fits(const hs_state& s, int B);  // its workgroups are numbered with 31 bits
 // Whether the rows of a state's dst (B queries, K slots, `row` bytes a row) are apart from each other.
 bool state_apart(const hs_state& s, int B, int K, int64_t row);
+// The bytes that `beams` beams of every query span from a state's pointer; false where they do not fit
+// 62 bits.
+bool state_span(const hs_state& s, int B, int beams, int64_t sb, int64_t sw, int64_t sr, uint64_t* n);
+// Whether no dst of a call shares a byte with another tensor of it, or with parent or count (but its own src
+// in place). Every state is sound by itself. *bad: a state whose dst does.
+bool states_apart(const hs_state* states, int n, int B, int W, int K, const int32_t* parent,
+                  int64_t parent_stride, const int32_t* count, int* bad);
 int launch_reorder(const hs_state* states, int n, int B, int W, int K, const int32_t* parent,
                    int64_t parent_stride, const int32_t* count, hipStream_t stream);
 int launch_draft_tree(const hs_tree_args& a, hipStream_t stream);
@@ -53,35 +60,6 @@ __device__ inline uint32_t wave_or_bits(uint32_t x) {
                     __builtin_amdgcn_readlane((int)x, 32) | __builtin_amdgcn_readlane((int)x, 48));
 }
 
-// The largest x with at least n of the wave's keys >= x, bit by bit from the highest one on which
-// two keys differ: the n-th largest key, or, with fewer than n keys, at most the smallest (0 with
-// none). u[j] of every lane, j < nu (the same in every lane), 0 = no key. All lanes are active.
-template <int NU>
-__device__ inline uint64_t nth_largest(const uint64_t (&u)[NU], int nu, int n) {
-  uint32_t or_lo = 0, or_hi = 0, nand_lo = 0, nand_hi = 0;  // bits some key has, and some lacks
-#pragma unroll
-  for (int j = 0; j < NU; ++j)
-    if (j < nu && u[j] != 0) {
-      or_lo |= (uint32_t)u[j];
-      or_hi |= (uint32_t)(u[j] >> 32);
-      nand_lo |= ~(uint32_t)u[j];
-      nand_hi |= ~(uint32_t)(u[j] >> 32);
-    }
-  const uint64_t some = ((uint64_t)wave_or_bits(or_hi) << 32) | wave_or_bits(or_lo);
-  uint64_t open = some & (((uint64_t)wave_or_bits(nand_hi) << 32) | wave_or_bits(nand_lo));
-  uint64_t x = some & ~open;  // the bits that every key has
-  while (open) {
-    const uint64_t bit = 1ull << (63 - __builtin_clzll(open));
-    open &= ~bit;
-    int c = 0;
-#pragma unroll
-    for (int j = 0; j < NU; ++j)
-      if (j < nu) c += __builtin_popcountll(__ballot(u[j] >= (x | bit)));
-    if (c >= n) x |= bit;
-  }
-  return x;
-}
-
 __device__ inline int wave_sum_i(int x) {
   x += dpp_i<0xB1>(x);
   x += dpp_i<0x4E>(x);
@@ -91,7 +69,7 @@ __device__ inline int wave_sum_i(int x) {
          __builtin_amdgcn_readlane(x, 32) + __builtin_amdgcn_readlane(x, 48);
 }
 
-// Sum and maximum of one fp64 value per lane, the same in every lane.
+// The sum of one fp64 value per lane, the same in every lane.
 template <int CTRL>
 __device__ inline double dpp_d(double v) {
   const uint64_t x = (uint64_t)__double_as_longlong(v);
@@ -112,14 +90,6 @@ __device__ inline double wave_sum_d(double v) {
   v += dpp_d<0x140>(v);
   return (lane_d(v, 0) + lane_d(v, 16)) + (lane_d(v, 32) + lane_d(v, 48));
 }
-__device__ inline double wave_max_d(double v) {
-  v = fmax(v, dpp_d<0xB1>(v));
-  v = fmax(v, dpp_d<0x4E>(v));
-  v = fmax(v, dpp_d<0x141>(v));
-  v = fmax(v, dpp_d<0x140>(v));
-  return fmax(fmax(lane_d(v, 0), lane_d(v, 16)), fmax(lane_d(v, 32), lane_d(v, 48)));
-}
-
 // An fp32 value (no NaN) as an unsigned integer that orders like it, -0 as +0, and back (0 as +0).
 __device__ inline uint32_t ordered_of(float f) {
   const int32_t x = __float_as_int(f), m = x >> 31;

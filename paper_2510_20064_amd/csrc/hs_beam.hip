@@ -240,7 +240,8 @@ __global__ __launch_bounds__(kThreads) void hs_beam_rows_kernel(StepArgs A) {
 
 // ---- launch 2: the rows' normalisers and the K best ------------------------------------------------------
 
-// The n-th largest x >= 1 of C words in LDS, as nth_largest; `of` maps a place to its key (0: none).
+// The largest x that n of the C words in LDS reach, `of` mapping a place to its key (0: none): the n-th
+// largest key, where there are n.
 template <typename F>
 __device__ inline uint64_t nth_of(F of, int C, int n, int lane) {
   uint64_t x = 0;
@@ -553,7 +554,7 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
     }
     lds_wave_fence();
     if (hits > 64) {
-      if (lane == 0) atomicAdd(&s_count, kPairs);  // no room: the second way
+      if (lane == 0) atomicAdd(&s_count, kPairs + 1);  // no room: the second way
       break;
     }
     for (int p = 0; p < hits; p += 64 / E) {

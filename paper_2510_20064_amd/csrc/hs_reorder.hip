@@ -3,6 +3,7 @@
 // loads come before its first store and no other thread touches those bytes, so a tensor can be
 // reordered in place whatever the parents are (cycles, one beam continued by many), with no second
 // buffer. Bound by HBM: every byte that changes hands is read once and written once.
+#include <algorithm>
 #include <utility>
 
 #include "hs_beam.h"
@@ -186,19 +187,147 @@ bool reorder_fits(const hs_state& s, int B) {
   return wgs < ((unsigned __int128)1 << 31);
 }
 
-// Three nested strides over rows: sorted, each must step over everything inside it.
+namespace {
+
+// What a call reads or writes of one tensor: rows of `row` bytes, along up to three strides.
+struct Region {
+  uint64_t at, end;  // its bytes lie in [at, end)
+  int state;         // -1: parent, count
+  bool writes;
+  int nd;
+  int64_t stride[3], n[3], row;  // ascending; none of a single row
+
+  Region() {}
+  Region(const void* p, int state, bool writes, int64_t row, int64_t sb, int64_t nb, int64_t sw,
+         int64_t nw, int64_t sr, int64_t nr)
+      : at((uint64_t)(uintptr_t)p), state(state), writes(writes), nd(0), row(row) {
+    const int64_t all[3][2] = {{sb, nb}, {sw, nw}, {sr, nr}};
+    for (const auto& d : all) {
+      if (d[1] == 1) continue;
+      int i = nd++;
+      for (; i > 0 && stride[i - 1] > d[0]; --i) {
+        stride[i] = stride[i - 1];
+        n[i] = n[i - 1];
+      }
+      stride[i] = d[0];
+      n[i] = d[1];
+    }
+    end = at + (uint64_t)extent(nd);
+  }
+  // The bytes that the first l strides span.
+  __int128 extent(int l) const {
+    __int128 e = row;
+    for (int i = 0; i < l; ++i) e += (__int128)stride[i] * (n[i] - 1);
+    return e;
+  }
+  // Each stride steps over everything inside it: no two rows share a byte.
+  bool nested() const {
+    for (int i = 0; i < nd; ++i)
+      if (stride[i] < extent(i)) return false;
+    return true;
+  }
+  bool same_strides(const Region& o) const {
+    return nd == o.nd && std::equal(stride, stride + nd, o.stride);
+  }
+};
+
+// Whether a row of a and one of b, which starts p bytes further on, share a byte. Both nested, with the same
+// strides: only the two steps of the largest stride that leave less than itself between the two can
+// bring them together, and so on inside.
+bool meet(const Region& a, const Region& b, int l, __int128 p) {
+  if (l == 0) return p < a.row && -p < b.row;
+  const int64_t s = a.stride[l - 1];
+  const __int128 down = p >= 0 ? p / s : -((-p + s - 1) / s);  // rounded down
+  for (__int128 i = down; i <= down + 1; ++i)  // steps of a less steps of b
+    if (i < a.n[l - 1] && -i < b.n[l - 1] && meet(a, b, l - 1, p - i * s)) return true;
+  return false;
+}
+
+// Regions in the order of `at`, each taken as the bytes that its first l strides span (all: its span):
+// the state of a written one that shares some with another, or -1.
+int first_shared(const Region* r, int m, bool all, int l) {
+  __int128 any = 0, written = 0;  // ends so far
+  int writer = -1;
+  for (int i = 0; i < m; ++i) {
+    const __int128 at = r[i].at, end = all ? (__int128)r[i].end : at + r[i].extent(l);
+    if (at < written) return r[writer].state;
+    if (r[i].writes && at < any) return r[i].state;
+    any = std::max(any, end);
+    if (r[i].writes && end > written) {
+      written = end;
+      writer = i;
+    }
+  }
+  return -1;
+}
+
+// The same for regions whose spans overlap, exactly: tensors that lie between each other's rows, as slices
+// of one buffer do, are apart.
+int shared_bytes(const Region* r, int m) {
+  for (int i = 0; i < m; ++i)
+    if (!r[i].nested() || !r[i].same_strides(r[0])) return first_shared(r, m, true, 0);
+  const int nd = r[0].nd;
+  for (int l = 0; l < nd; ++l) {  // all of them side by side inside one step of every stride from l on
+    __int128 most = 0;  // the bytes of a step
+    for (int i = 0; i < m; ++i)
+      most = std::max(most, (__int128)r[i].at - (__int128)r[0].at + r[i].extent(l));
+    bool fits = true;
+    for (int q = l; q < nd; ++q) {
+      int64_t n = 1;
+      for (int i = 0; i < m; ++i) n = std::max(n, r[i].n[q]);
+      fits = fits && r[0].stride[q] >= most;
+      most += (__int128)r[0].stride[q] * (n - 1);
+    }
+    if (fits && first_shared(r, m, false, l) < 0) return -1;
+  }
+  for (int i = 0; i < m; ++i)
+    for (int j = i + 1; j < m; ++j)
+      if ((r[i].writes || r[j].writes) &&
+          meet(r[i], r[j], nd, (__int128)r[j].at - (__int128)r[i].at))
+        return r[i].writes ? r[i].state : r[j].state;
+  return -1;
+}
+
+}  // namespace
+
 bool state_apart(const hs_state& s, int B, int K, int64_t row) {
-  struct {
-    int64_t stride, n;
-  } d[3] = {{s.dst_stride_b, B}, {s.dst_stride_w, K}, {s.dst_stride_row, s.rows}};
-  for (int i = 0; i < 3; ++i)
-    for (int j = i + 1; j < 3; ++j)
-      if (d[j].stride < d[i].stride) std::swap(d[i], d[j]);
-  __int128 inner = row;
-  for (int i = 0; i < 3; ++i) {
-    if (d[i].n == 1) continue;
-    if (d[i].stride < inner) return false;
-    inner += (__int128)d[i].stride * (d[i].n - 1);
+  return Region(s.dst, 0, true, row, s.dst_stride_b, B, s.dst_stride_w, K, s.dst_stride_row, s.rows)
+      .nested();
+}
+
+bool state_span(const hs_state& s, int B, int beams, int64_t sb, int64_t sw, int64_t sr, uint64_t* n) {
+  const __int128 row = (__int128)s.units * s.unit;
+  const __int128 all = row + (__int128)(B - 1) * sb + (__int128)(beams - 1) * sw +
+                       (__int128)(s.rows - 1) * sr;
+  if (all >= ((__int128)1 << 62)) return false;
+  *n = (uint64_t)all;
+  return true;
+}
+
+bool states_apart(const hs_state* states, int n, int B, int W, int K, const int32_t* parent,
+                  int64_t parent_stride, const int32_t* count, int* bad) {
+  Region r[2 * HS_MAX_STATES + 2];
+  int m = 0;
+  for (int i = 0; i < n; ++i) {
+    const hs_state& s = states[i];
+    const int64_t row = s.units * s.unit;
+    const bool inplace = s.src == s.dst;
+    if (!inplace)
+      r[m++] = Region(s.src, i, false, row, s.src_stride_b, B, s.src_stride_w, W, s.src_stride_row, s.rows);
+    r[m++] = Region(s.dst, i, true, row, s.dst_stride_b, B, s.dst_stride_w, inplace ? std::max(W, K) : K,
+                    s.dst_stride_row, s.rows);
+  }
+  r[m++] = Region(parent, -1, false, 4 * (int64_t)K, 4 * parent_stride, B, 0, 1, 0, 1);
+  if (count) r[m++] = Region(count, -1, false, 4 * (int64_t)B, 0, 1, 0, 1, 0, 1);
+  std::sort(r, r + m, [](const Region& a, const Region& b) { return a.at < b.at; });
+  if (first_shared(r, m, true, 0) < 0) return true;
+  for (int i = 0; i < m;) {  // regions whose spans hang together
+    uint64_t end = r[i].end;
+    int j = i + 1;
+    for (; j < m && r[j].at < end; ++j) end = std::max(end, r[j].end);
+    *bad = first_shared(r + i, j - i, true, 0) < 0 ? -1 : shared_bytes(r + i, j - i);
+    if (*bad >= 0) return false;
+    i = j;
   }
   return true;
 }

@@ -2,6 +2,7 @@
 (the pointers are fakes, never dereferenced) and the binding's checks before the library is called."""
 import ctypes
 import os
+import random
 import re
 
 import pytest
@@ -72,6 +73,21 @@ def test_beam_step_overlaps():
     assert _step(done=FAKE << 13, out_token=FAKE << 13) == 10
 
 
+def test_beam_step_outputs_and_workspace_apart():
+    out, ws, lg = FAKE << 9, FAKE << 12, FAKE
+    assert _step(out_parent=out + 60) == 10                    # the last slot of the last query
+    assert _step(out_token=FAKE << 10) == 10                   # parent and token in one buffer
+    assert _step(out_done=out, done=FAKE << 13) == 10
+    assert _step(workspace=sc_page(out), out_score=sc_page(out) + 64) == 10
+    assert _step(score=ws + 4096) == 10                        # in the workspace
+    assert _step(out_score=lg + 2 * (16 * 151936) - 4) == 10   # the last logits
+    assert _step(workspace=lg + 256) == 10
+
+
+def sc_page(p):
+    return p // 4096 * 4096
+
+
 def _state(**kw):
     v = dict(src=FAKE, dst=FAKE, src_stride_b=8 * 64, src_stride_w=64, src_stride_row=0,
              dst_stride_b=8 * 64, dst_stride_w=64, dst_stride_row=0, rows=1, units=4, unit=16)
@@ -122,6 +138,65 @@ def test_beam_reorder_overlaps():
     assert _reorder([_state(src=far, dst=far << 4), _state(src=far << 4, dst=far << 8)]) == 10
 
 
+def test_beam_reorder_writes_apart():
+    far = FAKE << 4
+    assert _reorder([_state(dst=far), _state(src=FAKE << 6, dst=far)]) == 10       # one dst for two
+    assert _reorder([_state(dst=far), _state(src=FAKE << 6, dst=far + 1023)]) == 10
+    assert _reorder([_state(), _state()]) == 10                                    # one state twice
+    assert _reorder([_state()], parent=FAKE + 1020) == 10
+    assert _reorder([_state()], parent=FAKE - 60) == 10
+    assert _reorder([_state()], count=FAKE - 4) == 10
+    # in place the beams that are only read count too: of query 0 they are query 1's slots
+    assert _reorder([_state(src_stride_b=4 * 64, dst_stride_b=4 * 64)], K=4, stride=8) == 2
+
+
+def _bytes_of(at, strides, counts, row):
+    (sb, sw, sr), (nb, nw, nr) = strides, counts
+    starts = [at + b * sb + w * sw + r * sr for b in range(nb) for w in range(nw) for r in range(nr)]
+    return starts, {s + i for s in starts for i in range(row)}
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_beam_reorder_refuses_every_overlap(seed):
+    """Small random layouts, most of them slices of one buffer: whenever two tensors of a call share a
+    byte that one of them writes (found byte by byte), the call is refused. Sound calls are not made."""
+    rng = random.Random(seed)
+    base, asked = 1 << 20, 0
+
+    def strides(row):
+        out, step = [0, 0, 0], row * rng.randint(1, 4)
+        for d in rng.sample(range(3), 3):
+            out[d] = step + rng.choice([0, 0, rng.randint(0, 8)])
+            step = out[d] * rng.randint(1, 4)
+        return out
+
+    while asked < 1500:
+        B, W, K, unit = rng.randint(1, 3), rng.randint(1, 3), rng.randint(1, 3), rng.choice([1, 2, 4])
+        n, units, nr = rng.randint(1, 4), rng.randint(1, 3), rng.randint(1, 3)
+        shared = strides(units * unit)
+        states, reads, writes, ok = [], [], [], True
+        for _ in range(n):
+            row = units * unit
+            ss = shared if rng.random() < 0.8 else strides(row)
+            ds = shared if rng.random() < 0.8 else strides(row)
+            src, dst = base + rng.randint(0, 200), base + rng.randint(0, 200)
+            if rng.random() < 0.4:
+                dst = src
+            if dst == src:
+                ds = ss
+            _, r = _bytes_of(src, ss, (B, W, nr), row)
+            starts, w = _bytes_of(dst, ds, (B, max(W, K) if dst == src else K, nr), row)
+            ok = ok and len(w) == len(starts) * row and (dst == src or not (r & w))
+            states.append(hs.hs_state(src, dst, *ss, *ds, nr, units, unit))
+            reads.append(r)
+            writes.append(w)
+        ok = ok and not any(i != j and writes[i] & (writes[j] | reads[j])
+                            for i in range(n) for j in range(n))
+        if not ok:
+            asked += 1
+            assert _reorder(states, B=B, W=W, K=K, parent=base - 4096, stride=4) in (2, 10)
+
+
 def _tree(**kw):
     v = dict(score=FAKE, parent=FAKE, token=FAKE, D=7, B=2, K=10, M=61)
     v.update(kw)
@@ -142,6 +217,18 @@ def test_draft_tree_codes():
     assert _tree(B=65536) == 8
     for bad in ("score", "parent", "token"):
         assert _tree(**{bad: None}) == 1, bad
+
+
+def test_draft_tree_outputs_apart():
+    far = FAKE << 4
+    last = 4 * 7 * 2 * 10
+    for out, size in (("node_token", 4 * 2 * 61), ("node_mask", 8 * 2 * 61), ("cand", 4 * 2 * 61 * 10),
+                      ("count", 8)):
+        assert _tree(**{out: FAKE + last - 4}) == 10, out
+        assert _tree(**{out: FAKE - size + 4}) == 10, out
+    assert _tree(node_token=far, node_parent=far) == 10
+    assert _tree(node_depth=far, node_slot=far + 4 * 2 * 61 - 4) == 10
+    assert _tree(cand=far, count=far + 4 * 2 * 61 * 10 - 4) == 10
 
 
 # ---- the binding: host tensors, refused before the library is called -----------------------------

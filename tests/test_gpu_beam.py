@@ -188,6 +188,24 @@ def test_step_crowded_units():
         check_step(z.to(dt), scores(g, 2, 3), 16, V)
 
 
+@pytest.mark.parametrize("K", [1, 2])
+def test_step_one_wave_finds_too_many(K):
+    """Two units full of the largest logit, which one wave reads (units 0 and 16 of one row), and units
+    between them whose largest lies below the bound by less than the test for reading them tells: the
+    only entries are those that found no room at first."""
+    note("one wave K=%d" % K)
+    x = torch.zeros((1, 1, 17 * 256))
+    vec = x.view(-1, 4)
+    v = torch.arange(len(vec))
+    unit = v // 256 * 4 + v % 64 // 16   # of fp32: the vectors of 16 lanes, in each quarter of 256
+    for u in range(17):
+        if u in (0, 16):
+            vec[unit == u] = 1000.0
+        else:
+            vec[torch.nonzero(unit == u)[0, 0], 0] = 1000.0 - 5e-4
+    check_step(x, torch.full((1, 1), -1.0), K, x.shape[2])
+
+
 def test_step_many_queries():
     note("65535 queries")
     g = torch.Generator().manual_seed(73)
@@ -485,6 +503,40 @@ def test_reorder_many_tensors_of_mixed_widths():
     check_reorder(x, p)
 
 
+def test_reorder_slices_of_one_buffer():
+    """Tensors between each other's rows: the layers of a stacked cache, keys beside values, in place
+    and from one half of a buffer to the other."""
+    note("reorder slices")
+    g = torch.Generator().manual_seed(31)
+    B, W, L, H, T, D = 2, 5, 3, 4, 7, 6
+    p = torch.randint(0, W, (B, W), generator=g, dtype=torch.int32)
+    n = torch.tensor([3, 7], dtype=torch.int32)
+    up = p.long()[:, :, None].cuda()
+    for axis, count in ((3, n), (3, None)):
+        buf = ints(g, (B, W, L, H, 2, T, D), torch.int16)
+        want = buf.clone()
+        moved = buf[torch.arange(B, device="cuda")[:, None], up[:, :, 0]]
+        for b in range(B):
+            c = T if count is None else int(count[b])
+            want[b, ..., :c, :] = moved[b, ..., :c, :]
+        states = [buf[:, :, l, :, kv] for l in range(L) for kv in range(2)]
+        hs.beam_reorder(states, p.cuda(), count=None if count is None else count.cuda(), axis=axis)
+        assert torch.equal(buf, want)
+    buf = ints(g, (2, B, W, L, 11))
+    kept, src = buf.clone(), [buf[0, :, :, l] for l in range(L)]
+    hs.beam_reorder(src, p.cuda(), out=[buf[1, :, :, l] for l in range(L)])
+    assert torch.equal(buf[0], kept[0])
+    assert torch.equal(buf[1], kept[0][torch.arange(B, device="cuda")[:, None], up[:, :, 0]])
+    pair = ints(g, (B, W, 2, 9), torch.uint8)       # from one half of every beam to the other
+    kept = pair.clone()
+    hs.beam_reorder(pair[:, :, 0], p.cuda(), out=pair[:, :, 1])
+    assert torch.equal(pair[:, :, 0], kept[:, :, 0])
+    assert torch.equal(pair[:, :, 1], kept[:, :, 0][torch.arange(B, device="cuda")[:, None], up[:, :, 0]])
+    one = ints(g, (B, W, 12))
+    with pytest.raises(hs.HsError):
+        hs.beam_reorder([one, one], p.cuda())
+
+
 def test_reorder_offsets_past_32_bits():
     note("long caches")
     gib = 1 << 30
@@ -735,3 +787,87 @@ def test_beam_search_with_ends_and_histories():
         ref_last, ref_done = ref["token"], ref["done"]
     assert hist.cpu().tolist() == ref_hist
     assert ref_done.any()
+
+
+def _growth_inputs(g, B, W, depth, V, dt):
+    x = [rows(g, B, 1 if d == 0 else W, V, dt) for d in range(depth)]
+    return [v.cuda() for v in x], ints(g, (B, W, 33))
+
+
+def _grow(growth, xs, V, stream=None):
+    for x in xs:
+        growth.level(x, V=V, stream=stream)
+    return growth.tree(stream=stream)
+
+
+def test_growth_captured_and_replayed():
+    """A whole tree in one graph, states included; every replay against an eager growth."""
+    note("growth graph")
+    g = torch.Generator().manual_seed(59)
+    B, depth, W, K, M, V = 2, 4, 3, 8, 16, 3000
+    xs, st = _growth_inputs(g, B, W, depth, V, torch.bfloat16)
+    growth = hs.TreeGrowth(B, depth, W, K, M, states=[st], device="cuda")
+    _grow(growth, xs, V)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = _grow(growth, xs, V)
+    for seed in range(4):
+        new, s0 = _growth_inputs(torch.Generator().manual_seed(seed), B, W, depth, V, torch.bfloat16)
+        for a, b in zip(xs, new):
+            a.copy_(b)
+        st.copy_(s0)
+        graph.replay()
+        eager = hs.TreeGrowth(B, depth, W, K, M, states=[s0], device="cuda")
+        want = _grow(eager, new, V)
+        torch.cuda.synchronize()
+        assert torch.equal(st, s0)
+        assert all(torch.equal(out[k], want[k]) for k in want), seed
+
+
+def test_two_growths_on_two_streams_and_a_restart():
+    note("two growths")
+    g = torch.Generator().manual_seed(61)
+    B, depth, W, K, M = 2, 3, 4, 9, 12
+    main = torch.cuda.current_stream()
+    sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+    jobs = []
+    for V, dt in ((5000, torch.float16), (1201, torch.float32)):
+        xs, st = _growth_inputs(g, B, W, depth, V, dt)
+        jobs.append((xs, st, st.clone(), V, hs.TreeGrowth(B, depth, W, K, M, states=[st], device="cuda")))
+    jobs[0][4].level(jobs[1][0][0], V=1201)   # a tree that is given up, of another row length and type
+    with pytest.raises(ValueError):
+        jobs[0][4].tree()
+    jobs[0][4].restart()
+    jobs[0][1].copy_(jobs[0][2])
+    for s in sides:
+        s.wait_stream(main)
+    outs = [None, None]
+    for d in range(depth):
+        for (xs, _, _, V, growth), s in zip(jobs, sides):
+            growth.level(xs[d], V=V, stream=s)
+    for i, ((_, _, _, _, growth), s) in enumerate(zip(jobs, sides)):
+        outs[i] = growth.tree(stream=s)
+        main.wait_stream(s)
+    for (xs, st, s0, V, _), out in zip(jobs, outs):
+        eager = hs.TreeGrowth(B, depth, W, K, M, states=[s0], device="cuda")
+        want = _grow(eager, xs, V)
+        assert torch.equal(st, s0)
+        assert all(torch.equal(out[k], want[k]) for k in want)
+
+
+def test_calls_that_make_their_tensors_for_another_stream():
+    note("made for a stream")
+    g = torch.Generator().manual_seed(67)
+    V = 4000
+    x, s = rows(g, 2, 3, V, torch.bfloat16).cuda(), scores(g, 2, 3).cuda()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    outs = [hs.beam_step(x, s, 7, V=V, stream=side) for _ in range(3)]
+    with torch.cuda.stream(side):
+        grown_to = [torch.stack([o[k] for o in outs]) for k in ("score", "parent", "token")]
+    tree = hs.draft_tree(*grown_to, 9, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    want = hs.beam_step(x, s, 7, V=V)
+    assert all(torch.equal(o[k], want[k]) for o in outs for k in want)
+    ref = hs.draft_tree(*grown_to, 9)
+    assert all(torch.equal(tree[k], ref[k]) for k in ref)
