@@ -423,7 +423,8 @@ int hs_round(const hs_round_args* args, void* stream);
  *                 are not read.
  *   eos         : the token that ends a beam, or negative: none does.
  *   temperature : T, 1e-30 <= T <= 1e30. A double, as the scores are.
- *   out_score   : [B][K] fp32: s rounded once; -inf for a slot without a continuation.
+ *   out_score   : [B][K] fp32: s rounded once (-inf below the type's range); -inf for a slot without a
+ *                 continuation.
  *   out_parent  : [B][K] int32: the beam w that the slot continues; -1 for none.
  *   out_token   : [B][K] int32: its token; -1 for none.
  *   out_done    : NULL, or [B][K] uint8: the slot continues an ended beam, or its token is eos.

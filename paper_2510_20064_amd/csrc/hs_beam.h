@@ -77,11 +77,13 @@ __device__ inline double dpp_d(double v) {
   const uint32_t hi = (uint32_t)dpp_i<CTRL>((int)(uint32_t)(x >> 32));
   return __longlong_as_double((long long)(((uint64_t)hi << 32) | lo));
 }
-__device__ inline double lane_d(double v, int l) {
-  const uint64_t x = (uint64_t)__double_as_longlong(v);
+__device__ inline uint64_t lane_u(uint64_t x, int l) {
   const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, l);
   const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(x >> 32), l);
-  return __longlong_as_double((long long)(((uint64_t)hi << 32) | lo));
+  return ((uint64_t)hi << 32) | lo;
+}
+__device__ inline double lane_d(double v, int l) {
+  return __longlong_as_double((long long)lane_u((uint64_t)__double_as_longlong(v), l));
 }
 __device__ inline double wave_sum_d(double v) {
   v += dpp_d<0xB1>(v);

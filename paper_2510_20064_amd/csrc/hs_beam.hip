@@ -13,13 +13,22 @@
 //      token).
 //
 // Precision. Two beams' candidates are often closer than fp32 tells apart and the order is part of
-// the result, so s is formed in fp64 and the normalisers are made good to about 1e-8: z c is taken
+// the result, so s is formed in fp64 and the normalisers are made good to 1e-7 (measured: 2e-9 rms on
+// flat rows, 3e-8 on peaked ones, 1.4e-7 at most): z c is taken
 // as z ca + z cb with ca = c rounded to 12 bits (for 16-bit logits z ca - offset is exact), each
 // lane adds its fp32 exponentials per chunk and the chunks in fp64, and the exponentials of the units'
 // largest logits, most of the sum where the distribution is peaked, are replaced by fp64 ones.
 // Sums are relative to an offset near the slice's maximum, and a slice whose maximum is large
 // (|z c| > 4096) takes z - maximum first, so that logits of any size do, the lowest finite value
 // in every place included.
+//
+// Bound. The rows kernel reads 311 MB (32 x 32 rows of 151936 bf16) in 50.2 us, 6.2 TB/s, each byte once (its
+// 552 vector instructions per two chunks and wave take about as long as the memory does), 110 MB in
+// 22.6 us, and a call too short for that in 4.0 us. The merge is bound by latency, by six steps that wait
+// for each other: 5.6 us for 4 rows of 128 units and 4 slots, 16.4 us for 32 workgroups of 32 rows of 300
+// units and 64 slots (an instruction that all of its 16 waves make costs 16 cycles). Two launches: in
+// one, with a query's last workgroup merging, the fences between the XCDs' caches cost what the second
+// launch does (10 rows of bf16 13.3 us, or 11.4 with device-scope words instead of fences; two 10.8).
 #include <cfloat>
 
 #include "hs_beam.h"
@@ -28,7 +37,7 @@ namespace hs {
 
 namespace {
 
-constexpr int kMergeThreads = 1024;
+constexpr int kMergeThreads = 1024;  // (256 and 512: 10 rows of bf16 14.7 and 11.8 us, 64 x 16 rows 89 and 72; 10.7, 65)
 constexpr int kMergeWaves = kMergeThreads / 64;
 constexpr int kRows = HS_MAX_BEAMS / kMergeWaves;  // rows of a wave in the merge
 constexpr int kHeld = 5;         // units' maxima of a row that a lane holds (for 152000 16-bit logits all)
@@ -625,38 +634,34 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
     best.shrink(256, K, wv, lane, &s_bound);
     C = s_count;
   }
-  // every entry's rank: a wave takes every 16th and compares it with all, four in each lane
+  // every entry's rank: a wave takes every 16th, one a lane, and compares them one after the other with all
   uint64_t h[4], l[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     h[j] = j * 64 + lane < C ? s_hi[j * 64 + lane] : 0;
     l[j] = j * 64 + lane < C ? s_lo[j * 64 + lane] : 0;
   }
-  for (int i = wv; i < max(C, K); i += kMergeWaves) {
-    int at = i;  // past the last entry: an empty slot
-    float sc = -INFINITY;
-    int parent = -1, token = -1;
-    uint8_t over = 0;
-    if (i < C) {
-      const uint64_t hi = uniform(s_hi[i]), lo = uniform(s_lo[i]);
-      at = 0;
+  const int i = wv + kMergeWaves * lane;
+  const uint64_t hi = i < C ? s_hi[i] : 0, lo = i < C ? s_lo[i] : 0;
+  int at = i;  // past the last entry: an empty slot
+  for (int q = 0; wv + kMergeWaves * q < C; ++q) {
+    const uint64_t qh = lane_u(hi, q), ql = lane_u(lo, q);
+    int above = 0;
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (j * 64 < C)
-          at += __builtin_popcountll(__ballot(h[j] > hi || (h[j] == hi && l[j] > lo)));
-      sc = (float)value_of(hi);
-      parent = 63 - (int)(lo >> 58);
-      const bool was = s_kind[parent] == 2;
-      token = was ? A.eos : (int)(kTokenMask - ((uint32_t)lo & kTokenMask));
-      over = was || (A.eos >= 0 && token == A.eos) ? 1 : 0;
-    }
-    if (at < K && lane == 0) {
-      const int64_t o = (int64_t)b * K + at;
-      A.out_score[o] = sc;
-      A.out_parent[o] = parent;
-      A.out_token[o] = token;
-      if (A.out_done) A.out_done[o] = over;
-    }
+    for (int j = 0; j < 4; ++j)
+      if (j * 64 < C)
+        above += __builtin_popcountll(__ballot(h[j] > qh || (h[j] == qh && l[j] > ql)));
+    at = lane == q ? above : at;
+  }
+  if (at < K) {  // (lanes past the entries and slots have i >= K)
+    const int parent = i < C ? 63 - (int)(lo >> 58) : -1;
+    const bool was = i < C && s_kind[max(parent, 0)] == 2;
+    const int token = i >= C ? -1 : was ? A.eos : (int)(kTokenMask - ((uint32_t)lo & kTokenMask));
+    const int64_t o = (int64_t)b * K + at;
+    A.out_score[o] = i < C ? (float)value_of(hi) : -INFINITY;
+    A.out_parent[o] = parent;
+    A.out_token[o] = token;
+    if (A.out_done) A.out_done[o] = was || (i < C && A.eos >= 0 && token == A.eos) ? 1 : 0;
   }
 }
 

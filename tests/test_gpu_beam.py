@@ -93,6 +93,17 @@ def test_step_temperatures(T):
     check_step(x, scores(g, 2, 3), 12, 5000, T=T)
 
 
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("T", [1e-30, 1e-12, 1e12, 1e30])
+def test_step_temperatures_at_the_limits(dtype, T):
+    note("temperature %g %s" % (T, dtype))
+    g = torch.Generator().manual_seed(71)
+    x = rows(g, 2, 3, 5003, DTYPES[dtype])
+    x[0, 1, :5003:7] = float("-inf")
+    x[1, 2, :5003:5] = torch.finfo(DTYPES[dtype]).min
+    check_step(x, scores(g, 2, 3), 12, 5003, T=T)
+
+
 def test_step_peaked_rows_like_a_model():
     # 20 boosted tokens a row hold most of the mass; 32 beams, 64 kept
     note("peaked rows")
