@@ -477,7 +477,7 @@ int hs_beam_step(const hs_beam_args* args, void* stream);
  *   count  : NULL, or [B] int32 device: only the first count[b] units of each row are copied (clamped to
  *            [0, units]); what lies behind them is left as it was.
  * W         : beams in src; K: slots in dst, 1 .. HS_MAX_BEAMS each (in place the buffer holds
- *             max(W, K)). Any alignment; what is a multiple of 4 bytes throughout moves by 16 at once.
+ *             max(W, K)). Any alignment.
  * n         : tensors, 1 .. HS_MAX_STATES. One launch for every 32 of them.
  */
 typedef struct hs_state {

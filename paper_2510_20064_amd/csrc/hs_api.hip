@@ -707,7 +707,7 @@ HS_API int hs_beam_reorder(const hs_state* states, int n, int B, int W, int K,
         !hs::state_span(s, B, W, s.src_stride_b, s.src_stride_w, s.src_stride_row, &from) ||
         !hs::state_span(s, B, K, s.dst_stride_b, s.dst_stride_w, s.dst_stride_row, &to))
       return fail(HS_ERR_LIMIT, "state %d: too large", i);
-    if (!hs::reorder_fits(s, B)) return fail(HS_ERR_LIMIT, "state %d: too many rows or bytes", i);
+    if (!hs::reorder_fits(s, B, count != nullptr)) return fail(HS_ERR_LIMIT, "state %d: too many rows or bytes", i);
     // two slots' bytes must be apart where both are written
     const int64_t row = s.units * s.unit;
     if (!hs::state_apart(s, B, s.src == s.dst ? std::max(W, K) : K, row))

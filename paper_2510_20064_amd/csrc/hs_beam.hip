@@ -37,7 +37,7 @@ namespace hs {
 
 namespace {
 
-constexpr int kMergeThreads = 1024;  // (256 and 512: 10 rows of bf16 14.7 and 11.8 us, 64 x 16 rows 89 and 72; 10.7, 65)
+constexpr int kMergeThreads = 1024;  // (256, 512: 10 rows of bf16 14.7, 11.8 us, 32 x 32 rows 89, 72; 10.7, 65)
 constexpr int kMergeWaves = kMergeThreads / 64;
 constexpr int kRows = HS_MAX_BEAMS / kMergeWaves;  // rows of a wave in the merge
 constexpr int kHeld = 5;         // units' maxima of a row that a lane holds (for 152000 16-bit logits all)

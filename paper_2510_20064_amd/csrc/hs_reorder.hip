@@ -1,5 +1,5 @@
 // hs_beam_reorder: dst[b][j] = src[b][parent[b][j]] for many tensors in one launch. A thread owns one
-// word (16 bytes, or 1) of a row position and moves it for every slot of the query: all of its
+// word (16 bytes; at a row's end 1) of a row position and moves it for every slot of the query: all of its
 // loads come before its first store and no other thread touches those bytes, so a tensor can be
 // reordered in place whatever the parents are (cycles, one beam continued by many), with no second
 // buffer. Bound by HBM: every byte that changes hands is read once and written once.
@@ -13,6 +13,7 @@ namespace hs {
 namespace {
 
 constexpr int kStates = 32;  // tensors of one launch (its arguments stay below 4 KB)
+constexpr int kChunk = 1024;  // a wave's bytes of a row: 16 a lane
 constexpr int kFew = 4;      // ... where they are few: 3 KB less of arguments, 1 us of the host's time
 
 struct MoveState {
@@ -21,7 +22,8 @@ struct MoveState {
   int64_t ssb, ssw, ssr, dsb, dsw, dsr;
   int64_t units, unit;
   FastDiv div_chunks, div_rows;
-  int chunks, rows;  // workgroups per row, rows per query
+  int chunks, rows;  // waves per row, rows per query
+  int queries;
 };
 template <int STATES>
 struct MoveArgs {
@@ -33,30 +35,21 @@ struct MoveArgs {
   MoveState st[STATES];
 };
 
-// A thread's word of up to BYTES bytes at `at` of a buffer of `bytes` bytes: what lies outside is not
-// read (0) and not written, by the bounds of the buffer's descriptor.
-// STREAM: nontemporal.
+typedef unsigned int Vec16 __attribute__((ext_vector_type(4)));
+
+// A thread's 16 bytes, or one, at `at` of a buffer: what lies outside is not read (0) and not written, by the
+// bounds of the buffer's descriptor. STREAM: nontemporal.
 template <int BYTES, bool STREAM>
 struct Word;
 template <bool STREAM>
 struct Word<16, STREAM> {
-  typedef unsigned int T __attribute__((ext_vector_type(4)));
+  typedef Vec16 T;
   static constexpr int kHow = STREAM ? 2 : 0;  // the instructions' nt bit
   static __device__ T load(__amdgpu_buffer_rsrc_t r, int at) {
     return __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, kHow);
   }
   static __device__ void store(T x, __amdgpu_buffer_rsrc_t r, int at) {
     __builtin_amdgcn_raw_buffer_store_b128(x, r, at, 0, kHow);
-  }
-};
-template <>
-struct Word<4, false> {
-  typedef uint32_t T;
-  static __device__ T load(__amdgpu_buffer_rsrc_t r, int at) {
-    return __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0);
-  }
-  static __device__ void store(T x, __amdgpu_buffer_rsrc_t r, int at) {
-    __builtin_amdgcn_raw_buffer_store_b32(x, r, at, 0, 0);
   }
 };
 template <>
@@ -93,10 +86,37 @@ __device__ __forceinline__ void move_words(int mine, uint64_t src, uint64_t ssw,
     Wd::store(x[j], buffer(dst, dsw, j, __builtin_amdgcn_readlane(mine, j) >= 0), at);
 }
 
-// KMAX: at least K.
-template <int BYTES, int KMAX, bool STREAM, int STATES>
+// The same for 16 bytes at any address (a buffer's 16 bytes must be at a multiple of 4), without descriptors.
+// bytes: a multiple of 16 above 0. Eight slots of 8 x 8 rows of 513 x 66 bytes, 4 tensors, half of them moved:
+// 11.0 us, byte by byte 51; 1.7 GB of 1023 x 198: 284, 5.3 TB/s. For aligned rows the descriptors read less:
+// 1 GB 205 us, so 241.
+template <int KMAX, bool STREAM>
+__device__ __forceinline__ void move_any(int mine, uint64_t src, uint64_t ssw, uint64_t dst, uint64_t dsw,
+                                         int bytes, int at) {
+  typedef Vec16 Any __attribute__((aligned(1)));
+  typedef __attribute__((address_space(1))) Any* Ptr;
+  const int from = min(at, bytes - 16);  // a lane past the end, or a slot that stays, reads what is there
+  Vec16 x[KMAX];
+#pragma unroll
+  for (int j = 0; j < KMAX; ++j) {
+    const int p = max(__builtin_amdgcn_readlane(mine, j), 0);
+    const Ptr q = (Ptr)(src + (uint64_t)(uint32_t)p * ssw + (uint64_t)from);
+    if constexpr (STREAM) x[j] = __builtin_nontemporal_load(q);
+    else x[j] = *q;
+  }
+#pragma unroll
+  for (int j = 0; j < KMAX; ++j)
+    if (__builtin_amdgcn_readlane(mine, j) >= 0 && at < bytes) {
+      const Ptr q = (Ptr)(dst + (uint64_t)j * dsw + (uint64_t)at);
+      if constexpr (STREAM) __builtin_nontemporal_store((Any)x[j], q);
+      else *q = x[j];
+    }
+}
+
+// KMAX: at least K. ALIGNED: every row of the tensors starts at a multiple of 4 bytes.
+template <bool ALIGNED, int KMAX, bool STREAM, int STATES>
 __global__ __launch_bounds__(kThreads) void hs_reorder_kernel(MoveArgs<STATES> A) {
-  using Wd = Word<BYTES, STREAM>;
+  constexpr int BYTES = 16;
   int i = 0;
 #pragma unroll
   for (int j = 1; j < STATES; ++j) i += blockIdx.x >= A.first[j] ? 1 : 0;
@@ -110,53 +130,54 @@ __global__ __launch_bounds__(kThreads) void hs_reorder_kernel(MoveArgs<STATES> A
         first = A.first[j];
       }
   }
-  const uint32_t u = blockIdx.x - first;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const uint32_t u = (blockIdx.x - first) * kWaves + wave;
   const uint32_t br = fdiv(u, S.div_chunks);
   const int64_t chunk = u - br * (uint32_t)S.chunks;
   const int b = (int)fdiv(br, S.div_rows);
+  if (b >= S.queries) return;  // past the tensor's end
   const int64_t r = br - (uint32_t)b * (uint32_t)S.rows;
   int64_t units = S.units;
   if (A.count) {
     const int64_t c = A.count[b];
     units = c < 0 ? 0 : c < units ? c : units;
   }
-  const int64_t begin = chunk * kThreads * BYTES, left = units * S.unit - begin;
-  if (left <= 0) return;  // the whole workgroup
-  const int bytes = (int)(left < kThreads * BYTES ? left : kThreads * BYTES);
+  const int64_t begin = chunk * kChunk, left = units * S.unit - begin;
+  if (left <= 0) return;  // all of the wave
+  const int bytes = (int)(left < kChunk ? left : kChunk);
   const bool inplace = S.src == S.dst;
   // lane j: slot j's parent, -1 where nothing moves
-  const int lane = threadIdx.x & 63;
   int mine = lane < A.K ? A.parent[b * A.parent_stride + lane] : -1;
   if (mine >= A.W || (inplace && mine == lane)) mine = -1;
   // (the same in every lane, told to the compiler: descriptors live in scalar registers)
   const uint64_t src = uniform((uint64_t)(S.src + b * S.ssb + r * S.ssr + begin));
   const uint64_t dst = uniform((uint64_t)(S.dst + b * S.dsb + r * S.dsr + begin));
   const uint64_t ssw = uniform((uint64_t)S.ssw), dsw = uniform((uint64_t)S.dsw);
-  move_words<Wd, KMAX>(mine, src, ssw, dst, dsw, bytes / BYTES * BYTES,
-                       (int)threadIdx.x * BYTES);
-  if (BYTES == 16 && (bytes & 15) != 0)  // a row's last one to three dwords
-    move_words<Word<4, false>, KMAX>(mine, src, ssw, dst, dsw, bytes,
-                                     bytes / 16 * 16 + (int)threadIdx.x * 4);
+  const int whole = bytes / BYTES * BYTES, at = lane * BYTES;
+  if (ALIGNED) move_words<Word<BYTES, STREAM>, KMAX>(mine, src, ssw, dst, dsw, whole, at);
+  else if (whole > 0) move_any<KMAX, STREAM>(mine, src, ssw, dst, dsw, whole, at);
+  if (whole != bytes)  // a row's last bytes
+    move_words<Word<1, false>, KMAX>(mine, src, ssw, dst, dsw, bytes, whole + lane);
 }
 
-template <int BYTES, bool STREAM, int STATES>
+template <bool ALIGNED, bool STREAM, int STATES>
 void launch_slots(const MoveArgs<STATES>& A, uint32_t grid, hipStream_t st) {
-  if (A.K <= 8) hs_reorder_kernel<BYTES, 8, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
-  else if (A.K <= 16) hs_reorder_kernel<BYTES, 16, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
-  else if (A.K <= 32) hs_reorder_kernel<BYTES, 32, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
-  else hs_reorder_kernel<BYTES, 64, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
+  if (A.K <= 8) hs_reorder_kernel<ALIGNED, 8, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
+  else if (A.K <= 16) hs_reorder_kernel<ALIGNED, 16, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
+  else if (A.K <= 32) hs_reorder_kernel<ALIGNED, 32, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
+  else hs_reorder_kernel<ALIGNED, 64, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
 }
 
-template <int BYTES, bool STREAM>
+template <bool ALIGNED, bool STREAM>
 void launch_words(const MoveArgs<kStates>& A, uint32_t grid, hipStream_t st) {
   if (A.n > kFew) {
-    launch_slots<BYTES, STREAM, kStates>(A, grid, st);
+    launch_slots<ALIGNED, STREAM, kStates>(A, grid, st);
     return;
   }
   MoveArgs<kFew> few{A.n, A.W, A.K, A.parent_stride, A.parent, A.count, {}, {}};
   for (int j = 0; j < kFew; ++j) few.first[j] = A.first[j];
   for (int j = 0; j < A.n; ++j) few.st[j] = A.st[j];
-  launch_slots<BYTES, STREAM, kFew>(few, grid, st);
+  launch_slots<ALIGNED, STREAM, kFew>(few, grid, st);
 }
 
 // Slots' bytes of a call from which on its words are nontemporal. Four caches of 8 slots x 8 heads x 1024
@@ -164,27 +185,42 @@ void launch_words(const MoveArgs<kStates>& A, uint32_t grid, hipStream_t st) {
 // 23.3 and 23.0, 268 MB 51 and 46, 1.07 GB 183 and 166; 2.1 GB of 64 slots 404 and 379.
 constexpr __int128 kStreamBytes = (__int128)100 << 20;
 
-// The word a tensor moves by: 16 bytes where every pointer, stride and unit is a multiple of 4 (what the
-// loads and stores need), else 1.
-int word_of(const hs_state& s) {
+// Whether every row of a tensor starts at a multiple of 4 bytes.
+bool aligned(const hs_state& s) {
   const uint64_t all = (uint64_t)(uintptr_t)s.src | (uint64_t)(uintptr_t)s.dst |
                        (uint64_t)s.src_stride_b | (uint64_t)s.src_stride_w |
                        (uint64_t)s.src_stride_row | (uint64_t)s.dst_stride_b |
-                       (uint64_t)s.dst_stride_w | (uint64_t)s.dst_stride_row | (uint64_t)s.unit;
-  return (all & 3) == 0 ? 16 : 1;
+                       (uint64_t)s.dst_stride_w | (uint64_t)s.dst_stride_row;
+  return (all & 3) == 0;
 }
 
-uint64_t chunks_of(const hs_state& s, int word) {
-  const uint64_t bytes = (uint64_t)s.units * (uint64_t)s.unit, per = (uint64_t)kThreads * word;
-  return bytes / per + (bytes % per != 0);
+// Rows one behind the other, all of their units moved, are one row (8 tensors of 128 queries x 8 slots x 8
+// rows of 66 bytes: 34.8 us as 8 rows, 5.8 as one).
+hs_state in_one_row(const hs_state& s, bool counted) {
+  hs_state one = s;
+  if (!counted && s.src_stride_row == s.units * s.unit && s.dst_stride_row == s.src_stride_row) {
+    one.units *= s.rows;
+    one.rows = 1;
+    one.src_stride_row = one.dst_stride_row = 0;
+  }
+  return one;
+}
+
+// The waves of a row. Short rows share workgroups (64 queries x 64 rows of 512 bytes, counted: 11.8 us with a
+// workgroup for each, 5.9); of four waves on none does (rows of 34 waves, counted: 12.9 us shared, 11.2).
+uint64_t chunks_of(const hs_state& s) {
+  const uint64_t bytes = (uint64_t)s.units * (uint64_t)s.unit;
+  const uint64_t n = bytes / kChunk + (bytes % kChunk != 0);
+  return n < kWaves ? n : (n + kWaves - 1) / kWaves * kWaves;
 }
 
 }  // namespace
 
-bool reorder_fits(const hs_state& s, int B) {
-  const unsigned __int128 wgs = (unsigned __int128)chunks_of(s, word_of(s)) *
-                                (unsigned __int128)s.rows * (unsigned __int128)B;
-  return wgs < ((unsigned __int128)1 << 31);
+bool reorder_fits(const hs_state& state, int B, bool counted) {
+  const hs_state s = in_one_row(state, counted);
+  const unsigned __int128 waves = (unsigned __int128)chunks_of(s) *
+                                  (unsigned __int128)s.rows * (unsigned __int128)B;
+  return waves < ((unsigned __int128)1 << 31);
 }
 
 namespace {
@@ -337,7 +373,7 @@ int launch_reorder(const hs_state* states, int n, int B, int W, int K, const int
   __int128 all = 0;
   for (int i = 0; i < n; ++i) all += (__int128)B * K * states[i].rows * states[i].units * states[i].unit;
   const bool stream_past = all >= kStreamBytes;
-  for (int word = 16; word >= 1; word /= 16) {  // the tensors of one word width together
+  for (int odd = 0; odd < 2; ++odd) {  // the aligned tensors together, then the others
     int i = 0;
     while (i < n) {
       MoveArgs<kStates> A;
@@ -349,10 +385,10 @@ int launch_reorder(const hs_state* states, int n, int B, int W, int K, const int
       A.count = count;
       uint64_t grid = 0;
       for (; i < n && A.n < kStates; ++i) {
-        const hs_state& s = states[i];
-        if (word_of(s) != word) continue;
-        const uint64_t chunks = chunks_of(s, word);
-        const uint64_t wgs = chunks * (uint64_t)s.rows * (uint64_t)B;
+        const hs_state s = in_one_row(states[i], count != nullptr);
+        if (aligned(s) == (odd != 0)) continue;
+        const uint64_t chunks = chunks_of(s);
+        const uint64_t wgs = (chunks * (uint64_t)s.rows * (uint64_t)B + kWaves - 1) / kWaves;
         if (grid + wgs >= (1ull << 31)) break;
         A.first[A.n] = (uint32_t)grid;
         MoveState& m = A.st[A.n++];
@@ -368,15 +404,17 @@ int launch_reorder(const hs_state* states, int n, int B, int W, int K, const int
         m.unit = s.unit;
         m.chunks = (int)chunks;
         m.rows = (int)s.rows;
+        m.queries = B;
         m.div_chunks = make_fastdiv((uint32_t)chunks);
         m.div_rows = make_fastdiv((uint32_t)s.rows);
         grid += wgs;
       }
       if (A.n == 0) break;
       for (int j = A.n; j < kStates; ++j) A.first[j] = 0xFFFFFFFFu;
-      if (word == 16 && stream_past) launch_words<16, true>(A, (uint32_t)grid, stream);
-      else if (word == 16) launch_words<16, false>(A, (uint32_t)grid, stream);
-      else launch_words<1, false>(A, (uint32_t)grid, stream);
+      if (!odd && stream_past) launch_words<true, true>(A, (uint32_t)grid, stream);
+      else if (!odd) launch_words<true, false>(A, (uint32_t)grid, stream);
+      else if (stream_past) launch_words<false, true>(A, (uint32_t)grid, stream);
+      else launch_words<false, false>(A, (uint32_t)grid, stream);
       if (hipGetLastError() != hipSuccess) return HS_ERR_HIP;
     }
   }

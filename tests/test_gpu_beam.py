@@ -514,6 +514,50 @@ def test_reorder_many_tensors_of_mixed_widths():
     check_reorder(x, p)
 
 
+@pytest.mark.parametrize("seed", range(24))
+def test_reorder_random_layouts(seed):
+    """Caches of any alignment: odd dims, odd lengths, odd starts, padded rows; every byte around them."""
+    rng = np.random.default_rng(2000 + seed)
+    g = torch.Generator().manual_seed(2000 + seed)
+    dtype = [torch.uint8, torch.float16, torch.int32][seed % 3]
+    B, W, H = int(rng.integers(1, 4)), int(rng.integers(1, 20)), int(rng.integers(1, 4))
+    inplace = bool(rng.integers(2))
+    K = W if inplace else int(rng.integers(1, 20))
+    T, D = int(rng.choice([1, 2, 7, 30, 61, 130])), int(rng.choice([1, 3, 8, 33, 64, 100]))
+    pad, off = int(rng.integers(0, 3)), int(rng.integers(0, 5))
+    counted = bool(rng.integers(2))
+    note("layout seed=%d %s B=%d W=%d K=%d H=%d T=%d D=%d pad=%d off=%d count=%d" %
+         (seed, dtype, B, W, K, H, T, D, pad, off, counted))
+
+    def cache(n, start):
+        flat = ints(g, (start + B * n * H * (T + pad) * D + 3,)).to(dtype)
+        return flat, flat[start:start + B * n * H * (T + pad) * D].view(B, n, H, T + pad, D)[:, :, :, :T]
+
+    tensors = [(cache(W, off + i), None if inplace else cache(K, 2 * i + 1)) for i in range(3)]
+    parent = torch.randint(-1, W + 1, (B, K), generator=g, dtype=torch.int32)
+    count = torch.randint(-1, T + 2, (B,), generator=g, dtype=torch.int32) if counted else None
+    want = []
+    for (sf, sv), d in tensors:
+        df, dv = (sf, sv) if d is None else d
+        ref = df.clone()
+        rv = ref[dv.storage_offset():].as_strided(dv.shape, dv.stride())
+        for b in range(B):
+            n = T if count is None else min(max(int(count[b]), 0), T)
+            for j in range(K):
+                p = int(parent[b, j])
+                if 0 <= p < W:
+                    rv[b, j, :, :n] = sv[b, p, :, :n]
+        want.append(ref)
+    kept = [sf.clone() for (sf, _), _ in tensors]
+    hs.beam_reorder([sv for (_, sv), _ in tensors], parent.cuda(),
+                    count=None if count is None else count.cuda(), axis=3,
+                    out=None if inplace else [d[1] for _, d in tensors])
+    for ((sf, _), d), ref, was in zip(tensors, want, kept):
+        assert torch.equal(sf if d is None else d[0], ref)
+        if d is not None:
+            assert torch.equal(sf, was)
+
+
 def test_reorder_slices_of_one_buffer():
     """Tensors between each other's rows: the layers of a stacked cache, keys beside values, in place
     and from one half of a buffer to the other."""
