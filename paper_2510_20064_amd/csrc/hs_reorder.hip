@@ -4,7 +4,7 @@
 // reordered in place whatever the parents are (cycles, one beam continued by many), with no second
 // buffer. Bound by HBM: every byte that changes hands is read once and written once.
 #include <algorithm>
-#include <utility>
+#include <type_traits>
 
 #include "hs_beam.h"
 
@@ -13,17 +13,21 @@ namespace hs {
 namespace {
 
 constexpr int kStates = 32;  // tensors of one launch (its arguments stay below 4 KB)
-constexpr int kChunk = 1024;  // a wave's bytes of a row: 16 a lane
 constexpr int kFew = 4;      // ... where they are few: 3 KB less of arguments, 1 us of the host's time
+constexpr int kChunk = 1024;             // a wave's bytes of a row: 16 a lane
+constexpr int kPiece = kWaves * kChunk;  // a workgroup's
+constexpr int kSpan = 4;                 // pieces of a workgroup where few slots may move,
+constexpr int kWideSlots = 8;            // in calls of at most so many slots
 
 struct MoveState {
   const char* src;
   char* dst;
   int64_t ssb, ssw, ssr, dsb, dsw, dsr;
   int64_t units, unit;
-  FastDiv div_chunks, div_rows;
-  int chunks, rows;  // waves per row, rows per query
+  FastDiv div_parts, div_rows;
+  int parts, rows;  // workgroups per row (where rows share them: waves), rows per query
   int queries;
+  int span;  // pieces of a workgroup: 1 or kSpan; 0: rows share workgroups
 };
 template <int STATES>
 struct MoveArgs {
@@ -37,86 +41,118 @@ struct MoveArgs {
 
 typedef unsigned int Vec16 __attribute__((ext_vector_type(4)));
 
-// A thread's 16 bytes, or one, at `at` of a buffer: what lies outside is not read (0) and not written, by the
-// bounds of the buffer's descriptor. STREAM: nontemporal.
-template <int BYTES, bool STREAM>
-struct Word;
-template <bool STREAM>
-struct Word<16, STREAM> {
-  typedef Vec16 T;
-  static constexpr int kHow = STREAM ? 2 : 0;  // the instructions' nt bit
-  static __device__ T load(__amdgpu_buffer_rsrc_t r, int at) {
-    return __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, kHow);
-  }
-  static __device__ void store(T x, __amdgpu_buffer_rsrc_t r, int at) {
-    __builtin_amdgcn_raw_buffer_store_b128(x, r, at, 0, kHow);
-  }
-};
-template <>
-struct Word<1, false> {
-  typedef uint8_t T;
-  static __device__ T load(__amdgpu_buffer_rsrc_t r, int at) {
-    return __builtin_amdgcn_raw_buffer_load_b8(r, at, 0, 0);
-  }
-  static __device__ void store(T x, __amdgpu_buffer_rsrc_t r, int at) {
-    __builtin_amdgcn_raw_buffer_store_b8(x, r, at, 0, 0);
-  }
-};
+// A thread's 16 bytes, or one, at byte `at` of `bytes` bytes from an address on that is the same in all lanes:
+// what lies outside is not read and not written. STREAM: nontemporal.
+// By the bounds of a buffer's descriptor; 16 bytes must then be at a multiple of 4.
 constexpr int kRawBuffer = 0x00020000;  // a descriptor's last word: plain 32-bit data
-
-// Moves the word at byte `at` < bytes of every slot, KMAX of them at most: every slot's word is in a
-// register between the loads and the stores. A slot that moves nothing (mine of its lane < 0) has a
-// descriptor of no bytes instead of a branch, so all loads go out together.
-template <typename Wd, int KMAX>
-__device__ __forceinline__ void move_words(int mine, uint64_t src, uint64_t ssw, uint64_t dst,
-                                           uint64_t dsw, int bytes, int at) {
-  auto buffer = [&](uint64_t base, uint64_t stride, int w, bool some) {
-    return __builtin_amdgcn_make_buffer_rsrc(
-        reinterpret_cast<void*>(uniform(base + (uint64_t)(uint32_t)w * stride)), 0,
-        (int)uniform(some ? (uint32_t)bytes : 0u), kRawBuffer);
-  };
-  typename Wd::T x[KMAX];
-#pragma unroll
-  for (int j = 0; j < KMAX; ++j) {
-    const int p = __builtin_amdgcn_readlane(mine, j);
-    x[j] = Wd::load(buffer(src, ssw, max(p, 0), p >= 0), at);
-  }
-#pragma unroll
-  for (int j = 0; j < KMAX; ++j)
-    Wd::store(x[j], buffer(dst, dsw, j, __builtin_amdgcn_readlane(mine, j) >= 0), at);
-}
-
-// The same for 16 bytes at any address (a buffer's 16 bytes must be at a multiple of 4), without descriptors.
-// bytes: a multiple of 16 above 0. Eight slots of 8 x 8 rows of 513 x 66 bytes, 4 tensors, half of them moved:
-// 11.0 us, byte by byte 51; 1.7 GB of 1023 x 198: 284, 5.3 TB/s. For aligned rows the descriptors read less:
-// 1 GB 205 us, so 241.
-template <int KMAX, bool STREAM>
-__device__ __forceinline__ void move_any(int mine, uint64_t src, uint64_t ssw, uint64_t dst, uint64_t dsw,
-                                         int bytes, int at) {
+struct Buffer {
+  __amdgpu_buffer_rsrc_t r;
+  __device__ Buffer(uint64_t base, int bytes)
+      : r(__builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(uniform(base)), 0,
+                                            (int)uniform((uint32_t)bytes), kRawBuffer)) {}
+};
+template <bool STREAM>
+struct Aligned : Buffer {
+  typedef Vec16 T;
+  static constexpr int kBytes = 16, kHow = STREAM ? 2 : 0;  // the instructions' nt bit
+  __device__ Aligned(uint64_t base, int bytes) : Buffer(base, bytes) {}
+  __device__ T load(int at) const { return __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, kHow); }
+  __device__ void store(T x, int at) const { __builtin_amdgcn_raw_buffer_store_b128(x, r, at, 0, kHow); }
+};
+struct Byte : Buffer {
+  typedef uint8_t T;
+  static constexpr int kBytes = 1;
+  __device__ Byte(uint64_t base, int bytes) : Buffer(base, bytes) {}
+  __device__ T load(int at) const { return __builtin_amdgcn_raw_buffer_load_b8(r, at, 0, 0); }
+  __device__ void store(T x, int at) const { __builtin_amdgcn_raw_buffer_store_b8(x, r, at, 0, 0); }
+};
+// At any address, without a descriptor; 16 bytes there can be read also where bytes is 0. For aligned rows the
+// descriptors read less: 1 GB 205 us, so 241.
+template <bool STREAM>
+struct Anywhere {
+  typedef Vec16 T;
   typedef Vec16 Any __attribute__((aligned(1)));
   typedef __attribute__((address_space(1))) Any* Ptr;
-  const int from = min(at, bytes - 16);  // a lane past the end, or a slot that stays, reads what is there
-  Vec16 x[KMAX];
-#pragma unroll
-  for (int j = 0; j < KMAX; ++j) {
-    const int p = max(__builtin_amdgcn_readlane(mine, j), 0);
-    const Ptr q = (Ptr)(src + (uint64_t)(uint32_t)p * ssw + (uint64_t)from);
-    if constexpr (STREAM) x[j] = __builtin_nontemporal_load(q);
-    else x[j] = *q;
+  static constexpr int kBytes = 16;
+  uint64_t base;
+  int bytes;
+  __device__ Anywhere(uint64_t base, int bytes) : base(base), bytes(bytes) {}
+  __device__ T load(int at) const {
+    const Ptr q = (Ptr)(base + (uint64_t)max(min(at, bytes - 16), 0));
+    if constexpr (STREAM) return __builtin_nontemporal_load(q);
+    else return *q;
   }
+  __device__ void store(T x, int at) const {
+    if (at >= bytes) return;
+    const Ptr q = (Ptr)(base + (uint64_t)at);
+    if constexpr (STREAM) __builtin_nontemporal_store((Any)x, q);
+    else *q = x;
+  }
+};
+
+struct Slots {
+  uint64_t src, dst, ssw, dsw;
+  int mine;        // lane j: slot j's parent, -1 where nothing moves
+  uint64_t moves;  // the slots that move
+};
+
+// A lane's words at `at`, `at` + step, ... (COUNT of them) before byte `bytes`, of M slots: the slots 0 to M - 1, or,
+// PICK, the M first that move. A slot that moves nothing has no bytes instead of a branch, so that all loads
+// go out together.
+template <typename Wd, int M, int COUNT, bool PICK>
+struct Tile {
+  typename Wd::T x[M][COUNT];
+
+  template <bool LOAD>
+  __device__ __forceinline__ void pass(const Slots& s, int at, int step, int bytes) {
+    uint64_t rest = s.moves;
 #pragma unroll
-  for (int j = 0; j < KMAX; ++j)
-    if (__builtin_amdgcn_readlane(mine, j) >= 0 && at < bytes) {
-      const Ptr q = (Ptr)(dst + (uint64_t)j * dsw + (uint64_t)at);
-      if constexpr (STREAM) __builtin_nontemporal_store((Any)x[j], q);
-      else *q = x[j];
+    for (int q = 0; q < M; ++q) {
+      const int j = PICK ? __builtin_ctzll(rest | 1ull << 63) : q, p = __builtin_amdgcn_readlane(s.mine, j);
+      const bool on = PICK ? rest != 0 : p >= 0;
+      const Wd w(LOAD ? s.src + (uint64_t)(uint32_t)(on ? p : 0) * s.ssw : s.dst + (uint64_t)j * s.dsw,
+                 on ? bytes : 0);
+#pragma unroll
+      for (int c = 0; c < COUNT; ++c) {
+        if constexpr (LOAD) x[q][c] = w.load(at + c * step);
+        else w.store(x[q][c], at + c * step);
+      }
+      rest &= rest - 1;
     }
+  }
+  __device__ __forceinline__ void load(const Slots& s, int at, int step, int bytes) {
+    pass<true>(s, at, step, bytes);
+  }
+  __device__ __forceinline__ void store(const Slots& s, int at, int step, int bytes) {
+    pass<false>(s, at, step, bytes);
+  }
+  // The loads all come before the stores.
+  __device__ __forceinline__ void move(const Slots& s, int at, int step, int bytes) {
+    load(s, at, step, bytes);
+    store(s, at, step, bytes);
+  }
+};
+
+// A lane's n words of each slot that moves: several at once where few do.
+template <typename Wd, int KMAX, bool WIDE>
+__device__ __forceinline__ void move_words(const Slots& s, int at, int n, int step, int bytes) {
+  if constexpr (WIDE) {
+    const int m = __builtin_popcountll(s.moves);
+    if (n > 2 && m <= KMAX / 4) {
+      Tile<Wd, KMAX / 4, kSpan, true>().move(s, at, step, bytes);
+    } else if (n > 1 && m <= KMAX / 2) {
+      for (int c = 0; c < n; c += 2) Tile<Wd, KMAX / 2, 2, true>().move(s, at + c * step, step, bytes);
+    } else {
+      for (int c = 0; c < n; ++c) Tile<Wd, KMAX, 1, false>().move(s, at + c * step, step, bytes);
+    }
+  } else {
+    Tile<Wd, KMAX, 1, false>().move(s, at, step, bytes);
+  }
 }
 
-// KMAX: at least K. ALIGNED: every row of the tensors starts at a multiple of 4 bytes.
-template <bool ALIGNED, int KMAX, bool STREAM, int STATES>
+// KMAX: at least K. WIDE: some tensor has a span above 1. ALIGNED: every row of the tensors starts at a multiple of 4 bytes.
+template <bool ALIGNED, int KMAX, bool WIDE, bool STREAM, int STATES>
 __global__ __launch_bounds__(kThreads) void hs_reorder_kernel(MoveArgs<STATES> A) {
-  constexpr int BYTES = 16;
   int i = 0;
 #pragma unroll
   for (int j = 1; j < STATES; ++j) i += blockIdx.x >= A.first[j] ? 1 : 0;
@@ -131,9 +167,11 @@ __global__ __launch_bounds__(kThreads) void hs_reorder_kernel(MoveArgs<STATES> A
       }
   }
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const uint32_t u = (blockIdx.x - first) * kWaves + wave;
-  const uint32_t br = fdiv(u, S.div_chunks);
-  const int64_t chunk = u - br * (uint32_t)S.chunks;
+  // a row of less than a workgroup's bytes has a wave for each of its chunks; a longer one has workgroups that
+  // move `span` pieces of kPiece bytes each, `parts` pieces apart
+  const uint32_t u = S.span == 0 ? (blockIdx.x - first) * kWaves + wave : blockIdx.x - first;
+  const uint32_t br = fdiv(u, S.div_parts);
+  const int64_t part = u - br * (uint32_t)S.parts;
   const int b = (int)fdiv(br, S.div_rows);
   if (b >= S.queries) return;  // past the tensor's end
   const int64_t r = br - (uint32_t)b * (uint32_t)S.rows;
@@ -142,30 +180,43 @@ __global__ __launch_bounds__(kThreads) void hs_reorder_kernel(MoveArgs<STATES> A
     const int64_t c = A.count[b];
     units = c < 0 ? 0 : c < units ? c : units;
   }
-  const int64_t begin = chunk * kChunk, left = units * S.unit - begin;
-  if (left <= 0) return;  // all of the wave
-  const int bytes = (int)(left < kChunk ? left : kChunk);
+  const int64_t all = units * S.unit, begin = S.span == 0 ? part * kChunk : part * kPiece + wave * kChunk;
+  if (all <= begin) return;  // all of the wave
+  // the wave's words end at `left` (that is below 2^31 where there is more than one), but for a row's last bytes
+  const int64_t left = (all & ~15ll) - begin;
+  const int span = WIDE && S.span > 1 ? S.span : 1, step = span > 1 ? S.parts * kPiece : kChunk;
+  const int n = span == 1 ? 1 : 1 + (left > step) + (left > 2ll * step) + (left > 3ll * step);
+  const int bytes = (int)(span > 1 || left < kChunk ? left : kChunk);
   const bool inplace = S.src == S.dst;
-  // lane j: slot j's parent, -1 where nothing moves
-  int mine = lane < A.K ? A.parent[b * A.parent_stride + lane] : -1;
-  if (mine >= A.W || (inplace && mine == lane)) mine = -1;
+  Slots s;
+  s.mine = lane < A.K ? A.parent[b * A.parent_stride + lane] : -1;
+  if (s.mine >= A.W || (inplace && s.mine == lane)) s.mine = -1;
+  s.moves = __ballot(s.mine >= 0);
   // (the same in every lane, told to the compiler: descriptors live in scalar registers)
-  const uint64_t src = uniform((uint64_t)(S.src + b * S.ssb + r * S.ssr + begin));
-  const uint64_t dst = uniform((uint64_t)(S.dst + b * S.dsb + r * S.dsr + begin));
-  const uint64_t ssw = uniform((uint64_t)S.ssw), dsw = uniform((uint64_t)S.dsw);
-  const int whole = bytes / BYTES * BYTES, at = lane * BYTES;
-  if (ALIGNED) move_words<Word<BYTES, STREAM>, KMAX>(mine, src, ssw, dst, dsw, whole, at);
-  else if (whole > 0) move_any<KMAX, STREAM>(mine, src, ssw, dst, dsw, whole, at);
-  if (whole != bytes)  // a row's last bytes
-    move_words<Word<1, false>, KMAX>(mine, src, ssw, dst, dsw, bytes, whole + lane);
+  s.src = uniform((uint64_t)(S.src + b * S.ssb + r * S.ssr + begin));
+  s.dst = uniform((uint64_t)(S.dst + b * S.dsb + r * S.dsr + begin));
+  s.ssw = uniform((uint64_t)S.ssw);
+  s.dsw = uniform((uint64_t)S.dsw);
+  using Wd = typename std::conditional<ALIGNED, Aligned<STREAM>, Anywhere<STREAM>>::type;
+  if (left > 0) move_words<Wd, KMAX, WIDE>(s, lane * 16, n, step, bytes);
+  if ((all & 15) != 0) {  // a row's last bytes
+    int last = -1;
+    for (int c = 0; c < span; ++c)
+      if (left >= (int64_t)c * step && left < (int64_t)c * step + kChunk) last = (int)left;
+    if (last >= 0)
+      Tile<Byte, KMAX, 1, false>().move(s, last + lane, 0, last + (int)(all & 15));
+  }
 }
 
 template <bool ALIGNED, bool STREAM, int STATES>
 void launch_slots(const MoveArgs<STATES>& A, uint32_t grid, hipStream_t st) {
-  if (A.K <= 8) hs_reorder_kernel<ALIGNED, 8, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
-  else if (A.K <= 16) hs_reorder_kernel<ALIGNED, 16, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
-  else if (A.K <= 32) hs_reorder_kernel<ALIGNED, 32, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
-  else hs_reorder_kernel<ALIGNED, 64, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
+  bool wide = false;
+  for (int i = 0; i < A.n; ++i) wide = wide || A.st[i].span > 1;
+  if (wide) hs_reorder_kernel<ALIGNED, kWideSlots, true, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
+  else if (A.K <= 8) hs_reorder_kernel<ALIGNED, 8, false, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
+  else if (A.K <= 16) hs_reorder_kernel<ALIGNED, 16, false, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
+  else if (A.K <= 32) hs_reorder_kernel<ALIGNED, 32, false, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
+  else hs_reorder_kernel<ALIGNED, 64, false, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
 }
 
 template <bool ALIGNED, bool STREAM>
@@ -206,21 +257,38 @@ hs_state in_one_row(const hs_state& s, bool counted) {
   return one;
 }
 
-// The waves of a row. Short rows share workgroups (64 queries x 64 rows of 512 bytes, counted: 11.8 us with a
-// workgroup for each, 5.9); of four waves on none does (rows of 34 waves, counted: 12.9 us shared, 11.2).
-uint64_t chunks_of(const hs_state& s) {
-  const uint64_t bytes = (uint64_t)s.units * (uint64_t)s.unit;
-  const uint64_t n = bytes / kChunk + (bytes % kChunk != 0);
-  return n < kWaves ? n : (n + kWaves - 1) / kWaves * kWaves;
+// Bytes of a slot, over all tensors, queries and rows, from which on a workgroup may have several pieces.
+constexpr __int128 kWideBytes = (__int128)16 << 20;
+
+// How a row is cut (MoveState's span). Rows that share workgroups are those of less than a workgroup's bytes (64
+// queries x 64 rows of 512 bytes, counted: 11.8 us with a workgroup for each, 5.9; but rows of 34 chunks
+// 12.9 shared, 11.2). A wave with one piece and one moving slot has one load in flight, hence up to four
+// pieces for it where few slots may move. In us, with one piece and four: 1 of 4 slots of 2.0 GB 88 and 49; 4
+// of 8 slots of 2.1 GB 205 and 187; all of 8 310 and 315. Of more slots half of the calls lose: 3 of 15 30
+// and 18, but 7 of 16 151 and 164, 11 of 12 219 and 250, 16 of 16 333 and 415. The pieces lie a multiple of 8
+// apart where there are enough, so that each XCD stays with its eighth of the memory's 4 KB pages (the 205
+// are 238 with pieces side by side).
+uint64_t row_bytes(const hs_state& s) { return (uint64_t)s.units * (uint64_t)s.unit; }
+int span_of(const hs_state& s, int K, bool wide) {
+  if (row_bytes(s) <= kChunk * (kWaves - 1)) return 0;
+  const bool few = K <= kWideSlots / 2 || (K <= kWideSlots && s.src == s.dst);
+  return wide && few && row_bytes(s) > kPiece && row_bytes(s) < (1u << 30) ? kSpan : 1;
+}
+uint64_t parts_of(const hs_state& s, int span) {
+  const uint64_t per = span == 0 ? kChunk : kPiece;
+  const uint64_t n = row_bytes(s) / per + (row_bytes(s) % per != 0);
+  if (span <= 1) return n;
+  const uint64_t parts = (n + span - 1) / span;
+  return n >= 32 ? (parts + 7) / 8 * 8 : parts;
 }
 
 }  // namespace
 
 bool reorder_fits(const hs_state& state, int B, bool counted) {
   const hs_state s = in_one_row(state, counted);
-  const unsigned __int128 waves = (unsigned __int128)chunks_of(s) *
+  const unsigned __int128 parts = (unsigned __int128)parts_of(s, span_of(s, 1, false)) *
                                   (unsigned __int128)s.rows * (unsigned __int128)B;
-  return waves < ((unsigned __int128)1 << 31);
+  return parts < ((unsigned __int128)1 << 31);
 }
 
 namespace {
@@ -373,6 +441,7 @@ int launch_reorder(const hs_state* states, int n, int B, int W, int K, const int
   __int128 all = 0;
   for (int i = 0; i < n; ++i) all += (__int128)B * K * states[i].rows * states[i].units * states[i].unit;
   const bool stream_past = all >= kStreamBytes;
+  const bool wide = all >= kWideBytes * K;
   for (int odd = 0; odd < 2; ++odd) {  // the aligned tensors together, then the others
     int i = 0;
     while (i < n) {
@@ -387,8 +456,9 @@ int launch_reorder(const hs_state* states, int n, int B, int W, int K, const int
       for (; i < n && A.n < kStates; ++i) {
         const hs_state s = in_one_row(states[i], count != nullptr);
         if (aligned(s) == (odd != 0)) continue;
-        const uint64_t chunks = chunks_of(s);
-        const uint64_t wgs = (chunks * (uint64_t)s.rows * (uint64_t)B + kWaves - 1) / kWaves;
+        const int span = span_of(s, K, wide);
+        const uint64_t parts = parts_of(s, span), of = span == 0 ? kWaves : 1;
+        const uint64_t wgs = (parts * (uint64_t)s.rows * (uint64_t)B + of - 1) / of;
         if (grid + wgs >= (1ull << 31)) break;
         A.first[A.n] = (uint32_t)grid;
         MoveState& m = A.st[A.n++];
@@ -402,10 +472,11 @@ int launch_reorder(const hs_state* states, int n, int B, int W, int K, const int
         m.dsr = s.dst_stride_row;
         m.units = s.units;
         m.unit = s.unit;
-        m.chunks = (int)chunks;
+        m.parts = (int)parts;
+        m.span = span;
         m.rows = (int)s.rows;
         m.queries = B;
-        m.div_chunks = make_fastdiv((uint32_t)chunks);
+        m.div_parts = make_fastdiv((uint32_t)parts);
         m.div_rows = make_fastdiv((uint32_t)s.rows);
         grid += wgs;
       }

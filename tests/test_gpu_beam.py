@@ -558,6 +558,57 @@ def test_reorder_random_layouts(seed):
             assert torch.equal(sf, was)
 
 
+@pytest.mark.parametrize("K,moved", [(1, 1), (2, 1), (2, 2), (4, 1), (4, 3), (8, 1), (8, 2), (8, 3), (8, 4),
+                                     (8, 5), (8, 8)])
+@pytest.mark.parametrize("odd", [0, 1])
+def test_reorder_long_rows(K, moved, odd):
+    """Rows long enough that a workgroup has several pieces of each: few and many slots that move, aligned
+    or not, lengths about the pieces' ends."""
+    note("long rows K=%d moved=%d odd=%d" % (K, moved, odd))
+    g = torch.Generator().manual_seed(K * 100 + moved * 10 + odd)
+    B, H = 3, 2
+    units = (1 << 20) * 3 + 4096 * 5 + 1019 - odd      # bytes of a row, 16 MB a slot in all
+    step = -(-(-(-units // 4096)) // 4 // 8) * 8 * 4096  # pieces of one workgroup lie so far apart
+    base = torch.randint(0, 256, (1 << 20,), generator=g, dtype=torch.uint8).cuda()
+    flat = base.repeat(B * K * H * (units + 64) // (1 << 20) + 1)
+    flat[: 1 << 21] ^= 0x5A
+    for i in range(0, flat.numel(), 1 << 20):            # every megabyte another
+        flat[i:i + 4096] += i >> 20
+    x = flat[16 + odd:][:B * K * H * (units + 48 + odd)].view(B, K, H, units + 48 + odd)[..., :units]
+    for off in (0, step - units, 2 * step + 1 - units, 3 * step + 1024 - units, 5 - units, 4096 + 7 - units):
+        count = torch.tensor([units + off, units, units - 17], dtype=torch.int32)
+        parent = torch.arange(K, dtype=torch.int32).repeat(B, 1)
+        movers = torch.randperm(K, generator=g)[:moved]
+        for j in movers.tolist():
+            parent[:, j] = (j + 1 + torch.randint(0, max(K - 1, 1), (B,), generator=g)) % K
+        want = flat.clone()
+        w = want[16 + odd:][:x.numel() + (48 + odd) * B * K * H].view(B, K, H, units + 48 + odd)
+        for b in range(B):
+            n = int(count[b])
+            w[b, :, :, :n] = x[b][parent[b].long().cuda()][:, :, :n]
+        hs.beam_reorder(x, parent.cuda(), count=count.cuda(), axis=3)
+        assert torch.equal(flat, want)
+
+
+@pytest.mark.parametrize("K", [1, 2, 4])
+def test_reorder_long_rows_into_another_buffer(K):
+    note("long rows out K=%d" % K)
+    g = torch.Generator().manual_seed(K)
+    n = (1 << 24) + 4097
+    x = torch.randint(0, 1 << 30, (2, 3, n // 4), generator=g, dtype=torch.int32).cuda()
+    out = torch.full((2, K, n // 4), -1, dtype=torch.int32, device="cuda")
+    parent = torch.randint(0, 3, (2, K), generator=g, dtype=torch.int32)
+    parent[1, K - 1] = -1
+    want = out.clone()
+    for b in range(2):
+        for j in range(K):
+            if parent[b, j] >= 0:
+                want[b, j] = x[b, int(parent[b, j])]
+    kept = x.clone()
+    hs.beam_reorder(x, parent.cuda(), out=out)
+    assert torch.equal(out, want) and torch.equal(x, kept)
+
+
 def test_reorder_slices_of_one_buffer():
     """Tensors between each other's rows: the layers of a stacked cache, keys beside values, in place
     and from one half of a buffer to the other."""
