@@ -263,8 +263,8 @@ constexpr __int128 kWideBytes = (__int128)16 << 20;
 // How a row is cut (MoveState's span). Rows that share workgroups are those of less than a workgroup's bytes (64
 // queries x 64 rows of 512 bytes, counted: 11.8 us with a workgroup for each, 5.9; but rows of 34 chunks
 // 12.9 shared, 11.2). A wave with one piece and one moving slot has one load in flight, hence up to four
-// pieces for it where few slots may move. In us, with one piece and four: 1 of 4 slots of 2.0 GB 88 and 49; 4
-// of 8 slots of 2.1 GB 205 and 187; all of 8 310 and 315. Of more slots half of the calls lose: 3 of 15 30
+// pieces for it where few slots may move. In us, with one piece and four: 1 of 4 slots of 1.0 GB 88 and 50; 4
+// of 8 slots of 2.1 GB 205 and 187; all of 8 of 1.1 GB 310 and 322. Of more slots half of the calls lose: 3 of 15 30
 // and 18, but 7 of 16 151 and 164, 11 of 12 219 and 250, 16 of 16 333 and 415. The pieces lie a multiple of 8
 // apart where there are enough, so that each XCD stays with its eighth of the memory's 4 KB pages (the 205
 // are 238 with pieces side by side).
