@@ -25,7 +25,7 @@
 // Bound. The rows kernel reads 311 MB (32 x 32 rows of 151936 bf16) in 50.2 us, 6.2 TB/s, each byte once (its
 // 552 vector instructions per two chunks and wave take about as long as the memory does), 110 MB in
 // 22.6 us, and a call too short for that in 4.0 us. The merge is bound by latency, by six steps that wait
-// for each other: 5.6 us for 4 rows of 128 units and 4 slots, 16.4 us for 32 workgroups of 32 rows of 300
+// for each other: 5.0 us for 4 rows of 128 units and 4 slots, 16.4 us for 32 workgroups of 32 rows of 300
 // units and 64 slots (an instruction that all of its 16 waves make costs 16 cycles). Two launches: in
 // one, with a query's last workgroup merging, the fences between the XCDs' caches cost what the second
 // launch does (10 rows of bf16 13.3 us, or 11.4 with device-scope words instead of fences; two 10.8).
@@ -39,8 +39,6 @@ namespace {
 
 constexpr int kMergeThreads = 1024;  // (256, 512: 10 rows of bf16 14.7, 11.8 us, 32 x 32 rows 89, 72; 10.7, 65)
 constexpr int kMergeWaves = kMergeThreads / 64;
-constexpr int kRows = HS_MAX_BEAMS / kMergeWaves;  // rows of a wave in the merge
-constexpr int kHeld = 5;         // units' maxima of a row that a lane holds (for 152000 16-bit logits all)
 constexpr int kAtOnce = 4;       // units that a wave reads at once
 constexpr int kPairs = 2048;     // entries of one query held in LDS, twice what a round can add
 constexpr int kTokenBits = 26;
@@ -325,11 +323,14 @@ struct PairList {
   }
 };
 
-template <int DT>
+// kRows: rows of a wave, at least W / 16. kHeld: units' maxima of a row that a lane holds: all (kAll), or the
+// others are read again.
+template <int DT, int kRows, int kHeld, bool kAll>
 __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A) {
   using Vt = Vec<DT>;
   using Raw = typename Vt::Raw;
   constexpr int E = Vt::kElems;
+  constexpr int kMost = kAll ? kHeld * 64 / kUnits : 1 << 30;  // slices of a row
   __shared__ double s_off[HS_MAX_BEAMS], s_lse[HS_MAX_BEAMS];  // a row's log2 normaliser: their sum
   __shared__ float s_score[HS_MAX_BEAMS];
   __shared__ float s_least[HS_MAX_BEAMS];    // a row's logits below it do not reach the bound
@@ -357,7 +358,7 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
     if (w >= W) break;
     const SliceRec* rec = A.rec + ((int64_t)b * W + w) * S;
     r0[r] = rec[min(lane, S - 1)];
-    r1[r] = rec[min(lane + 64, S - 1)];
+    if (kMost > 64) r1[r] = rec[min(lane + 64, S - 1)];
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) m[r][i] = top[w * nu + min(lane + 64 * i, nu - 1)];
     sc[r] = A.score[(int64_t)b * A.score_stride + w];
@@ -396,8 +397,10 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
       continue;
     }
     const SliceRec* rec = A.rec + ((int64_t)b * W + w) * S;
-    int best = max(fkey(r0[r].ref), fkey(r1[r].ref));
-    for (int s = lane + 128; s < S; s += 64) best = max(best, fkey(rec[s].ref));
+    int best = fkey(r0[r].ref);
+    if (kMost > 64) best = max(best, fkey(r1[r].ref));
+    if (kMost > 128)
+      for (int s = lane + 128; s < S; s += 64) best = max(best, fkey(rec[s].ref));
     const Offset to(fkey_inv(wave_max_i(best)), c32);  // the row's: from its largest reference
     double sum = 0.0;
     auto part = [&](const SliceRec& q, bool mine) {
@@ -409,8 +412,9 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
       }
     };
     part(r0[r], lane < S);
-    if (S > 64) part(r1[r], lane + 64 < S);
-    for (int s0 = 128; s0 < S; s0 += 64) part(rec[min(s0 + lane, S - 1)], s0 + lane < S);
+    if (kMost > 64 && S > 64) part(r1[r], lane + 64 < S);
+    if (kMost > 128)
+      for (int s0 = 128; s0 < S; s0 += 64) part(rec[min(s0 + lane, S - 1)], s0 + lane < S);
     sum = wave_sum_d(sum);
     const bool live = isfinite(sum) && sum > 0.0;
     const double lg = log2_of(sum);
@@ -425,7 +429,8 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
 #pragma unroll
     for (int i = 0; i < kHeld; ++i)
       if (lane + 64 * i < nu) most = fmaxf(most, m[r][i]);
-    for (int k = lane + 64 * kHeld; k < nu; k += 64) most = fmaxf(most, top[w * nu + k]);
+    if (!kAll)
+      for (int k = lane + 64 * kHeld; k < nu; k += 64) most = fmaxf(most, top[w * nu + k]);
     if (live && most > -INFINITY)
       atomicMax(&s_group[group_of(w) + lane], (uint32_t)(score_of(w, most) >> 32));
   }
@@ -478,7 +483,7 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
         at += __builtin_popcountll(who[i]);
       }
     }
-    for (int k0 = 64 * kHeld; k0 < nu; k0 += 64) {
+    for (int k0 = 64 * kHeld; !kAll && k0 < nu; k0 += 64) {
       const int k = k0 + lane;
       const bool pass = k < nu && top[w * nu + min(k, nu - 1)] >= least;
       units.add(pass, 0, place(w, k), lane);
@@ -665,11 +670,24 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
   }
 }
 
+// The smallest kernel that does. us with one kernel for all (4 rows, 5 maxima), with 5 and 10 maxima for the rows there
+// are, and with this rule: 10 rows of 300 units 10.8, 10.4, 10.9 and 10.3; 15 of 536 15.6, 15.3, 14.0 and 14.0; 4 of
+// 128 9.6, 9.2, 9.6 and 9.0; 64 of 64 27.7, 27.6, 27.6 and 25.9.
+template <int DT, int ROWS>
+void launch_merge(const StepArgs& A, int B, hipStream_t st) {
+  constexpr int kLong = ROWS > 2 ? 5 : 10;
+  if (A.nu <= 128) hs_beam_merge_kernel<DT, ROWS, 2, true><<<B, kMergeThreads, 0, st>>>(A);
+  else if (A.nu <= 320) hs_beam_merge_kernel<DT, ROWS, 5, true><<<B, kMergeThreads, 0, st>>>(A);
+  else hs_beam_merge_kernel<DT, ROWS, kLong, false><<<B, kMergeThreads, 0, st>>>(A);
+}
+
 template <int DT>
 void launch_step(const StepArgs& A, int B, hipStream_t st) {
   hs_beam_rows_kernel<DT><<<(A.units + kWaves - 1) / kWaves, kThreads, 0, st>>>(A);
   if (hipGetLastError() != hipSuccess) return;
-  hs_beam_merge_kernel<DT><<<B, kMergeThreads, 0, st>>>(A);
+  if (A.W <= kMergeWaves) launch_merge<DT, 1>(A, B, st);
+  else if (A.W <= 2 * kMergeWaves) launch_merge<DT, 2>(A, B, st);
+  else launch_merge<DT, HS_MAX_BEAMS / kMergeWaves>(A, B, st);
 }
 
 }  // namespace

@@ -104,6 +104,21 @@ def test_step_temperatures_at_the_limits(dtype, T):
     check_step(x, scores(g, 2, 3), 12, 5003, T=T)
 
 
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("units", [127, 128, 129, 319, 320, 321, 645])
+@pytest.mark.parametrize("W", [3, 17, 33])
+def test_step_borders_of_units_and_rows(dtype, units, W):
+    """Rows about the lengths, and beams about the numbers, at which another kernel is taken."""
+    per = 256 if dtype == "f32" else 512          # logits of a unit: 16 lanes, 4 vectors each
+    V = units * per - 5
+    note("borders %s W=%d V=%d" % (dtype, W, V))
+    g = torch.Generator().manual_seed(units + W)
+    x = rows(g, 1, W, V, DTYPES[dtype])
+    x[0, W // 2, V - 1] = 40.0                    # the last logit of a row, and of the last unit
+    x[0, W - 1, V - 2] = 40.0
+    check_step(x, scores(g, 1, W), 12, V)
+
+
 def test_step_peaked_rows_like_a_model():
     # 20 boosted tokens a row hold most of the mass; 32 beams, 64 kept
     note("peaked rows")
