@@ -324,9 +324,9 @@ struct PairList {
 };
 
 // kRows: rows of a wave, at least W / 16. kHeld: units' maxima of a row that a lane holds: all (kAll), or the
-// others are read again.
-template <int DT, int kRows, int kHeld, bool kAll>
-__global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A) {
+// others are read again. kPerCu: workgroups that a CU's registers hold.
+template <int DT, int kRows, int kHeld, bool kAll, int kPerCu>
+__global__ __launch_bounds__(kMergeThreads, 4 * kPerCu) void hs_beam_merge_kernel(StepArgs A) {
   using Vt = Vec<DT>;
   using Raw = typename Vt::Raw;
   constexpr int E = Vt::kElems;
@@ -336,8 +336,11 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
   __shared__ float s_least[HS_MAX_BEAMS];    // a row's logits below it do not reach the bound
   __shared__ uint8_t s_kind[HS_MAX_BEAMS];   // 0: gives nothing, 1: by its logits, 2: finished
   __shared__ uint32_t s_group[128];
-  __shared__ uint64_t s_uhi[kPairs], s_ulo[kPairs], s_hi[kPairs], s_lo[kPairs];
-  __shared__ Raw s_vec[kMergeWaves][64];
+  __shared__ __align__(16) uint64_t s_uhi[kPairs];
+  __shared__ uint64_t s_ulo[kPairs], s_hi[kPairs], s_lo[kPairs];
+  // (where s_uhi was, which is done with by then: 70 KB in all, so that a CU holds two workgroups)
+  static_assert(sizeof(s_uhi) >= kMergeWaves * 64 * sizeof(Raw), "s_vec lies in s_uhi");
+  Raw(*const s_vec)[64] = reinterpret_cast<Raw(*)[64]>(s_uhi);
   __shared__ uint8_t s_from[kMergeWaves][64], s_unit[kMergeWaves][64];
   __shared__ int s_units, s_count;
   __shared__ uint64_t s_bound;
@@ -673,12 +676,19 @@ __global__ __launch_bounds__(kMergeThreads) void hs_beam_merge_kernel(StepArgs A
 // The smallest kernel that does. us with one kernel for all (4 rows, 5 maxima), with 5 and 10 maxima for the rows there
 // are, and with this rule: 10 rows of 300 units 10.8, 10.4, 10.9 and 10.3; 15 of 536 15.6, 15.3, 14.0 and 14.0; 4 of
 // 128 9.6, 9.2, 9.6 and 9.0; 64 of 64 27.7, 27.6, 27.6 and 25.9.
+// Two workgroups per CU where there are more than CUs: 4000 x 1 rows of 4000 bf16 82 -> 54 us, 1024 x 2 of 8000 29 -> 23;
+// 13 x 5 of 50257 10.4 -> 10.7.
+template <int DT, int ROWS, int HELD, bool ALL>
+void launch_merge_of(const StepArgs& A, int B, hipStream_t st) {
+  constexpr int kMany = ROWS * HELD <= 10 ? 2 : 1;
+  if (B > 256) hs_beam_merge_kernel<DT, ROWS, HELD, ALL, kMany><<<B, kMergeThreads, 0, st>>>(A);
+  else hs_beam_merge_kernel<DT, ROWS, HELD, ALL, 1><<<B, kMergeThreads, 0, st>>>(A);
+}
 template <int DT, int ROWS>
 void launch_merge(const StepArgs& A, int B, hipStream_t st) {
-  constexpr int kLong = ROWS > 2 ? 5 : 10;
-  if (A.nu <= 128) hs_beam_merge_kernel<DT, ROWS, 2, true><<<B, kMergeThreads, 0, st>>>(A);
-  else if (A.nu <= 320) hs_beam_merge_kernel<DT, ROWS, 5, true><<<B, kMergeThreads, 0, st>>>(A);
-  else hs_beam_merge_kernel<DT, ROWS, kLong, false><<<B, kMergeThreads, 0, st>>>(A);
+  if (A.nu <= 128) launch_merge_of<DT, ROWS, 2, true>(A, B, st);
+  else if (A.nu <= 320) launch_merge_of<DT, ROWS, 5, true>(A, B, st);
+  else launch_merge_of<DT, ROWS, (ROWS > 2 ? 5 : 10), false>(A, B, st);
 }
 
 template <int DT>

@@ -248,6 +248,14 @@ def test_step_many_queries():
     assert (out["score"].double() - top[:, :K]).abs().max() <= NORM_TOL + 20 * 2.0 ** -24
 
 
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("W,V", [(1, 700), (1, 83000), (17, 3000), (40, 1000)])
+def test_step_more_queries_than_compute_units(dtype, W, V):
+    note("258 queries %s W=%d V=%d" % (dtype, W, V))
+    g = torch.Generator().manual_seed(W)
+    check_step(rows(g, 258, W, V, DTYPES[dtype]), scores(g, 258, W), 6, V)
+
+
 def test_step_offsets_past_32_bits():
     note("logits far apart")
     V, far = 3000, (1 << 32) + 4096
