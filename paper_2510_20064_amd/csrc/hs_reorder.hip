@@ -32,6 +32,7 @@ struct MoveState {
 template <int STATES>
 struct MoveArgs {
   int n, W, K;
+  int split;  // log2 of the waves that share a position's slots, KMAX each (not in place)
   int64_t parent_stride;
   const int32_t* parent;
   const int32_t* count;
@@ -93,11 +94,12 @@ struct Anywhere {
 struct Slots {
   uint64_t src, dst, ssw, dsw;
   int mine;        // lane j: slot j's parent, -1 where nothing moves
+  int first;       // the wave's first slot
   uint64_t moves;  // the slots that move
 };
 
-// A lane's words at `at`, `at` + step, ... (COUNT of them) before byte `bytes`, of M slots: the slots 0 to M - 1, or,
-// PICK, the M first that move. A slot that moves nothing has no bytes instead of a branch, so that all loads
+// A lane's words at `at`, `at` + step, ... (COUNT of them) before byte `bytes`, of M slots: from the wave's first one on,
+// or, PICK, the M first that move. A slot that moves nothing has no bytes instead of a branch, so that all loads
 // go out together.
 template <typename Wd, int M, int COUNT, bool PICK>
 struct Tile {
@@ -108,7 +110,7 @@ struct Tile {
     uint64_t rest = s.moves;
 #pragma unroll
     for (int q = 0; q < M; ++q) {
-      const int j = PICK ? __builtin_ctzll(rest | 1ull << 63) : q, p = __builtin_amdgcn_readlane(s.mine, j);
+      const int j = PICK ? __builtin_ctzll(rest | 1ull << 63) : s.first + q, p = __builtin_amdgcn_readlane(s.mine, j);
       const bool on = PICK ? rest != 0 : p >= 0;
       const Wd w(LOAD ? s.src + (uint64_t)(uint32_t)(on ? p : 0) * s.ssw : s.dst + (uint64_t)j * s.dsw,
                  on ? bytes : 0);
@@ -150,7 +152,7 @@ __device__ __forceinline__ void move_words(const Slots& s, int at, int n, int st
   }
 }
 
-// KMAX: at least K. WIDE: some tensor has a span above 1. ALIGNED: every row of the tensors starts at a multiple of 4 bytes.
+// KMAX: at least K, or its share of a wave. WIDE: some tensor has a span above 1. ALIGNED: every row of the tensors starts at a multiple of 4 bytes.
 template <bool ALIGNED, int KMAX, bool WIDE, bool STREAM, int STATES>
 __global__ __launch_bounds__(kThreads) void hs_reorder_kernel(MoveArgs<STATES> A) {
   int i = 0;
@@ -169,7 +171,8 @@ __global__ __launch_bounds__(kThreads) void hs_reorder_kernel(MoveArgs<STATES> A
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   // a row of less than a workgroup's bytes has a wave for each of its chunks; a longer one has workgroups that
   // move `span` pieces of kPiece bytes each, `parts` pieces apart
-  const uint32_t u = S.span == 0 ? (blockIdx.x - first) * kWaves + wave : blockIdx.x - first;
+  const int sub = WIDE ? wave : wave >> A.split;  // the wave's chunk of the workgroup's
+  const uint32_t u = S.span == 0 ? (blockIdx.x - first) * (kWaves >> A.split) + sub : blockIdx.x - first;
   const uint32_t br = fdiv(u, S.div_parts);
   const int64_t part = u - br * (uint32_t)S.parts;
   const int b = (int)fdiv(br, S.div_rows);
@@ -180,7 +183,7 @@ __global__ __launch_bounds__(kThreads) void hs_reorder_kernel(MoveArgs<STATES> A
     const int64_t c = A.count[b];
     units = c < 0 ? 0 : c < units ? c : units;
   }
-  const int64_t all = units * S.unit, begin = S.span == 0 ? part * kChunk : part * kPiece + wave * kChunk;
+  const int64_t all = units * S.unit, begin = S.span == 0 ? part * kChunk : part * (kPiece >> A.split) + sub * kChunk;
   if (all <= begin) return;  // all of the wave
   // the wave's words end at `left` (that is below 2^31 where there is more than one), but for a row's last bytes
   const int64_t left = (all & ~15ll) - begin;
@@ -192,6 +195,7 @@ __global__ __launch_bounds__(kThreads) void hs_reorder_kernel(MoveArgs<STATES> A
   s.mine = lane < A.K ? A.parent[b * A.parent_stride + lane] : -1;
   if (s.mine >= A.W || (inplace && s.mine == lane)) s.mine = -1;
   s.moves = __ballot(s.mine >= 0);
+  s.first = WIDE ? 0 : (wave & ((1 << A.split) - 1)) * KMAX;
   // (the same in every lane, told to the compiler: descriptors live in scalar registers)
   s.src = uniform((uint64_t)(S.src + b * S.ssb + r * S.ssr + begin));
   s.dst = uniform((uint64_t)(S.dst + b * S.dsb + r * S.dsr + begin));
@@ -213,8 +217,8 @@ void launch_slots(const MoveArgs<STATES>& A, uint32_t grid, hipStream_t st) {
   bool wide = false;
   for (int i = 0; i < A.n; ++i) wide = wide || A.st[i].span > 1;
   if (wide) hs_reorder_kernel<ALIGNED, kWideSlots, true, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
-  else if (A.K <= 8) hs_reorder_kernel<ALIGNED, 8, false, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
-  else if (A.K <= 16) hs_reorder_kernel<ALIGNED, 16, false, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
+  else if (A.K <= 8 << A.split) hs_reorder_kernel<ALIGNED, 8, false, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
+  else if (A.K <= 16 << A.split) hs_reorder_kernel<ALIGNED, 16, false, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
   else if (A.K <= 32) hs_reorder_kernel<ALIGNED, 32, false, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
   else hs_reorder_kernel<ALIGNED, 64, false, STREAM, STATES><<<grid, kThreads, 0, st>>>(A);
 }
@@ -225,7 +229,7 @@ void launch_words(const MoveArgs<kStates>& A, uint32_t grid, hipStream_t st) {
     launch_slots<ALIGNED, STREAM, kStates>(A, grid, st);
     return;
   }
-  MoveArgs<kFew> few{A.n, A.W, A.K, A.parent_stride, A.parent, A.count, {}, {}};
+  MoveArgs<kFew> few{A.n, A.W, A.K, A.split, A.parent_stride, A.parent, A.count, {}, {}};
   for (int j = 0; j < kFew; ++j) few.first[j] = A.first[j];
   for (int j = 0; j < A.n; ++j) few.st[j] = A.st[j];
   launch_slots<ALIGNED, STREAM, kFew>(few, grid, st);
@@ -269,24 +273,30 @@ constexpr __int128 kWideBytes = (__int128)16 << 20;
 // apart where there are enough, so that each XCD stays with its eighth of the memory's 4 KB pages (the 205
 // are 238 with pieces side by side).
 uint64_t row_bytes(const hs_state& s) { return (uint64_t)s.units * (uint64_t)s.unit; }
-int span_of(const hs_state& s, int K, bool wide) {
-  if (row_bytes(s) <= kChunk * (kWaves - 1)) return 0;
+int span_of(const hs_state& s, int K, bool wide, int split) {
+  if (row_bytes(s) <= (kPiece >> split) - kChunk) return 0;
   const bool few = K <= kWideSlots / 2 || (K <= kWideSlots && s.src == s.dst);
   return wide && few && row_bytes(s) > kPiece && row_bytes(s) < (1u << 30) ? kSpan : 1;
 }
-uint64_t parts_of(const hs_state& s, int span) {
-  const uint64_t per = span == 0 ? kChunk : kPiece;
+uint64_t parts_of(const hs_state& s, int span, int split) {
+  const uint64_t per = span == 0 ? kChunk : kPiece >> split;
   const uint64_t n = row_bytes(s) / per + (row_bytes(s) % per != 0);
   if (span <= 1) return n;
   const uint64_t parts = (n + span - 1) / span;
   return n >= 32 ? (parts + 7) / 8 * 8 : parts;
 }
 
+// The waves (as a power of two) that share a position's slots where nothing is in place: fewer registers each, more
+// waves per CU. us with one wave and with this rule: 13 queries of 30 slots of 0.27 MB at odd addresses 41 and
+// 26, 7 of 31 of 1.2 MB 48 and 42, 4 of 64 of 2.5 MB 140 and 132, 9 of 32 of 0.1 MB 10.0 and 6.8, 15 of 28 of
+// 2.6 MB 372 and 385; 7 of 9 slots (two waves) 4.7 and 4.4, but 8 of 16 of 8 MB 327 and 346.
+int split_of(int K, bool past) { return K <= 8 ? 0 : K > 16 ? 2 : past ? 0 : 1; }
+
 }  // namespace
 
 bool reorder_fits(const hs_state& state, int B, bool counted) {
   const hs_state s = in_one_row(state, counted);
-  const unsigned __int128 parts = (unsigned __int128)parts_of(s, span_of(s, 1, false)) *
+  const unsigned __int128 parts = (unsigned __int128)parts_of(s, 1, 2) *
                                   (unsigned __int128)s.rows * (unsigned __int128)B;
   return parts < ((unsigned __int128)1 << 31);
 }
@@ -442,6 +452,9 @@ int launch_reorder(const hs_state* states, int n, int B, int W, int K, const int
   for (int i = 0; i < n; ++i) all += (__int128)B * K * states[i].rows * states[i].units * states[i].unit;
   const bool stream_past = all >= kStreamBytes;
   const bool wide = all >= kWideBytes * K;
+  bool inplace = false;
+  for (int i = 0; i < n; ++i) inplace = inplace || states[i].src == states[i].dst;
+  const int split = inplace ? 0 : split_of(K, stream_past);
   for (int odd = 0; odd < 2; ++odd) {  // the aligned tensors together, then the others
     int i = 0;
     while (i < n) {
@@ -449,6 +462,7 @@ int launch_reorder(const hs_state* states, int n, int B, int W, int K, const int
       A.n = 0;
       A.W = W;
       A.K = K;
+      A.split = split;
       A.parent = parent;
       A.parent_stride = parent_stride;
       A.count = count;
@@ -456,8 +470,8 @@ int launch_reorder(const hs_state* states, int n, int B, int W, int K, const int
       for (; i < n && A.n < kStates; ++i) {
         const hs_state s = in_one_row(states[i], count != nullptr);
         if (aligned(s) == (odd != 0)) continue;
-        const int span = span_of(s, K, wide);
-        const uint64_t parts = parts_of(s, span), of = span == 0 ? kWaves : 1;
+        const int span = span_of(s, K, wide, split);
+        const uint64_t parts = parts_of(s, span, split), of = span == 0 ? kWaves >> split : 1;
         const uint64_t wgs = (parts * (uint64_t)s.rows * (uint64_t)B + of - 1) / of;
         if (grid + wgs >= (1ull << 31)) break;
         A.first[A.n] = (uint32_t)grid;

@@ -1000,3 +1000,31 @@ def test_calls_that_make_their_tensors_for_another_stream():
     assert all(torch.equal(o[k], want[k]) for o in outs for k in want)
     ref = hs.draft_tree(*grown_to, 9)
     assert all(torch.equal(tree[k], ref[k]) for k in ref)
+
+
+@pytest.mark.parametrize("K", [9, 16, 17, 32, 33, 64])
+@pytest.mark.parametrize("mixed", [False, True])
+def test_reorder_slots_shared_by_waves(K, mixed):
+    """Many slots into other buffers, short rows and long, counted; with a tensor in place among them too."""
+    note("shared slots K=%d mixed=%d" % (K, mixed))
+    g = torch.Generator().manual_seed(K)
+    W = K if mixed else 7
+    src = [ints(g, (3, W, 2, T, D), torch.int16) for T, D in ((1, 8), (5, 33), (40, 64), (300, 33), (61, 100))]
+    dst = [ints(g, (3, K) + tuple(s.shape[2:]), torch.int16) for s in src]
+    parent = torch.randint(-1, W + 1, (3, K), generator=g, dtype=torch.int32)
+    for count in (None, torch.tensor([1, 400, 37], dtype=torch.int32)):
+        out = [d.clone() for d in dst]
+        inp = [s.clone() for s in src]
+        if mixed:
+            out[2] = inp[2]
+        want = []
+        for s, d in zip(src, [src[2] if mixed and i == 2 else d for i, d in enumerate(dst)]):
+            w = d.clone()
+            for b in range(3):
+                n = s.shape[3] if count is None else int(count[b])
+                for j in range(K):
+                    if 0 <= int(parent[b, j]) < W:
+                        w[b, j, :, :n] = s[b, int(parent[b, j]), :, :n]
+            want.append(w)
+        hs.beam_reorder(inp, parent.cuda(), count=None if count is None else count.cuda(), axis=3, out=out)
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
