@@ -410,8 +410,9 @@ int hs_round(const hs_round_args* args, void* stream);
  *   s(w, v) = score[b][w] + log softmax(logits[b][w] / T)_v,
  * best first (EAGLE's dynamic draft tree grows by the cumulative log-probability of its nodes; with
  * K = W it is beam search). Scores are formed and compared in fp64 and are good to about
- * 1e-7; equal ones rank lower beam first, then lower token. Equal logits of a beam have equal
- * scores, larger ones larger.
+ * 1e-7; equal ones rank lower beam first, then larger logit, then lower token. Equal logits of a beam
+ * have equal scores; of unequal ones the larger ranks first, also where fp64 scores them the same (large T or
+ * scores).
  *   logits      : one view [B][W][V] (stride_k from beam to beam), dtype as in hs_eval_alpha. A
  *                 logit of -inf is no continuation; one of the type's lowest finite value is.
  *   score       : [B] rows of W fp32, score_stride elements apart (>= W). A beam whose score is not

@@ -455,8 +455,9 @@ __global__ __launch_bounds__(kMergeThreads, 4 * kPerCu) void hs_beam_merge_kerne
 
   // the units that reach it
   PairList units{s_uhi, s_ulo, &s_units};
-  auto place = [](int w, int k) {
-    return ((uint64_t)(63 - w) << 32) | (uint64_t)(0xFFFFFFFFu - (uint32_t)k);
+  // a unit of a list, with its largest logit where lists are cut; larger: lower beam, larger logit, lower unit
+  auto place = [](int w, uint32_t most, int k) {
+    return ((uint64_t)(63 - w) << 58) | ((uint64_t)most << kTokenBits) | (uint64_t)(kTokenMask - (uint32_t)k);
   };
 #pragma unroll
   for (int r = 0; r < kRows; ++r) {
@@ -482,20 +483,22 @@ __global__ __launch_bounds__(kMergeThreads, 4 * kPerCu) void hs_beam_merge_kerne
 #pragma unroll
       for (int i = 0; i < kHeld; ++i) {
         const int to = at + lanes_below(who[i]);
-        if (((who[i] >> lane) & 1) && to < kPairs) s_ulo[to] = place(w, lane + 64 * i);
+        if (((who[i] >> lane) & 1) && to < kPairs) s_ulo[to] = place(w, 0, lane + 64 * i);
         at += __builtin_popcountll(who[i]);
       }
     }
     for (int k0 = 64 * kHeld; !kAll && k0 < nu; k0 += 64) {
       const int k = k0 + lane;
       const bool pass = k < nu && top[w * nu + min(k, nu - 1)] >= least;
-      units.add(pass, 0, place(w, k), lane);
+      units.add(pass, 0, place(w, 0, k), lane);
     }
   }
   __syncthreads();
   int n = s_units;
-  // If they are too many (equal maxima), the 4 K first by (s, lower beam, lower chunk) do: all but
-  // three of them (units of its chunk, in no order with it) have an entry before any of a later unit
+  // If they are too many (maxima of equal score), the 4 K first by (s, lower beam, larger maximum, lower unit) do,
+  // which is the entries' order: all but three of them (units of its chunk, whose tokens lie between its
+  // own) have an entry before any of a later unit. The logits decide where fp64 scores them the same
+  // (large T, large scores)
   if (n > 4 * K + 64) {  // the same for all: nobody adds any more
     __syncthreads();
     if (t == 0) s_units = 0;
@@ -507,7 +510,7 @@ __global__ __launch_bounds__(kMergeThreads, 4 * kPerCu) void hs_beam_merge_kerne
       uint64_t h = 0;
       const int w = i < W * nu ? (int)fdiv((uint32_t)i, A.divU) : 0;
       if (i < W * nu && s_kind[w] == 1 && top[i] > -INFINITY) h = score_of(w, top[i]);
-      units.add(h != 0 && h >= bound, h, place(w, i - w * nu), lane);
+      units.add(h != 0 && h >= bound, h, place(w, h ? ordered_of(top[i]) : 0, i - w * nu), lane);
     }
     units.shrink(4 * K, 4 * K, wv, lane, &s_bound);
     n = s_units;
@@ -523,9 +526,9 @@ __global__ __launch_bounds__(kMergeThreads, 4 * kPerCu) void hs_beam_merge_kerne
     const uint64_t h = ended ? ordered_of((double)s_score[lane]) : 0;
     best.add(ended && h >= bound, h, ((uint64_t)(63 - lane) << 58) | kTokenMask, lane);
   };
-  auto row_of = [](uint64_t lo) { return 63 - (int)(lo >> 32); };
+  auto row_of = [](uint64_t lo) { return 63 - (int)(lo >> 58); };
   auto first_vector = [](uint64_t lo, int l) {  // of lane l in a unit
-    const int k = (int)(0xFFFFFFFFu - (uint32_t)lo);
+    const int k = (int)(kTokenMask - ((uint32_t)lo & kTokenMask));
     return (k / kUnits) * kBeamChunk + (l >> 4) * 64 + (k % kUnits) * 16 + (l & 15);
   };
   auto fetch = [&](uint64_t lo) {

@@ -1028,3 +1028,22 @@ def test_reorder_slots_shared_by_waves(K, mixed):
             want.append(w)
         hs.beam_reorder(inp, parent.cuda(), count=None if count is None else count.cuda(), axis=3, out=out)
         assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("W", [1, 3])
+@pytest.mark.parametrize("T,score", [(1e14, -1.0), (1e16, -1.0), (1e30, -1.0), (1.0, -1e16), (1.0, -1e17),
+                                     (1.0, -3.4e38)])
+def test_step_logits_that_score_the_same(dtype, W, T, score):
+    """Temperatures and scores at which fp64 cannot tell a beam's continuations apart, and rows of many units:
+    the larger logit still ranks first, wherever in the row it stands. (The beams' own scores are far enough
+    apart that every slot continues the first one.)"""
+    note("logits that score the same %s W=%d T=%g score=%g" % (dtype, W, T, score))
+    g = torch.Generator().manual_seed(89)
+    V = 151936
+    x = rows(g, 1, W, V, DTYPES[dtype])
+    s = torch.full((1, W), score) * torch.tensor([1.0, 1.5, 2.0])[:W] if score > -1e38 else \
+        torch.tensor([[score, float("-inf"), torch.finfo(torch.float32).min]])[:, :W]
+    for K in (1, 10, 64):
+        got = check_step(x, s, K, V, T=T)
+        assert got["parent"][0].tolist() == [0] * K
