@@ -7,6 +7,7 @@
 namespace hs {
 
 // ---- launches (host side, defined next to their kernels) ----------------------------------------
+// A launch that fails leaves its error to the entry, which clears it and says what it was.
 
 // How a step's rows are cut: nc chunks of kBeamChunk vectors, in S slices of `chunks`, one wave each.
 constexpr int kBeamChunk = 256;  // 16-byte vectors of a chunk, four per lane

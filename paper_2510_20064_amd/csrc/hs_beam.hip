@@ -697,7 +697,7 @@ void launch_merge(const StepArgs& A, int B, hipStream_t st) {
 template <int DT>
 void launch_step(const StepArgs& A, int B, hipStream_t st) {
   hs_beam_rows_kernel<DT><<<(A.units + kWaves - 1) / kWaves, kThreads, 0, st>>>(A);
-  if (hipGetLastError() != hipSuccess) return;
+  if (hipPeekAtLastError() != hipSuccess) return;
   if (A.W <= kMergeWaves) launch_merge<DT, 1>(A, B, st);
   else if (A.W <= 2 * kMergeWaves) launch_merge<DT, 2>(A, B, st);
   else launch_merge<DT, HS_MAX_BEAMS / kMergeWaves>(A, B, st);
@@ -774,7 +774,7 @@ int launch_beam_step(const BeamGeom& g, const hs_beam_args& a, hipStream_t strea
   if (g.dtype == HS_F32) launch_step<HS_F32>(A, g.B, stream);
   else if (g.dtype == HS_F16) launch_step<HS_F16>(A, g.B, stream);
   else launch_step<HS_BF16>(A, g.B, stream);
-  return hipGetLastError() == hipSuccess ? HS_OK : HS_ERR_HIP;
+  return hipPeekAtLastError() == hipSuccess ? HS_OK : HS_ERR_HIP;
 }
 
 }  // namespace hs

@@ -544,7 +544,7 @@ int launch_reorder(const hs_state* states, int n, int B, int W, int K, const int
       else if (!odd) launch_words<true, false>(A, (uint32_t)grid, stream);
       else if (stream_past) launch_words<false, true>(A, (uint32_t)grid, stream);
       else launch_words<false, false>(A, (uint32_t)grid, stream);
-      if (hipGetLastError() != hipSuccess) return HS_ERR_HIP;
+      if (hipPeekAtLastError() != hipSuccess) return HS_ERR_HIP;
     }
   }
   return HS_OK;

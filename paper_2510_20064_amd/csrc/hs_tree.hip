@@ -192,7 +192,7 @@ int launch_draft_tree(const hs_tree_args& a, hipStream_t stream) {
   else if (N <= 512) hs_tree_kernel<8><<<a.B, kThreads, 0, stream>>>(a);
   else if (N <= 1024) hs_tree_kernel<16><<<a.B, kThreads, 0, stream>>>(a);
   else hs_tree_kernel<kNodes / 64><<<a.B, kThreads, 0, stream>>>(a);
-  return hipGetLastError() == hipSuccess ? HS_OK : HS_ERR_HIP;
+  return hipPeekAtLastError() == hipSuccess ? HS_OK : HS_ERR_HIP;
 }
 
 }  // namespace hs
