@@ -225,7 +225,8 @@ HS_API int hs_stream_read(const void* x, size_t bytes, int grid, int unroll, int
     return fail(HS_ERR_ARG, "hs_stream_read: unroll must be 1, 2, 4 or 8 (got %d)", unroll);
   const int rc = hs::launch_stream_read(x, bytes / 16, grid, unroll, nontemporal != 0, out,
                                         (hipStream_t)stream);
-  return rc == HS_OK ? HS_OK : fail(rc, "hs_stream_read: launch failed");
+  if (rc) return fail(rc, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+  return HS_OK;
 }
 
 HS_API int hs_softmax_stats(const void* logits, int dtype, int64_t rows, int64_t V, int64_t ld,

@@ -304,7 +304,7 @@ int launch_argmax(const TeamGeom& g, const RowTable& rows, uint8_t* agree, int32
   if (g.dtype == HS_F32) hs_argmax_kernel<HS_F32><<<grid, kThreads, 0, stream>>>(A);
   else if (g.dtype == HS_F16) hs_argmax_kernel<HS_F16><<<grid, kThreads, 0, stream>>>(A);
   else hs_argmax_kernel<HS_BF16><<<grid, kThreads, 0, stream>>>(A);
-  return hipGetLastError() == hipSuccess ? HS_OK : HS_ERR_HIP;
+  return hipPeekAtLastError() == hipSuccess ? HS_OK : HS_ERR_HIP;
 }
 
 }  // namespace hs

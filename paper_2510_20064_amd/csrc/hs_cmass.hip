@@ -82,7 +82,7 @@ int launch_candidate_mass(const void* tptr, int64_t sb, int64_t sk, int dtype, i
   if (dtype == HS_F32) hs_cmass_kernel<HS_F32><<<grid, kThreads, 0, stream>>>(A);
   else if (dtype == HS_F16) hs_cmass_kernel<HS_F16><<<grid, kThreads, 0, stream>>>(A);
   else hs_cmass_kernel<HS_BF16><<<grid, kThreads, 0, stream>>>(A);
-  return hipGetLastError() == hipSuccess ? HS_OK : HS_ERR_HIP;
+  return hipPeekAtLastError() == hipSuccess ? HS_OK : HS_ERR_HIP;
 }
 
 }  // namespace hs

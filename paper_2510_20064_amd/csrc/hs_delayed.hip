@@ -89,7 +89,7 @@ int launch_delayed(const DelayArgs& a, hipStream_t stream) {
   const size_t lds = sizeof(double) * ((size_t)a.K * a.N + kLearnScratch) +
                      sizeof(float) * 2 * (size_t)a.K * a.N;
   hs_delayed_kernel<<<a.B, 64, lds, stream>>>(a);
-  return hipGetLastError() == hipSuccess ? HS_OK : HS_ERR_HIP;
+  return hipPeekAtLastError() == hipSuccess ? HS_OK : HS_ERR_HIP;
 }
 
 }  // namespace hs

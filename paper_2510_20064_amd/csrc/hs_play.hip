@@ -92,7 +92,7 @@ __global__ __launch_bounds__(64) void hs_regret_kernel(const double* loss, int L
 int launch_play(const double* w, int B, int N, int how, const double* u, int32_t* choice,
                 hipStream_t stream) {
   hs_play_kernel<<<B, 64, 0, stream>>>(w, B, N, how, u, choice);
-  return hipGetLastError() == hipSuccess ? HS_OK : HS_ERR_HIP;
+  return hipPeekAtLastError() == hipSuccess ? HS_OK : HS_ERR_HIP;
 }
 
 int launch_regret(const double* loss, int L, int B, int N, const int32_t* played, double* cum,
@@ -100,7 +100,7 @@ int launch_regret(const double* loss, int L, int B, int N, const int32_t* played
                   hipStream_t stream) {
   hs_regret_kernel<<<B, 64, 0, stream>>>(loss, L, B, N, played, cum, played_sum, regret, eal,
                                          eal_sum);
-  return hipGetLastError() == hipSuccess ? HS_OK : HS_ERR_HIP;
+  return hipPeekAtLastError() == hipSuccess ? HS_OK : HS_ERR_HIP;
 }
 
 }  // namespace hs

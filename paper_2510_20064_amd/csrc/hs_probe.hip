@@ -40,7 +40,7 @@ __global__ __launch_bounds__(kProbeThreads) void stream_read_kernel(const u32x4*
 template <int U, bool NT>
 int launch_one(const void* x, uint64_t n, int grid, uint32_t* out, hipStream_t s) {
   stream_read_kernel<U, NT><<<grid, kProbeThreads, 0, s>>>(static_cast<const u32x4*>(x), n, out);
-  return hipGetLastError() == hipSuccess ? HS_OK : HS_ERR_HIP;
+  return hipPeekAtLastError() == hipSuccess ? HS_OK : HS_ERR_HIP;
 }
 
 }  // namespace

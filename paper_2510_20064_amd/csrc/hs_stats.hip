@@ -150,7 +150,7 @@ int launch_softmax_stats(const void* x, int dtype, int64_t rows, int64_t V, int6
     launch_rows<HS_F16>(xp, rows, V, ld, nvec, c, row_max, row_lse, row_argmax, stream);
   else
     launch_rows<HS_BF16>(xp, rows, V, ld, nvec, c, row_max, row_lse, row_argmax, stream);
-  return hipGetLastError() == hipSuccess ? HS_OK : HS_ERR_HIP;
+  return hipPeekAtLastError() == hipSuccess ? HS_OK : HS_ERR_HIP;
 }
 
 }  // namespace hs

@@ -23,7 +23,7 @@ __global__ __launch_bounds__(64) void hs_tail_kernel(TailArgs a) {
 int launch_tail(const TailArgs& a, hipStream_t stream) {
   const size_t lds = sizeof(double) * (size_t)tail_lds_doubles(a);
   hs_tail_kernel<<<a.B, 64, lds, stream>>>(a);
-  return hipGetLastError() == hipSuccess ? HS_OK : HS_ERR_HIP;
+  return hipPeekAtLastError() == hipSuccess ? HS_OK : HS_ERR_HIP;
 }
 
 }  // namespace hs

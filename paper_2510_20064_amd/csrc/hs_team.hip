@@ -1409,7 +1409,7 @@ int launch_team_argmax(TeamArgs A, const TeamGeom& g, hipStream_t stream, bool* 
   A.learn = 0;
   A.teams = (int)teams;
   hs_team_argmax_kernel<DT, D><<<(unsigned)(A.teams * g.S), kThreads, 0, stream>>>(A);
-  return hipGetLastError() == hipSuccess ? HS_OK : HS_ERR_HIP;
+  return hipPeekAtLastError() == hipSuccess ? HS_OK : HS_ERR_HIP;
 }
 
 // Calls F<DT, D, NA>::run(args...) for the geometry and mode.
@@ -1540,7 +1540,7 @@ int launch_round(const TeamGeom& g, const RowTable& rows, float c, bool need_sum
   bool learned = false;
   int rc = dispatch<Launch>(g, need_arg, A, g, stream, &learned);
   if (rc) return rc;
-  if (hipGetLastError() != hipSuccess) return HS_ERR_HIP;
+  if (hipPeekAtLastError() != hipSuccess) return HS_ERR_HIP;
   return tail && !learned ? tail_after() : HS_OK;
 }
 

@@ -678,7 +678,7 @@ template <int DT>
 void launch_t(const TopArgs& A, int64_t nrows, hipStream_t st) {
   const int64_t wgs = ((int64_t)A.units + kWaves - 1) / kWaves;
   hs_topl_slice_kernel<DT><<<(unsigned)wgs, kThreads, 0, st>>>(A);
-  if (hipGetLastError() != hipSuccess) return;
+  if (hipPeekAtLastError() != hipSuccess) return;
   hs_topl_merge_kernel<DT><<<(unsigned)((nrows + kWaves - 1) / kWaves), kThreads, 0, st>>>(A);
 }
 
@@ -723,7 +723,7 @@ int launch_topl(const TeamGeom& g, const RowTable& rows, int L, float c, bool wa
   if (g.dtype == HS_BF16) launch_t<HS_BF16>(A, (int64_t)nrows, stream);
   else if (g.dtype == HS_F16) launch_t<HS_F16>(A, (int64_t)nrows, stream);
   else launch_t<HS_F32>(A, (int64_t)nrows, stream);
-  return hipGetLastError() == hipSuccess ? HS_OK : HS_ERR_HIP;
+  return hipPeekAtLastError() == hipSuccess ? HS_OK : HS_ERR_HIP;
 }
 
 }  // namespace hs

@@ -70,6 +70,27 @@ def tree(hs, D=7, B=2, K=10, M=61):
     return hs.load_library().hs_draft_tree(ctypes.byref(a), None)
 
 
+def topl(hs, B=2, N=2, K=4, V=32000, L=4, dtype=1):
+    views = (hs.hs_view * (N + 1))(*[hs.hs_view(FAKE * (i + 1) * 16, K * V, V) for i in range(N + 1)])
+    lib = hs.load_library()
+    return lib.hs_eval_topl(views, ctypes.cast(ctypes.byref(views, ctypes.sizeof(hs.hs_view)),
+                                               ctypes.POINTER(hs.hs_view)), N, B, K, V, dtype, L, 1.0, hs.SAMPLE,
+                            1 << 40, 1 << 41, 1 << 42, 1 << 50,
+                            lib.hs_eval_topl_workspace_size(B, N, K, V, L, dtype), None)
+
+
+def stats(hs, rows=2, V=64):
+    return hs.load_library().hs_softmax_stats(FAKE, 1, rows, V, V, 1.0, FAKE << 4, FAKE << 5, FAKE << 6, None)
+
+
+def stream_read(hs):
+    return hs.load_library().hs_stream_read(FAKE, 4096, 4, 1, 0, FAKE << 4, None)
+
+
+def play(hs):
+    return hs.load_library().hs_play(FAKE, 2, 3, 0, None, FAKE << 4, None)
+
+
 def main():
     rec = ctypes.CDLL(sys.argv[1], mode=ctypes.RTLD_GLOBAL)  # before anything that loads the runtime
     sys.path.insert(0, ROOT)
@@ -100,6 +121,16 @@ def test_a_failed_launch_is_an_error(recorder):
     for (name, kw, fail_at), a in zip(calls, ask(recorder, *calls)):
         assert a["rc"] == ERR_HIP, (name, kw, fail_at)
         assert len(a["launches"]) == fail_at + 1, (name, kw, fail_at)
+        assert a["error"].startswith("kernel launch failed: ") and "no error" not in a["error"], a["error"]
+        assert a["pending"] == 0
+
+
+def test_a_failed_launch_of_an_evaluation_is_an_error(recorder):
+    got = ask(recorder, ("topl", {}, -1), ("stats", {}, -1), ("stream_read", {}, -1), ("play", {}, -1))
+    assert [a["rc"] for a in got] == [OK] * 4 and [len(a["launches"]) for a in got] == [2, 1, 1, 1]
+    calls = [("topl", {}, 0), ("topl", {}, 1), ("stats", {}, 0), ("stream_read", {}, 0), ("play", {}, 0)]
+    for (name, kw, fail_at), a in zip(calls, ask(recorder, *calls)):
+        assert a["rc"] == ERR_HIP and len(a["launches"]) == fail_at + 1, (name, fail_at)
         assert a["error"].startswith("kernel launch failed: ") and "no error" not in a["error"], a["error"]
         assert a["pending"] == 0
 
