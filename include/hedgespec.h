@@ -479,7 +479,8 @@ int hs_beam_step(const hs_beam_args* args, void* stream);
  *            [0, units]); what lies behind them is left as it was.
  * W         : beams in src; K: slots in dst, 1 .. HS_MAX_BEAMS each (in place the buffer holds
  *             max(W, K)). Any alignment.
- * n         : tensors, 1 .. HS_MAX_STATES. One launch for every 32 of them.
+ * n         : tensors, 1 .. HS_MAX_STATES. One launch for every 32 of them (of up to 2^24 workgroups of 4 KB of a
+ *             slot, or of four short rows).
  */
 typedef struct hs_state {
   const void* src;

@@ -7,6 +7,8 @@
 namespace hs {
 
 // ---- launches (host side, defined next to their kernels) ----------------------------------------
+// Workgroups of 256 threads of one launch: the runtime takes fewer than 2^32 threads. (A multiple of the 8 XCDs.)
+constexpr uint32_t kMostGroups = (1u << 24) - 8;
 // A launch that fails leaves its error to the entry, which clears it and says what it was.
 
 // How a step's rows are cut: nc chunks of kBeamChunk vectors, in S slices of `chunks`, one wave each.
@@ -19,7 +21,7 @@ struct BeamGeom {
 bool beam_geom(int B, int W, int K, int64_t V, int dtype, BeamGeom* g);
 size_t beam_ws_bytes(const BeamGeom& g);
 int launch_beam_step(const BeamGeom& g, const hs_beam_args& a, hipStream_t stream);
-bool reorder_fits(const hs_state& s, int B, bool counted);  // its workgroups are numbered with 31 bits
+bool reorder_fits(const hs_state& s, int B, bool counted);  // its workgroups, of all launches, are numbered with 31 bits
 // Whether the rows of a state's dst (B queries, K slots, `row` bytes a row) are apart from each other.
 bool state_apart(const hs_state& s, int B, int K, int64_t row);
 // The bytes that `beams` beams of every query span from a state's pointer; false where they do not fit

@@ -29,6 +29,7 @@
 // units and 64 slots (an instruction that all of its 16 waves make costs 16 cycles). Two launches: in
 // one, with a query's last workgroup merging, the fences between the XCDs' caches cost what the second
 // launch does (10 rows of bf16 13.3 us, or 11.4 with device-scope words instead of fences; two 10.8).
+#include <algorithm>
 #include <cfloat>
 
 #include "hs_beam.h"
@@ -59,6 +60,7 @@ struct StepArgs {
   int nu;                   // units per row
   int64_t V, nvec, score_stride;
   uint32_t units;  // B * W * S
+  uint32_t group0;  // the launch's first workgroup of the rows kernel's
   FastDiv divS, divW, divU;  // by S, W and nu
   float ca, cb;
   double c, inv_c;  // c and 1 / c
@@ -165,7 +167,7 @@ __global__ __launch_bounds__(kThreads) void hs_beam_rows_kernel(StepArgs A) {
   constexpr int E = Vt::kElems;
   const int lane = threadIdx.x & 63;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t u = blockIdx.x * kWaves + wv;
+  const uint32_t u = (A.group0 + blockIdx.x) * kWaves + wv;
   if (u >= A.units) return;  // wave-uniform; the waves share nothing
   const uint32_t row = fdiv(u, A.divS);
   const int s = (int)(u - row * (uint32_t)A.S);
@@ -695,9 +697,12 @@ void launch_merge(const StepArgs& A, int B, hipStream_t st) {
 }
 
 template <int DT>
-void launch_step(const StepArgs& A, int B, hipStream_t st) {
-  hs_beam_rows_kernel<DT><<<(A.units + kWaves - 1) / kWaves, kThreads, 0, st>>>(A);
-  if (hipPeekAtLastError() != hipSuccess) return;
+void launch_step(StepArgs A, int B, hipStream_t st) {
+  const uint32_t groups = (A.units + kWaves - 1) / kWaves;
+  for (A.group0 = 0; A.group0 < groups; A.group0 += kMostGroups) {
+    hs_beam_rows_kernel<DT><<<std::min(groups - A.group0, kMostGroups), kThreads, 0, st>>>(A);
+    if (hipPeekAtLastError() != hipSuccess) return;
+  }
   if (A.W <= kMergeWaves) launch_merge<DT, 1>(A, B, st);
   else if (A.W <= 2 * kMergeWaves) launch_merge<DT, 2>(A, B, st);
   else launch_merge<DT, HS_MAX_BEAMS / kMergeWaves>(A, B, st);

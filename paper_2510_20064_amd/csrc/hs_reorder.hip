@@ -44,6 +44,7 @@ struct MoveArgs : MoveCall {
 };
 // Tensors that differ in their pointers only: the caches of a model's layers.
 struct AlikeArgs : MoveCall {
+  uint32_t group0;  // the launch's first workgroup of each tensor's
   MoveState st;
   const char* src[kStates];
   char* dst[kStates];
@@ -71,7 +72,7 @@ __device__ __forceinline__ uint32_t pick(const AlikeArgs& A, MoveState& S) {
   S = A.st;
   S.src = A.src[blockIdx.y];
   S.dst = A.dst[blockIdx.y];
-  return blockIdx.x;
+  return A.group0 + blockIdx.x;
 }
 
 typedef unsigned int Vec16 __attribute__((ext_vector_type(4)));
@@ -267,7 +268,11 @@ void launch_words(const MoveArgs<kStates>& A, uint32_t grid, hipStream_t st) {
       like.src[j] = A.st[j].src;
       like.dst[j] = A.st[j].dst;
     }
-    launch_slots<ALIGNED, STREAM>(like, wide, dim3(grid / A.n, A.n), st);
+    const uint32_t groups = grid / A.n;
+    for (like.group0 = 0; like.group0 < groups; like.group0 += kMostGroups) {
+      launch_slots<ALIGNED, STREAM>(like, wide, dim3(std::min(groups - like.group0, kMostGroups), A.n), st);
+      if (hipPeekAtLastError() != hipSuccess) return;
+    }
   } else if (A.n <= kFew) {
     MoveArgs<kFew> few;
     static_cast<MoveCall&>(few) = A;
@@ -517,7 +522,8 @@ int launch_reorder(const hs_state* states, int n, int B, int W, int K, const int
         const int span = span_of(s, K, wide, split);
         const uint64_t parts = parts_of(s, span, split), of = span == 0 ? kWaves >> split : 1;
         const uint64_t wgs = (parts * (uint64_t)s.rows * (uint64_t)B + of - 1) / of;
-        if (grid + wgs >= (1ull << 31)) break;
+        // (a tensor of more than a launch's workgroups is by itself, in several launches)
+        if (A.n > 0 && grid + wgs > kMostGroups) break;
         A.first[A.n] = (uint32_t)grid;
         MoveState& m = A.st[A.n++];
         m.src = reinterpret_cast<const char*>(s.src);

@@ -1047,3 +1047,33 @@ def test_step_logits_that_score_the_same(dtype, W, T, score):
     for K in (1, 10, 64):
         got = check_step(x, s, K, V, T=T)
         assert got["parent"][0].tolist() == [0] * K
+
+
+def test_step_of_more_workgroups_than_a_launch():
+    """65535 queries of 64 beams that share one row of logits: 18.9 million workgroups, 2^24 a launch."""
+    note("many workgroups: step")
+    g = torch.Generator().manual_seed(97)
+    B, W, V, K = 65535, 64, 70000, 5
+    x = rows(g, 1, 1, V, torch.bfloat16)
+    s = torch.stack([scores(g, 1, W)[0] for _ in range(3)])
+    s[1, 1:] = float("-inf")
+    out = hs.beam_step(x.cuda().expand(B, W, -1), s.cuda()[torch.arange(B, device="cuda") % 3], K, V=V)
+    ref = beam.beam_step(x.expand(3, W, -1)[:, :, :V].double().numpy(), s.numpy(), K)
+    torch.cuda.synchronize()
+    same_step({k: v[:3].cpu().numpy() for k, v in out.items()}, ref)
+    for v in out.values():
+        v = v.view(B // 3, 3, K)
+        assert torch.equal(v, v[:1].expand_as(v))
+
+
+@pytest.mark.parametrize("K", [1, 2])
+def test_reorder_of_more_workgroups_than_a_launch(K):
+    note("many workgroups: reorder K=%d" % K)
+    B, W, H = 65535, 2, 1030
+    x = torch.arange(B * W * H * 2, dtype=torch.int32, device="cuda").to(torch.uint8).view(B, W, H, 2)
+    parent = torch.tensor([[1, 0]], dtype=torch.int32, device="cuda").expand(B, W).contiguous()[:, :K]
+    count = torch.arange(B, dtype=torch.int32, device="cuda") % 3 - 1    # -1, 0 and 1 of one unit
+    want = x.clone()
+    want[2::3, :K, :, 0] = x[2::3].flip(1)[:, :K, :, 0]
+    hs.beam_reorder(x[..., :1], parent, count=count, axis=3)
+    assert torch.equal(x, want)

@@ -135,5 +135,29 @@ def test_a_failed_launch_of_an_evaluation_is_an_error(recorder):
         assert a["pending"] == 0
 
 
+def test_no_launch_is_larger_than_the_runtime_takes(recorder):
+    """A launch holds fewer than 2^32 threads along each of its dimensions: larger calls are several launches, which
+    together have every workgroup (a wave a slice of two chunks of 256 vectors; a workgroup four short rows, a row of up
+    to 16 KB of few slots, or 4 KB of a longer one)."""
+    calls = [("step", dict(B=65535, W=64, V=1 << 20, shared_rows=True), -1),
+             ("step", dict(B=65535, W=64, V=70000, shared_rows=True), -1),
+             ("step", dict(B=65535, W=64, V=200, shared_rows=True), -1),
+             ("reorder", dict(B=65535, W=1, K=1, rows=1030, units=1, unit=1, gap=1, counted=True), -1),
+             ("reorder", dict(n=33, B=65535, W=2, K=2, rows=30, units=1, unit=5000, gap=4, inplace=True), -1),
+             ("reorder", dict(B=1, W=1, K=1, units=1 << 37, unit=1), -1),
+             ("reorder", dict(B=3, W=16, K=16, units=1 << 35, unit=1), -1),
+             ("reorder", dict(n=2, B=40000, W=4, K=4, rows=500, units=5, unit=1000, gap=1, inplace=True), -1)]
+    least = [65535 * 64 * 256 / 4, 65535 * 64 * 18 / 4, 65535 * 64 / 4, 65535 * 1030 / 4, 33 * 65535 * 30,
+             (1 << 37) / 4096, 3 * (1 << 35) / 4096, 2 * 40000 * 500]
+    for (name, kw, _), need, a in zip(calls, least, ask(recorder, *calls)):
+        assert a["rc"] == OK, (name, kw, a["error"])
+        work = a["launches"][:-1] if name == "step" else a["launches"]
+        threads = {tuple(v[3:]) for v in work}
+        assert threads == {(256, 1, 1)}, (name, kw)
+        assert sum(v[0] * v[1] * v[2] for v in work) >= need, (name, kw)
+        if name == "step":
+            assert a["launches"][-1] == [kw["B"], 1, 1, 1024, 1, 1]
+
+
 if __name__ == "__main__":
     main()
