@@ -871,6 +871,9 @@ class TreeGrowth:
     states: the drafter's per-beam tensors [B][W]... (caches, hidden states; the root's in beam 0),
     which follow the W beams in place after every level but the last.
 
+    The constructor waits for the current stream, so that the levels may run on any stream, each ordered
+    behind the one before it; the growth is kept until that work is done.
+
         growth = TreeGrowth(B, depth, W, K, M, states=[hidden], device=dev)
         token = growth.level(draft(root))        # logits [B][1][V]; token [B][W] to draft from
         for _ in range(depth - 1):
@@ -891,6 +894,10 @@ class TreeGrowth:
         self.parent = torch.empty(shape, dtype=torch.int32, device=dev)
         self.token = torch.empty(shape, dtype=torch.int32, device=dev)
         self.root = torch.zeros((B, 1), dtype=torch.float32, device=dev)
+        if dev.type == "cuda" and not torch.cuda.is_current_stream_capturing():
+            # level() may run on any stream: the zeros are there, and nothing of the current stream still
+            # uses the memory of these tensors
+            torch.cuda.current_stream(dev).synchronize()
         states = [states] if isinstance(states, torch.Tensor) else list(states)
         _need(all(t.dim() >= 2 and t.shape[1] == W for t in states), "a state is [B][W]...")
         self._moves = [BeamReorder(states, self.parent[d][:, :W], count=count, axis=axis)

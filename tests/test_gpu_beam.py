@@ -1077,3 +1077,26 @@ def test_reorder_of_more_workgroups_than_a_launch(K):
     want[2::3, :K, :, 0] = x[2::3].flip(1)[:, :K, :, 0]
     hs.beam_reorder(x[..., :1], parent, count=count, axis=3)
     assert torch.equal(x, want)
+
+
+def test_growth_made_and_used_at_once_on_another_stream():
+    """The current stream is busy when the growth is made, and its memory held NaN before: the first level, on
+    a stream that waits for nothing, has the root's scores all the same."""
+    note("growth on a stream of its own")
+    g = torch.Generator().manual_seed(101)
+    B, depth, W, K, M, V = 2, 3, 4, 8, 12, 3000
+    xs, st = _growth_inputs(g, B, W, depth, V, torch.bfloat16)
+    s0 = st.clone()
+    side = torch.cuda.Stream()
+    busy = torch.zeros(1 << 28, device="cuda")
+    was = [torch.full((B, 1), float("nan"), device="cuda") for _ in range(256)]
+    torch.cuda.synchronize()
+    del was
+    for _ in range(50):
+        busy.add_(1.0)                             # 2 GB each
+    growth = hs.TreeGrowth(B, depth, W, K, M, states=[st], device="cuda")
+    out = _grow(growth, xs, V, stream=side)
+    torch.cuda.synchronize()
+    want = _grow(hs.TreeGrowth(B, depth, W, K, M, states=[s0], device="cuda"), xs, V)
+    assert torch.equal(st, s0)
+    assert all(torch.equal(out[k], want[k]) for k in want)
