@@ -902,7 +902,7 @@ class TreeGrowth:
         _need(all(t.dim() >= 2 and t.shape[1] == W for t in states), "a state is [B][W]...")
         self._moves = [BeamReorder(states, self.parent[d][:, :W], count=count, axis=axis)
                        for d in range(depth - 1)] if states else []
-        self._plans = [None] * depth
+        self._plans = {}  # by level, V and type; none is dropped, since a captured graph may hold its buffers
         self._tree = DraftTree(self.score, self.parent, self.token, M)
         self.d = 0
 
@@ -911,15 +911,15 @@ class TreeGrowth:
         [B][W] of the beams to draft from next (-1: an empty slot), until the next tree's same level."""
         d = self.d
         _need(d < self.depth, "the tree has all its levels: tree() ends it")
-        plan = self._plans[d]
-        if plan is None or plan.V != (logits.shape[2] if V is None else V) or \
-                plan.dtype != _dtype_code(logits):
+        key = d, logits.shape[-1] if V is None else V, _dtype_code(logits)
+        plan = self._plans.get(key)
+        if plan is None:
             up = self.root if d == 0 else self.score[d - 1][:, :self.W]
             with _on(stream):
                 plan = BeamStep(logits, up, self.K, V=V, temperature=self.temperature,
                                 out={"score": self.score[d], "parent": self.parent[d],
                                      "token": self.token[d]})
-            self._plans[d] = plan
+            self._plans[key] = plan
         plan.set_logits(logits)
         plan.run(stream)
         if d < len(self._moves):

@@ -1,9 +1,11 @@
 """Refusals of hs_beam_step, hs_beam_reorder and hs_draft_tree: the C ABI's codes before any HIP call
 (the pointers are fakes, never dereferenced) and the binding's checks before the library is called."""
 import ctypes
+import gc
 import os
 import random
 import re
+import weakref
 
 import pytest
 import torch
@@ -296,3 +298,26 @@ def test_draft_tree_and_growth_binding_refuse():
         kw = dict(B=1, depth=3, W=2, K=4, M=5, device="cpu")
         kw.update(bad)
         _refused(lambda: hs.TreeGrowth(**kw), "need 1 <= depth")
+
+
+def test_growth_keeps_what_a_captured_graph_uses(monkeypatch):
+    """A tree of one row length may be in a graph while one of another is grown: no level's plan and workspace are
+    given up for another's, and a length that comes again has the one it had. (Nothing is launched.)"""
+    made = []
+
+    class Step(hs.BeamStep):
+        def __init__(self, *a, **kw):
+            super().__init__(*a, **kw)
+            made.append(weakref.ref(self))
+
+    monkeypatch.setattr(hs, "BeamStep", Step)
+    monkeypatch.setattr(hs, "_one_device", lambda *t: torch.device("cpu"))
+    monkeypatch.setattr(hs, "_launch", lambda *a: None)
+    growth = hs.TreeGrowth(2, 2, 3, 4, 5, device="cpu")
+    for V, dt in ((64, torch.float32), (72, torch.float32), (64, torch.bfloat16), (64, torch.float32)):
+        for n in (1, 3):
+            growth.level(torch.zeros((2, n, V), dtype=dt))
+        growth.tree()
+    gc.collect()
+    assert all(r() is not None for r in made)
+    assert len(made) == 2 * 3 and len({r().workspace.data_ptr() for r in made}) == 6
