@@ -1100,3 +1100,122 @@ def test_growth_made_and_used_at_once_on_another_stream():
     want = _grow(hs.TreeGrowth(B, depth, W, K, M, states=[s0], device="cuda"), xs, V)
     assert torch.equal(st, s0)
     assert all(torch.equal(out[k], want[k]) for k in want)
+
+
+def logits_of(dtype):
+    """Logits of a 16-byte vector and of a chunk of 256, and a row length of an odd number of chunks (the last slice
+    is short) from which on 258 rows are cut into slices of two."""
+    return (4, 1024, 39001) if dtype == "f32" else (8, 2048, 70001)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("T", [1.0, 0.3])
+def test_step_slices_of_two_chunks(dtype, T):
+    """What one chunk of a slice holds against the other: nothing, the lowest value, logits higher by little, by
+    much and by nearly the type's range, no number."""
+    note("two chunks %s T=%g" % (dtype, T))
+    dt = DTYPES[dtype]
+    _, chunk, V = logits_of(dtype)
+    g = torch.Generator().manual_seed(103)
+    B, W, K = 258, 1, 6
+    x = rows(g, B, W, V, dt)
+    z = x[:, 0, :V]
+    place = torch.arange(V) // chunk
+    low, far = torch.finfo(dt).min, {"f32": 3e38, "bf16": 3e38, "f16": 6e4}[dtype]
+    high = {"f32": 1e6, "bf16": 1e6, "f16": 3e4}[dtype]
+    nan, inf = float("nan"), float("inf")
+    for b in range(B):
+        half = place % 2 == b % 2                      # the first or the second chunk of a slice
+        if b // 2 % 2:
+            half &= place // 2 % 3 == 1                # of some slices
+        one = int(torch.randint(0, len(place) // chunk, (1,), generator=g)) // 2 * 2 + b % 2
+        at = min(one * chunk + int(torch.randint(0, chunk, (1,), generator=g)), V - 1)
+        kind = b // 4 % 12
+        if kind == 0:
+            z[b, half] = -inf
+        elif kind == 1:
+            z[b, half] = low
+        elif kind in (2, 3, 4, 5):                     # about the 4 (in log2) at which the offset moves
+            z[b, half] = (z[b, half].float() + (2.0, 3.0, 6.0, 40.0)[kind - 2]).to(dt)
+        elif kind == 6:
+            z[b, half] = (z[b, half].float() + high).to(dt)
+        elif kind == 7:
+            z[b, half] = far
+        elif kind == 8:
+            z[b, half] = -far
+        elif kind == 9:
+            z[b, at] = nan if b % 8 < 4 else inf
+        elif kind == 10:                               # one logit in all
+            z[b] = -inf
+            z[b, at] = -3.0
+        else:                                          # one above the lowest
+            z[b] = low
+            z[b, at] = 1.5
+    check_step(x, scores(g, B, W), K, V, T=T)
+
+
+def normaliser_error(z, T, dtype):
+    """How far log softmax(z / T) may be off for fp64 logits z of one row, |z / T| log2(e) <= 4096: the kernel's terms
+    2^x, x = z c - off, u = 2^-24, each a share p of the sum.
+      - a term's exponential: 2 u (one unit in the last place); its exponent: two roundings of at most |x| u, and
+        2^-35 |z c| of c's lower part, times ln 2. off lies less than 1 above and 4 below the slice's
+        maximum, so |x| <= (max - z) c + 4. One term of each unit (the largest) has neither: it is replaced
+        in fp64, by a series of degree 8 in |f| <= ln 2 / 2: f^9 / 9! of 2^-1/2, 2.8e-10 of itself;
+      - the log2 E additions of a vector's terms in fp32: u of the sum each, and never more than the smaller addend
+        (the larger one is a number the sum could be rounded to), so that a term much larger than its vector's
+        others is kept;
+      - the logarithm 1e-11 (in log2), and fp64 roundings: 3e-10 with the 2.8e-10 above."""
+    E = 4 if dtype == "f32" else 8
+    u, add = 2.0 ** -24, 2 if dtype == "f32" else 3
+    c = 1.0 / (T * np.log(2.0))
+    n = -(-len(z) // (E * 256)) * E * 256
+    z = np.concatenate([z, np.full(n - len(z), -np.inf)])
+    m = z.max()
+    p = np.exp((z - m) / T)
+    p /= p.sum()
+    with np.errstate(invalid="ignore"):
+        e = np.where(p > 0, p * (2 * u + np.log(2.0) * (2 * u * ((m - z) * c + 4) + 2.0 ** -35 * np.abs(z) * c)), 0.0)
+    vec = np.arange(n) // E
+    unit = vec // 256 * 4 + vec % 64 // 16
+    for k in range(unit[-1] + 1):
+        mine = np.flatnonzero(unit == k)
+        e[mine[np.argmax(z[mine])]] = 0.0
+    of = p.reshape(-1, E)
+    sums = np.minimum(add * u * of.sum(1), add * (of.sum(1) - of.max(1)))
+    return e.sum() + sums.sum() + 3e-10
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("B", [6, 258])
+def test_step_normalisers(dtype, B):
+    """Scores near 0, where fp32 shows what the normalisers are good to: flat rows, a model's, and rows of one or two
+    logits that have nearly all of the mass."""
+    note("normalisers %s B=%d" % (dtype, B))
+    dt = DTYPES[dtype]
+    _, _, V = logits_of(dtype)
+    g = torch.Generator().manual_seed(107 + B)
+    x = rows(g, B, 1, V, dt, scale=1.0)
+    T, K = 0.9, 2
+    for b in range(B):
+        z = torch.randn(V, generator=g)
+        if b % 6 == 0:
+            z *= 0.3
+        elif b % 6 == 1:
+            z *= 3.0
+            z[torch.randint(0, V, (20,), generator=g)] += 8.0
+        elif b % 6 == 2:                               # a third banned, the rest below 0
+            z = torch.log_softmax(z * 2.0, 0)
+            z[::3] = float("-inf")
+        else:                                          # one or two logits, at any distance from an integer
+            at = torch.randint(0, V, (b % 6 - 2 if b % 6 < 5 else 1,), generator=g)
+            z[at] = 24.0 + 8.0 * torch.rand(1, generator=g)
+            if b % 6 == 5:
+                z -= 300.0
+        x[b, 0, :V] = z.to(dt)
+    ref = np.stack([np.sort(beam.row_log_softmax(x[b, 0, :V].double().numpy(), T))[::-1][:K] for b in range(B)])
+    s = torch.from_numpy((-ref[:, :1]).astype(np.float32))
+    out = hs.beam_step(x.cuda(), s.cuda(), K, V=V, temperature=T)["score"].cpu().double().numpy()
+    want = s.double().numpy() + ref
+    for b in range(B):
+        tol = normaliser_error(x[b, 0, :V].double().numpy(), T, dtype) + 2.0 ** -24 * np.abs(want[b])
+        assert np.all(np.abs(out[b] - want[b]) <= tol), (b, np.abs(out[b] - want[b]), tol)
