@@ -657,7 +657,9 @@ class BeamStep:
     logits [B][W][>= V] (V contiguous, rows 16-byte aligned), score [B][W] f32 (rows may be further
     apart), done [B][W] uint8 or bool with score's strides, or None. run() fills and returns `out`:
     score [B][K] f32, parent and token [B][K] i32 (-1: empty slot) and, where `out` has it, or done
-    or an eos is given, done [B][K] uint8. `workspace` may be shared by calls that do not overlap."""
+    or an eos is given, done [B][K] uint8. What the dict `out` lacks is made and added to it. `workspace` may
+    be shared by calls that do not overlap. What the plan makes belongs to the stream that is current then: order
+    a run on another one behind it, and keep the plan until that work is done."""
 
     def __init__(self, logits: torch.Tensor, score: torch.Tensor, K: int, V: Optional[int] = None,
                  temperature: float = 1.0, done: Optional[torch.Tensor] = None, eos: int = -1,
@@ -824,7 +826,8 @@ class DraftTree:
 
     score f32, parent and token i32: [D][B][K], as D calls of BeamStep leave them. run() fills and
     returns `out`: token, parent, depth, slot [B][M] i32, score [B][M] f32, mask [B][M] i64 (ancestor
-    bits), cand [B][M][K] i32 (candidate_mass takes it as cand[:, None]) and count [B] i32."""
+    bits), cand [B][M][K] i32 (candidate_mass takes it as cand[:, None]) and count [B] i32. What the dict `out`
+    lacks is made and added to it, and belongs to the stream that is current then (see BeamStep)."""
 
     def __init__(self, score: torch.Tensor, parent: torch.Tensor, token: torch.Tensor, M: int,
                  out: Optional[dict] = None):
@@ -867,6 +870,8 @@ class TreeGrowth:
     """EAGLE-2's dynamic draft tree, level by level, for B queries: from the root each of depth levels
     keeps the K best continuations, the W best of which are drafted further, and M - 1 nodes of all
     levels are verified with the root. Scheduling only: the steps run in the library's kernels.
+    The K best are those of all V tokens of every beam: a node's children are not first cut to a number of its own
+    best. With K >= M - 1 no node is lost that the M - 1 of all levels could contain.
 
     states: the drafter's per-beam tensors [B][W]... (caches, hidden states; the root's in beam 0),
     which follow the W beams in place after every level but the last.

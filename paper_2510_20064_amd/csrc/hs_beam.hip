@@ -13,10 +13,10 @@
 //      token).
 //
 // Precision. Two beams' candidates are often closer than fp32 tells apart and the order is part of
-// the result, so s is formed in fp64 and the normalisers are made good to 1e-7 (measured: 2e-9 rms on
-// flat rows, 3e-8 on peaked ones, 1.4e-7 at most): z c is taken
-// as z ca + z cb with ca = c rounded to 12 bits (for 16-bit logits z ca - offset is exact), each
-// lane adds its fp32 exponentials per chunk and the chunks in fp64, and the exponentials of the units'
+// the result, so s is formed in fp64 and the normalisers are made good to 1e-7 (measured: 3.5e-9 rms on
+// flat rows, 1.5e-8 on a model's, 3e-10 at most where one logit has the mass, 1.4e-7 at most of all): z c is
+// taken as z ca + z cb with ca = c rounded to 12 bits (for 16-bit logits z ca - offset is exact), the fp32
+// exponentials of a vector are added in pairs and the vectors in fp64, and the exponentials of the units'
 // largest logits, most of the sum where the distribution is peaked, are replaced by fp64 ones.
 // Sums are relative to an offset near the slice's maximum, and a slice whose maximum is large
 // (|z c| > 4096) takes z - maximum first, so that logits of any size do, the lowest finite value
@@ -28,7 +28,8 @@
 // for each other: 5.0 us for 4 rows of 128 units and 4 slots, 16.4 us for 32 workgroups of 32 rows of 300
 // units and 64 slots (an instruction that all of its 16 waves make costs 16 cycles). Two launches: in
 // one, with a query's last workgroup merging, the fences between the XCDs' caches cost what the second
-// launch does (10 rows of bf16 13.3 us, or 11.4 with device-scope words instead of fences; two 10.8).
+// launch does (10 rows of bf16 13.3 us, or 11.4 with device-scope words instead of fences; two 10.8). That was
+// measured on calls of few rows only, where there is nothing to merge behind.
 #include <algorithm>
 #include <cfloat>
 
@@ -38,7 +39,7 @@ namespace hs {
 
 namespace {
 
-constexpr int kMergeThreads = 1024;  // (256, 512: 10 rows of bf16 14.7, 11.8 us, 32 x 32 rows 89, 72; 10.7, 65)
+constexpr int kMergeThreads = 1024;  // (256, 512, 1024: 10 rows of bf16 14.7, 11.8, 10.7 us, 32 x 32 rows 89, 72, 65)
 constexpr int kMergeWaves = kMergeThreads / 64;
 constexpr int kAtOnce = 4;       // units that a wave reads at once
 constexpr int kPairs = 2048;     // entries of one query held in LDS, twice what a round can add
@@ -95,7 +96,7 @@ struct Offset {
   }
 };
 
-// 2^d for d < 1024 to 2e-10 of itself: 2^n e^(f ln 2), |f| <= 1/2, by the series of degree 8. (A wave
+// 2^d for d < 1024 to 2.8e-10 of itself: 2^n e^(f ln 2), |f| <= 1/2, by the series of degree 8. (A wave
 // computes it once or twice for a slice of 4096 logits: a quarter of the instructions of exp2().)
 __device__ inline double exp2_of(double d) {
   const double x = fmax(d, -2000.0), n = rint(x), f = (x - n) * 0.69314718055994530942;
@@ -158,7 +159,7 @@ __device__ inline void load_chunk(const char* row, int64_t v0, int64_t nvec, int
   }
 }
 
-// ---- launch 1: sums of slices, maxima of chunks ------------------------------------------------------
+// ---- launch 1: sums of slices, maxima of units -------------------------------------------------------
 
 template <int DT>
 __global__ __launch_bounds__(kThreads) void hs_beam_rows_kernel(StepArgs A) {

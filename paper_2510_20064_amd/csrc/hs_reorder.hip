@@ -318,7 +318,8 @@ constexpr __int128 kWideBytes = (__int128)16 << 20;
 // 12.9 shared, 11.2). A wave with one piece and one moving slot has one load in flight, hence up to four
 // pieces for it where few slots may move. In us, with one piece and four: 1 of 4 slots of 1.0 GB 88 and 50; 4
 // of 8 slots of 2.1 GB 205 and 187; all of 8 of 1.1 GB 310 and 322. Of more slots half of the calls lose: 3 of 15 30
-// and 18, but 7 of 16 151 and 164, 11 of 12 219 and 250, 16 of 16 333 and 415. The pieces lie a multiple of 8
+// and 18, but 7 of 16 151 and 164, 11 of 12 219 and 250, 16 of 16 333 and 415. (The host does not see how many of
+// a call's slots move: the rule bets on some of up to 8 in place, or 4, staying, and loses 4% where none does.) The pieces lie a multiple of 8
 // apart where there are enough, so that each XCD stays with its eighth of the memory's 4 KB pages (the 205
 // are 238 with pieces side by side).
 uint64_t row_bytes(const hs_state& s) { return (uint64_t)s.units * (uint64_t)s.unit; }
@@ -338,7 +339,8 @@ uint64_t parts_of(const hs_state& s, int span, int split) {
 // The waves (as a power of two) that share a position's slots where nothing is in place: fewer registers each, more
 // waves per CU. us with one wave and with this rule: 13 queries of 30 slots of 0.27 MB at odd addresses 41 and
 // 26, 7 of 31 of 1.2 MB 48 and 42, 4 of 64 of 2.5 MB 140 and 132, 9 of 32 of 0.1 MB 10.0 and 6.8, 15 of 28 of
-// 2.6 MB 372 and 385; 7 of 9 slots (two waves) 4.7 and 4.4, but 8 of 16 of 8 MB 327 and 346.
+// 2.6 MB 372 and 385 (what the rule loses: large aligned slots, 4%; K alone does not tell them from the others); 7 of 9
+// slots (two waves) 4.7 and 4.4, but 8 of 16 of 8 MB 327 and 346.
 int split_of(int K, bool past) { return K <= 8 ? 0 : K > 16 ? 2 : past ? 0 : 1; }
 
 }  // namespace
