@@ -535,6 +535,65 @@ typedef struct hs_tree_args {
 
 int hs_draft_tree(const hs_tree_args* args, void* stream);
 
+/*
+ * hs_verify - verification of a drafted chain or tree with given random numbers: which of its nodes the
+ * target accepts, and the token that the target draws behind the last of them. The tokens that come out are
+ * distributed as the target's own (speculative sampling, whose acceptance rate is Theorem 1's alpha, or, of a
+ * node's deterministic children, Theorem 2's mass on them).
+ * With p = softmax(target[b][n] / T) of a node n, and its children in the order of their numbers:
+ *   - without a drafter (the children are fixed: EAGLE's trees, greedy drafters), child c with token x is
+ *     accepted where u[b][c] S < p(x), S = what p has on all tokens but those of the children before it; of
+ *     children with one token the first alone can be. Behind a node of which no child is accepted the next token is
+ *     the first whose running sum of p, without all its children's tokens, exceeds u[b][0] times that mass;
+ *   - with a drafter (a chain whose token n + 1 was drawn from q = softmax(drafter[b][n] / T)), the
+ *     child is accepted where u q(x) < p(x), and otherwise the next token is drawn so from max(0, p - q), or
+ *     from p where that is 0 everywhere or q is no distribution;
+ *   - HS_GREEDY: a child is accepted where its token is the lowest index of the row's maximum, and that index is
+ *     the next token; u, drafter and temperature are not used.
+ * All of it in fp64; exponentials are good to 1.1e-12.
+ *   target      : one view [B][M][V] (stride_k from node to node), dtype as in hs_eval_alpha; node 0 is the
+ *                 root. A logit of -inf is no token. Behind a node whose row defines no distribution (all -inf, a
+ *                 NaN or a +inf logit) nothing is accepted and the next token is -1.
+ *   drafter     : ptr NULL: none. Otherwise a view [B][M - 1][V] of the same type; parent is then NULL.
+ *   token       : [B][M] int32: the nodes' tokens (the root's is not read). A token outside [0, V) is never
+ *                 accepted.
+ *   parent      : NULL: a chain, node n continues node n - 1. Otherwise [B][M] int32 (hs_draft_tree's
+ *                 node_parent); a node whose parents do not lead to the root is never reached.
+ *   count       : NULL: M nodes. Otherwise [B] int32: nodes of each query, the root included (clamped to
+ *                 [0, M]); those behind are not read. 0: no draft, nothing comes out.
+ *   depth       : 0 .. M - 1: nodes that lie further from the root are no part of the draft.
+ *   u           : [B][M] double in [0, 1): u[b][n] decides node n, u[b][0] draws the next token. HS_GREEDY: NULL.
+ *   out_path    : [B][M] int32: the root and the accepted nodes in their order, then -1.
+ *   out_token   : [B][M] int32: the tokens that come out: the accepted nodes', the next one, then -1.
+ *   out_length  : [B] int32: nodes on the path, which is the number of tokens that come out.
+ *   No output may overlap an input, another output or the workspace.
+ * workspace     : at least hs_verify_workspace_size() bytes of device memory, 256-byte aligned; scratch only.
+ * 1 <= M <= HS_MAX_POSITIONS, T from 1e-30 to 1e30. Deterministic.
+ */
+typedef struct hs_verify_args {
+  hs_view target;
+  hs_view drafter;
+  int B, M;
+  int64_t V;
+  int dtype;
+  int mode;
+  int depth;
+  double temperature;
+  const int32_t* token;
+  const int32_t* parent;
+  const int32_t* count;
+  const double* u;
+  int32_t* out_path;
+  int32_t* out_token;
+  int32_t* out_length;
+  void* workspace;
+  size_t workspace_bytes;
+} hs_verify_args;
+
+/* Bytes of device workspace hs_verify needs for this shape (0 on invalid shapes); drafter: nonzero with one. */
+size_t hs_verify_workspace_size(int B, int M, int64_t V, int dtype, int drafter);
+int hs_verify(const hs_verify_args* args, void* stream);
+
 /* Name of a status code; the thread's last error message; library version (major*10000+minor*100+patch). */
 const char* hs_status_string(int status);
 const char* hs_last_error(void);

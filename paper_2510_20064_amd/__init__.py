@@ -4,7 +4,7 @@ Argument marshalling only: every step runs in the library's HIP kernels. PyTorch
 device memory and the current HIP stream. The function names match the C ABI declared in
 include/hedgespec.h (hs_softmax_stats, hs_eval_alpha, hs_eval_topl, hs_accept_len,
 hs_hedge_update, hs_normalhedge_update, hs_delayed_update, hs_play, hs_regret_update,
-hs_round, hs_beam_step, hs_beam_reorder, hs_draft_tree). There is no CPU fallback: if the library is not built,
+hs_round, hs_beam_step, hs_beam_reorder, hs_draft_tree, hs_verify). There is no CPU fallback: if the library is not built,
 loading raises.
 """
 from __future__ import annotations
@@ -84,6 +84,17 @@ class hs_tree_args(ctypes.Structure):
                                        "node_score", "node_mask", "cand", "count")]
 
 
+class hs_verify_args(ctypes.Structure):
+    _fields_ = [
+        ("target", hs_view), ("drafter", hs_view), ("B", ctypes.c_int), ("M", ctypes.c_int),
+        ("V", ctypes.c_int64), ("dtype", ctypes.c_int), ("mode", ctypes.c_int), ("depth", ctypes.c_int),
+        ("temperature", ctypes.c_double), ("token", ctypes.c_void_p), ("parent", ctypes.c_void_p),
+        ("count", ctypes.c_void_p), ("u", ctypes.c_void_p), ("out_path", ctypes.c_void_p),
+        ("out_token", ctypes.c_void_p), ("out_length", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
 _lib = None
 
 
@@ -122,6 +133,9 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.hs_beam_step.argtypes = [ctypes.POINTER(hs_beam_args), P]
     lib.hs_beam_reorder.argtypes = [ctypes.POINTER(hs_state), I, I, I, I, P, I64, P, P]
     lib.hs_draft_tree.argtypes = [ctypes.POINTER(hs_tree_args), P]
+    lib.hs_verify_workspace_size.argtypes = [I, I, I64, I, I]
+    lib.hs_verify_workspace_size.restype = SZ
+    lib.hs_verify.argtypes = [ctypes.POINTER(hs_verify_args), P]
     lib.hs_set_wait_limit.argtypes = [I]
     lib.hs_set_wait_limit.restype = None
     lib.hs_stream_read.argtypes = [P, SZ, I, I, I, P, P]
@@ -131,7 +145,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     for name in ["hs_softmax_stats", "hs_eval_alpha", "hs_eval_alpha_noalloc", "hs_eval_topl", "hs_play", "hs_regret_update",
                  "hs_accept_len", "hs_hedge_update",
                  "hs_normalhedge_update", "hs_round", "hs_delayed_update", "hs_beam_step",
-                 "hs_beam_reorder", "hs_draft_tree", "hs_version"]:
+                 "hs_beam_reorder", "hs_draft_tree", "hs_verify", "hs_version"]:
         getattr(lib, name).restype = I
     _lib = lib
     return lib
@@ -943,3 +957,100 @@ class TreeGrowth:
     def restart(self) -> None:
         """Drops the levels grown: the next level() is the first of a new tree."""
         self.d = 0
+
+
+# ---- verifying a draft ----------------------------------------------------------------------------
+
+def verify_workspace_size(B: int, M: int, V: int, dtype: int, drafter: bool = False) -> int:
+    return int(load_library().hs_verify_workspace_size(B, M, V, dtype, int(drafter)))
+
+
+def _logits(t: torch.Tensor, B: int, M: int, V: int, dtype: int, what: str) -> hs_view:
+    _need(t.dim() == 3 and t.shape[0] == B and t.shape[1] == M and t.shape[2] >= V and _dtype_code(t) == dtype,
+          "%s must be [%d][%d][>= %d] of the target's type" % (what, B, M, V))
+    _need(t.stride(2) == 1, "%s rows must be contiguous" % what)
+    return hs_view(t.data_ptr(), t.stride(0) if B > 1 else 0, t.stride(1) if M > 1 else 0)
+
+
+class Verify:
+    """Pre-marshalled hs_verify call for fixed buffers: the nodes of a drafted chain or tree that the target
+    accepts, and the token that it draws behind them.
+
+    target [B][M][>= V] (V contiguous, rows 16-byte aligned), node 0 the root; token [B][M] i32 and u [B][M] f64
+    (uniform in [0, 1); not used, and may be None, with mode=GREEDY). parent [B][M] i32 (DraftTree's) or None: a
+    chain. drafter [B][M - 1][>= V]: the rows that a chain's tokens were drawn from; None: the children are fixed.
+    count [B] i32: nodes of each query. depth: the draft's longest path, M - 1 if None. run() fills and returns `out`:
+    path [B][M] i32 (the root and the accepted nodes, then -1), token [B][M] i32 (what comes out, then -1) and length
+    [B] i32 of both. What the dict `out` lacks is made and added to it, and belongs to the stream that is current then
+    (see BeamStep); `workspace` may be shared by calls that do not overlap."""
+
+    def __init__(self, target: torch.Tensor, token: torch.Tensor, u: Optional[torch.Tensor] = None,
+                 parent: Optional[torch.Tensor] = None, drafter: Optional[torch.Tensor] = None,
+                 count: Optional[torch.Tensor] = None, V: Optional[int] = None, temperature: float = 1.0,
+                 mode: int = SAMPLE, depth: Optional[int] = None, out: Optional[dict] = None,
+                 workspace: Optional[torch.Tensor] = None):
+        _need(target.dim() == 3, "target must be [B][M][V]")
+        B, M, ld = target.shape
+        V = ld if V is None else V
+        self.B, self.M, self.V, self.dtype = B, M, V, _dtype_code(target)
+        if M == 1:
+            drafter = None  # no token was drafted
+        _full(token, (B, M), torch.int32, "token")
+        _need(mode == GREEDY or u is not None, "sampling needs u")
+        if u is not None:
+            _full(u, (B, M), torch.float64, "u")
+        if parent is not None:
+            _full(parent, (B, M), torch.int32, "parent")
+        if count is not None:
+            _full(count, (B,), torch.int32, "count")
+        o = {} if out is None else out
+        dev = target.device
+        for name, shape in (("path", (B, M)), ("token", (B, M)), ("length", (B,))):
+            if name not in o:
+                o[name] = torch.empty(shape, dtype=torch.int32, device=dev)
+            _full(o[name], shape, torch.int32, "out[%r]" % name)
+        if workspace is None:
+            n = verify_workspace_size(B, M, V, self.dtype, drafter is not None)
+            workspace = torch.empty(max(n, 1), dtype=torch.uint8, device=dev)
+        _need(workspace.is_contiguous(), "workspace must be contiguous")
+        a = hs_verify_args()
+        a.B, a.M, a.V, a.dtype, a.mode = B, M, V, self.dtype, mode
+        a.depth, a.temperature = M - 1 if depth is None else depth, temperature
+        a.token, a.u = token.data_ptr(), None if u is None else u.data_ptr()
+        a.parent = None if parent is None else parent.data_ptr()
+        a.count = None if count is None else count.data_ptr()
+        a.out_path, a.out_token, a.out_length = (o[n].data_ptr() for n in ("path", "token", "length"))
+        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        self.token, self.u, self.parent, self.count = token, u, parent, count
+        self.out, self.workspace = o, workspace
+        self.args, self._ref, self.drafter = a, ctypes.byref(a), drafter
+        self.set_logits(target, drafter)
+        self.device = _one_device(target, token, u, parent, drafter, count, workspace, *o.values())
+        self._fn = load_library().hs_verify
+
+    def set_logits(self, target: torch.Tensor, drafter: Optional[torch.Tensor] = None) -> None:
+        """Other logits tensors of the same shapes and type."""
+        _need((drafter is None) == (self.drafter is None), "with a drafter or without one, as before")
+        view = _logits(target, self.B, self.M, self.V, self.dtype, "target")
+        other = hs_view() if drafter is None else \
+            _logits(drafter, self.B, self.M - 1, self.V, self.dtype, "drafter")
+        if hasattr(self, "device"):
+            _need(_one_device(target, drafter) == self.device, "logits device changed")
+        self.target, self.drafter = target, drafter
+        self.args.target, self.args.drafter = view, other
+
+    def run(self, stream=None) -> dict:
+        _launch(self._fn, self.device, stream, self._ref)
+        return self.out
+
+
+def verify(target: torch.Tensor, token: torch.Tensor, u: Optional[torch.Tensor] = None,
+           parent: Optional[torch.Tensor] = None, drafter: Optional[torch.Tensor] = None,
+           count: Optional[torch.Tensor] = None, V: Optional[int] = None, temperature: float = 1.0,
+           mode: int = SAMPLE, depth: Optional[int] = None, out: Optional[dict] = None,
+           workspace: Optional[torch.Tensor] = None, stream=None) -> dict:
+    """hs_verify, once (see Verify, which a loop keeps). What it makes belongs to `stream`."""
+    with _on(stream):
+        plan = Verify(target, token, u, parent=parent, drafter=drafter, count=count, V=V, temperature=temperature,
+                      mode=mode, depth=depth, out=out, workspace=workspace)
+    return plan.run(stream)

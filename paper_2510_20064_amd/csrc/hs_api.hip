@@ -9,6 +9,7 @@
 #include <mutex>
 
 #include "hs_beam.h"
+#include "hs_draft.h"
 
 #define HS_API extern "C" __attribute__((visibility("default")))
 
@@ -749,6 +750,81 @@ HS_API int hs_draft_tree(const hs_tree_args* a, void* stream) {
       if (overlap(outs[i], outs[o])) return fail(HS_ERR_ARG, "two outputs overlap");
   }
   const int rc = hs::launch_draft_tree(*a, (hipStream_t)stream);
+  if (rc) return fail(rc, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+  return ok();
+}
+
+HS_API size_t hs_verify_workspace_size(int B, int M, int64_t V, int dtype, int drafter) {
+  hs::VerifyGeom g;
+  if (!hs::verify_geom(B, M, V, dtype, drafter != 0 && M > 1, &g)) return 0;
+  return hs::verify_ws_bytes(g);
+}
+
+namespace {
+
+// The bytes of a logits view, from its pointer.
+uint64_t view_span(const hs_view& v, int B, int K, int64_t V, int dtype) {
+  const __int128 n = elem_bytes(dtype) * ((__int128)(B - 1) * v.stride_b + (__int128)(K - 1) * v.stride_k + V);
+  return (uint64_t)std::min(n, (__int128)1 << 62);
+}
+
+int check_workspace(const void* ws, size_t bytes, size_t need) {
+  if (!ws) return fail(HS_ERR_WORKSPACE, "workspace is NULL (need %zu bytes)", need);
+  if (bytes < need) return fail(HS_ERR_WORKSPACE, "workspace too small: %zu < %zu bytes", bytes, need);
+  if (((uintptr_t)ws & 255) != 0) return fail(HS_ERR_ALIGN, "workspace must be 256-byte aligned");
+  return HS_OK;
+}
+
+// No output may share bytes with an input or another output.
+template <int I, int O>
+int check_apart(const Bytes (&ins)[I], const Bytes (&outs)[O]) {
+  for (int o = 0; o < O; ++o) {
+    for (const Bytes& i : ins)
+      if (overlap(i, outs[o])) return fail(HS_ERR_ARG, "an output or the workspace overlaps an input");
+    for (int i = 0; i < o; ++i)
+      if (overlap(outs[i], outs[o])) return fail(HS_ERR_ARG, "two outputs, or one and the workspace, overlap");
+  }
+  return HS_OK;
+}
+
+}  // namespace
+
+HS_API int hs_verify(const hs_verify_args* a, void* stream) {
+  if (!a) return fail(HS_ERR_NULL, "args is NULL");
+  if (a->B < 1 || a->M < 1 || a->V < 1)
+    return fail(HS_ERR_SHAPE, "B, M and V must be >= 1 (got B=%d M=%d V=%lld)", a->B, a->M, (long long)a->V);
+  if (a->B > HS_MAX_QUERIES || a->M > HS_MAX_POSITIONS)
+    return fail(HS_ERR_LIMIT, "limits: B <= %d, M <= %d (got B=%d M=%d)", HS_MAX_QUERIES, HS_MAX_POSITIONS, a->B, a->M);
+  if (a->dtype != HS_F32 && a->dtype != HS_BF16 && a->dtype != HS_F16)
+    return fail(HS_ERR_DTYPE, "unknown dtype %d", a->dtype);
+  if (a->mode != HS_SAMPLE && a->mode != HS_GREEDY) return fail(HS_ERR_ARG, "unknown mode %d", a->mode);
+  int rc = check_view(&a->target, a->dtype, "target");
+  if (rc) return rc;
+  const bool sample = a->mode == HS_SAMPLE, drafter = sample && a->drafter.ptr && a->M > 1;
+  if (drafter && (rc = check_view(&a->drafter, a->dtype, "drafter"))) return rc;
+  if (!a->token || !a->out_path || !a->out_token || !a->out_length)
+    return fail(HS_ERR_NULL, "token, out_path, out_token and out_length are required");
+  if (sample && !a->u) return fail(HS_ERR_NULL, "sample mode needs u");
+  if (sample && !(a->temperature >= 1e-30 && a->temperature <= 1e30))
+    return fail(HS_ERR_TEMPERATURE, "temperature must be in [1e-30, 1e30] (got %g)", a->temperature);
+  if (sample && a->drafter.ptr && a->parent) return fail(HS_ERR_TREE, "a drafter's draft is a chain: parent must be NULL");
+  if (a->depth < 0 || a->depth >= a->M)
+    return fail(HS_ERR_SHAPE, "depth must be in [0, M - 1] (got %d, M=%d)", a->depth, a->M);
+  hs::VerifyGeom g;
+  if (!hs::verify_geom(a->B, a->M, a->V, a->dtype, drafter, &g))
+    return fail(HS_ERR_LIMIT, "V = %lld is beyond the limit of %lld logits per row", (long long)a->V,
+                (long long)hs::kMaxTeamSlices * hs::kVerifySlice * (16 / elem_bytes(a->dtype)));
+  const size_t need = hs::verify_ws_bytes(g);
+  if ((rc = check_workspace(a->workspace, a->workspace_bytes, need))) return rc;
+  const uint64_t nodes = (uint64_t)a->B * a->M;
+  const Bytes ins[] = {{a->target.ptr, view_span(a->target, a->B, a->M, a->V, a->dtype)},
+                       {drafter ? a->drafter.ptr : nullptr, view_span(a->drafter, a->B, a->M - 1, a->V, a->dtype)},
+                       {a->token, 4 * nodes}, {a->parent, 4 * nodes}, {a->count, 4ull * a->B},
+                       {sample ? a->u : nullptr, 8 * nodes}};
+  const Bytes outs[] = {{a->out_path, 4 * nodes}, {a->out_token, 4 * nodes}, {a->out_length, 4ull * a->B},
+                        {a->workspace, need}};
+  if ((rc = check_apart(ins, outs))) return rc;
+  rc = hs::launch_verify(g, *a, (hipStream_t)stream);
   if (rc) return fail(rc, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
   return ok();
 }

@@ -1,0 +1,21 @@
+// Declarations shared by the kernels that verify a draft (hs_verify.hip, hs_attend.hip, hs_append.hip) and
+// their host entries.
+#pragma once
+
+#include "hs_beam.h"
+
+namespace hs {
+
+// How a verification's rows are cut: S slices of kVerifySlice 16-byte vectors, one wave each.
+constexpr int kVerifySlice = 256;
+struct VerifyGeom {
+  int B, M, S;
+  int64_t V, nvec;
+  int dtype;
+  bool drafter;
+};
+bool verify_geom(int B, int M, int64_t V, int dtype, bool drafter, VerifyGeom* g);
+size_t verify_ws_bytes(const VerifyGeom& g);
+int launch_verify(const VerifyGeom& g, const hs_verify_args& a, hipStream_t stream);
+
+}  // namespace hs
