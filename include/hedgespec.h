@@ -58,6 +58,9 @@ extern "C" {
 #define HS_MAX_BEAMS 64     /* W, K: beams of a query in hs_beam_step and hs_draft_tree  */
 #define HS_MAX_DEPTH 32     /* D: grown steps of a draft tree in hs_draft_tree           */
 #define HS_MAX_STATES 1024  /* n: tensors of one hs_beam_reorder call                    */
+#define HS_MAX_HEADS 256    /* heads of hs_tree_attention and hs_cache_append            */
+#define HS_MAX_HEAD_DIM 256 /* their dimensions (multiples of 32)                        */
+#define HS_MAX_PAGE 256     /* tokens of a cache's page (32, 64, 128 or 256)             */
 /* V: at most 512 * 256 16-byte vectors per row (1048576 bf16 or fp16, or 524288 fp32
    logits), and for alpha the device must hold ceil(V / 2048) (bf16, fp16) or ceil(V / 1024)
    (fp32) evaluation workgroups at once: hs_eval_alpha returns HS_ERR_LIMIT otherwise. Agreement
@@ -593,6 +596,115 @@ typedef struct hs_verify_args {
 /* Bytes of device workspace hs_verify needs for this shape (0 on invalid shapes); drafter: nonzero with one. */
 size_t hs_verify_workspace_size(int B, int M, int64_t V, int dtype, int drafter);
 int hs_verify(const hs_verify_args* args, void* stream);
+
+/*
+ * A pool of pages that hold keys and values in 8 bits (OCP e4m3: values up to 448, NaN 0x7F and 0xFF), with a
+ * scale for every page and head: a value is its code times its scale.
+ *   k       : [pages][heads][page][dim], v: [pages][heads][dim][page] bytes, contiguous, 16-byte aligned: a page
+ *             holds the values of one dimension side by side.
+ *   k_scale, v_scale : [pages][heads] fp32. Those of hs_cache_append are powers of two from 2^-40 to 2^40; other ones
+ *             may be any finite number (keys), or 0 or from 2^-40 to 2^40 (values: what lies outside, negative or NaN
+ *             counts as the nearest of these two bounds, NaN as the lower).
+ *   A query's tokens are those of the pages of its row of a table: token t is in page table[b][t / page], at
+ *   t % page. Several queries, and one, may have a page more than once, to read.
+ *   1 <= heads <= HS_MAX_HEADS, dim a multiple of 32 up to HS_MAX_HEAD_DIM, page 32, 64, 128 or 256.
+ */
+typedef struct hs_cache {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  int64_t pages;
+  int heads, page, dim;
+} hs_cache;
+
+/*
+ * A [B][n][heads][dim] tensor of bf16 or fp16: element (b, n, h, d) is at
+ * ptr + (b * stride_b + n * stride_n + h * stride_h + d) * 2. Strides are in elements and, like ptr, multiples of 16
+ * bytes, and not negative.
+ */
+typedef struct hs_heads {
+  void* ptr;
+  int64_t stride_b, stride_n, stride_h;
+} hs_heads;
+
+/*
+ * hs_tree_attention - the target's (or a drafter's) attention over a draft: the queries of the M nodes of each
+ * query's chain or tree over the tokens in its cache and over the nodes on their own paths, whose keys and values
+ * are not in the cache yet. M = 1 is a single token's step.
+ *   out[b][n][i] = sum_t softmax_t(scale q[b][n][i] . k_t) v_t over the cached tokens t < length[b] and the
+ *   nodes j with bit j of mask[b][n], j < count[b]; cached head i / (heads / cache.heads) belongs to head i.
+ *   A query that sees nothing gives 0. Of nodes that a query does not see nothing matters, NaN included.
+ *   q, out      : [B][M][heads][dim]; k, v: [B][M][cache.heads][dim], of `dtype` (HS_BF16 or HS_F16).
+ *   heads       : a multiple of cache.heads, up to HS_MAX_HEADS.
+ *   cache       : see hs_cache; read only.
+ *   table       : [B] rows of `slots` int32, table_stride elements apart (>= slots). Tokens of an entry outside
+ *                 [0, pages) are not there.
+ *   length      : [B] int32: tokens in the cache (clamped to [0, slots * page]). What the pages hold behind them
+ *                 is not read into any result.
+ *   mask        : [B][M] uint64: hs_draft_tree's node_mask (ancestors and the node itself), or NULL: a chain, node n
+ *                 sees nodes 0 .. n.
+ *   count       : NULL: M nodes. Otherwise [B] int32 (clamped to [0, M]): the nodes behind are no part of the draft,
+ *                 and their rows of out stay as they were.
+ *   scale       : finite.
+ *   No output may overlap an input or the workspace, nor may two rows of out share bytes.
+ * Products are exact in fp32 sums; weights are rounded once to fp16 (16 bits of bf16 pairs for bf16 nodes), out once.
+ * workspace     : at least hs_tree_attention_workspace_size() bytes (which may be 0), 256-byte aligned; scratch only.
+ * 1 <= M <= HS_MAX_POSITIONS. Deterministic.
+ */
+typedef struct hs_tree_attention_args {
+  hs_heads q, k, v, out;
+  int B, M, heads, dtype;
+  hs_cache cache;
+  const int32_t* table;
+  int64_t table_stride;
+  int slots;
+  const int32_t* length;
+  const uint64_t* mask;
+  const int32_t* count;
+  double scale;
+  void* workspace;
+  size_t workspace_bytes;
+} hs_tree_attention_args;
+
+/* Bytes of device workspace hs_tree_attention needs for this shape (0: none, or an invalid shape). */
+size_t hs_tree_attention_workspace_size(int B, int M, int heads, int kv_heads, int dim, int page, int slots);
+int hs_tree_attention(const hs_tree_attention_args* args, void* stream);
+
+/*
+ * hs_cache_append - keys and values of new tokens to the cache: the accepted nodes of a verified draft, or a
+ * prompt's tokens. Query b's row path[b][i] (NULL: row i) of k and v becomes token length[b] + i, for i < count[b].
+ * For each page that gets tokens, each head, keys and values by themselves:
+ *   need  = the least power of two with |x| <= 448 need for the page's new finite x, from 2^-40 to 2^40;
+ *   scale = need, or where the page holds tokens before length[b] the larger of need and the scale it has;
+ *   new codes are x / scale, rounded to the nearest (ties to even; beyond 448 it is +-448; NaN and
+ *   infinities are NaN); codes that are there become code * old / scale, rounded so. With scales of powers of
+ *   two that changes a value only where it falls below 2^-6 of the new scale.
+ *   k, v        : [B][rows][cache.heads][dim] of `dtype` (HS_BF16 or HS_F16).
+ *   path        : NULL, or [B] rows of `taken` int32, path_stride elements apart (>= taken), hs_verify's out_path; an
+ *                 entry outside [0, rows) gives a token of zeros.
+ *   taken       : tokens of a query at most (with path NULL: <= rows).
+ *   count       : NULL: all `taken`; otherwise [B] int32 (clamped to [0, taken]), hs_verify's out_length.
+ *   table, slots, length : as in hs_tree_attention; tokens whose page is behind the table's slots or outside
+ *                 [0, pages) are dropped. length itself is left as it is: a negative one, or one beyond the slots,
+ *                 appends nothing.
+ *   A page that gets tokens must be in one query's table alone, and once; cached codes behind the new tokens stay.
+ * Each page is written by one workgroup a head. rows, taken <= 2^24. Deterministic.
+ */
+typedef struct hs_cache_append_args {
+  hs_heads k, v;
+  int B, rows, taken, dtype;
+  hs_cache cache;
+  const int32_t* table;
+  int64_t table_stride;
+  int slots;
+  const int32_t* length;
+  const int32_t* path;
+  int64_t path_stride;
+  const int32_t* count;
+} hs_cache_append_args;
+
+int hs_cache_append(const hs_cache_append_args* args, void* stream);
 
 /* Name of a status code; the thread's last error message; library version (major*10000+minor*100+patch). */
 const char* hs_status_string(int status);

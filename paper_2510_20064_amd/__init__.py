@@ -4,7 +4,8 @@ Argument marshalling only: every step runs in the library's HIP kernels. PyTorch
 device memory and the current HIP stream. The function names match the C ABI declared in
 include/hedgespec.h (hs_softmax_stats, hs_eval_alpha, hs_eval_topl, hs_accept_len,
 hs_hedge_update, hs_normalhedge_update, hs_delayed_update, hs_play, hs_regret_update,
-hs_round, hs_beam_step, hs_beam_reorder, hs_draft_tree, hs_verify). There is no CPU fallback: if the library is not built,
+hs_round, hs_beam_step, hs_beam_reorder, hs_draft_tree, hs_verify,
+hs_tree_attention, hs_cache_append). There is no CPU fallback: if the library is not built,
 loading raises.
 """
 from __future__ import annotations
@@ -30,6 +31,9 @@ MAX_TOPL = 32  # HS_MAX_TOPL
 MAX_BEAMS = 64
 MAX_DEPTH = 32
 MAX_STATES = 1024
+MAX_HEADS = 256
+MAX_HEAD_DIM = 256
+MAX_PAGE = 256
 
 
 class HsError(RuntimeError):
@@ -95,6 +99,31 @@ class hs_verify_args(ctypes.Structure):
     ]
 
 
+class hs_cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")] + [
+        ("pages", ctypes.c_int64), ("heads", ctypes.c_int), ("page", ctypes.c_int), ("dim", ctypes.c_int)]
+
+
+class hs_heads(ctypes.Structure):
+    _fields_ = [("ptr", ctypes.c_void_p)] + [(n, ctypes.c_int64) for n in ("stride_b", "stride_n", "stride_h")]
+
+
+class hs_tree_attention_args(ctypes.Structure):
+    _fields_ = [(n, hs_heads) for n in ("q", "k", "v", "out")] + [
+        (n, ctypes.c_int) for n in ("B", "M", "heads", "dtype")] + [
+        ("cache", hs_cache), ("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("slots", ctypes.c_int),
+        ("length", ctypes.c_void_p), ("mask", ctypes.c_void_p), ("count", ctypes.c_void_p),
+        ("scale", ctypes.c_double), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class hs_cache_append_args(ctypes.Structure):
+    _fields_ = [(n, hs_heads) for n in ("k", "v")] + [
+        (n, ctypes.c_int) for n in ("B", "rows", "taken", "dtype")] + [
+        ("cache", hs_cache), ("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("slots", ctypes.c_int),
+        ("length", ctypes.c_void_p), ("path", ctypes.c_void_p), ("path_stride", ctypes.c_int64),
+        ("count", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -136,6 +165,10 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.hs_verify_workspace_size.argtypes = [I, I, I64, I, I]
     lib.hs_verify_workspace_size.restype = SZ
     lib.hs_verify.argtypes = [ctypes.POINTER(hs_verify_args), P]
+    lib.hs_tree_attention_workspace_size.argtypes = [I, I, I, I, I, I, I]
+    lib.hs_tree_attention_workspace_size.restype = SZ
+    lib.hs_tree_attention.argtypes = [ctypes.POINTER(hs_tree_attention_args), P]
+    lib.hs_cache_append.argtypes = [ctypes.POINTER(hs_cache_append_args), P]
     lib.hs_set_wait_limit.argtypes = [I]
     lib.hs_set_wait_limit.restype = None
     lib.hs_stream_read.argtypes = [P, SZ, I, I, I, P, P]
@@ -145,7 +178,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     for name in ["hs_softmax_stats", "hs_eval_alpha", "hs_eval_alpha_noalloc", "hs_eval_topl", "hs_play", "hs_regret_update",
                  "hs_accept_len", "hs_hedge_update",
                  "hs_normalhedge_update", "hs_round", "hs_delayed_update", "hs_beam_step",
-                 "hs_beam_reorder", "hs_draft_tree", "hs_verify", "hs_version"]:
+                 "hs_beam_reorder", "hs_draft_tree", "hs_verify", "hs_tree_attention",
+                 "hs_cache_append", "hs_version"]:
         getattr(lib, name).restype = I
     _lib = lib
     return lib
@@ -1054,3 +1088,154 @@ def verify(target: torch.Tensor, token: torch.Tensor, u: Optional[torch.Tensor] 
         plan = Verify(target, token, u, parent=parent, drafter=drafter, count=count, V=V, temperature=temperature,
                       mode=mode, depth=depth, out=out, workspace=workspace)
     return plan.run(stream)
+
+
+class PagedCache:
+    """Keys and values of one attention layer in pages, in 8 bits (e4m3) with a scale for every page and head, for
+    TreeAttention and CacheAppend: k [pages][heads][page][dim] and v [pages][heads][dim][page], float8_e4m3fn or
+    uint8, contiguous; k_scale and v_scale [pages][heads] f32. A value is its code times its scale."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
+        _need(k.dim() == 4 and v.dim() == 4, "k must be [pages][heads][page][dim], v [pages][heads][dim][page]")
+        self.pages, self.heads, self.page, self.dim = k.shape
+        for t, shape, what in ((k, k.shape, "k"), (v, (*k.shape[:2], k.shape[3], k.shape[2]), "v")):
+            _need(t.dtype in (torch.float8_e4m3fn, torch.uint8), "%s must be float8_e4m3fn or uint8" % what)
+            _full(t, shape, t.dtype, what)
+        for t, what in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            _full(t, k.shape[:2], torch.float32, what)
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.tensors = {"k": k, "v": v, "k_scale": k_scale, "v_scale": v_scale}
+
+    @classmethod
+    def empty(cls, pages: int, heads: int, page: int, dim: int, device="cuda") -> "PagedCache":
+        """A pool of pages that hold nothing yet."""
+        code = dict(dtype=torch.float8_e4m3fn, device=device)
+        return cls(torch.empty((pages, heads, page, dim), **code), torch.empty((pages, heads, dim, page), **code),
+                   torch.empty((pages, heads), dtype=torch.float32, device=device),
+                   torch.empty((pages, heads), dtype=torch.float32, device=device))
+
+    def args(self) -> hs_cache:
+        return hs_cache(*[t.data_ptr() for t in self.tensors.values()], self.pages, self.heads, self.page, self.dim)
+
+
+def _heads(t: torch.Tensor, shape, dtype, what: str) -> hs_heads:
+    _need(tuple(t.shape) == tuple(shape) and t.dtype == dtype and t.stride(3) == 1,
+          "%s must be a %s tensor of shape %s with contiguous heads" % (what, dtype, list(shape)))
+    return hs_heads(t.data_ptr(), *[t.stride(d) if t.shape[d] > 1 else 0 for d in range(3)])
+
+
+def _table(a, table: torch.Tensor, length: torch.Tensor, B: int) -> None:
+    _need(table.dim() == 2 and table.shape[0] == B and table.dtype == torch.int32 and
+          (table.shape[1] == 1 or table.stride(1) == 1), "table must be an int32 [B][slots] tensor")
+    _full(length, (B,), torch.int32, "length")
+    a.table, a.slots, a.length = table.data_ptr(), table.shape[1], length.data_ptr()
+    a.table_stride = table.stride(0) if B > 1 else table.shape[1]
+
+
+def _half(t: torch.Tensor, what: str) -> int:
+    _need(t.dim() == 4 and t.dtype in (torch.bfloat16, torch.float16),
+          "%s must be a bfloat16 or float16 [B][n][heads][dim] tensor" % what)
+    return _dtype_code(t)
+
+
+class TreeAttention:
+    """Pre-marshalled hs_tree_attention call for fixed buffers: the attention of a draft's nodes over a PagedCache and
+    over the nodes on their own paths.
+
+    q [B][M][heads][dim], k and v [B][M][cache.heads][dim] (bf16 or fp16, heads contiguous and 16-byte aligned, as a
+    joint projection leaves them); table [B][slots] i32: the pages of each query; length [B] i32: tokens in the cache.
+    mask [B][M] i64: the nodes that each sees (DraftTree's ancestor bits) or None: a chain; count [B] i32: nodes of
+    each query, whose other rows of `out` stay as they were. scale: 1 / sqrt(dim) if None. run() fills and returns
+    `out` [B][M][heads][dim], made if None (rows behind count are then 0). What the plan makes belongs to the stream
+    that is current then (see BeamStep)."""
+
+    def __init__(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache: PagedCache, table: torch.Tensor,
+                 length: torch.Tensor, mask: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
+                 scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                 workspace: Optional[torch.Tensor] = None):
+        a = hs_tree_attention_args()
+        a.dtype = _half(q, "q")
+        B, M, heads, dim = q.shape
+        _need(dim == cache.dim, "q has %d dimensions, the cache %d" % (dim, cache.dim))
+        if out is None:
+            out = (torch.empty if count is None else torch.zeros)(q.shape, dtype=q.dtype, device=q.device)
+        a.q, a.out = _heads(q, q.shape, q.dtype, "q"), _heads(out, q.shape, q.dtype, "out")
+        a.k = _heads(k, (B, M, cache.heads, dim), q.dtype, "k")
+        a.v = _heads(v, (B, M, cache.heads, dim), q.dtype, "v")
+        a.B, a.M, a.heads, a.cache = B, M, heads, cache.args()
+        _table(a, table, length, B)
+        if mask is not None:
+            _full(mask, (B, M), torch.int64, "mask")
+        if count is not None:
+            _full(count, (B,), torch.int32, "count")
+        a.mask = None if mask is None else mask.data_ptr()
+        a.count = None if count is None else count.data_ptr()
+        a.scale = dim ** -0.5 if scale is None else scale
+        if workspace is None:
+            n = int(load_library().hs_tree_attention_workspace_size(B, M, heads, cache.heads, dim, cache.page, a.slots))
+            workspace = torch.empty(max(n, 1), dtype=torch.uint8, device=q.device)
+        _need(workspace.is_contiguous(), "workspace must be contiguous")
+        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        self.q, self.k, self.v, self.cache, self.table, self.length = q, k, v, cache, table, length
+        self.mask, self.count, self.out, self.workspace = mask, count, out, workspace
+        self.args, self._ref = a, ctypes.byref(a)
+        self.device = _one_device(q, k, v, *cache.tensors.values(), table, length, mask, count, out, workspace)
+        self._fn = load_library().hs_tree_attention
+
+    def run(self, stream=None) -> torch.Tensor:
+        _launch(self._fn, self.device, stream, self._ref)
+        return self.out
+
+
+def tree_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache: PagedCache, table: torch.Tensor,
+                   length: torch.Tensor, mask: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
+                   scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """hs_tree_attention, once (see TreeAttention, which a loop keeps). What it makes belongs to `stream`."""
+    with _on(stream):
+        plan = TreeAttention(q, k, v, cache, table, length, mask=mask, count=count, scale=scale, out=out,
+                             workspace=workspace)
+    return plan.run(stream)
+
+
+class CacheAppend:
+    """Pre-marshalled hs_cache_append call: rows of k and v [B][rows][cache.heads][dim] (bf16 or fp16) to the cache, as
+    the tokens from length [B] i32 on.
+
+    path [B][taken] i32: the rows of each query in their order (Verify's path), or None: all from the first on.
+    count [B] i32: how many of them (Verify's length), or None: all. The pages that get tokens must be in one query's
+    table alone. length stays as it is: add what was taken to it afterwards. run() returns the cache's tensors: k, v,
+    k_scale and v_scale."""
+
+    def __init__(self, cache: PagedCache, table: torch.Tensor, length: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                 path: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None):
+        a = hs_cache_append_args()
+        a.dtype = _half(k, "k")
+        B, rows = k.shape[:2]
+        shape = (B, rows, cache.heads, cache.dim)
+        a.k, a.v = _heads(k, shape, k.dtype, "k"), _heads(v, shape, k.dtype, "v")
+        a.B, a.rows, a.taken, a.cache = B, rows, rows, cache.args()
+        _table(a, table, length, B)
+        if path is not None:
+            _need(path.dim() == 2 and path.shape[0] == B and path.dtype == torch.int32 and
+                  (path.shape[1] == 1 or path.stride(1) == 1), "path must be an int32 [B][taken] tensor")
+            a.path, a.taken = path.data_ptr(), path.shape[1]
+            a.path_stride = path.stride(0) if B > 1 else path.shape[1]
+        if count is not None:
+            _full(count, (B,), torch.int32, "count")
+            a.count = count.data_ptr()
+        self.cache, self.table, self.length, self.k, self.v, self.path, self.count = \
+            cache, table, length, k, v, path, count
+        self.args, self._ref = a, ctypes.byref(a)
+        self.device = _one_device(k, v, *cache.tensors.values(), table, length, path, count)
+        self._fn = load_library().hs_cache_append
+
+    def run(self, stream=None) -> dict:
+        _launch(self._fn, self.device, stream, self._ref)
+        return dict(self.cache.tensors)
+
+
+def cache_append(cache: PagedCache, table: torch.Tensor, length: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                 path: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None, stream=None) -> dict:
+    """hs_cache_append, once (see CacheAppend, which a loop keeps)."""
+    return CacheAppend(cache, table, length, k, v, path=path, count=count).run(stream)

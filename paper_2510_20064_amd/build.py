@@ -13,7 +13,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhedgespec.so")
 SOURCES = ["hs_api.hip", "hs_stats.hip", "hs_team.hip", "hs_argmax.hip", "hs_tail.hip", "hs_delayed.hip",
            "hs_topl.hip", "hs_play.hip", "hs_probe.hip", "hs_cmass.hip",
-           "hs_beam.hip", "hs_reorder.hip", "hs_tree.hip", "hs_verify.hip"]
+           "hs_beam.hip", "hs_reorder.hip", "hs_tree.hip", "hs_verify.hip", "hs_attend.hip",
+           "hs_append.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

@@ -828,3 +828,140 @@ HS_API int hs_verify(const hs_verify_args* a, void* stream) {
   if (rc) return fail(rc, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
   return ok();
 }
+
+namespace {
+
+int check_heads(const hs_heads& x, const char* what) {
+  if (!x.ptr) return fail(HS_ERR_NULL, "%s: NULL pointer", what);
+  if (x.stride_b < 0 || x.stride_n < 0 || x.stride_h < 0) return fail(HS_ERR_SHAPE, "%s: negative stride", what);
+  if ((((uintptr_t)x.ptr | (uint64_t)x.stride_b * 2 | (uint64_t)x.stride_n * 2 | (uint64_t)x.stride_h * 2) & 15) != 0)
+    return fail(HS_ERR_ALIGN, "%s: heads must start on 16-byte boundaries", what);
+  return HS_OK;
+}
+
+// The bytes of a [B][n][heads][dim] tensor from its pointer.
+uint64_t heads_span(const hs_heads& x, int B, int n, int heads, int dim) {
+  const __int128 s = 2 * ((__int128)(B - 1) * x.stride_b + (__int128)(n - 1) * x.stride_n +
+                          (__int128)(heads - 1) * x.stride_h + dim);
+  return (uint64_t)std::min(s, (__int128)1 << 62);
+}
+
+// Whether the rows of a tensor that is written are apart from each other: each dimension steps over all that the
+// ones of smaller strides span.
+bool heads_apart(const hs_heads& x, int B, int n, int heads, int dim) {
+  struct Dim {
+    int64_t size, stride;
+  } d[3] = {{B, x.stride_b}, {n, x.stride_n}, {heads, x.stride_h}};
+  std::sort(d, d + 3, [](const Dim& a, const Dim& b) { return a.stride < b.stride; });
+  __int128 span = dim;
+  for (const Dim& i : d) {
+    if (i.size == 1) continue;
+    if (i.stride < span) return false;
+    span += (__int128)(i.size - 1) * i.stride;
+  }
+  return true;
+}
+
+int check_cache(const hs_cache& c) {
+  if (!c.k || !c.v || !c.k_scale || !c.v_scale) return fail(HS_ERR_NULL, "cache: k, v, k_scale and v_scale are required");
+  if (c.pages < 1 || c.heads < 1) return fail(HS_ERR_SHAPE, "cache: pages and heads must be >= 1");
+  if (c.heads > HS_MAX_HEADS || c.pages > INT32_MAX || c.dim > HS_MAX_HEAD_DIM || c.page > HS_MAX_PAGE)
+    return fail(HS_ERR_LIMIT, "limits: %d heads of %d dimensions, 2^31 - 1 pages of %d tokens", HS_MAX_HEADS,
+                HS_MAX_HEAD_DIM, HS_MAX_PAGE);
+  if (c.dim < 32 || c.dim % 32 != 0) return fail(HS_ERR_SHAPE, "cache: dim must be a multiple of 32 (got %d)", c.dim);
+  if (c.page < 32 || (c.page & (c.page - 1)) != 0)
+    return fail(HS_ERR_SHAPE, "cache: a page holds 32, 64, 128 or 256 tokens (got %d)", c.page);
+  if ((((uintptr_t)c.k | (uintptr_t)c.v) & 15) != 0) return fail(HS_ERR_ALIGN, "cache: k and v must be 16-byte aligned");
+  return HS_OK;
+}
+uint64_t cache_bytes(const hs_cache& c) {
+  return (uint64_t)c.pages * (uint64_t)c.heads * (uint64_t)(c.page * c.dim);
+}
+uint64_t scale_bytes(const hs_cache& c) { return 4 * (uint64_t)c.pages * (uint64_t)c.heads; }
+
+int check_table(const int32_t* table, int64_t stride, int slots, const int32_t* length) {
+  if (!table || !length) return fail(HS_ERR_NULL, "table and length are required");
+  if (slots < 1 || stride < slots) return fail(HS_ERR_SHAPE, "need slots >= 1 and table_stride >= slots");
+  return HS_OK;
+}
+uint64_t table_bytes(int B, int64_t stride, int slots) {
+  return (uint64_t)std::min(4 * ((__int128)(B - 1) * stride + slots), (__int128)1 << 62);
+}
+
+}  // namespace
+
+HS_API size_t hs_tree_attention_workspace_size(int B, int M, int heads, int kv_heads, int dim, int page, int slots) {
+  hs::AttendGeom g;
+  if (!hs::attend_geom(B, M, heads, kv_heads, dim, page, slots, &g)) return 0;
+  return hs::attend_ws_bytes(g);
+}
+
+HS_API int hs_tree_attention(const hs_tree_attention_args* a, void* stream) {
+  if (!a) return fail(HS_ERR_NULL, "args is NULL");
+  if (a->B < 1 || a->M < 1 || a->heads < 1)
+    return fail(HS_ERR_SHAPE, "B, M and heads must be >= 1 (got B=%d M=%d heads=%d)", a->B, a->M, a->heads);
+  if (a->B > HS_MAX_QUERIES || a->M > HS_MAX_POSITIONS || a->heads > HS_MAX_HEADS)
+    return fail(HS_ERR_LIMIT, "limits: B <= %d, M <= %d, heads <= %d (got B=%d M=%d heads=%d)", HS_MAX_QUERIES,
+                HS_MAX_POSITIONS, HS_MAX_HEADS, a->B, a->M, a->heads);
+  if (a->dtype != HS_BF16 && a->dtype != HS_F16) return fail(HS_ERR_DTYPE, "need bf16 or fp16 (got dtype %d)", a->dtype);
+  int rc = check_cache(a->cache);
+  if (rc) return rc;
+  if (a->heads % a->cache.heads != 0)
+    return fail(HS_ERR_SHAPE, "%d heads do not divide among %d cached ones", a->heads, a->cache.heads);
+  if ((rc = check_heads(a->q, "q")) || (rc = check_heads(a->k, "k")) || (rc = check_heads(a->v, "v")) ||
+      (rc = check_heads(a->out, "out")) || (rc = check_table(a->table, a->table_stride, a->slots, a->length)))
+    return rc;
+  if (!isfinite(a->scale) || !isfinite((float)(a->scale * 1.4426950408889634074)))
+    return fail(HS_ERR_ARG, "scale must be finite");
+  const int dim = a->cache.dim, kv = a->cache.heads;
+  if (!heads_apart(a->out, a->B, a->M, a->heads, dim)) return fail(HS_ERR_SHAPE, "rows of out share bytes");
+  hs::AttendGeom g;
+  if (!hs::attend_geom(a->B, a->M, a->heads, kv, dim, a->cache.page, a->slots, &g))
+    return fail(HS_ERR_LIMIT, "too many rows");
+  const size_t need = hs::attend_ws_bytes(g);
+  if (need && (rc = check_workspace(a->workspace, a->workspace_bytes, need))) return rc;
+  const uint64_t nodes = (uint64_t)a->B * a->M;
+  const Bytes ins[] = {{a->q.ptr, heads_span(a->q, a->B, a->M, a->heads, dim)},
+                       {a->k.ptr, heads_span(a->k, a->B, a->M, kv, dim)},
+                       {a->v.ptr, heads_span(a->v, a->B, a->M, kv, dim)},
+                       {a->cache.k, cache_bytes(a->cache)}, {a->cache.v, cache_bytes(a->cache)},
+                       {a->cache.k_scale, scale_bytes(a->cache)}, {a->cache.v_scale, scale_bytes(a->cache)},
+                       {a->table, table_bytes(a->B, a->table_stride, a->slots)}, {a->length, 4ull * a->B},
+                       {a->mask, 8 * nodes}, {a->count, 4ull * a->B}};
+  const Bytes outs[] = {{a->out.ptr, heads_span(a->out, a->B, a->M, a->heads, dim)},
+                        {need ? a->workspace : nullptr, need}};
+  if ((rc = check_apart(ins, outs))) return rc;
+  rc = hs::launch_attend(g, *a, (hipStream_t)stream);
+  if (rc) return fail(rc, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+  return ok();
+}
+
+HS_API int hs_cache_append(const hs_cache_append_args* a, void* stream) {
+  if (!a) return fail(HS_ERR_NULL, "args is NULL");
+  if (a->B < 1 || a->rows < 1 || a->taken < 1)
+    return fail(HS_ERR_SHAPE, "B, rows and taken must be >= 1 (got B=%d rows=%d taken=%d)", a->B, a->rows, a->taken);
+  if (a->B > HS_MAX_QUERIES || a->rows > (1 << 24) || a->taken > (1 << 24))
+    return fail(HS_ERR_LIMIT, "limits: B <= %d, rows and taken <= 2^24 (got B=%d rows=%d taken=%d)", HS_MAX_QUERIES,
+                a->B, a->rows, a->taken);
+  if (a->dtype != HS_BF16 && a->dtype != HS_F16) return fail(HS_ERR_DTYPE, "need bf16 or fp16 (got dtype %d)", a->dtype);
+  int rc = check_cache(a->cache);
+  if (rc) return rc;
+  if ((rc = check_heads(a->k, "k")) || (rc = check_heads(a->v, "v")) ||
+      (rc = check_table(a->table, a->table_stride, a->slots, a->length)))
+    return rc;
+  if (!a->path && a->taken > a->rows) return fail(HS_ERR_SHAPE, "without a path taken must be <= rows");
+  if (a->path && a->path_stride < a->taken) return fail(HS_ERR_SHAPE, "path_stride must be >= taken");
+  const int64_t span = std::min<int64_t>(((int64_t)a->taken + a->cache.page - 2) / a->cache.page + 1, a->slots);
+  if ((int64_t)a->B * a->cache.heads * span >= (int64_t)1 << 31) return fail(HS_ERR_LIMIT, "too many pages in one call");
+  const int dim = a->cache.dim, kv = a->cache.heads;
+  const Bytes ins[] = {{a->k.ptr, heads_span(a->k, a->B, a->rows, kv, dim)},
+                       {a->v.ptr, heads_span(a->v, a->B, a->rows, kv, dim)},
+                       {a->table, table_bytes(a->B, a->table_stride, a->slots)}, {a->length, 4ull * a->B},
+                       {a->path, table_bytes(a->B, a->path_stride, a->taken)}, {a->count, 4ull * a->B}};
+  const Bytes outs[] = {{a->cache.k, cache_bytes(a->cache)}, {a->cache.v, cache_bytes(a->cache)},
+                        {a->cache.k_scale, scale_bytes(a->cache)}, {a->cache.v_scale, scale_bytes(a->cache)}};
+  if ((rc = check_apart(ins, outs))) return rc;
+  rc = hs::launch_append(*a, (hipStream_t)stream);
+  if (rc) return fail(rc, "kernel launch failed: %s", hipGetErrorString(hipGetLastError()));
+  return ok();
+}

@@ -1,7 +1,13 @@
 """GPU parity of the calls that verify a draft, against oracle/draft.py in fp64.
 
 Tolerances. Paths, tokens and lengths of hs_verify are exact: its weights are fp64 and good to 1.1e-12, so that of
-a number's 2^53 values fewer than V 1.1e-12 lie where the two could differ."""
+a number's 2^53 values fewer than V 1.1e-12 lie where the two could differ. Codes and scales of hs_cache_append are
+exact. An output of hs_tree_attention over n tokens, o = sum p v, may be off by
+  eps / 2 |o|, its rounding (bf16 2^-8, fp16 2^-11), and of sum p |v|
+    2^-11, a weight's rounding to fp16 (what is below 2^-36 of the largest, n 2^-37 at most, is in the sums' share),
+    2 (dim + 8) 2^-24 a, the scores' fp32 sums of products, a = the largest scale * sum |q| |k|, in weight and sum,
+    2 (2^-22 + 2^-23 + 4 * 2^-24 a), exponential, scale and the three roundings on the way to it, and
+    2 (n + 300) 2^-24, the fp32 sums over n tokens and 128 splits of a row."""
 import numpy as np
 import pytest
 import torch
@@ -288,3 +294,475 @@ def test_verify_most_queries():
     want = draft.verify(z[some, :, :V].double().numpy(), token[some].numpy(), u[some].numpy())
     for k in want:
         assert np.array_equal(got[k][some.numpy()], want[k]), k
+
+
+# ---- hs_tree_attention -----------------------------------------------------------------------------------
+
+HALF = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+
+
+class Draft:
+    """Inputs of an attention: a pool whose unused codes are NaN, and drafts over it."""
+
+    def __init__(self, seed, B, M, heads, kv, dim, page, lengths, dtype, tree_=True, counts=None, spare=2):
+        g = torch.Generator().manual_seed(seed)
+        self.B, self.M, self.kv, self.dim, self.page = B, M, kv, dim, page
+        slots = max(1, -(-max(lengths) // page))
+        pages = B * slots + spare
+        x = (torch.randn((pages, kv, page, dim), generator=g) * 80).clamp(-448, 448).to(torch.float8_e4m3fn)
+        y = (torch.randn((pages, kv, dim, page), generator=g) * 80).clamp(-448, 448).to(torch.float8_e4m3fn)
+        self.ck, self.cv = x.view(torch.uint8), y.view(torch.uint8)
+        self.sk = torch.exp2(torch.randint(-8, -4, (pages, kv), generator=g).float())
+        self.sv = torch.exp2(torch.randint(-9, -4, (pages, kv), generator=g).float())
+        self.table = torch.randperm(pages, generator=g)[:B * slots].reshape(B, slots).int()
+        self.length = torch.tensor(lengths, dtype=torch.int32)
+        used = torch.zeros((pages, page), dtype=torch.bool)
+        for b, n in enumerate(lengths):
+            for j in range(slots):
+                used[self.table[b, j].long(), :max(0, min(page, n - j * page))] = True
+        self.ck[~used[:, None].expand(pages, kv, page)] = 0x7F
+        self.cv.copy_(torch.where(used[:, None, None], self.cv, torch.tensor(0xFF, dtype=torch.uint8)))
+        qkv = torch.randn((B, M, heads + 2 * kv, dim), generator=g).to(dtype)
+        self.q, self.k, self.v = qkv[:, :, :heads], qkv[:, :, heads:heads + kv], qkv[:, :, heads + kv:]
+        self.mask = None
+        if tree_:
+            self.mask = torch.zeros((B, M), dtype=torch.int64)
+            for n in range(M):
+                up = (torch.rand(B, generator=g) * n).long()
+                bits = self.mask[torch.arange(B), up] if n else torch.zeros(B, dtype=torch.int64)
+                self.mask[:, n] = bits | (1 << n if n < 63 else -(1 << 63))
+        self.count = None if counts is None else torch.tensor(counts, dtype=torch.int32)
+        self.scale = 1.5 * dim ** -0.5
+
+    def gpu(self):
+        up = lambda t: None if t is None else t if t.is_cuda else t.cuda()  # noqa: E731
+        cache = hs.PagedCache(*[up(t) for t in (self.ck, self.cv, self.sk, self.sv)])
+        out = torch.full(self.q.shape, -77.0, dtype=self.q.dtype, device="cuda")
+        return dict(q=up(self.q), k=up(self.k), v=up(self.v), cache=cache, table=up(self.table), length=up(self.length),
+                    mask=up(self.mask), count=up(self.count), scale=self.scale, out=out)
+
+    def check(self, got=None, **kw):
+        if got is None:
+            got = hs.tree_attention(**dict(self.gpu(), **kw))
+            torch.cuda.synchronize()
+        num = lambda t: None if t is None else t.cpu().numpy()  # noqa: E731
+        f64 = lambda t: t.cpu().double().numpy()  # noqa: E731
+        ref, mean, most = draft.attention(f64(self.q), f64(self.k), f64(self.v), num(self.ck), num(self.cv),
+                                          num(self.sk), num(self.sv), num(self.table), num(self.length),
+                                          mask=num(self.mask), count=num(self.count), scale=self.scale)
+        y = got.cpu().double().numpy()
+        for b in range(self.B):
+            n = self.M if self.count is None else min(max(int(self.count[b]), 0), self.M)
+            assert np.all(y[b, n:] == -77.0), b  # left as they were
+            o, r = y[b, :n], ref[b, :n]
+            bad = ~np.isfinite(r)
+            assert np.array_equal(np.isnan(o), np.isnan(r)) and np.array_equal(o[bad & ~np.isnan(r)], r[bad & ~np.isnan(r)])
+            a, tokens = most[b, :n][..., None], int(self.length[b]) + self.M
+            rel = 2.0 ** -11 + 2 * (self.dim + 8) * 2.0 ** -24 * a + 2 * (2.0 ** -22 + 2.0 ** -23 + 2.0 ** -22 * a) + \
+                2 * (tokens + 300) * 2.0 ** -24
+            tol = HALF[self.q.dtype] * np.abs(r) + rel * mean[b, :n]
+            with np.errstate(invalid="ignore"):
+                over = np.where(bad, 0.0, np.abs(o - r) - tol)
+            assert n == 0 or over.max() <= 0, (b, over.max(), np.unravel_index(over.argmax(), over.shape))
+        return got
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("M,heads,kv,dim,page,lengths", [
+    (1, 1, 1, 32, 32, [0]), (1, 1, 1, 32, 32, [1]), (1, 4, 4, 64, 32, [31, 32, 33]), (1, 8, 2, 128, 64, [63, 64, 65, 0]),
+    (2, 15, 3, 64, 32, [1999, 77, 0, 511]), (3, 5, 1, 96, 128, [127, 128, 129, 300]), (7, 8, 8, 128, 256, [255, 257, 999]),
+    (33, 2, 1, 160, 64, [700, 3]), (61, 4, 1, 128, 64, [1500, 64, 0]), (64, 8, 1, 64, 32, [255, 256, 257, 258]),
+    (16, 3, 3, 192, 64, [513, 40]), (5, 14, 2, 224, 32, [300, 1]), (9, 16, 2, 256, 128, [777, 1000, 4]),
+    (64, 2, 2, 256, 32, [95, 33]), (1, 32, 8, 128, 64, [4097])])
+def test_attention_sizes(dtype, M, heads, kv, dim, page, lengths):
+    note("attention %s M=%d heads=%d/%d dim=%d page=%d %s" % (dtype, M, heads, kv, dim, page, lengths))
+    Draft(M * 100 + heads + dim, len(lengths), M, heads, kv, dim, page, lengths, dtype).check()
+    Draft(M * 100 + heads + dim + 1, len(lengths), M, heads, kv, dim, page, lengths, dtype, tree_=False).check()
+
+
+def test_attention_counts():
+    note("attention counts")
+    for M, counts in ((5, [0, 1, 5, 9, -3, 4]), (40, [40, 33, 32, 31, 1, 0])):
+        d = Draft(M, 6, M, 6, 2, 64, 32, [100, 0, 64, 5, 33, 0], torch.bfloat16, counts=counts)
+        for b, n in enumerate(counts):  # nodes behind the count hold anything
+            d.k[b, max(n, 0):] = float("nan")
+            d.v[b, max(n, 0):] = float("inf")
+            d.mask[b, max(n, 0):] = 0
+        d.check()
+
+
+def test_attention_rows_that_see_nothing():
+    note("attention empty rows")
+    d = Draft(3, 3, 6, 4, 2, 64, 32, [0, 0, 40], torch.float16)
+    d.mask[:, 1:4] = 0
+    got = d.check()
+    assert torch.all(got[:2, 1:4] == 0)
+
+
+def test_attention_masked_nodes_may_hold_anything():
+    note("attention NaN and infinities in masked nodes")
+    for dtype in (torch.bfloat16, torch.float16):
+        for bad in (float("nan"), float("inf"), -float("inf")):
+            d = Draft(5, 2, 40, 4, 2, 64, 32, [50, 0], dtype)
+            d.v[0, 7, 1, 33] = bad   # reaches those that see nodes 7 and 35
+            d.v[1, 35, 0, :] = bad
+            d.check()
+            d = Draft(5, 2, 40, 4, 2, 64, 32, [50, 0], dtype)
+            seen = torch.tensor([[(int(m) >> 9) & 1 for m in d.mask[b]] for b in range(2)]).bool()
+            d.k[:, 9] = bad
+            d.v[:, 9] = bad
+            got = hs.tree_attention(**d.gpu()).cpu()
+            assert torch.isfinite(got[~seen]).all() and not torch.isfinite(got[seen]).any()
+
+
+def test_attention_large_values_of_bf16_nodes():
+    """bf16's range: the nodes' values are not held in fp16."""
+    note("attention large node values")
+    d = Draft(7, 2, 20, 4, 2, 64, 32, [50, 0], torch.bfloat16)
+    d.v *= 1e20
+    d.check()
+    d.v *= 1e-37
+    d.check()
+
+
+def test_attention_scales():
+    """Pages whose scales lie far apart, scales that are no powers of two, zeros, and cached NaN."""
+    note("attention scales")
+    g = torch.Generator().manual_seed(8)
+    d = Draft(9, 2, 3, 4, 2, 128, 32, [320, 200], torch.bfloat16)
+    d.sv.copy_(torch.exp2(torch.randint(-20, 20, d.sv.shape, generator=g).float()))
+    d.check()
+    d.sv.copy_(torch.exp2(torch.randint(-40, 41, d.sv.shape, generator=g).float()))
+    d.check()
+    d.sv.copy_(torch.rand(d.sv.shape, generator=g) + 0.01)
+    d.sk.copy_((torch.rand(d.sk.shape, generator=g) - 0.5) * 0.02)
+    d.check()
+    d.sk[d.table[0, 1].long()] = 0.0
+    d.sv[d.table[0, 2].long()] = 0.0
+    d.check()
+    d.cv[d.table[0, 3].long(), 1, 17, 5] = 0x7F
+    d.check()
+    d.ck[d.table[1, 3].long(), 0, 5, 3] = 0xFF
+    d.check()
+
+
+def test_attention_sharp_and_flat():
+    """Scores from equal to far apart: one token has all the weight, and late maxima."""
+    note("attention sharp and flat")
+    for scale in (0.0, 1e-3, 1.0, 8.0, -2.0):
+        d = Draft(10, 2, 4, 8, 2, 64, 64, [1500, 333], torch.float16)
+        d.scale = scale
+        d.check()
+
+
+def test_attention_tables():
+    """Pages that queries share, pages that are not there, lengths beyond the table and negative ones."""
+    note("attention tables")
+    d = Draft(11, 4, 5, 4, 2, 64, 32, [160, 160, 150, 90], torch.bfloat16)
+    d.table[1, :3] = d.table[0, :3]
+    d.table[1, 3] = d.table[1, 2]
+    d.table[2, 1], d.table[2, 4] = -1, 99999
+    d.table[3] = -7
+    d.check()
+    d.length[0], d.length[1] = 1 << 30, -5
+    d.check()
+    wide = torch.full((4, 9), -1, dtype=torch.int32)
+    wide[:, :5] = d.table
+    d.table = wide[:, :5]
+    full = wide.cuda()
+    d.check(table=full[:, :5])
+
+
+def test_attention_strides_and_streams():
+    note("attention strides and streams")
+    d = Draft(12, 3, 6, 8, 2, 128, 64, [200, 77, 0], torch.bfloat16)
+    args = d.gpu()
+    # heads before nodes, in and out, and the batch broadcast
+    args["q"] = args["q"].transpose(1, 2).contiguous().transpose(1, 2)
+    args["out"] = torch.full((3, 8, 6, 160), -77.0, dtype=torch.bfloat16, device="cuda").transpose(1, 2)[..., :128]
+    d.check(got=hs.tree_attention(**args))
+    d.k, d.v = d.k[:1].expand(d.k.shape), d.v[:1].expand(d.v.shape)
+    d.check(k=d.k[:1].cuda().expand(d.k.shape), v=d.v[:1].cuda().expand(d.v.shape))
+    s = torch.cuda.Stream()
+    args = d.gpu()
+    s.wait_stream(torch.cuda.current_stream())
+    got = hs.tree_attention(stream=s, **args)
+    s.synchronize()
+    d.check(got=got)
+
+
+@pytest.mark.parametrize("M", [1, 21])
+def test_attention_captured(M):
+    """A captured call, replayed as the cache grows, with eager calls between; two plans share a workspace in order."""
+    note("attention captured M=%d" % M)
+    d = Draft(13, 2, M, 8, 2, 128, 64, [4000, 3000], torch.bfloat16)
+    args = d.gpu()
+    plan = hs.TreeAttention(**args)
+    plan.run()
+    other = hs.TreeAttention(**dict(args, out=torch.empty_like(args["out"]), workspace=plan.workspace))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        plan.run()
+        other.run()
+    for n in ((1, 0), (300, 4000), (4000, 2500), (33, 64)):
+        d.length = torch.tensor(n, dtype=torch.int32)
+        args["length"].copy_(d.length)
+        args["q"].copy_(torch.randn(d.q.shape))
+        d.q = args["q"]
+        graph.replay()
+        torch.cuda.synchronize()
+        got = d.check(got=plan.out)
+        # (bits: a length beyond what was filled reads NaN)
+        again = hs.tree_attention(**dict(args, out=torch.empty_like(got)))
+        assert torch.equal(got.view(torch.int16), other.out.view(torch.int16))
+        assert torch.equal(again.view(torch.int16), got.view(torch.int16))
+
+
+def test_attention_is_the_same_wherever_a_query_stands():
+    note("attention positions")
+    d = Draft(14, 4, 9, 8, 2, 64, 32, [900, 900, 900, 900], torch.bfloat16)
+    for t in (d.q, d.k, d.v, d.table, d.mask):
+        t[3] = t[0]
+    got = d.check()
+    assert torch.equal(got[0], got[3])
+
+
+def test_attention_far_pages():
+    """Offsets beyond 32 bits: a pool of 5 GB of keys."""
+    note("attention far pages")
+    d = Draft(15, 2, 3, 4, 2, 256, 256, [700, 256], torch.bfloat16)
+    args = d.gpu()
+    far = 5 * (1 << 30) // (2 * 256 * 256)
+    big = hs.PagedCache.empty(far, 2, 256, 256)
+    ids = torch.arange(args["cache"].pages, device="cuda")
+    to = far - 1 - ids * 5000
+    for n, t in big.tensors.items():
+        t.view(torch.uint8 if t.dtype == torch.float8_e4m3fn else t.dtype)[to] = args["cache"].tensors[n]
+    assert int(to.min()) >= 0 and int(to.max()) * 2 * 65536 > 1 << 32
+    d.check(cache=big, table=to.int()[args["table"].long()])
+
+
+# ---- hs_cache_append ---------------------------------------------------------------------------------------
+
+def pool(g, pages, kv, page, dim):
+    codes = torch.randint(0, 256, (2, pages, kv, page * dim), generator=g).to(torch.uint8)
+    scale = torch.exp2(torch.randint(-9, -5, (2, pages, kv), generator=g).float())
+    return [codes[0].reshape(pages, kv, page, dim), codes[1].reshape(pages, kv, dim, page), scale[0], scale[1]]
+
+
+def check_append(state, table, length, k, v, path=None, count=None, gpu=None, **kw):
+    """One append to the tensors of `state` and, by the oracle, to their copies: every byte the same (any NaN is NaN)."""
+    up = lambda t: None if t is None else t if t.is_cuda else t.cuda()  # noqa: E731
+    dev = [up(t.clone()) for t in state] if gpu is None else gpu
+    hs.cache_append(hs.PagedCache(*dev), up(table), up(length), up(k), up(v), path=up(path), count=up(count), **kw)
+    torch.cuda.synchronize()
+    num = lambda t: None if t is None else t.cpu().numpy()  # noqa: E731
+    ref = [t.numpy().copy() for t in state]
+    draft.append(*ref, num(table), num(length), k.cpu().double().numpy(), v.cpu().double().numpy(), path=num(path),
+                 count=num(count))
+    got = [t.cpu().numpy() for t in dev]
+    for n in (0, 1):
+        same = (got[n] == ref[n]) | (((got[n] & 0x7F) == 0x7F) & ((ref[n] & 0x7F) == 0x7F))
+        assert same.all(), (n, np.argwhere(~same)[:4], got[n][~same][:4], ref[n][~same][:4])
+    for n in (2, 3):
+        assert np.array_equal(got[n], ref[n]), n
+    return [torch.from_numpy(t) for t in got]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("kv,dim,page,taken,lengths", [
+    (1, 32, 32, 1, [0, 1, 31, 32]), (2, 64, 32, 5, [0, 27, 28, 30, 95]), (3, 128, 64, 64, [0, 1, 63, 64, 200]),
+    (2, 96, 128, 300, [0, 5, 127, 128]), (1, 256, 256, 257, [0, 255, 256, 3]), (8, 128, 64, 13, [60, 50, 51, 52])])
+def test_append_sizes(dtype, kv, dim, page, taken, lengths):
+    note("append %s heads=%d dim=%d page=%d taken=%d %s" % (dtype, kv, dim, page, taken, lengths))
+    g = torch.Generator().manual_seed(kv * 100 + dim + taken)
+    B, slots = len(lengths), -(-(max(lengths) + taken) // page)
+    state = pool(g, B * slots + 1, kv, page, dim)
+    table = torch.randperm(B * slots + 1, generator=g)[:B * slots].reshape(B, slots).int()
+    for spread in (0.01, 1.0, 100.0):  # scales that stay, and that grow
+        k = (torch.randn((B, taken, kv, dim), generator=g) * spread).to(dtype)
+        v = (torch.randn((B, taken, kv, dim), generator=g) * spread).to(dtype)
+        check_append(state, table, torch.tensor(lengths, dtype=torch.int32), k, v)
+        count = torch.randint(-1, taken + 2, (B,), generator=g).int()
+        check_append(state, table, torch.tensor(lengths, dtype=torch.int32), k, v, count=count)
+
+
+def test_append_paths():
+    note("append paths")
+    g = torch.Generator().manual_seed(21)
+    B, rows, kv, dim, page = 6, 40, 2, 64, 32
+    state = pool(g, 20, kv, page, dim)
+    table = torch.randperm(20, generator=g)[:18].reshape(6, 3).int()
+    k, v = (torch.randn((B, rows, kv, dim), generator=g).to(torch.bfloat16) for _ in range(2))
+    path = torch.full((B, 9), -1, dtype=torch.int32)
+    path[:, :7] = torch.rand((B, rows), generator=g).argsort(1)[:, :7].sort(1).values.int()
+    path[1, 3] = path[1, 2]  # a row twice
+    count = torch.tensor([7, 5, 0, 1, 9, 100], dtype=torch.int32)  # (the last two take what is not there: zeros)
+    path[5, 0] = 40
+    length = torch.tensor([0, 29, 40, 63, 32, 60], dtype=torch.int32)
+    check_append(state, table, length, k, v, path=path, count=count)
+    wide = torch.full((B, 16), 3, dtype=torch.int32)
+    wide[:, :9] = path
+    check_append(state, table, length, k, v, path=wide.cuda()[:, :9], count=count)
+
+
+def test_append_strange_values_and_tables():
+    note("append strange values and tables")
+    g = torch.Generator().manual_seed(22)
+    B, rows, kv, dim, page = 8, 40, 2, 64, 32
+    for dtype in (torch.bfloat16, torch.float16):
+        state = pool(g, 30, kv, page, dim)
+        table = torch.randperm(30, generator=g)[:24].reshape(8, 3).int()
+        k, v = (torch.randn((B, rows, kv, dim), generator=g).to(dtype) for _ in range(2))
+        k[0], v[0] = 0.0, -0.0
+        k[1, 3, 0, 7], v[1, 30, 1, 9] = float("nan"), float("inf")
+        k[2], v[2] = float("nan"), -float("inf")
+        k[3], v[3] = torch.finfo(dtype).max, torch.finfo(dtype).tiny
+        v[4] = 448.0 * 2.0 ** -6   # at the top of a scale, and just above it
+        k[4] = (448.0 * 2.0 ** -6) * (1 + 2.0 ** -7)
+        table[5, 1], table[6, 0], table[6, 2] = -1, 30, 1 << 30
+        length = torch.tensor([5, 0, 20, 0, 0, 3, 20, 90], dtype=torch.int32)  # (the last leaves the table)
+        check_append(state, table, length, k, v)
+        length = torch.tensor([-1, 96, 1 << 30, -(1 << 31), 64, (1 << 31) - 1, 95, 3], dtype=torch.int32)
+        check_append(state, table, length, k, v)
+
+
+def test_append_scales_that_are_no_powers_of_two():
+    note("append other scales")
+    g = torch.Generator().manual_seed(23)
+    state = pool(g, 9, 2, 32, 64)
+    state[2].copy_(torch.rand((9, 2), generator=g) * 0.05)
+    state[3].copy_(torch.rand((9, 2), generator=g) * 0.005)
+    k, v = (torch.randn((4, 20, 2, 64), generator=g).to(torch.float16) for _ in range(2))
+    check_append(state, torch.arange(8).reshape(4, 2).int(), torch.tensor([3, 30, 31, 12], dtype=torch.int32), k, v)
+
+
+def test_append_step_by_step():
+    """Tokens one by one, with strides and another stream, end where the oracle's do; values stay within half a step
+    of 8 bits (2^-4 of themselves, or 2^-10 of the page's scale below its normal codes, once for every doubling)."""
+    note("append step by step")
+    g = torch.Generator().manual_seed(24)
+    B, kv, dim, page, n = 2, 2, 64, 32, 70
+    qkv = torch.randn((B, n, 8, dim), generator=g) * torch.linspace(0.1, 3.0, n)[None, :, None, None]
+    qkv = qkv.to(torch.bfloat16)
+    k, v = qkv[:, :, 4:6], qkv[:, :, 6:]
+    state = pool(g, 8, kv, page, dim)
+    table = torch.tensor([[6, 1, 3], [0, 7, 2]], dtype=torch.int32)
+    s = torch.cuda.Stream()
+    big = qkv.cuda()
+    for t in range(n):
+        dev = [x.cuda() for x in state]
+        s.wait_stream(torch.cuda.current_stream())
+        state = check_append(state, table, torch.tensor([t, t], dtype=torch.int32), big[:, t:t + 1, 4:6],
+                             big[:, t:t + 1, 6:], gpu=dev, stream=s if t % 2 else None)
+    for b in range(B):
+        for t in range(n):
+            p, o = int(table[b, t // page]), t % page
+            got = draft.VALUES[state[0][p, :, o].numpy()] * state[2][p].numpy()[:, None]
+            x = k[b, t].double().numpy()
+            assert np.all(np.abs(got - x) <= np.abs(x) * 2.0 ** -4 + state[2][p].numpy()[:, None] * 2.0 ** -9)
+
+
+def test_append_captured():
+    note("append captured")
+    g = torch.Generator().manual_seed(25)
+    state = pool(g, 9, 2, 32, 64)
+    dev = [t.cuda() for t in state]
+    k, v = (torch.zeros((2, 6, 2, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    table, length = torch.arange(8).reshape(2, 4).int().cuda(), torch.zeros(2, dtype=torch.int32, device="cuda")
+    count = torch.zeros(2, dtype=torch.int32, device="cuda")
+    plan = hs.CacheAppend(hs.PagedCache(*dev), table, length, k, v, count=count)
+    plan.run()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        plan.run()
+    for i in range(6):
+        k.copy_(torch.randn(k.shape, generator=g) * (i + 1))
+        v.copy_(torch.randn(k.shape, generator=g) * (6 - i))
+        count.copy_(torch.randint(0, 7, (2,), generator=g))
+        before = [t.cpu() for t in dev]
+        graph.replay()
+        torch.cuda.synchronize()
+        after = [t.cpu() for t in dev]
+        want = check_append(before, table, length, k, v, count=count)
+        for a, w in zip(after, want):
+            assert torch.equal(a, w), i
+        length += count
+
+
+def test_append_far_pages():
+    note("append far pages")
+    g = torch.Generator().manual_seed(26)
+    far = 5 * (1 << 30) // (2 * 256 * 256)
+    big = hs.PagedCache.empty(far, 2, 256, 256)
+    to = torch.tensor([far - 1, far - 4000], device="cuda")
+    small = pool(g, 2, 2, 256, 256)
+    for n, t in zip(big.tensors.values(), small):
+        n.view(t.dtype)[to] = t.cuda()
+    k, v = (torch.randn((1, 200, 2, 256), generator=g).to(torch.float16) for _ in range(2))
+    length = torch.tensor([100], dtype=torch.int32)
+    hs.cache_append(big, to.int()[None], length.cuda(), k.cuda(), v.cuda())
+    want = check_append(small, torch.tensor([[0, 1]], dtype=torch.int32), length, k, v)
+    for n, t in zip(big.tensors.values(), want):
+        assert torch.equal(n.view(t.dtype)[to].cpu(), t)
+
+
+# ---- together ----------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("mode", [hs.SAMPLE, hs.GREEDY])
+def test_rounds_of_a_tree_as_a_program_runs_them(mode):
+    """Prompts to the cache; then rounds of growth, the target's attention over the tree, its logits, the verification
+    and the accepted nodes' keys and values to the cache. Cache and attention follow a program that keeps every
+    accepted token's keys and values; paths follow the oracle."""
+    note("rounds mode=%d" % mode)
+    g = torch.Generator().manual_seed(41)
+    B, W, K, M, depth, V, kv, heads, dim, page = 3, 4, 6, 12, 3, 500, 2, 4, 64, 32
+    embed = torch.randn((V, dim), generator=g)
+    wq, wk, wv = (torch.randn((dim, n, dim), generator=g) * dim ** -0.5 for n in (heads, kv, kv))
+    wo = torch.randn((heads * dim, V), generator=g) * 2.0
+    project = lambda t, w: torch.einsum("...d,dhe->...he", embed[t.clamp(min=0).long()], w).to(torch.bfloat16)  # noqa: E731
+    cache = hs.PagedCache.empty(16, kv, page, dim)
+    table = torch.randperm(16, generator=g)[:15].reshape(B, 5).int().cuda()
+    length = torch.zeros(B, dtype=torch.int32, device="cuda")
+    prompt = torch.randint(0, V, (B, 37), generator=g)
+    given = torch.tensor([37, 20, 1], dtype=torch.int32, device="cuda")
+    hs.cache_append(cache, table, length, project(prompt, wk).cuda(), project(prompt, wv).cuda(), count=given)
+    length += given
+    kept = [prompt[b, :int(given[b])].tolist() for b in range(B)]  # tokens in the cache
+    root = torch.randint(0, V, (B,), generator=g)
+    growth = hs.TreeGrowth(B, depth, W, K, M, device="cuda:0")
+    for _ in range(6):
+        growth.level(torch.randn((B, 1, V + 4), generator=g).cuda().to(torch.bfloat16), V=V)
+        for _ in range(depth - 1):
+            growth.level(torch.randn((B, W, V + 4), generator=g).cuda().to(torch.bfloat16), V=V)
+        tree_ = growth.tree()
+        token = tree_["token"].cpu()
+        token[:, 0] = root.int()
+        q, k, v = (project(token, w).cuda() for w in (wq, wk, wv))
+        out = hs.tree_attention(q, k, v, cache, table, length, mask=tree_["mask"], count=tree_["count"])
+        logits = (out.float().reshape(B, M, -1) @ wo.cuda()).to(torch.bfloat16)
+        logits = torch.nn.functional.pad(logits, (0, 4))
+        u = numbers(g, B, M)
+        got = hs.verify(logits, tree_["token"], u.cuda(), parent=tree_["parent"], count=tree_["count"], V=V,
+                        mode=mode, depth=depth)
+        want = draft.verify(logits[:, :, :V].cpu().double().numpy(), token.numpy(), u.numpy(),
+                            parent=tree_["parent"].cpu().numpy(), count=tree_["count"].cpu().numpy(),
+                            greedy=mode == hs.GREEDY, depth=depth)
+        for n in want:
+            assert np.array_equal(got[n].cpu().numpy(), want[n]), n
+        # the root's and the accepted nodes' rows join the cache
+        hs.cache_append(cache, table, length, k, v, path=got["path"], count=got["length"])
+        length += got["length"]
+        for b in range(B):
+            n = int(got["length"][b])
+            kept[b] += token[b, got["path"][b, :n].cpu().long()].tolist()
+            root[b] = int(got["token"][b, n - 1])
+    assert [len(t) for t in kept] == length.tolist()
+    # what the cache holds is what was kept, within the steps of 8 bits (see test_append_step_by_step)
+    for b in range(B):
+        x = project(torch.tensor(kept[b]), wk).double().numpy()
+        for t in range(len(kept[b])):
+            p, o = int(table[b, t // page]), t % page
+            code = cache.k.view(torch.uint8)[p, :, o].cpu().numpy()
+            s = cache.k_scale[p].cpu().numpy()[:, None]
+            assert np.all(np.abs(draft.VALUES[code] * s - x[t]) <= np.abs(x[t]) * 2.0 ** -4 + s * 2.0 ** -9)
