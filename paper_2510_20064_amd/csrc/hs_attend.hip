@@ -28,6 +28,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -35,6 +36,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr float kHeadroom = 12.0f;  // weights are held as 2^12 w
 constexpr float kSlack = 3.0f;      // m follows a maximum more than this above it
 constexpr float kLowest = -1.7e38f; // m before the first token
+constexpr int kStage = 4;           // tiles of 32 tokens that a workgroup brings to LDS at once
 
 struct AttendArgs {
   const char* q;
@@ -56,27 +58,64 @@ struct AttendArgs {
   const uint64_t* mask;
   const int32_t* count;
   float scale2;  // scale log2(e)
-  int tiles, splits;  // of 32 rows, of a cached head; parts of the cached tokens at most
-  uint32_t items, group0;  // B * kv * splits
-  FastDiv div_splits, div_kv, div_tiles, div_group;
-  float* part;     // [B * kv * tiles][splits][32][D]
-  float2* part_ml; // [B * kv * tiles][splits][32]
+  int tiles;   // workgroups that share a cached head's rows
+  int chunks;  // ranges that all queries' cached tokens are cut into; 0: a query is one
+  uint32_t items, group0;  // (ranges, or queries) * kv
+  uint32_t row_groups;     // workgroups of the join for a query's cached head
+  FastDiv div_kv, div_tiles, div_group, div_rows;
+  float* part;      // [kv * tiles][2 * chunks][rows][D]
+  float2* part_ml;  // [kv * tiles][2 * chunks][rows]
 };
 
-// How a query's cached tokens are parted: `used` splits of `per` tiles of 32 tokens.
-struct Parts {
-  int tokens, used, per;
-};
-__device__ inline Parts parts_of(const AttendArgs& A, int b) {
-  Parts p;
-  const int most = (int)min((int64_t)A.slots << A.shift, (int64_t)INT_MAX - 31);
-  p.tokens = min(max(A.length[b], 0), most);
-  const int tiles = (p.tokens + 31) / 32;
-  const int n = min(max((tiles + kAttendLeast - 1) / kAttendLeast, 1), A.splits);
-  p.per = max((tiles + n - 1) / n, 1);
-  p.used = max((tiles + p.per - 1) / p.per, 1);
-  return p;
+__device__ inline int same(int x) { return (int)uniform((uint32_t)x); }  // (what every lane has, in a scalar register)
+__device__ inline int tokens_of(const AttendArgs& A, int b) {
+  const int most = (int)min((int64_t)A.slots << A.shift, (int64_t)INT_MAX - 31 * kStage);
+  return min(max(A.length[b], 0), most);
 }
+// Stages of a query's cached tokens; one without tokens counts for one.
+__device__ inline int stages_of(const AttendArgs& A, int b) {
+  return max((tokens_of(A, b) + 32 * kStage - 1) / (32 * kStage), 1);
+}
+// The stages of all queries, one behind the other, are cut into ranges of `per`: a workgroup does a range, and a query
+// may lie in several, whose parts the join adds. Range i has up to two parts of such queries: place 2 i is that of the
+// query with which the range starts, 2 i + 1 that of one that starts inside it.
+// One wave; a lane has the queries from lane * held on.
+struct Plan {
+  int per, held, upto, mine;  // upto: stages of the lanes up to and with this one, mine: this one's
+  __device__ Plan(const AttendArgs& A, int lane) {
+    held = (A.B + 63) / 64;
+    mine = 0;
+    for (int i = lane * held; i < min((lane + 1) * held, A.B); ++i) mine += stages_of(A, i);
+    upto = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int o = __shfl_up(upto, d, 64);
+      if (lane >= d) upto += o;
+    }
+    const int all = __builtin_amdgcn_readlane(upto, 63);
+    per = same((all + A.chunks - 1) / A.chunks);
+  }
+  // The query that stage `at` of all lies in, and the stages before it; -1: none.
+  __device__ int query(const AttendArgs& A, int at, int* before) const {
+    const uint64_t over = __ballot(upto > at);
+    if (!over) return -1;
+    const int l = __builtin_ctzll(over);
+    int n = __builtin_amdgcn_readlane(upto - mine, l), b = l * held;
+    for (;; ++b) {
+      const int w = same(stages_of(A, b));
+      if (at < n + w) break;
+      n += w;
+    }
+    *before = n;
+    return b;
+  }
+  __device__ int before(const AttendArgs& A, int b) const {
+    const int l = b / held;
+    int n = __builtin_amdgcn_readlane(upto - mine, l);
+    for (int i = l * held; i < b; ++i) n += same(stages_of(A, i));
+    return n;
+  }
+};
 __device__ inline int nodes_of(const AttendArgs& A, int b) {
   return A.count ? min(max(A.count[b], 0), A.M) : A.M;
 }
@@ -131,44 +170,92 @@ __device__ inline f16x8 narrow(const float* w) {
   return r;
 }
 
-// The token of a tile whose key is row rho of the first product: register i of lane half h is then token 16 h + i.
+// The token of a tile whose key is row rho of the first product (register i of lane half h is then token 16 h + i), and
+// the row of a token.
 __device__ inline int pi_of(int rho) {
   return ((rho >> 2) & 1) * 16 + (rho >> 4) * 8 + ((rho >> 3) & 1) * 4 + (rho & 3);
 }
+__device__ inline int rho_of(int token) {
+  return ((token >> 4) & 1) * 4 + ((token >> 3) & 1) * 16 + ((token >> 2) & 1) * 8 + (token & 3);
+}
 
-__device__ inline float other_half(float x) { return __shfl_xor(x, 32, 64); }
-
-// A tile of 32 cached tokens, as one wave holds it: lane (rho, h) dims 32 j + 16 h .. + 15 of the key of token
-// pi(rho), and tokens 16 h .. 16 h + 15 of the dims 32 j + rho of the values.
-template <int DB>
-struct Tile {
-  uint4 k[DB], v[DB];
-  float ks, vs;
-  int valid;
+// The values of lanes l and l + 32, combined in both.
+struct Halves {
+  float lo, hi;
 };
+__device__ inline Halves halves(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return Halves{__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
 
+// The pages of the tiles of stage t, lane i that of tile i, or -1. (By a vector load like the scales below: a scalar
+// one would be in the count that the wait for each read of LDS brings to 0.)
+__device__ inline int pages_of(const AttendArgs& A, int b, int t, int last, int lane) {
+  const int id = lane < kStage && t + lane < last ? A.table[b * A.table_stride + (((t + lane) * 32) >> A.shift)] : -1;
+  return id < A.pages ? id : -1;
+}
+// The scales of the tiles of a stage: lane i the keys' of tile i, lane kStage + i the values'. (What no tile has is read
+// from the first page, here and below, and not used.)
+__device__ inline float scales_of(const AttendArgs& A, int h, int pages, int lane) {
+  const int id = max(__shfl(pages, lane & (kStage - 1), 64), 0);
+  return lane < 2 * kStage ? (lane < kStage ? A.ks : A.vs)[(int64_t)id * A.kv + h] : 0.0f;
+}
+// Tokens of a stage's tile that there are.
+__device__ inline int valid_of(int pages, int t, int sub, int tokens) {
+  return __builtin_amdgcn_readlane(pages, sub) < 0 ? 0 : min(32, max(tokens - (t + sub) * 32, 0));
+}
+
+// A stage on its way to LDS. A tile's keys are 32 * D bytes one behind the other, its values D rows of 32 bytes; a wave
+// brings pieces of 1 KB of both. In LDS a row is 16 bytes longer than what it holds: an odd number of 16 bytes, so that 16
+// lanes that read 16 bytes of consecutive rows each use all banks once.
 template <int DB>
-__device__ inline void load_tile(const AttendArgs& A, int b, int h, int t, int tokens, int lane, Tile<DB>& T) {
+struct Staged {
+  static constexpr int kKeyPitch = 32 * DB + 16, kValuePitch = 32 * kStage + 16;
+  static constexpr int kKeys = 32 * kStage * kKeyPitch, kBytes = kKeys + 32 * DB * kValuePitch;
+};
+template <int DB, int NW>
+struct Loads {
+  static constexpr int kAll = kStage * DB, kN = (kAll + NW - 1) / NW;  // pieces of a stage's keys; of a wave
+  u32x4 k[kN], v[kN];
+};
+template <int DB, int NW>
+__device__ __forceinline__ void load_stage(const AttendArgs& A, int h, int t, int pages, int wv, int lane,
+                                           Loads<DB, NW>& L) {
   constexpr int D = 32 * DB;
-  const int token = t * 32;
-  int id = A.table[b * A.table_stride + (token >> A.shift)];
-  T.valid = min(32, tokens - token);
-  if (id < 0 || id >= A.pages) {  // no page: its tokens are not there
-    T.valid = 0;
-    id = 0;
+  const uint32_t ko = 16 * lane, vo = (lane >> 1) * A.page + 16 * (lane & 1);
+#pragma unroll
+  for (int i = 0; i < L.kN; ++i) {
+    const int piece = min(wv + NW * i, L.kAll - 1), sub = piece / DB, part = piece - sub * DB;
+    const int id = max(__builtin_amdgcn_readlane(pages, sub), 0), off = ((t + sub) * 32) & (A.page - 1);
+    const int64_t at = ((int64_t)id * A.kv + h) * A.page;
+    L.k[i] = *reinterpret_cast<const u32x4*>(A.ck + (at + off) * D + part * 1024 + ko);
+    L.v[i] = *reinterpret_cast<const u32x4*>(A.cv + at * D + off + part * 32 * A.page + vo);
   }
-  const int64_t at = (int64_t)id * A.kv + h;
-  const int off = token & (A.page - 1);
-  T.ks = A.ks[at];
-  T.vs = A.vs[at];
-  const int rho = lane & 31, half = lane >> 5;
-  const uint8_t* kp = A.ck + (at * A.page + off) * D;
-  const uint8_t* vp = A.cv + at * A.page * D + off;
-  const int ko = pi_of(rho) * D + 16 * half, vo = rho * A.page + 16 * half;
+}
+// pages, t, tokens: of the stage. What lies behind the last token may be any code: its values are held as 0.
+template <int DB, int NW>
+__device__ __forceinline__ void store_stage(uint8_t* lds, int t, int pages, int tokens, int wv, int lane,
+                                            Loads<DB, NW>& L) {
+  using St = Staged<DB>;
 #pragma unroll
-  for (int j = 0; j < DB; ++j) T.k[j] = *reinterpret_cast<const uint4*>(kp + (ko + 32 * j));
+  for (int i = 0; i < L.kN; ++i) {
+    const int piece = wv + NW * i, sub = piece / DB, part = piece - sub * DB;
+    if (L.kAll % NW != 0 && piece >= L.kAll) continue;
+    const int valid = valid_of(pages, t, sub, tokens);
+    if (valid < 32) {
+      asm volatile("");  // (a branch, not selects for every tile)
 #pragma unroll
-  for (int j = 0; j < DB; ++j) T.v[j] = *reinterpret_cast<const uint4*>(vp + (vo + 32 * j * A.page));
+      for (int e = 0; e < 4; ++e) {
+        const int c = min(max(valid - 16 * (lane & 1) - 4 * e, 0), 4);
+        L.v[i][e] &= c == 4 ? ~0u : (1u << (8 * c)) - 1;
+      }
+    }
+    const int q = part * 64 + lane, token = q / (2 * DB), c = q - token * (2 * DB);
+    *reinterpret_cast<u32x4*>(lds + (32 * sub + rho_of(token)) * St::kKeyPitch + 16 * c) = L.k[i];
+    *reinterpret_cast<u32x4*>(lds + St::kKeys + (32 * part + (lane >> 1)) * St::kValuePitch + 32 * sub + 16 * (lane & 1)) =
+        L.v[i];
+  }
 }
 
 // A wave's running state of 32 rows: lane (r, h) has row r.
@@ -178,13 +265,12 @@ struct State {
   float m, l;    // l: this half's share
 };
 
-// x: scores plus the log2 of the values' scale. Leaves 2^12 weights in x, and O and l relative to the new m.
+// m, and O and l with it, after scores (plus the log2 of the values' scale) of which the lane's largest is `top`. What
+// weights are relative to: 2^12 w = 2^(x - that).
 template <int DB>
-__device__ inline void weigh(State<DB>& S, float (&x)[16]) {
-  float top = x[0];
-#pragma unroll
-  for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
-  top = fmaxf(top, other_half(top));
+__device__ inline float follow(State<DB>& S, float top) {
+  const Halves t = halves(top);
+  top = fmaxf(t.lo, t.hi);
   if (__ballot(top > S.m + kSlack)) {
     const float m = fmaxf(S.m, top), f = __builtin_amdgcn_exp2f(S.m - m);
     S.m = m;
@@ -194,9 +280,13 @@ __device__ inline void weigh(State<DB>& S, float (&x)[16]) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) S.o[j][i] *= f;
   }
-  const float from = S.m - kHeadroom;
+  return S.m - kHeadroom;
+}
+__device__ inline float max16(const float (&x)[16]) {
+  float top = x[0];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(x[i] - from);
+  for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+  return top;
 }
 
 __device__ inline float sum16_of(const float (&w)[16]) {
@@ -208,119 +298,178 @@ __device__ inline float sum16_of(const float (&w)[16]) {
   return (a[0] + a[1]) + (a[2] + a[3]);
 }
 
-template <bool F16, int DB>
-__device__ inline void attend_tile(const AttendArgs& A, const V8<F16> (&q)[2 * DB], Tile<DB>& T, int lane,
-                                   State<DB>& S) {
-  const int half = lane >> 5;
-  f32x16 s = {};
+constexpr float kLeast = 1e-30f;  // the least factor of a product: infinite ones, which get no weight, stay infinite
+
+// N tiles of the stage in LDS from the `sub`-th on, of valid[n] tokens each: their products, which do not wait for each
+// other, then one step of the softmax.
+template <bool F16, int DB, int N>
+__device__ __forceinline__ void attend_tiles(const AttendArgs& A, const V8<F16> (&q)[2 * DB], const uint8_t* lds, int sub,
+                                             const int (&valid)[N], float scales, int lane, State<DB>& S) {
+  using St = Staged<DB>;
+  const int rho = lane & 31, half = lane >> 5;
+  const uint8_t* kp = lds + (32 * sub + rho) * St::kKeyPitch + 16 * half;
+  f32x16 s[N] = {};
 #pragma unroll
-  for (int j = 0; j < DB; ++j) {
-    s = mfma(widen<F16>(T.k[j].x, T.k[j].y), q[2 * j], s);
-    s = mfma(widen<F16>(T.k[j].z, T.k[j].w), q[2 * j + 1], s);
-  }
-  const float vs = fminf(fmaxf(T.vs, 0x1p-40f), 0x1p40f);
-  const float f = A.scale2 * T.ks, bias = __builtin_amdgcn_logf(vs);
-  float x[16];
+  for (int j = 0; j < DB; ++j)
 #pragma unroll
-  for (int i = 0; i < 16; ++i) x[i] = fmaf(s[i], f, bias);
-  if (T.valid < 32) {  // what lies behind the last token has no weight, and its codes may be any
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (16 * half + i >= T.valid) x[i] = -INFINITY;
-    uint32_t keep[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int n = min(max(T.valid - 16 * half - 4 * i, 0), 4);
-      keep[i] = n == 4 ? ~0u : (1u << (8 * n)) - 1;
+    for (int n = 0; n < N; ++n) {
+      const u32x4 k = *reinterpret_cast<const u32x4*>(kp + 32 * n * St::kKeyPitch + 32 * j);
+      s[n] = mfma(widen<F16>(k.x, k.y), q[2 * j], s[n]);
+      s[n] = mfma(widen<F16>(k.z, k.w), q[2 * j + 1], s[n]);
     }
+  float f[N], bias[N], inv[N], top = -INFINITY;
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const float vs = fminf(fmaxf(lane_f(scales, kStage + sub + n), 0x1p-40f), 0x1p40f);
+    f[n] = A.scale2 * lane_f(scales, sub + n);
+    if (fabsf(f[n]) < kLeast) f[n] = kLeast;
+    bias[n] = __builtin_amdgcn_logf(vs);
+    inv[n] = __builtin_amdgcn_rcpf(vs);
+    if (valid[n] < 32) {  // what lies behind the last token has no weight
+      asm volatile("");   // (a branch, not selects for every tile)
+      const float none = f[n] < 0.0f ? INFINITY : -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[n][i] = 16 * half + i < valid[n] ? s[n][i] : none;
+    }
+    float hi = s[n][0], lo = hi;  // the largest score is that of the largest product, or of the least
+#pragma unroll
+    for (int i = 1; i < 16; ++i) {
+      hi = fmaxf(hi, s[n][i]);
+      lo = fminf(lo, s[n][i]);
+    }
+    top = fmaxf(top, fmaf(f[n] < 0.0f ? lo : hi, f[n], bias[n]));
+  }
+  const float from = follow<DB>(S, top);
+  f16x8 p[N][2];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const float off = bias[n] - from;
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], f[n], off));
+    S.l = fmaf(sum16_of(x), inv[n], S.l);
+    p[n][0] = narrow(x);
+    p[n][1] = narrow(x + 8);
+  }
+  const uint8_t* vp = lds + St::kKeys + rho * St::kValuePitch + 32 * sub + 16 * half;
+#pragma unroll
+  for (int n = 0; n < N; ++n)
 #pragma unroll
     for (int j = 0; j < DB; ++j) {
-      T.v[j].x &= keep[0];
-      T.v[j].y &= keep[1];
-      T.v[j].z &= keep[2];
-      T.v[j].w &= keep[3];
+      const u32x4 v = *reinterpret_cast<const u32x4*>(vp + 32 * j * St::kValuePitch + 32 * n);
+      S.o[j] = mfma(widen<true>(v.x, v.y), p[n][0], S.o[j]);
+      S.o[j] = mfma(widen<true>(v.z, v.w), p[n][1], S.o[j]);
     }
-  }
-  weigh<DB>(S, x);
-  S.l = fmaf(sum16_of(x), 1.0f / vs, S.l);
-  const f16x8 p0 = narrow(x), p1 = narrow(x + 8);
-#pragma unroll
-  for (int j = 0; j < DB; ++j) {
-    S.o[j] = mfma(widen<true>(T.v[j].x, T.v[j].y), p0, S.o[j]);
-    S.o[j] = mfma(widen<true>(T.v[j].z, T.v[j].w), p1, S.o[j]);
-  }
 }
 
+// 32 nodes in LDS, in their own type: keys like a tile's, values by dimension.
+template <int DB>
+struct Nodes {
+  static constexpr int kKeyPitch = 64 * DB + 16, kValuePitch = 64 + 16;
+  static constexpr int kKeys = 32 * kKeyPitch, kBytes = kKeys + 32 * DB * kValuePitch;
+  static constexpr int kPieces = 32 * 4 * DB;  // of 16 bytes, of keys and of values
+};
+template <int DB, int T>
+struct NodeLoads {
+  static constexpr int kN = (Nodes<DB>::kPieces + T - 1) / T;
+  u32x4 k[kN], v[kN];
+};
+template <int DB, int T>
+__device__ __forceinline__ void load_nodes(const AttendArgs& A, int b, int h, int first, int nodes, int t,
+                                           NodeLoads<DB, T>& L) {
+  const char* kp = A.k + b * A.kb + h * A.kh;
+  const char* vp = A.v + b * A.vb + h * A.vh;
+#pragma unroll
+  for (int i = 0; i < L.kN; ++i) {
+    const int u = t + T * i, n = u / (4 * DB), c = u - n * (4 * DB);
+    L.k[i] = L.v[i] = u32x4{0, 0, 0, 0};
+    if (u < Nodes<DB>::kPieces && first + n < nodes) {
+      L.k[i] = *reinterpret_cast<const u32x4*>(kp + (first + n) * A.kn + 16 * c);
+      L.v[i] = *reinterpret_cast<const u32x4*>(vp + (first + n) * A.vn + 16 * c);
+    }
+  }
+}
 __device__ inline bool not_finite16(uint32_t x, bool f16) {
   return f16 ? (x & 0x7C00u) == 0x7C00u : (x & 0x7F80u) == 0x7F80u;
 }
+// Whether a value is not finite: 0 times it is no 0, so it is held as 0 and added to the rows that see it.
+template <bool F16, int DB, int T>
+__device__ __forceinline__ bool store_nodes(uint8_t* lds, int t, const NodeLoads<DB, T>& L) {
+  using Nd = Nodes<DB>;
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < L.kN; ++i) {
+    const int u = t + T * i, n = u / (4 * DB), c = u - n * (4 * DB);
+    if (u >= Nd::kPieces) continue;
+    *reinterpret_cast<u32x4*>(lds + rho_of(n) * Nd::kKeyPitch + 16 * c) = L.k[i];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      uint16_t y = (uint16_t)(L.v[i][e / 2] >> (16 * (e & 1)));
+      if (not_finite16(y, F16)) {
+        bad = true;
+        y = 0;
+      }
+      *reinterpret_cast<uint16_t*>(lds + Nd::kKeys + (8 * c + e) * Nd::kValuePitch + 2 * n) = y;
+    }
+  }
+  return bad;
+}
 
-// 32 nodes from `first` on, in their own type. bits: the nodes that the lane's row sees.
+// The 32 nodes in LDS, `first` the first of them. bits: the nodes that the lane's row sees; bad: there are values that
+// are not finite.
 template <bool F16, int DB>
-__device__ inline void attend_nodes(const AttendArgs& A, const V8<F16> (&q)[2 * DB], int b, int h, int first, int nodes,
-                                    uint64_t bits, int lane, State<DB>& S) {
+__device__ inline void attend_nodes(const AttendArgs& A, const V8<F16> (&q)[2 * DB], const uint8_t* lds, int b, int h,
+                                    int first, int nodes, uint64_t bits, bool bad, int lane, State<DB>& S) {
+  using Nd = Nodes<DB>;
   const int rho = lane & 31, half = lane >> 5;
-  const int mine = first + pi_of(rho);
-  const char* kp = A.k + b * A.kb + h * A.kh + (mine < nodes ? mine : 0) * A.kn + 32 * half;
+  const uint8_t* kp = lds + rho * Nd::kKeyPitch + 32 * half;
   f32x16 s = {};
 #pragma unroll
   for (int j = 0; j < DB; ++j)
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
-      s = mfma(*reinterpret_cast<const V8<F16>*>(kp + 64 * j + 16 * e), q[2 * j + e], s);
+    for (int e = 0; e < 2; ++e) s = mfma(*reinterpret_cast<const V8<F16>*>(kp + 64 * j + 16 * e), q[2 * j + e], s);
   float x[16];
   const uint32_t sees = (uint32_t)(bits >> (first + 16 * half)) & 0xFFFFu;
 #pragma unroll
   for (int i = 0; i < 16; ++i) x[i] = (sees >> i) & 1 ? s[i] * A.scale2 : -INFINITY;
-  weigh<DB>(S, x);
+  const float from = follow<DB>(S, max16(x));
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(x[i] - from);
   S.l += sum16_of(x);
-  // The nodes' values are fp16, or bf16, whose range fp16 lacks: the weights are then two bf16 (16 bits).
-  V8<F16> p[2], rest[2];
+  const uint8_t* vp = lds + Nd::kKeys + rho * Nd::kValuePitch + 32 * half;
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
-    if constexpr (F16) p[e] = narrow(x + 8 * e);
+    // The nodes' values are fp16, or bf16, whose range fp16 lacks: the weights are then two bf16 (16 bits).
+    V8<F16> p, rest;
+    if constexpr (F16) p = narrow(x + 8 * e);
     else
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        p[e][i] = (__bf16)x[8 * e + i];
-        rest[e][i] = (__bf16)(x[8 * e + i] - (float)p[e][i]);
+        p[i] = (__bf16)x[8 * e + i];
+        rest[i] = (__bf16)(x[8 * e + i] - (float)p[i]);
       }
+#pragma unroll
+    for (int j = 0; j < DB; ++j) {
+      const V8<F16> a = *reinterpret_cast<const V8<F16>*>(vp + 32 * j * Nd::kValuePitch + 16 * e);
+      S.o[j] = mfma(a, p, S.o[j]);
+      if constexpr (!F16) S.o[j] = mfma(a, rest, S.o[j]);
+    }
   }
-  bool bad = false;
-  const char* vp = A.v + b * A.vb + h * A.vh;
+  if (!bad) return;
+  const char* gp = A.v + b * A.vb + h * A.vh;
+#pragma unroll 1
+  for (int n = first; n < min(first + 32, nodes); ++n) {
+    const bool on = (bits >> n) & 1;
 #pragma unroll
-  for (int j = 0; j < DB; ++j)
+    for (int j = 0; j < DB; ++j)
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      uint16_t y[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int n = first + 16 * half + 8 * e + i;
-        y[i] = 0;
-        if (n < nodes) y[i] = *reinterpret_cast<const uint16_t*>(vp + n * A.vn + 2 * (32 * j + rho));
-        if (not_finite16(y[i], F16)) {  // 0 times it is no 0: it is added below to the rows that see it
-          bad = true;
-          y[i] = 0;
-        }
+      for (int i = 0; i < 16; ++i) {
+        const int d = 32 * j + 8 * (i >> 2) + 4 * half + (i & 3);
+        const uint16_t y = *reinterpret_cast<const uint16_t*>(gp + n * A.vn + 2 * d);
+        if (on && not_finite16(y, F16))
+          S.o[j][i] += F16 ? (float)__builtin_bit_cast(_Float16, y) : __uint_as_float((uint32_t)y << 16);
+        if ((i & 3) == 3) __builtin_amdgcn_sched_barrier(0);  // (a rare path that takes no registers from the others)
       }
-      V8<F16> a;
-      __builtin_memcpy(&a, y, 16);
-      S.o[j] = mfma(a, p[e], S.o[j]);
-      if constexpr (!F16) S.o[j] = mfma(a, rest[e], S.o[j]);
-    }
-  if (__ballot(bad)) {
-    for (int n = first; n < min(first + 32, nodes); ++n) {
-      const bool on = (bits >> n) & 1;
-#pragma unroll
-      for (int j = 0; j < DB; ++j)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int d = 32 * j + 8 * (i >> 2) + 4 * half + (i & 3);
-          const uint16_t y = *reinterpret_cast<const uint16_t*>(vp + n * A.vn + 2 * d);
-          if (on && not_finite16(y, F16))
-            S.o[j][i] += F16 ? (float)__builtin_bit_cast(_Float16, y) : __uint_as_float((uint32_t)y << 16);
-        }
-    }
   }
 }
 
@@ -332,37 +481,39 @@ __device__ inline void store4(char* p, f32x4 v) {
   *reinterpret_cast<uint2*>(p) = make_uint2(__builtin_bit_cast(uint32_t, x[0]), __builtin_bit_cast(uint32_t, x[1]));
 }
 
-template <bool F16, int DB>
-__global__ void __launch_bounds__(kThreads) hs_attend_kernel(const AttendArgs A) {
-  constexpr int D = 32 * DB, kPitch = D + 4;
-  __shared__ __attribute__((aligned(16))) float s_o[2][32 * kPitch];
-  __shared__ float s_m[kWaves][32], s_l[kWaves][32];
-  const int lane = threadIdx.x & 63, wv = (int)uniform(threadIdx.x >> 6);
-  const int rho = lane & 31, half = lane >> 5;
-  // eight items, then the next row tile of the same eight: an XCD reads an item's pages once
-  const uint32_t g = A.group0 + blockIdx.x, eight = g >> 3, lot = fdiv(eight, A.div_tiles);
-  const int tile = (int)(eight - lot * (uint32_t)A.tiles);
-  const uint32_t item = lot * 8 + (g & 7);
-  if (item >= A.items) return;
-  const uint32_t bh = fdiv(item, A.div_splits);
-  const int split = (int)(item - bh * (uint32_t)A.splits);
-  const int b = (int)fdiv(bh, A.div_kv), h = (int)bh - b * A.kv;
+// A query's stages that lie in the range [from, to) of all, `before` of which come before the query's.
+template <bool F16, int DB, int WR, int NW>
+__device__ __forceinline__ void attend_range(const AttendArgs& A, int b, int h, int tile, int wv, int nth, int per, int from,
+                                             int to, int before, uint8_t* s_stage, float (*s_m)[32],
+                                             float (*s_l)[32]) {
+  constexpr int D = 32 * DB, kPitch = D + 4, WT = NW / WR, kRows = 32 * WR, T = 64 * NW;
+  float(*s_o)[32 * kPitch] = reinterpret_cast<float(*)[32 * kPitch]>(s_stage);
+  int thread = threadIdx.x;
+  asm volatile("" : "+v"(thread));  // no address is formed before the loop over queries and kept through it
+  const int lane = thread & 63, rho = lane & 31, half = lane >> 5, wr = wv % WR, wt = wv / WR;
   const int nodes = nodes_of(A, b), rows = nodes * A.group;
-  if (tile * 32 >= rows) return;
-  const Parts P = parts_of(A, b);
-  if (split >= P.used) return;
+  if (tile * kRows >= rows) return;
+  const int tokens = same(tokens_of(A, b)), stages = same(stages_of(A, b));
+  const bool starts = before >= from, ends = before + stages <= to;  // the query's first, its last stage is in the range
+  const int first = starts ? 0 : (from - before) * kStage;
+  const int last = min(ends ? INT_MAX : (to - before) * kStage, (tokens + 31) / 32);
 
-  const int row = tile * 32 + rho;
-  const bool live = row < rows;
-  const int node = live ? (int)fdiv((uint32_t)row, A.div_group) : 0, head = h * A.group + (live ? row - node * A.group : 0);
+  const int row = tile * kRows + wr * 32 + rho;
+  const bool live = row < rows, busy = tile * kRows + wr * 32 < rows;  // busy: the wave has rows
+  const int node = live ? (int)fdiv((uint32_t)row, A.div_group) : 0;
+  const int head = h * A.group + (live ? row - node * A.group : 0);
+  // What comes first is asked for first: a draft's nodes (their keys and values go through LDS before the stages), the
+  // queries, the first stage.
+  NodeLoads<DB, T> nl;
+  if (ends) load_nodes<DB, T>(A, b, h, 0, nodes, thread, nl);
   V8<F16> q[2 * DB];
   const char* qp = A.q + b * A.qb + node * A.qn + head * A.qh + 32 * half;
 #pragma unroll
   for (int j = 0; j < DB; ++j)
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      uint4 x = *reinterpret_cast<const uint4*>(qp + 64 * j + 16 * e);
-      if (!live) x = make_uint4(0, 0, 0, 0);
+      u32x4 x = *reinterpret_cast<const u32x4*>(qp + 64 * j + 16 * e);
+      if (!live) x = u32x4{0, 0, 0, 0};
       __builtin_memcpy(&q[2 * j + e], &x, 16);
     }
   State<DB> S;
@@ -371,166 +522,254 @@ __global__ void __launch_bounds__(kThreads) hs_attend_kernel(const AttendArgs A)
   S.m = kLowest;
   S.l = 0.0f;
 
-  const int last = min((P.tokens + 31) / 32, (split + 1) * P.per);
-  int t = split * P.per + wv;
-  Tile<DB> one, two;
-  if (t < last) load_tile<DB>(A, b, h, t, P.tokens, lane, one);
-  while (t < last) {
-    if (t + kWaves < last) load_tile<DB>(A, b, h, t + kWaves, P.tokens, lane, two);
-    attend_tile<F16, DB>(A, q, one, lane, S);
-    t += kWaves;
-    if (t >= last) break;
-    if (t + kWaves < last) load_tile<DB>(A, b, h, t + kWaves, P.tokens, lane, one);
-    attend_tile<F16, DB>(A, q, two, lane, S);
-    t += kWaves;
+  Loads<DB, NW> L;
+  int pages = pages_of(A, b, first, last, lane), next = -1;  // of the stage that is on its way, of the one behind it
+  float coming = 0.0f;                                       // its scales
+  if (first < last) {
+    coming = scales_of(A, h, pages, lane);
+    next = pages_of(A, b, first + kStage, last, lane);
+    load_stage<DB, NW>(A, h, first, pages, wv, lane, L);
   }
-  if (split == P.used - 1 && wv < 2 && wv * 32 < nodes) {  // the last split has the nodes too
+  if (ends) {  // the query's last part has the nodes too
     uint64_t bits = 0;
     if (live) {
       bits = A.mask ? A.mask[(int64_t)b * A.M + node] : (2ull << node) - 1;
       if (nodes < 64) bits &= (1ull << nodes) - 1;
     }
-    attend_nodes<F16, DB>(A, q, b, h, wv * 32, nodes, bits, lane, S);
+#pragma unroll 1
+    for (int n = 0; n < nodes; n += 32) {
+      if (n > 0) {
+        load_nodes<DB, T>(A, b, h, n, nodes, thread, nl);
+        __syncthreads();  // the 32 before are read
+      }
+      const bool bad = __syncthreads_or(store_nodes<F16, DB, T>(s_stage, thread, nl));
+      if (busy && (n >> 5) % WT == wt) attend_nodes<F16, DB>(A, q, s_stage, b, h, n, nodes, bits, bad, lane, S);
+    }
+    __syncthreads();
   }
-  S.l += other_half(S.l);
 
-  // the waves' states, joined
-  if (half == 0) {
-    s_m[wv][rho] = S.m;
-    s_l[wv][rho] = S.l;
-  }
-  __syncthreads();
-  float m = s_m[0][rho], l = 0.0f;
-#pragma unroll
-  for (int w = 1; w < kWaves; ++w) m = fmaxf(m, s_m[w][rho]);
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) l = fmaf(s_l[w][rho], __builtin_amdgcn_exp2f(s_m[w][rho] - m), l);
-  const float f = __builtin_amdgcn_exp2f(S.m - m);
-#pragma unroll
-  for (int j = 0; j < DB; ++j)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) S.o[j][i] *= f;
-#pragma unroll
-  for (int step = 0; step < 2; ++step) {  // waves 2 and 3 to 0 and 1, then 1 to 0
-    const int from = step == 0 ? 2 : 1;
-    if (wv >= from && wv < 2 * from) {
-      float* to = &s_o[wv - from][rho * kPitch + 4 * half];
-#pragma unroll
-      for (int j = 0; j < DB; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<f32x4*>(to + 32 * j + 8 * i) =
-              f32x4{S.o[j][4 * i], S.o[j][4 * i + 1], S.o[j][4 * i + 2], S.o[j][4 * i + 3]};
-    }
+  for (int t = first; t < last; t += kStage) {
+    if (t > first) __syncthreads();  // the stage before is read
+    store_stage<DB, NW>(s_stage, t, pages, tokens, wv, lane, L);
+    const int here = pages;
+    const float scales = coming;
+    pages = next;
     __syncthreads();
-    if (wv < from) {
-      const float* at = &s_o[wv][rho * kPitch + 4 * half];
-#pragma unroll
-      for (int j = 0; j < DB; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f32x4 y = *reinterpret_cast<const f32x4*>(at + 32 * j + 8 * i);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) S.o[j][4 * i + k] += y[k];
-        }
+    if (t + kStage < last) {
+      coming = scales_of(A, h, pages, lane);
+      next = pages_of(A, b, t + 2 * kStage, last, lane);
+      load_stage<DB, NW>(A, h, t + kStage, pages, wv, lane, L);
     }
-    __syncthreads();
+    if (!busy) continue;
+    constexpr int N = WT <= 2 ? 2 : 1;  // tiles at once
+#pragma unroll
+    for (int i = 0; i < kStage; i += N * WT) {
+      const int sub = i + wt * N;
+      int valid[N];
+#pragma unroll
+      for (int n = 0; n < N; ++n) valid[n] = valid_of(here, t, sub + n, tokens);
+      attend_tiles<F16, DB, N>(A, q, s_stage, sub, valid, scales, lane, S);
+    }
   }
-  if (wv != 0) return;
-  const int64_t slot = ((int64_t)bh * A.tiles + tile) * A.splits + split;
-  if (P.used == 1) {
-    const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;  // (a NaN stays)
-    if (live) {
-      char* op = A.out + b * A.ob + node * A.on + head * A.oh + 8 * half;
-#pragma unroll
-      for (int j = 0; j < DB; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          store4<F16>(op + 64 * j + 16 * i, f32x4{S.o[j][4 * i] * inv, S.o[j][4 * i + 1] * inv,
-                                                  S.o[j][4 * i + 2] * inv, S.o[j][4 * i + 3] * inv});
+
+  float m = S.m, l = halves(S.l).lo + halves(S.l).hi;
+  if constexpr (WT > 1) {  // the states of the waves of a group, joined
+    if (half == 0) {
+      s_m[wv][rho] = m;
+      s_l[wv][rho] = l;
     }
-    return;
+    __syncthreads();  // (and the last stage is read)
+    m = s_m[wr][rho];
+#pragma unroll
+    for (int w = 1; w < WT; ++w) m = fmaxf(m, s_m[w * WR + wr][rho]);
+    l = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WT; ++w)
+      l = fmaf(s_l[w * WR + wr][rho], __builtin_amdgcn_exp2f(s_m[w * WR + wr][rho] - m), l);
+    const float f = __builtin_amdgcn_exp2f(S.m - m);
+#pragma unroll
+    for (int j = 0; j < DB; ++j)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) S.o[j][i] *= f;
+#pragma unroll
+    for (int from = WT / 2; from >= 1; from /= 2) {  // the upper half of the waves to the lower
+      if (wt >= from && wt < 2 * from) {
+        float* to = &s_o[(wt - from) * WR + wr][rho * kPitch + 4 * half];
+#pragma unroll
+        for (int j = 0; j < DB; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<f32x4*>(to + 32 * j + 8 * i) =
+                f32x4{S.o[j][4 * i], S.o[j][4 * i + 1], S.o[j][4 * i + 2], S.o[j][4 * i + 3]};
+      }
+      __syncthreads();
+      if (wt < from) {
+        const float* at = &s_o[wt * WR + wr][rho * kPitch + 4 * half];
+#pragma unroll
+        for (int j = 0; j < DB; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const f32x4 y = *reinterpret_cast<const f32x4*>(at + 32 * j + 8 * i);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) S.o[j][4 * i + k] += y[k];
+          }
+      }
+      if (from > 1) __syncthreads();
+    }
+    if (wt != 0) return;
   }
   if (!live) return;
-  float* op = A.part + (slot * 32 + rho) * D + 4 * half;
+  if (starts && ends) {
+    const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;  // (a NaN stays)
+    char* op = A.out + b * A.ob + node * A.on + head * A.oh + 8 * half;
+#pragma unroll
+    for (int j = 0; j < DB; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        store4<F16>(op + 64 * j + 16 * i, f32x4{S.o[j][4 * i] * inv, S.o[j][4 * i + 1] * inv, S.o[j][4 * i + 2] * inv,
+                                                S.o[j][4 * i + 3] * inv});
+    return;
+  }
+  const int64_t at = ((int64_t)(h * A.tiles + tile) * (2 * A.chunks) + 2 * nth + (before > from ? 1 : 0)) * kRows + wr * 32 + rho;
+  float* op = A.part + at * D + 4 * half;
 #pragma unroll
   for (int j = 0; j < DB; ++j)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       *reinterpret_cast<f32x4*>(op + 32 * j + 8 * i) =
           f32x4{S.o[j][4 * i], S.o[j][4 * i + 1], S.o[j][4 * i + 2], S.o[j][4 * i + 3]};
-  if (half == 0) A.part_ml[slot * 32 + rho] = make_float2(m, l);
+  if (half == 0) A.part_ml[at] = make_float2(m, l);
 }
 
-// A wave a row: its splits, joined.
-template <bool F16, int DB>
-__global__ void __launch_bounds__(kThreads) hs_attend_join_kernel(const AttendArgs A) {
-  constexpr int D = 32 * DB;
-  const int lane = threadIdx.x & 63;
-  const uint32_t u = uniform((A.group0 + blockIdx.x) * kWaves + (threadIdx.x >> 6));
-  const uint32_t bt = u >> 5;  // (query, cached head, tile)
-  if (bt >= (uint32_t)A.B * (uint32_t)A.kv * (uint32_t)A.tiles) return;
-  const uint32_t bh = fdiv(bt, A.div_tiles);
-  const int tile = (int)(bt - bh * (uint32_t)A.tiles);
-  const int b = (int)fdiv(bh, A.div_kv), h = (int)bh - b * A.kv;
-  const int row = tile * 32 + (int)(u & 31);
-  if (row >= nodes_of(A, b) * A.group) return;
-  const int used = parts_of(A, b).used;
-  if (used == 1) return;
-  const int64_t slot = (int64_t)bt * A.splits;
-  const float2* ml = A.part_ml + slot * 32 + (u & 31);
-  float m = kLowest;
-  for (int s = 0; s < used; ++s) m = fmaxf(m, ml[s * 32].x);
-  float l = 0.0f, o[(D + 63) / 64] = {};
-  for (int s = 0; s < used; ++s) {
-    const float2 y = ml[s * 32];
-    const float f = __builtin_amdgcn_exp2f(y.x - m);
-    l = fmaf(y.y, f, l);
-    const float* p = A.part + ((slot + s) * 32 + (u & 31)) * D;
-#pragma unroll
-    for (int i = 0; i < (D + 63) / 64; ++i)
-      if (i * 64 + lane < D) o[i] = fmaf(p[i * 64 + lane], f, o[i]);
+// A workgroup of NW waves has 32 rows for each of WR groups of its waves. It brings kStage tiles at a time to LDS, of
+// which the WT = NW / WR waves of a group take every WT-th each; their states are joined at the end. The next stage is on
+// its way to registers meanwhile.
+template <bool F16, int DB, int WR, int NW>
+__global__ void __launch_bounds__(64 * NW, DB <= 4 ? 2 : 1) hs_attend_kernel(const AttendArgs A) {
+  constexpr int kPitch = 32 * DB + 4, WT = NW / WR;
+  using St = Staged<DB>;
+  constexpr int kBytes = St::kBytes > Nodes<DB>::kBytes ? St::kBytes : Nodes<DB>::kBytes;
+  __shared__ __attribute__((aligned(16))) uint8_t s_stage[kBytes];
+  static_assert(WT == 1 || kBytes >= WT / 2 * WR * 32 * kPitch * 4, "the join shares the stage's memory");
+  static_assert(WT <= kStage, "a wave has a tile of every stage");
+  __shared__ float s_m[NW][32], s_l[NW][32];
+  const int lane = threadIdx.x & 63, wv = (int)uniform(threadIdx.x >> 6);
+  // eight items, then the next rows of the same eight: an XCD reads an item's pages once
+  const uint32_t g = A.group0 + blockIdx.x, eight = g >> 3, lot = fdiv(eight, A.div_tiles);
+  const int tile = (int)(eight - lot * (uint32_t)A.tiles);
+  const uint32_t item = lot * 8 + (g & 7);
+  if (item >= A.items) return;
+  const int nth = (int)fdiv(item, A.div_kv), h = (int)item - nth * A.kv;
+  // the range's stages, of all queries'; of a query that is its own range they are its own
+  int per = 0, from = 0, to = INT_MAX, b = nth, before = 0;
+  if (A.chunks) {
+    const Plan plan(A, lane);
+    per = plan.per;
+    from = nth * per;
+    to = from + per;
+    b = plan.query(A, from, &before);
+    if (b < 0) return;
   }
-  const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
-  const int node = (int)fdiv((uint32_t)row, A.div_group), head = h * A.group + row - node * A.group;
-  char* op = A.out + b * A.ob + node * A.on + head * A.oh;
-#pragma unroll
-  for (int i = 0; i < (D + 63) / 64; ++i)
-    if (i * 64 + lane < D) {
-      const float y = o[i] * inv;
-      if constexpr (F16) reinterpret_cast<_Float16*>(op)[i * 64 + lane] = (_Float16)y;
-      else reinterpret_cast<__bf16*>(op)[i * 64 + lane] = (__bf16)y;
+  for (bool again = false;; again = true) {  // the queries of the range
+    if (again) {
+      before += same(stages_of(A, b));
+      if (!A.chunks || ++b >= A.B || before >= to) return;
+      __syncthreads();  // (the last query's join is read)
     }
+    attend_range<F16, DB, WR, NW>(A, b, h, tile, wv, nth, per, from, to, before, s_stage, s_m, s_l);
+  }
+}
+// The parts of a query's rows, joined: 32 rows of a cached head a workgroup, a wave a row at a time.
+constexpr int kJoinRows = 32;
+template <bool F16, int DB, int WR>
+__global__ void __launch_bounds__(kThreads) hs_attend_join_kernel(const AttendArgs A) {
+  constexpr int D = 32 * DB, kRows = 32 * WR, kPer = (D + 63) / 64, kAhead = 8;
+  const int lane = threadIdx.x & 63, wv = (int)uniform(threadIdx.x >> 6);
+  const uint32_t bh = fdiv(blockIdx.x, A.div_rows);
+  const int b = (int)fdiv(bh, A.div_kv), h = (int)bh - b * A.kv;
+  const int row0 = (int)(blockIdx.x - bh * A.row_groups) * kJoinRows, rows = nodes_of(A, b) * A.group;
+  if (row0 >= rows) return;
+  const Plan plan(A, lane);
+  const int before = plan.before(A, b), r0 = before / plan.per, r1 = (before + same(stages_of(A, b)) - 1) / plan.per;
+  if (r0 == r1) return;  // one part
+  for (int row = row0 + wv; row < min(row0 + kJoinRows, rows); row += kWaves) {
+    const int tile = row / kRows;
+    const int64_t base = (int64_t)(h * A.tiles + tile) * (2 * A.chunks) * kRows + (row - tile * kRows);
+    auto place = [&](int r) -> int64_t { return base + (int64_t)(2 * r + (before > r * plan.per ? 1 : 0)) * kRows; };
+    float m = kLowest, l = 0.0f, o[kPer] = {};
+    for (int s = r0; s <= r1; s += 64) {  // 64 parts at a time, a lane each
+      const float2 ml = s + lane <= r1 ? A.part_ml[place(s + lane)] : make_float2(kLowest, 0.0f);
+      const float top = fkey_inv(wave_max_i(fkey(ml.x))), now = fmaxf(m, top), old = __builtin_amdgcn_exp2f(m - now);
+      m = now;
+      const float f = __builtin_amdgcn_exp2f(ml.x - m);
+      l = l * old + wave_sum_f(ml.y * f);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) o[i] *= old;
+      const int n = min(64, r1 - s + 1);
+      for (int k = 0; k < n; k += kAhead) {
+        float y[kAhead][kPer];
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {
+          const float* p = A.part + place(s + min(k + a, n - 1)) * D;
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) y[a][i] = i * 64 + lane < D ? p[i * 64 + lane] : 0.0f;
+        }
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {
+          const float w = k + a < n ? lane_f(f, min(k + a, 63)) : 0.0f;
+          if (k + a < n)
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) o[i] = fmaf(y[a][i], w, o[i]);
+        }
+      }
+    }
+    const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
+    const int node = (int)fdiv((uint32_t)row, A.div_group), head = h * A.group + row - node * A.group;
+    char* op = A.out + b * A.ob + node * A.on + head * A.oh;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (i * 64 + lane < D) {
+        const float y = o[i] * inv;
+        if constexpr (F16) reinterpret_cast<_Float16*>(op)[i * 64 + lane] = (_Float16)y;
+        else reinterpret_cast<__bf16*>(op)[i * 64 + lane] = (__bf16)y;
+      }
+  }
+}
+
+template <bool F16, int DB, int WR, int NW>
+void launch_rows(AttendArgs A, hipStream_t st) {
+  const uint64_t groups = ((uint64_t)A.items + 7) / 8 * 8 * A.tiles;
+  constexpr uint64_t kMost = kMostGroups / (NW / kWaves);
+  for (uint64_t at = 0; at < groups; at += kMost) {
+    A.group0 = (uint32_t)at;
+    hs_attend_kernel<F16, DB, WR, NW><<<(uint32_t)std::min<uint64_t>(groups - at, kMost), 64 * NW, 0, st>>>(A);
+    if (hipPeekAtLastError() != hipSuccess) return;
+  }
+  if (!A.chunks) return;
+  const uint32_t joins = (uint32_t)A.B * A.kv * A.row_groups;  // (few: ranges are for few queries and heads)
+  hs_attend_join_kernel<F16, DB, WR><<<joins, kThreads, 0, st>>>(A);
 }
 
 template <bool F16, int DB>
-void launch_dim(AttendArgs A, hipStream_t st) {
-  const uint64_t groups = ((uint64_t)A.items + 7) / 8 * 8 * A.tiles;
-  for (uint64_t at = 0; at < groups; at += kMostGroups) {
-    A.group0 = (uint32_t)at;
-    hs_attend_kernel<F16, DB><<<(uint32_t)std::min<uint64_t>(groups - at, kMostGroups), kThreads, 0, st>>>(A);
-    if (hipPeekAtLastError() != hipSuccess) return;
-  }
-  if (A.splits == 1) return;
-  const uint64_t joins = (uint64_t)A.B * A.kv * A.tiles * 32 / kWaves;
-  for (uint64_t at = 0; at < joins; at += kMostGroups) {
-    A.group0 = (uint32_t)at;
-    hs_attend_join_kernel<F16, DB><<<(uint32_t)std::min<uint64_t>(joins - at, kMostGroups), kThreads, 0, st>>>(A);
-    if (hipPeekAtLastError() != hipSuccess) return;
-  }
+void launch_dim(const AttendArgs& A, const AttendGeom& g, hipStream_t st) {
+  if constexpr (DB <= 4)
+    if (g.wr == 8) return launch_rows<F16, DB, 8, 8>(A, st);
+  if (g.wr == 4) return launch_rows<F16, DB, 4, 4>(A, st);
+  if (g.wr == 2) return launch_rows<F16, DB, 2, 4>(A, st);
+  launch_rows<F16, DB, 1, 4>(A, st);
 }
 
 template <bool F16>
-void launch_type(const AttendArgs& A, int dim, hipStream_t st) {
-  switch (dim / 32) {
-    case 1: return launch_dim<F16, 1>(A, st);
-    case 2: return launch_dim<F16, 2>(A, st);
-    case 3: return launch_dim<F16, 3>(A, st);
-    case 4: return launch_dim<F16, 4>(A, st);
-    case 5: return launch_dim<F16, 5>(A, st);
-    case 6: return launch_dim<F16, 6>(A, st);
-    case 7: return launch_dim<F16, 7>(A, st);
-    default: return launch_dim<F16, 8>(A, st);
+void launch_type(const AttendArgs& A, const AttendGeom& g, hipStream_t st) {
+  switch (g.dim / 32) {
+    case 1: return launch_dim<F16, 1>(A, g, st);
+    case 2: return launch_dim<F16, 2>(A, g, st);
+    case 3: return launch_dim<F16, 3>(A, g, st);
+    case 4: return launch_dim<F16, 4>(A, g, st);
+    case 5: return launch_dim<F16, 5>(A, g, st);
+    case 6: return launch_dim<F16, 6>(A, g, st);
+    case 7: return launch_dim<F16, 7>(A, g, st);
+    default: return launch_dim<F16, 8>(A, g, st);
   }
 }
 
@@ -546,16 +785,20 @@ bool attend_geom(int B, int M, int heads, int kv, int dim, int page, int slots, 
   g->heads = heads;
   g->kv = kv;
   g->dim = dim;
-  g->tiles = (M * (heads / kv) + 31) / 32;
-  const int64_t groups = (int64_t)B * kv * g->tiles, most = ((int64_t)slots * page + 31) / 32;
-  const int64_t want = (1024 + groups - 1) / groups, can = (most + kAttendLeast - 1) / kAttendLeast;
-  g->splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, can), 128));
-  return groups * g->splits < ((int64_t)1 << 31);
+  const int rows = M * (heads / kv);
+  g->wr = rows > 128 && dim <= 128 ? 8 : rows > 64 ? 4 : rows > 32 ? 2 : 1;
+  g->tiles = (rows + 32 * g->wr - 1) / (32 * g->wr);
+  // Ranges for the workgroups that the device holds at once, two of 4 waves a CU or one of 8; a workgroup a query and
+  // head where there are four times as many of those.
+  const int64_t groups = (int64_t)B * kv * g->tiles, hold = g->wr == 8 || dim > 128 ? 256 : 512;
+  const int64_t stages = ((int64_t)slots * page + 32 * kStage - 1) / (32 * kStage) * B;
+  g->chunks = groups >= 4 * hold ? 0 : (int)std::min(std::max<int64_t>(hold / ((int64_t)kv * g->tiles), 1), stages);
+  return groups < ((int64_t)1 << 30);
 }
 
 size_t attend_ws_bytes(const AttendGeom& g) {
-  if (g.splits == 1) return 0;
-  const size_t slots = (size_t)g.B * g.kv * g.tiles * g.splits * 32;
+  if (!g.chunks) return 0;
+  const size_t slots = (size_t)g.kv * g.tiles * (2 * g.chunks) * (32 * g.wr);
   return align256(slots * g.dim * sizeof(float)) + align256(slots * sizeof(float2));
 }
 
@@ -589,18 +832,19 @@ int launch_attend(const AttendGeom& g, const hs_tree_attention_args& a, hipStrea
   A.count = a.count;
   A.scale2 = (float)(a.scale * 1.4426950408889634074);
   A.tiles = g.tiles;
-  A.splits = g.splits;
-  A.items = (uint32_t)((int64_t)g.B * g.kv * g.splits);
-  A.div_splits = make_fastdiv((uint32_t)g.splits);
+  A.chunks = g.chunks;
+  A.items = (uint32_t)((int64_t)(g.chunks ? g.chunks : g.B) * g.kv);
   A.div_kv = make_fastdiv((uint32_t)g.kv);
   A.div_tiles = make_fastdiv((uint32_t)g.tiles);
   A.div_group = make_fastdiv((uint32_t)A.group);
-  const size_t slots = (size_t)g.B * g.kv * g.tiles * g.splits * 32;
+  A.row_groups = (uint32_t)(g.M * A.group + kJoinRows - 1) / kJoinRows;
+  A.div_rows = make_fastdiv(A.row_groups);
+  const size_t slots = (size_t)g.kv * g.tiles * (2 * g.chunks) * (32 * g.wr);
   A.part = reinterpret_cast<float*>(a.workspace);
   A.part_ml = reinterpret_cast<float2*>(reinterpret_cast<char*>(a.workspace) +
                                         align256(slots * g.dim * sizeof(float)));
-  if (a.dtype == HS_F16) launch_type<true>(A, g.dim, stream);
-  else launch_type<false>(A, g.dim, stream);
+  if (a.dtype == HS_F16) launch_type<true>(A, g, stream);
+  else launch_type<false>(A, g, stream);
   return hipPeekAtLastError() == hipSuccess ? HS_OK : HS_ERR_HIP;
 }
 
