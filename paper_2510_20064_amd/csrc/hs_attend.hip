@@ -61,10 +61,10 @@ struct AttendArgs {
   int tiles;   // workgroups that share a cached head's rows
   int chunks;  // ranges that all queries' cached tokens are cut into; 0: a query is one
   uint32_t items, group0;  // (ranges, or queries) * kv
-  uint32_t row_groups;     // workgroups of the join for a query's cached head
+  uint32_t row_tiles;      // 32 rows of a query's cached head
   FastDiv div_kv, div_tiles, div_group, div_rows;
-  float* part;      // [kv * tiles][2 * chunks][rows][D]
-  float2* part_ml;  // [kv * tiles][2 * chunks][rows]
+  float* part;      // [kv * tiles][2 * chunks][WR][D / 8][2][32 rows][4]
+  float2* part_ml;  // [kv * tiles][2 * chunks][WR][32 rows]
 };
 
 __device__ inline int same(int x) { return (int)uniform((uint32_t)x); }  // (what every lane has, in a scalar register)
@@ -618,8 +618,8 @@ __device__ __forceinline__ void attend_range(const AttendArgs& A, int b, int h, 
     }
     if (wt != 0) return;
   }
-  if (!live) return;
   if (starts && ends) {
+    if (!live) return;
     const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;  // (a NaN stays)
     char* op = A.out + b * A.ob + node * A.on + head * A.oh + 8 * half;
 #pragma unroll
@@ -630,15 +630,15 @@ __device__ __forceinline__ void attend_range(const AttendArgs& A, int b, int h, 
                                                 S.o[j][4 * i + 3] * inv});
     return;
   }
-  const int64_t at = ((int64_t)(h * A.tiles + tile) * (2 * A.chunks) + 2 * nth + (before > from ? 1 : 0)) * kRows + wr * 32 + rho;
-  float* op = A.part + at * D + 4 * half;
+  const int64_t at = (((int64_t)(h * A.tiles + tile) * (2 * A.chunks) + 2 * nth + (before > from ? 1 : 0)) * WR + wr) * 32;
+  float* op = A.part + at * D + 4 * lane;  // (as the registers are: a wave writes 1 KB at a time)
 #pragma unroll
   for (int j = 0; j < DB; ++j)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      *reinterpret_cast<f32x4*>(op + 32 * j + 8 * i) =
+      *reinterpret_cast<f32x4*>(op + (4 * j + i) * 256) =
           f32x4{S.o[j][4 * i], S.o[j][4 * i + 1], S.o[j][4 * i + 2], S.o[j][4 * i + 3]};
-  if (half == 0) A.part_ml[at] = make_float2(m, l);
+  if (half == 0) A.part_ml[at + rho] = make_float2(m, l);
 }
 
 // A workgroup of NW waves has 32 rows for each of WR groups of its waves. It brings kStage tiles at a time to LDS, of
@@ -679,61 +679,54 @@ __global__ void __launch_bounds__(64 * NW, DB <= 4 ? 2 : 1) hs_attend_kernel(con
     attend_range<F16, DB, WR, NW>(A, b, h, tile, wv, nth, per, from, to, before, s_stage, s_m, s_l);
   }
 }
-// The parts of a query's rows, joined: 32 rows of a cached head a workgroup, a wave a row at a time.
-constexpr int kJoinRows = 32;
+// The parts of a query's rows, joined: a wave 8 dims of 32 rows, as they were in the registers.
 template <bool F16, int DB, int WR>
 __global__ void __launch_bounds__(kThreads) hs_attend_join_kernel(const AttendArgs A) {
-  constexpr int D = 32 * DB, kRows = 32 * WR, kPer = (D + 63) / 64, kAhead = 8;
-  const int lane = threadIdx.x & 63, wv = (int)uniform(threadIdx.x >> 6);
-  const uint32_t bh = fdiv(blockIdx.x, A.div_rows);
+  constexpr int D = 32 * DB, kAhead = 8;
+  const int lane = threadIdx.x & 63, i = (int)uniform(threadIdx.x >> 6), rho = lane & 31, half = lane >> 5;
+  const uint32_t group = blockIdx.x / DB, bh = fdiv(group, A.div_rows);
+  const int j = (int)(blockIdx.x - group * DB), rt = (int)(group - bh * A.row_tiles);
   const int b = (int)fdiv(bh, A.div_kv), h = (int)bh - b * A.kv;
-  const int row0 = (int)(blockIdx.x - bh * A.row_groups) * kJoinRows, rows = nodes_of(A, b) * A.group;
-  if (row0 >= rows) return;
+  const int rows = nodes_of(A, b) * A.group;
+  if (rt * 32 >= rows) return;
   const Plan plan(A, lane);
   const int before = plan.before(A, b), r0 = before / plan.per, r1 = (before + same(stages_of(A, b)) - 1) / plan.per;
   if (r0 == r1) return;  // one part
-  for (int row = row0 + wv; row < min(row0 + kJoinRows, rows); row += kWaves) {
-    const int tile = row / kRows;
-    const int64_t base = (int64_t)(h * A.tiles + tile) * (2 * A.chunks) * kRows + (row - tile * kRows);
-    auto place = [&](int r) -> int64_t { return base + (int64_t)(2 * r + (before > r * plan.per ? 1 : 0)) * kRows; };
-    float m = kLowest, l = 0.0f, o[kPer] = {};
-    for (int s = r0; s <= r1; s += 64) {  // 64 parts at a time, a lane each
-      const float2 ml = s + lane <= r1 ? A.part_ml[place(s + lane)] : make_float2(kLowest, 0.0f);
-      const float top = fkey_inv(wave_max_i(fkey(ml.x))), now = fmaxf(m, top), old = __builtin_amdgcn_exp2f(m - now);
-      m = now;
-      const float f = __builtin_amdgcn_exp2f(ml.x - m);
-      l = l * old + wave_sum_f(ml.y * f);
+  const int tile = rt / WR;
+  const int64_t base = (int64_t)(h * A.tiles + tile) * (2 * A.chunks);
+  auto place = [&](int r) -> int64_t {  // the first of the 32 rows of part r
+    return ((base + 2 * r + (before > r * plan.per ? 1 : 0)) * WR + (rt - tile * WR)) * 32;
+  };
+  float m = kLowest;
+  for (int r = r0; r <= r1; r += kAhead)
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) o[i] *= old;
-      const int n = min(64, r1 - s + 1);
-      for (int k = 0; k < n; k += kAhead) {
-        float y[kAhead][kPer];
+    for (int a = 0; a < kAhead; ++a) m = fmaxf(m, A.part_ml[place(min(r + a, r1)) + rho].x);
+  float l = 0.0f;
+  f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int r = r0; r <= r1; r += kAhead) {
+    f32x4 y[kAhead];
+    float2 ml[kAhead];
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a) {
-          const float* p = A.part + place(s + min(k + a, n - 1)) * D;
-#pragma unroll
-          for (int i = 0; i < kPer; ++i) y[a][i] = i * 64 + lane < D ? p[i * 64 + lane] : 0.0f;
-        }
-#pragma unroll
-        for (int a = 0; a < kAhead; ++a) {
-          const float w = k + a < n ? lane_f(f, min(k + a, 63)) : 0.0f;
-          if (k + a < n)
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) o[i] = fmaf(y[a][i], w, o[i]);
-        }
-      }
+    for (int a = 0; a < kAhead; ++a) {
+      const int64_t at = place(min(r + a, r1));
+      ml[a] = A.part_ml[at + rho];
+      y[a] = *reinterpret_cast<const f32x4*>(A.part + at * D + (4 * j + i) * 256 + 4 * lane);
     }
-    const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
-    const int node = (int)fdiv((uint32_t)row, A.div_group), head = h * A.group + row - node * A.group;
-    char* op = A.out + b * A.ob + node * A.on + head * A.oh;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i)
-      if (i * 64 + lane < D) {
-        const float y = o[i] * inv;
-        if constexpr (F16) reinterpret_cast<_Float16*>(op)[i * 64 + lane] = (_Float16)y;
-        else reinterpret_cast<__bf16*>(op)[i * 64 + lane] = (__bf16)y;
+    for (int a = 0; a < kAhead; ++a)
+      if (r + a <= r1) {
+        const float f = __builtin_amdgcn_exp2f(ml[a].x - m);
+        l = fmaf(ml[a].y, f, l);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[k] = fmaf(y[a][k], f, o[k]);
       }
   }
+  const int row = rt * 32 + rho;
+  if (row >= rows) return;
+  const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
+  const int node = (int)fdiv((uint32_t)row, A.div_group), head = h * A.group + row - node * A.group;
+  store4<F16>(A.out + b * A.ob + node * A.on + head * A.oh + 2 * (32 * j + 8 * i + 4 * half),
+              f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv});
 }
 
 template <bool F16, int DB, int WR, int NW>
@@ -746,7 +739,7 @@ void launch_rows(AttendArgs A, hipStream_t st) {
     if (hipPeekAtLastError() != hipSuccess) return;
   }
   if (!A.chunks) return;
-  const uint32_t joins = (uint32_t)A.B * A.kv * A.row_groups;  // (few: ranges are for few queries and heads)
+  const uint32_t joins = (uint32_t)A.B * A.kv * A.row_tiles * DB;  // (few: ranges are for few queries and heads)
   hs_attend_join_kernel<F16, DB, WR><<<joins, kThreads, 0, st>>>(A);
 }
 
@@ -837,8 +830,8 @@ int launch_attend(const AttendGeom& g, const hs_tree_attention_args& a, hipStrea
   A.div_kv = make_fastdiv((uint32_t)g.kv);
   A.div_tiles = make_fastdiv((uint32_t)g.tiles);
   A.div_group = make_fastdiv((uint32_t)A.group);
-  A.row_groups = (uint32_t)(g.M * A.group + kJoinRows - 1) / kJoinRows;
-  A.div_rows = make_fastdiv(A.row_groups);
+  A.row_tiles = (uint32_t)(g.M * A.group + 31) / 32;
+  A.div_rows = make_fastdiv(A.row_tiles);
   const size_t slots = (size_t)g.kv * g.tiles * (2 * g.chunks) * (32 * g.wr);
   A.part = reinterpret_cast<float*>(a.workspace);
   A.part_ml = reinterpret_cast<float2*>(reinterpret_cast<char*>(a.workspace) +
