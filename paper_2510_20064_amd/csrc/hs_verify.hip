@@ -33,7 +33,7 @@ namespace {
 constexpr int kLoads = kVerifySlice / 64;  // of 16 bytes per lane
 constexpr int kWalkThreads = 1024;
 constexpr int kWalkWaves = kWalkThreads / 64;
-constexpr int kHeldParts = kMaxTeamSlices / 64;  // a row's parts per lane
+constexpr int kMostHeld = kMaxTeamSlices / 64;  // a row's parts per lane
 
 struct Part {
   double sum;  // of the slice's weights relative to m (not finite: a NaN or +inf logit)
@@ -60,6 +60,8 @@ struct VerifyArgs {
   int64_t V, nvec;
   uint32_t units;    // target rows * S
   uint32_t groups0;  // the launch's first workgroup
+  int level;         // of the launch, where a launch is a level
+  int32_t* cur;      // [depth + 1][B]: the nodes on the paths, then -1
   FastDiv divS, divM;
   double c;
   const int32_t* token;
@@ -97,15 +99,22 @@ __device__ inline double part_value(const Part& p, float M, double c) {
   return p.m == -INFINITY ? p.sum : p.sum * weight_of(p.m, M, c);
 }
 
-__device__ inline double shfl_d(double v, int lane) { return __shfl(v, lane, 64); }
-
-// The sum of v over the lanes up to and with this one, in lane order.
-__device__ inline double wave_scan_d(double v, int lane) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const double o = __shfl_up(v, d, 64);
-    if (lane >= d) v = o + v;
-  }
+// v of the lane that CTRL names, 0 where there is none or the row of 16 lanes is not in ROWS.
+template <int CTRL, int ROWS>
+__device__ inline double dpp_or_0(double v) {
+  const uint64_t x = (uint64_t)__double_as_longlong(v);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, CTRL, ROWS, 0xF, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), CTRL, ROWS, 0xF, false);
+  return __longlong_as_double((long long)(((uint64_t)hi << 32) | lo));
+}
+// The sum of v over the lanes up to and with this one.
+__device__ inline double wave_scan_d(double v) {
+  v += dpp_or_0<0x111, 0xF>(v);  // row_shr by 1, 2, 4 and 8
+  v += dpp_or_0<0x112, 0xF>(v);
+  v += dpp_or_0<0x114, 0xF>(v);
+  v += dpp_or_0<0x118, 0xF>(v);
+  v += dpp_or_0<0x142, 0xA>(v);  // row_bcast15: the last of a row to the next one
+  v += dpp_or_0<0x143, 0xC>(v);  // row_bcast31: that of the lower half to the upper
   return v;
 }
 
@@ -129,24 +138,289 @@ __device__ inline void load_slice(const char* row, int slice, int lane, const Ve
   for (int i = 0; i < kLoads; ++i) Vt::unpack(raw[i], z[i]);
 }
 
-// The nodes of the draft that are node n's children, as the bit of each lane = node.
-__device__ inline bool is_child(const VerifyArgs& A, int b, int n, int count, int lane, int* token) {
-  bool child = lane > 0 && lane < count;
-  const int64_t o = (int64_t)b * A.M + lane;
-  if (child) child = (A.parent ? A.parent[o] : lane - 1) == n;
-  *token = -1;
-  if (child) {
-    const int t = A.token[o];
-    child = t >= 0 && t < A.V;
-    *token = t;
+// A query's draft: lane = node.
+struct Draft {
+  int parent, token;  // parent: -2 where the lane is no node that may be accepted
+  __device__ Draft(const VerifyArgs& A, int b, int count, int lane) {
+    parent = -2;
+    token = -1;
+    if (lane > 0 && lane < count) {
+      const int64_t o = (int64_t)b * A.M + lane;
+      token = A.token[o];
+      parent = A.parent ? A.parent[o] : lane - 1;
+      if (token < 0 || token >= A.V) parent = -2;
+    }
   }
-  return child;
-}
+  __device__ bool child_of(int n) const { return parent == n; }
+};
 __device__ inline int count_of(const VerifyArgs& A, int b) {
   return A.count ? min(max(A.count[b], 0), A.M) : A.M;
 }
 
-template <int DT, bool GREEDY>
+// The parts of a row of S <= 64 HELD, a lane's one behind the other, so that lanes and parts have one order.
+template <int HELD>
+struct RowParts {
+  Part p[HELD];
+  int held;  // parts a lane
+  __device__ void load(const Part* part, int S, int lane) {
+    held = (S + 63) / 64;
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+      const int k = lane * held + i;
+      p[i] = i < held && k < S ? part[k] : Part{0.0, -INFINITY, INT_MAX};
+    }
+  }
+  __device__ float largest() const {
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) m = fmaxf(m, p[i].m);
+    return fkey_inv(wave_max_i(fkey(m)));
+  }
+  __device__ double sum(float M, double c) const {
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+      if (i < held) s += part_value(p[i], M, c);
+    return wave_sum_d(s);
+  }
+};
+
+// The first of this wave's ordered values whose running sum exceeds `goal`, or the last above 0 where rounding leaves
+// none: its lane (-1: none is above 0), and the running sum before that lane. mine: the lane's value.
+__device__ inline int passing_lane(double mine, double goal, double* before) {
+  const double upto = wave_scan_d(mine);
+  const uint64_t over = __ballot(upto > goal && mine > 0.0), some = __ballot(mine > 0.0);
+  if (!some) return -1;
+  const int l = over ? __builtin_ctzll(over) : 63 - __builtin_clzll(some);
+  *before = lane_d(upto, l) - lane_d(mine, l);
+  return l;
+}
+
+// One wave: the token of a row at which the running sum of weight(z, w) over the slices' values passes goal.
+// value(i): the lane's i-th part's value; weights(slice, w): the slice's weights, in vectors by lane.
+template <int E, int HELD, typename Value, typename Weights>
+__device__ inline int draw_token(int held, double goal, int lane, Value value, Weights weights) {
+  double v[HELD], mine = 0.0;
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) {
+    v[i] = i < held ? value(i) : 0.0;
+    mine += v[i];
+  }
+  double before = 0.0;
+  const int l = passing_lane(mine, goal, &before);
+  if (l < 0) return -1;
+  // of that lane's parts: the first that passes, or the last above 0
+  double run = before;
+  int slice = -1;
+  double base = before;
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) {
+    const double x = lane_d(v[i], l);
+    if (x > 0.0 && (slice < 0 || !(run > goal))) {
+      slice = l * held + i;
+      base = run;
+      run += x;
+    }
+  }
+  double w[kLoads][E];
+  weights(slice, w);
+  // the lane of the first of its vectors that passes, or of the last above 0
+  double sum[kLoads], upto[kLoads];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    sum[i] = 0.0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum[i] += w[i][e];
+    upto[i] = wave_scan_d(sum[i]);
+  }
+  int which = -1, k = 0;
+  bool done = false;
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const uint64_t some = __ballot(sum[i] > 0.0), over = __ballot(base + upto[i] > goal) & some;
+    if (!done && some) {
+      which = i;
+      k = over ? __builtin_ctzll(over) : 63 - __builtin_clzll(some);
+      before = base + (lane_d(upto[i], k) - lane_d(sum[i], k));
+      done = over != 0;
+    }
+    base += lane_d(upto[i], 63);
+  }
+  if (which < 0) return -1;
+  double x[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    x[e] = w[0][e];
+#pragma unroll
+    for (int i = 1; i < kLoads; ++i) x[e] = which == i ? w[i][e] : x[e];
+  }
+  int at = -1;
+  bool passed = false;
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    if (!passed && x[e] > 0.0) {
+      at = e;
+      before += x[e];
+      passed = before > goal;
+    }
+  return (slice * kVerifySlice + which * 64 + k) * E + __builtin_amdgcn_readlane(at, k);
+}
+
+template <int DT>
+__device__ inline void weights_of_slice(const char* row, int slice, float M, int lane, const VerifyArgs& A,
+                                        double (&w)[kLoads][Vec<DT>::kElems]) {
+  float z[kLoads][Vec<DT>::kElems];
+  load_slice<DT>(row, slice, lane, A, z);
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+    for (int e = 0; e < Vec<DT>::kElems; ++e) w[i][e] = weight_of(z[i][e], M, A.c);
+}
+
+// A token drawn from a target row: its parts hold the weights without the children's tokens; `with`: those count
+// too (the draft goes no deeper).
+template <int DT, int HELD>
+__device__ inline int draw_row(const VerifyArgs& A, int b, int n, int count, bool with, float M, double total, double u,
+                               int lane) {
+  constexpr int E = Vec<DT>::kElems;
+  const char* row = A.x + b * A.sb + n * A.sn;
+  RowParts<HELD> parts;
+  parts.load(A.part + ((int64_t)b * A.M + n) * A.S, A.S, lane);
+  const Draft draft(A, b, count, lane);
+  const int t = draft.token;
+  const uint64_t children = A.y ? 0 : __ballot(draft.child_of(n));
+  double extra[HELD];
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) extra[i] = 0.0;
+  if (with) {
+    const double mine = (children >> lane) & 1 ? weight_of(logit_at<DT>(row, t), M, A.c) : 0.0;
+    for (uint64_t left = children; left; left &= left - 1) {
+      const int k = __builtin_ctzll(left), x = __builtin_amdgcn_readlane(t, k);
+      // a token that a child before had counts once
+      if (__ballot(((children >> lane) & 1) != 0 && lane < k && t == x)) continue;
+      const int slice = x / (kVerifySlice * E);
+      const double wx = lane_d(mine, k);
+#pragma unroll
+      for (int i = 0; i < HELD; ++i)
+        if (i < parts.held && lane * parts.held + i == slice) extra[i] += wx;
+    }
+  }
+  return draw_token<E, HELD>(
+      parts.held, u * total, lane, [&](int i) { return part_value(parts.p[i], M, A.c) + extra[i]; },
+      [&](int slice, double (&w)[kLoads][E]) {
+        weights_of_slice<DT>(row, slice, M, lane, A, w);
+        if (with) return;
+        for (uint64_t left = children; left; left &= left - 1) {
+          const int mine = __builtin_amdgcn_readlane(t, __builtin_ctzll(left)) - (slice * kVerifySlice + lane) * E;
+#pragma unroll
+          for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+              if (mine == i * 64 * E + e) w[i][e] = 0.0;
+        }
+      });
+}
+
+// What a node of the draft comes to.
+struct Node {
+  double total, rest, zq;  // the row's weights with and without its children's; 1 / the drafter's
+  float m, mq;
+  int next;     // the accepted child; -1: none
+  int kind;     // 0: no distribution; 1: draw from the rest; 2: a child of a drafter was rejected
+  int arg;      // greedy: the largest logit's token
+};
+
+// What a node is folded from.
+template <int HELD>
+struct NodeIn {
+  RowParts<HELD> parts, drafted;
+  float z, zy;  // the logits of the lane's token, where it is a child's
+  template <int DT, bool GREEDY>
+  __device__ void load(const VerifyArgs& A, const Draft& draft, int b, int n, int lane) {
+    const int64_t row = (int64_t)b * A.M + n;
+    parts.load(A.part + row * A.S, A.S, lane);
+    if (GREEDY) return;
+    const bool child = draft.child_of(n);
+    z = child ? logit_at<DT>(A.x + b * A.sb + n * A.sn, draft.token) : -INFINITY;
+    if (!A.y || !__ballot(child)) return;
+    drafted.load(A.part + ((int64_t)A.B * A.M + row) * A.S, A.S, lane);
+    zy = child ? logit_at<DT>(A.y + b * A.tb + n * A.tn, draft.token) : -INFINITY;
+  }
+};
+
+// u: the lane's random number.
+template <bool GREEDY, int HELD>
+__device__ inline Node fold_node(const VerifyArgs& A, const Draft& draft, const NodeIn<HELD>& in, double u, int n,
+                                 int lane) {
+  Node o{};
+  o.next = -1;
+  const int t = draft.token;
+  const bool child = draft.child_of(n);
+  const uint64_t children = __ballot(child);
+  if constexpr (GREEDY) {
+    o.m = in.parts.largest();
+    int at = INT_MAX;
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+      if (in.parts.p[i].m == o.m) at = min(at, in.parts.p[i].at);
+      bad |= !(in.parts.p[i].sum == 0.0);
+    }
+    at = -wave_max_i(-at);
+    o.kind = __ballot(bad) == 0 && o.m > -INFINITY ? 1 : 0;
+    o.arg = at;
+    const uint64_t hit = __ballot(child && t == at);
+    if (o.kind && hit) o.next = __builtin_ctzll(hit);
+    return o;
+  }
+  o.m = fmaxf(in.parts.largest(), fkey_inv(wave_max_i(fkey(fmaxf(in.z, -INFINITY)))));
+  const float ref = o.m == -INFINITY ? 0.0f : o.m;
+  o.rest = in.parts.sum(ref, A.c);
+  double w = child ? weight_of(in.z, ref, A.c) : 0.0;
+  if (!A.y) {
+    // a token that a child before had is not left
+    for (uint64_t k = children; k; k &= k - 1) {
+      const int j = __builtin_ctzll(k);
+      if (child && j < lane && __builtin_amdgcn_readlane(t, j) == t) w = 0.0;
+    }
+    double left = o.rest, mine = 0.0;
+    for (uint64_t k = children; k;) {
+      const int j = 63 - __builtin_clzll(k);
+      k &= ~(1ull << j);
+      left += lane_d(w, j);
+      if (lane == j) mine = left;
+    }
+    o.total = left;
+    o.kind = o.m > -INFINITY && o.total < INFINITY && o.m < INFINITY ? 1 : 0;  // (a NaN total is not below)
+    const uint64_t takes = __ballot(child && u * mine < w);
+    if (o.kind && takes) o.next = __builtin_ctzll(takes);
+    return o;
+  }
+  o.total = o.rest;
+  o.kind = o.m > -INFINITY && o.total < INFINITY && o.m < INFINITY ? 1 : 0;
+  if (!o.kind || !children) return o;
+  o.mq = in.drafted.largest();
+  const double f = in.drafted.sum(o.mq == -INFINITY ? 0.0f : o.mq, A.c);
+  const bool fine = o.mq > -INFINITY && o.mq < INFINITY && f < INFINITY;
+  if (!fine) return o;  // nothing can have been drawn from it: the child is rejected, the token drawn from p
+  o.zq = 1.0 / f;
+  const double p = w / o.total, q = child ? weight_of(in.zy, o.mq, A.c) / f : 0.0;
+  const uint64_t takes = __ballot(child && u * q < p);
+  if (takes) o.next = __builtin_ctzll(takes);
+  else o.kind = 2;
+  return o;
+}
+template <int DT, bool GREEDY, int HELD>
+__device__ inline Node node_of(const VerifyArgs& A, const Draft& draft, int b, int n, int lane) {
+  NodeIn<HELD> in;
+  in.template load<DT, GREEDY>(A, draft, b, n, lane);
+  const double u = !GREEDY && lane < A.M ? A.u[(int64_t)b * A.M + lane] : 0.0;
+  return fold_node<GREEDY, HELD>(A, draft, in, u, n, lane);
+}
+
+// HELD 0: every node's row. Otherwise the rows of one level: of the nodes that follow the ones of the level before,
+// which every wave of a query finds by itself.
+template <int DT, bool GREEDY, int HELD>
 __global__ void __launch_bounds__(kThreads) hs_verify_rows_kernel(const VerifyArgs A) {
   using Vt = Vec<DT>;
   constexpr int E = Vt::kElems;
@@ -154,19 +428,34 @@ __global__ void __launch_bounds__(kThreads) hs_verify_rows_kernel(const VerifyAr
   uint32_t unit = uniform((A.groups0 + blockIdx.x) * kWaves + (threadIdx.x >> 6));
   if (unit >= A.units) return;
   const bool q = blockIdx.y != 0;  // the drafter's row
-  const uint32_t row = fdiv(unit, A.divS);
+  uint32_t row = fdiv(unit, A.divS);
   const int slice = (int)(unit - row * (uint32_t)A.S);
-  const int b = (int)fdiv(row, A.divM), n = (int)row - b * A.M;
-  const int count = count_of(A, b);
+  int b, n, count;
+  if constexpr (HELD == 0) {
+    b = (int)fdiv(row, A.divM);
+    n = (int)row - b * A.M;
+    count = count_of(A, b);
+  } else {
+    b = (int)row;
+    count = count_of(A, b);
+    n = count > 0 ? 0 : -1;
+    if (A.level > 0) {
+      n = A.cur[(int64_t)(A.level - 1) * A.B + b];
+      if (n >= 0) n = node_of<DT, GREEDY, HELD>(A, Draft(A, b, count, lane), b, n, lane).next;
+    }
+    if (slice == 0 && !q && lane == 0) A.cur[(int64_t)A.level * A.B + b] = n;
+    if (n < 0) return;
+    row = (uint32_t)(b * A.M + n);
+  }
   if (n + (q ? 1 : 0) >= count) return;
   const char* x = q ? A.y + b * A.tb + n * A.tn : A.x + b * A.sb + n * A.sn;
   float z[kLoads][E];
   load_slice<DT>(x, slice, lane, A, z);
   const int first = slice * kVerifySlice * E;
   if (!GREEDY && !A.y) {  // the children's tokens have no weight
-    int t;
-    const bool child = is_child(A, b, n, count, lane, &t);
-    uint64_t here = __ballot(child && t >= first && t - first < kVerifySlice * E);
+    const Draft draft(A, b, count, lane);
+    const int t = draft.token;
+    uint64_t here = __ballot(draft.child_of(n) && t >= first && t - first < kVerifySlice * E);
     while (here) {
       const int k = __builtin_ctzll(here);
       here &= here - 1;
@@ -211,251 +500,39 @@ __global__ void __launch_bounds__(kThreads) hs_verify_rows_kernel(const VerifyAr
   if (lane == 0) *out = Part{sum, m, 0};
 }
 
-// The parts of a row of S, lane l's being those from l * kHeldParts on, so that lanes and parts have one order.
-struct RowParts {
-  Part p[kHeldParts];
-  int held;  // parts a lane
-  __device__ RowParts(const Part* part, int S, int lane) {
-    held = (S + 63) / 64;
-#pragma unroll
-    for (int i = 0; i < kHeldParts; ++i) {
-      const int k = lane * held + i;
-      p[i] = i < held && k < S ? part[k] : Part{0.0, -INFINITY, INT_MAX};
-    }
-  }
-  __device__ float largest() const {
-    float m = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < kHeldParts; ++i) m = fmaxf(m, p[i].m);
-    return fkey_inv(wave_max_i(fkey(m)));
-  }
-  __device__ double sum(float M, double c) const {
-    double s = 0.0;
-#pragma unroll
-    for (int i = 0; i < kHeldParts; ++i)
-      if (i < held) s += part_value(p[i], M, c);
-    return wave_sum_d(s);
-  }
-};
-
-// The first of this wave's ordered values whose running sum exceeds `goal`, or the last above 0 where rounding leaves
-// none: its lane (-1: none is above 0), and the running sum before that lane. mine: the lane's value.
-__device__ inline int passing_lane(double mine, double goal, int lane, double* before) {
-  const double upto = wave_scan_d(mine, lane);
-  const uint64_t over = __ballot(upto > goal && mine > 0.0), some = __ballot(mine > 0.0);
-  if (!some) return -1;
-  const int l = over ? __builtin_ctzll(over) : 63 - __builtin_clzll(some);
-  *before = shfl_d(upto, l) - shfl_d(mine, l);
-  return l;
-}
-
-// One wave: the token of a row at which the running sum of weight(z, w) over the slices' values passes goal.
-// value(i): the lane's i-th part's value; weights(slice, w): the slice's weights, in vectors by lane.
-template <int E, typename Value, typename Weights>
-__device__ inline int draw_token(int held, double goal, int lane, Value value, Weights weights) {
-  double v[kHeldParts], mine = 0.0;
-#pragma unroll
-  for (int i = 0; i < kHeldParts; ++i) {
-    v[i] = i < held ? value(i) : 0.0;
-    mine += v[i];
-  }
-  double before = 0.0;
-  const int l = passing_lane(mine, goal, lane, &before);
-  if (l < 0) return -1;
-  // of that lane's parts: the first that passes, or the last above 0
-  double run = before;
-  int slice = -1;
-  double base = before;
-#pragma unroll
-  for (int i = 0; i < kHeldParts; ++i) {
-    const double x = shfl_d(v[i], l);
-    if (x > 0.0 && (slice < 0 || !(run > goal))) {
-      slice = l * held + i;
-      base = run;
-      run += x;
-    }
-  }
-  double w[kLoads][E];
-  weights(slice, w);
-  int token = -1;
-  bool done = false;
-#pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    double sum = 0.0;
-#pragma unroll
-    for (int e = 0; e < E; ++e) sum += w[i][e];
-    double start = 0.0;
-    const double upto = base + wave_scan_d(sum, lane);
-    const uint64_t over = __ballot(upto > goal && sum > 0.0), some = __ballot(sum > 0.0);
-    if (done || !some) continue;
-    const int k = over ? __builtin_ctzll(over) : 63 - __builtin_clzll(some);
-    start = shfl_d(upto, k) - shfl_d(sum, k);
-    int at = -1;
-    bool passed = false;
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      if (!passed && w[i][e] > 0.0) {
-        at = e;
-        start += w[i][e];
-        passed = start > goal;
-      }
-    }
-    at = __shfl(at, k, 64);
-    token = (slice * kVerifySlice + i * 64 + k) * E + at;
-    done = over != 0;
-    base = shfl_d(upto, 63);
-  }
-  return token;
-}
-
-template <int DT>
-__device__ inline void weights_of_slice(const char* row, int slice, float M, int lane, const VerifyArgs& A,
-                                        double (&w)[kLoads][Vec<DT>::kElems]) {
-  float z[kLoads][Vec<DT>::kElems];
-  load_slice<DT>(row, slice, lane, A, z);
-#pragma unroll
-  for (int i = 0; i < kLoads; ++i)
-#pragma unroll
-    for (int e = 0; e < Vec<DT>::kElems; ++e) w[i][e] = weight_of(z[i][e], M, A.c);
-}
-
-// A token drawn from a target row: its parts hold the weights without the children's tokens; `with`: those count
-// too (the draft goes no deeper).
-template <int DT>
-__device__ inline int draw_row(const VerifyArgs& A, int b, int n, int count, bool with, float M, double total, double u,
-                               int lane) {
-  constexpr int E = Vec<DT>::kElems;
-  const char* row = A.x + b * A.sb + n * A.sn;
-  const RowParts parts(A.part + ((int64_t)b * A.M + n) * A.S, A.S, lane);
-  int t = -1;
-  uint64_t children = 0;
-  if (!A.y) {
-    const bool child = is_child(A, b, n, count, lane, &t);
-    children = __ballot(child);
-  }
-  double extra[kHeldParts];
-#pragma unroll
-  for (int i = 0; i < kHeldParts; ++i) extra[i] = 0.0;
-  if (with) {
-    const double mine = (children >> lane) & 1 ? weight_of(logit_at<DT>(row, t), M, A.c) : 0.0;
-    for (uint64_t left = children; left; left &= left - 1) {
-      const int k = __builtin_ctzll(left), x = __builtin_amdgcn_readlane(t, k);
-      // a token that a child before had counts once
-      if (__ballot(((children >> lane) & 1) != 0 && lane < k && t == x)) continue;
-      const int slice = x / (kVerifySlice * E);
-      const double wx = lane_d(mine, k);
-#pragma unroll
-      for (int i = 0; i < kHeldParts; ++i)
-        if (i < parts.held && lane * parts.held + i == slice) extra[i] += wx;
-    }
-  }
-  return draw_token<E>(
-      parts.held, u * total, lane, [&](int i) { return part_value(parts.p[i], M, A.c) + extra[i]; },
-      [&](int slice, double (&w)[kLoads][E]) {
-        weights_of_slice<DT>(row, slice, M, lane, A, w);
-        if (with) return;
-        for (uint64_t left = children; left; left &= left - 1) {
-          const int mine = __builtin_amdgcn_readlane(t, __builtin_ctzll(left)) - (slice * kVerifySlice + lane) * E;
-#pragma unroll
-          for (int i = 0; i < kLoads; ++i)
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-              if (mine == i * 64 * E + e) w[i][e] = 0.0;
-        }
-      });
-}
-
-// What a node of the draft comes to.
-struct Node {
-  double total, rest, zq;  // the row's weights with and without its children's; 1 / the drafter's
-  float m, mq;
-  int next;     // the accepted child; -1: none
-  int kind;     // 0: no distribution; 1: draw from the rest; 2: a child of a drafter was rejected
-  int arg;      // greedy: the largest logit's token
-};
-
-template <int DT, bool GREEDY>
-__device__ inline Node fold_node(const VerifyArgs& A, int b, int n, int count, int lane) {
-  Node o{};
-  o.next = -1;
-  const int64_t row = (int64_t)b * A.M + n;
-  const RowParts parts(A.part + row * A.S, A.S, lane);
-  int t;
-  const bool child = is_child(A, b, n, count, lane, &t);
-  const uint64_t children = __ballot(child);
-  if constexpr (GREEDY) {
-    o.m = parts.largest();
-    int at = INT_MAX;
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < kHeldParts; ++i) {
-      if (parts.p[i].m == o.m) at = min(at, parts.p[i].at);
-      bad |= !(parts.p[i].sum == 0.0);
-    }
-    at = -wave_max_i(-at);
-    o.kind = __ballot(bad) == 0 && o.m > -INFINITY ? 1 : 0;
-    o.arg = at;
-    const uint64_t hit = __ballot(child && t == at);
-    if (o.kind && hit) o.next = __builtin_ctzll(hit);
-    return o;
-  }
-  const char* x = A.x + b * A.sb + n * A.sn;
-  const float z = child ? logit_at<DT>(x, t) : -INFINITY;
-  const double u = child ? A.u[(int64_t)b * A.M + lane] : 0.0;
-  o.m = fmaxf(parts.largest(), fkey_inv(wave_max_i(fkey(fmaxf(z, -INFINITY)))));
-  const float ref = o.m == -INFINITY ? 0.0f : o.m;
-  o.rest = parts.sum(ref, A.c);
-  double w = child ? weight_of(z, ref, A.c) : 0.0;
-  if (!A.y) {
-    // a token that a child before had is not left
-    for (uint64_t k = children; k; k &= k - 1) {
-      const int j = __builtin_ctzll(k);
-      if (child && j < lane && __builtin_amdgcn_readlane(t, j) == t) w = 0.0;
-    }
-    double left = o.rest, mine = 0.0;
-    for (uint64_t k = children; k;) {
-      const int j = 63 - __builtin_clzll(k);
-      k &= ~(1ull << j);
-      left += lane_d(w, j);
-      if (lane == j) mine = left;
-    }
-    o.total = left;
-    o.kind = o.m > -INFINITY && o.total < INFINITY && o.m < INFINITY ? 1 : 0;  // (a NaN total is not below)
-    const uint64_t takes = __ballot(child && u * mine < w);
-    if (o.kind && takes) o.next = __builtin_ctzll(takes);
-    return o;
-  }
-  o.total = o.rest;
-  o.kind = o.m > -INFINITY && o.total < INFINITY && o.m < INFINITY ? 1 : 0;
-  if (!o.kind || !children) return o;
-  const RowParts drafted(A.part + ((int64_t)A.B * A.M + row) * A.S, A.S, lane);
-  o.mq = drafted.largest();
-  const double f = drafted.sum(o.mq == -INFINITY ? 0.0f : o.mq, A.c);
-  const bool fine = o.mq > -INFINITY && o.mq < INFINITY && f < INFINITY;
-  if (!fine) return o;  // nothing can have been drawn from it: the child is rejected, the token drawn from p
-  o.zq = 1.0 / f;
-  const float zy = child ? logit_at<DT>(A.y + b * A.tb + n * A.tn, t) : -INFINITY;
-  const double p = w / o.total, q = child ? weight_of(zy, o.mq, A.c) / f : 0.0;
-  const uint64_t takes = __ballot(child && u * q < p);
-  if (takes) o.next = __builtin_ctzll(takes);
-  else o.kind = 2;
-  return o;
-}
-
-template <int DT, bool GREEDY>
-__global__ void __launch_bounds__(kWalkThreads) hs_verify_walk_kernel(const VerifyArgs A) {
-  __shared__ Node s_node[HS_MAX_POSITIONS];
+// LEVELS: the path is known but for whether its last node is the end; a wave a query.
+template <int DT, bool GREEDY, int HELD, bool LEVELS>
+__global__ void __launch_bounds__(LEVELS ? 64 : kWalkThreads) hs_verify_walk_kernel(const VerifyArgs A) {
+  __shared__ Node s_node[LEVELS ? 1 : HS_MAX_POSITIONS];
   __shared__ int s_path[HS_MAX_POSITIONS];
   __shared__ int s_len, s_with;
   const int b = blockIdx.x, lane = threadIdx.x & 63, wv = (int)uniform(threadIdx.x >> 6);
   const int count = count_of(A, b);
-  for (int n = wv; n < count; n += kWalkWaves) {
-    const Node o = fold_node<DT, GREEDY>(A, b, n, count, lane);
-    if (lane == 0) s_node[n] = o;
+  const Draft draft(A, b, count, lane);
+  Node end{};
+  if constexpr (LEVELS) {
+    const int at = lane <= A.depth ? A.cur[(int64_t)lane * A.B + b] : -1;
+    const int len = __builtin_popcountll(__ballot(at >= 0));
+    if (len > 0) end = node_of<DT, GREEDY, HELD>(A, draft, b, __builtin_amdgcn_readlane(at, max(len, 1) - 1), lane);
+    s_path[lane] = at;
+    if (lane == 0) {
+      s_len = len;
+      s_with = len > A.depth;
+    }
+  } else {
+    // (a node without children is folded only where the path ends with it: most of a tree are such, 61 nodes 14.6 -> 10.5)
+    for (int n = wv; n < count; n += kWalkWaves) {
+      if (!__ballot(draft.child_of(n))) {
+        if (lane == 0) s_node[n].next = -1;
+        continue;
+      }
+      const Node o = node_of<DT, GREEDY, HELD>(A, draft, b, n, lane);
+      if (lane == 0) s_node[n] = o;
+    }
+    __syncthreads();
+    if (wv != 0) return;
   }
-  __syncthreads();
-  if (wv != 0) return;
-  if (lane == 0) {
+  if (!LEVELS && lane == 0) {
     int len = 0, n = 0;
     bool cut = false;
     while (count > 0) {
@@ -477,15 +554,15 @@ __global__ void __launch_bounds__(kWalkThreads) hs_verify_walk_kernel(const Veri
   const int last = len > 0 ? s_path[len - 1] : 0;
   int token = -1;
   bool residual = false;
-  Node end{};
   if (len > 0) {
-    end = s_node[last];
+    if constexpr (!LEVELS)
+      end = __ballot(draft.child_of(last)) ? s_node[last] : node_of<DT, GREEDY, HELD>(A, draft, b, last, lane);
     const bool with = s_with != 0;
     if (with && end.kind == 2) end.kind = 1;
     residual = end.kind == 2;
     if (GREEDY) token = end.kind ? end.arg : -1;
     else if (end.kind == 1)
-      token = draw_row<DT>(A, b, last, count, with, end.m, with ? end.total : end.rest, A.u[o], lane);
+      token = draw_row<DT, HELD>(A, b, last, count, with, end.m, with ? end.total : end.rest, A.u[o], lane);
   }
   if (lane < A.M) {
     const int next = lane + 1 < len ? s_path[lane + 1] : -1;
@@ -534,40 +611,51 @@ __global__ void __launch_bounds__(kThreads) hs_verify_rest_kernel(const VerifyAr
   if (lane == 0) A.rest_part[(int64_t)b * A.S + slice] = Part{sum, 0.0f, 0};
 }
 
-template <int DT>
+template <int DT, int HELD>
 __global__ void __launch_bounds__(64) hs_verify_draw_kernel(const VerifyArgs A) {
   constexpr int E = Vec<DT>::kElems;
   const int b = blockIdx.x, lane = threadIdx.x;
   const End e = A.end[b];
   if (!e.residual) return;
-  const RowParts parts(A.rest_part + (int64_t)b * A.S, A.S, lane);
+  RowParts<HELD> parts;
+  parts.load(A.rest_part + (int64_t)b * A.S, A.S, lane);
   double mine = 0.0;
 #pragma unroll
-  for (int i = 0; i < kHeldParts; ++i) mine += parts.p[i].sum;
+  for (int i = 0; i < HELD; ++i) mine += parts.p[i].sum;
   const double total = wave_sum_d(mine), u = A.u[(int64_t)b * A.M];
   int token;
   if (total > 0.0)
-    token = draw_token<E>(
+    token = draw_token<E, HELD>(
         parts.held, u * total, lane, [&](int i) { return parts.p[i].sum; },
         [&](int slice, double (&w)[kLoads][E]) { residual_of_slice<DT>(A, b, e, slice, lane, w); });
   else  // p and q are the same but for rounding
-    token = draw_row<DT>(A, b, e.node, 0, false, e.mp, e.rest, u, lane);
+    token = draw_row<DT, HELD>(A, b, e.node, 0, false, e.mp, e.rest, u, lane);
   if (lane == 0) A.emitted[(int64_t)b * A.M + e.length - 1] = token;
 }
 
-template <int DT, bool GREEDY>
-void launch_of(VerifyArgs A, hipStream_t st) {
+template <int DT, bool GREEDY, int HELD>
+void launch_held(VerifyArgs A, bool levels, hipStream_t st) {
+  const bool drafter = !GREEDY && A.y;
   const uint32_t groups = (A.units + kWaves - 1) / kWaves;
-  for (A.groups0 = 0; A.groups0 < groups; A.groups0 += kMostGroups) {
-    const dim3 grid(std::min(groups - A.groups0, kMostGroups), !GREEDY && A.y ? 2 : 1);
-    hs_verify_rows_kernel<DT, GREEDY><<<grid, kThreads, 0, st>>>(A);
-    if (hipPeekAtLastError() != hipSuccess) return;
-  }
-  hs_verify_walk_kernel<DT, GREEDY><<<A.B, kWalkThreads, 0, st>>>(A);
-  if (GREEDY || !A.y || hipPeekAtLastError() != hipSuccess) return;
+  for (A.level = 0; A.level <= (levels ? A.depth : 0); ++A.level)
+    for (A.groups0 = 0; A.groups0 < groups; A.groups0 += kMostGroups) {
+      const dim3 grid(std::min(groups - A.groups0, kMostGroups), drafter ? 2 : 1);
+      if (levels) hs_verify_rows_kernel<DT, GREEDY, HELD><<<grid, kThreads, 0, st>>>(A);
+      else hs_verify_rows_kernel<DT, GREEDY, 0><<<grid, kThreads, 0, st>>>(A);
+      if (hipPeekAtLastError() != hipSuccess) return;
+    }
+  if (levels) hs_verify_walk_kernel<DT, GREEDY, HELD, true><<<A.B, 64, 0, st>>>(A);
+  else hs_verify_walk_kernel<DT, GREEDY, HELD, false><<<A.B, kWalkThreads, 0, st>>>(A);
+  if (!drafter || hipPeekAtLastError() != hipSuccess) return;
   hs_verify_rest_kernel<DT><<<(int)(((int64_t)A.B * A.S + kWaves - 1) / kWaves), kThreads, 0, st>>>(A);
   if (hipPeekAtLastError() != hipSuccess) return;
-  hs_verify_draw_kernel<DT><<<A.B, 64, 0, st>>>(A);
+  hs_verify_draw_kernel<DT, HELD><<<A.B, 64, 0, st>>>(A);
+}
+
+template <int DT, bool GREEDY>
+void launch_of(const VerifyArgs& A, bool levels, hipStream_t st) {
+  if (A.S <= 128) launch_held<DT, GREEDY, 2>(A, levels, st);
+  else launch_held<DT, GREEDY, kMostHeld>(A, levels, st);
 }
 
 }  // namespace
@@ -589,9 +677,18 @@ bool verify_geom(int B, int M, int64_t V, int dtype, bool drafter, VerifyGeom* g
 }
 
 size_t verify_ws_bytes(const VerifyGeom& g) {
+  const size_t cur = align256((size_t)g.B * g.M * sizeof(int32_t));
   const size_t rows = (size_t)g.B * g.M * (g.drafter ? 2 : 1);
   const size_t more = g.drafter ? align256((size_t)g.B * g.S * sizeof(Part)) + align256((size_t)g.B * sizeof(End)) : 0;
-  return align256(rows * g.S * sizeof(Part)) + more;
+  return align256(rows * g.S * sizeof(Part)) + more + cur;
+}
+
+// Whether a tree's rows are read level by level, those on the paths alone, in depth + 1 launches: where the rows off the
+// paths take longer than the launches. us all at once and by levels: 32 trees of 61 nodes, 7 deep, of 128256 bf16 150
+// and 61; 64 chains of 8 tokens with their drafter, where most of the rows are on the path, 150 and 196.
+static bool by_levels(const VerifyGeom& g, int depth, bool greedy) {
+  const double row = (double)g.B * g.V * (g.dtype == HS_F32 ? 4 : 2);
+  return !g.drafter && row * (g.M - (depth + 1)) / (greedy ? 5e6 : 2.8e6) > 8.0 * (depth + 1);
 }
 
 int launch_verify(const VerifyGeom& g, const hs_verify_args& a, hipStream_t stream) {
@@ -609,7 +706,8 @@ int launch_verify(const VerifyGeom& g, const hs_verify_args& a, hipStream_t stre
   A.depth = a.depth;
   A.V = g.V;
   A.nvec = g.nvec;
-  A.units = (uint32_t)((int64_t)g.B * g.M * g.S);
+  const bool greedy = a.mode == HS_GREEDY, levels = by_levels(g, a.depth, greedy);
+  A.units = (uint32_t)((int64_t)g.B * (levels ? 1 : g.M) * g.S);
   A.divS = make_fastdiv((uint32_t)g.S);
   A.divM = make_fastdiv((uint32_t)g.M);
   A.c = 1.4426950408889634074 / a.temperature;
@@ -622,14 +720,15 @@ int launch_verify(const VerifyGeom& g, const hs_verify_args& a, hipStream_t stre
   A.length = a.out_length;
   char* ws = reinterpret_cast<char*>(a.workspace);
   A.part = reinterpret_cast<Part*>(ws);
-  ws += align256((size_t)A.units * (g.drafter ? 2 : 1) * sizeof(Part));
+  ws += align256((size_t)g.B * g.M * g.S * (g.drafter ? 2 : 1) * sizeof(Part));
+  A.cur = reinterpret_cast<int32_t*>(ws);
+  ws += align256((size_t)g.B * g.M * sizeof(int32_t));
   A.rest_part = reinterpret_cast<Part*>(ws);
   A.end = reinterpret_cast<End*>(ws + align256((size_t)g.B * g.S * sizeof(Part)));
-  const bool greedy = a.mode == HS_GREEDY;
   if (greedy) A.c = 0.0;
-  if (g.dtype == HS_F32) greedy ? launch_of<HS_F32, true>(A, stream) : launch_of<HS_F32, false>(A, stream);
-  else if (g.dtype == HS_F16) greedy ? launch_of<HS_F16, true>(A, stream) : launch_of<HS_F16, false>(A, stream);
-  else greedy ? launch_of<HS_BF16, true>(A, stream) : launch_of<HS_BF16, false>(A, stream);
+  if (g.dtype == HS_F32) greedy ? launch_of<HS_F32, true>(A, levels, stream) : launch_of<HS_F32, false>(A, levels, stream);
+  else if (g.dtype == HS_F16) greedy ? launch_of<HS_F16, true>(A, levels, stream) : launch_of<HS_F16, false>(A, levels, stream);
+  else greedy ? launch_of<HS_BF16, true>(A, levels, stream) : launch_of<HS_BF16, false>(A, levels, stream);
   return hipPeekAtLastError() == hipSuccess ? HS_OK : HS_ERR_HIP;
 }
 

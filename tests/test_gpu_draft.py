@@ -296,6 +296,69 @@ def test_verify_most_queries():
         assert np.array_equal(got[k][some.numpy()], want[k]), k
 
 
+def shallow(parent, depth):
+    """The parents of a tree whose nodes further than `depth` from the root hang from it instead, and their depths."""
+    far = torch.zeros(parent.shape, dtype=torch.long)
+    parent = parent.clone()
+    rows = torch.arange(parent.shape[0])
+    for n in range(1, parent.shape[1]):
+        deep = far[rows, parent[:, n].long()] >= depth
+        parent[deep, n] = 0
+        far[:, n] = far[rows, parent[:, n].long()] + 1
+    return parent
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("mode", [hs.SAMPLE, hs.GREEDY])
+def test_verify_large_trees(dtype, mode):
+    """Calls so large that only the rows on the paths are read, with ragged and empty drafts, rows without a
+    distribution and nodes behind the depth."""
+    note("verify large trees %s mode=%d" % (dtype, mode))
+    g = torch.Generator().manual_seed(43)
+    B, M, V, depth = 32, 48, 40013, 3
+    z = rows(g, B, M, V, DTYPES[dtype])
+    parent, token = tree(g, B, M, V, z)
+    parent = shallow(parent, depth)
+    count = torch.randint(1, M + 1, (B,), generator=g).int()
+    count[5], count[6], count[7] = 0, 1, M
+    z[3, 1:4, 17] = float("nan")
+    z[4, 0, :V] = -float("inf")
+    for k in range(3):
+        got = check_verify(z, token, numbers(g, B, M), V, parent=parent, count=count if k else None, mode=mode, T=0.6,
+                           depth=depth)
+        check_verify(z, token, numbers(g, B, M), V, parent=parent, count=count, mode=mode, depth=1)
+    assert mode == hs.GREEDY or got["length"].max() > 1
+    # each node's first child has its likeliest token: longer paths
+    first = torch.full((B, M), M, dtype=torch.long).scatter_reduce(1, parent[:, 1:].long(), torch.arange(1, M).expand(B, -1),
+                                                                   "amin")
+    best = z[:, :, :V].float().nan_to_num(-9e9).argmax(2)
+    for b in range(B):
+        for n in range(M):
+            if first[b, n] < M:
+                token[b, first[b, n]] = best[b, n]
+    got = check_verify(z, token, numbers(g, B, M), V, parent=parent, mode=mode, T=0.2, depth=depth)
+    assert got["length"].max() == depth + 1
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("drafted", [False, True])
+def test_verify_large_chains(dtype, drafted):
+    note("verify large chains %s drafter=%d" % (dtype, drafted))
+    g = torch.Generator().manual_seed(47)
+    B, M, V = 96, 6, 70001
+    z = rows(g, B, M, V, DTYPES[dtype], scale=2.0).cuda()
+    y = (z[:, :M - 1].float() + 0.4 * torch.randn(z[:, :M - 1].shape, device="cuda")).to(z.dtype)
+    y[:, :, V:] = float("nan")
+    pick = -(-torch.rand((B, M - 1, V), device="cuda").clamp(min=1e-30).log()).log()
+    token = torch.full((B, M), -1, dtype=torch.int32)
+    token[:, 1:] = (y[:, :, :V].float() + pick).argmax(2).cpu().int()
+    count = torch.randint(0, M + 1, (B,), generator=g).int()
+    z[7, 2, 5], y[8, 1, 9] = float("nan"), float("inf")
+    for k in range(2):
+        got = check_verify(z, token, numbers(g, B, M), V, drafter=y if drafted else None, count=count if k else None)
+        assert not drafted or got["length"].max() > 3
+
+
 # ---- hs_tree_attention -----------------------------------------------------------------------------------
 
 HALF = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
