@@ -29,12 +29,16 @@ struct AppendArgs {
 };
 
 constexpr float kTop = 448.0f;
+constexpr int kHold = 2;                     // squares of a thread that stay in registers
+constexpr int kSlab = 64;                  // dims of a page's values that are in LDS at once
+constexpr int kPitch = HS_MAX_PAGE / 4 + 1;  // words of a dim
 constexpr uint32_t kNan8 = 0x7F;
 
-template <bool F16>
-__device__ inline void unpack8(const uint4& r, float (&z)[8]) {
-  Vec16<F16>::unpack(r, z);
-}
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef short i16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
 __device__ inline bool finite(float x) { return (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u; }
 
 // Four values as codes, the first in the low byte.
@@ -56,6 +60,43 @@ __device__ inline uint32_t rescaled(uint32_t u, float f) {
   return codes_of(y);
 }
 
+// Eight values as codes of x / now, now a power of two, |x| <= 448 now.
+template <bool F16>
+__device__ inline uint2 plain_codes(const uint4& r, float now) {
+  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+  i16x2 y[2] = {};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if constexpr (F16) {
+      y[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(y[i], __builtin_bit_cast(f16x2, w[2 * i]), now, false);
+      y[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(y[i], __builtin_bit_cast(f16x2, w[2 * i + 1]), now, true);
+    } else {
+      y[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(y[i], __builtin_bit_cast(bf16x2, w[2 * i]), now, false);
+      y[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(y[i], __builtin_bit_cast(bf16x2, w[2 * i + 1]), now, true);
+    }
+  }
+  return make_uint2(__builtin_bit_cast(uint32_t, y[0]), __builtin_bit_cast(uint32_t, y[1]));
+}
+
+// Four words of four bytes, bytes and words exchanged.
+__device__ inline void transpose4(uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t* u) {
+  const uint32_t ab = __builtin_amdgcn_perm(b, a, 0x05010400u), cd = __builtin_amdgcn_perm(d, c, 0x05010400u);
+  const uint32_t AB = __builtin_amdgcn_perm(b, a, 0x07030602u), CD = __builtin_amdgcn_perm(d, c, 0x07030602u);
+  u[0] = __builtin_amdgcn_perm(cd, ab, 0x05040100u);
+  u[1] = __builtin_amdgcn_perm(cd, ab, 0x07060302u);
+  u[2] = __builtin_amdgcn_perm(CD, AB, 0x05040100u);
+  u[3] = __builtin_amdgcn_perm(CD, AB, 0x07060302u);
+}
+
+// The largest x >= 0 of the workgroup.
+__device__ inline uint32_t largest(int x, int* s_most) {
+  x = wave_max_i(x);
+  __syncthreads();  // (the one before is read)
+  if ((threadIdx.x & 63) == 0) s_most[threadIdx.x >> 6] = x;
+  __syncthreads();
+  return (uint32_t)max(max(s_most[0], s_most[1]), max(s_most[2], s_most[3]));
+}
+
 // The least power of two s with most <= 448 s, from 2^-40 to 2^40: most = a 2^e with 1/2 <= a < 1, 448 = 7/8 2^9.
 __device__ inline float scale_of(float most) {
   if (!(most > 0.0f)) return 0x1p-40f;
@@ -63,9 +104,18 @@ __device__ inline float scale_of(float most) {
   return ldexpf(1.0f, min(max(e, -40), 40));
 }
 
+// The work is cut in squares of four tokens and eight dims, a thread a square, so that consecutive lanes read consecutive
+// bytes of a row; a thread's first kHold squares stay in registers between the pass for the largest and the pass that
+// writes (a page of 128 tokens of 128 dims; what does not fit is read again). A square's values by dimension are words of
+// four tokens: through LDS, so that consecutive lanes write consecutive words of a dimension.
+// Bound: 8 prompts of 8192 tokens of 8 heads of 128 (302 MB read and written) 87 us, 3.5 TB/s; waiting for the chain
+// count, length, table, rows (73% of the waves' time) with the five workgroups a CU holds. Values written from the squares, 4
+// bytes a row, 127; every value tested for infinities and clamped, 145; both of the writing loops in one, with 168
+// registers, 122.
 template <bool F16>
 __global__ void __launch_bounds__(kThreads) hs_append_kernel(const AppendArgs A) {
-  __shared__ float s_most[kWaves];
+  __shared__ int s_most[kWaves];
+  __shared__ uint32_t s_words[kSlab * kPitch];
   const uint32_t unit = A.group0 + blockIdx.x;
   if (unit >= A.units) return;
   const int kind = blockIdx.y, t = threadIdx.x;
@@ -86,78 +136,152 @@ __global__ void __launch_bounds__(kThreads) hs_append_kernel(const AppendArgs A)
   const int64_t at = (int64_t)id * A.kv + h;
   const char* x = A.x[kind] + b * A.xb[kind] + h * A.xh[kind];
   const int32_t* path = A.path ? A.path + b * A.path_stride + from : nullptr;
-  const int vecs = A.dim / 8;
+  const int vecs = A.dim / 8, lo4 = first / 4, squares = ((first + num + 3) / 4 - lo4) * vecs;
 
-  auto row_of = [&](int i) -> int { return path ? path[i] : (int)from + i; };
-  auto load = [&](int row, int c, float (&z)[8]) {
-    uint4 r = make_uint4(0, 0, 0, 0);
-    if (row >= 0 && row < A.rows) r = *reinterpret_cast<const uint4*>(x + row * A.xn[kind] + 16 * c);
-    unpack8<F16>(r, z);
-  };
-
-  float most = 0.0f;
-  for (int v = t; v < num * vecs; v += kThreads) {
-    const int i = (int)fdiv((uint32_t)v, A.div_vec), c = v - i * vecs;
-    float z[8];
-    load(row_of(i), c, z);
+  // square v's four rows from the page's token 4 (lo4 + v / vecs) on; 0 where there is no new one
+  auto load = [&](int v, uint4 (&r)[4]) {
+    const int g = (int)fdiv((uint32_t)v, A.div_vec), c = v - g * vecs;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) most = fmaxf(most, finite(z[k]) ? fabsf(z[k]) : 0.0f);
-  }
-  most = __int_as_float(wave_max_i(__float_as_int(most)));  // not negative: ordered like its bits
-  if ((t & 63) == 0) s_most[t >> 6] = most;
+    for (int k = 0; k < 4; ++k) {
+      const int i = 4 * (lo4 + g) + k - first;
+      r[k] = make_uint4(0, 0, 0, 0);
+      if (i < 0 || i >= num) continue;
+      const int row = path ? path[i] : (int)from + i;
+      if (row >= 0 && row < A.rows) r[k] = *reinterpret_cast<const uint4*>(x + row * A.xn[kind] + 16 * c);
+    }
+  };
+  // the largest |x| by its 16 bits, which order like it, two at a time; with an infinity or NaN among them, of the rest
+  constexpr uint32_t kInf = F16 ? 0x7C00u : 0x7F80u;
+  u16x2 top = {0, 0};
   const float was = A.scale[kind][at];
-  __syncthreads();
-  most = fmaxf(fmaxf(s_most[0], s_most[1]), fmaxf(s_most[2], s_most[3]));
+  auto grow = [&](const uint4 (&r)[4]) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t w[4] = {r[k].x, r[k].y, r[k].z, r[k].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, w[e] & 0x7FFF7FFFu));
+    }
+  };
+  uint4 held[kHold][4];
+#pragma unroll
+  for (int i = 0; i < kHold; ++i) {
+    held[i][0] = held[i][1] = held[i][2] = held[i][3] = make_uint4(0, 0, 0, 0);
+    if (t + kThreads * i < squares) load(t + kThreads * i, held[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < kHold; ++i) grow(held[i]);
+  for (int v = t + kThreads * kHold; v < squares; v += kThreads) {
+    uint4 r[4];
+    load(v, r);
+    grow(r);
+  }
+  uint32_t bits = largest(max((int)top[0], (int)top[1]), s_most);
+  const bool all_finite = bits < kInf;
+  if (!all_finite) {
+    int rest = 0;
+    for (int v = t; v < squares; v += kThreads) {
+      uint4 r[4];
+      load(v, r);
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t w[4] = {r[k].x, r[k].y, r[k].z, r[k].w};
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t y = (w[e / 2] >> (16 * (e & 1))) & 0x7FFFu;
+          rest = max(rest, y < kInf ? (int)y : 0);
+        }
+      }
+    }
+    bits = largest(rest, s_most);
+  }
+  const float most = Vec16<F16>::lo(bits);
   const float need = scale_of(most), now = first > 0 ? fmaxf(need, was) : need;
   const bool grows = first > 0 && now != was;
   const float ratio = was / now;
   if (t == 0) A.scale[kind][at] = now;
-
+  // Where every quotient is in the range and the scale a power of two, one instruction converts two values.
+  const bool plain = all_finite && __builtin_amdgcn_frexp_mantf(now) == 0.5f && most <= kTop * now;
   uint8_t* const page = A.cache[kind] + at * A.page * A.dim;
-  if (kind == 0) {  // [token][dim]
-    for (int v = t + (grows ? 0 : first * vecs); v < (first + num) * vecs; v += kThreads) {
-      const int i = (int)fdiv((uint32_t)v, A.div_vec), c = v - i * vecs;
-      uint2* const to = reinterpret_cast<uint2*>(page + i * A.dim + 8 * c);
-      if (i < first) {
+  const int shift = A.shift - 2, words = squares / vecs;  // log2 of a dim's words; its words that have new tokens
+  if (grows) {  // the codes that are there, but those of a word with new tokens
+    if (kind == 0) {
+      for (int v = t; v < first * vecs; v += kThreads) {
+        uint2* const to = reinterpret_cast<uint2*>(page + 8 * v);
         const uint2 old = *to;
         *to = make_uint2(rescaled(old.x, ratio), rescaled(old.y, ratio));
-        continue;
       }
-      float z[8];
-      load(row_of(i - first), c, z);
-      const float lo[4] = {z[0] / now, z[1] / now, z[2] / now, z[3] / now};
-      const float hi[4] = {z[4] / now, z[5] / now, z[6] / now, z[7] / now};
-      *to = make_uint2(codes_of(lo), codes_of(hi));
+    } else {
+      for (int v = t; v < A.dim << shift; v += kThreads) {
+        uint32_t* const to = reinterpret_cast<uint32_t*>(page + 4 * v);
+        if ((v & ((1 << shift) - 1)) < lo4) *to = rescaled(*to, ratio);
+      }
     }
-    return;
   }
-  // [dim][token]: a thread does four tokens of eight dims
-  const int lo4 = grows ? 0 : first / 4, hi4 = (first + num + 3) / 4;
-  for (int v = t; v < (hi4 - lo4) * vecs; v += kThreads) {
+  auto keys = [&](int v, const uint2 (&y)[4]) {  // [token][dim]
     const int g = (int)fdiv((uint32_t)v, A.div_vec), c = v - g * vecs, tok = 4 * (lo4 + g);
-    float z[4][8];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int i = tok + k - first;
-      load(i >= 0 && i < num ? row_of(i) : -1, c, z[k]);
-    }
+    for (int k = 0; k < 4; ++k)
+      if (tok + k >= first && tok + k < first + num) *reinterpret_cast<uint2*>(page + (tok + k) * A.dim + 8 * c) = y[k];
+  };
+  auto values = [&](int v, int d0, const uint2 (&y)[4]) {  // [dim][token]: to LDS
+    const int g = (int)fdiv((uint32_t)v, A.div_vec), d = 8 * (v - g * vecs) - d0;
+    if (d < 0 || d >= kSlab) return;
+    uint32_t u[8];
+    transpose4(y[0].x, y[1].x, y[2].x, y[3].x, u);
+    transpose4(y[0].y, y[1].y, y[2].y, y[3].y, u + 4);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      uint32_t* const to = reinterpret_cast<uint32_t*>(page + (8 * c + e) * A.page + tok);
-      const float y[4] = {z[0][e] / now, z[1][e] / now, z[2][e] / now, z[3][e] / now};
-      uint32_t u = codes_of(y);
-      if (tok < first || tok + 4 > first + num) {
-        const uint32_t old = *to, kept = grows ? rescaled(old, ratio) : old;
+    for (int e = 0; e < 8; ++e) s_words[(d + e) * kPitch + g] = u[e];
+  };
+  auto write = [&](int d0) {  // and from there
+    __syncthreads();
+    const int g = t & ((1 << shift) - 1), tok = 4 * (lo4 + g);
+    const bool edge = tok < first || tok + 4 > first + num;  // codes of other tokens are in the word
+    if (g < words)
+      for (int d = t >> shift; d < min(kSlab, A.dim - d0); d += kThreads >> shift) {
+        uint32_t* const to = reinterpret_cast<uint32_t*>(page + (d0 + d) * A.page + tok);
+        uint32_t u = s_words[d * kPitch + g];
+        if (edge) {
+          const uint32_t old = *to, kept = grows ? rescaled(old, ratio) : old;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const uint32_t byte = 0xFFu << (8 * k);
-          if (tok + k < first) u = (u & ~byte) | (kept & byte);
-          else if (tok + k >= first + num) u = (u & ~byte) | (old & byte);
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t byte = 0xFFu << (8 * k);
+            if (tok + k < first) u = (u & ~byte) | (kept & byte);
+            else if (tok + k >= first + num) u = (u & ~byte) | (old & byte);
+          }
         }
+        *to = u;
       }
-      *to = u;
+    __syncthreads();
+  };
+  auto all = [&](auto codes, bool again) {
+    for (int d0 = 0; d0 < (kind == 0 ? 1 : A.dim); d0 += kSlab) {
+      auto square = [&](int v, const uint4 (&r)[4]) {
+        const uint2 y[4] = {codes(r[0]), codes(r[1]), codes(r[2]), codes(r[3])};
+        if (kind == 0) keys(v, y);
+        else values(v, d0, y);
+      };
+      if (!again) {
+#pragma unroll
+        for (int i = 0; i < kHold; ++i)
+          if (t + kThreads * i < squares) square(t + kThreads * i, held[i]);
+      }
+#pragma unroll 1
+      for (int v = t + (again ? 0 : kThreads * kHold); v < squares; v += kThreads) {
+        uint4 r[4];
+        load(v, r);
+        square(v, r);
+      }
+      if (kind != 0) write(d0);
     }
-  }
+  };
+  if (plain) all([&](const uint4& r) { return plain_codes<F16>(r, now); }, false);
+  else
+    all([&](const uint4& r) {
+      float z[8];
+      Vec16<F16>::unpack(r, z);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) z[k] /= now;
+      const float lo[4] = {z[0], z[1], z[2], z[3]}, hi[4] = {z[4], z[5], z[6], z[7]};
+      return make_uint2(codes_of(lo), codes_of(hi));
+    }, true);
 }
 
 }  // namespace
