@@ -679,54 +679,60 @@ __global__ void __launch_bounds__(64 * NW, DB <= 4 ? 2 : 1) hs_attend_kernel(con
     attend_range<F16, DB, WR, NW>(A, b, h, tile, wv, nth, per, from, to, before, s_stage, s_m, s_l);
   }
 }
-// The parts of a query's rows, joined: a wave 8 dims of 32 rows, as they were in the registers.
+// The parts of a query's rows, joined: a wave 8 dims of 32 rows at a time, as they were in the registers. A workgroup does
+// the dims 32 j .. 32 j + 31, j = blockIdx.y, + gridDim.y, ..
 template <bool F16, int DB, int WR>
 __global__ void __launch_bounds__(kThreads) hs_attend_join_kernel(const AttendArgs A) {
   constexpr int D = 32 * DB, kAhead = 8;
   const int lane = threadIdx.x & 63, i = (int)uniform(threadIdx.x >> 6), rho = lane & 31, half = lane >> 5;
-  const uint32_t group = blockIdx.x / DB, bh = fdiv(group, A.div_rows);
-  const int j = (int)(blockIdx.x - group * DB), rt = (int)(group - bh * A.row_tiles);
+  const uint32_t bh = fdiv(blockIdx.x, A.div_rows);
+  const int rt = (int)(blockIdx.x - bh * A.row_tiles);
   const int b = (int)fdiv(bh, A.div_kv), h = (int)bh - b * A.kv;
   const int rows = nodes_of(A, b) * A.group;
   if (rt * 32 >= rows) return;
   const Plan plan(A, lane);
   const int before = plan.before(A, b), r0 = before / plan.per, r1 = (before + same(stages_of(A, b)) - 1) / plan.per;
   if (r0 == r1) return;  // one part
-  const int tile = rt / WR;
+  const int tile = rt / WR, row = rt * 32 + rho;
   const int64_t base = (int64_t)(h * A.tiles + tile) * (2 * A.chunks);
   auto place = [&](int r) -> int64_t {  // the first of the 32 rows of part r
     return ((base + 2 * r + (before > r * plan.per ? 1 : 0)) * WR + (rt - tile * WR)) * 32;
   };
-  float m = kLowest;
-  for (int r = r0; r <= r1; r += kAhead)
+  const int node = (int)fdiv((uint32_t)min(row, rows - 1), A.div_group), head = h * A.group + row - node * A.group;
+  for (int j = blockIdx.y; j < DB; j += gridDim.y) {
+    float m = kLowest, l = 0.0f;
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int r = r0; r <= r1; r += kAhead) {
+      f32x4 y[kAhead];
+      float2 ml[kAhead];
 #pragma unroll
-    for (int a = 0; a < kAhead; ++a) m = fmaxf(m, A.part_ml[place(min(r + a, r1)) + rho].x);
-  float l = 0.0f;
-  f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int r = r0; r <= r1; r += kAhead) {
-    f32x4 y[kAhead];
-    float2 ml[kAhead];
+      for (int a = 0; a < kAhead; ++a)
+        if (r + a <= r1) {
+          const int64_t at = place(r + a);
+          ml[a] = A.part_ml[at + rho];
+          y[a] = *reinterpret_cast<const f32x4*>(A.part + at * D + (4 * j + i) * 256 + 4 * lane);
+        }
+      const float old = m;
 #pragma unroll
-    for (int a = 0; a < kAhead; ++a) {
-      const int64_t at = place(min(r + a, r1));
-      ml[a] = A.part_ml[at + rho];
-      y[a] = *reinterpret_cast<const f32x4*>(A.part + at * D + (4 * j + i) * 256 + 4 * lane);
+      for (int a = 0; a < kAhead; ++a)
+        if (r + a <= r1) m = fmaxf(m, ml[a].x);
+      const float less = __builtin_amdgcn_exp2f(old - m);
+      l *= less;
+      o *= less;
+#pragma unroll
+      for (int a = 0; a < kAhead; ++a)
+        if (r + a <= r1) {
+          const float f = __builtin_amdgcn_exp2f(ml[a].x - m);
+          l = fmaf(ml[a].y, f, l);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) o[k] = fmaf(y[a][k], f, o[k]);
+        }
     }
-#pragma unroll
-    for (int a = 0; a < kAhead; ++a)
-      if (r + a <= r1) {
-        const float f = __builtin_amdgcn_exp2f(ml[a].x - m);
-        l = fmaf(ml[a].y, f, l);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) o[k] = fmaf(y[a][k], f, o[k]);
-      }
+    const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
+    if (row < rows)
+      store4<F16>(A.out + b * A.ob + node * A.on + head * A.oh + 2 * (32 * j + 8 * i + 4 * half),
+                  f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv});
   }
-  const int row = rt * 32 + rho;
-  if (row >= rows) return;
-  const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
-  const int node = (int)fdiv((uint32_t)row, A.div_group), head = h * A.group + row - node * A.group;
-  store4<F16>(A.out + b * A.ob + node * A.on + head * A.oh + 2 * (32 * j + 8 * i + 4 * half),
-              f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv});
 }
 
 template <bool F16, int DB, int WR, int NW>
@@ -739,8 +745,8 @@ void launch_rows(AttendArgs A, hipStream_t st) {
     if (hipPeekAtLastError() != hipSuccess) return;
   }
   if (!A.chunks) return;
-  const uint32_t joins = (uint32_t)A.B * A.kv * A.row_tiles * DB;  // (few: ranges are for few queries and heads)
-  hs_attend_join_kernel<F16, DB, WR><<<joins, kThreads, 0, st>>>(A);
+  const uint32_t joins = (uint32_t)A.B * A.kv * A.row_tiles;  // (few: ranges are for few queries and heads)
+  hs_attend_join_kernel<F16, DB, WR><<<dim3(joins, joins < 512 ? DB : 1), kThreads, 0, st>>>(A);
 }
 
 template <bool F16, int DB>
