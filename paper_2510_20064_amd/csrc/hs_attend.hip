@@ -29,6 +29,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -36,7 +37,11 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr float kHeadroom = 12.0f;  // weights are held as 2^12 w
 constexpr float kSlack = 3.0f;      // m follows a maximum more than this above it
 constexpr float kLowest = -1.7e38f; // m before the first token
+constexpr int kWaves16 = 3;
 constexpr int kStage = 4;           // tiles of 32 tokens that a workgroup brings to LDS at once
+
+// Waves of a SIMD, by the registers that they take.
+constexpr int waves_of(int rw, int dim) { return dim > 128 ? rw == 16 ? 2 : 1 : rw == 16 ? kWaves16 : 2; }
 
 struct AttendArgs {
   const char* q;
@@ -61,10 +66,10 @@ struct AttendArgs {
   int tiles;   // workgroups that share a cached head's rows
   int chunks;  // ranges that all queries' cached tokens are cut into; 0: a query is one
   uint32_t items, group0;  // (ranges, or queries) * kv
-  uint32_t row_tiles;      // 32 rows of a query's cached head
+  uint32_t row_tiles;      // 32 (16) rows of a query's cached head
   FastDiv div_kv, div_tiles, div_group, div_rows;
-  float* part;      // [kv * tiles][2 * chunks][WR][D / 8][2][32 rows][4]
-  float2* part_ml;  // [kv * tiles][2 * chunks][WR][32 rows]
+  float* part;      // [kv * tiles][2 * chunks][WR][groups of a State][64 lanes][4]
+  float2* part_ml;  // [kv * tiles][2 * chunks][WR][32 or 16 rows]
 };
 
 __device__ inline int same(int x) { return (int)uniform((uint32_t)x); }  // (what every lane has, in a scalar register)
@@ -140,6 +145,13 @@ __device__ inline f32x16 mfma(f16x8 a, f16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 
+__device__ inline f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ inline f32x4 mfma(f16x8 a, f16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
 // Eight codes as bf16 or fp16.
 template <bool F16>
 __device__ inline V8<F16> widen(uint32_t lo, uint32_t hi) {
@@ -170,23 +182,48 @@ __device__ inline f16x8 narrow(const float* w) {
   return r;
 }
 
-// The token of a tile whose key is row rho of the first product (register i of lane half h is then token 16 h + i), and
-// the row of a token.
-__device__ inline int pi_of(int rho) {
-  return ((rho >> 2) & 1) * 16 + (rho >> 4) * 8 + ((rho >> 3) & 1) * 4 + (rho & 3);
-}
-__device__ inline int rho_of(int token) {
-  return ((token >> 4) & 1) * 4 + ((token >> 3) & 1) * 16 + ((token >> 2) & 1) * 8 + (token & 3);
+// The row of a token's key in its tile, so that a lane's scores are consecutive tokens: of 32 rows register i of lane half
+// h is token 16 h + i, of 16 rows register i of product a and lane quarter g token 8 g + 4 a + i.
+template <int RW>
+__device__ inline int row_of(int token) {
+  if constexpr (RW == 32)
+    return ((token >> 4) & 1) * 4 + ((token >> 3) & 1) * 16 + ((token >> 2) & 1) * 8 + (token & 3);
+  else return ((token >> 2) & 1) * 16 + (token >> 3) * 4 + (token & 3);
 }
 
-// The values of lanes l and l + 32, combined in both.
-struct Halves {
-  float lo, hi;
+// The largest value, and the sum, of the lanes that have a row: l and l + 32, or of 16 rows also l + 16 and l + 48.
+struct Pair {
+  float a, b;
 };
-__device__ inline Halves halves(float x) {
+__device__ inline Pair halves(float x) {
   const uint32_t u = __float_as_uint(x);
   const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-  return Halves{__uint_as_float(r[0]), __uint_as_float(r[1])};
+  return Pair{__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+__device__ inline Pair quarters(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return Pair{__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+template <int RW>
+__device__ inline float row_max(float x) {
+  const Pair p = halves(x);
+  x = fmaxf(p.a, p.b);
+  if constexpr (RW == 16) {
+    const Pair q = quarters(x);
+    x = fmaxf(q.a, q.b);
+  }
+  return x;
+}
+template <int RW>
+__device__ inline float row_sum(float x) {
+  const Pair p = halves(x);
+  x = p.a + p.b;
+  if constexpr (RW == 16) {
+    const Pair q = quarters(x);
+    x = q.a + q.b;
+  }
+  return x;
 }
 
 // The pages of the tiles of stage t, lane i that of tile i, or -1. (By a vector load like the scales below: a scalar
@@ -234,7 +271,7 @@ __device__ __forceinline__ void load_stage(const AttendArgs& A, int h, int t, in
   }
 }
 // pages, t, tokens: of the stage. What lies behind the last token may be any code: its values are held as 0.
-template <int DB, int NW>
+template <int RW, int DB, int NW>
 __device__ __forceinline__ void store_stage(uint8_t* lds, int t, int pages, int tokens, int wv, int lane,
                                             Loads<DB, NW>& L) {
   using St = Staged<DB>;
@@ -252,50 +289,69 @@ __device__ __forceinline__ void store_stage(uint8_t* lds, int t, int pages, int 
       }
     }
     const int q = part * 64 + lane, token = q / (2 * DB), c = q - token * (2 * DB);
-    *reinterpret_cast<u32x4*>(lds + (32 * sub + rho_of(token)) * St::kKeyPitch + 16 * c) = L.k[i];
+    *reinterpret_cast<u32x4*>(lds + (32 * sub + row_of<RW>(token)) * St::kKeyPitch + 16 * c) = L.k[i];
     *reinterpret_cast<u32x4*>(lds + St::kKeys + (32 * part + (lane >> 1)) * St::kValuePitch + 32 * sub + 16 * (lane & 1)) =
         L.v[i];
   }
 }
 
-// A wave's running state of 32 rows: lane (r, h) has row r.
-template <int DB>
+// A wave's running state of RW = 32 or 16 rows: lane (r, c), l = RW c + r, has row r; O in groups of four dims, group n
+// those from kDims n + 4 c on.
+template <int DB, int RW>
 struct State {
-  f32x16 o[DB];  // o[j][i]: dim 32 j + 8 (i / 4) + 4 h + i % 4
-  float m, l;    // l: this half's share
+  static constexpr int kGroups = DB * RW / 8, kDims = 256 / RW;
+  f32x16 o32[RW == 32 ? DB : 1];
+  f32x4 o16[RW == 16 ? 2 * DB : 1];
+  float m, l;  // l: this lane's share
+  __device__ f32x4 get(int n) const {
+    if constexpr (RW == 16) return o16[n];
+    else return f32x4{o32[n / 4][n % 4 * 4], o32[n / 4][n % 4 * 4 + 1], o32[n / 4][n % 4 * 4 + 2], o32[n / 4][n % 4 * 4 + 3]};
+  }
+  __device__ void set(int n, f32x4 v) {
+    if constexpr (RW == 16) o16[n] = v;
+    else
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o32[n / 4][n % 4 * 4 + k] = v[k];
+  }
+  __device__ void clear() {
+#pragma unroll
+    for (int n = 0; n < kGroups; ++n) set(n, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+    m = kLowest;
+    l = 0.0f;
+  }
+  __device__ void scale(float f) {
+#pragma unroll
+    for (int n = 0; n < kGroups; ++n) set(n, get(n) * f);
+  }
 };
 
 // m, and O and l with it, after scores (plus the log2 of the values' scale) of which the lane's largest is `top`. What
 // weights are relative to: 2^12 w = 2^(x - that).
-template <int DB>
-__device__ inline float follow(State<DB>& S, float top) {
-  const Halves t = halves(top);
-  top = fmaxf(t.lo, t.hi);
+template <int DB, int RW>
+__device__ inline float follow(State<DB, RW>& S, float top) {
+  top = row_max<RW>(top);
   if (__ballot(top > S.m + kSlack)) {
     const float m = fmaxf(S.m, top), f = __builtin_amdgcn_exp2f(S.m - m);
     S.m = m;
     S.l *= f;
-#pragma unroll
-    for (int j = 0; j < DB; ++j)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) S.o[j][i] *= f;
+    S.scale(f);
   }
   return S.m - kHeadroom;
 }
-__device__ inline float max16(const float (&x)[16]) {
+template <int N>
+__device__ inline float max_of(const float (&x)[N]) {
   float top = x[0];
 #pragma unroll
-  for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+  for (int i = 1; i < N; ++i) top = fmaxf(top, x[i]);
   return top;
 }
-
-__device__ inline float sum16_of(const float (&w)[16]) {
-  float a[8];
+template <int N>
+__device__ inline float sum_of(const float (&w)[N]) {
+  float a[N / 2];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) a[i] = w[2 * i] + w[2 * i + 1];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) a[i] = a[2 * i] + a[2 * i + 1];
-  return (a[0] + a[1]) + (a[2] + a[3]);
+  for (int i = 0; i < N / 2; ++i) a[i] = w[2 * i] + w[2 * i + 1];
+  if constexpr (N > 2) return sum_of(a);
+  else return a[0];
 }
 
 constexpr float kLeast = 1e-30f;  // the least factor of a product: infinite ones, which get no weight, stay infinite
@@ -304,7 +360,7 @@ constexpr float kLeast = 1e-30f;  // the least factor of a product: infinite one
 // other, then one step of the softmax.
 template <bool F16, int DB, int N>
 __device__ __forceinline__ void attend_tiles(const AttendArgs& A, const V8<F16> (&q)[2 * DB], const uint8_t* lds, int sub,
-                                             const int (&valid)[N], float scales, int lane, State<DB>& S) {
+                                             const int (&valid)[N], float scales, int lane, State<DB, 32>& S) {
   using St = Staged<DB>;
   const int rho = lane & 31, half = lane >> 5;
   const uint8_t* kp = lds + (32 * sub + rho) * St::kKeyPitch + 16 * half;
@@ -339,7 +395,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& A, const V8<F16> 
     }
     top = fmaxf(top, fmaf(f[n] < 0.0f ? lo : hi, f[n], bias[n]));
   }
-  const float from = follow<DB>(S, top);
+  const float from = follow(S, top);
   f16x8 p[N][2];
 #pragma unroll
   for (int n = 0; n < N; ++n) {
@@ -347,7 +403,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& A, const V8<F16> 
     float x[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], f[n], off));
-    S.l = fmaf(sum16_of(x), inv[n], S.l);
+    S.l = fmaf(sum_of(x), inv[n], S.l);
     p[n][0] = narrow(x);
     p[n][1] = narrow(x + 8);
   }
@@ -357,9 +413,54 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& A, const V8<F16> 
 #pragma unroll
     for (int j = 0; j < DB; ++j) {
       const u32x4 v = *reinterpret_cast<const u32x4*>(vp + 32 * j * St::kValuePitch + 32 * n);
-      S.o[j] = mfma(widen<true>(v.x, v.y), p[n][0], S.o[j]);
-      S.o[j] = mfma(widen<true>(v.z, v.w), p[n][1], S.o[j]);
+      S.o32[j] = mfma(widen<true>(v.x, v.y), p[n][0], S.o32[j]);
+      S.o32[j] = mfma(widen<true>(v.z, v.w), p[n][1], S.o32[j]);
     }
+}
+
+// The same for 16 rows, one tile: products of 16 x 16 x 32.
+template <bool F16, int DB>
+__device__ __forceinline__ void attend_tiles(const AttendArgs& A, const V8<F16> (&q)[DB], const uint8_t* lds, int sub,
+                                             const int (&valid)[1], float scales, int lane, State<DB, 16>& S) {
+  using St = Staged<DB>;
+  const int rho = lane & 15, g = lane >> 4;
+  const uint8_t* kp = lds + (32 * sub + rho) * St::kKeyPitch + 8 * g;
+  f32x4 s[2] = {};
+#pragma unroll
+  for (int j = 0; j < DB; ++j)
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+      const u32x2 k = *reinterpret_cast<const u32x2*>(kp + 16 * a * St::kKeyPitch + 32 * j);
+      s[a] = mfma(widen<F16>(k.x, k.y), q[j], s[a]);
+    }
+  const float vs = fminf(fmaxf(lane_f(scales, kStage + sub), 0x1p-40f), 0x1p40f);
+  float f = A.scale2 * lane_f(scales, sub);
+  if (fabsf(f) < kLeast) f = kLeast;
+  const float bias = __builtin_amdgcn_logf(vs);
+  if (valid[0] < 32) {
+    asm volatile("");
+    const float none = f < 0.0f ? INFINITY : -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i / 4][i % 4] = 8 * g + i < valid[0] ? s[i / 4][i % 4] : none;
+  }
+  float hi = s[0][0], lo = hi;
+#pragma unroll
+  for (int i = 1; i < 8; ++i) {
+    hi = fmaxf(hi, s[i / 4][i % 4]);
+    lo = fminf(lo, s[i / 4][i % 4]);
+  }
+  const float off = bias - follow(S, fmaf(f < 0.0f ? lo : hi, f, bias));
+  float x[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(s[i / 4][i % 4], f, off));
+  S.l = fmaf(sum_of(x), __builtin_amdgcn_rcpf(vs), S.l);
+  const f16x8 p = narrow(x);
+  const uint8_t* vp = lds + St::kKeys + rho * St::kValuePitch + 32 * sub + 8 * g;
+#pragma unroll
+  for (int n = 0; n < 2 * DB; ++n) {
+    const u32x2 v = *reinterpret_cast<const u32x2*>(vp + 16 * n * St::kValuePitch);
+    S.o16[n] = mfma(widen<true>(v.x, v.y), p, S.o16[n]);
+  }
 }
 
 // 32 nodes in LDS, in their own type: keys like a tile's, values by dimension.
@@ -393,7 +494,7 @@ __device__ inline bool not_finite16(uint32_t x, bool f16) {
   return f16 ? (x & 0x7C00u) == 0x7C00u : (x & 0x7F80u) == 0x7F80u;
 }
 // Whether a value is not finite: 0 times it is no 0, so it is held as 0 and added to the rows that see it.
-template <bool F16, int DB, int T>
+template <bool F16, int RW, int DB, int T>
 __device__ __forceinline__ bool store_nodes(uint8_t* lds, int t, const NodeLoads<DB, T>& L) {
   using Nd = Nodes<DB>;
   bool bad = false;
@@ -401,7 +502,7 @@ __device__ __forceinline__ bool store_nodes(uint8_t* lds, int t, const NodeLoads
   for (int i = 0; i < L.kN; ++i) {
     const int u = t + T * i, n = u / (4 * DB), c = u - n * (4 * DB);
     if (u >= Nd::kPieces) continue;
-    *reinterpret_cast<u32x4*>(lds + rho_of(n) * Nd::kKeyPitch + 16 * c) = L.k[i];
+    *reinterpret_cast<u32x4*>(lds + row_of<RW>(n) * Nd::kKeyPitch + 16 * c) = L.k[i];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       uint16_t y = (uint16_t)(L.v[i][e / 2] >> (16 * (e & 1)));
@@ -417,28 +518,40 @@ __device__ __forceinline__ bool store_nodes(uint8_t* lds, int t, const NodeLoads
 
 // The 32 nodes in LDS, `first` the first of them. bits: the nodes that the lane's row sees; bad: there are values that
 // are not finite.
-template <bool F16, int DB>
-__device__ inline void attend_nodes(const AttendArgs& A, const V8<F16> (&q)[2 * DB], const uint8_t* lds, int b, int h,
-                                    int first, int nodes, uint64_t bits, bool bad, int lane, State<DB>& S) {
+template <bool F16, int DB, int RW, int NQ>
+__device__ inline void attend_nodes(const AttendArgs& A, const V8<F16> (&q)[NQ], const uint8_t* lds, int b, int h,
+                                    int first, int nodes, uint64_t bits, bool bad, int lane, State<DB, RW>& S) {
   using Nd = Nodes<DB>;
-  const int rho = lane & 31, half = lane >> 5;
-  const uint8_t* kp = lds + rho * Nd::kKeyPitch + 32 * half;
-  f32x16 s = {};
+  constexpr int NX = RW / 2;  // a lane's nodes
+  const int rho = lane % RW, c = lane / RW;
+  float x[NX];
+  const uint8_t* kp = lds + rho * Nd::kKeyPitch + (RW == 32 ? 32 : 16) * c;
+  const uint32_t sees = (uint32_t)(bits >> (first + NX * c)) & ((1u << NX) - 1);
+  if constexpr (RW == 32) {
+    f32x16 s = {};
 #pragma unroll
-  for (int j = 0; j < DB; ++j)
+    for (int j = 0; j < DB; ++j)
 #pragma unroll
-    for (int e = 0; e < 2; ++e) s = mfma(*reinterpret_cast<const V8<F16>*>(kp + 64 * j + 16 * e), q[2 * j + e], s);
-  float x[16];
-  const uint32_t sees = (uint32_t)(bits >> (first + 16 * half)) & 0xFFFFu;
+      for (int e = 0; e < 2; ++e) s = mfma(*reinterpret_cast<const V8<F16>*>(kp + 64 * j + 16 * e), q[2 * j + e], s);
 #pragma unroll
-  for (int i = 0; i < 16; ++i) x[i] = (sees >> i) & 1 ? s[i] * A.scale2 : -INFINITY;
-  const float from = follow<DB>(S, max16(x));
+    for (int i = 0; i < NX; ++i) x[i] = (sees >> i) & 1 ? s[i] * A.scale2 : -INFINITY;
+  } else {
+    f32x4 s[2] = {};
 #pragma unroll
-  for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(x[i] - from);
-  S.l += sum16_of(x);
-  const uint8_t* vp = lds + Nd::kKeys + rho * Nd::kValuePitch + 32 * half;
+    for (int j = 0; j < DB; ++j)
 #pragma unroll
-  for (int e = 0; e < 2; ++e) {
+      for (int a = 0; a < 2; ++a)
+        s[a] = mfma(*reinterpret_cast<const V8<F16>*>(kp + 16 * a * Nd::kKeyPitch + 64 * j), q[j], s[a]);
+#pragma unroll
+    for (int i = 0; i < NX; ++i) x[i] = (sees >> i) & 1 ? s[i / 4][i % 4] * A.scale2 : -INFINITY;
+  }
+  const float from = follow(S, max_of(x));
+#pragma unroll
+  for (int i = 0; i < NX; ++i) x[i] = __builtin_amdgcn_exp2f(x[i] - from);
+  S.l += sum_of(x);
+  const uint8_t* vp = lds + Nd::kKeys + rho * Nd::kValuePitch + 2 * NX * c;
+#pragma unroll
+  for (int e = 0; e < NX / 8; ++e) {
     // The nodes' values are fp16, or bf16, whose range fp16 lacks: the weights are then two bf16 (16 bits).
     V8<F16> p, rest;
     if constexpr (F16) p = narrow(x + 8 * e);
@@ -449,10 +562,15 @@ __device__ inline void attend_nodes(const AttendArgs& A, const V8<F16> (&q)[2 * 
         rest[i] = (__bf16)(x[8 * e + i] - (float)p[i]);
       }
 #pragma unroll
-    for (int j = 0; j < DB; ++j) {
-      const V8<F16> a = *reinterpret_cast<const V8<F16>*>(vp + 32 * j * Nd::kValuePitch + 16 * e);
-      S.o[j] = mfma(a, p, S.o[j]);
-      if constexpr (!F16) S.o[j] = mfma(a, rest, S.o[j]);
+    for (int n = 0; n < 32 * DB / RW; ++n) {
+      const V8<F16> a = *reinterpret_cast<const V8<F16>*>(vp + RW * n * Nd::kValuePitch + 16 * e);
+      if constexpr (RW == 32) {
+        S.o32[n] = mfma(a, p, S.o32[n]);
+        if constexpr (!F16) S.o32[n] = mfma(a, rest, S.o32[n]);
+      } else {
+        S.o16[n] = mfma(a, p, S.o16[n]);
+        if constexpr (!F16) S.o16[n] = mfma(a, rest, S.o16[n]);
+      }
     }
   }
   if (!bad) return;
@@ -461,15 +579,17 @@ __device__ inline void attend_nodes(const AttendArgs& A, const V8<F16> (&q)[2 * 
   for (int n = first; n < min(first + 32, nodes); ++n) {
     const bool on = (bits >> n) & 1;
 #pragma unroll
-    for (int j = 0; j < DB; ++j)
+    for (int k = 0; k < S.kGroups; ++k) {
+      f32x4 o = S.get(k);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int d = 32 * j + 8 * (i >> 2) + 4 * half + (i & 3);
-        const uint16_t y = *reinterpret_cast<const uint16_t*>(gp + n * A.vn + 2 * d);
+      for (int i = 0; i < 4; ++i) {
+        const uint16_t y = *reinterpret_cast<const uint16_t*>(gp + n * A.vn + 2 * (S.kDims * k + 4 * c + i));
         if (on && not_finite16(y, F16))
-          S.o[j][i] += F16 ? (float)__builtin_bit_cast(_Float16, y) : __uint_as_float((uint32_t)y << 16);
-        if ((i & 3) == 3) __builtin_amdgcn_sched_barrier(0);  // (a rare path that takes no registers from the others)
+          o[i] += F16 ? (float)__builtin_bit_cast(_Float16, y) : __uint_as_float((uint32_t)y << 16);
       }
+      S.set(k, o);
+      __builtin_amdgcn_sched_barrier(0);  // (a rare path that takes no registers from the others)
+    }
   }
 }
 
@@ -482,15 +602,15 @@ __device__ inline void store4(char* p, f32x4 v) {
 }
 
 // A query's stages that lie in the range [from, to) of all, `before` of which come before the query's.
-template <bool F16, int DB, int WR, int NW>
+template <bool F16, int DB, int RW, int WR, int NW>
 __device__ __forceinline__ void attend_range(const AttendArgs& A, int b, int h, int tile, int wv, int nth, int per, int from,
                                              int to, int before, uint8_t* s_stage, float (*s_m)[32],
                                              float (*s_l)[32]) {
-  constexpr int D = 32 * DB, kPitch = D + 4, WT = NW / WR, kRows = 32 * WR, T = 64 * NW;
-  float(*s_o)[32 * kPitch] = reinterpret_cast<float(*)[32 * kPitch]>(s_stage);
+  constexpr int D = 32 * DB, kPitch = D + 4, WT = NW / WR, kRows = RW * WR, T = 64 * NW;
+  float(*s_o)[RW * kPitch] = reinterpret_cast<float(*)[RW * kPitch]>(s_stage);
   int thread = threadIdx.x;
   asm volatile("" : "+v"(thread));  // no address is formed before the loop over queries and kept through it
-  const int lane = thread & 63, rho = lane & 31, half = lane >> 5, wr = wv % WR, wt = wv / WR;
+  const int lane = thread & 63, rho = lane % RW, c = lane / RW, wr = wv % WR, wt = wv / WR;
   const int nodes = nodes_of(A, b), rows = nodes * A.group;
   if (tile * kRows >= rows) return;
   const int tokens = same(tokens_of(A, b)), stages = same(stages_of(A, b));
@@ -498,29 +618,25 @@ __device__ __forceinline__ void attend_range(const AttendArgs& A, int b, int h, 
   const int first = starts ? 0 : (from - before) * kStage;
   const int last = min(ends ? INT_MAX : (to - before) * kStage, (tokens + 31) / 32);
 
-  const int row = tile * kRows + wr * 32 + rho;
-  const bool live = row < rows, busy = tile * kRows + wr * 32 < rows;  // busy: the wave has rows
+  const int row = tile * kRows + wr * RW + rho;
+  const bool live = row < rows, busy = tile * kRows + wr * RW < rows;  // busy: the wave has rows
   const int node = live ? (int)fdiv((uint32_t)row, A.div_group) : 0;
   const int head = h * A.group + (live ? row - node * A.group : 0);
   // What comes first is asked for first: a draft's nodes (their keys and values go through LDS before the stages), the
   // queries, the first stage.
   NodeLoads<DB, T> nl;
   if (ends) load_nodes<DB, T>(A, b, h, 0, nodes, thread, nl);
-  V8<F16> q[2 * DB];
-  const char* qp = A.q + b * A.qb + node * A.qn + head * A.qh + 32 * half;
+  constexpr int NQ = DB * RW / 16;
+  V8<F16> q[NQ];
+  const char* qp = A.q + b * A.qb + node * A.qn + head * A.qh + (RW == 32 ? 32 : 16) * c;
 #pragma unroll
-  for (int j = 0; j < DB; ++j)
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      u32x4 x = *reinterpret_cast<const u32x4*>(qp + 64 * j + 16 * e);
-      if (!live) x = u32x4{0, 0, 0, 0};
-      __builtin_memcpy(&q[2 * j + e], &x, 16);
-    }
-  State<DB> S;
-#pragma unroll
-  for (int j = 0; j < DB; ++j) S.o[j] = f32x16{};
-  S.m = kLowest;
-  S.l = 0.0f;
+  for (int j = 0; j < NQ; ++j) {
+    u32x4 x = *reinterpret_cast<const u32x4*>(qp + (RW == 32 ? 64 * (j / 2) + 16 * (j % 2) : 64 * j));
+    if (!live) x = u32x4{0, 0, 0, 0};
+    __builtin_memcpy(&q[j], &x, 16);
+  }
+  State<DB, RW> S;
+  S.clear();
 
   Loads<DB, NW> L;
   int pages = pages_of(A, b, first, last, lane), next = -1;  // of the stage that is on its way, of the one behind it
@@ -542,15 +658,15 @@ __device__ __forceinline__ void attend_range(const AttendArgs& A, int b, int h, 
         load_nodes<DB, T>(A, b, h, n, nodes, thread, nl);
         __syncthreads();  // the 32 before are read
       }
-      const bool bad = __syncthreads_or(store_nodes<F16, DB, T>(s_stage, thread, nl));
-      if (busy && (n >> 5) % WT == wt) attend_nodes<F16, DB>(A, q, s_stage, b, h, n, nodes, bits, bad, lane, S);
+      const bool bad = __syncthreads_or(store_nodes<F16, RW, DB, T>(s_stage, thread, nl));
+      if (busy && (n >> 5) % WT == wt) attend_nodes<F16, DB, RW>(A, q, s_stage, b, h, n, nodes, bits, bad, lane, S);
     }
     __syncthreads();
   }
 
   for (int t = first; t < last; t += kStage) {
     if (t > first) __syncthreads();  // the stage before is read
-    store_stage<DB, NW>(s_stage, t, pages, tokens, wv, lane, L);
+    store_stage<RW, DB, NW>(s_stage, t, pages, tokens, wv, lane, L);
     const int here = pages;
     const float scales = coming;
     pages = next;
@@ -561,20 +677,21 @@ __device__ __forceinline__ void attend_range(const AttendArgs& A, int b, int h, 
       load_stage<DB, NW>(A, h, t + kStage, pages, wv, lane, L);
     }
     if (!busy) continue;
-    constexpr int N = WT <= 2 ? 2 : 1;  // tiles at once
+    constexpr int N = RW == 32 && WT <= 2 ? 2 : 1;  // tiles at once
 #pragma unroll
     for (int i = 0; i < kStage; i += N * WT) {
       const int sub = i + wt * N;
       int valid[N];
 #pragma unroll
       for (int n = 0; n < N; ++n) valid[n] = valid_of(here, t, sub + n, tokens);
-      attend_tiles<F16, DB, N>(A, q, s_stage, sub, valid, scales, lane, S);
+      if constexpr (RW == 32) attend_tiles<F16, DB, N>(A, q, s_stage, sub, valid, scales, lane, S);
+      else attend_tiles<F16, DB>(A, q, s_stage, sub, valid, scales, lane, S);
     }
   }
 
-  float m = S.m, l = halves(S.l).lo + halves(S.l).hi;
+  float m = S.m, l = row_sum<RW>(S.l);
   if constexpr (WT > 1) {  // the states of the waves of a group, joined
-    if (half == 0) {
+    if (c == 0) {
       s_m[wv][rho] = m;
       s_l[wv][rho] = l;
     }
@@ -586,71 +703,49 @@ __device__ __forceinline__ void attend_range(const AttendArgs& A, int b, int h, 
 #pragma unroll
     for (int w = 0; w < WT; ++w)
       l = fmaf(s_l[w * WR + wr][rho], __builtin_amdgcn_exp2f(s_m[w * WR + wr][rho] - m), l);
-    const float f = __builtin_amdgcn_exp2f(S.m - m);
+    S.scale(__builtin_amdgcn_exp2f(S.m - m));
 #pragma unroll
-    for (int j = 0; j < DB; ++j)
+    for (int half = WT / 2; half >= 1; half /= 2) {  // the upper half of the waves to the lower
+      if (wt >= half && wt < 2 * half) {
+        float* at = &s_o[(wt - half) * WR + wr][rho * kPitch + 4 * c];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) S.o[j][i] *= f;
-#pragma unroll
-    for (int from = WT / 2; from >= 1; from /= 2) {  // the upper half of the waves to the lower
-      if (wt >= from && wt < 2 * from) {
-        float* to = &s_o[(wt - from) * WR + wr][rho * kPitch + 4 * half];
-#pragma unroll
-        for (int j = 0; j < DB; ++j)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<f32x4*>(to + 32 * j + 8 * i) =
-                f32x4{S.o[j][4 * i], S.o[j][4 * i + 1], S.o[j][4 * i + 2], S.o[j][4 * i + 3]};
+        for (int n = 0; n < S.kGroups; ++n) *reinterpret_cast<f32x4*>(at + S.kDims * n) = S.get(n);
       }
       __syncthreads();
-      if (wt < from) {
-        const float* at = &s_o[wt * WR + wr][rho * kPitch + 4 * half];
+      if (wt < half) {
+        const float* at = &s_o[wt * WR + wr][rho * kPitch + 4 * c];
 #pragma unroll
-        for (int j = 0; j < DB; ++j)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const f32x4 y = *reinterpret_cast<const f32x4*>(at + 32 * j + 8 * i);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) S.o[j][4 * i + k] += y[k];
-          }
+        for (int n = 0; n < S.kGroups; ++n) S.set(n, S.get(n) + *reinterpret_cast<const f32x4*>(at + S.kDims * n));
       }
-      if (from > 1) __syncthreads();
+      if (half > 1) __syncthreads();
     }
     if (wt != 0) return;
   }
   if (starts && ends) {
     if (!live) return;
     const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;  // (a NaN stays)
-    char* op = A.out + b * A.ob + node * A.on + head * A.oh + 8 * half;
+    char* op = A.out + b * A.ob + node * A.on + head * A.oh + 8 * c;
 #pragma unroll
-    for (int j = 0; j < DB; ++j)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        store4<F16>(op + 64 * j + 16 * i, f32x4{S.o[j][4 * i] * inv, S.o[j][4 * i + 1] * inv, S.o[j][4 * i + 2] * inv,
-                                                S.o[j][4 * i + 3] * inv});
+    for (int n = 0; n < S.kGroups; ++n) store4<F16>(op + 2 * S.kDims * n, S.get(n) * inv);
     return;
   }
-  const int64_t at = (((int64_t)(h * A.tiles + tile) * (2 * A.chunks) + 2 * nth + (before > from ? 1 : 0)) * WR + wr) * 32;
+  const int64_t at = (((int64_t)(h * A.tiles + tile) * (2 * A.chunks) + 2 * nth + (before > from ? 1 : 0)) * WR + wr) * RW;
   float* op = A.part + at * D + 4 * lane;  // (as the registers are: a wave writes 1 KB at a time)
 #pragma unroll
-  for (int j = 0; j < DB; ++j)
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      *reinterpret_cast<f32x4*>(op + (4 * j + i) * 256) =
-          f32x4{S.o[j][4 * i], S.o[j][4 * i + 1], S.o[j][4 * i + 2], S.o[j][4 * i + 3]};
-  if (half == 0) A.part_ml[at + rho] = make_float2(m, l);
+  for (int n = 0; n < S.kGroups; ++n) *reinterpret_cast<f32x4*>(op + n * 256) = S.get(n);
+  if (c == 0) A.part_ml[at + rho] = make_float2(m, l);
 }
 
-// A workgroup of NW waves has 32 rows for each of WR groups of its waves. It brings kStage tiles at a time to LDS, of
+// A workgroup of NW waves has RW rows for each of WR groups of its waves. It brings kStage tiles at a time to LDS, of
 // which the WT = NW / WR waves of a group take every WT-th each; their states are joined at the end. The next stage is on
 // its way to registers meanwhile.
-template <bool F16, int DB, int WR, int NW>
-__global__ void __launch_bounds__(64 * NW, DB <= 4 ? 2 : 1) hs_attend_kernel(const AttendArgs A) {
+template <bool F16, int DB, int RW, int WR, int NW>
+__global__ void __launch_bounds__(64 * NW, waves_of(RW, 32 * DB)) hs_attend_kernel(const AttendArgs A) {
   constexpr int kPitch = 32 * DB + 4, WT = NW / WR;
   using St = Staged<DB>;
   constexpr int kBytes = St::kBytes > Nodes<DB>::kBytes ? St::kBytes : Nodes<DB>::kBytes;
   __shared__ __attribute__((aligned(16))) uint8_t s_stage[kBytes];
-  static_assert(WT == 1 || kBytes >= WT / 2 * WR * 32 * kPitch * 4, "the join shares the stage's memory");
+  static_assert(WT == 1 || kBytes >= WT / 2 * WR * RW * kPitch * 4, "the join shares the stage's memory");
   static_assert(WT <= kStage, "a wave has a tile of every stage");
   __shared__ float s_m[NW][32], s_l[NW][32];
   const int lane = threadIdx.x & 63, wv = (int)uniform(threadIdx.x >> 6);
@@ -676,30 +771,31 @@ __global__ void __launch_bounds__(64 * NW, DB <= 4 ? 2 : 1) hs_attend_kernel(con
       if (!A.chunks || ++b >= A.B || before >= to) return;
       __syncthreads();  // (the last query's join is read)
     }
-    attend_range<F16, DB, WR, NW>(A, b, h, tile, wv, nth, per, from, to, before, s_stage, s_m, s_l);
+    attend_range<F16, DB, RW, WR, NW>(A, b, h, tile, wv, nth, per, from, to, before, s_stage, s_m, s_l);
   }
 }
-// The parts of a query's rows, joined: a wave 8 dims of 32 rows at a time, as they were in the registers. A workgroup does
-// the dims 32 j .. 32 j + 31, j = blockIdx.y, + gridDim.y, ..
-template <bool F16, int DB, int WR>
+// The parts of a query's rows, joined: a wave a group of dims of RW rows at a time, as they were in the registers. A
+// workgroup does four groups, those from 4 blockIdx.y on, 4 (blockIdx.y + gridDim.y), ..
+template <bool F16, int DB, int RW, int WR>
 __global__ void __launch_bounds__(kThreads) hs_attend_join_kernel(const AttendArgs A) {
   constexpr int D = 32 * DB, kAhead = 8;
-  const int lane = threadIdx.x & 63, i = (int)uniform(threadIdx.x >> 6), rho = lane & 31, half = lane >> 5;
+  using St = State<DB, RW>;
+  const int lane = threadIdx.x & 63, rho = lane % RW, c = lane / RW;
   const uint32_t bh = fdiv(blockIdx.x, A.div_rows);
   const int rt = (int)(blockIdx.x - bh * A.row_tiles);
   const int b = (int)fdiv(bh, A.div_kv), h = (int)bh - b * A.kv;
   const int rows = nodes_of(A, b) * A.group;
-  if (rt * 32 >= rows) return;
+  if (rt * RW >= rows) return;
   const Plan plan(A, lane);
   const int before = plan.before(A, b), r0 = before / plan.per, r1 = (before + same(stages_of(A, b)) - 1) / plan.per;
   if (r0 == r1) return;  // one part
-  const int tile = rt / WR, row = rt * 32 + rho;
+  const int tile = rt / WR, row = rt * RW + rho;
   const int64_t base = (int64_t)(h * A.tiles + tile) * (2 * A.chunks);
-  auto place = [&](int r) -> int64_t {  // the first of the 32 rows of part r
-    return ((base + 2 * r + (before > r * plan.per ? 1 : 0)) * WR + (rt - tile * WR)) * 32;
+  auto place = [&](int r) -> int64_t {  // the first of the RW rows of part r
+    return ((base + 2 * r + (before > r * plan.per ? 1 : 0)) * WR + (rt - tile * WR)) * RW;
   };
   const int node = (int)fdiv((uint32_t)min(row, rows - 1), A.div_group), head = h * A.group + row - node * A.group;
-  for (int j = blockIdx.y; j < DB; j += gridDim.y) {
+  for (int n = 4 * blockIdx.y + (int)uniform(threadIdx.x >> 6); n < St::kGroups; n += 4 * gridDim.y) {
     float m = kLowest, l = 0.0f;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int r = r0; r <= r1; r += kAhead) {
@@ -710,7 +806,7 @@ __global__ void __launch_bounds__(kThreads) hs_attend_join_kernel(const AttendAr
         if (r + a <= r1) {
           const int64_t at = place(r + a);
           ml[a] = A.part_ml[at + rho];
-          y[a] = *reinterpret_cast<const f32x4*>(A.part + at * D + (4 * j + i) * 256 + 4 * lane);
+          y[a] = *reinterpret_cast<const f32x4*>(A.part + at * D + n * 256 + 4 * lane);
         }
       const float old = m;
 #pragma unroll
@@ -730,32 +826,33 @@ __global__ void __launch_bounds__(kThreads) hs_attend_join_kernel(const AttendAr
     }
     const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
     if (row < rows)
-      store4<F16>(A.out + b * A.ob + node * A.on + head * A.oh + 2 * (32 * j + 8 * i + 4 * half),
-                  f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv});
+      store4<F16>(A.out + b * A.ob + node * A.on + head * A.oh + 2 * (St::kDims * n + 4 * c), o * inv);
   }
 }
 
-template <bool F16, int DB, int WR, int NW>
+template <bool F16, int DB, int RW, int WR, int NW>
 void launch_rows(AttendArgs A, hipStream_t st) {
   const uint64_t groups = ((uint64_t)A.items + 7) / 8 * 8 * A.tiles;
   constexpr uint64_t kMost = kMostGroups / (NW / kWaves);
   for (uint64_t at = 0; at < groups; at += kMost) {
     A.group0 = (uint32_t)at;
-    hs_attend_kernel<F16, DB, WR, NW><<<(uint32_t)std::min<uint64_t>(groups - at, kMost), 64 * NW, 0, st>>>(A);
+    hs_attend_kernel<F16, DB, RW, WR, NW><<<(uint32_t)std::min<uint64_t>(groups - at, kMost), 64 * NW, 0, st>>>(A);
     if (hipPeekAtLastError() != hipSuccess) return;
   }
   if (!A.chunks) return;
   const uint32_t joins = (uint32_t)A.B * A.kv * A.row_tiles;  // (few: ranges are for few queries and heads)
-  hs_attend_join_kernel<F16, DB, WR><<<dim3(joins, joins < 512 ? DB : 1), kThreads, 0, st>>>(A);
+  hs_attend_join_kernel<F16, DB, RW, WR>
+      <<<dim3(joins, joins < 512 ? (State<DB, RW>::kGroups + 3) / 4 : 1), kThreads, 0, st>>>(A);
 }
 
 template <bool F16, int DB>
 void launch_dim(const AttendArgs& A, const AttendGeom& g, hipStream_t st) {
   if constexpr (DB <= 4)
-    if (g.wr == 8) return launch_rows<F16, DB, 8, 8>(A, st);
-  if (g.wr == 4) return launch_rows<F16, DB, 4, 4>(A, st);
-  if (g.wr == 2) return launch_rows<F16, DB, 2, 4>(A, st);
-  launch_rows<F16, DB, 1, 4>(A, st);
+    if (g.wr == 8) return launch_rows<F16, DB, 32, 8, 8>(A, st);
+  if (g.wr == 4) return launch_rows<F16, DB, 32, 4, 4>(A, st);
+  if (g.wr == 2) return launch_rows<F16, DB, 32, 2, 4>(A, st);
+  if (g.rw == 32) return launch_rows<F16, DB, 32, 1, 4>(A, st);
+  launch_rows<F16, DB, 16, 1, 4>(A, st);
 }
 
 template <bool F16>
@@ -785,11 +882,12 @@ bool attend_geom(int B, int M, int heads, int kv, int dim, int page, int slots, 
   g->kv = kv;
   g->dim = dim;
   const int rows = M * (heads / kv);
+  g->rw = rows > 16 ? 32 : 16;
   g->wr = rows > 128 && dim <= 128 ? 8 : rows > 64 ? 4 : rows > 32 ? 2 : 1;
-  g->tiles = (rows + 32 * g->wr - 1) / (32 * g->wr);
-  // Ranges for the workgroups that the device holds at once, two of 4 waves a CU or one of 8; a workgroup a query and
-  // head where there are four times as many of those.
-  const int64_t groups = (int64_t)B * kv * g->tiles, hold = g->wr == 8 || dim > 128 ? 256 : 512;
+  g->tiles = (rows + g->rw * g->wr - 1) / (g->rw * g->wr);
+  // Ranges for the workgroups that the device holds at once; a workgroup a query and head where there are four times as
+  // many of those.
+  const int64_t groups = (int64_t)B * kv * g->tiles, hold = 256 * waves_of(g->rw, dim) / (g->wr == 8 ? 2 : 1);
   const int64_t stages = ((int64_t)slots * page + 32 * kStage - 1) / (32 * kStage) * B;
   g->chunks = groups >= 4 * hold ? 0 : (int)std::min(std::max<int64_t>(hold / ((int64_t)kv * g->tiles), 1), stages);
   return groups < ((int64_t)1 << 30);
@@ -797,7 +895,7 @@ bool attend_geom(int B, int M, int heads, int kv, int dim, int page, int slots, 
 
 size_t attend_ws_bytes(const AttendGeom& g) {
   if (!g.chunks) return 0;
-  const size_t slots = (size_t)g.kv * g.tiles * (2 * g.chunks) * (32 * g.wr);
+  const size_t slots = (size_t)g.kv * g.tiles * (2 * g.chunks) * (g.rw * g.wr);
   return align256(slots * g.dim * sizeof(float)) + align256(slots * sizeof(float2));
 }
 
@@ -836,9 +934,9 @@ int launch_attend(const AttendGeom& g, const hs_tree_attention_args& a, hipStrea
   A.div_kv = make_fastdiv((uint32_t)g.kv);
   A.div_tiles = make_fastdiv((uint32_t)g.tiles);
   A.div_group = make_fastdiv((uint32_t)A.group);
-  A.row_tiles = (uint32_t)(g.M * A.group + 31) / 32;
+  A.row_tiles = (uint32_t)((g.M * A.group + g.rw - 1) / g.rw);
   A.div_rows = make_fastdiv(A.row_tiles);
-  const size_t slots = (size_t)g.kv * g.tiles * (2 * g.chunks) * (32 * g.wr);
+  const size_t slots = (size_t)g.kv * g.tiles * (2 * g.chunks) * (g.rw * g.wr);
   A.part = reinterpret_cast<float*>(a.workspace);
   A.part_ml = reinterpret_cast<float2*>(reinterpret_cast<char*>(a.workspace) +
                                         align256(slots * g.dim * sizeof(float)));

@@ -18,10 +18,10 @@ bool verify_geom(int B, int M, int64_t V, int dtype, bool drafter, VerifyGeom* g
 size_t verify_ws_bytes(const VerifyGeom& g);
 int launch_verify(const VerifyGeom& g, const hs_verify_args& a, hipStream_t stream);
 
-// How an attention is cut: `tiles` workgroups of 32 * wr rows of a cached head, and all queries' cached tokens into
+// How an attention is cut: `tiles` workgroups of rw * wr rows of a cached head, and all queries' cached tokens into
 // `chunks` ranges (0: a query is one).
 struct AttendGeom {
-  int B, M, heads, kv, dim, wr, tiles, chunks;
+  int B, M, heads, kv, dim, rw, wr, tiles, chunks;
 };
 bool attend_geom(int B, int M, int heads, int kv, int dim, int page, int slots, AttendGeom* g);
 size_t attend_ws_bytes(const AttendGeom& g);  // 0: none
