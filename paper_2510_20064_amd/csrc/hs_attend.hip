@@ -885,11 +885,16 @@ bool attend_geom(int B, int M, int heads, int kv, int dim, int page, int slots, 
   g->rw = rows > 16 ? 32 : 16;
   g->wr = rows > 128 && dim <= 128 ? 8 : rows > 64 ? 4 : rows > 32 ? 2 : 1;
   g->tiles = (rows + g->rw * g->wr - 1) / (g->rw * g->wr);
-  // Ranges for the workgroups that the device holds at once; a workgroup a query and head where there are four times as
-  // many of those.
+  // Ranges for the workgroups that the device holds at once; a workgroup a query and head, and no join, where there are
+  // four times as many of those, or where caches are so short that the join costs more than cutting them saves. us cut and
+  // whole at 8 heads of 128, one token: one query of 128 tokens 12.3 and 8.9, of 256 13.2 and 10.5, of 512 13.2 and 13.5;
+  // 32 queries of 512 18.6 and 14.2, of 1024 27.5 and 21.8. Trees of 61 nodes: one query of 128 tokens 20.8 and 17.3, of 512
+  // 22.1 and 30.9; 32 queries of 512 44.5 and 41.2. Longer caches are cut whatever their number: their lengths differ, and
+  // the longest alone would set the time (32 trees over up to 8192 tokens: 220 cut, 318 whole).
   const int64_t groups = (int64_t)B * kv * g->tiles, hold = 256 * waves_of(g->rw, dim) / (g->wr == 8 ? 2 : 1);
-  const int64_t stages = ((int64_t)slots * page + 32 * kStage - 1) / (32 * kStage) * B;
-  g->chunks = groups >= 4 * hold ? 0 : (int)std::min(std::max<int64_t>(hold / ((int64_t)kv * g->tiles), 1), stages);
+  const int64_t each = ((int64_t)slots * page + 32 * kStage - 1) / (32 * kStage);  // stages of a query
+  const bool whole = groups >= 4 * hold || each <= std::min<int64_t>(std::max<int64_t>(groups / 32, 2), 8);
+  g->chunks = whole ? 0 : (int)std::min(std::max<int64_t>(hold / ((int64_t)kv * g->tiles), 1), each * B);
   return groups < ((int64_t)1 << 30);
 }
 

@@ -340,6 +340,19 @@ def test_verify_large_trees(dtype, mode):
     assert got["length"].max() == depth + 1
 
 
+@pytest.mark.parametrize("mode", [hs.SAMPLE, hs.GREEDY])
+def test_verify_large_trees_of_long_rows(mode):
+    """Rows of more slices than a wave holds two a lane."""
+    note("verify large trees of long rows mode=%d" % mode)
+    g = torch.Generator().manual_seed(53)
+    B, M, V, depth = 6, 40, 300007, 2
+    z = rows(g, B, M, V, torch.bfloat16)
+    parent, token = tree(g, B, M, V, z)
+    parent = shallow(parent, depth)
+    for count in (None, torch.tensor([40, 0, 1, 2, 39, 17], dtype=torch.int32)):
+        check_verify(z, token, numbers(g, B, M), V, parent=parent, count=count, mode=mode, T=0.5, depth=depth)
+
+
 @pytest.mark.parametrize("dtype", list(DTYPES))
 @pytest.mark.parametrize("drafted", [False, True])
 def test_verify_large_chains(dtype, drafted):
@@ -441,6 +454,45 @@ def test_attention_sizes(dtype, M, heads, kv, dim, page, lengths):
     note("attention %s M=%d heads=%d/%d dim=%d page=%d %s" % (dtype, M, heads, kv, dim, page, lengths))
     Draft(M * 100 + heads + dim, len(lengths), M, heads, kv, dim, page, lengths, dtype).check()
     Draft(M * 100 + heads + dim + 1, len(lengths), M, heads, kv, dim, page, lengths, dtype, tree_=False).check()
+
+
+@pytest.mark.parametrize("M,heads,kv,dim,page,B,most", [
+    (1, 8, 8, 64, 32, 100, 1100), (1, 8, 8, 64, 32, 100, 500), (1, 2, 2, 32, 32, 300, 2000), (2, 16, 16, 32, 32, 200, 300),
+    (5, 20, 4, 64, 32, 70, 1100), (20, 8, 8, 64, 64, 66, 1300)])
+def test_attention_many_queries(M, heads, kv, dim, page, B, most):
+    """More queries than lanes, with lengths that differ widely, some of them zero."""
+    note("attention many M=%d heads=%d/%d dim=%d B=%d most=%d" % (M, heads, kv, dim, B, most))
+    g = torch.Generator().manual_seed(B + M)
+    lengths = [int(n) for n in (torch.rand(B, generator=g) ** 3 * most).long()]
+    lengths[0], lengths[B // 2], lengths[B - 1] = 0, most, 0
+    counts = [int(n) for n in torch.randint(0, M + 1, (B,), generator=g)]
+    Draft(B, B, M, heads, kv, dim, page, lengths, torch.bfloat16).check()
+    Draft(B, B, M, heads, kv, dim, page, lengths, torch.float16, counts=counts).check()
+
+
+@pytest.mark.parametrize("M,heads,kv,dim,page,lengths", [
+    (4, 4, 1, 64, 32, [700, 5]), (17, 1, 1, 64, 32, [700, 5]), (16, 2, 1, 128, 32, [300, 1]), (11, 3, 1, 128, 64, [300, 64]),
+    (64, 1, 1, 128, 32, [400]), (13, 5, 1, 128, 32, [400, 0]), (64, 2, 1, 128, 64, [600]), (43, 3, 1, 128, 64, [600]),
+    (64, 4, 1, 128, 64, [600]), (52, 5, 1, 128, 64, [600, 9]), (64, 8, 1, 192, 64, [333, 64]), (64, 16, 2, 256, 32, [77]),
+    (33, 4, 1, 160, 32, [500])])
+@pytest.mark.parametrize("slots", [0, 40])
+def test_attention_row_counts(M, heads, kv, dim, page, lengths, slots):
+    """Rows of a head on both sides of each variant's size, with tables for short and for long caches."""
+    note("attention rows M=%d heads=%d/%d dim=%d slots=%d" % (M, heads, kv, dim, slots))
+    d = Draft(M + heads, len(lengths), M, heads, kv, dim, page, lengths, torch.bfloat16)
+    if slots:
+        wide = torch.full((len(lengths), max(slots, d.table.shape[1])), -1, dtype=torch.int32)
+        wide[:, :d.table.shape[1]] = d.table
+        d.table = wide
+    d.check()
+
+
+@pytest.mark.parametrize("M", [1, 30])
+@pytest.mark.parametrize("tokens", [127, 128, 129, 255, 256, 257, 384, 1023, 1025])
+def test_attention_short_and_long_tables(M, tokens):
+    note("attention tables of %d tokens M=%d" % (tokens, M))
+    d = Draft(tokens + M, 2, M, 4, 2, 64, 32, [tokens, tokens // 2], torch.float16)
+    d.check()
 
 
 def test_attention_counts():
