@@ -11,9 +11,11 @@
 //
 // Launches:
 //   1. hs_verify_rows_kernel, a wave per slice of a row: of its weights the sum, relative to its largest logit,
-//      without the tokens of the row's children;
-//   2. hs_verify_walk_kernel, a workgroup per query: every node's normaliser and accepted child, a wave a node;
-//      the path; of its last row the slice in which the running sum passes, read again for the token;
+//      without the tokens of the row's children. Every node's row in one launch, or, of a large tree (by_levels), a
+//      launch per level for the nodes that the level before accepted: no row off the paths is read;
+//   2. hs_verify_walk_kernel, a workgroup per query: the normaliser and accepted child of every node that has children,
+//      a wave a node; the path; of its last row the slice in which the running sum passes, read again for the token.
+//      Behind levels the path is known, and a wave a query does the rest;
 //   3. with a drafter hs_verify_rest_kernel, a wave per slice of the two rows where the path ended at a rejection:
 //      the sum of max(0, p - q); and hs_verify_draw_kernel, a workgroup per query: the token.
 //
@@ -21,6 +23,12 @@
 // probability, so weights and sums are fp64 and an exponential good to 1.1e-12 of itself: a draw from a flat row of
 // 152 thousand tokens differs from exact arithmetic once in 6 million (with fp32 exponentials, whose errors leave
 // 3.5e-9 in a slice's sum, about once in 2000).
+//
+// What bounds it. Few rows: the launches and the latencies of a row read twice (a chain of 5 tokens over 4 thousand fp32
+// 14 us in four launches; 61 nodes over 152 thousand bf16 10 in the rows and 12 in the walk). Many: the fp64 rate in the
+// rows kernel, at ten instructions a logit (64 chains of 8 tokens and their drafter, 128256 bf16: 123 million logits in
+// 106 to 125 us, 1.0 to 1.2 a ps, 2.3 TB/s; with seventeen, 123 to 140), then 11 for the walk and 24 for what a rejection
+// leaves. 32 trees of 61 nodes by levels: 60, eight launches of 2.6 to 7.
 #include <algorithm>
 #include <cfloat>
 
@@ -64,6 +72,7 @@ struct VerifyArgs {
   int32_t* cur;      // [depth + 1][B]: the nodes on the paths, then -1
   FastDiv divS, divM;
   double c;
+  float reach;       // 120 / c
   const int32_t* token;
   const int32_t* parent;
   const int32_t* count;
@@ -91,6 +100,43 @@ __device__ inline double weight_of(double d) {
   p = fma(p, f, 1.0);
   return ldexp(p, (int)n);
 }
+// 2^(i / 128): by the series of the exponential, from its least term on.
+struct Powers {
+  double at[128];
+};
+constexpr Powers powers_of_two() {
+  Powers t{};
+  for (int i = 0; i < 128; ++i) {
+    const double x = i * (0.6931471805599453094 / 128);
+    double p = 1.0;
+    for (int k = 24; k >= 1; --k) p = 1.0 + x / k * p;
+    t.at[i] = p;
+  }
+  return t;
+}
+__device__ const Powers kPowers = powers_of_two();
+
+// weight_of(z, m) added to `sum`, for a row's largest logit m, by ten instructions in fp64 instead of seventeen:
+// d = (z - m) c is rounded to a multiple k of 1/128 by adding 1.5 * 2^45, whose last bits are then 128 k; the rest
+// r = d - k, |r| <= 2^-8, is exact, 2^r by the polynomial of degree 3 that has 2^r's value and slope at 0 and meets it at
+// +-0.91 2^-8 (3.9e-13 of itself, and 1 at 0: a flat row's weights are 1), and 2^k a power from LDS and an exponent.
+// Below `low`, 120 under the largest, weights are 2^-120: they do not reach a sum that holds 1. NaN stays.
+struct Sums {
+  const double* powers;
+  double c, m;
+  float low;
+  __device__ void add(float z, double& sum) const {
+    const double x = (double)(z < low ? low : z) - m, s = fma(x, c, 0x1.8p45), r = fma(x, c, 0x1.8p45 - s);
+    const int k = (int)(uint32_t)(uint64_t)__double_as_longlong(s);
+    const uint64_t t = (uint64_t)__double_as_longlong(powers[k & 127]);
+    const uint32_t hi = (uint32_t)(t >> 32) + ((uint32_t)(k & ~127) << 13);
+    double p = 5.55041255195012004e-02;
+    p = fma(p, r, 2.40226628539921244e-01);
+    p = fma(p, r, 6.93147180559945286e-01);
+    p = fma(p, r, 1.0);
+    sum = fma(__longlong_as_double((long long)(((uint64_t)hi << 32) | (uint32_t)t)), p, sum);
+  }
+};
 __device__ inline double weight_of(float z, float m, double c) {
   return weight_of(((double)z - (double)m) * c);
 }
@@ -449,8 +495,13 @@ __global__ void __launch_bounds__(kThreads) hs_verify_rows_kernel(const VerifyAr
   }
   if (n + (q ? 1 : 0) >= count) return;
   const char* x = q ? A.y + b * A.tb + n * A.tn : A.x + b * A.sb + n * A.sn;
+  __shared__ double2 s_powers[GREEDY ? 1 : kWaves][64];  // a wave's own: the table arrives with its logits
+  const int wv = (int)uniform(threadIdx.x >> 6);
+  double2 power;
+  if (!GREEDY) power = reinterpret_cast<const double2*>(kPowers.at)[lane];
   float z[kLoads][E];
   load_slice<DT>(x, slice, lane, A, z);
+  if (!GREEDY) s_powers[wv][lane] = power;
   const int first = slice * kVerifySlice * E;
   if (!GREEDY && !A.y) {  // the children's tokens have no weight
     const Draft draft(A, b, count, lane);
@@ -492,10 +543,20 @@ __global__ void __launch_bounds__(kThreads) hs_verify_rows_kernel(const VerifyAr
   }
   const float ref = m == -INFINITY ? 0.0f : m;
   double s[4] = {0.0, 0.0, 0.0, 0.0};
+  // (beyond 2^16 the last bit of m is not far below 120 / c)
+  if (uniform((uint32_t)(m > -INFINITY && fabs((double)m * A.c) <= 65536.0))) {
+    lds_wave_fence();
+    const Sums by{reinterpret_cast<const double*>(s_powers[wv]), A.c, (double)m, m - A.reach};
 #pragma unroll
-  for (int i = 0; i < kLoads; ++i)
+    for (int i = 0; i < kLoads; ++i)
 #pragma unroll
-    for (int e = 0; e < E; ++e) s[e & 3] += weight_of(z[i][e], ref, A.c);
+      for (int e = 0; e < E; ++e) by.add(z[i][e], s[e & 3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+      for (int e = 0; e < E; ++e) s[e & 3] += weight_of(z[i][e], ref, A.c);
+  }
   const double sum = wave_sum_d((s[0] + s[1]) + (s[2] + s[3]));
   if (lane == 0) *out = Part{sum, m, 0};
 }
@@ -725,6 +786,7 @@ int launch_verify(const VerifyGeom& g, const hs_verify_args& a, hipStream_t stre
   ws += align256((size_t)g.B * g.M * sizeof(int32_t));
   A.rest_part = reinterpret_cast<Part*>(ws);
   A.end = reinterpret_cast<End*>(ws + align256((size_t)g.B * g.S * sizeof(Part)));
+  A.reach = (float)(120.0 / A.c);
   if (greedy) A.c = 0.0;
   if (g.dtype == HS_F32) greedy ? launch_of<HS_F32, true>(A, levels, stream) : launch_of<HS_F32, false>(A, levels, stream);
   else if (g.dtype == HS_F16) greedy ? launch_of<HS_F16, true>(A, levels, stream) : launch_of<HS_F16, false>(A, levels, stream);
