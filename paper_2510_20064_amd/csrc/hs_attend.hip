@@ -6,15 +6,32 @@
 // The values' scales go into the weights: with x_rt = s_rt + log2 vs_t, w_rt = 2^(x_rt - m_r) and m_r following the
 // largest x, o_r = sum w v / sum w / vs: a weight is rounded relative to what it adds, whatever its page's scale.
 //
-// Layout. Products are S^T = K Q^T and O^T = V^T P^T on 32 x 32 x 16 tiles, so that a row's scores, weights,
-// maximum and sum all stay in the two lanes (r, r + 32) that hold its column, and the weights are the second
-// product's operand as they stand: the scores' registers of lane half h are tokens 16 h .. 16 h + 15 of a tile of
-// 32 if the tile's K rows are taken in the order pi below. A page holds its values by dimension, so those 16 tokens
-// of one dimension are one 16-byte load. No operand goes through LDS.
+// Layout. Products are S^T = K Q^T and O^T = V^T P^T, so that a row's scores, weights, maximum and sum all stay in the
+// lanes that hold its column, and the weights are the second product's operand as they stand: the scores' registers of a
+// lane are consecutive tokens of a tile of 32 if the tile's K rows are taken in the order of row_of. A page holds its
+// values by dimension, so those tokens of one dimension are 16 (8) bytes in a row. Tiles are 32 x 32 x 16 with 32 rows a
+// wave, or 16 x 16 x 32 with 16 for up to 16 rows: a third less registers and half the exponentials, three waves a SIMD
+// where there are two (32 single tokens over 16 thousand: 128 us and 118 to 120; four waves spill, 187; two, 118, lose on
+// short caches).
+// A workgroup brings stages of four tiles to LDS, the next one on its way to registers: its waves share a stage's rows of
+// queries or its tiles. From memory to registers without LDS, each wave its own tiles, a load of keys took 32 bytes of 32
+// lines (61 nodes over 16 thousand tokens 101 us and 46, 32 such over 8 thousand 509 and 230).
 // Codes of 8 bits become bf16 or fp16 without error (3 bits of mantissa, 2^-9 to 448), one instruction for two.
-// Weights are rounded to fp16 (relative 2^-12, half of a bf16 query's own rounding), as 2^12 w, so that what lies
+// Weights are rounded to fp16 (relative 2^-11, an eighth of a bf16 output's own rounding), as 2^12 w, so that what lies
 // below 2^-36 of the largest is lost and not what lies below 2^-24; m follows only in steps above 2^3 (w stays
 // below 2^16), which spares most tiles the multiplication of O. Sums and O are fp32.
+//
+// Split. The stages of all queries are cut into as many equal ranges as the device holds workgroups, so that lengths that
+// differ, and one query alone, load it alike; what a range holds of a query that others share goes to the workspace, and
+// hs_attend_join_kernel adds the parts in their order. See attend_geom for when a query is a workgroup's instead.
+//
+// What bounds it, heads of 128, eight cached for 32. One token over 512: two launches and four dependent reads (length,
+// table, scales, codes), 13 us. 32 tokens over up to 16 thousand, 537 MB: the memory, 116 to 119 us with the join's 6,
+// 4.6 TB/s, where a large copy reaches 5.9. 32 trees of 61 nodes over up to 8 thousand, 131 GFLOP: 216 to 231 us, 0.6
+// PFLOP/s: a tile of 32 tokens and 32 rows is 16 products of 16 passes and some 200 vector instructions (16 exponentials of
+// four cycles each a lane, 64 conversions), which a wave does one after the other, and the two waves that a SIMD holds do
+// not fill each other's waits. No gain: two tiles at once or one, the next tile's scores before this one's weights, other
+// wave priorities, the values' loads before the softmax; 64 rows a wave spill.
 #include <algorithm>
 #include <cfloat>
 
@@ -37,11 +54,10 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr float kHeadroom = 12.0f;  // weights are held as 2^12 w
 constexpr float kSlack = 3.0f;      // m follows a maximum more than this above it
 constexpr float kLowest = -1.7e38f; // m before the first token
-constexpr int kWaves16 = 3;
 constexpr int kStage = 4;           // tiles of 32 tokens that a workgroup brings to LDS at once
 
 // Waves of a SIMD, by the registers that they take.
-constexpr int waves_of(int rw, int dim) { return dim > 128 ? rw == 16 ? 2 : 1 : rw == 16 ? kWaves16 : 2; }
+constexpr int waves_of(int rw, int dim) { return dim > 128 ? rw == 16 ? 2 : 1 : rw == 16 ? 3 : 2; }
 
 struct AttendArgs {
   const char* q;
@@ -893,7 +909,8 @@ bool attend_geom(int B, int M, int heads, int kv, int dim, int page, int slots, 
   // the longest alone would set the time (32 trees over up to 8192 tokens: 220 cut, 318 whole).
   const int64_t groups = (int64_t)B * kv * g->tiles, hold = 256 * waves_of(g->rw, dim) / (g->wr == 8 ? 2 : 1);
   const int64_t each = ((int64_t)slots * page + 32 * kStage - 1) / (32 * kStage);  // stages of a query
-  const bool whole = groups >= 4 * hold || each <= std::min<int64_t>(std::max<int64_t>(groups / 32, 2), 8);
+  const bool whole = groups >= 4 * hold || each * B >= 1 << 30 ||  // (the stages of all are counted in 32 bits)
+                     each <= std::min<int64_t>(std::max<int64_t>(groups / 32, 2), 8);
   g->chunks = whole ? 0 : (int)std::min(std::max<int64_t>(hold / ((int64_t)kv * g->tiles), 1), each * B);
   return groups < ((int64_t)1 << 30);
 }
