@@ -27,11 +27,13 @@
 //
 // What bounds it, heads of 128, eight cached for 32. One token over 512: two launches and four dependent reads (length,
 // table, scales, codes), 13 us. 32 tokens over up to 16 thousand, 537 MB: the memory, 116 to 119 us with the join's 6,
-// 4.6 TB/s, where a large copy reaches 5.9. 32 trees of 61 nodes over up to 8 thousand, 131 GFLOP: 216 to 231 us, 0.6
-// PFLOP/s: a tile of 32 tokens and 32 rows is 16 products of 16 passes and some 200 vector instructions (16 exponentials of
-// four cycles each a lane, 64 conversions), which a wave does one after the other, and the two waves that a SIMD holds do
-// not fill each other's waits. No gain: two tiles at once or one, the next tile's scores before this one's weights, other
-// wave priorities, the values' loads before the softmax; 64 rows a wave spill.
+// 4.6 TB/s, where a large copy reaches 4.8. 32 trees of 61 nodes over up to 8 thousand, 131 GFLOP: 208 to 220 us, 0.6
+// PFLOP/s, where a large product reaches 1.4: a wave does a tile's two products (16 of 32 cycles), its softmax (16
+// exponentials, some 60 other instructions) and its 16 to 32 reads of LDS one after the other, and the two waves that the
+// registers leave a SIMD fill half of each other's waits; no part of them takes more than an eighth of the time. No gain:
+// two tiles at once or one, the next tile's scores before this one's weights, a product's operands read under the
+// softmax before it, two buffers and one barrier a stage, other wave priorities, the values' loads before the softmax;
+// 64 rows a wave spill.
 #include <algorithm>
 #include <cfloat>
 
@@ -261,10 +263,13 @@ __device__ inline int valid_of(int pages, int t, int sub, int tokens) {
 
 // A stage on its way to LDS. A tile's keys are 32 * D bytes one behind the other, its values D rows of 32 bytes; a wave
 // brings pieces of 1 KB of both. In LDS a row is 16 bytes longer than what it holds: an odd number of 16 bytes, so that 16
-// lanes that read 16 bytes of consecutive rows each use all banks once.
-template <int DB>
+// lanes that read 16 bytes of consecutive rows each use all banks once. WIDE, where each of eight waves reads every tile:
+// the codes are widened on the way to LDS, once instead of by each wave (32 trees of 61 nodes 230 us and 219, at twice
+// the bytes; with four waves no gain).
+template <int DB, bool WIDE>
 struct Staged {
-  static constexpr int kKeyPitch = 32 * DB + 16, kValuePitch = 32 * kStage + 16;
+  static constexpr int kCode = WIDE ? 2 : 1;  // bytes
+  static constexpr int kKeyPitch = 32 * DB * kCode + 16, kValuePitch = 32 * kStage * kCode + 16;
   static constexpr int kKeys = 32 * kStage * kKeyPitch, kBytes = kKeys + 32 * DB * kValuePitch;
 };
 template <int DB, int NW>
@@ -287,10 +292,10 @@ __device__ __forceinline__ void load_stage(const AttendArgs& A, int h, int t, in
   }
 }
 // pages, t, tokens: of the stage. What lies behind the last token may be any code: its values are held as 0.
-template <int RW, int DB, int NW>
+template <bool F16, int RW, int DB, int NW, bool WIDE>
 __device__ __forceinline__ void store_stage(uint8_t* lds, int t, int pages, int tokens, int wv, int lane,
                                             Loads<DB, NW>& L) {
-  using St = Staged<DB>;
+  using St = Staged<DB, WIDE>;
 #pragma unroll
   for (int i = 0; i < L.kN; ++i) {
     const int piece = wv + NW * i, sub = piece / DB, part = piece - sub * DB;
@@ -305,9 +310,29 @@ __device__ __forceinline__ void store_stage(uint8_t* lds, int t, int pages, int 
       }
     }
     const int q = part * 64 + lane, token = q / (2 * DB), c = q - token * (2 * DB);
-    *reinterpret_cast<u32x4*>(lds + (32 * sub + row_of<RW>(token)) * St::kKeyPitch + 16 * c) = L.k[i];
-    *reinterpret_cast<u32x4*>(lds + St::kKeys + (32 * part + (lane >> 1)) * St::kValuePitch + 32 * sub + 16 * (lane & 1)) =
-        L.v[i];
+    uint8_t* kp = lds + (32 * sub + row_of<RW>(token)) * St::kKeyPitch + 16 * c * St::kCode;
+    uint8_t* vp = lds + St::kKeys + (32 * part + (lane >> 1)) * St::kValuePitch + (32 * sub + 16 * (lane & 1)) * St::kCode;
+    if constexpr (WIDE) {
+      reinterpret_cast<V8<F16>*>(kp)[0] = widen<F16>(L.k[i].x, L.k[i].y);
+      reinterpret_cast<V8<F16>*>(kp)[1] = widen<F16>(L.k[i].z, L.k[i].w);
+      reinterpret_cast<f16x8*>(vp)[0] = widen<true>(L.v[i].x, L.v[i].y);
+      reinterpret_cast<f16x8*>(vp)[1] = widen<true>(L.v[i].z, L.v[i].w);
+    } else {
+      *reinterpret_cast<u32x4*>(kp) = L.k[i];
+      *reinterpret_cast<u32x4*>(vp) = L.v[i];
+    }
+  }
+}
+// Sixteen staged codes, as two operands.
+template <bool F16, bool WIDE>
+__device__ __forceinline__ void operands(const uint8_t* at, V8<F16> (&x)[2]) {
+  if constexpr (WIDE) {
+    x[0] = reinterpret_cast<const V8<F16>*>(at)[0];
+    x[1] = reinterpret_cast<const V8<F16>*>(at)[1];
+  } else {
+    const u32x4 c = *reinterpret_cast<const u32x4*>(at);
+    x[0] = widen<F16>(c.x, c.y);
+    x[1] = widen<F16>(c.z, c.w);
   }
 }
 
@@ -374,20 +399,21 @@ constexpr float kLeast = 1e-30f;  // the least factor of a product: infinite one
 
 // N tiles of the stage in LDS from the `sub`-th on, of valid[n] tokens each: their products, which do not wait for each
 // other, then one step of the softmax.
-template <bool F16, int DB, int N>
+template <bool F16, int DB, int N, bool WIDE>
 __device__ __forceinline__ void attend_tiles(const AttendArgs& A, const V8<F16> (&q)[2 * DB], const uint8_t* lds, int sub,
                                              const int (&valid)[N], float scales, int lane, State<DB, 32>& S) {
-  using St = Staged<DB>;
+  using St = Staged<DB, WIDE>;
   const int rho = lane & 31, half = lane >> 5;
-  const uint8_t* kp = lds + (32 * sub + rho) * St::kKeyPitch + 16 * half;
+  const uint8_t* kp = lds + (32 * sub + rho) * St::kKeyPitch + 16 * half * St::kCode;
   f32x16 s[N] = {};
 #pragma unroll
   for (int j = 0; j < DB; ++j)
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      const u32x4 k = *reinterpret_cast<const u32x4*>(kp + 32 * n * St::kKeyPitch + 32 * j);
-      s[n] = mfma(widen<F16>(k.x, k.y), q[2 * j], s[n]);
-      s[n] = mfma(widen<F16>(k.z, k.w), q[2 * j + 1], s[n]);
+      V8<F16> k[2];
+      operands<F16, WIDE>(kp + 32 * n * St::kKeyPitch + 32 * j * St::kCode, k);
+      s[n] = mfma(k[0], q[2 * j], s[n]);
+      s[n] = mfma(k[1], q[2 * j + 1], s[n]);
     }
   float f[N], bias[N], inv[N], top = -INFINITY;
 #pragma unroll
@@ -423,14 +449,15 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& A, const V8<F16> 
     p[n][0] = narrow(x);
     p[n][1] = narrow(x + 8);
   }
-  const uint8_t* vp = lds + St::kKeys + rho * St::kValuePitch + 32 * sub + 16 * half;
+  const uint8_t* vp = lds + St::kKeys + rho * St::kValuePitch + (32 * sub + 16 * half) * St::kCode;
 #pragma unroll
   for (int n = 0; n < N; ++n)
 #pragma unroll
     for (int j = 0; j < DB; ++j) {
-      const u32x4 v = *reinterpret_cast<const u32x4*>(vp + 32 * j * St::kValuePitch + 32 * n);
-      S.o32[j] = mfma(widen<true>(v.x, v.y), p[n][0], S.o32[j]);
-      S.o32[j] = mfma(widen<true>(v.z, v.w), p[n][1], S.o32[j]);
+      f16x8 v[2];
+      operands<true, WIDE>(vp + 32 * j * St::kValuePitch + 32 * n * St::kCode, v);
+      S.o32[j] = mfma(v[0], p[n][0], S.o32[j]);
+      S.o32[j] = mfma(v[1], p[n][1], S.o32[j]);
     }
 }
 
@@ -438,7 +465,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& A, const V8<F16> 
 template <bool F16, int DB>
 __device__ __forceinline__ void attend_tiles(const AttendArgs& A, const V8<F16> (&q)[DB], const uint8_t* lds, int sub,
                                              const int (&valid)[1], float scales, int lane, State<DB, 16>& S) {
-  using St = Staged<DB>;
+  using St = Staged<DB, false>;
   const int rho = lane & 15, g = lane >> 4;
   const uint8_t* kp = lds + (32 * sub + rho) * St::kKeyPitch + 8 * g;
   f32x4 s[2] = {};
@@ -682,7 +709,7 @@ __device__ __forceinline__ void attend_range(const AttendArgs& A, int b, int h, 
 
   for (int t = first; t < last; t += kStage) {
     if (t > first) __syncthreads();  // the stage before is read
-    store_stage<RW, DB, NW>(s_stage, t, pages, tokens, wv, lane, L);
+    store_stage<F16, RW, DB, NW, WR == 8>(s_stage, t, pages, tokens, wv, lane, L);
     const int here = pages;
     const float scales = coming;
     pages = next;
@@ -700,7 +727,7 @@ __device__ __forceinline__ void attend_range(const AttendArgs& A, int b, int h, 
       int valid[N];
 #pragma unroll
       for (int n = 0; n < N; ++n) valid[n] = valid_of(here, t, sub + n, tokens);
-      if constexpr (RW == 32) attend_tiles<F16, DB, N>(A, q, s_stage, sub, valid, scales, lane, S);
+      if constexpr (RW == 32) attend_tiles<F16, DB, N, WR == 8>(A, q, s_stage, sub, valid, scales, lane, S);
       else attend_tiles<F16, DB>(A, q, s_stage, sub, valid, scales, lane, S);
     }
   }
@@ -758,7 +785,7 @@ __device__ __forceinline__ void attend_range(const AttendArgs& A, int b, int h, 
 template <bool F16, int DB, int RW, int WR, int NW>
 __global__ void __launch_bounds__(64 * NW, waves_of(RW, 32 * DB)) hs_attend_kernel(const AttendArgs A) {
   constexpr int kPitch = 32 * DB + 4, WT = NW / WR;
-  using St = Staged<DB>;
+  using St = Staged<DB, WR == 8>;
   constexpr int kBytes = St::kBytes > Nodes<DB>::kBytes ? St::kBytes : Nodes<DB>::kBytes;
   __shared__ __attribute__((aligned(16))) uint8_t s_stage[kBytes];
   static_assert(WT == 1 || kBytes >= WT / 2 * WR * RW * kPitch * 4, "the join shares the stage's memory");
