@@ -818,10 +818,15 @@ __global__ void __launch_bounds__(64 * NW, waves_of(RW, 32 * DB)) hs_attend_kern
   }
 }
 // The parts of a query's rows, joined: a wave a group of dims of RW rows at a time, as they were in the registers. A
-// workgroup does four groups, those from 4 blockIdx.y on, 4 (blockIdx.y + gridDim.y), ..
-template <bool F16, int DB, int RW, int WR>
-__global__ void __launch_bounds__(kThreads) hs_attend_join_kernel(const AttendArgs A) {
+// workgroup does four groups, those from 4 blockIdx.y on, 4 (blockIdx.y + gridDim.y), .. With W > 1 it does one group,
+// blockIdx.y, its W waves every W-th part each, joined through LDS: a wave alone reads eight parts at a time (one query's
+// call, eight heads: one token over 4096, 32 parts, 16.5 us and by four waves 14.2; over 32768, 96 parts, 32.8 and by
+// sixteen 25.6; a tree of 61 nodes, whose 33 MB of parts are the bound, 45.2 and 45.3).
+template <bool F16, int DB, int RW, int WR, int W>
+__global__ void __launch_bounds__(W > 1 ? 64 * W : kThreads) hs_attend_join_kernel(const AttendArgs A) {
   constexpr int D = 32 * DB, kAhead = 8;
+  __shared__ f32x4 s_o[W > 1 ? W : 1][64];
+  __shared__ float2 s_ml[W > 1 ? W : 1][64];
   using St = State<DB, RW>;
   const int lane = threadIdx.x & 63, rho = lane % RW, c = lane / RW;
   const uint32_t bh = fdiv(blockIdx.x, A.div_rows);
@@ -838,34 +843,52 @@ __global__ void __launch_bounds__(kThreads) hs_attend_join_kernel(const AttendAr
     return ((base + 2 * r + (before > r * plan.per ? 1 : 0)) * WR + (rt - tile * WR)) * RW;
   };
   const int node = (int)fdiv((uint32_t)min(row, rows - 1), A.div_group), head = h * A.group + row - node * A.group;
-  for (int n = 4 * blockIdx.y + (int)uniform(threadIdx.x >> 6); n < St::kGroups; n += 4 * gridDim.y) {
+  const int wv = (int)uniform(threadIdx.x >> 6), r00 = W > 1 ? r0 + wv : r0;
+  for (int n = W > 1 ? blockIdx.y : 4 * blockIdx.y + wv; n < St::kGroups; n += W > 1 ? St::kGroups : 4 * gridDim.y) {
     float m = kLowest, l = 0.0f;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int r = r0; r <= r1; r += kAhead) {
+    for (int r = r00; r <= r1; r += W * kAhead) {
       f32x4 y[kAhead];
       float2 ml[kAhead];
 #pragma unroll
       for (int a = 0; a < kAhead; ++a)
-        if (r + a <= r1) {
-          const int64_t at = place(r + a);
+        if (r + W * a <= r1) {
+          const int64_t at = place(r + W * a);
           ml[a] = A.part_ml[at + rho];
           y[a] = *reinterpret_cast<const f32x4*>(A.part + at * D + n * 256 + 4 * lane);
         }
       const float old = m;
 #pragma unroll
       for (int a = 0; a < kAhead; ++a)
-        if (r + a <= r1) m = fmaxf(m, ml[a].x);
+        if (r + W * a <= r1) m = fmaxf(m, ml[a].x);
       const float less = __builtin_amdgcn_exp2f(old - m);
       l *= less;
       o *= less;
 #pragma unroll
       for (int a = 0; a < kAhead; ++a)
-        if (r + a <= r1) {
+        if (r + W * a <= r1) {
           const float f = __builtin_amdgcn_exp2f(ml[a].x - m);
           l = fmaf(ml[a].y, f, l);
 #pragma unroll
           for (int k = 0; k < 4; ++k) o[k] = fmaf(y[a][k], f, o[k]);
         }
+    }
+    if constexpr (W > 1) {
+      s_o[wv][lane] = o;
+      s_ml[wv][lane] = make_float2(m, l);
+      __syncthreads();
+      if (wv != 0) return;
+#pragma unroll
+      for (int w = 1; w < W; ++w) m = fmaxf(m, s_ml[w][lane].x);
+      l = 0.0f;
+      o = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        const float f = __builtin_amdgcn_exp2f(s_ml[w][lane].x - m);
+        l = fmaf(s_ml[w][lane].y, f, l);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[k] = fmaf(s_o[w][lane][k], f, o[k]);
+      }
     }
     const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
     if (row < rows)
@@ -884,8 +907,11 @@ void launch_rows(AttendArgs A, hipStream_t st) {
   }
   if (!A.chunks) return;
   const uint32_t joins = (uint32_t)A.B * A.kv * A.row_tiles;  // (few: ranges are for few queries and heads)
-  hs_attend_join_kernel<F16, DB, RW, WR>
-      <<<dim3(joins, joins < 512 ? (State<DB, RW>::kGroups + 3) / 4 : 1), kThreads, 0, st>>>(A);
+  constexpr int kGroups = State<DB, RW>::kGroups;
+  const int parts = A.chunks / A.B;  // of a query, where lengths are alike
+  if (parts > 32) hs_attend_join_kernel<F16, DB, RW, WR, 16><<<dim3(joins, kGroups), 1024, 0, st>>>(A);
+  else if (parts > 8) hs_attend_join_kernel<F16, DB, RW, WR, 4><<<dim3(joins, kGroups), 256, 0, st>>>(A);
+  else hs_attend_join_kernel<F16, DB, RW, WR, 1><<<dim3(joins, joins < 512 ? (kGroups + 3) / 4 : 1), kThreads, 0, st>>>(A);
 }
 
 template <bool F16, int DB>
