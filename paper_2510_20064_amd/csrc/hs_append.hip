@@ -29,7 +29,7 @@ struct AppendArgs {
 };
 
 constexpr float kTop = 448.0f;
-constexpr int kHold = 2;                     // squares of a thread that stay in registers
+constexpr int kHold = 2;                     // squares of a thread
 constexpr int kSlab = 64;                  // dims of a page's values that are in LDS at once
 constexpr int kPitch = HS_MAX_PAGE / 4 + 1;  // words of a dim
 constexpr uint32_t kNan8 = 0x7F;
@@ -89,12 +89,16 @@ __device__ inline void transpose4(uint32_t a, uint32_t b, uint32_t c, uint32_t d
 }
 
 // The largest x >= 0 of the workgroup.
+template <int NT>
 __device__ inline uint32_t largest(int x, int* s_most) {
   x = wave_max_i(x);
   __syncthreads();  // (the one before is read)
   if ((threadIdx.x & 63) == 0) s_most[threadIdx.x >> 6] = x;
   __syncthreads();
-  return (uint32_t)max(max(s_most[0], s_most[1]), max(s_most[2], s_most[3]));
+  x = s_most[0];
+#pragma unroll
+  for (int w = 1; w < NT / 64; ++w) x = max(x, s_most[w]);
+  return (uint32_t)x;
 }
 
 // The least power of two s with most <= 448 s, from 2^-40 to 2^40: most = a 2^e with 1/2 <= a < 1, 448 = 7/8 2^9.
@@ -105,16 +109,17 @@ __device__ inline float scale_of(float most) {
 }
 
 // The work is cut in squares of four tokens and eight dims, a thread a square, so that consecutive lanes read consecutive
-// bytes of a row; a thread's first kHold squares stay in registers between the pass for the largest and the pass that
-// writes (a page of 128 tokens of 128 dims; what does not fit is read again). A square's values by dimension are words of
-// four tokens: through LDS, so that consecutive lanes write consecutive words of a dimension.
+// bytes of a row. A workgroup has 256, 512 or 1024 threads, as many as hold a page's squares two a thread (1024: a page of
+// 256 tokens of 256 dims) in registers between the pass for the largest and the pass that writes. A square's values by
+// dimension are words of four tokens: through LDS, so that consecutive lanes write consecutive words of a dimension.
 // Bound: 8 prompts of 8192 tokens of 8 heads of 128 (302 MB read and written) 87 us, 3.5 TB/s; waiting for the chain
 // count, length, table, rows (73% of the waves' time) with the five workgroups a CU holds. Values written from the squares, 4
 // bytes a row, 127; every value tested for infinities and clamped, 145; both of the writing loops in one, with 168
-// registers, 122.
-template <bool F16>
-__global__ void __launch_bounds__(kThreads) hs_append_kernel(const AppendArgs A) {
-  __shared__ int s_most[kWaves];
+// registers, 122; one square a thread of twice the threads 112. Pages of 256 tokens of 256 dims by 256 threads, which read
+// twice what they do not hold, 63 us for two prompts of 7420 tokens and four heads, by 1024 27.
+template <bool F16, int NT>
+__global__ void __launch_bounds__(NT) hs_append_kernel(const AppendArgs A) {
+  __shared__ int s_most[NT / 64];
   __shared__ uint32_t s_words[kSlab * kPitch];
   const uint32_t unit = A.group0 + blockIdx.x;
   if (unit >= A.units) return;
@@ -166,20 +171,15 @@ __global__ void __launch_bounds__(kThreads) hs_append_kernel(const AppendArgs A)
 #pragma unroll
   for (int i = 0; i < kHold; ++i) {
     held[i][0] = held[i][1] = held[i][2] = held[i][3] = make_uint4(0, 0, 0, 0);
-    if (t + kThreads * i < squares) load(t + kThreads * i, held[i]);
+    if (t + NT * i < squares) load(t + NT * i, held[i]);
   }
 #pragma unroll
   for (int i = 0; i < kHold; ++i) grow(held[i]);
-  for (int v = t + kThreads * kHold; v < squares; v += kThreads) {
-    uint4 r[4];
-    load(v, r);
-    grow(r);
-  }
-  uint32_t bits = largest(max((int)top[0], (int)top[1]), s_most);
+  uint32_t bits = largest<NT>(max((int)top[0], (int)top[1]), s_most);
   const bool all_finite = bits < kInf;
   if (!all_finite) {
     int rest = 0;
-    for (int v = t; v < squares; v += kThreads) {
+    for (int v = t; v < squares; v += NT) {
       uint4 r[4];
       load(v, r);
       for (int k = 0; k < 4; ++k) {
@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(kThreads) hs_append_kernel(const AppendArgs A)
         }
       }
     }
-    bits = largest(rest, s_most);
+    bits = largest<NT>(rest, s_most);
   }
   const float most = Vec16<F16>::lo(bits);
   const float need = scale_of(most), now = first > 0 ? fmaxf(need, was) : need;
@@ -203,13 +203,13 @@ __global__ void __launch_bounds__(kThreads) hs_append_kernel(const AppendArgs A)
   const int shift = A.shift - 2, words = squares / vecs;  // log2 of a dim's words; its words that have new tokens
   if (grows) {  // the codes that are there, but those of a word with new tokens
     if (kind == 0) {
-      for (int v = t; v < first * vecs; v += kThreads) {
+      for (int v = t; v < first * vecs; v += NT) {
         uint2* const to = reinterpret_cast<uint2*>(page + 8 * v);
         const uint2 old = *to;
         *to = make_uint2(rescaled(old.x, ratio), rescaled(old.y, ratio));
       }
     } else {
-      for (int v = t; v < A.dim << shift; v += kThreads) {
+      for (int v = t; v < A.dim << shift; v += NT) {
         uint32_t* const to = reinterpret_cast<uint32_t*>(page + 4 * v);
         if ((v & ((1 << shift) - 1)) < lo4) *to = rescaled(*to, ratio);
       }
@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(kThreads) hs_append_kernel(const AppendArgs A)
     const int g = t & ((1 << shift) - 1), tok = 4 * (lo4 + g);
     const bool edge = tok < first || tok + 4 > first + num;  // codes of other tokens are in the word
     if (g < words)
-      for (int d = t >> shift; d < min(kSlab, A.dim - d0); d += kThreads >> shift) {
+      for (int d = t >> shift; d < min(kSlab, A.dim - d0); d += NT >> shift) {
         uint32_t* const to = reinterpret_cast<uint32_t*>(page + (d0 + d) * A.page + tok);
         uint32_t u = s_words[d * kPitch + g];
         if (edge) {
@@ -261,13 +261,14 @@ __global__ void __launch_bounds__(kThreads) hs_append_kernel(const AppendArgs A)
       if (!again) {
 #pragma unroll
         for (int i = 0; i < kHold; ++i)
-          if (t + kThreads * i < squares) square(t + kThreads * i, held[i]);
-      }
+          if (t + NT * i < squares) square(t + NT * i, held[i]);
+      } else {
 #pragma unroll 1
-      for (int v = t + (again ? 0 : kThreads * kHold); v < squares; v += kThreads) {
-        uint4 r[4];
-        load(v, r);
-        square(v, r);
+        for (int v = t; v < squares; v += NT) {
+          uint4 r[4];
+          load(v, r);
+          square(v, r);
+        }
       }
       if (kind != 0) write(d0);
     }
@@ -282,6 +283,13 @@ __global__ void __launch_bounds__(kThreads) hs_append_kernel(const AppendArgs A)
       const float lo[4] = {z[0], z[1], z[2], z[3]}, hi[4] = {z[4], z[5], z[6], z[7]};
       return make_uint2(codes_of(lo), codes_of(hi));
     }, true);
+}
+
+template <bool F16>
+void launch_threads(const AppendArgs& A, dim3 grid, int nt, hipStream_t st) {
+  if (nt == 1024) hs_append_kernel<F16, 1024><<<grid, 1024, 0, st>>>(A);
+  else if (nt == 512) hs_append_kernel<F16, 512><<<grid, 512, 0, st>>>(A);
+  else hs_append_kernel<F16, kThreads><<<grid, kThreads, 0, st>>>(A);
 }
 
 }  // namespace
@@ -321,11 +329,14 @@ int launch_append(const hs_cache_append_args& a, hipStream_t stream) {
   A.div_vec = make_fastdiv((uint32_t)(A.dim / 8));
   const uint64_t units = (uint64_t)A.B * A.kv * A.span;
   A.units = (uint32_t)units;
-  for (uint64_t at = 0; at < units; at += kMostGroups) {
+  // as many threads as keep a page's new tokens in registers: all of it, or what `taken` leaves of it
+  const int64_t squares = (int64_t)std::min((a.taken + 6) / 4, A.page / 4) * (A.dim / 8);
+  const int nt = squares > 2 * 512 ? 1024 : squares > 2 * kThreads ? 512 : kThreads;
+  for (uint64_t at = 0; at < units; at += kMostGroups / (nt / kThreads)) {
     A.group0 = (uint32_t)at;
-    const dim3 grid((uint32_t)std::min<uint64_t>(units - at, kMostGroups), 2);
-    if (a.dtype == HS_F16) hs_append_kernel<true><<<grid, kThreads, 0, stream>>>(A);
-    else hs_append_kernel<false><<<grid, kThreads, 0, stream>>>(A);
+    const dim3 grid((uint32_t)std::min<uint64_t>(units - at, kMostGroups / (nt / kThreads)), 2);
+    if (a.dtype == HS_F16) launch_threads<true>(A, grid, nt, stream);
+    else launch_threads<false>(A, grid, nt, stream);
     if (hipPeekAtLastError() != hipSuccess) return HS_ERR_HIP;
   }
   return HS_OK;

@@ -702,6 +702,26 @@ def test_append_sizes(dtype, kv, dim, page, taken, lengths):
         check_append(state, table, torch.tensor(lengths, dtype=torch.int32), k, v, count=count)
 
 
+@pytest.mark.parametrize("kv,dim,page,taken,lengths", [
+    (2, 256, 128, 260, [0, 5, 127, 128]), (1, 256, 256, 1, [0, 255, 256]), (1, 128, 256, 130, [200, 3]),
+    (2, 256, 64, 64, [63, 0, 33]), (1, 224, 128, 77, [100, 128]), (1, 256, 128, 66, [126, 61, 3]),
+    (1, 256, 256, 130, [253, 2]), (3, 160, 256, 255, [1, 2])])
+def test_append_large_pages(kv, dim, page, taken, lengths):
+    """Workgroups of each size, with pages that are full, begun or ended inside a square."""
+    note("append large pages kv=%d dim=%d page=%d taken=%d %s" % (kv, dim, page, taken, lengths))
+    g = torch.Generator().manual_seed(dim + page + taken)
+    B = len(lengths)
+    slots = (max(lengths) + taken + page - 1) // page
+    for dtype in (torch.bfloat16, torch.float16):
+        state = pool(g, B * slots + 1, kv, page, dim)
+        table = torch.randperm(B * slots + 1, generator=g)[:B * slots].reshape(B, slots).int()
+        k = torch.randn((B, taken, kv, dim), generator=g).to(dtype) * 3
+        v = torch.randn((B, taken, kv, dim), generator=g).to(dtype) * 0.1
+        check_append(state, table, torch.tensor(lengths, dtype=torch.int32), k, v)
+        v[0, taken // 2, 0, 3] = float("nan")  # the slow way
+        check_append(state, table, torch.tensor(lengths, dtype=torch.int32), k, v)
+
+
 def test_append_paths():
     note("append paths")
     g = torch.Generator().manual_seed(21)
