@@ -184,6 +184,15 @@ __device__ inline void load_slice(const char* row, int slice, int lane, const Ve
   for (int i = 0; i < kLoads; ++i) Vt::unpack(raw[i], z[i]);
 }
 
+// The i-th of a lane's vectors of a slice.
+template <int DT>
+__device__ inline void load_vector(const char* row, int slice, int i, int lane, const VerifyArgs& A,
+                                   float (&z)[Vec<DT>::kElems]) {
+  using Vt = Vec<DT>;
+  const int64_t v = (int64_t)slice * kVerifySlice + i * 64 + lane;
+  Vt::unpack(v < A.nvec ? Vt::load_raw(row, v, A.V) : Vt::neg_raw(), z);
+}
+
 // A query's draft: lane = node.
 struct Draft {
   int parent, token;  // parent: -2 where the lane is no node that may be accepted
@@ -242,10 +251,16 @@ __device__ inline int passing_lane(double mine, double goal, double* before) {
   return l;
 }
 
-// One wave: the token of a row at which the running sum of weight(z, w) over the slices' values passes goal.
-// value(i): the lane's i-th part's value; weights(slice, w): the slice's weights, in vectors by lane.
+// What the waves of a draw tell each other.
+struct Draw {
+  double total[kLoads];
+  int some[kLoads], over[kLoads], token;
+};
+// kLoads waves: the token of a row at which the running sum over the slices' values passes goal. value(i): the lane's i-th
+// part's value; weights(slice, i, w): the weights of the i-th of the lane's vectors of a slice, the wv-th wave's. (One wave
+// for all of a slice: a draw from the residual 6.6 to 8.0 us and so 4.6 to 5.1, the walk of 61 nodes 12.0 and 10.9.)
 template <int E, int HELD, typename Value, typename Weights>
-__device__ inline int draw_token(int held, double goal, int lane, Value value, Weights weights) {
+__device__ inline int draw_token(int held, double goal, int lane, int wv, Draw* s, Value value, Weights weights) {
   double v[HELD], mine = 0.0;
 #pragma unroll
   for (int i = 0; i < HELD; ++i) {
@@ -268,66 +283,49 @@ __device__ inline int draw_token(int held, double goal, int lane, Value value, W
       run += x;
     }
   }
-  double w[kLoads][E];
-  weights(slice, w);
-  // the lane of the first of its vectors that passes, or of the last above 0
-  double sum[kLoads], upto[kLoads];
+  double w[E], sum = 0.0;
+  weights(slice, wv, w);
 #pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    sum[i] = 0.0;
-#pragma unroll
-    for (int e = 0; e < E; ++e) sum[i] += w[i][e];
-    upto[i] = wave_scan_d(sum[i]);
+  for (int e = 0; e < E; ++e) sum += w[e];
+  const double upto = wave_scan_d(sum);
+  const uint64_t some = __ballot(sum > 0.0);
+  if (lane == 63) {
+    s->total[wv] = upto;
+    s->some[wv] = some != 0;
   }
-  int which = -1, k = 0;
-  bool done = false;
-#pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    const uint64_t some = __ballot(sum[i] > 0.0), over = __ballot(base + upto[i] > goal) & some;
-    if (!done && some) {
-      which = i;
-      k = over ? __builtin_ctzll(over) : 63 - __builtin_clzll(some);
-      before = base + (lane_d(upto[i], k) - lane_d(sum[i], k));
-      done = over != 0;
-    }
-    base += lane_d(upto[i], 63);
-  }
-  if (which < 0) return -1;
-  double x[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    x[e] = w[0][e];
-#pragma unroll
-    for (int i = 1; i < kLoads; ++i) x[e] = which == i ? w[i][e] : x[e];
-  }
-  int at = -1;
-  bool passed = false;
-#pragma unroll
-  for (int e = 0; e < E; ++e)
-    if (!passed && x[e] > 0.0) {
-      at = e;
-      before += x[e];
-      passed = before > goal;
-    }
-  return (slice * kVerifySlice + which * 64 + k) * E + __builtin_amdgcn_readlane(at, k);
-}
-
-template <int DT>
-__device__ inline void weights_of_slice(const char* row, int slice, float M, int lane, const VerifyArgs& A,
-                                        double (&w)[kLoads][Vec<DT>::kElems]) {
-  float z[kLoads][Vec<DT>::kElems];
-  load_slice<DT>(row, slice, lane, A, z);
-#pragma unroll
+  __syncthreads();
+  for (int i = 0; i < wv; ++i) base += s->total[i];
+  // the lane of the wave's first vector that passes, or of the last above 0; so of the waves
+  const uint64_t over = __ballot(base + upto > goal) & some;
+  if (lane == 63) s->over[wv] = over != 0;
+  __syncthreads();
+  int which = -1;
   for (int i = 0; i < kLoads; ++i)
+    if (s->some[i] && (which < 0 || !s->over[which])) which = i;
+  if (which < 0) return -1;
+  if (wv == which) {
+    const int k = over ? __builtin_ctzll(over) : 63 - __builtin_clzll(some);
+    before = base + (lane_d(upto, k) - lane_d(sum, k));
+    int at = -1;
+    bool passed = false;
 #pragma unroll
-    for (int e = 0; e < Vec<DT>::kElems; ++e) w[i][e] = weight_of(z[i][e], M, A.c);
+    for (int e = 0; e < E; ++e)
+      if (!passed && w[e] > 0.0) {
+        at = e;
+        before += w[e];
+        passed = before > goal;
+      }
+    if (lane == k) s->token = (slice * kVerifySlice + which * 64 + k) * E + at;
+  }
+  __syncthreads();
+  return s->token;
 }
 
 // A token drawn from a target row: its parts hold the weights without the children's tokens; `with`: those count
 // too (the draft goes no deeper).
 template <int DT, int HELD>
 __device__ inline int draw_row(const VerifyArgs& A, int b, int n, int count, bool with, float M, double total, double u,
-                               int lane) {
+                               int lane, int wv, Draw* s) {
   constexpr int E = Vec<DT>::kElems;
   const char* row = A.x + b * A.sb + n * A.sn;
   RowParts<HELD> parts;
@@ -352,17 +350,18 @@ __device__ inline int draw_row(const VerifyArgs& A, int b, int n, int count, boo
     }
   }
   return draw_token<E, HELD>(
-      parts.held, u * total, lane, [&](int i) { return part_value(parts.p[i], M, A.c) + extra[i]; },
-      [&](int slice, double (&w)[kLoads][E]) {
-        weights_of_slice<DT>(row, slice, M, lane, A, w);
+      parts.held, u * total, lane, wv, s, [&](int i) { return part_value(parts.p[i], M, A.c) + extra[i]; },
+      [&](int slice, int i, double (&w)[E]) {
+        float z[E];
+        load_vector<DT>(row, slice, i, lane, A, z);
+#pragma unroll
+        for (int e = 0; e < E; ++e) w[e] = weight_of(z[e], M, A.c);
         if (with) return;
         for (uint64_t left = children; left; left &= left - 1) {
-          const int mine = __builtin_amdgcn_readlane(t, __builtin_ctzll(left)) - (slice * kVerifySlice + lane) * E;
+          const int mine = __builtin_amdgcn_readlane(t, __builtin_ctzll(left)) - (slice * kVerifySlice + i * 64 + lane) * E;
 #pragma unroll
-          for (int i = 0; i < kLoads; ++i)
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-              if (mine == i * 64 * E + e) w[i][e] = 0.0;
+          for (int e = 0; e < E; ++e)
+            if (mine == e) w[e] = 0.0;
         }
       });
 }
@@ -561,12 +560,14 @@ __global__ void __launch_bounds__(kThreads) hs_verify_rows_kernel(const VerifyAr
   if (lane == 0) *out = Part{sum, m, 0};
 }
 
-// LEVELS: the path is known but for whether its last node is the end; a wave a query.
+// LEVELS: the path is known but for whether its last node is the end. The draw is its first kLoads waves', of which each
+// finds the path's end for itself.
 template <int DT, bool GREEDY, int HELD, bool LEVELS>
-__global__ void __launch_bounds__(LEVELS ? 64 : kWalkThreads) hs_verify_walk_kernel(const VerifyArgs A) {
+__global__ void __launch_bounds__(LEVELS ? 64 * kLoads : kWalkThreads) hs_verify_walk_kernel(const VerifyArgs A) {
   __shared__ Node s_node[LEVELS ? 1 : HS_MAX_POSITIONS];
   __shared__ int s_path[HS_MAX_POSITIONS];
   __shared__ int s_len, s_with;
+  __shared__ Draw s_draw;
   const int b = blockIdx.x, lane = threadIdx.x & 63, wv = (int)uniform(threadIdx.x >> 6);
   const int count = count_of(A, b);
   const Draft draft(A, b, count, lane);
@@ -575,8 +576,8 @@ __global__ void __launch_bounds__(LEVELS ? 64 : kWalkThreads) hs_verify_walk_ker
     const int at = lane <= A.depth ? A.cur[(int64_t)lane * A.B + b] : -1;
     const int len = __builtin_popcountll(__ballot(at >= 0));
     if (len > 0) end = node_of<DT, GREEDY, HELD>(A, draft, b, __builtin_amdgcn_readlane(at, max(len, 1) - 1), lane);
-    s_path[lane] = at;
-    if (lane == 0) {
+    if (wv == 0) s_path[lane] = at;
+    if (threadIdx.x == 0) {
       s_len = len;
       s_with = len > A.depth;
     }
@@ -591,9 +592,9 @@ __global__ void __launch_bounds__(LEVELS ? 64 : kWalkThreads) hs_verify_walk_ker
       if (lane == 0) s_node[n] = o;
     }
     __syncthreads();
-    if (wv != 0) return;
+    if (wv >= kLoads) return;
   }
-  if (!LEVELS && lane == 0) {
+  if (!LEVELS && threadIdx.x == 0) {
     int len = 0, n = 0;
     bool cut = false;
     while (count > 0) {
@@ -609,7 +610,7 @@ __global__ void __launch_bounds__(LEVELS ? 64 : kWalkThreads) hs_verify_walk_ker
     s_len = len;
     s_with = len > A.depth;  // the draft ends here, whatever the children
   }
-  lds_wave_fence();
+  __syncthreads();
   const int len = s_len;
   const int64_t o = (int64_t)b * A.M;
   const int last = len > 0 ? s_path[len - 1] : 0;
@@ -623,8 +624,9 @@ __global__ void __launch_bounds__(LEVELS ? 64 : kWalkThreads) hs_verify_walk_ker
     residual = end.kind == 2;
     if (GREEDY) token = end.kind ? end.arg : -1;
     else if (end.kind == 1)
-      token = draw_row<DT, HELD>(A, b, last, count, with, end.m, with ? end.total : end.rest, A.u[o], lane);
+      token = draw_row<DT, HELD>(A, b, last, count, with, end.m, with ? end.total : end.rest, A.u[o], lane, wv, &s_draw);
   }
+  if (wv != 0) return;
   if (lane < A.M) {
     const int next = lane + 1 < len ? s_path[lane + 1] : -1;
     A.path[o + lane] = lane < len ? s_path[lane] : -1;
@@ -637,7 +639,11 @@ __global__ void __launch_bounds__(LEVELS ? 64 : kWalkThreads) hs_verify_walk_ker
   }
 }
 
-// max(0, p - q) of the slice's tokens
+// max(0, p - q) of a token
+__device__ inline double residual(float z, float y, const End& e, const VerifyArgs& A) {
+  return fmax(0.0, weight_of(z, e.mp, A.c) * e.zp - weight_of(y, e.mq, A.c) * e.zq);
+}
+// and of the slice's
 template <int DT>
 __device__ inline void residual_of_slice(const VerifyArgs& A, int b, const End& e, int slice, int lane,
                                          double (&w)[kLoads][Vec<DT>::kElems]) {
@@ -649,7 +655,7 @@ __device__ inline void residual_of_slice(const VerifyArgs& A, int b, const End& 
   for (int i = 0; i < kLoads; ++i)
 #pragma unroll
     for (int k = 0; k < E; ++k)
-      w[i][k] = fmax(0.0, weight_of(z[i][k], e.mp, A.c) * e.zp - weight_of(y[i][k], e.mq, A.c) * e.zq);
+      w[i][k] = residual(z[i][k], y[i][k], e, A);
 }
 
 template <int DT>
@@ -673,9 +679,10 @@ __global__ void __launch_bounds__(kThreads) hs_verify_rest_kernel(const VerifyAr
 }
 
 template <int DT, int HELD>
-__global__ void __launch_bounds__(64) hs_verify_draw_kernel(const VerifyArgs A) {
+__global__ void __launch_bounds__(64 * kLoads) hs_verify_draw_kernel(const VerifyArgs A) {
   constexpr int E = Vec<DT>::kElems;
-  const int b = blockIdx.x, lane = threadIdx.x;
+  __shared__ Draw s_draw;
+  const int b = blockIdx.x, lane = threadIdx.x & 63, wv = (int)uniform(threadIdx.x >> 6);
   const End e = A.end[b];
   if (!e.residual) return;
   RowParts<HELD> parts;
@@ -687,11 +694,17 @@ __global__ void __launch_bounds__(64) hs_verify_draw_kernel(const VerifyArgs A) 
   int token;
   if (total > 0.0)
     token = draw_token<E, HELD>(
-        parts.held, u * total, lane, [&](int i) { return parts.p[i].sum; },
-        [&](int slice, double (&w)[kLoads][E]) { residual_of_slice<DT>(A, b, e, slice, lane, w); });
+        parts.held, u * total, lane, wv, &s_draw, [&](int i) { return parts.p[i].sum; },
+        [&](int slice, int i, double (&w)[E]) {
+          float z[E], y[E];
+          load_vector<DT>(A.x + b * A.sb + e.node * A.sn, slice, i, lane, A, z);
+          load_vector<DT>(A.y + b * A.tb + e.node * A.tn, slice, i, lane, A, y);
+#pragma unroll
+          for (int k = 0; k < E; ++k) w[k] = residual(z[k], y[k], e, A);
+        });
   else  // p and q are the same but for rounding
-    token = draw_row<DT, HELD>(A, b, e.node, 0, false, e.mp, e.rest, u, lane);
-  if (lane == 0) A.emitted[(int64_t)b * A.M + e.length - 1] = token;
+    token = draw_row<DT, HELD>(A, b, e.node, 0, false, e.mp, e.rest, u, lane, wv, &s_draw);
+  if (threadIdx.x == 0) A.emitted[(int64_t)b * A.M + e.length - 1] = token;
 }
 
 template <int DT, bool GREEDY, int HELD>
@@ -705,12 +718,12 @@ void launch_held(VerifyArgs A, bool levels, hipStream_t st) {
       else hs_verify_rows_kernel<DT, GREEDY, 0><<<grid, kThreads, 0, st>>>(A);
       if (hipPeekAtLastError() != hipSuccess) return;
     }
-  if (levels) hs_verify_walk_kernel<DT, GREEDY, HELD, true><<<A.B, 64, 0, st>>>(A);
+  if (levels) hs_verify_walk_kernel<DT, GREEDY, HELD, true><<<A.B, 64 * kLoads, 0, st>>>(A);
   else hs_verify_walk_kernel<DT, GREEDY, HELD, false><<<A.B, kWalkThreads, 0, st>>>(A);
   if (!drafter || hipPeekAtLastError() != hipSuccess) return;
   hs_verify_rest_kernel<DT><<<(int)(((int64_t)A.B * A.S + kWaves - 1) / kWaves), kThreads, 0, st>>>(A);
   if (hipPeekAtLastError() != hipSuccess) return;
-  hs_verify_draw_kernel<DT, HELD><<<A.B, 64, 0, st>>>(A);
+  hs_verify_draw_kernel<DT, HELD><<<A.B, 64 * kLoads, 0, st>>>(A);
 }
 
 template <int DT, bool GREEDY>
