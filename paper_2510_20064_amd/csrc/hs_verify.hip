@@ -25,10 +25,10 @@
 // 3.5e-9 in a slice's sum, about once in 2000).
 //
 // What bounds it. Few rows: the launches and the latencies of a row read twice (a chain of 4 tokens over 32 thousand fp32
-// 14 us in four launches; 61 nodes over 152 thousand bf16 10 in the rows and 12 in the walk). Many: the fp64 rate in the
+// 14 us in four launches; 61 nodes over 152 thousand bf16 10 in the rows and 11 in the walk). Many: the fp64 rate in the
 // rows kernel, at ten instructions a logit (64 chains of 8 tokens and their drafter, 151936 bf16: 165 million logits in
-// 106 to 125 us, 3 TB/s; with seventeen, 123 to 140), then 11 for the walk and 24 for what a rejection
-// leaves. 32 trees of 61 nodes by levels: 60, eight launches of 2.6 to 7.
+// 106 to 125 us, 3 TB/s; with seventeen, 123 to 140), then 10 for the walk and 22 for what a rejection
+// leaves. 32 trees of 61 nodes by levels: 55, launches of 2.5 to 7.
 #include <algorithm>
 #include <cfloat>
 
@@ -758,8 +758,8 @@ size_t verify_ws_bytes(const VerifyGeom& g) {
 }
 
 // Whether a tree's rows are read level by level, those on the paths alone, in depth + 1 launches: where the rows off the
-// paths take longer than the launches. us all at once and by levels: 32 trees of 61 nodes, 7 deep, of 128256 bf16 150
-// and 61; 64 chains of 8 tokens with their drafter, where most of the rows are on the path, 165 and 196.
+// paths take longer than the launches. us all at once and by levels: 32 trees of 61 nodes, 7 deep, of 128256 bf16 154
+// and 55; 64 chains of 8 tokens with their drafter, where most of the rows are on the path, 165 and 196.
 static bool by_levels(const VerifyGeom& g, int depth, bool greedy) {
   const double row = (double)g.B * g.V * (g.dtype == HS_F32 ? 4 : 2);
   return !g.drafter && row * (g.M - (depth + 1)) / (greedy ? 5e6 : 2.8e6) > 8.0 * (depth + 1);
