@@ -28,11 +28,11 @@
 // What bounds it, heads of 128, eight cached for 32. One token over 512: two launches and four dependent reads (length,
 // table, scales, codes), 13 us. 32 tokens over up to 16 thousand, 537 MB: the memory, 116 to 119 us with the join's 6,
 // 4.6 TB/s, where a large copy reaches 4.8. 32 trees of 61 nodes over up to 8 thousand, 131 GFLOP: 208 to 220 us, 0.6
-// PFLOP/s, where a large product reaches 1.4: a wave does a tile's two products (16 of 32 cycles), its softmax (16
-// exponentials, some 60 other instructions) and its 16 to 32 reads of LDS one after the other, and the two waves that the
-// registers leave a SIMD fill half of each other's waits; no part of them takes more than an eighth of the time. No gain:
-// two tiles at once or one, the next tile's scores before this one's weights, a product's operands read under the
-// softmax before it, two buffers and one barrier a stage, other wave priorities, the values' loads before the softmax;
+// PFLOP/s, where a large product reaches 1.4: the matrix units are busy 32% of the time, the vector units 43% (152
+// instructions a wave and tile), LDS 26%, and a wave waits 48% of its time, which the second wave that the registers leave
+// a SIMD fills half. No part takes more than an eighth when it is left out. No gain: two tiles at once or one, the next
+// tile's scores before this one's weights, a product's operands read under the softmax before it, two buffers and one
+// barrier a stage, other wave priorities, the values' loads before the softmax;
 // 64 rows a wave spill.
 #include <algorithm>
 #include <cfloat>
