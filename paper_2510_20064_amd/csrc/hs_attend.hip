@@ -30,7 +30,7 @@
 // 4.6 TB/s, where a large copy reaches 4.8. 32 trees of 61 nodes over up to 8 thousand, 131 GFLOP: 208 to 220 us, 0.6
 // PFLOP/s, where a large product reaches 1.4: the matrix units are busy 32% of the time, the vector units 43% (152
 // instructions a wave and tile), LDS 26%, and a wave waits 48% of its time, which the second wave that the registers leave
-// a SIMD fills half. No part takes more than an eighth when it is left out. No gain: two tiles at once or one, the next
+// a SIMD fills half. No part takes more than an eighth when it is left out. No gain: the next
 // tile's scores before this one's weights, a product's operands read under the softmax before it, two buffers and one
 // barrier a stage, other wave priorities, the values' loads before the softmax;
 // 64 rows a wave spill.
@@ -720,7 +720,9 @@ __device__ __forceinline__ void attend_range(const AttendArgs& A, int b, int h, 
       load_stage<DB, NW>(A, h, t + kStage, pages, wv, lane, L);
     }
     if (!busy) continue;
-    constexpr int N = RW == 32 && WT <= 2 ? 2 : 1;  // tiles at once
+    // Tiles at once: two where they do not spill (32 trees of 61 nodes 217 us and with one 220; of 31, with four waves, 132
+    // and with one 129).
+    constexpr int N = WR == 8 ? 2 : 1;
 #pragma unroll
     for (int i = 0; i < kStage; i += N * WT) {
       const int sub = i + wt * N;
