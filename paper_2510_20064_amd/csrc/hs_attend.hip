@@ -920,7 +920,8 @@ template <bool F16, int DB>
 void launch_dim(const AttendArgs& A, const AttendGeom& g, hipStream_t st) {
   if constexpr (DB <= 4)
     if (g.wr == 8) return launch_rows<F16, DB, 32, 8, 8>(A, st);
-  if (g.wr == 4) return launch_rows<F16, DB, 32, 4, 4>(A, st);
+  if constexpr (DB <= 7)
+    if (g.wr == 4) return launch_rows<F16, DB, 32, 4, 4>(A, st);
   if (g.wr == 2) return launch_rows<F16, DB, 32, 2, 4>(A, st);
   if (g.rw == 32) return launch_rows<F16, DB, 32, 1, 4>(A, st);
   launch_rows<F16, DB, 16, 1, 4>(A, st);
@@ -954,7 +955,8 @@ bool attend_geom(int B, int M, int heads, int kv, int dim, int page, int slots, 
   g->dim = dim;
   const int rows = M * (heads / kv);
   g->rw = rows > 16 ? 32 : 16;
-  g->wr = rows > 128 && dim <= 128 ? 8 : rows > 64 ? 4 : rows > 32 ? 2 : 1;
+  // (Four groups of rows of 256 dimensions spill: 16 trees of 61 nodes 200 us, in groups of two 164; one of 45 95 and 66.)
+  g->wr = rows > 128 && dim <= 128 ? 8 : rows > 64 && dim <= 224 ? 4 : rows > 32 ? 2 : 1;
   g->tiles = (rows + g->rw * g->wr - 1) / (g->rw * g->wr);
   // Ranges for the workgroups that the device holds at once; a workgroup a query and head, and no join, where there are
   // four times as many of those, or where caches are so short that the join costs more than cutting them saves. us cut and

@@ -474,7 +474,7 @@ def test_attention_many_queries(M, heads, kv, dim, page, B, most):
     (4, 4, 1, 64, 32, [700, 5]), (17, 1, 1, 64, 32, [700, 5]), (16, 2, 1, 128, 32, [300, 1]), (11, 3, 1, 128, 64, [300, 64]),
     (64, 1, 1, 128, 32, [400]), (13, 5, 1, 128, 32, [400, 0]), (64, 2, 1, 128, 64, [600]), (43, 3, 1, 128, 64, [600]),
     (64, 4, 1, 128, 64, [600]), (52, 5, 1, 128, 64, [600, 9]), (64, 8, 1, 192, 64, [333, 64]), (64, 16, 2, 256, 32, [77]),
-    (33, 4, 1, 160, 32, [500])])
+    (33, 4, 1, 160, 32, [500]), (64, 5, 1, 224, 64, [333, 64]), (41, 3, 1, 256, 64, [333, 64]), (16, 4, 1, 256, 32, [90])])
 @pytest.mark.parametrize("slots", [0, 40])
 def test_attention_row_counts(M, heads, kv, dim, page, lengths, slots):
     """Rows of a head on both sides of each variant's size, with tables for short and for long caches."""
