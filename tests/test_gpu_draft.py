@@ -3,7 +3,8 @@
 Tolerances. Paths, tokens and lengths of hs_verify are exact: its weights are fp64 and good to 1.1e-12, so that of
 a number's 2^53 values fewer than V 1.1e-12 lie where the two could differ. Codes and scales of hs_cache_append are
 exact. An output of hs_tree_attention over n tokens, o = sum p v, may be off by
-  eps / 2 |o|, its rounding (bf16 2^-8, fp16 2^-11), and of sum p |v|
+  eps / 2 |o|, its rounding (bf16 2^-8, fp16 2^-11; below the type's least normal number, where steps are as wide as just
+  above it, eps / 2 of that: fp16 2^-25, so that -2.94e-6, between steps of 2^-24, is held as -2.92e-6), and of sum p |v|
     2^-11, a weight's rounding to fp16 (what is below 2^-36 of the largest, n 2^-37 at most, is in the sums' share),
     2 (dim + 8) 2^-24 a, the scores' fp32 sums of products, a = the largest scale * sum |q| |k|, in weight and sum,
     2 (2^-22 + 2^-23 + 4 * 2^-24 a), exponential, scale and the three roundings on the way to it, and
@@ -436,7 +437,7 @@ class Draft:
             a, tokens = most[b, :n][..., None], int(self.length[b]) + self.M
             rel = 2.0 ** -11 + 2 * (self.dim + 8) * 2.0 ** -24 * a + 2 * (2.0 ** -22 + 2.0 ** -23 + 2.0 ** -22 * a) + \
                 2 * (tokens + 300) * 2.0 ** -24
-            tol = HALF[self.q.dtype] * np.abs(r) + rel * mean[b, :n]
+            tol = HALF[self.q.dtype] * np.maximum(np.abs(r), torch.finfo(self.q.dtype).tiny) + rel * mean[b, :n]
             with np.errstate(invalid="ignore"):
                 over = np.where(bad, 0.0, np.abs(o - r) - tol)
             assert n == 0 or over.max() <= 0, (b, over.max(), np.unravel_index(over.argmax(), over.shape))
