@@ -25,10 +25,11 @@
 // 3.5e-9 in a slice's sum, about once in 2000).
 //
 // What bounds it. Few rows: the launches and the latencies of a row read twice (a chain of 4 tokens over 32 thousand fp32
-// 14 us in four launches; 61 nodes over 152 thousand bf16 10 in the rows and 11 in the walk). Many: the fp64 rate in the
-// rows kernel, at ten instructions a logit (64 chains of 8 tokens and their drafter, 151936 bf16: 165 million logits in
-// 106 to 125 us, 3 TB/s; with seventeen, 123 to 140), then 10 for the walk and 22 for what a rejection
-// leaves. 32 trees of 61 nodes by levels: 55, launches of 2.5 to 7.
+// 14 us in four launches; 61 nodes over 152 thousand bf16 10 in the rows and 11 in the walk). Many: the vector units in
+// the rows kernel, which are never idle, at 19 instructions a logit, ten of them fp64, all at one rate (64 chains of 8
+// tokens and their drafter, 151936 bf16: 165 million logits in 98 to 110 us, 3.3 TB/s; with 21, 106 to 125; with seventeen
+// in fp64, 123 to 140), then 10 for the walk and 22 for what a rejection leaves. 32 trees of 61 nodes by levels: 55,
+// launches of 2.5 to 7.
 #include <algorithm>
 #include <cfloat>
 
@@ -126,15 +127,14 @@ struct Sums {
   double c, m;
   float low;
   __device__ void add(float z, double& sum) const {
-    const double x = (double)(z < low ? low : z) - m, s = fma(x, c, 0x1.8p45), r = fma(x, c, 0x1.8p45 - s);
+    const double x = (double)__builtin_elementwise_maximum(z, low) - m, s = fma(x, c, 0x1.8p45), r = fma(x, c, 0x1.8p45 - s);
     const int k = (int)(uint32_t)(uint64_t)__double_as_longlong(s);
-    const uint64_t t = (uint64_t)__double_as_longlong(powers[k & 127]);
-    const uint32_t hi = (uint32_t)(t >> 32) + ((uint32_t)(k & ~127) << 13);
+    const double power = ldexp(powers[k & 127], k >> 7);
     double p = 5.55041255195012004e-02;
     p = fma(p, r, 2.40226628539921244e-01);
     p = fma(p, r, 6.93147180559945286e-01);
     p = fma(p, r, 1.0);
-    sum = fma(__longlong_as_double((long long)(((uint64_t)hi << 32) | (uint32_t)t)), p, sum);
+    sum = fma(power, p, sum);
   }
 };
 __device__ inline double weight_of(float z, float m, double c) {
