@@ -250,11 +250,11 @@ __device__ inline int pages_of(const AttendArgs& A, int b, int t, int last, int 
   const int id = lane < kStage && t + lane < last ? A.table[b * A.table_stride + (((t + lane) * 32) >> A.shift)] : -1;
   return id < A.pages ? id : -1;
 }
-// The scales of the tiles of a stage: lane i the keys' of tile i, lane kStage + i the values'. (What no tile has is read
-// from the first page, here and below, and not used.)
+// The scales of the tiles of a stage: lane i the keys' of tile i, lane kStage + i the values'; 1 where there is no tile,
+// whose products are computed like the others'. (Its codes are read from the first page, below, and not used.)
 __device__ inline float scales_of(const AttendArgs& A, int h, int pages, int lane) {
-  const int id = max(__shfl(pages, lane & (kStage - 1), 64), 0);
-  return lane < 2 * kStage ? (lane < kStage ? A.ks : A.vs)[(int64_t)id * A.kv + h] : 0.0f;
+  const int id = __shfl(pages, lane & (kStage - 1), 64);
+  return lane < 2 * kStage && id >= 0 ? (lane < kStage ? A.ks : A.vs)[(int64_t)id * A.kv + h] : 1.0f;
 }
 // Tokens of a stage's tile that there are.
 __device__ inline int valid_of(int pages, int t, int sub, int tokens) {

@@ -589,6 +589,31 @@ def test_attention_tables():
     d.check(table=full[:, :5])
 
 
+@pytest.mark.parametrize("M,heads", [(1, 4), (16, 1), (5, 3), (20, 2), (30, 4), (40, 6), (61, 8)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_attention_scales_of_pages_that_no_query_has(dtype, M, heads):
+    """Pages without a token of any query, the first of the pool among them, hold any scale: for caches that end inside a
+    stage and pages that are not there, in each variant of rows."""
+    note("attention scales of unused pages %s M=%d heads=%d" % (dtype, M, heads))
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        lengths = [1, 33, 129, 0, 300, 511, 96]
+        d = Draft(M + heads, len(lengths), M, heads, 1, 64, 32, lengths, dtype)
+        other = [int(p) for p in range(len(d.ck)) if p not in d.table.flatten().tolist()][0]
+        for t in (d.ck, d.cv, d.sk, d.sv):  # the first page is in no table
+            t[[0, other]] = t[[other, 0]]
+        d.table[d.table == 0] = other
+        d.table[4, 2], d.table[5, 7] = -1, len(d.ck) + 3
+        held = torch.zeros(len(d.ck), dtype=torch.bool)
+        for b, n in enumerate(lengths):
+            for p in d.table[b, :-(-n // 32)].tolist():
+                if 0 <= p < len(held):
+                    held[p] = True
+        assert not held[0]
+        d.sk[~held] = bad
+        d.sv[~held] = bad
+        d.check()
+
+
 def test_attention_strides_and_streams():
     note("attention strides and streams")
     d = Draft(12, 3, 6, 8, 2, 128, 64, [200, 77, 0], torch.bfloat16)
