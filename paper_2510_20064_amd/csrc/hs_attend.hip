@@ -92,12 +92,12 @@ struct AttendArgs {
 
 __device__ inline int same(int x) { return (int)uniform((uint32_t)x); }  // (what every lane has, in a scalar register)
 __device__ inline int tokens_of(const AttendArgs& A, int b) {
-  const int most = (int)min((int64_t)A.slots << A.shift, (int64_t)INT_MAX - 31 * kStage);
-  return min(max(A.length[b], 0), most);
+  return min(max(A.length[b], 0), (int)min((int64_t)A.slots << A.shift, (int64_t)INT_MAX));
 }
-// Stages of a query's cached tokens; one without tokens counts for one.
+// Stages of a query's cached tokens; one without tokens counts for one. (Up to 2^31 - 1 tokens: rounded up without sign,
+// here and where tokens are counted in tiles.)
 __device__ inline int stages_of(const AttendArgs& A, int b) {
-  return max((tokens_of(A, b) + 32 * kStage - 1) / (32 * kStage), 1);
+  return max((int)(((uint32_t)tokens_of(A, b) + 32 * kStage - 1) / (32 * kStage)), 1);
 }
 // The stages of all queries, one behind the other, are cut into ranges of `per`: a workgroup does a range, and a query
 // may lie in several, whose parts the join adds. Range i has up to two parts of such queries: place 2 i is that of the
@@ -285,7 +285,7 @@ __device__ __forceinline__ void load_stage(const AttendArgs& A, int h, int t, in
 #pragma unroll
   for (int i = 0; i < L.kN; ++i) {
     const int piece = min(wv + NW * i, L.kAll - 1), sub = piece / DB, part = piece - sub * DB;
-    const int id = max(__builtin_amdgcn_readlane(pages, sub), 0), off = ((t + sub) * 32) & (A.page - 1);
+    const int id = max(__builtin_amdgcn_readlane(pages, sub), 0), off = (int)(((uint32_t)(t + sub) * 32) & (uint32_t)(A.page - 1));
     const int64_t at = ((int64_t)id * A.kv + h) * A.page;
     L.k[i] = *reinterpret_cast<const u32x4*>(A.ck + (at + off) * D + part * 1024 + ko);
     L.v[i] = *reinterpret_cast<const u32x4*>(A.cv + at * D + off + part * 32 * A.page + vo);
@@ -659,7 +659,7 @@ __device__ __forceinline__ void attend_range(const AttendArgs& A, int b, int h, 
   const int tokens = same(tokens_of(A, b)), stages = same(stages_of(A, b));
   const bool starts = before >= from, ends = before + stages <= to;  // the query's first, its last stage is in the range
   const int first = starts ? 0 : (from - before) * kStage;
-  const int last = min(ends ? INT_MAX : (to - before) * kStage, (tokens + 31) / 32);
+  const int last = min(ends ? INT_MAX : (to - before) * kStage, (int)(((uint32_t)tokens + 31) / 32));
 
   const int row = tile * kRows + wr * RW + rho;
   const bool live = row < rows, busy = tile * kRows + wr * RW < rows;  // busy: the wave has rows

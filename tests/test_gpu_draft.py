@@ -683,6 +683,28 @@ def test_attention_far_pages():
     d.check(cache=big, table=to.int()[args["table"].long()])
 
 
+@pytest.mark.parametrize("M,heads,slots", [(1, 1, 1 << 23), (1, 1, (1 << 23) + 5), (20, 2, 1 << 23)])
+def test_attention_over_as_many_tokens_as_an_int_counts(M, heads, slots):
+    """2^31 - 1 tokens, of pages that a table has many times: the last token, whose score is 200 above the others', is
+    there (all others' weight is 2^31 e^-200), and work is cut among the workgroups."""
+    note("attention over 2^31 - 1 tokens M=%d slots=%d" % (M, slots))
+    dim, page = 32, 256
+    code = torch.zeros((2, 1, page, dim), dtype=torch.uint8)
+    values = code.transpose(2, 3).contiguous()
+    code[1, 0, page - 2] = 0x38   # 1; the last token of the last page but one is the last of all
+    values[1, 0, :, page - 2] = torch.arange(1, dim + 1).to(torch.float32).to(torch.float8_e4m3fn).view(torch.uint8)
+    one = torch.ones((2, 1), device="cuda")
+    cache = hs.PagedCache(code.cuda(), values.cuda(), one, one.clone())
+    table = torch.zeros((2, slots), dtype=torch.int32, device="cuda")
+    table[0, (1 << 23) - 1] = 1
+    length = torch.tensor([(1 << 31) - 1, 100], dtype=torch.int32, device="cuda")
+    q = torch.full((2, M, heads, dim), 200.0 / dim, dtype=torch.bfloat16, device="cuda")
+    k = torch.zeros((2, M, 1, dim), dtype=torch.bfloat16, device="cuda")
+    got = hs.tree_attention(q, k, k, cache, table, length, scale=1.0).cpu()
+    want = values[1, 0, :, page - 2].view(torch.float8_e4m3fn).to(torch.bfloat16)
+    assert torch.equal(got[0], want.expand(got[0].shape)) and torch.all(got[1] == 0)
+
+
 # ---- hs_cache_append ---------------------------------------------------------------------------------------
 
 def pool(g, pages, kv, page, dim):
