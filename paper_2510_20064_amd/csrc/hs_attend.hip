@@ -4,7 +4,7 @@
 // ks and vs the scales of t's page,
 //   o_r = sum_t p_rt vs_t v_t / sum_t p_rt,   p_rt = 2^(s_rt - m_r).
 // The values' scales go into the weights: with x_rt = s_rt + log2 vs_t, w_rt = 2^(x_rt - m_r) and m_r following the
-// largest x, o_r = sum w v / sum w / vs: a weight is rounded relative to what it adds, whatever its page's scale.
+// largest x, o_r = sum w v / sum w / vs.
 //
 // Layout. Products are S^T = K Q^T and O^T = V^T P^T, so that a row's scores, weights, maximum and sum all stay in the
 // lanes that hold its column, and the weights are the second product's operand as they stand: the scores' registers of a
@@ -20,6 +20,12 @@
 // Weights are rounded to fp16 (relative 2^-11, an eighth of a bf16 output's own rounding), as 2^12 w, so that what lies
 // below 2^-36 of the largest is lost and not what lies below 2^-24; m follows only in steps above 2^3 (w stays
 // below 2^16), which spares most tiles the multiplication of O. Sums and O are fp32.
+// m follows x whatever a page's codes are, so a page whose scale an outlier set would take fp16's range from pages of finer
+// scales. While tiles whose scale is more than 2^kSpread below the largest met are added, O and their weights are held larger
+// (see lifted). Nodes' values have no scale: m follows them as if it were 2^kNodes, so that pages down to 2^-20 are no finer
+// ones, and their weights, which that makes larger than fp16, are two bf16 each. (One query's tree 41.6 us and 42.2, 32 trees
+// 198 and 204, fp16 nodes of short drafts 15.0 and 15.6; all weights as two bf16, whose range is fp32's, 47.3, 249 and 15.9; a
+// range done once more where its scales lie apart, as a second loop, 43.4, 207 and 15.2.)
 //
 // Split. The stages of all queries are cut into as many equal ranges as the device holds workgroups, so that lengths that
 // differ, and one query alone, load it alike; what a range holds of a query that others share goes to the workspace, and
@@ -56,6 +62,9 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr float kHeadroom = 12.0f;  // weights are held as 2^12 w
 constexpr float kSlack = 3.0f;      // m follows a maximum more than this above it
 constexpr float kLowest = -1.7e38f; // m before the first token
+constexpr float kSpread = 4.0f;     // log2 of how far a page's scale may be below others'
+constexpr float kNodes = -16.0f;    // log2 of the scale that m takes nodes' values to have
+constexpr float kHugeNodes = 24.0f; // and where some are 2^90 or more: 64 of the largest at weights of 2^(15 - 24) are fp32
 constexpr int kStage = 4;           // tiles of 32 tokens that a workgroup brings to LDS at once
 
 // Waves of a SIMD, by the registers that they take.
@@ -199,6 +208,45 @@ __device__ inline f16x8 narrow(const float* w) {
   __builtin_memcpy(&r, x, 16);
   return r;
 }
+
+// Eight weights as two bf16 each, whose sum is good to 2^-16 of the weight: its upper 16 bits, and what they leave out,
+// rounded.
+struct Weights {
+  bf16x8 hi, lo;
+  __device__ explicit Weights(const float* w) {
+    uint32_t u[4];
+    bf16x2 x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t a = __float_as_uint(w[2 * i]), b = __float_as_uint(w[2 * i + 1]);
+      u[i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+      const f32x2 rest = {w[2 * i] - __uint_as_float(a & 0xFFFF0000u), w[2 * i + 1] - __uint_as_float(b & 0xFFFF0000u)};
+      x[i] = __builtin_convertvector(rest, bf16x2);
+    }
+    __builtin_memcpy(&hi, u, 16);
+    __builtin_memcpy(&lo, x, 16);
+  }
+};
+
+// Eight fp16 values as sums of two bf16, exactly: of their 11 bits the upper 8, and the rest.
+struct Parts {
+  bf16x8 hi, lo;
+  __device__ explicit Parts(u32x4 y) {
+    uint32_t u[4], r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t w = y[i];  // (a bit cast of a vector's element itself takes the first)
+      const f16x2 h = __builtin_bit_cast(f16x2, w);
+      const float a = (float)h[0], b = (float)h[1];
+      const uint32_t ua = __float_as_uint(a), ub = __float_as_uint(b);
+      u[i] = __builtin_amdgcn_perm(ub, ua, 0x07060302u);
+      r[i] = __builtin_amdgcn_perm(__float_as_uint(b - __uint_as_float(ub & 0xFFFF0000u)),
+                                   __float_as_uint(a - __uint_as_float(ua & 0xFFFF0000u)), 0x07060302u);
+    }
+    __builtin_memcpy(&hi, u, 16);
+    __builtin_memcpy(&lo, r, 16);
+  }
+};
 
 // The row of a token's key in its tile, so that a lane's scores are consecutive tokens: of 32 rows register i of lane half
 // h is token 16 h + i, of 16 rows register i of product a and lane quarter g token 8 g + 4 a + i.
@@ -344,6 +392,7 @@ struct State {
   f32x16 o32[RW == 32 ? DB : 1];
   f32x4 o16[RW == 16 ? 2 * DB : 1];
   float m, l;  // l: this lane's share
+  float base;  // log2 of the largest scale of values met
   __device__ f32x4 get(int n) const {
     if constexpr (RW == 16) return o16[n];
     else return f32x4{o32[n / 4][n % 4 * 4], o32[n / 4][n % 4 * 4 + 1], o32[n / 4][n % 4 * 4 + 2], o32[n / 4][n % 4 * 4 + 3]};
@@ -359,6 +408,7 @@ struct State {
     for (int n = 0; n < kGroups; ++n) set(n, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
     m = kLowest;
     l = 0.0f;
+    base = -INFINITY;
   }
   __device__ void scale(float f) {
 #pragma unroll
@@ -378,6 +428,35 @@ __device__ inline float follow(State<DB, RW>& S, float top) {
     S.scale(f);
   }
   return S.m - kHeadroom;
+}
+// Whether one of N tiles that have tokens is of a page whose scale of values is far below the largest met. bias: log2 of
+// the scales.
+template <int DB, int RW, int N>
+__device__ __forceinline__ bool apart(State<DB, RW>& S, const float (&bias)[N], const int (&valid)[N]) {
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+    if (valid[n] > 0) S.base = fmaxf(S.base, bias[n]);
+  bool far = false;
+#pragma unroll
+  for (int n = 0; n < N; ++n) far |= valid[n] > 0 && bias[n] < S.base - kSpread;
+  return __ballot(far) != 0;
+}
+// While such tiles are added, O and their weights are held 2^lift times as large, lift per row: as much as brings the row's
+// largest weight of these tiles to 2^12, unless O would overflow. top: the lane's largest score, as in follow.
+template <int DB, int RW>
+__device__ inline float lifted(State<DB, RW>& S, float top) {
+  float most = 0.0f;
+#pragma unroll
+  for (int n = 0; n < S.kGroups; ++n) {
+    const f32x4 o = S.get(n);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(o[i]) <= FLT_MAX ? fabsf(o[i]) : 0.0f);
+    __builtin_amdgcn_sched_barrier(0);  // (a rare path that takes no registers from the others)
+  }
+  const int e = __builtin_amdgcn_frexp_expf(row_max<RW>(most));
+  const float lift = rintf(fmaxf(fminf(S.m - row_max<RW>(top), (float)(124 - max(e, 0))), 0.0f));
+  S.scale(__builtin_amdgcn_exp2f(lift));
+  return lift;
 }
 template <int N>
 __device__ inline float max_of(const float (&x)[N]) {
@@ -437,7 +516,14 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& A, const V8<F16> 
     }
     top = fmaxf(top, fmaf(f[n] < 0.0f ? lo : hi, f[n], bias[n]));
   }
-  const float from = follow(S, top);
+  float from = follow(S, top), lift = 0.0f;
+  const bool far = apart(S, bias, valid);
+  if (far) {
+    lift = lifted(S, top);
+    from -= lift;
+#pragma unroll
+    for (int n = 0; n < N; ++n) inv[n] *= __builtin_amdgcn_exp2f(-lift);
+  }
   f16x8 p[N][2];
 #pragma unroll
   for (int n = 0; n < N; ++n) {
@@ -459,6 +545,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& A, const V8<F16> 
       S.o32[j] = mfma(v[0], p[n][0], S.o32[j]);
       S.o32[j] = mfma(v[1], p[n][1], S.o32[j]);
     }
+  if (far) S.scale(__builtin_amdgcn_exp2f(-lift));
 }
 
 // The same for 16 rows, one tile: products of 16 x 16 x 32.
@@ -492,11 +579,19 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& A, const V8<F16> 
     hi = fmaxf(hi, s[i / 4][i % 4]);
     lo = fminf(lo, s[i / 4][i % 4]);
   }
-  const float off = bias - follow(S, fmaf(f < 0.0f ? lo : hi, f, bias));
+  const float top = fmaf(f < 0.0f ? lo : hi, f, bias);
+  float from = follow(S, top), inv = __builtin_amdgcn_rcpf(vs), lift = 0.0f;
+  const bool far = apart<DB, 16, 1>(S, {bias}, valid);
+  if (far) {
+    lift = lifted(S, top);
+    from -= lift;
+    inv *= __builtin_amdgcn_exp2f(-lift);
+  }
+  const float off = bias - from;
   float x[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(s[i / 4][i % 4], f, off));
-  S.l = fmaf(sum_of(x), __builtin_amdgcn_rcpf(vs), S.l);
+  S.l = fmaf(sum_of(x), inv, S.l);
   const f16x8 p = narrow(x);
   const uint8_t* vp = lds + St::kKeys + rho * St::kValuePitch + 32 * sub + 8 * g;
 #pragma unroll
@@ -504,6 +599,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& A, const V8<F16> 
     const u32x2 v = *reinterpret_cast<const u32x2*>(vp + 16 * n * St::kValuePitch);
     S.o16[n] = mfma(widen<true>(v.x, v.y), p, S.o16[n]);
   }
+  if (far) S.scale(__builtin_amdgcn_exp2f(-lift));
 }
 
 // 32 nodes in LDS, in their own type: keys like a tile's, values by dimension.
@@ -536,7 +632,8 @@ __device__ __forceinline__ void load_nodes(const AttendArgs& A, int b, int h, in
 __device__ inline bool not_finite16(uint32_t x, bool f16) {
   return f16 ? (x & 0x7C00u) == 0x7C00u : (x & 0x7F80u) == 0x7F80u;
 }
-// Whether a value is not finite: 0 times it is no 0, so it is held as 0 and added to the rows that see it.
+// Whether a value is not finite or, of bf16, 2^90 or more. (One that is not finite is held as 0, for 0 times it is no 0, and
+// added to the rows that see it.)
 template <bool F16, int RW, int DB, int T>
 __device__ __forceinline__ bool store_nodes(uint8_t* lds, int t, const NodeLoads<DB, T>& L) {
   using Nd = Nodes<DB>;
@@ -549,9 +646,9 @@ __device__ __forceinline__ bool store_nodes(uint8_t* lds, int t, const NodeLoads
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       uint16_t y = (uint16_t)(L.v[i][e / 2] >> (16 * (e & 1)));
-      if (not_finite16(y, F16)) {
+      if ((y & 0x7FFFu) >= (F16 ? 0x7C00u : 0x6C80u)) {
         bad = true;
-        y = 0;
+        if (not_finite16(y, F16)) y = 0;
       }
       *reinterpret_cast<uint16_t*>(lds + Nd::kKeys + (8 * c + e) * Nd::kValuePitch + 2 * n) = y;
     }
@@ -560,7 +657,7 @@ __device__ __forceinline__ bool store_nodes(uint8_t* lds, int t, const NodeLoads
 }
 
 // The 32 nodes in LDS, `first` the first of them. bits: the nodes that the lane's row sees; bad: there are values that
-// are not finite.
+// are not finite, or huge.
 template <bool F16, int DB, int RW, int NQ>
 __device__ inline void attend_nodes(const AttendArgs& A, const V8<F16> (&q)[NQ], const uint8_t* lds, int b, int h,
                                     int first, int nodes, uint64_t bits, bool bad, int lane, State<DB, RW>& S) {
@@ -588,31 +685,30 @@ __device__ inline void attend_nodes(const AttendArgs& A, const V8<F16> (&q)[NQ],
 #pragma unroll
     for (int i = 0; i < NX; ++i) x[i] = (sees >> i) & 1 ? s[i / 4][i % 4] * A.scale2 : -INFINITY;
   }
-  const float from = follow(S, max_of(x));
+  const float scale = bad && !F16 ? kHugeNodes : kNodes, from = follow(S, max_of(x) + scale);
+  S.base = fmaxf(S.base, scale);
 #pragma unroll
   for (int i = 0; i < NX; ++i) x[i] = __builtin_amdgcn_exp2f(x[i] - from);
   S.l += sum_of(x);
   const uint8_t* vp = lds + Nd::kKeys + rho * Nd::kValuePitch + 2 * NX * c;
 #pragma unroll
   for (int e = 0; e < NX / 8; ++e) {
-    // The nodes' values are fp16, or bf16, whose range fp16 lacks: the weights are then two bf16 (16 bits).
-    V8<F16> p, rest;
-    if constexpr (F16) p = narrow(x + 8 * e);
-    else
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        p[i] = (__bf16)x[8 * e + i];
-        rest[i] = (__bf16)(x[8 * e + i] - (float)p[i]);
-      }
+    const Weights p(x + 8 * e);
 #pragma unroll
     for (int n = 0; n < 32 * DB / RW; ++n) {
-      const V8<F16> a = *reinterpret_cast<const V8<F16>*>(vp + RW * n * Nd::kValuePitch + 16 * e);
-      if constexpr (RW == 32) {
-        S.o32[n] = mfma(a, p, S.o32[n]);
-        if constexpr (!F16) S.o32[n] = mfma(a, rest, S.o32[n]);
+      const u32x4 y = *reinterpret_cast<const u32x4*>(vp + RW * n * Nd::kValuePitch + 16 * e);
+      auto product = [&](bf16x8 v, bf16x8 w) {
+        if constexpr (RW == 32) S.o32[n] = mfma(v, w, S.o32[n]);
+        else S.o16[n] = mfma(v, w, S.o16[n]);
+      };
+      if constexpr (F16) {  // (both rests: below 2^-15 of the product)
+        const Parts v(y);
+        product(v.hi, p.hi);
+        product(v.hi, p.lo);
+        product(v.lo, p.hi);
       } else {
-        S.o16[n] = mfma(a, p, S.o16[n]);
-        if constexpr (!F16) S.o16[n] = mfma(a, rest, S.o16[n]);
+        product(__builtin_bit_cast(bf16x8, y), p.hi);
+        product(__builtin_bit_cast(bf16x8, y), p.lo);
       }
     }
   }
@@ -729,7 +825,15 @@ __device__ __forceinline__ void attend_range(const AttendArgs& A, int b, int h, 
       int valid[N];
 #pragma unroll
       for (int n = 0; n < N; ++n) valid[n] = valid_of(here, t, sub + n, tokens);
-      if constexpr (RW == 32) attend_tiles<F16, DB, N, WR == 8>(A, q, s_stage, sub, valid, scales, lane, S);
+      if constexpr (N == 2) {
+        const float a = fmaxf(lane_f(scales, kStage + sub), 0x1p-40f), b = fmaxf(lane_f(scales, kStage + sub + 1), 0x1p-40f);
+        const int passes = __ballot(a < 0x1p-4f * b || b < 0x1p-4f * a) ? 2 : 1;  // one by one, if they lie apart
+#pragma unroll 1
+        for (int pass = 0; pass < passes; ++pass) {
+          const int these[2] = {pass == 0 ? valid[0] : 0, pass == passes - 1 ? valid[1] : 0};
+          attend_tiles<F16, DB, N, WR == 8>(A, q, s_stage, sub, these, scales, lane, S);
+        }
+      } else if constexpr (RW == 32) attend_tiles<F16, DB, N, WR == 8>(A, q, s_stage, sub, valid, scales, lane, S);
       else attend_tiles<F16, DB>(A, q, s_stage, sub, valid, scales, lane, S);
     }
   }

@@ -562,6 +562,56 @@ def test_attention_scales():
     d.check()
 
 
+@pytest.mark.parametrize("M,heads", [(1, 4), (5, 3), (20, 2), (40, 6), (61, 8)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_attention_values_of_pages_far_finer_than_others(dtype, M, heads):
+    """A page whose scale is far above the others', and which has no code in half of the dimensions: there the others'
+    values are all, as good as without it."""
+    note("attention pages far finer %s M=%d heads=%d" % (dtype, M, heads))
+    for spread in (6, 20, 27, 34, 40, 60, 79):
+        d = Draft(M + spread, 3, M, heads, 1, 64, 32, [400, 33, 150], dtype)
+        top = 40.0 if dtype == torch.bfloat16 else 10.0
+        d.sv[:] = 2.0 ** max(top - spread, -40.0)
+        d.v *= 2.0 ** (max(top - spread, -40.0) + 6)
+        for p in (d.table[0, 3], d.table[0, 9], d.table[1, 0]):
+            d.sv[p.long()] = 2.0 ** top
+            d.cv[p.long(), 0, 32:] = torch.where((d.cv[p.long(), 0, 32:] & 0x7F) == 0x7F, d.cv[p.long(), 0, 32:], 0)
+        if dtype == torch.float16:  # codes of 0 and 2: 448 * 2^10 would be no fp16
+            d.cv[:, :, :32] = torch.where((d.cv[:, :, :32] & 0x7F) == 0x7F, d.cv[:, :, :32], d.cv[:, :, :32] & 0xC0)
+        d.check()
+
+
+@pytest.mark.parametrize("M,heads", [(1, 4), (5, 3), (20, 2), (40, 6), (61, 8)])
+def test_attention_any_finite_value_of_bf16_nodes(M, heads):
+    """Nodes' values up to the largest bf16; and one of them alone, beside dimensions that hold cached values only."""
+    note("attention huge node values M=%d heads=%d" % (M, heads))
+    for e in (80, 89, 90, 100, 112, 120, 127):
+        d = Draft(M + e, 3, M, heads, 1, 64, 32, [400, 33, 0], torch.bfloat16)
+        d.v.copy_((d.v * 2.0 ** (e - 2)).clamp_(-3.38e38, 3.38e38))
+        d.check()
+    for e in (80, 92, 104):
+        d = Draft(M + e, 3, M, heads, 1, 64, 32, [400, 33, 0], torch.bfloat16)
+        d.v.zero_()
+        d.v[:, M // 2, :, 7] = 2.0 ** e
+        d.check()
+
+
+@pytest.mark.parametrize("M,heads", [(1, 4), (5, 3), (20, 2), (40, 6), (61, 8)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_attention_small_and_large_values(dtype, M, heads):
+    """Values of cache and nodes alike, from far below 1 to far above."""
+    note("attention small and large values %s M=%d heads=%d" % (dtype, M, heads))
+    g = torch.Generator().manual_seed(61)
+    for size in (-40, -34, -27, -20, -14, -3, 5, 12) + ((25, 39) if dtype == torch.bfloat16 else ()):
+        d = Draft(M + 99 + size, 3, M, heads, 1, 64, 32, [400, 33, 150], dtype)
+        d.sv[:] = 2.0 ** (torch.randint(0, 2, d.sv.shape, generator=g).float() + size)
+        d.v *= 2.0 ** (size + 6)
+        if dtype == torch.float16 and size > 5:
+            d.v.clamp_(-6e4, 6e4)
+            d.cv.copy_(torch.where((d.cv & 0x7F) == 0x7F, d.cv, d.cv & 0xBF))  # codes below 2, values below 2^14
+        d.check()
+
+
 def test_attention_sharp_and_flat():
     """Scores from equal to far apart: one token has all the weight, and late maxima."""
     note("attention sharp and flat")
