@@ -603,8 +603,8 @@ int hs_verify(const hs_verify_args* args, void* stream);
  *   k       : [pages][heads][page][dim], v: [pages][heads][dim][page] bytes, contiguous, 16-byte aligned: a page
  *             holds the values of one dimension side by side.
  *   k_scale, v_scale : [pages][heads] fp32. Those of hs_cache_append are powers of two from 2^-40 to 2^40; other ones
- *             may be any finite number (keys), or 0 or from 2^-40 to 2^40 (values: what lies outside, negative or NaN
- *             counts as the nearest of these two bounds, NaN as the lower).
+ *             may be any finite number (keys), or 0 or from 2^-40 to 2^40 (values: another one counts as the nearest of
+ *             these two bounds, a negative one and NaN as the lower).
  *   A query's tokens are those of the pages of its row of a table: token t is in page table[b][t / page], at
  *   t % page. Several queries, and one, may have a page more than once, to read.
  *   1 <= heads <= HS_MAX_HEADS, dim a multiple of 32 up to HS_MAX_HEAD_DIM, page 32, 64, 128 or 256.

@@ -339,9 +339,10 @@ __device__ __forceinline__ void load_stage(const AttendArgs& A, int h, int t, in
     L.v[i] = *reinterpret_cast<const u32x4*>(A.cv + at * D + off + part * 32 * A.page + vo);
   }
 }
-// pages, t, tokens: of the stage. What lies behind the last token may be any code: its values are held as 0.
+// pages, t, tokens, scales: of the stage. What lies behind the last token may be any code: its values are held as 0. So are
+// those of a page whose scale is 0, but for NaN: the weights count as if it were 2^-40.
 template <bool F16, int RW, int DB, int NW, bool WIDE>
-__device__ __forceinline__ void store_stage(uint8_t* lds, int t, int pages, int tokens, int wv, int lane,
+__device__ __forceinline__ void store_stage(uint8_t* lds, int t, int pages, int tokens, float scales, int wv, int lane,
                                             Loads<DB, NW>& L) {
   using St = Staged<DB, WIDE>;
 #pragma unroll
@@ -356,6 +357,11 @@ __device__ __forceinline__ void store_stage(uint8_t* lds, int t, int pages, int 
         const int c = min(max(valid - 16 * (lane & 1) - 4 * e, 0), 4);
         L.v[i][e] &= c == 4 ? ~0u : (1u << (8 * c)) - 1;
       }
+    }
+    if (__float_as_uint(lane_f(scales, kStage + sub)) << 1 == 0) {  // (+-0, by scalar instructions)
+      asm volatile("");
+#pragma unroll
+      for (int e = 0; e < 4; ++e) L.v[i][e] &= (((L.v[i][e] & 0x7F7F7F7Fu) + 0x01010101u) >> 7 & 0x01010101u) * 0xFFu;
     }
     const int q = part * 64 + lane, token = q / (2 * DB), c = q - token * (2 * DB);
     uint8_t* kp = lds + (32 * sub + row_of<RW>(token)) * St::kKeyPitch + 16 * c * St::kCode;
@@ -805,7 +811,7 @@ __device__ __forceinline__ void attend_range(const AttendArgs& A, int b, int h, 
 
   for (int t = first; t < last; t += kStage) {
     if (t > first) __syncthreads();  // the stage before is read
-    store_stage<F16, RW, DB, NW, WR == 8>(s_stage, t, pages, tokens, wv, lane, L);
+    store_stage<F16, RW, DB, NW, WR == 8>(s_stage, t, pages, tokens, coming, wv, lane, L);
     const int here = pages;
     const float scales = coming;
     pages = next;

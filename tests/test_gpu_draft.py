@@ -597,6 +597,26 @@ def test_attention_any_finite_value_of_bf16_nodes(M, heads):
 
 
 @pytest.mark.parametrize("M,heads", [(1, 4), (5, 3), (20, 2), (40, 6), (61, 8)])
+def test_attention_value_scales_of_zero(M, heads):
+    """Values of a page whose scale is 0 are 0, and their weights count."""
+    note("attention value scales of zero M=%d heads=%d" % (M, heads))
+    for zero in (0.0, -0.0):
+        d = Draft(M + 7, 3, M, heads, 1, 64, 32, [400, 33, 150], torch.bfloat16)
+        d.sv[d.table[0, 1:9].long()] = zero
+        d.sv[d.table[1].long()] = zero
+        d.check()
+        d.cv[d.table[0, 3].long(), 0, 20, 9] = 0x7F
+        d.cv[d.table[1, 0].long(), 0, 7, 31] = 0xFF
+        d.check()
+        d = Draft(M + 8, 3, M, heads, 1, 64, 32, [400, 33, 150], torch.bfloat16)
+        d.sv[:] = zero
+        d.v.zero_()
+        assert torch.all(d.check() == 0)
+        d.v.fill_(1e-30)
+        d.check()
+
+
+@pytest.mark.parametrize("M,heads", [(1, 4), (5, 3), (20, 2), (40, 6), (61, 8)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 def test_attention_small_and_large_values(dtype, M, heads):
     """Values of cache and nodes alike, from far below 1 to far above."""
