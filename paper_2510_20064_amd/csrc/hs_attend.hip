@@ -304,6 +304,11 @@ __device__ inline float scales_of(const AttendArgs& A, int h, int pages, int lan
   const int id = __shfl(pages, lane & (kStage - 1), 64);
   return lane < 2 * kStage && id >= 0 ? (lane < kStage ? A.ks : A.vs)[(int64_t)id * A.kv + h] : 1.0f;
 }
+// And with the keys' times the products' own, finite: infinite times a product of 0 is no 0. (Apart, for it waits.)
+__device__ inline float factors_of(const AttendArgs& A, float scales, int lane) {
+  const float f = scales * A.scale2;
+  return lane < kStage ? fabsf(f) == INFINITY ? copysignf(FLT_MAX, f) : f : scales;
+}
 // Tokens of a stage's tile that there are.
 __device__ inline int valid_of(int pages, int t, int sub, int tokens) {
   return __builtin_amdgcn_readlane(pages, sub) < 0 ? 0 : min(32, max(tokens - (t + sub) * 32, 0));
@@ -339,8 +344,17 @@ __device__ __forceinline__ void load_stage(const AttendArgs& A, int h, int t, in
     L.v[i] = *reinterpret_cast<const u32x4*>(A.cv + at * D + off + part * 32 * A.page + vo);
   }
 }
+__device__ inline bool is_zero(float x) { return __float_as_uint(x) << 1 == 0; }  // (+-0, by scalar instructions)
+// Of 16 codes those that are NaN, 0 for others.
+__device__ inline u32x4 nans_of(u32x4 x) {
+  asm volatile("");  // (a branch, not selects for every tile)
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] &= (((x[e] & 0x7F7F7F7Fu) + 0x01010101u) >> 7 & 0x01010101u) * 0xFFu;
+  return x;
+}
 // pages, t, tokens, scales: of the stage. What lies behind the last token may be any code: its values are held as 0. So are
-// those of a page whose scale is 0, but for NaN: the weights count as if it were 2^-40.
+// codes of a page whose scale is 0, but for NaN: a page's weights count as if its values' were 2^-40, and products as if its
+// keys' were 1 (infinite ones, which get no weight, stay so).
 template <bool F16, int RW, int DB, int NW, bool WIDE>
 __device__ __forceinline__ void store_stage(uint8_t* lds, int t, int pages, int tokens, float scales, int wv, int lane,
                                             Loads<DB, NW>& L) {
@@ -358,11 +372,8 @@ __device__ __forceinline__ void store_stage(uint8_t* lds, int t, int pages, int 
         L.v[i][e] &= c == 4 ? ~0u : (1u << (8 * c)) - 1;
       }
     }
-    if (__float_as_uint(lane_f(scales, kStage + sub)) << 1 == 0) {  // (+-0, by scalar instructions)
-      asm volatile("");
-#pragma unroll
-      for (int e = 0; e < 4; ++e) L.v[i][e] &= (((L.v[i][e] & 0x7F7F7F7Fu) + 0x01010101u) >> 7 & 0x01010101u) * 0xFFu;
-    }
+    if (is_zero(lane_f(scales, kStage + sub))) L.v[i] = nans_of(L.v[i]);
+    if (is_zero(lane_f(scales, sub))) L.k[i] = nans_of(L.k[i]);
     const int q = part * 64 + lane, token = q / (2 * DB), c = q - token * (2 * DB);
     uint8_t* kp = lds + (32 * sub + row_of<RW>(token)) * St::kKeyPitch + 16 * c * St::kCode;
     uint8_t* vp = lds + St::kKeys + (32 * part + (lane >> 1)) * St::kValuePitch + (32 * sub + 16 * (lane & 1)) * St::kCode;
@@ -480,8 +491,6 @@ __device__ inline float sum_of(const float (&w)[N]) {
   else return a[0];
 }
 
-constexpr float kLeast = 1e-30f;  // the least factor of a product: infinite ones, which get no weight, stay infinite
-
 // N tiles of the stage in LDS from the `sub`-th on, of valid[n] tokens each: their products, which do not wait for each
 // other, then one step of the softmax.
 template <bool F16, int DB, int N, bool WIDE>
@@ -504,8 +513,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& A, const V8<F16> 
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     const float vs = fminf(fmaxf(lane_f(scales, kStage + sub + n), 0x1p-40f), 0x1p40f);
-    f[n] = A.scale2 * lane_f(scales, sub + n);
-    if (fabsf(f[n]) < kLeast) f[n] = kLeast;
+    f[n] = lane_f(scales, sub + n);
     bias[n] = __builtin_amdgcn_logf(vs);
     inv[n] = __builtin_amdgcn_rcpf(vs);
     if (valid[n] < 32) {  // what lies behind the last token has no weight
@@ -570,8 +578,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& A, const V8<F16> 
       s[a] = mfma(widen<F16>(k.x, k.y), q[j], s[a]);
     }
   const float vs = fminf(fmaxf(lane_f(scales, kStage + sub), 0x1p-40f), 0x1p40f);
-  float f = A.scale2 * lane_f(scales, sub);
-  if (fabsf(f) < kLeast) f = kLeast;
+  const float f = lane_f(scales, sub);
   const float bias = __builtin_amdgcn_logf(vs);
   if (valid[0] < 32) {
     asm volatile("");
@@ -811,9 +818,10 @@ __device__ __forceinline__ void attend_range(const AttendArgs& A, int b, int h, 
 
   for (int t = first; t < last; t += kStage) {
     if (t > first) __syncthreads();  // the stage before is read
-    store_stage<F16, RW, DB, NW, WR == 8>(s_stage, t, pages, tokens, coming, wv, lane, L);
+    const float factors = factors_of(A, coming, lane);
+    store_stage<F16, RW, DB, NW, WR == 8>(s_stage, t, pages, tokens, factors, wv, lane, L);
     const int here = pages;
-    const float scales = coming;
+    const float scales = lane < kStage && factors == 0.0f ? 1.0f : factors;
     pages = next;
     __syncthreads();
     if (t + kStage < last) {

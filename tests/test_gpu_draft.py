@@ -596,6 +596,53 @@ def test_attention_any_finite_value_of_bf16_nodes(M, heads):
         d.check()
 
 
+class Sharp(Draft):
+    """Scores that lie far apart, where a dimension may hold nothing but values of tokens of little weight. A weight is held as
+    2^12 w in fp16, w relative to a maximum that is at most 2^4 (what scales may differ by) above the row's largest weight of
+    any page: below 2^-14 fp16's steps are 2^-24, so that w is off by 2^-25 2^-12 = 2^-37 of that maximum, 2^-33 of the largest
+    weight, and that is at most 1. Each of n tokens may so add 2^-33 |v| to an output."""
+
+    def check(self, got=None, **kw):
+        if got is None:
+            got = hs.tree_attention(**dict(self.gpu(), **kw))
+            torch.cuda.synchronize()
+        f64 = lambda t: t.cpu().double().numpy()  # noqa: E731
+        ref, mean, most = draft.attention(f64(self.q), f64(self.k), f64(self.v), self.ck.numpy(), self.cv.numpy(),
+                                          self.sk.numpy(), self.sv.numpy(), self.table.numpy(), self.length.numpy(),
+                                          mask=self.mask.numpy(), scale=self.scale)
+        y = got.cpu().double().numpy()
+        large = max(448 * float(self.sv.abs().max()), float(self.v.abs().max()))
+        for b in range(self.B):
+            a, n = most[b][..., None], int(self.length[b]) + self.M
+            rel = 2.0 ** -11 + 2 * (self.dim + 8) * 2.0 ** -24 * a + 2 * (2.0 ** -22 + 2.0 ** -23 + 2.0 ** -22 * a) + \
+                2 * (n + 300) * 2.0 ** -24
+            tol = HALF[self.q.dtype] * np.abs(ref[b]) + rel * mean[b] + n * 2.0 ** -33 * large
+            assert np.all(np.abs(y[b] - ref[b]) <= tol), (b, (np.abs(y[b] - ref[b]) - tol).max())
+
+
+@pytest.mark.parametrize("M,heads", [(1, 4), (5, 3), (20, 2), (40, 6), (61, 8)])
+def test_attention_any_finite_key_scales(M, heads):
+    """Scales of 0, smallest and largest ones, of either sign, with queries that make products large or nothing of them."""
+    note("attention any key scales M=%d heads=%d" % (M, heads))
+    # (the scale of the call, of the keys, what the queries are multiplied with)
+    for scale, sk, size in ((0.0, None, 1e30), (0.0, -1.0, 1e30), (-0.0, None, 1.0), (1e-38, 1e-3, 1e30), (-1e-38, 1.0, 1e30),
+                            (1.0, -1e-33, 1e30), (-1.0, 1e-40, 1e30), (1e-3, 0.0, 1.0), (1e-30, 1e-30, 1e30), (1.0, 1e30, 1e-31),
+                            (1e-20, 1e30, 1e-12), (-1e20, 1e-30, 1e9)):
+        d = Sharp(M + 5, 3, M, heads, 1, 64, 32, [400, 33, 150], torch.bfloat16)
+        d.scale = scale
+        d.q.copy_((d.q.float() * size).to(d.q.dtype))
+        d.k.zero_()  # (the nodes' own products would not be finite)
+        if sk is not None:
+            d.sk[:] = sk
+        d.check()
+    d = Sharp(M + 5, 3, M, heads, 1, 64, 32, [400, 33, 150], torch.bfloat16)
+    d.scale = 10.0
+    far = d.table[0, 2:5].long()
+    d.sk[far] = 3e38  # 10 times that is infinite, and codes of 0 make nothing of it
+    d.ck[far] = 0
+    d.check()
+
+
 @pytest.mark.parametrize("M,heads", [(1, 4), (5, 3), (20, 2), (40, 6), (61, 8)])
 def test_attention_value_scales_of_zero(M, heads):
     """Values of a page whose scale is 0 are 0, and their weights count."""
