@@ -61,7 +61,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float kHeadroom = 12.0f;  // weights are held as 2^12 w
 constexpr float kSlack = 3.0f;      // m follows a maximum more than this above it
-constexpr float kLowest = -1.7e38f; // m before the first token
+constexpr float kLowest = -FLT_MAX; // m before the first token
 constexpr float kSpread = 4.0f;     // log2 of how far a page's scale may be below others'
 constexpr float kNodes = -16.0f;    // log2 of the scale that m takes nodes' values to have
 constexpr float kHugeNodes = 24.0f; // and where some are 2^90 or more: 64 of the largest at weights of 2^(15 - 24) are fp32
@@ -446,22 +446,22 @@ __device__ inline float follow(State<DB, RW>& S, float top) {
   }
   return S.m - kHeadroom;
 }
-// Whether one of N tiles that have tokens is of a page whose scale of values is far below the largest met. bias: log2 of
-// the scales.
-template <int DB, int RW, int N>
-__device__ __forceinline__ bool apart(State<DB, RW>& S, const float (&bias)[N], const int (&valid)[N]) {
-#pragma unroll
-  for (int n = 0; n < N; ++n)
-    if (valid[n] > 0) S.base = fmaxf(S.base, bias[n]);
-  bool far = false;
-#pragma unroll
-  for (int n = 0; n < N; ++n) far |= valid[n] > 0 && bias[n] < S.base - kSpread;
-  return __ballot(far) != 0;
-}
-// While such tiles are added, O and their weights are held 2^lift times as large, lift per row: as much as brings the row's
-// largest weight of these tiles to 2^12, unless O would overflow. top: the lane's largest score, as in follow.
+// Whether a tile that has tokens is of a page whose scale of values is far below the largest met. bias: log2 of the scale.
 template <int DB, int RW>
-__device__ inline float lifted(State<DB, RW>& S, float top) {
+__device__ __forceinline__ bool apart(State<DB, RW>& S, float bias, int valid) {
+  if (valid == 0) return false;
+  S.base = fmaxf(S.base, bias);
+  return bias < S.base - kSpread;
+}
+// Whether scores are so large that fp32 holds them in steps of 1/2 or more: a weight's exponent is no longer their difference
+// if what is added to a product is rounded before. Products are then rounded first, and m follows them alone.
+__device__ inline bool is_big(float top) { return fabsf(top) > 0x1p22f && fabsf(top) < INFINITY; }
+// While such a tile is added, O is held 2^lift times as large, lift per row, and off, what is added to products, and inv, what
+// a weight counts for in the sum, are such that its weights are: as much as brings the row's largest weight of the tile to
+// 2^12, unless O would overflow; of big scores what O needs where weights are 2^(s - m). top: the lane's largest score, as
+// in follow. To be undone by S.scale(2^-lift).
+template <int DB, int RW>
+__device__ inline float lifted(State<DB, RW>& S, float top, bool big, float bias, float& off, float& inv) {
   float most = 0.0f;
 #pragma unroll
   for (int n = 0; n < S.kGroups; ++n) {
@@ -471,7 +471,10 @@ __device__ inline float lifted(State<DB, RW>& S, float top) {
     __builtin_amdgcn_sched_barrier(0);  // (a rare path that takes no registers from the others)
   }
   const int e = __builtin_amdgcn_frexp_expf(row_max<RW>(most));
-  const float lift = rintf(fmaxf(fminf(S.m - row_max<RW>(top), (float)(124 - max(e, 0))), 0.0f));
+  float lift = rintf(fmaxf(fminf(S.m - row_max<RW>(top), (float)(124 - max(e, 0))), 0.0f));
+  if (big) lift = -(bias + kHeadroom);
+  off = big ? -S.m : off + lift;
+  inv *= __builtin_amdgcn_exp2f(-lift);
   S.scale(__builtin_amdgcn_exp2f(lift));
   return lift;
 }
@@ -491,82 +494,75 @@ __device__ inline float sum_of(const float (&w)[N]) {
   else return a[0];
 }
 
-// N tiles of the stage in LDS from the `sub`-th on, of valid[n] tokens each: their products, which do not wait for each
-// other, then one step of the softmax.
-template <bool F16, int DB, int N, bool WIDE>
-__device__ __forceinline__ void attend_tiles(const AttendArgs& A, const V8<F16> (&q)[2 * DB], const uint8_t* lds, int sub,
-                                             const int (&valid)[N], float scales, int lane, State<DB, 32>& S) {
+// The `sub`-th tile of the stage in LDS, of `valid` tokens: products, one step of the softmax, products.
+template <bool F16, int DB, bool WIDE>
+__device__ __forceinline__ void attend_tile(const V8<F16> (&q)[2 * DB], const uint8_t* lds, int sub, int valid, float scales,
+                                            int lane, State<DB, 32>& S) {
   using St = Staged<DB, WIDE>;
   const int rho = lane & 31, half = lane >> 5;
   const uint8_t* kp = lds + (32 * sub + rho) * St::kKeyPitch + 16 * half * St::kCode;
-  f32x16 s[N] = {};
+  f32x16 s = {};
 #pragma unroll
-  for (int j = 0; j < DB; ++j)
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-      V8<F16> k[2];
-      operands<F16, WIDE>(kp + 32 * n * St::kKeyPitch + 32 * j * St::kCode, k);
-      s[n] = mfma(k[0], q[2 * j], s[n]);
-      s[n] = mfma(k[1], q[2 * j + 1], s[n]);
-    }
-  float f[N], bias[N], inv[N], top = -INFINITY;
-#pragma unroll
-  for (int n = 0; n < N; ++n) {
-    const float vs = fminf(fmaxf(lane_f(scales, kStage + sub + n), 0x1p-40f), 0x1p40f);
-    f[n] = lane_f(scales, sub + n);
-    bias[n] = __builtin_amdgcn_logf(vs);
-    inv[n] = __builtin_amdgcn_rcpf(vs);
-    if (valid[n] < 32) {  // what lies behind the last token has no weight
-      asm volatile("");   // (a branch, not selects for every tile)
-      const float none = f[n] < 0.0f ? INFINITY : -INFINITY;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[n][i] = 16 * half + i < valid[n] ? s[n][i] : none;
-    }
-    float hi = s[n][0], lo = hi;  // the largest score is that of the largest product, or of the least
-#pragma unroll
-    for (int i = 1; i < 16; ++i) {
-      hi = fmaxf(hi, s[n][i]);
-      lo = fminf(lo, s[n][i]);
-    }
-    top = fmaxf(top, fmaf(f[n] < 0.0f ? lo : hi, f[n], bias[n]));
+  for (int j = 0; j < DB; ++j) {
+    V8<F16> k[2];
+    operands<F16, WIDE>(kp + 32 * j * St::kCode, k);
+    s = mfma(k[0], q[2 * j], s);
+    s = mfma(k[1], q[2 * j + 1], s);
   }
-  float from = follow(S, top), lift = 0.0f;
-  const bool far = apart(S, bias, valid);
-  if (far) {
-    lift = lifted(S, top);
-    from -= lift;
+  const float vs = fminf(fmaxf(lane_f(scales, kStage + sub), 0x1p-40f), 0x1p40f), bias = __builtin_amdgcn_logf(vs);
+  const float f = lane_f(scales, sub);
+  float inv = __builtin_amdgcn_rcpf(vs);
+  if (valid < 32) {    // what lies behind the last token has no weight
+    asm volatile("");  // (a branch, not selects for every tile)
+    const float none = f < 0.0f ? INFINITY : -INFINITY;
 #pragma unroll
-    for (int n = 0; n < N; ++n) inv[n] *= __builtin_amdgcn_exp2f(-lift);
+    for (int i = 0; i < 16; ++i) s[i] = 16 * half + i < valid ? s[i] : none;
   }
-  f16x8 p[N][2];
+  float hi = s[0], lo = hi;  // the largest score is that of the largest product, or of the least
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    const float off = bias[n] - from;
-    float x[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], f[n], off));
-    S.l = fmaf(sum_of(x), inv[n], S.l);
-    p[n][0] = narrow(x);
-    p[n][1] = narrow(x + 8);
+  for (int i = 1; i < 16; ++i) {
+    hi = fmaxf(hi, s[i]);
+    lo = fminf(lo, s[i]);
   }
+  const float best = f < 0.0f ? lo : hi;
+  float top = fmaf(best, f, bias);
+  const bool rare = __ballot(apart(S, bias, valid) || is_big(top)) != 0;
+  bool big = false;
+  if (rare && __ballot(is_big(top))) {
+    big = true;
+    top = best * f;
+  }
+  float off = bias - follow(S, top), lift = 0.0f;
+  if (rare) lift = lifted(S, top, big, bias, off, inv);
+  float x[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] = fmaf(s[i], f, off);
+  if (big) {
+    asm volatile("");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = s[i] * f + off;
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(x[i]);
+  S.l = fmaf(sum_of(x), inv, S.l);
+  const f16x8 p[2] = {narrow(x), narrow(x + 8)};
   const uint8_t* vp = lds + St::kKeys + rho * St::kValuePitch + (32 * sub + 16 * half) * St::kCode;
 #pragma unroll
-  for (int n = 0; n < N; ++n)
-#pragma unroll
-    for (int j = 0; j < DB; ++j) {
-      f16x8 v[2];
-      operands<true, WIDE>(vp + 32 * j * St::kValuePitch + 32 * n * St::kCode, v);
-      S.o32[j] = mfma(v[0], p[n][0], S.o32[j]);
-      S.o32[j] = mfma(v[1], p[n][1], S.o32[j]);
-    }
-  if (far) S.scale(__builtin_amdgcn_exp2f(-lift));
+  for (int j = 0; j < DB; ++j) {
+    f16x8 v[2];
+    operands<true, WIDE>(vp + 32 * j * St::kValuePitch, v);
+    S.o32[j] = mfma(v[0], p[0], S.o32[j]);
+    S.o32[j] = mfma(v[1], p[1], S.o32[j]);
+  }
+  if (rare) S.scale(__builtin_amdgcn_exp2f(-lift));
 }
 
-// The same for 16 rows, one tile: products of 16 x 16 x 32.
-template <bool F16, int DB>
-__device__ __forceinline__ void attend_tiles(const AttendArgs& A, const V8<F16> (&q)[DB], const uint8_t* lds, int sub,
-                                             const int (&valid)[1], float scales, int lane, State<DB, 16>& S) {
-  using St = Staged<DB, false>;
+// The same for 16 rows: products of 16 x 16 x 32.
+template <bool F16, int DB, bool WIDE>
+__device__ __forceinline__ void attend_tile(const V8<F16> (&q)[DB], const uint8_t* lds, int sub, int valid, float scales,
+                                            int lane, State<DB, 16>& S) {
+  using St = Staged<DB, WIDE>;
+  static_assert(!WIDE, "codes");
   const int rho = lane & 15, g = lane >> 4;
   const uint8_t* kp = lds + (32 * sub + rho) * St::kKeyPitch + 8 * g;
   f32x4 s[2] = {};
@@ -577,14 +573,14 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& A, const V8<F16> 
       const u32x2 k = *reinterpret_cast<const u32x2*>(kp + 16 * a * St::kKeyPitch + 32 * j);
       s[a] = mfma(widen<F16>(k.x, k.y), q[j], s[a]);
     }
-  const float vs = fminf(fmaxf(lane_f(scales, kStage + sub), 0x1p-40f), 0x1p40f);
+  const float vs = fminf(fmaxf(lane_f(scales, kStage + sub), 0x1p-40f), 0x1p40f), bias = __builtin_amdgcn_logf(vs);
   const float f = lane_f(scales, sub);
-  const float bias = __builtin_amdgcn_logf(vs);
-  if (valid[0] < 32) {
+  float inv = __builtin_amdgcn_rcpf(vs);
+  if (valid < 32) {
     asm volatile("");
     const float none = f < 0.0f ? INFINITY : -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s[i / 4][i % 4] = 8 * g + i < valid[0] ? s[i / 4][i % 4] : none;
+    for (int i = 0; i < 8; ++i) s[i / 4][i % 4] = 8 * g + i < valid ? s[i / 4][i % 4] : none;
   }
   float hi = s[0][0], lo = hi;
 #pragma unroll
@@ -592,18 +588,26 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& A, const V8<F16> 
     hi = fmaxf(hi, s[i / 4][i % 4]);
     lo = fminf(lo, s[i / 4][i % 4]);
   }
-  const float top = fmaf(f < 0.0f ? lo : hi, f, bias);
-  float from = follow(S, top), inv = __builtin_amdgcn_rcpf(vs), lift = 0.0f;
-  const bool far = apart<DB, 16, 1>(S, {bias}, valid);
-  if (far) {
-    lift = lifted(S, top);
-    from -= lift;
-    inv *= __builtin_amdgcn_exp2f(-lift);
+  const float best = f < 0.0f ? lo : hi;
+  float top = fmaf(best, f, bias);
+  const bool rare = __ballot(apart(S, bias, valid) || is_big(top)) != 0;
+  bool big = false;
+  if (rare && __ballot(is_big(top))) {
+    big = true;
+    top = best * f;
   }
-  const float off = bias - from;
+  float off = bias - follow(S, top), lift = 0.0f;
+  if (rare) lift = lifted(S, top, big, bias, off, inv);
   float x[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(s[i / 4][i % 4], f, off));
+  for (int i = 0; i < 8; ++i) x[i] = fmaf(s[i / 4][i % 4], f, off);
+  if (big) {
+    asm volatile("");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = s[i / 4][i % 4] * f + off;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_exp2f(x[i]);
   S.l = fmaf(sum_of(x), inv, S.l);
   const f16x8 p = narrow(x);
   const uint8_t* vp = lds + St::kKeys + rho * St::kValuePitch + 32 * sub + 8 * g;
@@ -612,7 +616,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& A, const V8<F16> 
     const u32x2 v = *reinterpret_cast<const u32x2*>(vp + 16 * n * St::kValuePitch);
     S.o16[n] = mfma(widen<true>(v.x, v.y), p, S.o16[n]);
   }
-  if (far) S.scale(__builtin_amdgcn_exp2f(-lift));
+  if (rare) S.scale(__builtin_amdgcn_exp2f(-lift));
 }
 
 // 32 nodes in LDS, in their own type: keys like a tile's, values by dimension.
@@ -830,26 +834,9 @@ __device__ __forceinline__ void attend_range(const AttendArgs& A, int b, int h, 
       load_stage<DB, NW>(A, h, t + kStage, pages, wv, lane, L);
     }
     if (!busy) continue;
-    // Tiles at once: two where they do not spill (32 trees of 61 nodes 217 us and with one 220; of 31, with four waves, 132
-    // and with one 129).
-    constexpr int N = WR == 8 ? 2 : 1;
 #pragma unroll
-    for (int i = 0; i < kStage; i += N * WT) {
-      const int sub = i + wt * N;
-      int valid[N];
-#pragma unroll
-      for (int n = 0; n < N; ++n) valid[n] = valid_of(here, t, sub + n, tokens);
-      if constexpr (N == 2) {
-        const float a = fmaxf(lane_f(scales, kStage + sub), 0x1p-40f), b = fmaxf(lane_f(scales, kStage + sub + 1), 0x1p-40f);
-        const int passes = __ballot(a < 0x1p-4f * b || b < 0x1p-4f * a) ? 2 : 1;  // one by one, if they lie apart
-#pragma unroll 1
-        for (int pass = 0; pass < passes; ++pass) {
-          const int these[2] = {pass == 0 ? valid[0] : 0, pass == passes - 1 ? valid[1] : 0};
-          attend_tiles<F16, DB, N, WR == 8>(A, q, s_stage, sub, these, scales, lane, S);
-        }
-      } else if constexpr (RW == 32) attend_tiles<F16, DB, N, WR == 8>(A, q, s_stage, sub, valid, scales, lane, S);
-      else attend_tiles<F16, DB>(A, q, s_stage, sub, valid, scales, lane, S);
-    }
+    for (int i = 0; i < kStage; i += WT)
+      attend_tile<F16, DB, WR == 8>(q, s_stage, i + wt, valid_of(here, t, i + wt, tokens), scales, lane, S);
   }
 
   float m = S.m, l = row_sum<RW>(S.l);

@@ -644,6 +644,61 @@ def test_attention_any_finite_key_scales(M, heads):
 
 
 @pytest.mark.parametrize("M,heads", [(1, 4), (5, 3), (20, 2), (40, 6), (61, 8)])
+def test_attention_lowest_scores(M, heads):
+    """Of tokens whose scores are all far below 0 the largest has the weight, down to the lowest fp32 (2.36e38 times log2 e)."""
+    note("attention lowest scores M=%d heads=%d" % (M, heads))
+    dim, page = 64, 32
+    for scale in (-1e30, -1e38, -1.5e38, -2.3e38):
+        code = torch.full((4, 1, page, dim), 0x38, dtype=torch.uint8)
+        code[:, :, 1::2] = 0x3C  # keys of 1 and 1.5: scores of 2/3 scale and scale; the nodes' are 3/4 scale
+        code[2, 0, 16] = 0x30    # one of 1/3, or of a node 1/4
+        values = torch.randint(0x30, 0x40, (4, 1, dim, page), generator=torch.Generator().manual_seed(3)).to(torch.uint8)
+        one = torch.ones((4, 1), device="cuda")
+        cache = hs.PagedCache(code.cuda(), values.cuda(), one, one.clone())
+        table = torch.tensor([[0, 1, 2, 3], [0, 1, 3, 3], [3, 3, 3, 3]], dtype=torch.int32, device="cuda")
+        length = torch.tensor([128, 1, 0], dtype=torch.int32, device="cuda")
+        q = torch.full((3, M, heads, dim), 1.0 / 96, dtype=torch.float32).to(torch.bfloat16).cuda()
+        k = torch.full((3, M, 1, dim), 1.125, dtype=torch.bfloat16, device="cuda")
+        v = torch.randn((3, M, 1, dim), generator=torch.Generator().manual_seed(4)).to(torch.bfloat16).cuda()
+        own = torch.tensor([[1 << n for n in range(M)]], dtype=torch.int64).expand(3, M).contiguous().cuda()
+        got = hs.tree_attention(q, k, v, cache, table, length, mask=own, scale=scale)
+        want = v.expand(3, M, heads, dim).clone()
+        want[0] = values[2, 0, :, 16].view(torch.float8_e4m3fn).to(torch.bfloat16).cuda()  # the one of 1/3
+        want[1] = values[0, 0, :, 0].view(torch.float8_e4m3fn).to(torch.bfloat16).cuda()   # 2/3, before the node's 3/4
+        assert torch.equal(got, want), scale
+
+
+@pytest.mark.parametrize("M,heads", [(1, 4), (5, 3), (20, 2), (40, 6), (61, 8)])
+@pytest.mark.parametrize("apart", [0, 2, 40])
+def test_attention_large_scores(M, heads, apart):
+    """Scores that fp32 holds in steps of 1/8 to 1e31: the largest token has all the weight, of early and late pages, with
+    values of any scale."""
+    note("attention large scores M=%d heads=%d scales 2^%d apart" % (M, heads, apart))
+    dim, page, n = 64, 32, 300
+    g = torch.Generator().manual_seed(17)
+    for scale in (1e5, 3e7, 1e9, 1e15, 1e30, 3e36, -1e5, -1e8, -1e12, -3e36):
+        code = torch.randint(0x28, 0x38, (10, 1, page, dim), generator=g).to(torch.uint8)  # 1/4 to 15/16
+        values = torch.randint(0x30, 0x40, (10, 1, dim, page), generator=g).to(torch.uint8)
+        best = [5, 70, 130, 299]  # of each query
+        code = code.repeat(4, 1, 1, 1)
+        values = values.repeat(4, 1, 1, 1)
+        for b, t in enumerate(best):
+            code[10 * b + t // page, 0, t % page] = 0x40 if scale > 0 else 0x10  # 2, or 1/16
+        sv = torch.exp2(torch.randint(-apart, apart + 1, (40, 1), generator=g).float())
+        cache = hs.PagedCache(code.cuda(), values.cuda(), torch.ones((40, 1), device="cuda"), sv.cuda())
+        table = torch.arange(40).reshape(4, 10).int().cuda()
+        length = torch.full((4,), n, dtype=torch.int32, device="cuda")
+        q = torch.full((4, M, heads, dim), 1.0 / 64, dtype=torch.bfloat16, device="cuda")
+        k = torch.full((4, M, 1, dim), 0.5, dtype=torch.bfloat16, device="cuda")
+        v = torch.randn((4, M, 1, dim), generator=g).to(torch.bfloat16).cuda()
+        got = hs.tree_attention(q, k, v, cache, table, length, scale=scale).cpu()
+        for b, t in enumerate(best):
+            p = 10 * b + t // page
+            want = values[p, 0, :, t % page].view(torch.float8_e4m3fn).float() * sv[p]
+            assert torch.all((got[b].float() - want).abs() <= want.abs() * 2.0 ** -7), (scale, b)
+
+
+@pytest.mark.parametrize("M,heads", [(1, 4), (5, 3), (20, 2), (40, 6), (61, 8)])
 def test_attention_value_scales_of_zero(M, heads):
     """Values of a page whose scale is 0 are 0, and their weights count."""
     note("attention value scales of zero M=%d heads=%d" % (M, heads))
