@@ -1121,3 +1121,68 @@ def test_rounds_of_a_tree_as_a_program_runs_them(mode):
             code = cache.k.view(torch.uint8)[p, :, o].cpu().numpy()
             s = cache.k_scale[p].cpu().numpy()[:, None]
             assert np.all(np.abs(draft.VALUES[code] * s - x[t]) <= np.abs(x[t]) * 2.0 ** -4 + s * 2.0 ** -9)
+
+
+@pytest.mark.parametrize("mode", [hs.SAMPLE, hs.GREEDY])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_rounds_see_and_keep_what_the_cache_should_hold(dtype, mode):
+    """As above; in every round the attention is the oracle's over the cache's codes as they are, and in the end keys and
+    values are those of the tokens that were kept, so that a round that reads or writes a wrong place is seen."""
+    note("rounds, attention and values %s mode=%d" % (dtype, mode))
+    g = torch.Generator().manual_seed(43)
+    B, W, K, M, depth, V, kv, heads, dim, page = 3, 4, 6, 12, 3, 300, 2, 4, 64, 32
+    embed = torch.randn((V, dim), generator=g)
+    wq, wk, wv = (torch.randn((dim, n, dim), generator=g) * dim ** -0.5 for n in (heads, kv, kv))
+    wo = torch.randn((heads * dim, V), generator=g) * 2.0
+    project = lambda t, w: torch.einsum("...d,dhe->...he", embed[t.clamp(min=0).long()], w).to(dtype)  # noqa: E731
+    cache = hs.PagedCache.empty(16, kv, page, dim)
+    for t in (cache.k_scale, cache.v_scale):
+        t.fill_(float("nan"))  # what no append has written matters to nobody
+    table = torch.randperm(16, generator=g)[:15].reshape(B, 5).int().cuda()
+    length = torch.zeros(B, dtype=torch.int32, device="cuda")
+    prompt = torch.randint(0, V, (B, 37), generator=g)
+    given = torch.tensor([37, 20, 1], dtype=torch.int32, device="cuda")
+    hs.cache_append(cache, table, length, project(prompt, wk).cuda(), project(prompt, wv).cuda(), count=given)
+    length += given
+    kept = [prompt[b, :int(given[b])].tolist() for b in range(B)]
+    root = torch.randint(0, V, (B,), generator=g)
+    growth = hs.TreeGrowth(B, depth, W, K, M, device="cuda:0")
+    for _ in range(6):
+        growth.level(torch.randn((B, 1, V + 4), generator=g).cuda().to(torch.bfloat16), V=V)
+        for _ in range(depth - 1):
+            growth.level(torch.randn((B, W, V + 4), generator=g).cuda().to(torch.bfloat16), V=V)
+        tree_ = growth.tree()
+        token = tree_["token"].cpu()
+        token[:, 0] = root.int()
+        q, k, v = (project(token, w) for w in (wq, wk, wv))
+        out = hs.tree_attention(q.cuda(), k.cuda(), v.cuda(), cache, table, length, mask=tree_["mask"],
+                                count=tree_["count"])
+        codes = [t.cpu() for t in cache.tensors.values()]
+        ref, mean, most = draft.attention(*[t.double().numpy() for t in (q, k, v)], codes[0].view(torch.uint8).numpy(),
+                                          codes[1].view(torch.uint8).numpy(), codes[2].numpy(), codes[3].numpy(),
+                                          table.cpu().numpy(), length.cpu().numpy(), mask=tree_["mask"].cpu().numpy(),
+                                          count=tree_["count"].cpu().numpy(), scale=dim ** -0.5)
+        for b in range(B):
+            n, a = int(tree_["count"][b]), most[b][..., None]
+            rel = 2.0 ** -11 + 2 * (dim + 8) * 2.0 ** -24 * a + 2 * (2.0 ** -22 + 2.0 ** -23 + 2.0 ** -22 * a) + \
+                2 * (int(length[b]) + M + 300) * 2.0 ** -24
+            tol = HALF[dtype] * np.maximum(np.abs(ref[b]), torch.finfo(dtype).tiny) + rel * mean[b]
+            assert n > 1 and np.all((np.abs(out[b].cpu().double().numpy() - ref[b]) <= tol)[:n]), b
+        logits = torch.nn.functional.pad((out.float().reshape(B, M, -1) @ wo.cuda()).to(torch.bfloat16), (0, 4))
+        got = hs.verify(logits, tree_["token"], numbers(g, B, M).cuda(), parent=tree_["parent"], count=tree_["count"],
+                        V=V, mode=mode, depth=depth)
+        hs.cache_append(cache, table, length, k.cuda(), v.cuda(), path=got["path"], count=got["length"])
+        length += got["length"]
+        for b in range(B):
+            n = int(got["length"][b])
+            kept[b] += token[b, got["path"][b, :n].cpu().long()].tolist()
+            root[b] = int(got["token"][b, n - 1])
+    assert [len(t) for t in kept] == length.tolist()
+    for codes, scale, w in ((cache.k.transpose(2, 3), cache.k_scale, wk), (cache.v, cache.v_scale, wv)):
+        codes, scale = codes.contiguous().view(torch.uint8).cpu().numpy(), scale.cpu().numpy()  # [pages][heads][dim][page]
+        for b in range(B):
+            x = project(torch.tensor(kept[b]), w).double().numpy()
+            for t in range(len(kept[b])):
+                p, o = int(table[b, t // page]), t % page
+                y = draft.VALUES[codes[p, :, :, o]] * scale[p][:, None]
+                assert np.all(np.abs(y - x[t]) <= np.abs(x[t]) * 2.0 ** -4 + scale[p][:, None] * 2.0 ** -9), (b, t)
