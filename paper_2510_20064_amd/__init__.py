@@ -1064,6 +1064,8 @@ class Verify:
 
     def set_logits(self, target: torch.Tensor, drafter: Optional[torch.Tensor] = None) -> None:
         """Other logits tensors of the same shapes and type."""
+        if self.M == 1:
+            drafter = None
         _need((drafter is None) == (self.drafter is None), "with a drafter or without one, as before")
         view = _logits(target, self.B, self.M, self.V, self.dtype, "target")
         other = hs_view() if drafter is None else \

@@ -373,6 +373,23 @@ def test_verify_large_chains(dtype, drafted):
         assert not drafted or got["length"].max() > 3
 
 
+def test_verify_of_roots_alone_takes_a_drafter_without_rows():
+    """M = 1 as a loop over drafts of any length has it: a drafter of no rows, when the plan is made and later."""
+    note("verify roots with a drafter of no rows")
+    g = torch.Generator().manual_seed(59)
+    z, none = rows(g, 3, 1, 64, torch.float32).cuda(), torch.empty((3, 0, 64), device="cuda")
+    token, u = torch.full((3, 1), -1, dtype=torch.int32, device="cuda"), numbers(g, 3, 1).cuda()
+    plan = hs.Verify(z, token, u, drafter=none)
+    first = {n: t.clone() for n, t in plan.run().items()}
+    other = rows(g, 3, 1, 64, torch.float32).cuda()
+    for drafter in (none, None):
+        plan.set_logits(other, drafter)
+        got, want = plan.run(), hs.verify(other, token, u)
+        assert all(torch.equal(got[n], want[n]) for n in want)
+        plan.set_logits(z, drafter)
+        assert all(torch.equal(plan.run()[n], first[n]) for n in first)
+
+
 # ---- hs_tree_attention -----------------------------------------------------------------------------------
 
 HALF = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
