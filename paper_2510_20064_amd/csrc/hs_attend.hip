@@ -446,38 +446,6 @@ __device__ inline float follow(State<DB, RW>& S, float top) {
   }
   return S.m - kHeadroom;
 }
-// Whether a tile that has tokens is of a page whose scale of values is far below the largest met. bias: log2 of the scale.
-template <int DB, int RW>
-__device__ __forceinline__ bool apart(State<DB, RW>& S, float bias, int valid) {
-  if (valid == 0) return false;
-  S.base = fmaxf(S.base, bias);
-  return bias < S.base - kSpread;
-}
-// Whether scores are so large that fp32 holds them in steps of 1/2 or more: a weight's exponent is no longer their difference
-// if what is added to a product is rounded before. Products are then rounded first, and m follows them alone.
-__device__ inline bool is_big(float top) { return fabsf(top) > 0x1p22f && fabsf(top) < INFINITY; }
-// While such a tile is added, O is held 2^lift times as large, lift per row, and off, what is added to products, and inv, what
-// a weight counts for in the sum, are such that its weights are: as much as brings the row's largest weight of the tile to
-// 2^12, unless O would overflow; of big scores what O needs where weights are 2^(s - m). top: the lane's largest score, as
-// in follow. To be undone by S.scale(2^-lift).
-template <int DB, int RW>
-__device__ inline float lifted(State<DB, RW>& S, float top, bool big, float bias, float& off, float& inv) {
-  float most = 0.0f;
-#pragma unroll
-  for (int n = 0; n < S.kGroups; ++n) {
-    const f32x4 o = S.get(n);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(o[i]) <= FLT_MAX ? fabsf(o[i]) : 0.0f);
-    __builtin_amdgcn_sched_barrier(0);  // (a rare path that takes no registers from the others)
-  }
-  const int e = __builtin_amdgcn_frexp_expf(row_max<RW>(most));
-  float lift = rintf(fmaxf(fminf(S.m - row_max<RW>(top), (float)(124 - max(e, 0))), 0.0f));
-  if (big) lift = -(bias + kHeadroom);
-  off = big ? -S.m : off + lift;
-  inv *= __builtin_amdgcn_exp2f(-lift);
-  S.scale(__builtin_amdgcn_exp2f(lift));
-  return lift;
-}
 template <int N>
 __device__ inline float max_of(const float (&x)[N]) {
   float top = x[0];
@@ -494,129 +462,187 @@ __device__ inline float sum_of(const float (&w)[N]) {
   else return a[0];
 }
 
-// The `sub`-th tile of the stage in LDS, of `valid` tokens: products, one step of the softmax, products.
-template <bool F16, int DB, bool WIDE>
-__device__ __forceinline__ void attend_tile(const V8<F16> (&q)[2 * DB], const uint8_t* lds, int sub, int valid, float scales,
-                                            int lane, State<DB, 32>& S) {
+// A lane's products of a tile: those of its row with RW / 2 tokens, the first of which is RW / 2 times its part of the wave.
+template <int RW>
+struct Scores {
+  f32x16 a{};
+  __device__ float at(int i) const { return a[i]; }
+  __device__ void set(int i, float x) { a[i] = x; }
+};
+template <>
+struct Scores<16> {
+  f32x4 a[2]{};
+  __device__ float at(int i) const { return a[i / 4][i % 4]; }
+  __device__ void set(int i, float x) { a[i / 4][i % 4] = x; }
+};
+// A tile of the stage in LDS: its tokens, the factor of its products, log2 of its values' scale and what a weight counts for in
+// the sum; the largest score's product, and that score with the scale.
+struct Tile {
+  int valid;
+  float f, bias, inv, best, top;
+};
+// The products of N tiles from the `sub`-th on, which do not wait for each other.
+template <bool F16, int DB, int RW, bool WIDE, int N, int NQ>
+__device__ __forceinline__ void multiply(const V8<F16> (&q)[NQ], const uint8_t* lds, int sub, const int (&valid)[N],
+                                         float scales, int lane, Scores<RW> (&s)[N], Tile (&t)[N]) {
   using St = Staged<DB, WIDE>;
-  const int rho = lane & 31, half = lane >> 5;
-  const uint8_t* kp = lds + (32 * sub + rho) * St::kKeyPitch + 16 * half * St::kCode;
-  f32x16 s = {};
-#pragma unroll
-  for (int j = 0; j < DB; ++j) {
-    V8<F16> k[2];
-    operands<F16, WIDE>(kp + 32 * j * St::kCode, k);
-    s = mfma(k[0], q[2 * j], s);
-    s = mfma(k[1], q[2 * j + 1], s);
-  }
-  const float vs = fminf(fmaxf(lane_f(scales, kStage + sub), 0x1p-40f), 0x1p40f), bias = __builtin_amdgcn_logf(vs);
-  const float f = lane_f(scales, sub);
-  float inv = __builtin_amdgcn_rcpf(vs);
-  if (valid < 32) {    // what lies behind the last token has no weight
-    asm volatile("");  // (a branch, not selects for every tile)
-    const float none = f < 0.0f ? INFINITY : -INFINITY;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = 16 * half + i < valid ? s[i] : none;
-  }
-  float hi = s[0], lo = hi;  // the largest score is that of the largest product, or of the least
-#pragma unroll
-  for (int i = 1; i < 16; ++i) {
-    hi = fmaxf(hi, s[i]);
-    lo = fminf(lo, s[i]);
-  }
-  const float best = f < 0.0f ? lo : hi;
-  float top = fmaf(best, f, bias);
-  const bool rare = __ballot(apart(S, bias, valid) || is_big(top)) != 0;
-  bool big = false;
-  if (rare && __ballot(is_big(top))) {
-    big = true;
-    top = best * f;
-  }
-  float off = bias - follow(S, top), lift = 0.0f;
-  if (rare) lift = lifted(S, top, big, bias, off, inv);
-  float x[16];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) x[i] = fmaf(s[i], f, off);
-  if (big) {
-    asm volatile("");
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = s[i] * f + off;
-  }
-#pragma unroll
-  for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(x[i]);
-  S.l = fmaf(sum_of(x), inv, S.l);
-  const f16x8 p[2] = {narrow(x), narrow(x + 8)};
-  const uint8_t* vp = lds + St::kKeys + rho * St::kValuePitch + (32 * sub + 16 * half) * St::kCode;
-#pragma unroll
-  for (int j = 0; j < DB; ++j) {
-    f16x8 v[2];
-    operands<true, WIDE>(vp + 32 * j * St::kValuePitch, v);
-    S.o32[j] = mfma(v[0], p[0], S.o32[j]);
-    S.o32[j] = mfma(v[1], p[1], S.o32[j]);
-  }
-  if (rare) S.scale(__builtin_amdgcn_exp2f(-lift));
-}
-
-// The same for 16 rows: products of 16 x 16 x 32.
-template <bool F16, int DB, bool WIDE>
-__device__ __forceinline__ void attend_tile(const V8<F16> (&q)[DB], const uint8_t* lds, int sub, int valid, float scales,
-                                            int lane, State<DB, 16>& S) {
-  using St = Staged<DB, WIDE>;
-  static_assert(!WIDE, "codes");
-  const int rho = lane & 15, g = lane >> 4;
-  const uint8_t* kp = lds + (32 * sub + rho) * St::kKeyPitch + 8 * g;
-  f32x4 s[2] = {};
+  const int rho = lane % RW, c = lane / RW;
+  const uint8_t* kp = lds + (32 * sub + rho) * St::kKeyPitch + RW / 2 * c * St::kCode;
 #pragma unroll
   for (int j = 0; j < DB; ++j)
 #pragma unroll
-    for (int a = 0; a < 2; ++a) {
-      const u32x2 k = *reinterpret_cast<const u32x2*>(kp + 16 * a * St::kKeyPitch + 32 * j);
-      s[a] = mfma(widen<F16>(k.x, k.y), q[j], s[a]);
+    for (int n = 0; n < N; ++n) {
+      if constexpr (RW == 32) {
+        V8<F16> k[2];
+        operands<F16, WIDE>(kp + 32 * n * St::kKeyPitch + 32 * j * St::kCode, k);
+        s[n].a = mfma(k[0], q[2 * j], s[n].a);
+        s[n].a = mfma(k[1], q[2 * j + 1], s[n].a);
+      } else {
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+          const u32x2 k = *reinterpret_cast<const u32x2*>(kp + (32 * n + 16 * a) * St::kKeyPitch + 32 * j);
+          s[n].a[a] = mfma(widen<F16>(k.x, k.y), q[j], s[n].a[a]);
+        }
+      }
     }
-  const float vs = fminf(fmaxf(lane_f(scales, kStage + sub), 0x1p-40f), 0x1p40f), bias = __builtin_amdgcn_logf(vs);
-  const float f = lane_f(scales, sub);
-  float inv = __builtin_amdgcn_rcpf(vs);
-  if (valid < 32) {
-    asm volatile("");
-    const float none = f < 0.0f ? INFINITY : -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s[i / 4][i % 4] = 8 * g + i < valid ? s[i / 4][i % 4] : none;
-  }
-  float hi = s[0][0], lo = hi;
+  for (int n = 0; n < N; ++n) {
+    const float vs = fminf(fmaxf(lane_f(scales, kStage + sub + n), 0x1p-40f), 0x1p40f);
+    t[n].valid = valid[n];
+    t[n].f = lane_f(scales, sub + n);
+    t[n].bias = __builtin_amdgcn_logf(vs);
+    t[n].inv = __builtin_amdgcn_rcpf(vs);
+    if (valid[n] < 32) {  // what lies behind the last token has no weight
+      asm volatile("");   // (a branch, not selects for every tile)
+      const float none = t[n].f < 0.0f ? INFINITY : -INFINITY;
 #pragma unroll
-  for (int i = 1; i < 8; ++i) {
-    hi = fmaxf(hi, s[i / 4][i % 4]);
-    lo = fminf(lo, s[i / 4][i % 4]);
+      for (int i = 0; i < RW / 2; ++i) s[n].set(i, RW / 2 * c + i < valid[n] ? s[n].at(i) : none);
+    }
+    float hi = s[n].at(0), lo = hi;  // the largest score is that of the largest product, or of the least
+#pragma unroll
+    for (int i = 1; i < RW / 2; ++i) {
+      hi = fmaxf(hi, s[n].at(i));
+      lo = fminf(lo, s[n].at(i));
+    }
+    t[n].best = t[n].f < 0.0f ? lo : hi;
+    t[n].top = fmaf(t[n].best, t[n].f, t[n].bias);
   }
-  const float best = f < 0.0f ? lo : hi;
-  float top = fmaf(best, f, bias);
-  const bool rare = __ballot(apart(S, bias, valid) || is_big(top)) != 0;
+}
+// The largest scale of values met with a tile's, which counts if it has tokens, and whether that is far below the largest
+// (as log2).
+__device__ inline float met(float base, const Tile& t) { return t.valid > 0 ? fmaxf(base, t.bias) : base; }
+__device__ inline bool is_far(float base, const Tile& t) { return t.valid > 0 && t.bias < base - kSpread; }
+// Whether scores are so large that fp32 holds them in steps of 1/2 or more: a weight's exponent is no longer their difference
+// if what is added to a product is rounded before.
+__device__ inline bool is_big(float top) { return fabsf(top) > 0x1p22f && fabsf(top) < INFINITY; }
+// O and the `sub`-th tile's values with weights p.
+template <int DB, int RW, bool WIDE>
+__device__ __forceinline__ void add_values(const uint8_t* lds, int sub, const f16x8 (&p)[RW / 16], int lane, State<DB, RW>& S) {
+  using St = Staged<DB, WIDE>;
+  const int rho = lane % RW, c = lane / RW;
+  const uint8_t* vp = lds + St::kKeys + rho * St::kValuePitch + (32 * sub + RW / 2 * c) * St::kCode;
+  if constexpr (RW == 32) {
+#pragma unroll
+    for (int j = 0; j < DB; ++j) {
+      f16x8 v[2];
+      operands<true, WIDE>(vp + 32 * j * St::kValuePitch, v);
+      S.o32[j] = mfma(v[0], p[0], S.o32[j]);
+      S.o32[j] = mfma(v[1], p[1], S.o32[j]);
+    }
+  } else {
+#pragma unroll
+    for (int n = 0; n < 2 * DB; ++n) {
+      const u32x2 v = *reinterpret_cast<const u32x2*>(vp + 16 * n * St::kValuePitch);
+      S.o16[n] = mfma(widen<true>(v.x, v.y), p[0], S.o16[n]);
+    }
+  }
+}
+template <int N>
+__device__ inline void narrow_all(const float (&x)[N], f16x8 (&p)[N / 8]) {
+#pragma unroll
+  for (int i = 0; i < N / 8; ++i) p[i] = narrow(x + 8 * i);
+}
+
+// What comes before the weights of a tile of a scale far below the largest met, or of big scores, m having followed top. While
+// it is added, O is held 2^lift times as large, lift per row, and its weights are: as much as brings the row's largest of the
+// tile to 2^12, unless O would overflow. Of big scores products are rounded first, m follows them alone, and weights are
+// 2^(s - m): lift is what O needs for that. To be undone by S.scale(2^-lift).
+template <int DB, int RW>
+__device__ inline float lifted(State<DB, RW>& S, float top, bool big, Tile& t, float& off) {
+  float most = 0.0f;
+#pragma unroll
+  for (int n = 0; n < S.kGroups; ++n) {
+    const f32x4 o = S.get(n);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(o[i]) <= FLT_MAX ? fabsf(o[i]) : 0.0f);
+    __builtin_amdgcn_sched_barrier(0);  // (a rare path that takes no registers from the others)
+  }
+  const int e = __builtin_amdgcn_frexp_expf(row_max<RW>(most));
+  float lift = rintf(fmaxf(fminf(S.m - row_max<RW>(top), (float)(124 - max(e, 0))), 0.0f));
+  if (big) lift = -(t.bias + kHeadroom);
+  off = big ? -S.m : off + lift;
+  t.inv *= __builtin_amdgcn_exp2f(-lift);
+  S.scale(__builtin_amdgcn_exp2f(lift));
+  return lift;
+}
+
+// The `sub`-th tile of the stage in LDS, of `valid` tokens: products, one step of the softmax, products.
+template <bool F16, int DB, int RW, bool WIDE, int NQ>
+__device__ __forceinline__ void attend_tile(const V8<F16> (&q)[NQ], const uint8_t* lds, int sub, int valid, float scales,
+                                            int lane, State<DB, RW>& S) {
+  Scores<RW> s[1];
+  Tile t[1];
+  multiply<F16, DB, RW, WIDE>(q, lds, sub, {valid}, scales, lane, s, t);
+  S.base = met(S.base, t[0]);
+  float top = t[0].top;
+  const bool rare = __ballot(is_far(S.base, t[0]) || is_big(top)) != 0;
   bool big = false;
   if (rare && __ballot(is_big(top))) {
     big = true;
-    top = best * f;
+    top = t[0].best * t[0].f;
   }
-  float off = bias - follow(S, top), lift = 0.0f;
-  if (rare) lift = lifted(S, top, big, bias, off, inv);
-  float x[8];
+  float off = t[0].bias - follow(S, top), lift = 0.0f;
+  if (rare) lift = lifted(S, top, big, t[0], off);
+  float x[RW / 2];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = fmaf(s[i / 4][i % 4], f, off);
+  for (int i = 0; i < RW / 2; ++i) x[i] = fmaf(s[0].at(i), t[0].f, off);
   if (big) {
     asm volatile("");
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = s[i / 4][i % 4] * f + off;
+    for (int i = 0; i < RW / 2; ++i) x[i] = s[0].at(i) * t[0].f + off;
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_exp2f(x[i]);
-  S.l = fmaf(sum_of(x), inv, S.l);
-  const f16x8 p = narrow(x);
-  const uint8_t* vp = lds + St::kKeys + rho * St::kValuePitch + 32 * sub + 8 * g;
-#pragma unroll
-  for (int n = 0; n < 2 * DB; ++n) {
-    const u32x2 v = *reinterpret_cast<const u32x2*>(vp + 16 * n * St::kValuePitch);
-    S.o16[n] = mfma(widen<true>(v.x, v.y), p, S.o16[n]);
-  }
+  for (int i = 0; i < RW / 2; ++i) x[i] = __builtin_amdgcn_exp2f(x[i]);
+  S.l = fmaf(sum_of(x), t[0].inv, S.l);
+  f16x8 p[RW / 16];
+  narrow_all(x, p);
+  add_values<DB, RW, WIDE>(lds, sub, p, lane, S);
   if (rare) S.scale(__builtin_amdgcn_exp2f(-lift));
+}
+// Two tiles at once, whose products do not wait for each other. False, with nothing added, if they are not plain ones.
+template <bool F16, int DB, bool WIDE, int NQ>
+__device__ __forceinline__ bool attend_two(const V8<F16> (&q)[NQ], const uint8_t* lds, int sub, const int (&valid)[2],
+                                           float scales, int lane, State<DB, 32>& S) {
+  Scores<32> s[2];
+  Tile t[2];
+  multiply<F16, DB, 32, WIDE>(q, lds, sub, valid, scales, lane, s, t);
+  const float base = met(met(S.base, t[0]), t[1]), top = fmaxf(t[0].top, t[1].top);
+  if (__ballot(is_far(base, t[0]) || is_far(base, t[1]) || is_big(t[0].top) || is_big(t[1].top))) return false;
+  S.base = base;
+  const float from = follow(S, top);
+  f16x8 p[2][2];
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    const float off = t[n].bias - from;
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(s[n].at(i), t[n].f, off));
+    S.l = fmaf(sum_of(x), t[n].inv, S.l);
+    narrow_all(x, p[n]);
+  }
+#pragma unroll
+  for (int n = 0; n < 2; ++n) add_values<DB, 32, WIDE>(lds, sub + n, p[n], lane, S);
+  return true;
 }
 
 // 32 nodes in LDS, in their own type: keys like a tile's, values by dimension.
@@ -834,9 +860,20 @@ __device__ __forceinline__ void attend_range(const AttendArgs& A, int b, int h, 
       load_stage<DB, NW>(A, h, t + kStage, pages, wv, lane, L);
     }
     if (!busy) continue;
+    if constexpr (WR == 8) {  // (two tiles at once: 32 trees of 61 nodes 209 us, one at a time 218; with four waves no gain)
 #pragma unroll
-    for (int i = 0; i < kStage; i += WT)
-      attend_tile<F16, DB, WR == 8>(q, s_stage, i + wt, valid_of(here, t, i + wt, tokens), scales, lane, S);
+      for (int i = 0; i < kStage; i += 2) {
+        const int valid[2] = {valid_of(here, t, i, tokens), valid_of(here, t, i + 1, tokens)};
+        if (!attend_two<F16, DB, true>(q, s_stage, i, valid, scales, lane, S))
+#pragma unroll 1
+          for (int n = i; n < i + 2; ++n)
+            attend_tile<F16, DB, RW, true>(q, s_stage, n, valid_of(here, t, n, tokens), scales, lane, S);
+      }
+    } else {
+#pragma unroll
+      for (int i = wt; i < kStage + wt; i += WT)
+        attend_tile<F16, DB, RW, false>(q, s_stage, i, valid_of(here, t, i, tokens), scales, lane, S);
+    }
   }
 
   float m = S.m, l = row_sum<RW>(S.l);
