@@ -1013,9 +1013,10 @@ class Verify:
     target [B][M][>= V] (V contiguous, rows 16-byte aligned), node 0 the root; token [B][M] i32 and u [B][M] f64
     (uniform in [0, 1); not used, and may be None, with mode=GREEDY). parent [B][M] i32 (DraftTree's) or None: a
     chain. drafter [B][M - 1][>= V]: the rows that a chain's tokens were drawn from; None: the children are fixed.
-    count [B] i32: nodes of each query. depth: the draft's longest path, M - 1 if None. run() fills and returns `out`:
-    path [B][M] i32 (the root and the accepted nodes, then -1), token [B][M] i32 (what comes out, then -1) and length
-    [B] i32 of both. What the dict `out` lacks is made and added to it, and belongs to the stream that is current then
+    count [B] i32: nodes of each query. depth: the draft's longest path, M - 1 if None; give a tree's own, for large
+    batches are then read level by level, only the rows on the paths (32 trees of 61 nodes 164 -> 53 us). run() fills
+    and returns `out`: path [B][M] i32 (the root and the accepted nodes, then -1), token [B][M] i32 (what comes out,
+    then -1) and length [B] i32 of both. What the dict `out` lacks is made and added to it, and belongs to the stream that is current then
     (see BeamStep); `workspace` may be shared by calls that do not overlap."""
 
     def __init__(self, target: torch.Tensor, token: torch.Tensor, u: Optional[torch.Tensor] = None,

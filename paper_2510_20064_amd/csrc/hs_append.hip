@@ -112,9 +112,9 @@ __device__ inline float scale_of(float most) {
 // bytes of a row. A workgroup has 256, 512 or 1024 threads, as many as hold a page's squares two a thread (1024: a page of
 // 256 tokens of 256 dims) in registers between the pass for the largest and the pass that writes. A square's values by
 // dimension are words of four tokens: through LDS, so that consecutive lanes write consecutive words of a dimension.
-// Bound: 8 prompts of 8192 tokens of 8 heads of 128 (302 MB read and written) 87 us, 3.5 TB/s; waiting for the chain
-// count, length, table, rows (73% of the waves' time) with the five workgroups a CU holds. Values written from the squares, 4
-// bytes a row, 127; every value tested for infinities and clamped, 145; both of the writing loops in one, with 168
+// Bound: 8 prompts of 8192 tokens of 8 heads of 128 (302 MB read and written) 77 to 85 us, 3.6 to 3.9 TB/s; waiting for the
+// chain count, length, table, rows (73% of the waves' time) with the five workgroups a CU holds. Steps, when it took 87: values
+// written from the squares, 4 bytes a row, 127; every value tested for infinities and clamped, 145; both of the writing loops in one, with 168
 // registers, 122; one square a thread of twice the threads 112. Pages of 256 tokens of 256 dims by 256 threads, which read
 // twice what they do not hold, 63 us for two prompts of 7420 tokens and four heads, by 1024 27.
 template <bool F16, int NT>

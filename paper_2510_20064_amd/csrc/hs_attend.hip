@@ -17,26 +17,30 @@
 // queries or its tiles. From memory to registers without LDS, each wave its own tiles, a load of keys took 32 bytes of 32
 // lines (61 nodes over 16 thousand tokens 101 us and 46, 32 such over 8 thousand 509 and 230).
 // Codes of 8 bits become bf16 or fp16 without error (3 bits of mantissa, 2^-9 to 448), one instruction for two.
-// Weights are rounded to fp16 (relative 2^-11, an eighth of a bf16 output's own rounding), as 2^12 w, so that what lies
-// below 2^-36 of the largest is lost and not what lies below 2^-24; m follows only in steps above 2^3 (w stays
+// Weights are rounded to fp16 (relative 2^-11, an eighth of a bf16 output's own rounding), as 2^12 w, so that what is lost lies
+// below 2^-36 of the largest x and not below 2^-24; m follows only in steps above 2^3 (w stays
 // below 2^16), which spares most tiles the multiplication of O. Sums and O are fp32.
 // m follows x whatever a page's codes are, so a page whose scale an outlier set would take fp16's range from pages of finer
-// scales. While tiles whose scale is more than 2^kSpread below the largest met are added, O and their weights are held larger
-// (see lifted). Nodes' values have no scale: m follows them as if it were 2^kNodes, so that pages down to 2^-20 are no finer
-// ones, and their weights, which that makes larger than fp16, are two bf16 each. (One query's tree 41.6 us and 42.2, 32 trees
-// 198 and 204, fp16 nodes of short drafts 15.0 and 15.6; all weights as two bf16, whose range is fp32's, 47.3, 249 and 15.9; a
-// range done once more where its scales lie apart, as a second loop, 43.4, 207 and 15.2.)
+// scales. While a tile whose scale is more than 2^kSpread below the largest met is added, O and its weights are held larger,
+// and also while one of scores beyond 2^22 is, whose products are rounded first (see lifted). Nodes' values have no scale: m
+// follows them as if it were 2^kNodes, so that pages down to 2^-20 are no finer ones, and their weights, which that makes
+// larger than fp16, are two bf16 each. That costs tiles that need none of it 3 to 6% (one query's tree 41.4 us and 42.6, 32
+// trees 198 and 207 to 210, fp16 nodes of short drafts 15.0 and 15.9, a token 13.2 and 13.6). Weights as two bf16 for all,
+// whose range is fp32's: 47.3, 249, 15.9 and 13.3.
 //
-// Split. The stages of all queries are cut into as many equal ranges as the device holds workgroups, so that lengths that
-// differ, and one query alone, load it alike; what a range holds of a query that others share goes to the workspace, and
-// hs_attend_join_kernel adds the parts in their order. See attend_geom for when a query is a workgroup's instead.
+// Split. The stages of all queries' cached tokens are cut into as many equal ranges as the device holds workgroups, so that
+// lengths that differ, and one query alone, load it alike; what a range holds of a query that others share goes to the
+// workspace, and hs_attend_join_kernel adds the parts in their order. See attend_geom for when a query is a workgroup's
+// instead. Nodes do not count: the range with a query's end has up to 64 of them too, and with few stages a range (one tree
+// over 16 thousand: four) sets the time.
 //
 // What bounds it, heads of 128, eight cached for 32. One token over 512: two launches and four dependent reads (length,
-// table, scales, codes), 13 us. 32 tokens over up to 16 thousand, 537 MB: the memory, 116 to 119 us with the join's 6,
-// 4.6 TB/s, where a large copy reaches 4.8. 32 trees of 61 nodes over up to 8 thousand, 131 GFLOP: 208 to 220 us, 0.6
-// PFLOP/s, where a large product reaches 1.4: the matrix units are busy 32% of the time, the vector units 43% (152
-// instructions a wave and tile), LDS 26%, and a wave waits 48% of its time, which the second wave that the registers leave
-// a SIMD fills half. No part takes more than an eighth when it is left out. No gain: the next
+// table, scales, codes), 13.6 us. 32 tokens over up to 16 thousand, 537 MB: the memory, 115 to 118 us with the join's 5.4,
+// 4.6 TB/s, where a large copy reaches 4.8. 32 trees of 61 nodes over up to 8 thousand, 131 GFLOP: 200 to 210 us with the
+// join's 16 in a run of calls (245 from an idle card), 0.64 PFLOP/s, where a large product reaches 1.4: the matrix units are
+// busy 29% of the time, the vector units 42% (161 instructions a wave and tile), LDS 25%, and a wave waits 50% of its time,
+// which the second wave that the registers leave a SIMD fills half. No part took more than an eighth when it was left out. No
+// gain: the next
 // tile's scores before this one's weights, a product's operands read under the softmax before it, two buffers and one
 // barrier a stage, other wave priorities, the values' loads before the softmax;
 // 64 rows a wave spill.
@@ -860,7 +864,7 @@ __device__ __forceinline__ void attend_range(const AttendArgs& A, int b, int h, 
       load_stage<DB, NW>(A, h, t + kStage, pages, wv, lane, L);
     }
     if (!busy) continue;
-    if constexpr (WR == 8) {  // (two tiles at once: 32 trees of 61 nodes 209 us, one at a time 218; with four waves no gain)
+    if constexpr (WR == 8) {  // (two tiles at once: 32 trees of 61 nodes 210 us, one at a time 214; with four waves no gain)
 #pragma unroll
       for (int i = 0; i < kStage; i += 2) {
         const int valid[2] = {valid_of(here, t, i, tokens), valid_of(here, t, i + 1, tokens)};
@@ -965,7 +969,7 @@ __global__ void __launch_bounds__(64 * NW, waves_of(RW, 32 * DB)) hs_attend_kern
 // workgroup does four groups, those from 4 blockIdx.y on, 4 (blockIdx.y + gridDim.y), .. With W > 1 it does one group,
 // blockIdx.y, its W waves every W-th part each, joined through LDS: a wave alone reads eight parts at a time (one query's
 // call, eight heads: one token over 4096, 32 parts, 16.5 us and by four waves 14.2; over 32768, 96 parts, 32.8 and by
-// sixteen 25.6; a tree of 61 nodes, whose 33 MB of parts are the bound, 45.2 and 45.3).
+// sixteen, of whose registers 15 to 17 spill, 25.6; a tree of 61 nodes, whose 33 MB of parts are the bound, 45.2 and 45.3).
 template <bool F16, int DB, int RW, int WR, int W>
 __global__ void __launch_bounds__(W > 1 ? 64 * W : kThreads) hs_attend_join_kernel(const AttendArgs A) {
   constexpr int D = 32 * DB, kAhead = 8;
@@ -1097,7 +1101,10 @@ bool attend_geom(int B, int M, int heads, int kv, int dim, int page, int slots, 
   g->dim = dim;
   const int rows = M * (heads / kv);
   g->rw = rows > 16 ? 32 : 16;
-  // (Four groups of rows of 256 dimensions spill: 16 trees of 61 nodes 200 us, in groups of two 164; one of 45 95 and 66.)
+  // (Four groups of rows of 256 dimensions spill: 16 trees of 61 nodes 200 us, in groups of two 164; one of 45 95 and 66. Those
+  // of 160 to 224 by four and by two, 16 trees over 1024 tokens, 32 heads of 8: 61 nodes 64 and 84, 68 and 92, 91 and 109 us;
+  // 20 nodes, whose 80 rows leave four groups a third idle, 42 and 38, 48 and 43, 60 and 50. At 224 dimensions 33 registers
+  // spill, at 256 15 with 64 rows, 26 with 16 rows and up to 2 with 32.)
   g->wr = rows > 128 && dim <= 128 ? 8 : rows > 64 && dim <= 224 ? 4 : rows > 32 ? 2 : 1;
   g->tiles = (rows + g->rw * g->wr - 1) / (g->rw * g->wr);
   // Ranges for the workgroups that the device holds at once; a workgroup a query and head, and no join, where there are

@@ -25,11 +25,11 @@
 // 3.5e-9 in a slice's sum, about once in 2000).
 //
 // What bounds it. Few rows: the launches and the latencies of a row read twice (a chain of 4 tokens over 32 thousand fp32
-// 14 us in four launches; 61 nodes over 152 thousand bf16 10 in the rows and 11 in the walk). Many: the vector units in
+// 14 us in four launches; 61 nodes over 152 thousand bf16 9 in the rows and 11 in the walk). Many: the vector units in
 // the rows kernel, which are never idle, at 19 instructions a logit, ten of them fp64, all at one rate (64 chains of 8
-// tokens and their drafter, 151936 bf16: 165 million logits in 98 to 110 us, 3.3 TB/s; with 21, 106 to 125; with seventeen
-// in fp64, 123 to 140), then 10 for the walk and 22 for what a rejection leaves. 32 trees of 61 nodes by levels: 55,
-// launches of 2.5 to 7.
+// tokens and their drafter, 151936 bf16: 165 million logits in 96 to 105 us, 3.4 TB/s; with 21, 106 to 125; with seventeen
+// in fp64, 123 to 140), then 9 for the walk and 21 for what a rejection leaves. 32 trees of 61 nodes by levels: 55 to 58,
+// launches of 2.1 to 7 that wait for cur, parts, token and logit one behind the other before their row's first load.
 #include <algorithm>
 #include <cfloat>
 
@@ -758,8 +758,11 @@ size_t verify_ws_bytes(const VerifyGeom& g) {
 }
 
 // Whether a tree's rows are read level by level, those on the paths alone, in depth + 1 launches: where the rows off the
-// paths take longer than the launches. us all at once and by levels: 32 trees of 61 nodes, 7 deep, of 128256 bf16 154
-// and 55; 64 chains of 8 tokens with their drafter, where most of the rows are on the path, 165 and 196.
+// paths surely take longer than the launches, by a rate of rows and 8 us a level that are on the safe side. us all at once and
+// by levels, trees of 61 nodes, 7 deep, of 128256 bf16, paths of 2 to 3 nodes: 4 trees 35 and 42, 8 50 and 43, 13 (the rule's
+// border) 68 to 70 and 46, 32 164 and 53; greedy 8 25 and 33, 13 36 and 34, 24 (the border) 69 and 36, 32 89 and 38.
+// 64 chains of 8 tokens of 151936 with their drafter, all on the path, 102 and 167, of fixed tokens 55 and 71, greedy 29 and
+// 60. With depth M - 1, which a call that does not know better gives, no row counts as off the paths.
 static bool by_levels(const VerifyGeom& g, int depth, bool greedy) {
   const double row = (double)g.B * g.V * (g.dtype == HS_F32 ? 4 : 2);
   return !g.drafter && row * (g.M - (depth + 1)) / (greedy ? 5e6 : 2.8e6) > 8.0 * (depth + 1);
