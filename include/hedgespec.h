@@ -651,10 +651,10 @@ typedef struct hs_heads {
  *   scale       : finite. Scores times log2 e are fp32 sums and products: from 2^22 on they are told apart only as fp32
  *                 tells them apart, and those below -3.4e38 have no weight.
  *   No output may overlap an input or the workspace, nor may two rows of out share bytes.
- * Products are exact in fp32 sums. A cached token's weight is rounded once to fp16 (2^-11 of itself, or 2^-33 of the row's
- * largest weight, if that is more), a node's to 15 bits, out once. Values may have any scales and any finite size: where
- * pages' scales lie more than 16 times apart, weights are rounded relative to the largest of each 32 or 64 tokens (a query
- * whose nodes hold values of 2^100 or more may lose some of these bits).
+ * Products are exact in fp32 sums. A cached token's weight is rounded once to fp16 (2^-11 of itself, or 2^-32 of the row's
+ * largest weight, if that is more), a node's to 15 bits, out once. Values may have any scales and any finite size: those of
+ * pages with scales more than 32 times below others' are rounded relative to the largest weight of 32 tokens, which takes
+ * up to twice the time (a query whose nodes hold values of 2^100 or more may lose some of these bits).
  * workspace     : at least hs_tree_attention_workspace_size() bytes (which may be 0), 256-byte aligned; scratch only.
  * 1 <= M <= HS_MAX_POSITIONS. Deterministic.
  */

@@ -23,10 +23,12 @@
 // m follows x whatever a page's codes are, so a page whose scale an outlier set would take fp16's range from pages of finer
 // scales. While a tile whose scale is more than 2^kSpread below the largest met is added, O and its weights are held larger,
 // and also while one of scores beyond 2^22 is, whose products are rounded first (see lifted). Nodes' values have no scale: m
-// follows them as if it were 2^kNodes, so that pages down to 2^-20 are no finer ones, and their weights, which that makes
+// follows them as if it were 2^kNodes, so that pages down to 2^-21 are no finer ones, and their weights, which that makes
 // larger than fp16, are two bf16 each. That costs tiles that need none of it 3 to 6% (one query's tree 41.4 us and 42.6, 32
-// trees 198 and 207 to 210, fp16 nodes of short drafts 15.0 and 15.9, a token 13.2 and 13.6). Weights as two bf16 for all,
-// whose range is fp32's: 47.3, 249, 15.9 and 13.3.
+// trees 198 and 207 to 210, fp16 nodes of short drafts 15.0 and 15.9, a token 13.2 and 13.6) and trees whose tiles all do
+// up to twice the time (64.8, 371; a token 14.1). Weights as two bf16 for all, whose range is fp32's: 47.3, 249, 15.9 and
+// 13.3. kSpread trades what fp16 loses, 2^(kSpread - 37) of the largest weight, for pages that take the longer way: values
+// of one distribution have scales 4 times apart, and pages of 8 times the values 32; with 4 for it those made 258 us of 201.
 //
 // Split. The stages of all queries' cached tokens are cut into as many equal ranges as the device holds workgroups, so that
 // lengths that differ, and one query alone, load it alike; what a range holds of a query that others share goes to the
@@ -66,7 +68,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr float kHeadroom = 12.0f;  // weights are held as 2^12 w
 constexpr float kSlack = 3.0f;      // m follows a maximum more than this above it
 constexpr float kLowest = -FLT_MAX; // m before the first token
-constexpr float kSpread = 4.0f;     // log2 of how far a page's scale may be below others'
+constexpr float kSpread = 5.0f;     // log2 of how far a page's scale may be below others'
 constexpr float kNodes = -16.0f;    // log2 of the scale that m takes nodes' values to have
 constexpr float kHugeNodes = 24.0f; // and where some are 2^90 or more: 64 of the largest at weights of 2^(15 - 24) are fp32
 constexpr int kStage = 4;           // tiles of 32 tokens that a workgroup brings to LDS at once

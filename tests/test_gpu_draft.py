@@ -615,7 +615,7 @@ def test_attention_any_finite_value_of_bf16_nodes(M, heads):
 
 class Sharp(Draft):
     """Scores that lie far apart, where a dimension may hold nothing but values of tokens of little weight. A weight is held as
-    2^12 w in fp16, w relative to a maximum that is at most 2^4 (what scales may differ by) above the row's largest weight of
+    2^12 w in fp16, w relative to a maximum that is at most 2^4 (what scales differ by here) above the row's largest weight of
     any page: below 2^-14 fp16's steps are 2^-24, so that w is off by 2^-25 2^-12 = 2^-37 of that maximum, 2^-33 of the largest
     weight, and that is at most 1. Each of n tokens may so add 2^-33 |v| to an output."""
 
